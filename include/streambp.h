@@ -407,6 +407,72 @@ int streambp_attention_backward_static(const void *q, const void *k, const void 
                                        float *dv, int engine, void *cuda_stream);
 
 /*
+ * (No counterpart in the paper's method; what its training runs do with the gradients this library forms.)
+ * One AdamW step over many tensors, and the norm of all gradients with its clip factor.
+ *
+ * Per element, with g' = g * (grad_scale ? *grad_scale : 1), t the step number and lr, beta1, beta2, eps of cfg:
+ *     m <- beta1 m + (1 - beta1) g'          v <- beta2 v + (1 - beta2) g'^2
+ *     p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32.  `param` has param_dtype; with `master` (an fp32 copy, STREAMBP_BF16 parameters only) the step works on the
+ * copy and `param` is the copy rounded once (the old `param` is not read); without it p is the stored parameter.
+ * `grad` is fp32, as every gradient of this library is.
+ *
+ * state_dtype STREAMBP_STATE_F32: m and v are float[count].  STREAMBP_STATE_MX8: m and v are uint8[count] e4m3 codes in
+ * blocks of STREAMBP_MX8_BLOCK consecutive elements, m_scale and v_scale one byte s per block (ceil(count / 32) bytes,
+ * the last block may be shorter): code c of the block stands for e4m3(c) * 2^(s - 127).  s is the block's largest biased
+ * fp32 exponent less 7, at least 1; 255 marks a block that held an infinity or a NaN (all its values read as NaN).  What
+ * is held in `v` is the ROOT of the second moment, and a root that is not zero is held as at least 2^-9 * 2^(s - 127).
+ * The update of the parameter uses the new moments before they are rounded.  Start from zero codes and scale bytes of 1
+ * (any byte below 255 does).
+ *
+ * step: NULL (t = cfg->step >= 1), or one int64 in device memory that is read when the kernel runs (a value below 1
+ * counts as 1), so that a captured step can be replayed.  grad_scale: NULL or one float in device memory; if it is not
+ * finite the call changes nothing.  Tensors of a call must not overlap; count 0 is allowed (its pointers may be NULL).
+ * n is not limited: up to 256 tensors share a launch.  STREAMBP_E_SHAPE also for hyperparameters outside their range
+ * (lr, eps, weight_decay >= 0 and finite, 0 <= beta < 1).
+ */
+#define STREAMBP_MX8_BLOCK 32
+typedef enum { STREAMBP_STATE_F32 = 0, STREAMBP_STATE_MX8 = 1 } streambp_state_dtype;
+typedef struct {
+    void *param;
+    float *master;        /* optional */
+    const float *grad;
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;   /* STREAMBP_STATE_MX8 only */
+    int64_t count;
+    float weight_decay;
+} streambp_adamw_tensor;
+typedef struct {
+    float lr, beta1, beta2, eps;
+    int32_t param_dtype;  /* streambp_dtype */
+    int32_t state_dtype;  /* streambp_state_dtype */
+    int64_t step;
+} streambp_adamw_cfg;
+int streambp_adamw_step(const streambp_adamw_cfg *cfg, const streambp_adamw_tensor *tensors, int32_t n,
+                        const float *grad_scale, const int64_t *step, void *cuda_stream);
+
+/*
+ * *norm = sqrt(sum of g^2 over all n gradient tensors) (the squares are summed in 64 bits in a fixed order: the same
+ * gradients give the same bits), and, unless scale is NULL, *scale = min(1, max_norm / (*norm + 1e-6)), or NaN if the
+ * sum is not finite, which makes the AdamW step that reads it change nothing.  grads, counts: HOST arrays of device
+ * pointers and element counts (count 0 allowed; n = 0 gives norm 0).  norm, scale: device floats.  Two calls that may
+ * run at the same time need workspaces of their own.
+ */
+size_t streambp_grad_norm_workspace_bytes(void);
+int streambp_grad_norm(const float *const *grads, const int64_t *counts, int32_t n, float max_norm, float *norm,
+                       float *scale, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Values <-> the 8-bit form above, for starting a state from given moments, checkpoints and inspection.  keep_nonzero:
+ * positive values are held as at least the smallest code (the rule of the second moment's root).  out_dtype float or
+ * bf16 (both exact).
+ */
+int streambp_mx8_encode(const float *values, int64_t count, int32_t keep_nonzero, uint8_t *codes, uint8_t *scales,
+                        void *cuda_stream);
+int streambp_mx8_decode(const uint8_t *codes, const uint8_t *scales, int64_t count, void *out, int32_t out_dtype,
+                        void *cuda_stream);
+
+/*
  * Optional device timing by kernel class (0 = linear products, 1 = attention forward,
  * 2 = attention backward).  While enabled, each launch of those classes is bracketed by CUDA
  * events on the caller's stream.  streambp_profile_enable(1) also clears earlier records;

@@ -39,6 +39,8 @@ EXPORTS = (
     "streambp_layer_workspace_bytes_grouped", "streambp_layer_backward_grouped", "streambp_test_workspace_guard",
     "streambp_lmhead_workspace_bytes_grouped", "streambp_lmhead_ce_backward_grouped",
     "streambp_lmhead_rl_backward_grouped",
+    "streambp_adamw_step", "streambp_grad_norm_workspace_bytes", "streambp_grad_norm", "streambp_mx8_encode",
+    "streambp_mx8_decode",
 )
 
 
@@ -66,6 +68,17 @@ class GemmProblemC(C.Structure):
                 ("A", C.c_void_p * 3), ("lda", C.c_int64 * 3), ("B", C.c_void_p * 3), ("ldb", C.c_int64 * 3),
                 ("K", C.c_int64 * 3), ("C", C.c_void_p), ("ldc", C.c_int64), ("out_dtype", C.c_int32),
                 ("accumulate", C.c_int32)]
+
+
+class AdamWTensorC(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p),
+                ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("count", C.c_int64),
+                ("weight_decay", C.c_float)]
+
+
+class AdamWCfgC(C.Structure):
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
+                ("param_dtype", C.c_int32), ("state_dtype", C.c_int32), ("step", C.c_int64)]
 
 
 class ModelCfgC(C.Structure):
@@ -165,6 +178,16 @@ def lib() -> C.CDLL:
     L.streambp_test_workspace_guard.argtypes = [vp, sz, i32, vp]
     L.streambp_test_per_device_value.restype = C.c_int
     L.streambp_test_per_device_value.argtypes = [C.c_int, C.c_int]
+    L.streambp_adamw_step.restype = C.c_int
+    L.streambp_adamw_step.argtypes = [C.POINTER(AdamWCfgC), C.POINTER(AdamWTensorC), i32, vp, vp, vp]
+    L.streambp_grad_norm_workspace_bytes.restype = sz
+    L.streambp_grad_norm_workspace_bytes.argtypes = []
+    L.streambp_grad_norm.restype = C.c_int
+    L.streambp_grad_norm.argtypes = [C.POINTER(vp), C.POINTER(i64), i32, C.c_float, vp, vp, vp, sz, vp]
+    L.streambp_mx8_encode.restype = C.c_int
+    L.streambp_mx8_encode.argtypes = [vp, i64, i32, vp, vp, vp]
+    L.streambp_mx8_decode.restype = C.c_int
+    L.streambp_mx8_decode.argtypes = [vp, vp, i64, vp, i32, vp]
     _lib = L
     return L
 
@@ -199,6 +222,46 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     s = stream if stream is not None else torch.cuda.current_stream()
     return s.cuda_stream
+
+
+def _shared_device(what: str, *tensors: Optional[torch.Tensor]) -> torch.device:
+    """The CUDA device that all the tensors lie on; refuses others, and tensors that are not contiguous."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{what}: tensors must be contiguous CUDA tensors")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError(f"{what}: tensors lie on {dev} and {t.device}")
+    return dev
+
+
+class _Launch:
+    """The tensors' device made current for a call (it need not be the caller's), and the stream the call goes to: the
+    given one, which must belong to that device, or that device's current stream."""
+
+    def __init__(self, what: str, device: torch.device, stream: Optional[torch.cuda.Stream]):
+        if stream is not None and stream.device != device:
+            raise ValueError(f"{what}: the stream belongs to {stream.device}, the tensors lie on {device}")
+        self.other = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        self.device, self.stream = device, stream
+
+    def __enter__(self) -> int:
+        if self.other is not None:
+            self.other.__enter__()
+        return (self.stream if self.stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
+
+
+def _want(ok: bool, what: str, rule: str) -> None:
+    if not ok:
+        raise ValueError(f"{what}: {rule}")
 
 
 @dataclass
@@ -576,4 +639,122 @@ def lmhead_rl_backward(cfg: HeadConfig, objective: int, beta: float, clip_eps: f
         st = lib().streambp_lmhead_rl_backward_grouped(*head, wgrad_group, *tail)
     if check:
         _check(st, name)
+    return st
+
+
+# ---- AdamW ------------------------------------------------------------------------------------------------------
+MX8_BLOCK = 32
+STATE_F32, STATE_MX8 = 0, 1
+
+
+class AdamWPlan:
+    """The tensors of an AdamW step, checked once and laid out for the calls (host memory only; the tensors are kept
+    alive).  Each entry is a dict: param (fp32 or bf16), grad (fp32), m, v, optional master (fp32, bf16 parameters
+    only), optional weight_decay (0).  m and v are fp32, or uint8 codes with m_scale and v_scale (uint8, one per 32
+    elements).  All entries share the parameter's and the moments' types and one device; tensors that a step writes
+    must not overlap."""
+
+    def __init__(self, tensors: Sequence[Dict]):
+        what = "AdamWPlan"
+        _want(len(tensors) > 0, what, "needs at least one tensor")
+        self.tensors = [dict(t) for t in tensors]
+        every = [x for t in self.tensors for x in t.values() if isinstance(x, torch.Tensor)]
+        self.device = _shared_device(what, *every)
+        p0, m0 = self.tensors[0]["param"], self.tensors[0]["m"]
+        self.param_dtype = _dtype_code(p0.dtype)
+        _want(m0.dtype in (torch.float32, torch.uint8), what, "m is fp32 or uint8 codes")
+        self.state_dtype = STATE_MX8 if m0.dtype == torch.uint8 else STATE_F32
+        n = len(self.tensors)
+        self.c = (AdamWTensorC * n)()
+        self.grads, self.counts = (C.c_void_p * n)(), (C.c_int64 * n)()
+        written = []
+        for i, t in enumerate(self.tensors):
+            p, g, m, v, ma = t["param"], t["grad"], t["m"], t["v"], t.get("master")
+            ms, vs, count = t.get("m_scale"), t.get("v_scale"), p.numel()
+            _want(p.dtype == p0.dtype and m.dtype == m0.dtype and v.dtype == m0.dtype, what, "mixed types")
+            _want(g.dtype == torch.float32 and g.numel() == count, what, "grad is fp32 of the parameter's size")
+            _want(m.numel() == count and v.numel() == count, what, "m and v have the parameter's size")
+            _want(ma is None or (p.dtype == torch.bfloat16 and ma.dtype == torch.float32 and ma.numel() == count), what,
+                  "master is fp32, of the parameter's size, and goes with bf16 parameters")
+            if self.state_dtype == STATE_MX8:
+                blocks = (count + MX8_BLOCK - 1) // MX8_BLOCK
+                _want(all(s is not None and s.dtype == torch.uint8 and s.numel() == blocks for s in (ms, vs)), what,
+                      "m_scale and v_scale are uint8, one per 32 elements")
+            else:
+                _want(ms is None and vs is None, what, "scales go with 8-bit moments")
+            self.c[i] = AdamWTensorC(_ptr(p), _ptr(ma), _ptr(g), _ptr(m), _ptr(v), _ptr(ms), _ptr(vs), count,
+                                     float(t.get("weight_decay", 0.0)))
+            self.grads[i], self.counts[i] = _ptr(g), count
+            written += [(x.data_ptr(), x.data_ptr() + x.numel() * x.element_size())
+                        for x in (p, ma, m, v, ms, vs) if x is not None and x.numel()]
+        written.sort()
+        _want(all(a[1] <= b[0] for a, b in zip(written, written[1:])), what, "tensors that a step writes overlap")
+
+    def __len__(self) -> int:
+        return len(self.tensors)
+
+
+def adamw_step(plan: AdamWPlan, lr: float, beta1: float, beta2: float, eps: float, step, grad_scale=None, stream=None,
+               check: bool = True) -> int:
+    """streambp_adamw_step.  step: an int >= 1, or an int64 CUDA tensor of one value that the kernel reads;
+    grad_scale: None or an fp32 CUDA tensor of one value (see grad_norm)."""
+    on_device = isinstance(step, torch.Tensor)
+    if on_device:
+        _want(step.dtype == torch.int64 and step.numel() == 1 and step.device == plan.device, "adamw_step",
+              "step is an int or one int64 on the tensors' device")
+    if grad_scale is not None:
+        _want(grad_scale.dtype == torch.float32 and grad_scale.numel() == 1 and grad_scale.device == plan.device,
+              "adamw_step", "grad_scale is one fp32 value on the tensors' device")
+    c = AdamWCfgC(lr, beta1, beta2, eps, plan.param_dtype, plan.state_dtype, 0 if on_device else int(step))
+    with _Launch("adamw_step", plan.device, stream) as s:
+        st = lib().streambp_adamw_step(C.byref(c), plan.c, len(plan), _ptr(grad_scale), _ptr(step) if on_device else None, s)
+    if check:
+        _check(st, "streambp_adamw_step")
+    return st
+
+
+def grad_norm_workspace_bytes() -> int:
+    return int(lib().streambp_grad_norm_workspace_bytes())
+
+
+def grad_norm(plan: AdamWPlan, max_norm: float, norm: torch.Tensor, scale: Optional[torch.Tensor],
+              workspace: torch.Tensor, stream=None, check: bool = True) -> int:
+    """streambp_grad_norm over the gradients of a plan: norm and scale (or None) are fp32 CUDA tensors of one value."""
+    for t in (norm, scale):
+        _want(t is None or (t.dtype == torch.float32 and t.numel() == 1), "grad_norm", "norm and scale are one fp32 value each")
+    _want(_shared_device("grad_norm", norm, scale, workspace) == plan.device, "grad_norm", "outputs lie on another device")
+    with _Launch("grad_norm", plan.device, stream) as s:
+        st = lib().streambp_grad_norm(plan.grads, plan.counts, len(plan), max_norm, _ptr(norm), _ptr(scale),
+                                      _ptr(workspace), workspace.numel() * workspace.element_size(), s)
+    if check:
+        _check(st, "streambp_grad_norm")
+    return st
+
+
+def mx8_encode(values: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, keep_nonzero: bool = False, stream=None,
+               check: bool = True) -> int:
+    """streambp_mx8_encode: fp32 values -> uint8 codes and one scale byte per 32 of them."""
+    n = values.numel()
+    _want(values.dtype == torch.float32 and codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and
+          codes.numel() == n and scales.numel() == (n + MX8_BLOCK - 1) // MX8_BLOCK, "mx8_encode",
+          "fp32 values, uint8 codes of the same size, one uint8 scale per 32")
+    dev = _shared_device("mx8_encode", values, codes, scales)
+    with _Launch("mx8_encode", dev, stream) as s:
+        st = lib().streambp_mx8_encode(_ptr(values), n, 1 if keep_nonzero else 0, _ptr(codes), _ptr(scales), s)
+    if check:
+        _check(st, "streambp_mx8_encode")
+    return st
+
+
+def mx8_decode(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream=None, check: bool = True) -> int:
+    """streambp_mx8_decode: the values (fp32 or bf16) that the codes stand for."""
+    n = codes.numel()
+    _want(codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and out.numel() == n and
+          scales.numel() == (n + MX8_BLOCK - 1) // MX8_BLOCK, "mx8_decode",
+          "uint8 codes, one uint8 scale per 32, as many values out")
+    dev = _shared_device("mx8_decode", codes, scales, out)
+    with _Launch("mx8_decode", dev, stream) as s:
+        st = lib().streambp_mx8_decode(_ptr(codes), _ptr(scales), n, _ptr(out), _dtype_code(out.dtype), s)
+    if check:
+        _check(st, "streambp_mx8_decode")
     return st

@@ -1,0 +1,534 @@
+// What applies the gradients of the streamed backward: the norm of all gradients with its clip factor, and one AdamW
+// step over many tensors per launch, with moments in 32 bits or in 8.
+//
+// Both kernels read a list of tensors from their launch parameters (no table in device memory, nothing to allocate or
+// to copy, so a captured graph replays them as they are) and walk it in pieces of kPiece elements: piece -> tensor by a
+// binary search over the running piece counts, the same for the whole block.  Every element is read once and written
+// once; what bounds them is HBM.
+//
+// Moments in 8 bits: blocks of 32 consecutive elements of a tensor share a power of two 2^(s - 127) (one byte s) and
+// hold e4m3 codes.  s = (biased exponent of the block's largest magnitude) - 7, at least 1: the largest code is then
+// below 256 and never saturates, and decoding is exact in fp32 and in bf16.  The second moment is held as its ROOT,
+// which halves the exponent range it needs (17 octaves from the smallest code to the largest are 34 of v), and a root
+// that is not zero is held as at least the smallest code 2^-9: a second moment rounded to zero beside a first moment
+// that is not would make the next step's quotient jump by 1 / sqrt(1 - beta2).
+#include <cuda_fp8.h>
+
+#include <cmath>
+#include <cstring>
+
+#include "common.cuh"
+#include "sm100.cuh"
+
+namespace sbp {
+namespace {
+
+constexpr int kThreads = 256, kGroup = 4;                 // a thread's unit: 4 consecutive elements (16 bytes of fp32)
+constexpr int kUnroll = 4;                                // units per thread and piece, all loaded before the first is used
+constexpr int kPiece = kThreads * kGroup * kUnroll;       // 4096 elements; a multiple of the 32 of a block of codes
+constexpr int kBlock = STREAMBP_MX8_BLOCK;
+static_assert(kPiece % kBlock == 0 && kBlock == 8 * kGroup, "eight neighbouring threads hold a block of codes");
+
+template <int CAP>
+struct StepParams {
+    streambp_adamw_tensor t[CAP];
+    int piece_begin[CAP + 1];        // pieces of tensor i: piece_begin[i] .. piece_begin[i + 1] - 1
+    int n;
+    float lr, beta1, beta2, eps;
+    float step_size, inv_root_bc2;   // lr / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
+    const float *grad_scale;         // optional
+    const int64_t *step;             // optional: the step number is read from the device
+};
+
+// the tensor that piece `b` belongs to: largest i with piece_begin[i] <= b
+__device__ __forceinline__ int find_tensor(const int *begin, int n, int b) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (begin[mid] <= b) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// Four elements from `p`, or the first `valid` of them and zeros.
+__device__ __forceinline__ void load4(const float *p, int valid, float (&v)[4]) {
+    if (valid >= 4) {
+        const float4 t = *reinterpret_cast<const float4 *>(p);
+        v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = e < valid ? p[e] : 0.f;
+    }
+}
+__device__ __forceinline__ void load4(const bf16 *p, int valid, float (&v)[4]) {
+    if (valid >= 4) {
+        const uint2 t = *reinterpret_cast<const uint2 *>(p);
+        v[0] = __uint_as_float(t.x << 16); v[1] = __uint_as_float(t.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(t.y << 16); v[3] = __uint_as_float(t.y & 0xFFFF0000u);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = e < valid ? __bfloat162float(p[e]) : 0.f;
+    }
+}
+__device__ __forceinline__ void store4(float *p, int valid, const float (&v)[4]) {
+    if (valid >= 4) {
+        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (e < valid) p[e] = v[e];
+    }
+}
+__device__ __forceinline__ void store4(bf16 *p, int valid, const float (&v)[4]) {
+    if (valid >= 4) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+        *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (e < valid) p[e] = __float2bfloat16_rn(v[e]);
+    }
+}
+__device__ __forceinline__ uint32_t load_codes(const uint8_t *p, int valid) {
+    if (valid >= 4) return *reinterpret_cast<const uint32_t *>(p);
+    uint32_t w = 0;
+    for (int e = 0; e < valid; e++) w |= (uint32_t)p[e] << (8 * e);
+    return w;
+}
+__device__ __forceinline__ void store_codes(uint8_t *p, int valid, uint32_t w) {
+    if (valid >= 4) {
+        *reinterpret_cast<uint32_t *>(p) = w;
+    } else {
+        for (int e = 0; e < valid; e++) p[e] = (uint8_t)(w >> (8 * e));
+    }
+}
+
+// 2^(s - 127) and its inverse; s = 255 stands for NaN (a block that held an infinity or a NaN)
+__device__ __forceinline__ float scale_value(uint32_t s) { return s == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(s << 23); }
+__device__ __forceinline__ void decode4(uint32_t codes, float scale, float (&v)[4]) {
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> (16 * e)), __NV_E4M3);
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+        v[2 * e] = f.x * scale;
+        v[2 * e + 1] = f.y * scale;
+    }
+}
+// biased exponent of the largest magnitude of a value, as the block scale sees it
+__device__ __forceinline__ uint32_t exponent_of(const float (&v)[4]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 4; e++) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
+    return m >> 23;
+}
+__device__ __forceinline__ uint32_t scale_byte(uint32_t exponent) {
+    return exponent == 255u ? 255u : (exponent > 8u ? exponent - 7u : 1u);
+}
+template <bool KEEP>
+__device__ __forceinline__ uint32_t encode4(const float (&v)[4], uint32_t s) {
+    const float inv = s == 255u ? 0.f : __uint_as_float((254u - s) << 23);
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+        float a = v[2 * e] * inv, b = v[2 * e + 1] * inv;
+        if (KEEP) {
+            if (v[2 * e] > 0.f) a = fmaxf(a, 0.001953125f);
+            if (v[2 * e + 1] > 0.f) b = fmaxf(b, 0.001953125f);
+        }
+        w |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) << (16 * e);
+    }
+    return w;
+}
+// the largest of two 16-bit fields over the eight neighbouring threads that hold a block
+__device__ __forceinline__ uint32_t block_max2(uint32_t v) {
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) v = __vmaxu2(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+struct Rates {
+    float gs, lr, b1, b2, eps, step_size, inv_root_bc2;
+};
+
+// one element: new moments and parameter (sums in fp32; the quotient to 2 ulp, far below the rounding of the result)
+__device__ __forceinline__ void update(const Rates &r, float g, float decay, float &m, float &v, float &u, float &p) {
+    g *= r.gs;
+    m = fmaf(r.b1, m, (1.f - r.b1) * g);
+    v = fmaf(r.b2, v, (1.f - r.b2) * g * g);
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(u) : "f"(v));
+    p = fmaf(p, decay, -r.step_size * __fdividef(m, fmaf(u, r.inv_root_bc2, r.eps)));
+}
+
+// P: parameter type, MX8: moments in 8 bits.  With a master copy the parameter is the rounded master and is not read.
+template <typename P, bool MX8, int CAP>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ StepParams<CAP> a) {
+    pdl_enter();
+    __shared__ float s_rate[2];
+    Rates r{a.grad_scale ? *a.grad_scale : 1.f, a.lr, a.beta1, a.beta2, a.eps, a.step_size, a.inv_root_bc2};
+    if (!isfinite(r.gs)) return;              // the gradients were not finite: the step is left out, the same for every block
+    if (a.step) {
+        if (threadIdx.x == 0) {
+            const long long t = *a.step;
+            const double n = t < 1 ? 1.0 : (double)t;
+            s_rate[0] = (float)((double)a.lr / (1.0 - pow((double)a.beta1, n)));
+            s_rate[1] = (float)(1.0 / sqrt(1.0 - pow((double)a.beta2, n)));
+        }
+        __syncthreads();
+        r.step_size = s_rate[0];
+        r.inv_root_bc2 = s_rate[1];
+    }
+    const int pieces = a.piece_begin[a.n];
+    for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        const int i = find_tensor(a.piece_begin, a.n, piece);
+        const streambp_adamw_tensor &t = a.t[i];
+        const long long base = (long long)(piece - a.piece_begin[i]) * kPiece, left = t.count - base;
+        P *param = static_cast<P *>(t.param) + base;
+        float *master = t.master ? t.master + base : nullptr;
+        const float *grad = t.grad + base;
+        const float decay = 1.f - r.lr * t.weight_decay;
+        float g[kUnroll][4], p[kUnroll][4], m[kUnroll][4], v[kUnroll][4];
+        int valid[kUnroll], off[kUnroll];
+#pragma unroll
+        for (int k = 0; k < kUnroll; k++) {
+            off[k] = (k * kThreads + (int)threadIdx.x) * kGroup;
+            const long long rest = left - off[k];
+            valid[k] = rest >= 4 ? 4 : (rest > 0 ? (int)rest : 0);
+        }
+        if constexpr (MX8) {
+            uint8_t *mc = static_cast<uint8_t *>(t.m) + base, *vc = static_cast<uint8_t *>(t.v) + base;
+            uint8_t *ms = t.m_scale + base / kBlock, *vs = t.v_scale + base / kBlock;
+            uint32_t cm[kUnroll], cv[kUnroll], sm[kUnroll], sv[kUnroll];
+#pragma unroll
+            for (int k = 0; k < kUnroll; k++) {
+                load4(grad + off[k], valid[k], g[k]);
+                if (master) load4(master + off[k], valid[k], p[k]);
+                else load4(param + off[k], valid[k], p[k]);
+                cm[k] = load_codes(mc + off[k], valid[k]);
+                cv[k] = load_codes(vc + off[k], valid[k]);
+                sm[k] = valid[k] > 0 ? ms[off[k] / kBlock] : 1u;
+                sv[k] = valid[k] > 0 ? vs[off[k] / kBlock] : 1u;
+            }
+#pragma unroll
+            for (int k = 0; k < kUnroll; k++) {
+                float u[4];
+                decode4(cm[k], scale_value(sm[k]), m[k]);
+                decode4(cv[k], scale_value(sv[k]), u);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    float vv = u[e] * u[e];
+                    update(r, g[k][e], decay, m[k][e], vv, u[e], p[k][e]);
+                    if (e >= valid[k]) m[k][e] = u[e] = 0.f;
+                }
+                const uint32_t big = block_max2(exponent_of(m[k]) | (exponent_of(u) << 16));
+                const uint32_t nm = scale_byte(big & 0xffffu), nv = scale_byte(big >> 16);
+                store_codes(mc + off[k], valid[k], encode4<false>(m[k], nm));
+                store_codes(vc + off[k], valid[k], encode4<true>(u, nv));
+                if (valid[k] > 0 && (threadIdx.x & 7) == 0) {
+                    ms[off[k] / kBlock] = (uint8_t)nm;
+                    vs[off[k] / kBlock] = (uint8_t)nv;
+                }
+                if (master) store4(master + off[k], valid[k], p[k]);
+                store4(param + off[k], valid[k], p[k]);
+            }
+        } else {
+            float *mp = static_cast<float *>(t.m) + base, *vp = static_cast<float *>(t.v) + base;
+#pragma unroll
+            for (int k = 0; k < kUnroll; k++) {
+                load4(grad + off[k], valid[k], g[k]);
+                if (master) load4(master + off[k], valid[k], p[k]);
+                else load4(param + off[k], valid[k], p[k]);
+                load4(mp + off[k], valid[k], m[k]);
+                load4(vp + off[k], valid[k], v[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < kUnroll; k++) {
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    float u;
+                    update(r, g[k][e], decay, m[k][e], v[k][e], u, p[k][e]);
+                }
+                store4(mp + off[k], valid[k], m[k]);
+                store4(vp + off[k], valid[k], v[k]);
+                if (master) store4(master + off[k], valid[k], p[k]);
+                store4(param + off[k], valid[k], p[k]);
+            }
+        }
+    }
+}
+
+// ---- norm of all gradients -----------------------------------------------------------------------------------
+// Block b sums the squares of its pieces in 64 bits (squares of fp32 values neither overflow nor vanish there, and the
+// conversions and products are far from what the 1.6e12 elements a second of the read need of the fp64 units) into
+// partial[b]; one block then adds the partials in their order.  No atomics: the same gradients give the same bits.
+constexpr int kNormCap = 512;
+struct NormParams {
+    const float *grad[kNormCap];
+    long long count[kNormCap];
+    int piece_begin[kNormCap + 1];
+    int n;
+    int first;                       // 0: add to what an earlier launch of the same call left in the partials
+    double *partial;
+};
+constexpr int kNormUnroll = 8, kNormPiece = kThreads * kGroup * kNormUnroll;
+
+__device__ __forceinline__ double block_sum_f64(double v, double *red) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double t = 0.0;
+    if (threadIdx.x < 32) {
+        t = threadIdx.x < (blockDim.x >> 5) ? red[threadIdx.x] : 0.0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    }
+    return t;                        // complete in warp 0
+}
+
+__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_constant__ NormParams a) {
+    pdl_enter();
+    __shared__ double red[32];
+    double sum = 0.0;
+    const int pieces = a.piece_begin[a.n];
+    for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        const int i = find_tensor(a.piece_begin, a.n, piece);
+        const long long base = (long long)(piece - a.piece_begin[i]) * kNormPiece, left = a.count[i] - base;
+        const float *g = a.grad[i] + base;
+        float x[kNormUnroll][4];
+#pragma unroll
+        for (int k = 0; k < kNormUnroll; k++) {
+            const int off = (k * kThreads + (int)threadIdx.x) * kGroup;
+            const long long rest = left - off;
+            load4(g + off, rest >= 4 ? 4 : (rest > 0 ? (int)rest : 0), x[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kNormUnroll; k++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum = fma((double)x[k][e], (double)x[k][e], sum);
+    }
+    const double s = block_sum_f64(sum, red);
+    if (threadIdx.x == 0) a.partial[blockIdx.x] = a.first ? s : a.partial[blockIdx.x] + s;
+}
+
+__global__ void __launch_bounds__(1024) grad_norm_finish_kernel(const double *partial, int n, float max_norm, float *norm,
+                                                                float *scale) {
+    pdl_enter();
+    __shared__ double red[32];
+    double v = 0.0;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) v += partial[i];
+    const double s = sqrt(block_sum_f64(v, red));
+    if (threadIdx.x == 0) {
+        *norm = (float)s;
+        if (scale) *scale = isfinite(s) ? (float)fmin(1.0, (double)max_norm / (s + 1e-6)) : __uint_as_float(0x7fc00000u);
+    }
+}
+
+// ---- moments in 8 bits <-> values -----------------------------------------------------------------------------
+template <bool KEEP>
+__global__ void __launch_bounds__(kThreads) mx8_encode_kernel(const float *x, long long count, uint8_t *codes, uint8_t *scale) {
+    pdl_enter();
+    const long long step = (long long)gridDim.x * kThreads * kGroup;
+    // every thread of a warp runs the same number of turns: the block maximum is exchanged between neighbours
+    for (long long base = (long long)blockIdx.x * kThreads * kGroup; base < count; base += step) {
+        const long long at = base + (long long)threadIdx.x * kGroup, rest = count - at;
+        const int valid = rest >= 4 ? 4 : (rest > 0 ? (int)rest : 0);
+        float v[4];
+        load4(x + at, valid, v);
+        const uint32_t s = scale_byte(block_max2(exponent_of(v)));
+        store_codes(codes + at, valid, encode4<KEEP>(v, s));
+        if (valid > 0 && (threadIdx.x & 7) == 0) scale[at / kBlock] = (uint8_t)s;
+    }
+}
+template <typename T>
+__global__ void __launch_bounds__(kThreads) mx8_decode_kernel(const uint8_t *codes, const uint8_t *scale, long long count, T *out) {
+    pdl_enter();
+    const long long step = (long long)gridDim.x * kThreads * kGroup;
+    for (long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) * kGroup; at < count; at += kUnroll * step) {
+        uint32_t w[kUnroll], s[kUnroll];
+        int valid[kUnroll];
+#pragma unroll
+        for (int k = 0; k < kUnroll; k++) {
+            const long long o = at + k * step, rest = count - o;
+            valid[k] = rest >= 4 ? 4 : (rest > 0 ? (int)rest : 0);
+            if (valid[k] > 0) {
+                w[k] = load_codes(codes + o, valid[k]);
+                s[k] = scale[o / kBlock];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kUnroll; k++) {
+            if (valid[k] == 0) continue;
+            float v[4];
+            decode4(w[k], scale_value(s[k]), v);
+            store4(out + at + k * step, valid[k], v);
+        }
+    }
+}
+
+bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int begin_call() {
+    call_state().cuda_error = 0;
+    call_state().launches = 0;
+    return STREAMBP_OK;
+}
+
+int grid_for(int64_t pieces, int per_sm) {
+    const int64_t most = (int64_t)sm_count() * per_sm;
+    return (int)(pieces < most ? pieces : most);
+}
+
+// Launches over `n` tensors of up to CAP at a time.  Two capacities: launch parameters are copied by the driver for every
+// launch, and the usual layer of a dozen tensors should not pay for two hundred.
+template <typename P, bool MX8, int CAP>
+int launch_adamw(const streambp_adamw_cfg &c, const streambp_adamw_tensor *tensors, int n, const float *grad_scale,
+                 const int64_t *step, float step_size, float inv_root_bc2, cudaStream_t st) {
+    StepParams<CAP> a;
+    int i = 0;
+    while (i < n) {
+        a.n = 0;
+        int64_t pieces = 0;
+        for (; i < n && a.n < CAP; i++) {
+            if (tensors[i].count == 0) continue;
+            const int64_t more = (tensors[i].count + kPiece - 1) / kPiece;
+            if (pieces + more > 0x40000000) break;
+            a.t[a.n] = tensors[i];
+            a.piece_begin[a.n++] = (int)pieces;
+            pieces += more;
+        }
+        if (a.n == 0) break;
+        a.piece_begin[a.n] = (int)pieces;
+        a.lr = c.lr; a.beta1 = c.beta1; a.beta2 = c.beta2; a.eps = c.eps;
+        a.step_size = step_size;
+        a.inv_root_bc2 = inv_root_bc2;
+        a.grad_scale = grad_scale;
+        a.step = step;
+        SBP_LAUNCH((adamw_kernel<P, MX8, CAP>), grid_for(pieces, 8), kThreads, 0, st, a);
+    }
+    return STREAMBP_OK;
+}
+template <typename P, bool MX8>
+int launch_adamw_any(const streambp_adamw_cfg &c, const streambp_adamw_tensor *tensors, int n, const float *grad_scale,
+                     const int64_t *step, float step_size, float inv_root_bc2, cudaStream_t st) {
+    if (n <= 32) return launch_adamw<P, MX8, 32>(c, tensors, n, grad_scale, step, step_size, inv_root_bc2, st);
+    return launch_adamw<P, MX8, 256>(c, tensors, n, grad_scale, step, step_size, inv_root_bc2, st);
+}
+
+}  // namespace
+}  // namespace sbp
+
+using namespace sbp;
+
+extern "C" {
+
+int streambp_adamw_step(const streambp_adamw_cfg *cfg, const streambp_adamw_tensor *tensors, int32_t n,
+                        const float *grad_scale, const int64_t *step, void *cuda_stream) {
+    if (!cfg || (n > 0 && !tensors)) return STREAMBP_E_NULL;
+    if (n < 0) return STREAMBP_E_SHAPE;
+    if (cfg->param_dtype != STREAMBP_F32 && cfg->param_dtype != STREAMBP_BF16) return STREAMBP_E_DTYPE;
+    if (cfg->state_dtype != STREAMBP_STATE_F32 && cfg->state_dtype != STREAMBP_STATE_MX8) return STREAMBP_E_DTYPE;
+    if (!(cfg->lr >= 0.f) || !(cfg->beta1 >= 0.f && cfg->beta1 < 1.f) || !(cfg->beta2 >= 0.f && cfg->beta2 < 1.f) ||
+        !(cfg->eps >= 0.f) || std::isinf(cfg->lr) || std::isinf(cfg->eps) || (!step && cfg->step < 1))
+        return STREAMBP_E_SHAPE;
+    if ((grad_scale && (reinterpret_cast<uintptr_t>(grad_scale) & 3u)) || (step && (reinterpret_cast<uintptr_t>(step) & 7u)))
+        return STREAMBP_E_ALIGN;
+    const bool mx8 = cfg->state_dtype == STREAMBP_STATE_MX8;
+    for (int i = 0; i < n; i++) {
+        const streambp_adamw_tensor &t = tensors[i];
+        if (t.count < 0 || t.count > (1ll << 40) || !(t.weight_decay >= 0.f) || std::isinf(t.weight_decay)) return STREAMBP_E_SHAPE;
+        if (t.count == 0) continue;
+        if (!t.param || !t.grad || !t.m || !t.v || (mx8 && (!t.m_scale || !t.v_scale))) return STREAMBP_E_NULL;
+        if (!al16(t.param) || !al16(t.master) || !al16(t.grad) || !al16(t.m) || !al16(t.v)) return STREAMBP_E_ALIGN;
+        if (t.master && cfg->param_dtype != STREAMBP_BF16) return STREAMBP_E_DTYPE;
+    }
+    begin_call();
+    const double t = step ? 1.0 : (double)cfg->step;
+    const float step_size = (float)((double)cfg->lr / (1.0 - std::pow((double)cfg->beta1, t)));
+    const float inv_root_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow((double)cfg->beta2, t)));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    NvtxRange range("streambp_adamw_step");
+    if (cfg->param_dtype == STREAMBP_F32)
+        return mx8 ? launch_adamw_any<float, true>(*cfg, tensors, n, grad_scale, step, step_size, inv_root_bc2, st)
+                   : launch_adamw_any<float, false>(*cfg, tensors, n, grad_scale, step, step_size, inv_root_bc2, st);
+    return mx8 ? launch_adamw_any<bf16, true>(*cfg, tensors, n, grad_scale, step, step_size, inv_root_bc2, st)
+               : launch_adamw_any<bf16, false>(*cfg, tensors, n, grad_scale, step, step_size, inv_root_bc2, st);
+}
+
+size_t streambp_grad_norm_workspace_bytes(void) { return kHeaderBytes + sizeof(double) * 4096; }
+
+int streambp_grad_norm(const float *const *grads, const int64_t *counts, int32_t n, float max_norm, float *norm,
+                       float *scale, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!norm || !workspace || (n > 0 && (!grads || !counts))) return STREAMBP_E_NULL;
+    if (n < 0 || (scale && !(max_norm > 0.f))) return STREAMBP_E_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) || (reinterpret_cast<uintptr_t>(norm) & 3u) ||
+        (reinterpret_cast<uintptr_t>(scale) & 3u))
+        return STREAMBP_E_ALIGN;
+    for (int i = 0; i < n; i++) {
+        if (counts[i] < 0 || counts[i] > (1ll << 40)) return STREAMBP_E_SHAPE;
+        if (counts[i] > 0 && !grads[i]) return STREAMBP_E_NULL;
+        if (counts[i] > 0 && !al16(grads[i])) return STREAMBP_E_ALIGN;
+    }
+    if (workspace_bytes < streambp_grad_norm_workspace_bytes()) return STREAMBP_E_WORKSPACE;
+    begin_call();
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    NvtxRange range("streambp_grad_norm");
+    NormParams a;
+    a.partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + kHeaderBytes);
+    int most = sm_count() * 4;                      // blocks of every launch of the call: they share the partials
+    if (most > 4096) most = 4096;
+    int used = 0, i = 0;
+    while (i < n) {
+        a.n = 0;
+        int64_t pieces = 0;
+        for (; i < n && a.n < kNormCap; i++) {
+            if (counts[i] == 0) continue;
+            const int64_t more = (counts[i] + kNormPiece - 1) / kNormPiece;
+            if (pieces + more > 0x40000000) break;
+            a.grad[a.n] = grads[i];
+            a.count[a.n] = counts[i];
+            a.piece_begin[a.n++] = (int)pieces;
+            pieces += more;
+        }
+        if (a.n == 0) break;
+        a.piece_begin[a.n] = (int)pieces;
+        a.first = used == 0;
+        // the first launch of a call that needs more than one sets every partial, the others add to them
+        const bool one = a.first && i == n;
+        const int grid = one && pieces < most ? (int)pieces : most;
+        used = grid;
+        SBP_LAUNCH(grad_norm_kernel, grid, kThreads, 0, st, a);
+    }
+    SBP_LAUNCH(grad_norm_finish_kernel, 1, 1024, 0, st, a.partial, used, max_norm, norm, scale);
+    return STREAMBP_OK;
+}
+
+int streambp_mx8_encode(const float *values, int64_t count, int32_t keep_nonzero, uint8_t *codes, uint8_t *scales,
+                        void *cuda_stream) {
+    if (count < 0 || count > (1ll << 40)) return STREAMBP_E_SHAPE;
+    if (count == 0) return STREAMBP_OK;
+    if (!values || !codes || !scales) return STREAMBP_E_NULL;
+    if (!al16(values) || !al16(codes)) return STREAMBP_E_ALIGN;
+    begin_call();
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int grid = grid_for((count + kThreads * kGroup - 1) / (kThreads * kGroup), 8);
+    if (keep_nonzero) SBP_LAUNCH(mx8_encode_kernel<true>, grid, kThreads, 0, st, values, (long long)count, codes, scales);
+    else SBP_LAUNCH(mx8_encode_kernel<false>, grid, kThreads, 0, st, values, (long long)count, codes, scales);
+    return STREAMBP_OK;
+}
+
+int streambp_mx8_decode(const uint8_t *codes, const uint8_t *scales, int64_t count, void *out, int32_t out_dtype,
+                        void *cuda_stream) {
+    if (count < 0 || count > (1ll << 40)) return STREAMBP_E_SHAPE;
+    if (out_dtype != STREAMBP_F32 && out_dtype != STREAMBP_BF16) return STREAMBP_E_DTYPE;
+    if (count == 0) return STREAMBP_OK;
+    if (!codes || !scales || !out) return STREAMBP_E_NULL;
+    if (!al16(codes) || !al16(out)) return STREAMBP_E_ALIGN;
+    begin_call();
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int grid = grid_for((count + kPiece - 1) / kPiece, 8);
+    if (out_dtype == STREAMBP_F32) SBP_LAUNCH(mx8_decode_kernel<float>, grid, kThreads, 0, st, codes, scales, (long long)count, (float *)out);
+    else SBP_LAUNCH(mx8_decode_kernel<bf16>, grid, kThreads, 0, st, codes, scales, (long long)count, (bf16 *)out);
+    return STREAMBP_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,77 @@
+"""Host-side refusals of the optimizer entry points (no GPU: arguments are checked before any CUDA call)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2506_03077_b200 import binding as B
+from paper_2506_03077_b200 import build as build_mod
+
+P = 0x10000     # an aligned address that is never read: every call here is refused on the host
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build_mod.build()
+    return B.lib()
+
+
+def adamw(lib, tensor=None, n=1, grad_scale=None, device_step=None, **cfg):
+    c = dict(lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, param_dtype=B.STREAMBP_BF16, state_dtype=B.STATE_F32, step=1)
+    c.update(cfg)
+    t = dict(param=P, master=None, grad=P, m=P, v=P, m_scale=None, v_scale=None, count=64, weight_decay=0.0)
+    t.update(tensor or {})
+    cc, tt = B.AdamWCfgC(**c), B.AdamWTensorC(**t)
+    return lib.streambp_adamw_step(C.byref(cc), C.byref(tt), n, grad_scale, device_step, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(param_dtype=7), B.E_DTYPE), (dict(state_dtype=2), B.E_DTYPE), (dict(lr=-1.0), B.E_SHAPE),
+    (dict(lr=float("nan")), B.E_SHAPE), (dict(lr=float("inf")), B.E_SHAPE), (dict(beta1=1.0), B.E_SHAPE),
+    (dict(beta2=-0.1), B.E_SHAPE), (dict(beta2=float("nan")), B.E_SHAPE), (dict(eps=-1e-8), B.E_SHAPE),
+    (dict(step=0), B.E_SHAPE), (dict(n=-1), B.E_SHAPE), (dict(grad_scale=P + 2), B.E_ALIGN),
+    (dict(step=0, grad_scale=P + 1), B.E_SHAPE), (dict(step=0, device_step=P + 4), B.E_ALIGN),
+    (dict(tensor=dict(param=None)), B.E_NULL), (dict(tensor=dict(grad=None)), B.E_NULL), (dict(tensor=dict(m=None)), B.E_NULL),
+    (dict(tensor=dict(v=None)), B.E_NULL), (dict(tensor=dict(param=P + 8)), B.E_ALIGN), (dict(tensor=dict(grad=P + 4)), B.E_ALIGN),
+    (dict(tensor=dict(m=P + 4)), B.E_ALIGN), (dict(tensor=dict(v=P + 4)), B.E_ALIGN), (dict(tensor=dict(master=P + 4)), B.E_ALIGN),
+    (dict(tensor=dict(count=-1)), B.E_SHAPE), (dict(tensor=dict(weight_decay=-0.1)), B.E_SHAPE),
+    (dict(tensor=dict(weight_decay=float("nan"))), B.E_SHAPE),
+    (dict(param_dtype=B.STREAMBP_F32, tensor=dict(master=P)), B.E_DTYPE),
+    (dict(state_dtype=B.STATE_MX8), B.E_NULL), (dict(state_dtype=B.STATE_MX8, tensor=dict(m_scale=P)), B.E_NULL),
+])
+def test_adamw_refusals(lib, kw, status):
+    assert adamw(lib, **kw) == status
+
+
+def test_adamw_of_nothing(lib):
+    assert adamw(lib, n=0) == B.OK
+    assert adamw(lib, tensor=dict(count=0, param=None, grad=None, m=None, v=None)) == B.OK
+    assert lib.streambp_adamw_step(None, None, 0, None, None, None) == B.E_NULL
+
+
+def test_grad_norm_refusals(lib):
+    need = lib.streambp_grad_norm_workspace_bytes()
+    def call(grad=P, count=8, n=1, most=1.0, norm=P, scale=P, ws=P, size=need):
+        return lib.streambp_grad_norm((C.c_void_p * 1)(grad), (C.c_int64 * 1)(count), n, most, norm, scale, ws, size, None)
+    assert call(norm=None) == B.E_NULL and call(ws=None) == B.E_NULL and call(grad=None) == B.E_NULL
+    assert call(n=-1) == B.E_SHAPE and call(count=-1) == B.E_SHAPE
+    assert call(most=0.0) == B.E_SHAPE and call(most=-1.0) == B.E_SHAPE and call(most=float("nan")) == B.E_SHAPE
+    assert call(ws=P + 128) == B.E_ALIGN and call(norm=P + 2) == B.E_ALIGN and call(scale=P + 1) == B.E_ALIGN
+    assert call(grad=P + 4) == B.E_ALIGN and call(size=need - 1) == B.E_WORKSPACE
+
+
+def test_mx8_refusals(lib):
+    assert lib.streambp_mx8_encode(P, -1, 0, P, P, None) == B.E_SHAPE and lib.streambp_mx8_decode(P, P, -1, P, 0, None) == B.E_SHAPE
+    assert lib.streambp_mx8_encode(None, 8, 0, P, P, None) == B.E_NULL and lib.streambp_mx8_encode(P, 8, 0, P, None, None) == B.E_NULL
+    assert lib.streambp_mx8_encode(P + 4, 8, 0, P, P, None) == B.E_ALIGN and lib.streambp_mx8_encode(P, 8, 0, P + 4, P, None) == B.E_ALIGN
+    assert lib.streambp_mx8_decode(P, P, 8, None, 0, None) == B.E_NULL and lib.streambp_mx8_decode(P, P, 8, P, 5, None) == B.E_DTYPE
+    assert lib.streambp_mx8_decode(P, P, 8, P + 2, 1, None) == B.E_ALIGN and lib.streambp_mx8_decode(P + 1, P, 8, P, 1, None) == B.E_ALIGN
+    assert lib.streambp_mx8_encode(None, 0, 0, None, None, None) == B.OK and lib.streambp_mx8_decode(None, None, 0, None, 0, None) == B.OK
+
+
+def test_plan_refuses_host_tensors():
+    t = {k: torch.zeros(8) for k in ("param", "grad", "m", "v")}
+    with pytest.raises(ValueError):
+        B.AdamWPlan([t])
+    with pytest.raises(ValueError):
+        B.AdamWPlan([])
