@@ -252,7 +252,9 @@ class _Launch:
     def __enter__(self) -> int:
         if self.other is not None:
             self.other.__enter__()
-        return (self.stream if self.stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
+        if self.stream is not None:
+            return self.stream.cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self.device.index)      # current_stream() without building an object
 
     def __exit__(self, *exc):
         if self.other is not None:
@@ -658,37 +660,44 @@ class AdamWPlan:
         what = "AdamWPlan"
         _want(len(tensors) > 0, what, "needs at least one tensor")
         self.tensors = [dict(t) for t in tensors]
-        every = [x for t in self.tensors for x in t.values() if isinstance(x, torch.Tensor)]
-        self.device = _shared_device(what, *every)
         p0, m0 = self.tensors[0]["param"], self.tensors[0]["m"]
-        self.param_dtype = _dtype_code(p0.dtype)
-        _want(m0.dtype in (torch.float32, torch.uint8), what, "m is fp32 or uint8 codes")
-        self.state_dtype = STATE_MX8 if m0.dtype == torch.uint8 else STATE_F32
-        n = len(self.tensors)
+        self.device = _shared_device(what, p0)
+        self.param_dtype, index, f32 = _dtype_code(p0.dtype), p0.get_device(), torch.float32
+        _want(m0.dtype in (f32, torch.uint8), what, "m is fp32 or uint8 codes")
+        mx8 = m0.dtype == torch.uint8
+        self.state_dtype = STATE_MX8 if mx8 else STATE_F32
+        n, size_p, size_m = len(self.tensors), p0.element_size(), m0.element_size()
         self.c = (AdamWTensorC * n)()
         self.grads, self.counts = (C.c_void_p * n)(), (C.c_int64 * n)()
         written = []
         for i, t in enumerate(self.tensors):
-            p, g, m, v, ma = t["param"], t["grad"], t["m"], t["v"], t.get("master")
-            ms, vs, count = t.get("m_scale"), t.get("v_scale"), p.numel()
-            _want(p.dtype == p0.dtype and m.dtype == m0.dtype and v.dtype == m0.dtype, what, "mixed types")
-            _want(g.dtype == torch.float32 and g.numel() == count, what, "grad is fp32 of the parameter's size")
-            _want(m.numel() == count and v.numel() == count, what, "m and v have the parameter's size")
-            _want(ma is None or (p.dtype == torch.bfloat16 and ma.dtype == torch.float32 and ma.numel() == count), what,
-                  "master is fp32, of the parameter's size, and goes with bf16 parameters")
-            if self.state_dtype == STATE_MX8:
+            p, g, m, v, ma, ms, vs = (t.get(k) for k in ("param", "grad", "m", "v", "master", "m_scale", "v_scale"))
+            count, c = p.numel(), self.c[i]
+            for x in (p, g, m, v) if ma is None else (p, g, m, v, ma):
+                if x.get_device() != index or not x.is_contiguous() or x.numel() != count:
+                    raise ValueError(f"{what}: tensors of an entry are contiguous, of one size and on one CUDA device")
+            if p.dtype != p0.dtype or m.dtype != m0.dtype or v.dtype != m0.dtype or g.dtype != f32:
+                raise ValueError(f"{what}: grad is fp32; parameters share a type, moments share a type")
+            if ma is not None:
+                _want(p.dtype == torch.bfloat16 and ma.dtype == f32, what, "master is fp32 and goes with bf16 parameters")
+                c.master = a = ma.data_ptr()
+                written.append((a, a + 4 * count))
+            if mx8:
                 blocks = (count + MX8_BLOCK - 1) // MX8_BLOCK
-                _want(all(s is not None and s.dtype == torch.uint8 and s.numel() == blocks for s in (ms, vs)), what,
-                      "m_scale and v_scale are uint8, one per 32 elements")
-            else:
-                _want(ms is None and vs is None, what, "scales go with 8-bit moments")
-            self.c[i] = AdamWTensorC(_ptr(p), _ptr(ma), _ptr(g), _ptr(m), _ptr(v), _ptr(ms), _ptr(vs), count,
-                                     float(t.get("weight_decay", 0.0)))
-            self.grads[i], self.counts[i] = _ptr(g), count
-            written += [(x.data_ptr(), x.data_ptr() + x.numel() * x.element_size())
-                        for x in (p, ma, m, v, ms, vs) if x is not None and x.numel()]
-        written.sort()
-        _want(all(a[1] <= b[0] for a, b in zip(written, written[1:])), what, "tensors that a step writes overlap")
+                for x in (ms, vs):
+                    if x is None or x.dtype != torch.uint8 or x.numel() != blocks or x.get_device() != index or not x.is_contiguous():
+                        raise ValueError(f"{what}: m_scale and v_scale are contiguous uint8, one per 32 elements")
+                c.m_scale, c.v_scale = ms.data_ptr(), vs.data_ptr()
+                written += [(c.m_scale or 0, (c.m_scale or 0) + blocks), (c.v_scale or 0, (c.v_scale or 0) + blocks)]
+            elif ms is not None or vs is not None:
+                raise ValueError(f"{what}: scales go with 8-bit moments")
+            c.param, c.m, c.v, c.count = pa, ma_, va, _ = p.data_ptr(), m.data_ptr(), v.data_ptr(), count
+            c.weight_decay = t.get("weight_decay", 0.0)
+            c.grad = self.grads[i] = g.data_ptr()
+            self.counts[i] = count
+            written += [(pa, pa + size_p * count), (ma_, ma_ + size_m * count), (va, va + size_m * count)]
+        written = sorted(x for x in written if x[0] < x[1])
+        _want(all(x[1] <= y[0] for x, y in zip(written, written[1:])), what, "tensors that a step writes overlap")
 
     def __len__(self) -> int:
         return len(self.tensors)

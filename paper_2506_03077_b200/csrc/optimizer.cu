@@ -16,6 +16,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "common.cuh"
 #include "sm100.cuh"
@@ -114,30 +115,33 @@ __device__ __forceinline__ void decode4(uint32_t codes, float scale, float (&v)[
         v[2 * e + 1] = f.y * scale;
     }
 }
-// biased exponent of the largest magnitude of a value, as the block scale sees it
+// the larger magnitude, a NaN if either is one
+__device__ __forceinline__ float max_abs(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+// biased exponent of the largest magnitude of four values, as the block scale sees it (255: an infinity or a NaN)
 __device__ __forceinline__ uint32_t exponent_of(const float (&v)[4]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int e = 0; e < 4; e++) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
-    return m >> 23;
+    return __float_as_uint(max_abs(max_abs(v[0], v[1]), max_abs(v[2], v[3]))) << 1 >> 24;
 }
 __device__ __forceinline__ uint32_t scale_byte(uint32_t exponent) {
     return exponent == 255u ? 255u : (exponent > 8u ? exponent - 7u : 1u);
 }
-template <bool KEEP>
-__device__ __forceinline__ uint32_t encode4(const float (&v)[4], uint32_t s) {
+// KEEP (values that are not negative): what `nonzero(e)` says is not zero becomes at least the smallest code
+template <bool KEEP, typename F>
+__device__ __forceinline__ uint32_t encode4(const float (&v)[4], uint32_t s, F nonzero) {
     const float inv = s == 255u ? 0.f : __uint_as_float((254u - s) << 23);
-    uint32_t w = 0;
+    float y[4];
 #pragma unroll
-    for (int e = 0; e < 2; e++) {
-        float a = v[2 * e] * inv, b = v[2 * e + 1] * inv;
-        if (KEEP) {
-            if (v[2 * e] > 0.f) a = fmaxf(a, 0.001953125f);
-            if (v[2 * e + 1] > 0.f) b = fmaxf(b, 0.001953125f);
-        }
-        w |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) << (16 * e);
+    for (int e = 0; e < 4; e++) y[e] = v[e] * inv;
+    if (KEEP && fminf(fminf(y[0], y[1]), fminf(y[2], y[3])) < 0.001953125f) {      // rare, or a block that holds zeros
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (nonzero(e)) y[e] = fmaxf(y[e], 0.001953125f);
     }
-    return w;
+    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3) |
+           (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE, __NV_E4M3) << 16;
 }
 // the largest of two 16-bit fields over the eight neighbouring threads that hold a block
 __device__ __forceinline__ uint32_t block_max2(uint32_t v) {
@@ -148,20 +152,175 @@ __device__ __forceinline__ uint32_t block_max2(uint32_t v) {
 
 struct Rates {
     float gs, lr, b1, b2, eps, step_size, inv_root_bc2;
+    float g1, g2, root_b2;      // gs (1 - beta1), gs sqrt(1 - beta2), sqrt(beta2)
 };
-
-// one element: new moments and parameter (sums in fp32; the quotient to 2 ulp, far below the rounding of the result)
-__device__ __forceinline__ void update(const Rates &r, float g, float decay, float &m, float &v, float &u, float &p) {
-    g *= r.gs;
-    m = fmaf(r.b1, m, (1.f - r.b1) * g);
-    v = fmaf(r.b2, v, (1.f - r.b2) * g * g);
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(u) : "f"(v));
-    p = fmaf(p, decay, -r.step_size * __fdividef(m, fmaf(u, r.inv_root_bc2, r.eps)));
+__device__ __forceinline__ float fast_sqrt(float x) {
+    float y;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// the parameter from the new moment m and root u (quotient to 2 ulp, far below the rounding of the result)
+__device__ __forceinline__ float moved(const Rates &r, float p, float decay, float m, float u) {
+    return fmaf(-r.step_size, m * fast_rcp(fmaf(u, r.inv_root_bc2, r.eps)), p * decay);
 }
 
+// One piece of one tensor.  FULL: all of its kPiece elements exist, so that every load is unconditional and all of them
+// are issued before the first is used (with the tests for a tensor's end between them the loads went out one by one).
+template <typename P, bool MASTER, bool FULL>
+__device__ __forceinline__ void step_piece_f32(const streambp_adamw_tensor &t, long long base, const Rates &r) {
+    const long long left = t.count - base;
+    P *param = static_cast<P *>(t.param) + base;
+    float *master = t.master + base;
+    const float *grad = t.grad + base;
+    float *mp = static_cast<float *>(t.m) + base, *vp = static_cast<float *>(t.v) + base;
+    const float decay = 1.f - r.lr * t.weight_decay;
+    float g[kUnroll][4], p[kUnroll][4], m[kUnroll][4], v[kUnroll][4];
+    int valid[kUnroll], off[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; k++) {
+        off[k] = (k * kThreads + (int)threadIdx.x) * kGroup;
+        const long long rest = left - off[k];
+        valid[k] = FULL || rest >= 4 ? 4 : (rest > 0 ? (int)rest : 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; k++) {
+        load4(grad + off[k], valid[k], g[k]);
+        if constexpr (MASTER) load4(master + off[k], valid[k], p[k]);
+        else load4(param + off[k], valid[k], p[k]);
+        load4(mp + off[k], valid[k], m[k]);
+        load4(vp + off[k], valid[k], v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; k++) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const float x = g[k][e] * r.gs;
+            m[k][e] = fmaf(r.b1, m[k][e], (1.f - r.b1) * x);
+            v[k][e] = fmaf(r.b2, v[k][e], (1.f - r.b2) * x * x);
+            p[k][e] = moved(r, p[k][e], decay, m[k][e], fast_sqrt(v[k][e]));
+        }
+        store4(mp + off[k], valid[k], m[k]);
+        store4(vp + off[k], valid[k], v[k]);
+        if constexpr (MASTER) store4(master + off[k], valid[k], p[k]);
+        store4(param + off[k], valid[k], p[k]);
+    }
+}
+
+// Moments in 8 bits: a thread takes eight consecutive elements (8 bytes of codes), four threads hold a block.
+template <typename P, bool MASTER, bool FULL>
+__device__ __forceinline__ void step_piece_mx8(const streambp_adamw_tensor &t, long long base, const Rates &r) {
+    constexpr int kEach = 8;
+    P *param = static_cast<P *>(t.param) + base;
+    float *master = t.master + base;
+    const float *grad = t.grad + base;
+    uint8_t *mc = static_cast<uint8_t *>(t.m) + base, *vc = static_cast<uint8_t *>(t.v) + base;
+    uint8_t *ms = t.m_scale + base / kBlock, *vs = t.v_scale + base / kBlock;
+    const float decay = 1.f - r.lr * t.weight_decay;
+#pragma unroll 1
+    for (int k = 0; k < kPiece / (kThreads * kEach); k++) {
+        const int off = (k * kThreads + (int)threadIdx.x) * kEach;
+        const long long rest = t.count - base - off;
+        const int valid = FULL || rest >= 8 ? 8 : (rest > 0 ? (int)rest : 0);
+        const int lo = FULL ? 4 : (valid < 4 ? valid : 4), hi = valid - lo;
+        float g[8], p[8], m[8], u[8];
+        uint32_t cm[2], cv[2];
+        auto half = [](float (&a)[8], int h) -> float(&)[4] { return *reinterpret_cast<float(*)[4]>(a + 4 * h); };
+        load4(grad + off, lo, half(g, 0));
+        load4(grad + off + 4, hi, half(g, 1));
+        if constexpr (MASTER) {
+            load4(master + off, lo, half(p, 0));
+            load4(master + off + 4, hi, half(p, 1));
+        } else if constexpr (FULL && std::is_same<P, bf16>::value) {
+            Vec<bf16> x;
+            x.load(reinterpret_cast<const bf16 *>(param) + off);
+#pragma unroll
+            for (int e = 0; e < 8; e++) p[e] = x.v[e];
+        } else {
+            load4(param + off, lo, half(p, 0));
+            load4(param + off + 4, hi, half(p, 1));
+        }
+        if constexpr (FULL) {
+            const uint2 a = *reinterpret_cast<const uint2 *>(mc + off), b = *reinterpret_cast<const uint2 *>(vc + off);
+            cm[0] = a.x; cm[1] = a.y; cv[0] = b.x; cv[1] = b.y;
+        } else {
+            cm[0] = load_codes(mc + off, lo); cm[1] = load_codes(mc + off + 4, hi);
+            cv[0] = load_codes(vc + off, lo); cv[1] = load_codes(vc + off + 4, hi);
+        }
+        const uint32_t sm = FULL || valid > 0 ? ms[off / kBlock] : 1u, sv = FULL || valid > 0 ? vs[off / kBlock] : 1u;
+        // beta1 and the root of beta2 go into the scales of the old moments: fewer operations an element than decoding
+        // first and updating then, in a kernel that runs close to the issue rate
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            decode4(cm[h], scale_value(sm) * r.b1, half(m, h));
+            decode4(cv[h], scale_value(sv) * r.root_b2, half(u, h));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const float x = g[e] * r.g2;
+            m[e] = fmaf(g[e], r.g1, m[e]);
+            u[e] = fast_sqrt(fmaf(u[e], u[e], x * x));
+            p[e] = moved(r, p[e], decay, m[e], u[e]);
+            if (!FULL && e >= valid) m[e] = u[e] = 0.f;
+        }
+        const uint32_t em = max(exponent_of(half(m, 0)), exponent_of(half(m, 1))),
+                       eu = max(exponent_of(half(u, 0)), exponent_of(half(u, 1)));
+        uint32_t big = em | (eu << 16);
+        big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        const uint32_t nm = scale_byte(big & 0xffffu), nv = scale_byte(big >> 16);
+        uint32_t wm[2], wv[2];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            wm[h] = encode4<false>(half(m, h), nm, [](int) { return false; });
+            // not zero is decided from what the root is made of: its square may have vanished in fp32
+            wv[h] = encode4<true>(half(u, h), nv, [&](int e) {
+                return 4 * h + e < valid && (g[4 * h + e] * r.g2 != 0.f || (cv[h] >> (8 * e) & 0x7fu) != 0u);
+            });
+        }
+        if constexpr (FULL) {
+            *reinterpret_cast<uint2 *>(mc + off) = make_uint2(wm[0], wm[1]);
+            *reinterpret_cast<uint2 *>(vc + off) = make_uint2(wv[0], wv[1]);
+        } else {
+            store_codes(mc + off, lo, wm[0]); store_codes(mc + off + 4, hi, wm[1]);
+            store_codes(vc + off, lo, wv[0]); store_codes(vc + off + 4, hi, wv[1]);
+        }
+        if ((FULL || valid > 0) && (threadIdx.x & 3) == 0) {
+            ms[off / kBlock] = (uint8_t)nm;
+            vs[off / kBlock] = (uint8_t)nv;
+        }
+        if constexpr (MASTER) {
+            store4(master + off, lo, half(p, 0));
+            store4(master + off + 4, hi, half(p, 1));
+        }
+        if constexpr (FULL && std::is_same<P, bf16>::value) {
+            Vec<bf16> x;
+#pragma unroll
+            for (int e = 0; e < 8; e++) x.v[e] = p[e];
+            x.store(reinterpret_cast<bf16 *>(param) + off);
+        } else {
+            store4(param + off, lo, half(p, 0));
+            store4(param + off + 4, hi, half(p, 1));
+        }
+    }
+}
+template <typename P, bool MX8, bool MASTER, bool FULL>
+__device__ __forceinline__ void step_piece(const streambp_adamw_tensor &t, long long base, const Rates &r) {
+    if constexpr (MX8) step_piece_mx8<P, MASTER, FULL>(t, base, r);
+    else step_piece_f32<P, MASTER, FULL>(t, base, r);
+}
+
+// Blocks per SM: moments in 8 bits are bound by the issue rate and by the loads in flight together, five blocks of 48
+// registers beat four of 64 and three of 80 (233 M bf16 parameters: 0.54 ms a step, 5.2 TB/s; 0.55, 0.61); moments in
+// 32 bits need nothing but loads in flight, three blocks with four units of them a thread run at the copy rate (40 M
+// parameters with a master copy: 0.186 ms, 6.4 TB/s).
 // P: parameter type, MX8: moments in 8 bits.  With a master copy the parameter is the rounded master and is not read.
 template <typename P, bool MX8, int CAP>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ StepParams<CAP> a) {
+__global__ void __launch_bounds__(kThreads, MX8 ? 5 : 3) adamw_kernel(const __grid_constant__ StepParams<CAP> a) {
     pdl_enter();
     __shared__ float s_rate[2];
     Rates r{a.grad_scale ? *a.grad_scale : 1.f, a.lr, a.beta1, a.beta2, a.eps, a.step_size, a.inv_root_bc2};
@@ -177,94 +336,36 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
         r.step_size = s_rate[0];
         r.inv_root_bc2 = s_rate[1];
     }
+    r.g1 = r.gs * (1.f - r.b1);
+    r.g2 = r.gs * sqrtf(1.f - r.b2);
+    r.root_b2 = sqrtf(r.b2);
     const int pieces = a.piece_begin[a.n];
     for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
         const int i = find_tensor(a.piece_begin, a.n, piece);
         const streambp_adamw_tensor &t = a.t[i];
-        const long long base = (long long)(piece - a.piece_begin[i]) * kPiece, left = t.count - base;
-        P *param = static_cast<P *>(t.param) + base;
-        float *master = t.master ? t.master + base : nullptr;
-        const float *grad = t.grad + base;
-        const float decay = 1.f - r.lr * t.weight_decay;
-        float g[kUnroll][4], p[kUnroll][4], m[kUnroll][4], v[kUnroll][4];
-        int valid[kUnroll], off[kUnroll];
-#pragma unroll
-        for (int k = 0; k < kUnroll; k++) {
-            off[k] = (k * kThreads + (int)threadIdx.x) * kGroup;
-            const long long rest = left - off[k];
-            valid[k] = rest >= 4 ? 4 : (rest > 0 ? (int)rest : 0);
-        }
-        if constexpr (MX8) {
-            uint8_t *mc = static_cast<uint8_t *>(t.m) + base, *vc = static_cast<uint8_t *>(t.v) + base;
-            uint8_t *ms = t.m_scale + base / kBlock, *vs = t.v_scale + base / kBlock;
-            uint32_t cm[kUnroll], cv[kUnroll], sm[kUnroll], sv[kUnroll];
-#pragma unroll
-            for (int k = 0; k < kUnroll; k++) {
-                load4(grad + off[k], valid[k], g[k]);
-                if (master) load4(master + off[k], valid[k], p[k]);
-                else load4(param + off[k], valid[k], p[k]);
-                cm[k] = load_codes(mc + off[k], valid[k]);
-                cv[k] = load_codes(vc + off[k], valid[k]);
-                sm[k] = valid[k] > 0 ? ms[off[k] / kBlock] : 1u;
-                sv[k] = valid[k] > 0 ? vs[off[k] / kBlock] : 1u;
-            }
-#pragma unroll
-            for (int k = 0; k < kUnroll; k++) {
-                float u[4];
-                decode4(cm[k], scale_value(sm[k]), m[k]);
-                decode4(cv[k], scale_value(sv[k]), u);
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    float vv = u[e] * u[e];
-                    update(r, g[k][e], decay, m[k][e], vv, u[e], p[k][e]);
-                    if (e >= valid[k]) m[k][e] = u[e] = 0.f;
-                }
-                const uint32_t big = block_max2(exponent_of(m[k]) | (exponent_of(u) << 16));
-                const uint32_t nm = scale_byte(big & 0xffffu), nv = scale_byte(big >> 16);
-                store_codes(mc + off[k], valid[k], encode4<false>(m[k], nm));
-                store_codes(vc + off[k], valid[k], encode4<true>(u, nv));
-                if (valid[k] > 0 && (threadIdx.x & 7) == 0) {
-                    ms[off[k] / kBlock] = (uint8_t)nm;
-                    vs[off[k] / kBlock] = (uint8_t)nv;
-                }
-                if (master) store4(master + off[k], valid[k], p[k]);
-                store4(param + off[k], valid[k], p[k]);
-            }
+        const long long base = (long long)(piece - a.piece_begin[i]) * kPiece;
+        const bool full = t.count - base >= kPiece;
+        if (std::is_same<P, bf16>::value && t.master) {
+            if (full) step_piece<P, MX8, true, true>(t, base, r);
+            else step_piece<P, MX8, true, false>(t, base, r);
         } else {
-            float *mp = static_cast<float *>(t.m) + base, *vp = static_cast<float *>(t.v) + base;
-#pragma unroll
-            for (int k = 0; k < kUnroll; k++) {
-                load4(grad + off[k], valid[k], g[k]);
-                if (master) load4(master + off[k], valid[k], p[k]);
-                else load4(param + off[k], valid[k], p[k]);
-                load4(mp + off[k], valid[k], m[k]);
-                load4(vp + off[k], valid[k], v[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < kUnroll; k++) {
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    float u;
-                    update(r, g[k][e], decay, m[k][e], v[k][e], u, p[k][e]);
-                }
-                store4(mp + off[k], valid[k], m[k]);
-                store4(vp + off[k], valid[k], v[k]);
-                if (master) store4(master + off[k], valid[k], p[k]);
-                store4(param + off[k], valid[k], p[k]);
-            }
+            if (full) step_piece<P, MX8, false, true>(t, base, r);
+            else step_piece<P, MX8, false, false>(t, base, r);
         }
     }
 }
 
 // ---- norm of all gradients -----------------------------------------------------------------------------------
-// Block b sums the squares of its pieces in 64 bits (squares of fp32 values neither overflow nor vanish there, and the
-// conversions and products are far from what the 1.6e12 elements a second of the read need of the fp64 units) into
-// partial[b]; one block then adds the partials in their order.  No atomics: the same gradients give the same bits.
-constexpr int kNormCap = 512;
+// Block b sums the squares of its pieces into partial[b]; one block then adds the partials in their order.  No atomics:
+// the same gradients give the same bits.  A thread forms the squares of eight elements at a time in fp32 and adds them
+// up in 64 bits (every square in 64 bits made the fp64 units the bound: 287 us for 233 M elements against 145 us of
+// reading).  Where such a sum leaves the range in which fp32 squares are exact to a rounding -- gradients above 1e19, or
+// all below 1e-13 -- the eight are squared again in 64 bits, so no norm of fp32 values overflows or vanishes.
+template <int CAP>
 struct NormParams {
-    const float *grad[kNormCap];
-    long long count[kNormCap];
-    int piece_begin[kNormCap + 1];
+    const float *grad[CAP];
+    long long count[CAP];
+    int piece_begin[CAP + 1];
     int n;
     int first;                       // 0: add to what an earlier launch of the same call left in the partials
     double *partial;
@@ -285,7 +386,34 @@ __device__ __forceinline__ double block_sum_f64(double v, double *red) {
     return t;                        // complete in warp 0
 }
 
-__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_constant__ NormParams a) {
+__device__ __forceinline__ double squares8(const float (&a)[4], const float (&b)[4]) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; e++) s = fmaf(a[e], a[e], fmaf(b[e], b[e], s));
+    if (s < 1e30f && s > 1e-26f) return (double)s;
+    double d = 0.0;
+#pragma unroll
+    for (int e = 0; e < 4; e++) d += (double)a[e] * a[e] + (double)b[e] * b[e];
+    return d;
+}
+
+template <bool FULL>
+__device__ __forceinline__ double norm_piece(const float *g, long long left) {
+    float x[kNormUnroll][4];
+#pragma unroll
+    for (int k = 0; k < kNormUnroll; k++) {
+        const int off = (k * kThreads + (int)threadIdx.x) * kGroup;
+        const long long rest = left - off;
+        load4(g + off, FULL || rest >= 4 ? 4 : (rest > 0 ? (int)rest : 0), x[k]);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < kNormUnroll; k += 2) sum += squares8(x[k], x[k + 1]);
+    return sum;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_constant__ NormParams<CAP> a) {
     pdl_enter();
     __shared__ double red[32];
     double sum = 0.0;
@@ -293,18 +421,7 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_consta
     for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
         const int i = find_tensor(a.piece_begin, a.n, piece);
         const long long base = (long long)(piece - a.piece_begin[i]) * kNormPiece, left = a.count[i] - base;
-        const float *g = a.grad[i] + base;
-        float x[kNormUnroll][4];
-#pragma unroll
-        for (int k = 0; k < kNormUnroll; k++) {
-            const int off = (k * kThreads + (int)threadIdx.x) * kGroup;
-            const long long rest = left - off;
-            load4(g + off, rest >= 4 ? 4 : (rest > 0 ? (int)rest : 0), x[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kNormUnroll; k++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) sum = fma((double)x[k][e], (double)x[k][e], sum);
+        sum += left >= kNormPiece ? norm_piece<true>(a.grad[i] + base, left) : norm_piece<false>(a.grad[i] + base, left);
     }
     const double s = block_sum_f64(sum, red);
     if (threadIdx.x == 0) a.partial[blockIdx.x] = a.first ? s : a.partial[blockIdx.x] + s;
@@ -335,32 +452,47 @@ __global__ void __launch_bounds__(kThreads) mx8_encode_kernel(const float *x, lo
         float v[4];
         load4(x + at, valid, v);
         const uint32_t s = scale_byte(block_max2(exponent_of(v)));
-        store_codes(codes + at, valid, encode4<KEEP>(v, s));
+        store_codes(codes + at, valid, encode4<KEEP>(v, s, [&](int e) { return v[e] > 0.f; }));
         if (valid > 0 && (threadIdx.x & 7) == 0) scale[at / kBlock] = (uint8_t)s;
     }
 }
+// 16 codes (one 16-byte load, half a block) per thread and turn, two turns in flight
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx8_decode_kernel(const uint8_t *codes, const uint8_t *scale, long long count, T *out) {
     pdl_enter();
-    const long long step = (long long)gridDim.x * kThreads * kGroup;
-    for (long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) * kGroup; at < count; at += kUnroll * step) {
-        uint32_t w[kUnroll], s[kUnroll];
-        int valid[kUnroll];
+    const long long step = (long long)gridDim.x * kThreads * 16;
+    for (long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) * 16; at < count; at += 2 * step) {
+        uint4 w[2];
+        uint32_t s[2];
 #pragma unroll
-        for (int k = 0; k < kUnroll; k++) {
-            const long long o = at + k * step, rest = count - o;
-            valid[k] = rest >= 4 ? 4 : (rest > 0 ? (int)rest : 0);
-            if (valid[k] > 0) {
-                w[k] = load_codes(codes + o, valid[k]);
-                s[k] = scale[o / kBlock];
-            }
+        for (int k = 0; k < 2; k++) {
+            const long long o = at + k * step;
+            if (o + 16 <= count) w[k] = *reinterpret_cast<const uint4 *>(codes + o);
+            if (o < count) s[k] = scale[o / kBlock];
         }
 #pragma unroll
-        for (int k = 0; k < kUnroll; k++) {
-            if (valid[k] == 0) continue;
-            float v[4];
-            decode4(w[k], scale_value(s[k]), v);
-            store4(out + at + k * step, valid[k], v);
+        for (int k = 0; k < 2; k++) {
+            const long long o = at + k * step;
+            if (o + 16 <= count) {
+                const uint32_t q[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                float v[16];
+#pragma unroll
+                for (int e = 0; e < 4; e++) decode4(q[e], scale_value(s[k]), *reinterpret_cast<float(*)[4]>(v + 4 * e));
+#pragma unroll
+                for (int e = 0; e < 16; e += Vec<T>::N) {
+                    Vec<T> x;
+#pragma unroll
+                    for (int i = 0; i < Vec<T>::N; i++) x.v[i] = v[e + i];
+                    x.store(out + o + e);
+                }
+            } else {
+                for (long long e = o; e < count; e += 4) {
+                    const int valid = count - e < 4 ? (int)(count - e) : 4;
+                    float v[4];
+                    decode4(load_codes(codes + e, valid), scale_value(s[k]), v);
+                    store4(out + e, valid, v);
+                }
+            }
         }
     }
 }
@@ -404,6 +536,36 @@ int launch_adamw(const streambp_adamw_cfg &c, const streambp_adamw_tensor *tenso
         a.grad_scale = grad_scale;
         a.step = step;
         SBP_LAUNCH((adamw_kernel<P, MX8, CAP>), grid_for(pieces, 8), kThreads, 0, st, a);
+    }
+    return STREAMBP_OK;
+}
+template <int CAP>
+int launch_norm(const float *const *grads, const int64_t *counts, int n, double *partial, int *used, cudaStream_t st) {
+    NormParams<CAP> a;
+    a.partial = partial;
+    const int most = sm_count() * 4 < 4096 ? sm_count() * 4 : 4096;   // blocks of a launch: those of a call share the partials
+    int i = 0;
+    *used = 0;
+    while (i < n) {
+        a.n = 0;
+        int64_t pieces = 0;
+        for (; i < n && a.n < CAP; i++) {
+            if (counts[i] == 0) continue;
+            const int64_t more = (counts[i] + kNormPiece - 1) / kNormPiece;
+            if (pieces + more > 0x40000000) break;
+            a.grad[a.n] = grads[i];
+            a.count[a.n] = counts[i];
+            a.piece_begin[a.n++] = (int)pieces;
+            pieces += more;
+        }
+        if (a.n == 0) break;
+        a.piece_begin[a.n] = (int)pieces;
+        a.first = *used == 0;
+        // the first launch of a call that needs more than one sets every partial, the others add to them
+        const bool one = a.first && i == n;
+        const int grid = one && pieces < most ? (int)pieces : most;
+        *used = grid;
+        SBP_LAUNCH(grad_norm_kernel<CAP>, grid, kThreads, 0, st, a);
     }
     return STREAMBP_OK;
 }
@@ -472,33 +634,11 @@ int streambp_grad_norm(const float *const *grads, const int64_t *counts, int32_t
     begin_call();
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     NvtxRange range("streambp_grad_norm");
-    NormParams a;
-    a.partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + kHeaderBytes);
-    int most = sm_count() * 4;                      // blocks of every launch of the call: they share the partials
-    if (most > 4096) most = 4096;
-    int used = 0, i = 0;
-    while (i < n) {
-        a.n = 0;
-        int64_t pieces = 0;
-        for (; i < n && a.n < kNormCap; i++) {
-            if (counts[i] == 0) continue;
-            const int64_t more = (counts[i] + kNormPiece - 1) / kNormPiece;
-            if (pieces + more > 0x40000000) break;
-            a.grad[a.n] = grads[i];
-            a.count[a.n] = counts[i];
-            a.piece_begin[a.n++] = (int)pieces;
-            pieces += more;
-        }
-        if (a.n == 0) break;
-        a.piece_begin[a.n] = (int)pieces;
-        a.first = used == 0;
-        // the first launch of a call that needs more than one sets every partial, the others add to them
-        const bool one = a.first && i == n;
-        const int grid = one && pieces < most ? (int)pieces : most;
-        used = grid;
-        SBP_LAUNCH(grad_norm_kernel, grid, kThreads, 0, st, a);
-    }
-    SBP_LAUNCH(grad_norm_finish_kernel, 1, 1024, 0, st, a.partial, used, max_norm, norm, scale);
+    double *partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + kHeaderBytes);
+    int used = 0;
+    if (n <= 32) SBP_TRY(launch_norm<32>(grads, counts, n, partial, &used, st));
+    else SBP_TRY(launch_norm<512>(grads, counts, n, partial, &used, st));
+    SBP_LAUNCH(grad_norm_finish_kernel, 1, 1024, 0, st, partial, used, max_norm, norm, scale);
     return STREAMBP_OK;
 }
 
@@ -525,7 +665,7 @@ int streambp_mx8_decode(const uint8_t *codes, const uint8_t *scales, int64_t cou
     if (!al16(codes) || !al16(out)) return STREAMBP_E_ALIGN;
     begin_call();
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const int grid = grid_for((count + kPiece - 1) / kPiece, 8);
+    const int grid = grid_for((count + kThreads * 32 - 1) / (kThreads * 32), 8);
     if (out_dtype == STREAMBP_F32) SBP_LAUNCH(mx8_decode_kernel<float>, grid, kThreads, 0, st, codes, scales, (long long)count, (float *)out);
     else SBP_LAUNCH(mx8_decode_kernel<bf16>, grid, kThreads, 0, st, codes, scales, (long long)count, (bf16 *)out);
     return STREAMBP_OK;

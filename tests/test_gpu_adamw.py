@@ -85,7 +85,8 @@ def check_step(case, before, step, gs=1.0, h=H):
         v = b2 * old["v64"] + (1 - b2) * g * g
         # three roundings of a term, one of the sum, one of the scaled gradient
         em = 5 * E32 * (np.abs(b1 * old["m64"]) + np.abs((1 - b1) * g))
-        ev = 7 * E32 * v
+        # the squared gradient: three roundings of its factor count twice, the product and the sum once
+        ev = 8 * E32 * v
         p0 = old["master" if "master" in old else "param"].double().cpu().numpy()
         root = np.sqrt(v)
         den = root / np.sqrt(1 - b2 ** step) + eps
@@ -228,9 +229,10 @@ def test_grad_norm(sizes):
     ref = np.sqrt(sum((t["grad"].double() ** 2).sum().item() for t in c.tensors))
     for most in (ref * 0.25, ref * 4):
         B.grad_norm(c.plan, most, norm, scale, ws[:-256])
-        assert abs(norm.item() - ref) <= 2 * E32 * ref
+        # eight squares and their sum in fp32: nine roundings of the sum, half of that for its root, one of the result
+        assert abs(norm.item() - ref) <= 6 * E32 * ref
         want = min(1.0, f32(most) / (ref + 1e-6))
-        assert abs(scale.item() - want) <= 4 * E32 * want
+        assert abs(scale.item() - want) <= 8 * E32 * want
     first = norm.clone()
     B.grad_norm(c.plan, 1.0, norm, None, ws[:-256])
     assert torch.equal(first, norm) and bool((ws[-256:] == FENCE).all())
@@ -241,11 +243,11 @@ def test_grad_norm_of_huge_tiny_and_broken_gradients():
     ws = B.alloc_workspace(B.grad_norm_workspace_bytes())
     norm, scale = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
     g = c.tensors[0]["grad"]
-    for size in (1e30, 1e-30):
+    for size in (1e30, 1e-30, 1e-20, 1e-14):
         g.fill_(size)
         B.grad_norm(c.plan, 1.0, norm, scale, ws)
         ref = f32(size) * np.sqrt(1000.0)
-        assert abs(norm.item() - ref) <= 2 * E32 * ref
+        assert abs(norm.item() - ref) <= 6 * E32 * ref
     g[999] = float("inf")
     B.grad_norm(c.plan, 1.0, norm, scale, ws)
     assert np.isinf(norm.item()) and np.isnan(scale.item())
