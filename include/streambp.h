@@ -361,6 +361,33 @@ int streambp_gemm_swiglu(const void *A, int64_t lda, const void *w_gate, const v
                          int64_t N, int64_t K, void *g, void *u, void *m, int32_t dtype, void *cuda_stream);
 
 /*
+ * (No counterpart in the paper's method, whose layer has a gated MLP; the products of layers that have none.)
+ * A product with bias, activation and residual in its epilogue, and the gradient of that epilogue.
+ *     z = A W^T + bias,   C = act(z) + residual
+ * A: [M, K] (lda), W: [N, K] (ldw), bias: [N] or NULL, residual: [M, N] (ldr) or NULL, C: [M, N] (ldc), pre: [M, N] (ldp)
+ * or NULL receives z (what the gradient needs); all of `dtype`.  Bias, activation and residual are applied in fp32 to the
+ * accumulated product and rounded once; the activation reads the unrounded z.  residual may be C itself (same ld).
+ * bf16 runs on the tcgen05 product kernel where A and W are 16-byte aligned with leading dimensions that are multiples
+ * of 8; N, ldc, ldr and ldp are free (multiples of 8 are faster).  float, and bf16 operands outside that rule, run on
+ * CUDA cores.  STREAMBP_E_ALIGN where a pointer does not have its elements' alignment.
+ *   ACT_GELU is z/2 (1 + erf(z / sqrt 2)), ACT_GELU_TANH its tanh form, ACT_SILU z sigmoid(z).
+ *
+ * Backward: dZ = dC act'(pre) (rounded once; dZ may be dC or pre, or NULL where only dbias is wanted) and, unless NULL,
+ * dbias[n] (+)= sum over rows of the unrounded dZ.  pre may be NULL for ACT_NONE.  The residual's gradient is dC; dA and dW
+ * are the products streambp_gemm (NN) and (TN) form from dZ.  The sums are added in a fixed order.
+ */
+typedef enum {
+    STREAMBP_ACT_NONE = 0, STREAMBP_ACT_RELU = 1, STREAMBP_ACT_GELU = 2, STREAMBP_ACT_GELU_TANH = 3, STREAMBP_ACT_SILU = 4
+} streambp_activation;
+int streambp_gemm_epilogue(const void *A, int64_t lda, const void *W, int64_t ldw, int64_t M, int64_t N, int64_t K,
+                           const void *bias, int32_t activation, const void *residual, int64_t ldr, void *C, int64_t ldc,
+                           void *pre, int64_t ldp, int32_t dtype, void *cuda_stream);
+size_t streambp_gemm_epilogue_workspace_bytes(int64_t M, int64_t N);
+int streambp_gemm_epilogue_backward(const void *dC, int64_t ldd, const void *pre, int64_t ldp, int32_t activation, int64_t M,
+                                    int64_t N, void *dZ, int64_t ldz, float *dbias, int accumulate, int32_t dtype,
+                                    void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
  * Building blocks exposed for tests and profiling: the partitioned attention of Sec. 3.2.2
  * (S^(i) = Q^(i) K^(:i)T, causal softmax, O^(i) = P^(i) V^(:i)) for one chunk of n query rows that
  * sit at absolute rows q0 .. q0+n-1 and attend to keys 0 .. q0+n-1, and its backward.

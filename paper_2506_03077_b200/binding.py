@@ -40,7 +40,8 @@ EXPORTS = (
     "streambp_lmhead_workspace_bytes_grouped", "streambp_lmhead_ce_backward_grouped",
     "streambp_lmhead_rl_backward_grouped",
     "streambp_adamw_step", "streambp_grad_norm_workspace_bytes", "streambp_grad_norm", "streambp_mx8_encode",
-    "streambp_mx8_decode",
+    "streambp_mx8_decode", "streambp_gemm_epilogue", "streambp_gemm_epilogue_workspace_bytes",
+    "streambp_gemm_epilogue_backward",
 )
 
 
@@ -178,6 +179,12 @@ def lib() -> C.CDLL:
     L.streambp_test_workspace_guard.argtypes = [vp, sz, i32, vp]
     L.streambp_test_per_device_value.restype = C.c_int
     L.streambp_test_per_device_value.argtypes = [C.c_int, C.c_int]
+    L.streambp_gemm_epilogue.restype = C.c_int
+    L.streambp_gemm_epilogue.argtypes = [vp, i64, vp, i64, i64, i64, i64, vp, i32, vp, i64, vp, i64, vp, i64, i32, vp]
+    L.streambp_gemm_epilogue_workspace_bytes.restype = sz
+    L.streambp_gemm_epilogue_workspace_bytes.argtypes = [i64, i64]
+    L.streambp_gemm_epilogue_backward.restype = C.c_int
+    L.streambp_gemm_epilogue_backward.argtypes = [vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, C.c_int, i32, vp, sz, vp]
     L.streambp_adamw_step.restype = C.c_int
     L.streambp_adamw_step.argtypes = [C.POINTER(AdamWCfgC), C.POINTER(AdamWTensorC), i32, vp, vp, vp]
     L.streambp_grad_norm_workspace_bytes.restype = sz
@@ -547,6 +554,66 @@ def gemm_swiglu(A, w_gate, w_up, g, u, m, stream=None, check: bool = True) -> in
                                     _ptr(u), _ptr(m), _dtype_code(A.dtype), _stream_ptr(stream))
     if check:
         _check(st, "streambp_gemm_swiglu")
+    return st
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _rows(what: str, dev: int, dtype: torch.dtype, shape: tuple, t: Optional[torch.Tensor]) -> tuple:
+    """(address, leading dimension) of a matrix whose rows are contiguous; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.get_device() != dev or t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{what}: expected a {dtype} tensor {shape} on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    rows, cols = t.stride()
+    if (cols != 1 and shape[1] > 1) or (rows < shape[1] and shape[0] > 1):
+        raise ValueError(f"{what}: rows must be contiguous and must not overlap (strides {t.stride()})")
+    return t.data_ptr(), max(rows, shape[1])
+
+
+def gemm_epilogue(A, W, C_out, bias=None, activation: str = "none", residual=None, pre=None, stream=None,
+                  check: bool = True) -> int:
+    """streambp_gemm_epilogue: C = act(A W^T + bias) + residual, the sum before act in `pre` if given.  A [M, K],
+    W [N, K], the others [M, N]; rows contiguous, any leading dimension; residual may be C_out."""
+    what, dev, dt = "gemm_epilogue", A.get_device(), A.dtype
+    _want(A.is_cuda and A.dim() == 2 and W.dim() == 2, what, "A and W are CUDA matrices")
+    (M, K), N = A.shape, W.shape[0]
+    a, w = _rows(what, dev, dt, (M, K), A), _rows(what, dev, dt, (N, K), W)
+    c, r, z = (_rows(what, dev, dt, (M, N), t) for t in (C_out, residual, pre))
+    if bias is not None and (bias.get_device() != dev or bias.dtype != dt or tuple(bias.shape) != (N,) or not bias.is_contiguous()):
+        raise ValueError(f"{what}: bias is a contiguous {dt} vector of {N} on cuda:{dev}")
+    with _Launch(what, A.device, stream) as s:
+        st = lib().streambp_gemm_epilogue(a[0], a[1], w[0], w[1], M, N, K, None if bias is None else bias.data_ptr(),
+                                          ACTIVATIONS[activation], r[0], r[1], c[0], c[1], z[0], z[1], _dtype_code(dt), s)
+    if check:
+        _check(st, "streambp_gemm_epilogue")
+    return st
+
+
+def gemm_epilogue_workspace_bytes(M: int, N: int) -> int:
+    return int(lib().streambp_gemm_epilogue_workspace_bytes(M, N))
+
+
+def gemm_epilogue_backward(dC, pre, activation: str, dZ=None, dbias=None, workspace=None, accumulate: bool = False,
+                           stream=None, check: bool = True) -> int:
+    """streambp_gemm_epilogue_backward: dZ = dC act'(pre), dbias (fp32 [N]) = or += column sums of dZ."""
+    what, dev, dt = "gemm_epilogue_backward", dC.get_device(), dC.dtype
+    _want(dC.is_cuda and dC.dim() == 2, what, "dC is a CUDA matrix")
+    M, N = dC.shape
+    d, z, g = (_rows(what, dev, dt, (M, N), t) for t in (dC, pre, dZ))
+    if dbias is not None and (dbias.get_device() != dev or dbias.dtype != torch.float32 or tuple(dbias.shape) != (N,) or
+                              not dbias.is_contiguous()):
+        raise ValueError(f"{what}: dbias is a contiguous fp32 vector of {N} on cuda:{dev}")
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        raise ValueError(f"{what}: workspace is contiguous, on cuda:{dev}")
+    with _Launch(what, dC.device, stream) as s:
+        st = lib().streambp_gemm_epilogue_backward(d[0], d[1], z[0], z[1], ACTIVATIONS[activation], M, N, g[0], g[1],
+                                                   None if dbias is None else dbias.data_ptr(), 1 if accumulate else 0,
+                                                   _dtype_code(dt), None if workspace is None else workspace.data_ptr(),
+                                                   0 if workspace is None else workspace.numel() * workspace.element_size(), s)
+    if check:
+        _check(st, "streambp_gemm_epilogue_backward")
     return st
 
 

@@ -2,6 +2,7 @@
 #include <atomic>
 #include <cstdlib>
 #include <cstring>
+#include <type_traits>
 #include <vector>
 
 #include <cstdio>
@@ -325,6 +326,24 @@ int check_layer_grads(const streambp_layer_cfg *c, const streambp_layer_grads *g
         }
     }
     return STREAMBP_OK;
+}
+// [rows, cols] of `es`-byte elements behind a pointer: aligned to its elements, rows that do not overlap
+int check_matrix(const void *p, int64_t ld, int64_t cols, int es) {
+    if (!aligned(p, es)) return STREAMBP_E_ALIGN;
+    return ld < cols ? STREAMBP_E_SHAPE : STREAMBP_OK;
+}
+template <typename T>
+int run_epilogue(const void *A, int64_t lda, const void *W, int64_t ldw, int64_t M, int64_t N, int64_t K, const void *bias,
+                 int act, const void *residual, int64_t ldr, void *C, int64_t ldc, void *pre, int64_t ldp, cudaStream_t st) {
+    const GemmEpilogue<T> g{M, N, K, (const T *)A, lda, (const T *)W, ldw, (const T *)bias, act,
+                            (const T *)residual, ldr, (T *)C, ldc, (T *)pre, ldp};
+    ProfScope prof(KC_GEMM, 2.0 * (double)M * (double)N * (double)K, st);
+    if constexpr (std::is_same<T, bf16>::value) {
+        const int e = gemm_engine();
+        if (e != 1 && gemm_tc_epilogue_supported(g)) return gemm_tc_epilogue(g, st);
+        if (e == 2) return STREAMBP_E_SHAPE;
+    }
+    return gemm_simt_epilogue<T>(g, st);
 }
 // weights with the bias pointers dropped when the configuration has no bias
 streambp_layer_weights effective(const streambp_layer_cfg *c, const streambp_layer_weights *w) {
@@ -786,6 +805,69 @@ int streambp_gemm_grouped(const streambp_gemm_problem *problems, int32_t n, int3
     call_state().launches = 0;
     if (!gemm_tc_group_supported(gp, n)) return STREAMBP_E_SHAPE;
     return gemm_tc_group(gp, n, sched, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int streambp_gemm_epilogue(const void *A, int64_t lda, const void *W, int64_t ldw, int64_t M, int64_t N, int64_t K,
+                           const void *bias, int32_t activation, const void *residual, int64_t ldr, void *C, int64_t ldc,
+                           void *pre, int64_t ldp, int32_t dtype, void *cuda_stream) {
+    if (!A || !W || !C) return STREAMBP_E_NULL;
+    if (dtype != STREAMBP_F32 && dtype != STREAMBP_BF16) return STREAMBP_E_DTYPE;
+    const int64_t most = 1ll << 30;
+    if (M < 1 || N < 1 || K < 1 || M > most || N > most || K > most || activation < STREAMBP_ACT_NONE ||
+        activation > STREAMBP_ACT_SILU)
+        return STREAMBP_E_SHAPE;
+    const int es = dtype == STREAMBP_F32 ? 4 : 2;
+    SBP_TRY(check_matrix(A, lda, K, es));
+    SBP_TRY(check_matrix(W, ldw, K, es));
+    SBP_TRY(check_matrix(C, ldc, N, es));
+    if (residual) SBP_TRY(check_matrix(residual, ldr, N, es));
+    if (pre) SBP_TRY(check_matrix(pre, ldp, N, es));
+    if (bias) SBP_TRY(check_matrix(bias, N, N, es));
+    if ((residual == C && ldr != ldc) || pre == C || (pre && pre == residual)) return STREAMBP_E_SHAPE;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    call_state().cuda_error = 0;
+    call_state().launches = 0;
+    if (dtype == STREAMBP_F32)
+        return run_epilogue<float>(A, lda, W, ldw, M, N, K, bias, activation, residual, ldr, C, ldc, pre, ldp, st);
+    return run_epilogue<bf16>(A, lda, W, ldw, M, N, K, bias, activation, residual, ldr, C, ldc, pre, ldp, st);
+}
+
+size_t streambp_gemm_epilogue_workspace_bytes(int64_t M, int64_t N) {
+    if (M < 1 || N < 1 || M > (1ll << 30) || N > (1ll << 30)) return 0;
+    Arena a(nullptr);
+    a.take_bytes(kHeaderBytes);
+    a.take<float>((size_t)gemm_epilogue_splits(M, N) * (size_t)N);
+    return a.size();
+}
+
+int streambp_gemm_epilogue_backward(const void *dC, int64_t ldd, const void *pre, int64_t ldp, int32_t activation, int64_t M,
+                                    int64_t N, void *dZ, int64_t ldz, float *dbias, int accumulate, int32_t dtype,
+                                    void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!dC || (!dZ && !dbias) || (activation != STREAMBP_ACT_NONE && !pre) || (dbias && !workspace)) return STREAMBP_E_NULL;
+    if (dtype != STREAMBP_F32 && dtype != STREAMBP_BF16) return STREAMBP_E_DTYPE;
+    if (M < 1 || N < 1 || M > (1ll << 30) || N > (1ll << 30) || activation < STREAMBP_ACT_NONE || activation > STREAMBP_ACT_SILU)
+        return STREAMBP_E_SHAPE;
+    const int es = dtype == STREAMBP_F32 ? 4 : 2;
+    SBP_TRY(check_matrix(dC, ldd, N, es));
+    if (activation != STREAMBP_ACT_NONE) SBP_TRY(check_matrix(pre, ldp, N, es));
+    if (dZ) SBP_TRY(check_matrix(dZ, ldz, N, es));
+    if ((dZ == dC && ldz != ldd) || (dZ && dZ == pre && activation != STREAMBP_ACT_NONE && ldz != ldp)) return STREAMBP_E_SHAPE;
+    float *partials = nullptr;
+    if (dbias) {
+        if (!aligned(dbias, 4) || !aligned(workspace, 256)) return STREAMBP_E_ALIGN;
+        if (workspace_bytes < streambp_gemm_epilogue_workspace_bytes(M, N)) return STREAMBP_E_WORKSPACE;
+        Arena a(workspace);
+        a.take_bytes(kHeaderBytes);
+        partials = a.take<float>((size_t)gemm_epilogue_splits(M, N) * (size_t)N);
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    call_state().cuda_error = 0;
+    call_state().launches = 0;
+    if (dtype == STREAMBP_F32)
+        return gemm_epilogue_bwd<float>((const float *)dC, ldd, (const float *)pre, ldp, activation, M, N, (float *)dZ, ldz,
+                                        dbias, accumulate != 0, partials, st);
+    return gemm_epilogue_bwd<bf16>((const bf16 *)dC, ldd, (const bf16 *)pre, ldp, activation, M, N, (bf16 *)dZ, ldz, dbias,
+                                   accumulate != 0, partials, st);
 }
 
 int streambp_gemm_swiglu(const void *A, int64_t lda, const void *w_gate, const void *w_up, int64_t ldb, int64_t M,

@@ -317,6 +317,35 @@ bool gemm_tc_group_supported(const GemmProb *probs, int n);
 // enabling the dynamic tile schedule; nullptr selects the static one.
 int gemm_tc_group(const GemmProb *probs, int n, int *sched, cudaStream_t st);
 
+// C = act(A W^T + bias) + residual, optionally the sum before act in `pre` (A [M, K], W [N, K], the others [M, N]; T is
+// the type of all of them).  residual may be C itself.
+template <typename T>
+struct GemmEpilogue {
+    int64_t M, N, K;
+    const T *A;
+    int64_t lda;
+    const T *W;
+    int64_t ldw;
+    const T *bias;        // optional [N]
+    int act;              // streambp_activation
+    const T *residual;    // optional
+    int64_t ldr;
+    T *C;
+    int64_t ldc;
+    T *pre;               // optional
+    int64_t ldp;
+};
+bool gemm_tc_epilogue_supported(const GemmEpilogue<bf16> &g);
+int gemm_tc_epilogue(const GemmEpilogue<bf16> &g, cudaStream_t st);
+template <typename T>
+int gemm_simt_epilogue(const GemmEpilogue<T> &g, cudaStream_t st);
+// dZ = dC * act'(pre) (dZ may be dC or pre, or nullptr where only the column sums are wanted) and, unless nullptr,
+// dbias[n] (+)= sum over rows of dZ before it is rounded; partials: [gemm_epilogue_splits(M, N), N] floats
+int gemm_epilogue_splits(int64_t M, int64_t N);
+template <typename T>
+int gemm_epilogue_bwd(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int act, int64_t M, int64_t N, T *dZ, int64_t ldz,
+                      float *dbias, bool accumulate, float *partials, cudaStream_t st);
+
 // Reads and clears the flag a tensor-core kernel raises when one of its bounded waits expires.
 int gemm_tc_take_fault();
 int gemm_tc_variant();   // 2: CTA-pair kernel, 1: single-CTA kernel, 0: tensor maps unavailable

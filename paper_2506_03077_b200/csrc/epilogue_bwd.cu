@@ -1,0 +1,149 @@
+// Gradient of the product epilogue C = act(z) + residual, z = A W^T + bias: dz = dC * act'(z), dbias = column sums of dz
+// (the residual's gradient is dC itself; dA = dz W and dW = dz^T A are products).
+//
+// HBM-bound: dC and z are read once, dz is written once.  A block owns a strip of 64 columns (a 128-byte row segment in
+// bf16, eight threads of one 16-byte load each) and walks its rows 32 at a time, keeping the sums of its columns in
+// registers; a grid of (strips, row splits) fills the GPU, each split leaves its sums in `partials`, and a second small
+// kernel adds the splits in their order: no atomics, the same inputs give the same bits.
+#include "activation.cuh"
+#include "sm100.cuh"
+
+namespace sbp {
+namespace {
+
+constexpr int kStrip = 64, kRowsAtOnce = 32;
+
+template <typename T, int ACT, bool VEC>
+__global__ void __launch_bounds__(256)
+    epilogue_bwd_kernel(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int N, int64_t rows_per_split, T *dZ,
+                        int64_t ldz, float *partials) {
+    pdl_enter();
+    constexpr bool FAST = sizeof(T) == 2;
+    __shared__ float s_sum[8][kStrip + 1];
+    const int tc = threadIdx.x & 7, tr = threadIdx.x >> 3;
+    const int col0 = blockIdx.x * kStrip + tc * 8;
+    const int64_t first = blockIdx.y * rows_per_split, end = first + rows_per_split < M ? first + rows_per_split : M;
+    float sum[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) sum[e] = 0.f;
+    const int cols = N - col0 >= 8 ? 8 : (N - col0 > 0 ? N - col0 : 0);
+    if (VEC && cols == 8) {
+        constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;           // rows in flight per thread
+        for (int64_t r0 = first + tr; r0 < end; r0 += kRowsAtOnce * kAhead) {
+            Vec<T> d[kAhead][8 / Vec<T>::N], z[kAhead][8 / Vec<T>::N];
+#pragma unroll
+            for (int a = 0; a < kAhead; a++) {
+                const int64_t r = r0 + a * kRowsAtOnce;
+                if (r < end) {
+#pragma unroll
+                    for (int v = 0; v < 8 / Vec<T>::N; v++) {
+                        d[a][v].load(dC + r * ldd + col0 + v * Vec<T>::N);
+                        if (ACT != STREAMBP_ACT_NONE) z[a][v].load(pre + r * ldp + col0 + v * Vec<T>::N);
+                    }
+                }
+            }
+#pragma unroll
+            for (int a = 0; a < kAhead; a++) {
+                const int64_t r = r0 + a * kRowsAtOnce;
+                if (r < end) {
+#pragma unroll
+                    for (int v = 0; v < 8 / Vec<T>::N; v++) {
+#pragma unroll
+                        for (int e = 0; e < Vec<T>::N; e++) {
+                            if (ACT != STREAMBP_ACT_NONE) d[a][v].v[e] *= slope<ACT, FAST>(z[a][v].v[e]);
+                            sum[v * Vec<T>::N + e] += d[a][v].v[e];
+                        }
+                        if (dZ) d[a][v].store(dZ + r * ldz + col0 + v * Vec<T>::N);
+                    }
+                }
+            }
+        }
+    } else {
+        for (int64_t r = first + tr; r < end; r += kRowsAtOnce)
+            for (int e = 0; e < 8; e++)
+                if (e < cols) {
+                    float d = to_f32(dC[r * ldd + col0 + e]);
+                    if (ACT != STREAMBP_ACT_NONE) d *= slope<ACT, FAST>(to_f32(pre[r * ldp + col0 + e]));
+                    sum[e] += d;
+                    if (dZ) dZ[r * ldz + col0 + e] = from_f32<T>(d);
+                }
+    }
+    if (!partials) return;
+    // the 32 row threads of a column: four of a warp by shuffles (lanes 8 apart), then the eight warps
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 8);
+        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 16);
+    }
+    if ((threadIdx.x & 31) < 8) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) s_sum[threadIdx.x >> 5][tc * 8 + e] = sum[e];
+    }
+    __syncthreads();
+    const int c = blockIdx.x * kStrip + threadIdx.x;
+    if (threadIdx.x < kStrip && c < N) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; w++) s += s_sum[w][threadIdx.x];
+        partials[(int64_t)blockIdx.y * N + c] = s;
+    }
+}
+
+__global__ void __launch_bounds__(256) epilogue_sum_kernel(const float *partials, int splits, int N, float *dbias, int accumulate) {
+    pdl_enter();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= N) return;
+    float s = 0.f;
+    for (int i = 0; i < splits; i++) s += partials[(int64_t)i * N + c];
+    dbias[c] = accumulate ? dbias[c] + s : s;
+}
+
+template <typename T, int ACT>
+int launch(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int64_t N, T *dZ, int64_t ldz, float *dbias,
+           bool accumulate, float *partials, cudaStream_t st) {
+    auto rows16 = [](const void *q, int64_t ld) {
+        return !q || ((reinterpret_cast<uintptr_t>(q) & 15u) == 0 && (ld * (int64_t)sizeof(T)) % 16 == 0);
+    };
+    const int splits = gemm_epilogue_splits(M, N);
+    const int64_t per = (M + splits - 1) / splits;
+    const dim3 grid((unsigned)((N + kStrip - 1) / kStrip), (unsigned)splits);
+    float *sums = dbias ? partials : nullptr;
+    if (rows16(dC, ldd) && rows16(ACT != STREAMBP_ACT_NONE ? pre : nullptr, ldp) && rows16(dZ, ldz))
+        SBP_LAUNCH((epilogue_bwd_kernel<T, ACT, true>), grid, 256, 0, st, dC, ldd, pre, ldp, M, (int)N, per, dZ, ldz, sums);
+    else
+        SBP_LAUNCH((epilogue_bwd_kernel<T, ACT, false>), grid, 256, 0, st, dC, ldd, pre, ldp, M, (int)N, per, dZ, ldz, sums);
+    if (dbias)
+        SBP_LAUNCH(epilogue_sum_kernel, (unsigned)((N + 255) / 256), 256, 0, st, partials, splits, (int)N, dbias, accumulate ? 1 : 0);
+    return STREAMBP_OK;
+}
+
+}  // namespace
+
+// Row splits: about six blocks for each of the 148 SMs, at least 32 rows each.  A function of the sizes alone, so that
+// the workspace query needs no GPU and the order of the sums is the same everywhere.
+int gemm_epilogue_splits(int64_t M, int64_t N) {
+    const int64_t strips = (N + kStrip - 1) / kStrip, rows = (M + kRowsAtOnce - 1) / kRowsAtOnce;
+    int64_t s = (148 * 6 + strips - 1) / strips;
+    if (s > rows) s = rows;
+    return s < 1 ? 1 : (int)s;
+}
+
+template <typename T>
+int gemm_epilogue_bwd(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int act, int64_t M, int64_t N, T *dZ, int64_t ldz,
+                      float *dbias, bool accumulate, float *partials, cudaStream_t st) {
+    switch (act) {
+        case STREAMBP_ACT_NONE: return launch<T, STREAMBP_ACT_NONE>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
+        case STREAMBP_ACT_RELU: return launch<T, STREAMBP_ACT_RELU>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
+        case STREAMBP_ACT_GELU: return launch<T, STREAMBP_ACT_GELU>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
+        case STREAMBP_ACT_GELU_TANH:
+            return launch<T, STREAMBP_ACT_GELU_TANH>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
+        case STREAMBP_ACT_SILU: return launch<T, STREAMBP_ACT_SILU>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
+        default: return STREAMBP_E_SHAPE;
+    }
+}
+template int gemm_epilogue_bwd<float>(const float *, int64_t, const float *, int64_t, int, int64_t, int64_t, float *, int64_t,
+                                      float *, bool, float *, cudaStream_t);
+template int gemm_epilogue_bwd<bf16>(const bf16 *, int64_t, const bf16 *, int64_t, int, int64_t, int64_t, bf16 *, int64_t,
+                                     float *, bool, float *, cudaStream_t);
+
+}  // namespace sbp

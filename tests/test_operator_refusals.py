@@ -75,3 +75,35 @@ def test_plan_refuses_host_tensors():
         B.AdamWPlan([t])
     with pytest.raises(ValueError):
         B.AdamWPlan([])
+
+
+def epilogue(lib, **kw):
+    a = dict(A=P, lda=64, W=P, ldw=64, M=16, N=32, K=64, bias=P, act=3, residual=P + 0x1000, ldr=32, C=P, ldc=32, pre=P + 0x2000,
+             ldp=32, dtype=B.STREAMBP_BF16)
+    a.update(kw)
+    return lib.streambp_gemm_epilogue(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(A=None), B.E_NULL), (dict(W=None), B.E_NULL), (dict(C=None), B.E_NULL), (dict(dtype=2), B.E_DTYPE),
+    (dict(M=0), B.E_SHAPE), (dict(N=0), B.E_SHAPE), (dict(K=0), B.E_SHAPE), (dict(M=1 << 31), B.E_SHAPE),
+    (dict(act=-1), B.E_SHAPE), (dict(act=5), B.E_SHAPE), (dict(lda=63), B.E_SHAPE), (dict(ldw=1), B.E_SHAPE),
+    (dict(ldc=31), B.E_SHAPE), (dict(ldr=31), B.E_SHAPE), (dict(ldp=31), B.E_SHAPE), (dict(A=P + 1), B.E_ALIGN),
+    (dict(C=P + 1), B.E_ALIGN), (dict(bias=P + 1), B.E_ALIGN), (dict(residual=P + 1), B.E_ALIGN), (dict(pre=P + 3), B.E_ALIGN),
+    (dict(dtype=B.STREAMBP_F32, W=P + 2), B.E_ALIGN), (dict(residual=P, ldr=40), B.E_SHAPE), (dict(pre=P), B.E_SHAPE),
+    (dict(pre=P + 0x1000), B.E_SHAPE),
+])
+def test_gemm_epilogue_refusals(lib, kw, status):
+    assert epilogue(lib, **kw) == status
+
+
+def test_gemm_epilogue_backward_refusals(lib):
+    need = lib.streambp_gemm_epilogue_workspace_bytes(16, 32)
+    assert need > 0 and lib.streambp_gemm_epilogue_workspace_bytes(0, 32) == 0 and lib.streambp_gemm_epilogue_workspace_bytes(16, -1) == 0
+    def call(dC=P, ldd=32, pre=P + 0x1000, ldp=32, act=4, M=16, N=32, dZ=P + 0x2000, ldz=32, dbias=P, acc=0, dtype=1, ws=P, size=need):
+        return lib.streambp_gemm_epilogue_backward(dC, ldd, pre, ldp, act, M, N, dZ, ldz, dbias, acc, dtype, ws, size, None)
+    assert call(dC=None) == B.E_NULL and call(pre=None) == B.E_NULL and call(dZ=None, dbias=None) == B.E_NULL and call(ws=None) == B.E_NULL
+    assert call(dtype=3) == B.E_DTYPE and call(act=9) == B.E_SHAPE and call(M=0) == B.E_SHAPE and call(N=0) == B.E_SHAPE
+    assert call(ldd=31) == B.E_SHAPE and call(ldp=31) == B.E_SHAPE and call(ldz=31) == B.E_SHAPE
+    assert call(dC=P + 1) == B.E_ALIGN and call(dZ=P + 1) == B.E_ALIGN and call(dbias=P + 2) == B.E_ALIGN and call(ws=P + 64) == B.E_ALIGN
+    assert call(size=need - 1) == B.E_WORKSPACE and call(dZ=P, ldz=40) == B.E_SHAPE and call(dZ=P + 0x1000, ldz=40) == B.E_SHAPE
