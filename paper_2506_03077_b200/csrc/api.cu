@@ -616,9 +616,10 @@ int streambp_last_device_status(void *workspace, void *cuda_stream) {
     WsHeader h;
     if (!cuda_ok(cudaMemcpyAsync(&h, workspace, sizeof(h), cudaMemcpyDeviceToHost, st))) return STREAMBP_E_CUDA;
     if (!cuda_ok(cudaStreamSynchronize(st))) return STREAMBP_E_CUDA;
-    const int f1 = gemm_tc_take_fault(), f2 = attention_tc_take_fault(), f3 = wait_probe_take_fault();
-    if (f1 < 0 || f2 < 0 || f3 < 0) return STREAMBP_E_CUDA;
-    if (f1 > 0 || f2 > 0 || f3 > 0) return STREAMBP_E_DEVICE_TIMEOUT;
+    const int f1 = gemm_tc_take_fault(), f2 = attention_tc_take_fault(), f3 = wait_probe_take_fault(),
+              f4 = gemm_epilogue_take_fault();
+    if (f1 < 0 || f2 < 0 || f3 < 0 || f4 < 0) return STREAMBP_E_CUDA;
+    if (f1 > 0 || f2 > 0 || f3 > 0 || f4 > 0) return STREAMBP_E_DEVICE_TIMEOUT;
     return h.status;
 }
 

@@ -337,6 +337,7 @@ struct GemmEpilogue {
 };
 bool gemm_tc_epilogue_supported(const GemmEpilogue<bf16> &g);
 int gemm_tc_epilogue(const GemmEpilogue<bf16> &g, cudaStream_t st);
+int gemm_epilogue_take_fault();
 template <typename T>
 int gemm_simt_epilogue(const GemmEpilogue<T> &g, cudaStream_t st);
 // dZ = dC * act'(pre) (dZ may be dC or pre, or nullptr where only the column sums are wanted) and, unless nullptr,

@@ -5,6 +5,8 @@
 // bf16, eight threads of one 16-byte load each) and walks its rows 32 at a time, keeping the sums of its columns in
 // registers; a grid of (strips, row splits) fills the GPU, each split leaves its sums in `partials`, and a second small
 // kernel adds the splits in their order: no atomics, the same inputs give the same bits.
+#include <type_traits>
+
 #include "activation.cuh"
 #include "sm100.cuh"
 
@@ -28,36 +30,32 @@ __global__ void __launch_bounds__(256)
     for (int e = 0; e < 8; e++) sum[e] = 0.f;
     const int cols = N - col0 >= 8 ? 8 : (N - col0 > 0 ? N - col0 : 0);
     if (VEC && cols == 8) {
-        constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;           // rows in flight per thread
-        for (int64_t r0 = first + tr; r0 < end; r0 += kRowsAtOnce * kAhead) {
-            Vec<T> d[kAhead][8 / Vec<T>::N], z[kAhead][8 / Vec<T>::N];
+        constexpr int kAhead = sizeof(T) == 2 ? 4 : 2, V = 8 / Vec<T>::N;           // rows in flight per thread
+        auto some = [&](int64_t r0, auto count) {
+            constexpr int n = decltype(count)::value;
+            Vec<T> d[n][V], z[n][V];
 #pragma unroll
-            for (int a = 0; a < kAhead; a++) {
-                const int64_t r = r0 + a * kRowsAtOnce;
-                if (r < end) {
+            for (int a = 0; a < n; a++)
 #pragma unroll
-                    for (int v = 0; v < 8 / Vec<T>::N; v++) {
-                        d[a][v].load(dC + r * ldd + col0 + v * Vec<T>::N);
-                        if (ACT != STREAMBP_ACT_NONE) z[a][v].load(pre + r * ldp + col0 + v * Vec<T>::N);
-                    }
+                for (int v = 0; v < V; v++) {
+                    d[a][v].load(dC + (r0 + a * kRowsAtOnce) * ldd + col0 + v * Vec<T>::N);
+                    if (ACT != STREAMBP_ACT_NONE) z[a][v].load(pre + (r0 + a * kRowsAtOnce) * ldp + col0 + v * Vec<T>::N);
                 }
-            }
 #pragma unroll
-            for (int a = 0; a < kAhead; a++) {
-                const int64_t r = r0 + a * kRowsAtOnce;
-                if (r < end) {
+            for (int a = 0; a < n; a++)
 #pragma unroll
-                    for (int v = 0; v < 8 / Vec<T>::N; v++) {
+                for (int v = 0; v < V; v++) {
 #pragma unroll
-                        for (int e = 0; e < Vec<T>::N; e++) {
-                            if (ACT != STREAMBP_ACT_NONE) d[a][v].v[e] *= slope<ACT, FAST>(z[a][v].v[e]);
-                            sum[v * Vec<T>::N + e] += d[a][v].v[e];
-                        }
-                        if (dZ) d[a][v].store(dZ + r * ldz + col0 + v * Vec<T>::N);
+                    for (int e = 0; e < Vec<T>::N; e++) {
+                        if (ACT != STREAMBP_ACT_NONE) d[a][v].v[e] *= slope<ACT, FAST>(z[a][v].v[e]);
+                        sum[v * Vec<T>::N + e] += d[a][v].v[e];
                     }
+                    if (dZ) d[a][v].store(dZ + (r0 + a * kRowsAtOnce) * ldz + col0 + v * Vec<T>::N);
                 }
-            }
-        }
+        };
+        int64_t r = first + tr;
+        for (; r + (kAhead - 1) * kRowsAtOnce < end; r += kAhead * kRowsAtOnce) some(r, std::integral_constant<int, kAhead>());
+        for (; r < end; r += kRowsAtOnce) some(r, std::integral_constant<int, 1>());
     } else {
         for (int64_t r = first + tr; r < end; r += kRowsAtOnce)
             for (int e = 0; e < 8; e++)

@@ -31,7 +31,6 @@
 #include <cstdlib>
 #include <cstring>
 
-#include "activation.cuh"
 #include "sm100.cuh"
 
 namespace sbp {
@@ -79,7 +78,7 @@ bool tensor_maps_available() { return encode_fn() != nullptr; }
 
 // 2-D tensor map over a row-major [rows, cols] matrix with leading dimension ld (elements).
 bool make_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, uint32_t box_cols,
-                     uint32_t box_rows, bool f32) {
+                     uint32_t box_rows, bool f32, CUtensorMapSwizzle swizzle) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
@@ -87,7 +86,7 @@ bool make_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t c
     const cuuint32_t box[2] = {box_cols, box_rows};
     const cuuint32_t estr[2] = {1, 1};
     const CUresult r = fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         call_state().cuda_error = (int)r;
@@ -121,7 +120,7 @@ namespace {
 // Operand layouts, output type and accumulation are per-problem run-time flags.
 // ---------------------------------------------------------------------------------------------
 constexpr int MAX_PROBS = 4, MAX_SEGS = 8, RING = 4;
-constexpr uint32_t F_A_MN = 1u, F_B_MN = 2u, F_OUT_F32 = 4u, F_ACC = 8u, F_SWIGLU = 16u, F_ROPE = 32u, F_EPI_VEC = 64u;
+constexpr uint32_t F_A_MN = 1u, F_B_MN = 2u, F_OUT_F32 = 4u, F_ACC = 8u, F_SWIGLU = 16u, F_ROPE = 32u;
 
 struct GroupParams {
     CUtensorMap map_a[MAX_SEGS];
@@ -138,10 +137,6 @@ struct GroupParams {
     const bf16 *bias[MAX_PROBS];
     const float2 *rope[MAX_PROBS];     // F_ROPE: (cos, sin) of 64 frequencies per row of the problem
     uint32_t flags[MAX_PROBS];
-    // EPI kernels (one problem per launch): C = act(A B^T + bias) + residual, the sum before act in `pre`
-    const bf16 *residual;
-    bf16 *pre;
-    long long ldr, ldp;
     int nprob;
     int *sched;                        // {next tile, CTAs finished}, both zero at launch; or nullptr: static schedule
     const int *gate;                   // optional: the kernel returns at once when *gate == 0
@@ -400,90 +395,6 @@ __device__ __forceinline__ void epilogue_rows(const GroupParams &p, const TileRe
     }
 }
 
-// The activation epilogue of one warp: 32 rows of the tile, all BN columns (a thread owns a row, as above).  Residual
-// rows are requested before the accumulator columns are waited for; bias, activation and residual are applied to the
-// fp32 accumulator and rounded once (the kept pre-activation is rounded from the same fp32 value, it is not what the
-// activation reads).  VEC: rows of all three matrices and the bias start on 16-byte boundaries; otherwise single elements.
-// It runs beside the main loop of the next tile and is hidden by it from K of about 1024 on.
-template <int ACT, bool VEC>
-__device__ __forceinline__ void epilogue_act(const GroupParams &p, const TileRef &t, int row, uint32_t taddr) {
-    const int Nq = p.N[0];
-    const bool live = row < p.M[0];
-    const bf16 *bias = p.bias[0];
-    const bf16 *res = p.residual ? p.residual + (long long)row * p.ldr : nullptr;
-    bf16 *pre = p.pre ? p.pre + (long long)row * p.ldp : nullptr;
-    bf16 *out = reinterpret_cast<bf16 *>(p.C[0]) + (long long)row * p.ldc[0];
-#pragma unroll 1
-    for (int c = 0; c < BN / 32; c++) {
-        const int col0 = t.n0 + c * 32;
-        if (col0 >= Nq) break;                                   // uniform across the warp
-        const bool whole = VEC && col0 + 32 <= Nq;
-        uint4 rs[4];
-        if (whole && res && live) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) rs[j] = *reinterpret_cast<const uint4 *>(res + col0 + 8 * j);
-        }
-        uint32_t r[32];
-        tmem_ld32(taddr + c * 32, r);
-        if (!live) continue;
-        if (whole) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                float z[8];
-#pragma unroll
-                for (int e = 0; e < 8; e++) z[e] = __uint_as_float(r[8 * j + e]);
-                if (bias) {
-                    Vec<bf16> b;
-                    b.load(bias + col0 + 8 * j);
-#pragma unroll
-                    for (int e = 0; e < 8; e++) z[e] += b.v[e];
-                }
-                Vec<bf16> y;
-#pragma unroll
-                for (int e = 0; e < 8; e++) y.v[e] = z[e];
-                if (pre) y.store(pre + col0 + 8 * j);
-#pragma unroll
-                for (int e = 0; e < 8; e++) y.v[e] = activate<ACT, true>(z[e]);
-                if (res) {
-                    const uint32_t w[4] = {rs[j].x, rs[j].y, rs[j].z, rs[j].w};
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        y.v[2 * e] += __uint_as_float(w[e] << 16);
-                        y.v[2 * e + 1] += __uint_as_float(w[e] & 0xFFFF0000u);
-                    }
-                }
-                y.store(out + col0 + 8 * j);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 32; e++) {
-                const int col = col0 + e;
-                if (col < Nq) {
-                    float z = __uint_as_float(r[e]);
-                    if (bias) z += __bfloat162float(bias[col]);
-                    if (pre) pre[col] = __float2bfloat16_rn(z);
-                    float y = activate<ACT, true>(z);
-                    if (res) y += __bfloat162float(res[col]);
-                    out[col] = __float2bfloat16_rn(y);
-                }
-            }
-        }
-    }
-}
-template <int ACT>
-__device__ __forceinline__ void epilogue_act_any(const GroupParams &p, const TileRef &t, int row, uint32_t taddr) {
-    if (p.flags[0] & F_EPI_VEC) epilogue_act<ACT, true>(p, t, row, taddr);
-    else epilogue_act<ACT, false>(p, t, row, taddr);
-}
-// EPI: the kernel's only epilogue is the one above (the other kernels do not carry its code)
-template <int EPI>
-__device__ __forceinline__ void epilogue_of(const GroupParams &p, const TileRef &t, int m_base, int quarter, int lane,
-                                            uint32_t acc, uint32_t epi, uint32_t &staged) {
-    if constexpr (EPI < 0) epilogue_rows(p, t, m_base, quarter, lane, acc, epi, staged);
-    else epilogue_act_any<EPI>(p, t, m_base + quarter * 32 + lane, acc + ((uint32_t)(quarter * 32) << 16));
-}
-
-template <int EPI>
 __global__ void __launch_bounds__(NUM_THREADS, 1) gemm_group_kernel(const __grid_constant__ GroupParams p) {
     pdl_enter();
     extern __shared__ uint8_t smem_raw[];
@@ -607,7 +518,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1) gemm_group_kernel(const __grid
             local++;
             if (!mbar_wait(bar_tfull + 8 * buf, use & 1u, abort_flag)) break;
             tc_fence_after();
-            epilogue_of<EPI>(p, t, t.m0, quarter, lane, tmem_base + buf * BN, epi, staged);
+            epilogue_rows(p, t, t.m0, quarter, lane, tmem_base + buf * BN, epi, staged);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_tempty + 8 * buf);
@@ -701,7 +612,6 @@ __device__ __forceinline__ bool mma_tile_pair(const GroupParams &p, const TileRe
     return true;
 }
 
-template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1)
     gemm_pair_kernel(const __grid_constant__ GroupParams p) {
     pdl_enter();
@@ -846,7 +756,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1)
             local++;
             if (!mbar_wait(bar_tfull + 8 * buf, use & 1u, abort_flag)) break;
             tc_fence_after();
-            epilogue_of<EPI>(p, t, t.m0 + BM * (int)rank, quarter, lane, tmem_base + buf * BN, epi, staged);
+            epilogue_rows(p, t, t.m0 + BM * (int)rank, quarter, lane, tmem_base + buf * BN, epi, staged);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
@@ -894,7 +804,7 @@ bool pair_kernel_available() {
     static PerDevice cache;
     return cache.get([] {
         int state = 0;
-        if (cudaFuncSetAttribute(gemm_pair_kernel<-1>, cudaFuncAttributeMaxDynamicSharedMemorySize, PAIR_SMEM_BYTES) ==
+        if (cudaFuncSetAttribute(gemm_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PAIR_SMEM_BYTES) ==
             cudaSuccess) {
             cudaLaunchConfig_t cfg;
             memset(&cfg, 0, sizeof(cfg));
@@ -902,7 +812,7 @@ bool pair_kernel_available() {
             cfg.blockDim = dim3(NUM_THREADS, 1, 1);
             cfg.dynamicSmemBytes = PAIR_SMEM_BYTES;
             int clusters = 0;
-            if (cudaOccupancyMaxActiveClusters(&clusters, gemm_pair_kernel<-1>, &cfg) == cudaSuccess && clusters >= 1)
+            if (cudaOccupancyMaxActiveClusters(&clusters, gemm_pair_kernel, &cfg) == cudaSuccess && clusters >= 1)
                 state = 1;
         }
         cudaGetLastError();
@@ -1005,83 +915,18 @@ int gemm_tc_group(const GemmProb *probs, int n, int *sched, cudaStream_t st) {
     p.gate = call_state().gate;
     static PerDevice configured;
     if (!configured.get([] {
-            return cuda_ok(cudaFuncSetAttribute(gemm_group_kernel<-1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES)) ? 1 : 0;
+            return cuda_ok(cudaFuncSetAttribute(gemm_group_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES)) ? 1 : 0;
         }))
         return STREAMBP_E_CUDA;
     if (pair) {
         const int pairs = std::max(1, sm_count() / 2);
         const int grid = 2 * (tiles < pairs ? (int)tiles : pairs);
-        SBP_LAUNCH(gemm_pair_kernel<-1>, grid, NUM_THREADS, PAIR_SMEM_BYTES, st, p);
+        SBP_LAUNCH(gemm_pair_kernel, grid, NUM_THREADS, PAIR_SMEM_BYTES, st, p);
         return STREAMBP_OK;
     }
     const int grid = tiles < sm_count() ? (int)tiles : sm_count();
-    SBP_LAUNCH(gemm_group_kernel<-1>, grid, NUM_THREADS, SMEM_BYTES, st, p);
+    SBP_LAUNCH(gemm_group_kernel, grid, NUM_THREADS, SMEM_BYTES, st, p);
     return STREAMBP_OK;
-}
-
-namespace {
-template <int ACT>
-int launch_epilogue(const GroupParams &p, int64_t tiles, bool pair, cudaStream_t st) {
-    static PerDevice configured;
-    if (!configured.get([] {
-            return cuda_ok(cudaFuncSetAttribute(gemm_pair_kernel<ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, PAIR_SMEM_BYTES)) &&
-                           cuda_ok(cudaFuncSetAttribute(gemm_group_kernel<ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES))
-                       ? 1
-                       : 0;
-        }))
-        return STREAMBP_E_CUDA;
-    if (pair) {
-        const int pairs = std::max(1, sm_count() / 2);
-        SBP_LAUNCH(gemm_pair_kernel<ACT>, 2 * (tiles < pairs ? (int)tiles : pairs), NUM_THREADS, PAIR_SMEM_BYTES, st, p);
-        return STREAMBP_OK;
-    }
-    SBP_LAUNCH(gemm_group_kernel<ACT>, tiles < sm_count() ? (int)tiles : sm_count(), NUM_THREADS, SMEM_BYTES, st, p);
-    return STREAMBP_OK;
-}
-}  // namespace
-
-bool gemm_tc_epilogue_supported(const GemmEpilogue<bf16> &g) {
-    // the output matrices are written by plain stores of any alignment: only the operands have rules
-    return gemm_tc_supported(OP_NT, g.M, g.N, g.K, g.lda, g.ldw, 8, g.A, g.W, g.A, false);
-}
-
-int gemm_tc_epilogue(const GemmEpilogue<bf16> &g, cudaStream_t st) {
-    if (!gemm_tc_epilogue_supported(g)) return STREAMBP_E_SHAPE;
-    const bool pair = pair_kernel_available();
-    GroupParams p;
-    memset(&p, 0, sizeof(p));
-    p.nprob = 1;
-    if (!make_tensor_map(&p.map_a[0], g.A, g.M, g.K, g.lda, BK, BM, false) ||
-        !make_tensor_map(&p.map_b[0], g.W, g.N, g.K, g.ldw, BK, pair ? BN / 2 : BN, false))
-        return STREAMBP_E_CUDA;
-    const int tile_m = pair ? PAIR_BM : BM;
-    p.seg_kb[0] = (int)((g.K + BK - 1) / BK);
-    p.tiles_m[0] = (int)((g.M + tile_m - 1) / tile_m);
-    p.M[0] = (int)g.M;
-    p.N[0] = (int)g.N;
-    p.C[0] = g.C;
-    p.ldc[0] = g.ldc;
-    p.bias[0] = g.bias;
-    p.residual = g.residual;
-    p.ldr = g.ldr;
-    p.pre = g.pre;
-    p.ldp = g.ldp;
-    auto rows16 = [](const void *q, int64_t ld) { return !q || ((reinterpret_cast<uintptr_t>(q) & 15u) == 0 && ld % 8 == 0); };
-    p.flags[0] = rows16(g.C, g.ldc) && rows16(g.residual, g.ldr) && rows16(g.pre, g.ldp) && rows16(g.bias, 8) ? F_EPI_VEC : 0u;
-    const int64_t tiles = (int64_t)p.tiles_m[0] * ((g.N + BN - 1) / BN);
-    if (tiles > (1ll << 30)) return STREAMBP_E_SHAPE;
-    for (int i = 1; i <= MAX_PROBS; i++) {
-        p.seg_begin[i] = 1;
-        p.tile_begin[i] = (int)tiles;
-    }
-    switch (g.act) {
-        case STREAMBP_ACT_NONE: return launch_epilogue<STREAMBP_ACT_NONE>(p, tiles, pair, st);
-        case STREAMBP_ACT_RELU: return launch_epilogue<STREAMBP_ACT_RELU>(p, tiles, pair, st);
-        case STREAMBP_ACT_GELU: return launch_epilogue<STREAMBP_ACT_GELU>(p, tiles, pair, st);
-        case STREAMBP_ACT_GELU_TANH: return launch_epilogue<STREAMBP_ACT_GELU_TANH>(p, tiles, pair, st);
-        case STREAMBP_ACT_SILU: return launch_epilogue<STREAMBP_ACT_SILU>(p, tiles, pair, st);
-        default: return STREAMBP_E_SHAPE;
-    }
 }
 
 int gemm_tc(GemmOp op, int64_t M, int64_t N, int64_t K, const bf16 *A, int64_t lda, const bf16 *B, int64_t ldb,

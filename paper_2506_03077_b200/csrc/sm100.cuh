@@ -359,9 +359,10 @@ __device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t cols)
 }
 
 // ---- host side: tensor maps ----------------------------------------------------------------------
-// 2-D tensor map over a row-major [rows, cols] matrix with leading dimension ld (elements), 128-byte swizzle.
+// 2-D tensor map over a row-major [rows, cols] matrix with leading dimension ld (elements), 128-byte swizzle unless another
+// is given.
 bool make_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, uint32_t box_cols,
-                     uint32_t box_rows, bool f32);
+                     uint32_t box_rows, bool f32, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B);
 bool tensor_maps_available();
 int sm_count();
 
