@@ -483,12 +483,12 @@ int launch_pair(EpiParams p, const GemmEpilogue<bf16> &g, cudaStream_t st) {
         return STREAMBP_E_CUDA;
     const int pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
     p.tiles_m = (int)((g.M + PM - 1) / PM);
-#ifdef FORCE_BN
-    p.bn = FORCE_BN;
-#else
-    p.bn = 256;
-#endif
-    const int64_t tiles = (int64_t)p.tiles_m * ((g.N + p.bn - 1) / p.bn);
+    // 256 columns a tile, or 224 where those need no more waves of pairs than the wider ones (each wave is then shorter:
+    // 1500 x 5325 x 4096, two waves either way: 92 us against 98; the time of a wave falls by 2-6 %, so never for more waves)
+    auto tiles_of = [&](int bn) { return (int64_t)p.tiles_m * ((g.N + bn - 1) / bn); };
+    const int64_t wide = tiles_of(256), narrow = tiles_of(224);
+    p.bn = wide > pairs && (narrow + pairs - 1) / pairs == (wide + pairs - 1) / pairs ? 224 : 256;
+    const int64_t tiles = p.bn == 256 ? wide : narrow;
     if (tiles > (1ll << 30)) return STREAMBP_E_SHAPE;
     p.tiles = (int)tiles;
     if (!make_tensor_map(&p.map_a, g.A, g.M, g.K, g.lda, BK, 128, false) ||
@@ -502,10 +502,9 @@ int launch_pair(EpiParams p, const GemmEpilogue<bf16> &g, cudaStream_t st) {
 
 template <int ACT>
 int launch_any(const EpiParams &p, const GemmEpilogue<bf16> &g, cudaStream_t st) {
-#ifndef ROWS_MAX
-#define ROWS_MAX 128
-#endif
-    if (gemm_tc_variant() == 2 && g.M > ROWS_MAX) return launch_pair<ACT>(p, g, st);
+    // one tile of up to 128 rows: 4096 x 14336 with 128 rows takes 39 us against 82 by pairs, 1 row of 4096 x 4096 14 us
+    // against 31; two tiles of 128 rows (256 x 4096 x 4096) take what one pair tile does
+    if (gemm_tc_variant() == 2 && g.M > 128) return launch_pair<ACT>(p, g, st);
     if (g.M <= 16) return launch_rows<ACT, 16>(p, g, st);
     if (g.M <= 32) return launch_rows<ACT, 32>(p, g, st);
     if (g.M <= 64) return launch_rows<ACT, 64>(p, g, st);
