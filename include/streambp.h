@@ -412,6 +412,35 @@ int streambp_attention_backward(const void *q, const void *k, const void *v, con
                                 int engine, void *cuda_stream);
 
 /*
+ * (No counterpart in the paper, whose attention sees the whole prefix.)  The partitioned attention for layers whose
+ * attention has a sliding window and a few first tokens that stay visible: query row t sees key j iff
+ *     j <= t and (t - j < window or j < sinks)
+ * (window >= 1 counts the row's own key; a window of q0 + n or more is the attention above).  Arguments, layouts, lse and
+ * the chunk (rows q0 .. q0+n-1, keys 0 .. q0+n-1) as above; head_dim 64 or 128, both on tensor cores for bf16; q0 + n <= 2^30.
+ * Only key tiles that some query sees are read, so a chunk costs what its window holds however long the prefix is; rows of
+ * k and v that no query sees may hold anything.  Values that a query tile's key tiles do hold must be finite: a hidden key
+ * has weight 0 there, and 0 times an infinity is NaN.
+ *
+ * Backward: lse and o are those of the forward call.  grad_dtype STREAMBP_F32: dq is overwritten, dk and dv [q0+n,
+ * n_kv_heads, head_dim] are overwritten (accumulate = 0) or added to (1: the key-prefix accumulators of a streamed
+ * backward).  grad_dtype STREAMBP_BF16 (bf16 storage only, accumulate = 0): all three are overwritten, rounded once from
+ * fp32 sums.  Overwritten dk and dv rows that no query sees become 0.  Every later query adds to the gradients of the
+ * sinks; their sums are formed in segments through the workspace and joined in a fixed order, so all results are
+ * reproducible bit by bit.  engine: 0 automatic, 1 CUDA cores, 2 tensor cores (bf16); the forward also takes 3 / 4 =
+ * tensor cores with one / two 128-query tiles per CTA.
+ */
+int streambp_attention_window_forward(const void *q, const void *k, const void *v, int64_t n, int64_t q0,
+                                      int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                      int64_t window, int64_t sinks, void *o, float *lse, int engine, void *cuda_stream);
+size_t streambp_attention_window_workspace_bytes(int64_t n, int64_t q0, int32_t n_q_heads, int32_t n_kv_heads,
+                                                 int32_t head_dim, int64_t window, int64_t sinks);
+int streambp_attention_window_backward(const void *q, const void *k, const void *v, const void *o, const void *d_o,
+                                       const float *lse, int64_t n, int64_t q0, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int32_t dtype, int64_t window, int64_t sinks, int32_t grad_dtype,
+                                       int accumulate, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
+                                       int engine, void *cuda_stream);
+
+/*
  * (No counterpart in the paper.)  streambp_attention_backward for callers that have no device buffer
  * to offer for `delta` and cannot obtain one when they call: host code in a latency-critical loop
  * where cudaMalloc / cudaFree would stall the whole device, a plug-in whose host framework already owns

@@ -41,7 +41,8 @@ EXPORTS = (
     "streambp_lmhead_rl_backward_grouped",
     "streambp_adamw_step", "streambp_grad_norm_workspace_bytes", "streambp_grad_norm", "streambp_mx8_encode",
     "streambp_mx8_decode", "streambp_gemm_epilogue", "streambp_gemm_epilogue_workspace_bytes",
-    "streambp_gemm_epilogue_backward",
+    "streambp_gemm_epilogue_backward", "streambp_attention_window_forward", "streambp_attention_window_workspace_bytes",
+    "streambp_attention_window_backward",
 )
 
 
@@ -185,6 +186,13 @@ def lib() -> C.CDLL:
     L.streambp_gemm_epilogue_workspace_bytes.argtypes = [i64, i64]
     L.streambp_gemm_epilogue_backward.restype = C.c_int
     L.streambp_gemm_epilogue_backward.argtypes = [vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, C.c_int, i32, vp, sz, vp]
+    L.streambp_attention_window_forward.restype = C.c_int
+    L.streambp_attention_window_forward.argtypes = [vp, vp, vp, i64, i64, i32, i32, i32, i32, i64, i64, vp, vp, C.c_int, vp]
+    L.streambp_attention_window_workspace_bytes.restype = sz
+    L.streambp_attention_window_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i64, i64]
+    L.streambp_attention_window_backward.restype = C.c_int
+    L.streambp_attention_window_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i32, i32, i32, i32, i64, i64, i32,
+                                                     C.c_int, vp, vp, vp, vp, sz, C.c_int, vp]
     L.streambp_adamw_step.restype = C.c_int
     L.streambp_adamw_step.argtypes = [C.POINTER(AdamWCfgC), C.POINTER(AdamWTensorC), i32, vp, vp, vp]
     L.streambp_grad_norm_workspace_bytes.restype = sz
@@ -683,6 +691,57 @@ def attention_backward_static(q, k, v, o, d_o, lse, q0: int, dq, dk, dv, engine:
                                                   engine, _stream_ptr(stream))
     if check:
         _check(st, "streambp_attention_backward_static")
+    return st
+
+
+def _window_args(what: str, q, k, v, q0: int, others) -> tuple:
+    """Checks of a windowed call: q [n, Hq, dh], k and v [q0 + n, Hkv, dh], `others` (tensor, shape, dtypes) each."""
+    _want(q.dim() == 3 and k.dim() == 3 and q0 >= 0, what, "q [n, Hq, dh] and k [q0 + n, Hkv, dh], q0 >= 0")
+    n, Hq, dh = q.shape
+    _want(tuple(k.shape) == (q0 + n, k.shape[1], dh) and k.shape == v.shape, what, f"k and v are [{q0 + n}, Hkv, {dh}]")
+    _want(k.dtype == q.dtype and v.dtype == q.dtype, what, "q, k and v share a type")
+    for t, shape, dtypes in others:
+        _want(tuple(t.shape) == shape and t.dtype in dtypes, what, f"expected {shape} {dtypes}, got {tuple(t.shape)} {t.dtype}")
+    return n, Hq, k.shape[1], dh
+
+
+def attention_window_forward(q, k, v, q0: int, window: int, sinks: int, o, lse, engine: int = 0, stream=None,
+                             check: bool = True) -> int:
+    """streambp_attention_window_forward; q, o: [n, Hq, dh], k, v: [q0+n, Hkv, dh], lse: [Hq, n] fp32."""
+    what, Hq_n = "attention_window_forward", (q.shape[1], q.shape[0])
+    n, Hq, Hkv, dh = _window_args(what, q, k, v, q0, ((o, tuple(q.shape), (q.dtype,)), (lse, Hq_n, (torch.float32,))))
+    dev = _shared_device(what, q, k, v, o, lse)
+    with _Launch(what, dev, stream) as s:
+        st = lib().streambp_attention_window_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), n, q0, Hq, Hkv, dh,
+                                                     _dtype_code(q.dtype), window, sinks, o.data_ptr(), lse.data_ptr(), engine, s)
+    if check:
+        _check(st, "streambp_attention_window_forward")
+    return st
+
+
+def attention_window_workspace_bytes(n: int, q0: int, n_q_heads: int, n_kv_heads: int, head_dim: int, window: int,
+                                     sinks: int) -> int:
+    return int(lib().streambp_attention_window_workspace_bytes(n, q0, n_q_heads, n_kv_heads, head_dim, window, sinks))
+
+
+def attention_window_backward(q, k, v, o, d_o, lse, q0: int, window: int, sinks: int, dq, dk, dv, workspace,
+                              accumulate: bool = False, engine: int = 0, stream=None, check: bool = True) -> int:
+    """streambp_attention_window_backward; dq, dk, dv share a type (fp32, or bf16 for bf16 storage): overwritten, or with
+    accumulate=True (fp32) dk and dv are added to."""
+    what, kv = "attention_window_backward", tuple(k.shape)
+    grads = (dq.dtype,)
+    _want(dq.dtype in (torch.float32, torch.bfloat16), what, "gradients are fp32 or bf16")
+    n, Hq, Hkv, dh = _window_args(what, q, k, v, q0, (
+        (o, tuple(q.shape), (q.dtype,)), (d_o, tuple(q.shape), (q.dtype,)), (lse, (q.shape[1], q.shape[0]), (torch.float32,)),
+        (dq, tuple(q.shape), grads), (dk, kv, grads), (dv, kv, grads)))
+    dev = _shared_device(what, q, k, v, o, d_o, lse, dq, dk, dv, workspace)
+    with _Launch(what, dev, stream) as s:
+        st = lib().streambp_attention_window_backward(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), d_o.data_ptr(), lse.data_ptr(), n, q0, Hq, Hkv, dh,
+            _dtype_code(q.dtype), window, sinks, _dtype_code(dq.dtype), 1 if accumulate else 0, dq.data_ptr(), dk.data_ptr(),
+            dv.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), engine, s)
+    if check:
+        _check(st, "streambp_attention_window_backward")
     return st
 
 

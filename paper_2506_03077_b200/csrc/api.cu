@@ -10,6 +10,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "common.cuh"
+#include "window.cuh"
 
 namespace sbp {
 
@@ -345,6 +346,35 @@ int run_epilogue(const void *A, int64_t lda, const void *W, int64_t ldw, int64_t
     }
     return gemm_simt_epilogue<T>(g, st);
 }
+// sizes of a windowed call; window and sinks beyond the keys act like the number of keys
+int window_shape(int64_t n, int64_t q0, int32_t Hq, int32_t Hkv, int32_t dh, int64_t window, int64_t sinks, WindowShape *w) {
+    if (n < 1 || q0 < 0 || n > (1 << 30) || q0 > (1 << 30) || q0 + n > (1 << 30) || Hq < 1 || Hkv < 1 || Hq > 65535 || Hq % Hkv ||
+        (dh != 64 && dh != 128) || window < 1 || sinks < 0)
+        return STREAMBP_E_SHAPE;
+    const int64_t kv = q0 + n;
+    *w = WindowShape{(int)n, (int)q0, Hq, Hkv, (int)(window < kv ? window : kv), (int)(sinks < kv ? sinks : kv)};
+    if (w->window == kv || w->sinks == kv) {      // every earlier key is visible: one window over all of them
+        w->window = (int)kv;
+        w->sinks = 0;
+    }
+    return STREAMBP_OK;
+}
+// scratch of the windowed backward: delta, then the sums of the sink segments (the larger of the two engines' needs)
+struct WindowScratch { float *delta, *part; };
+template <int TILE_>
+size_t window_part_floats(const WindowShape &w, int dh) {
+    const KeyWork<TILE_> k = key_work<TILE_>(w);
+    return k.segs > 1 ? (size_t)k.st * k.segs * w.Hkv * 2 * (w.sinks < TILE_ ? w.sinks : TILE_) * dh : 0;
+}
+size_t window_scratch(const WindowShape &w, int dh, void *base, WindowScratch *out) {
+    Arena a(base);
+    a.take_bytes(kHeaderBytes);
+    out->delta = a.take<float>((size_t)w.Hq * w.n);
+    const size_t x = window_part_floats<128>(w, dh), y = window_part_floats<32>(w, dh);
+    out->part = a.take<float>(x > y ? x : y);
+    return a.size();
+}
+
 // weights with the bias pointers dropped when the configuration has no bias
 streambp_layer_weights effective(const streambp_layer_cfg *c, const streambp_layer_weights *w) {
     streambp_layer_weights e = *w;
@@ -617,9 +647,9 @@ int streambp_last_device_status(void *workspace, void *cuda_stream) {
     if (!cuda_ok(cudaMemcpyAsync(&h, workspace, sizeof(h), cudaMemcpyDeviceToHost, st))) return STREAMBP_E_CUDA;
     if (!cuda_ok(cudaStreamSynchronize(st))) return STREAMBP_E_CUDA;
     const int f1 = gemm_tc_take_fault(), f2 = attention_tc_take_fault(), f3 = wait_probe_take_fault(),
-              f4 = gemm_epilogue_take_fault();
-    if (f1 < 0 || f2 < 0 || f3 < 0 || f4 < 0) return STREAMBP_E_CUDA;
-    if (f1 > 0 || f2 > 0 || f3 > 0 || f4 > 0) return STREAMBP_E_DEVICE_TIMEOUT;
+              f4 = gemm_epilogue_take_fault(), f5 = attention_window_take_fault();
+    if (f1 < 0 || f2 < 0 || f3 < 0 || f4 < 0 || f5 < 0) return STREAMBP_E_CUDA;
+    if (f1 > 0 || f2 > 0 || f3 > 0 || f4 > 0 || f5 > 0) return STREAMBP_E_DEVICE_TIMEOUT;
     return h.status;
 }
 
@@ -693,6 +723,84 @@ int streambp_attention_backward(const void *q, const void *k, const void *v, con
     if (engine < 0 || (engine > 2 && engine != 5)) return STREAMBP_E_SHAPE;
     return attn_bwd<bf16>((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o, lse, n,
                           q0, n_q_heads, n_kv_heads, head_dim, delta, dq, dk, dv, st, engine);
+}
+
+int streambp_attention_window_forward(const void *q, const void *k, const void *v, int64_t n, int64_t q0, int32_t n_q_heads,
+                                      int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int64_t window, int64_t sinks,
+                                      void *o, float *lse, int engine, void *cuda_stream) {
+    if (!q || !k || !v || !o || !lse) return STREAMBP_E_NULL;
+    if (dtype != STREAMBP_F32 && dtype != STREAMBP_BF16) return STREAMBP_E_DTYPE;
+    WindowShape w;
+    SBP_TRY(window_shape(n, q0, n_q_heads, n_kv_heads, head_dim, window, sinks, &w));
+    if (engine < 0 || engine > 4) return STREAMBP_E_SHAPE;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || !aligned(lse, 4)) return STREAMBP_E_ALIGN;
+    if (dtype == STREAMBP_F32 && engine >= 2) return STREAMBP_E_DTYPE;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    call_state().cuda_error = 0;
+    call_state().launches = 0;
+    if (dtype == STREAMBP_F32)
+        return attention_window_fwd_simt<float>((const float *)q, (const float *)k, (const float *)v, w, head_dim, (float *)o, lse, st);
+    const bool tc = attention_window_tc_available();
+    if (engine >= 2 && !tc) return STREAMBP_E_SHAPE;
+    if (engine != 1 && tc)
+        return attention_window_fwd_tc((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, w, head_dim, (bf16 *)o, lse, st,
+                                       engine == 3 ? 1 : (engine == 4 ? 2 : 0));
+    return attention_window_fwd_simt<bf16>((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, w, head_dim, (bf16 *)o, lse, st);
+}
+
+size_t streambp_attention_window_workspace_bytes(int64_t n, int64_t q0, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                 int64_t window, int64_t sinks) {
+    WindowShape w;
+    WindowScratch s;
+    if (window_shape(n, q0, n_q_heads, n_kv_heads, head_dim, window, sinks, &w) != STREAMBP_OK) return 0;
+    return window_scratch(w, head_dim, nullptr, &s);
+}
+
+int streambp_attention_window_backward(const void *q, const void *k, const void *v, const void *o, const void *d_o,
+                                       const float *lse, int64_t n, int64_t q0, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int32_t dtype, int64_t window, int64_t sinks, int32_t grad_dtype,
+                                       int accumulate, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
+                                       int engine, void *cuda_stream) {
+    if (!q || !k || !v || !o || !d_o || !lse || !dq || !dk || !dv || !workspace) return STREAMBP_E_NULL;
+    if ((dtype != STREAMBP_F32 && dtype != STREAMBP_BF16) || (grad_dtype != STREAMBP_F32 && grad_dtype != STREAMBP_BF16) ||
+        (grad_dtype == STREAMBP_BF16 && (dtype != STREAMBP_BF16 || accumulate)))
+        return STREAMBP_E_DTYPE;
+    WindowShape w;
+    SBP_TRY(window_shape(n, q0, n_q_heads, n_kv_heads, head_dim, window, sinks, &w));
+    if (engine < 0 || engine > 2) return STREAMBP_E_SHAPE;
+    if (!attention_bwd_aligned(q, k, v, o, d_o, lse, nullptr, dq, dk, dv) || !aligned(workspace, 256)) return STREAMBP_E_ALIGN;
+    if (dtype == STREAMBP_F32 && engine == 2) return STREAMBP_E_DTYPE;
+    WindowScratch s;
+    if (workspace_bytes < window_scratch(w, head_dim, workspace, &s)) return STREAMBP_E_WORKSPACE;
+    const bool tc = dtype == STREAMBP_BF16 && engine != 1 && attention_window_tc_available();
+    if (engine == 2 && !tc) return STREAMBP_E_SHAPE;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    call_state().cuda_error = 0;
+    call_state().launches = 0;
+    WsHeader *hdr = static_cast<WsHeader *>(workspace);
+    const int mode = grad_dtype == STREAMBP_BF16 ? GRAD_BF16_SET : (accumulate ? GRAD_F32_ADD : GRAD_F32_SET);
+    // keys that no query of the chunk sees have no owner among the key tiles: their gradients are zero
+    const int tile = tc ? 128 : 32;
+    const int64_t unseen = tc ? (int64_t)key_work<128>(w).lo * 128 : (int64_t)key_work<32>(w).lo * 32;
+    if (mode != GRAD_F32_ADD && unseen > 0) {
+        const size_t bytes = (size_t)unseen * n_kv_heads * head_dim * (grad_dtype == STREAMBP_BF16 ? 2 : 4);
+        SBP_TRY(fill_zero(dk, bytes, st));
+        SBP_TRY(fill_zero(dv, bytes, st));
+    }
+    int rc;
+    if (tc)
+        rc = attention_window_bwd_tc((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o, lse, w,
+                                     head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
+    else if (dtype == STREAMBP_BF16)
+        rc = attention_window_bwd_simt<bf16>((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o,
+                                             lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
+    else
+        rc = attention_window_bwd_simt<float>((const float *)q, (const float *)k, (const float *)v, (const float *)o,
+                                              (const float *)d_o, lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
+    SBP_TRY(rc);
+    const int segs = tc ? key_work<128>(w).segs : key_work<32>(w).segs;
+    if (segs > 1) return attention_window_join(s.part, tile, segs, w, head_dim, mode, dk, dv, st);
+    return STREAMBP_OK;
 }
 
 int streambp_product_kernel(void) { return gemm_tc_variant(); }
@@ -866,9 +974,9 @@ int streambp_gemm_epilogue_backward(const void *dC, int64_t ldd, const void *pre
     call_state().launches = 0;
     if (dtype == STREAMBP_F32)
         return gemm_epilogue_bwd<float>((const float *)dC, ldd, (const float *)pre, ldp, activation, M, N, (float *)dZ, ldz,
-                                        dbias, accumulate != 0, partials, st);
+                                        dbias, accumulate != 0, partials, static_cast<WsHeader *>(workspace), st);
     return gemm_epilogue_bwd<bf16>((const bf16 *)dC, ldd, (const bf16 *)pre, ldp, activation, M, N, (bf16 *)dZ, ldz, dbias,
-                                   accumulate != 0, partials, st);
+                                   accumulate != 0, partials, static_cast<WsHeader *>(workspace), st);
 }
 
 int streambp_gemm_swiglu(const void *A, int64_t lda, const void *w_gate, const void *w_up, int64_t ldb, int64_t M,

@@ -1,0 +1,969 @@
+// Attention with a sliding window and sink keys on tcgen05 tensor cores (bf16 operands, head_dim 64 or 128): the queries
+// of one chunk against the key tiles their window reaches and the tiles that hold sinks; nothing else is loaded.
+//
+// Forward (attn_window_fwd_kernel): a CTA owns TEAMS adjacent 128-query tiles of one head.
+//   warp 0      : TMA producer -- the query tiles once, then K and V tiles of 128 keys through rings
+//   warp 1      : MMA issuer (warp-uniform issue) -- per key tile and team S = Q K^T into tensor memory when the team has
+//                 handed over its previous P, then O += P V with P read from tensor memory (packed over the columns of S:
+//                 the product that reads P is queued before the one that overwrites S, one thread's MMAs run in order)
+//   other warps : softmax, four per team -- a thread owns a query row: 128 scores in registers, row maximum and sum private;
+//                 the running output is rescaled only when a row's maximum grows by more than 2^8 (exact: the final
+//                 division uses the same reference)
+// A row may see nothing of the first tiles of its CTA's list: its maximum stays -infinity and it adds exact zeros until it
+// sees a key.  Every query sees its own key, so no row ends empty.
+//
+// Backward (attn_window_bwd_kernel): two CTA roles in one grid, both deterministic (no floating-point atomics).
+//   dK/dV: one CTA per (key tile, KV head) loops over the query heads of the group and the query tiles that see the tile;
+//          a sink tile, which every later query sees, is cut into segments of query tiles that are joined in order by
+//          window_join_kernel (fp32 sums in the workspace, only the sinks' rows)
+//   dQ   : one CTA per (query tile, head) loops over the key tiles of its span
+// The pipelines of both are those of the causal backward (attention_tc.cu): softmax work split in time (P for dV first,
+// then dS), packed operands in tensor memory, every product a full tile.
+//
+// All mbarrier waits are bounded (sm100.cuh).
+#include <cstring>
+
+#include "sm100.cuh"
+#include "window.cuh"
+
+namespace sbp {
+namespace {
+
+constexpr int TILE = 128;                 // queries per team, keys per tile
+constexpr int SUB_BYTES = TILE * 64 * 2;  // one [128 rows][64 columns] swizzled sub-tile
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Descriptor steps of a [128 rows][DH] tile stored as 64-column sub-tiles: K-major (contraction along the columns, 16 a
+// step) and MN-major (contraction along the rows, 16 a step).
+__device__ __forceinline__ uint32_t klo(uint32_t tile) { return desc_lo(tile, 16); }
+__host__ __device__ constexpr uint32_t kstep(int kk) { return (uint32_t)((kk >> 2) * (SUB_BYTES >> 4) + (kk & 3) * 2); }
+__device__ __forceinline__ uint32_t mnlo(uint32_t tile) { return desc_lo(tile, SUB_BYTES); }
+__host__ __device__ constexpr uint32_t mnstep(int kk) { return (uint32_t)(kk * 128); }
+
+template <int DH>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int head, int row) {
+#pragma unroll
+    for (int c = 0; c < DH / 64; c++) tma_load_2d(dst + c * SUB_BYTES, map, bar, head * DH + c * 64, row);
+}
+
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&h);
+}
+// bits [0, n) of 32, n clamped
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
+// Which of the keys k0 + base .. + 31 the query row sees, as bits.
+__device__ __forceinline__ uint32_t visible_keys(const WindowShape &w, int row, int k0, int base) {
+    const int at = k0 + base;
+    return below(row + 1 - at) & (~below(row - w.window + 1 - at) | below(w.sinks - at));
+}
+// Which of the query rows q0 + base .. + 31 see the key, as bits.
+__device__ __forceinline__ uint32_t visible_rows(const WindowShape &w, int key, int q0, int base) {
+    const int at = q0 + base;
+    const uint32_t behind = ~below(key - at);
+    return key < w.sinks ? behind : behind & below(key + w.window - at);
+}
+// Whether a (query tile, key tile) pair holds hidden pairs: the diagonal or the window's far edge crosses it.
+__device__ __forceinline__ bool mixed(const WindowShape &w, int q0, int k0) {
+    return k0 + TILE - 1 > q0 || (q0 + TILE - 1 - k0 >= w.window && k0 + TILE > w.sinks);
+}
+
+__device__ __forceinline__ void leave(volatile int *abort_flag) {
+    if (*abort_flag) {   // give copies that are still in flight time to land before shared memory is released
+        const unsigned long long t0 = global_timer();
+        while (global_timer() - t0 < 200000ull) { }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------------------------------------------
+struct FwdParams {
+    WindowShape w;
+    bf16 *o;            // [n, Hq, DH]
+    float *lse;         // [Hq, n]
+    float scale_log2;   // log2(e) / sqrt(head_dim)
+};
+
+template <int DH, int TEAMS, int ST> struct Fwd {       // ST: stages of the K and of the V ring
+    static constexpr int kTile = TILE * DH * 2;
+    static constexpr int kThreads = 64 + 128 * TEAMS;
+    static constexpr int kSmem = (TEAMS + 2 * ST) * kTile + 1024 + 256;
+    static constexpr uint32_t kCols = TEAMS == 2 ? 512 : 256;
+    static constexpr int kBlocks = TEAMS == 1 ? 2 : 1;
+};
+
+template <int DH, int TEAMS, int ST>
+__global__ void __launch_bounds__(Fwd<DH, TEAMS, ST>::kThreads, Fwd<DH, TEAMS, ST>::kBlocks)
+    attn_window_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                           const __grid_constant__ CUtensorMap map_v, const FwdParams p) {
+    pdl_enter();
+    typedef Fwd<DH, TEAMS, ST> F;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    const uint32_t sQ = base, sK = sQ + TEAMS * F::kTile, sV = sK + ST * F::kTile;
+    uint8_t *aux = smem_raw + (base - raw) + (TEAMS + 2 * ST) * F::kTile;
+    const uint32_t bars = smem_u32(aux);
+    const uint32_t q_full = bars, k_full = bars + 8, k_empty = k_full + 8 * ST, v_full = k_empty + 8 * ST,
+                   v_empty = v_full + 8 * ST, s_full = v_empty + 8 * ST, p_full = s_full + 16, o_done = p_full + 16;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(aux + 192);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(aux + 200);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int h = blockIdx.x, g = h / (p.w.Hq / p.w.Hkv);
+    const int qt0 = (int)(gridDim.y - 1 - blockIdx.y) * TEAMS * TILE;     // the longest spans are dispatched first
+    // rows of team x (absolute): first[x] .. last[x], none if last < first
+    int first[TEAMS], last[TEAMS];
+#pragma unroll
+    for (int x = 0; x < TEAMS; x++) {
+        const int r = qt0 + x * TILE, rows = p.w.n - r < TILE ? p.w.n - r : TILE;
+        first[x] = p.w.q0 + r;
+        last[x] = rows > 0 ? first[x] + rows - 1 : first[x] - 1;
+    }
+    const int last_all = TEAMS == 2 && last[TEAMS - 1] >= first[TEAMS - 1] ? last[TEAMS - 1] : last[0];
+    const KeySpan span = key_span<TILE>(p.w, first[0], last_all);
+    const int count = span.count();
+    auto active = [&](int x, int kt) { return TEAMS == 1 || (last[x] >= first[x] && sees<TILE>(p.w, kt, first[x], last[x])); };
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        for (int s = 0; s < ST; s++) {
+            mbar_init(k_full + 8 * s, 1);
+            mbar_init(k_empty + 8 * s, 1);
+            mbar_init(v_full + 8 * s, 1);
+            mbar_init(v_empty + 8 * s, 1);
+        }
+        for (int x = 0; x < 2; x++) {
+            mbar_init(s_full + 8 * x, 1);
+            mbar_init(p_full + 8 * x, 4);
+            mbar_init(o_done + 8 * x, 1);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), F::kCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;      // S of the teams (128 columns each), then their O (DH columns each)
+
+    if (warp == 0) {
+        if (lane == 0) {
+            const int teams = TEAMS == 2 && last[TEAMS - 1] >= first[TEAMS - 1] ? 2 : 1;
+            mbar_expect_tx(q_full, teams * F::kTile);
+            for (int x = 0; x < teams; x++) load_tile<DH>(sQ + x * F::kTile, &map_q, q_full, h, qt0 + x * TILE);
+            for (int j = 0; j < count; j++) {
+                const uint32_t st = j % ST, ph = (j / ST) & 1;
+                const int row = span.tile(j) * TILE;
+                if (!mbar_wait(k_empty + 8 * st, ph ^ 1u, abort_flag)) break;
+                mbar_expect_tx(k_full + 8 * st, F::kTile);
+                load_tile<DH>(sK + st * F::kTile, &map_k, k_full + 8 * st, g, row);
+                if (!mbar_wait(v_empty + 8 * st, ph ^ 1u, abort_flag)) break;
+                mbar_expect_tx(v_full + 8 * st, F::kTile);
+                load_tile<DH>(sV + st * F::kTile, &map_v, v_full + 8 * st, g, row);
+            }
+        }
+    } else if (warp == 1) {
+        constexpr uint32_t idesc_s = make_idesc(TILE, TILE, false, false);
+        constexpr uint32_t idesc_pv = make_idesc(TILE, DH, false, true);
+        bool alive = mbar_wait_warp(q_full, 0, abort_flag);
+        uint32_t used[TEAMS] = {};                      // P tiles taken from each team
+        auto issue_s = [&](int x, int j) {              // S_x = Q_x K_j^T (K_j is in shared memory)
+            const uint32_t q_lo = klo(sQ + x * F::kTile), k_lo = klo(sK + (j % ST) * F::kTile);
+#pragma unroll
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tmem + x * TILE, q_lo + kstep(kk), k_lo + kstep(kk), idesc_s, kk != 0);
+            umma_commit_w(s_full + 8 * x);
+        };
+        auto issue_pv = [&](int x, int j) -> bool {     // O_x += P_x V_j once the team has stored P_x
+            if (!mbar_wait_warp(p_full + 8 * x, used[x] & 1, abort_flag)) return false;
+            tc_fence_after();
+            const uint32_t v_lo = mnlo(sV + (j % ST) * F::kTile);
+#pragma unroll
+            for (int kk = 0; kk < 8; kk++)
+                umma_ts_w(tmem + TEAMS * TILE + x * DH, tmem + x * TILE + kk * 8, v_lo + mnstep(kk), idesc_pv, used[x] | (uint32_t)kk);
+            used[x]++;
+            if (span.tile(j) == last[x] / TILE) umma_commit_w(o_done + 8 * x);
+            return true;
+        };
+        if (alive) alive = mbar_wait_warp(k_full, 0, abort_flag);
+        if (alive) {
+            tc_fence_after();
+#pragma unroll
+            for (int x = 0; x < TEAMS; x++)
+                if (active(x, span.tile(0))) issue_s(x, 0);
+            umma_commit_w(k_empty);
+        }
+        for (int j = 0; j < count && alive; j++) {
+            const uint32_t st = j % ST, ph = (j / ST) & 1;
+            const int n = j + 1;
+            if (!mbar_wait_warp(v_full + 8 * st, ph, abort_flag)) { alive = false; break; }
+            if (n < count && !mbar_wait_warp(k_full + 8 * (n % ST), (n / ST) & 1, abort_flag)) { alive = false; break; }
+            tc_fence_after();
+#pragma unroll
+            for (int x = 0; x < TEAMS; x++) {
+                if (alive && active(x, span.tile(j))) alive = issue_pv(x, j);
+                if (alive && n < count && active(x, span.tile(n))) issue_s(x, n);
+            }
+            if (!alive) break;
+            umma_commit_w(v_empty + 8 * st);
+            if (n < count) umma_commit_w(k_empty + 8 * (n % ST));
+        }
+    } else {
+        const int x = TEAMS == 2 ? (warp - 2) >> 2 : 0;
+        const int quarter = warp & 3;
+        const int row = quarter * 32 + lane;
+        const int q_first = x == 0 ? first[0] : first[TEAMS - 1], q_last = x == 0 ? last[0] : last[TEAMS - 1];
+        const int q_abs = q_first + row;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t tS = tmem + x * TILE + lane_base, tO = tmem + TEAMS * TILE + x * DH + lane_base;
+        float m_used = -INFINITY, l = 0.f;
+        uint32_t done = 0;                                        // key tiles this team has taken
+        bool alive = true;
+        for (int j = 0; j < count && alive; j++) {
+            const int kt = span.tile(j);
+            if (TEAMS == 2 && !(q_last >= q_first && sees<TILE>(p.w, kt, q_first, q_last))) continue;
+            if (!mbar_wait(s_full + 8 * x, done & 1, abort_flag)) { alive = false; break; }
+            tc_fence_after();
+            uint32_t r[128];
+#pragma unroll
+            for (int c = 0; c < 4; c++) tmem_ld32_async(tS + c * 32, r + c * 32);
+            tmem_wait_ld();
+            if (mixed(p.w, q_first, kt * TILE)) {
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    const uint32_t see = visible_keys(p.w, q_abs, kt * TILE, c * 32);
+#pragma unroll
+                    for (int e = 0; e < 32; e++)
+                        if (!(see >> e & 1u)) r[c * 32 + e] = 0xff800000u;              // -inf
+                }
+            }
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int e = 0; e < 128; e += 4) {
+#pragma unroll
+                for (int t = 0; t < 4; t++) m4[t] = fmaxf(m4[t], __uint_as_float(r[e + t]));
+            }
+            const float mt = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2;
+            float factor = 1.f;
+            const bool grow = mt > m_used + 8.f;                  // also true on the first tile with a visible key
+            if (grow) {
+                factor = fast_exp2(m_used - mt);
+                m_used = mt;
+                l *= factor;
+            }
+            // S complete implies the product with the previous P complete (same issuing thread, in order): O is at rest
+            if (done > 0 && __any_sync(0xffffffffu, grow)) {
+#pragma unroll 1
+                for (int c = 0; c < DH / 32; c++) {
+                    uint32_t o[32];
+                    tmem_ld32(tO + c * 32, o);
+#pragma unroll
+                    for (int e = 0; e < 32; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                    tmem_st32(tO + c * 32, o);
+                }
+            }
+            const float neg_m = m_used == -INFINITY ? 0.f : -m_used;        // nothing seen so far: exact zeros
+            float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < 8; c++) {                        // 16 scores -> 8 packed words per step
+                uint32_t pk[8];
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float p0 = fast_exp2(fmaf(__uint_as_float(r[c * 16 + e]), p.scale_log2, neg_m));
+                    const float p1 = fast_exp2(fmaf(__uint_as_float(r[c * 16 + e + 1]), p.scale_log2, neg_m));
+                    l4[(e >> 1) & 3] += p0 + p1;
+                    pk[e >> 1] = pack_bf16(p0, p1);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; e++) r[c * 8 + e] = pk[e];  // packed P reuses the registers of consumed scores
+            }
+            l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+            // P overwrites the first 64 columns of S (this thread's own lane)
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                uint32_t wd[16];
+#pragma unroll
+                for (int e = 0; e < 16; e++) wd[e] = r[c * 16 + e];
+                tmem_st16(tS + c * 16, wd);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full + 8 * x);
+            done++;
+        }
+        if (alive && done > 0 && mbar_wait(o_done + 8 * x, 0, abort_flag)) {
+            tc_fence_after();
+            const float inv = 1.f / l;
+            const int qr = qt0 + x * TILE + row;
+#pragma unroll 1
+            for (int c = 0; c < DH / 32; c++) {
+                uint32_t o[32];
+                tmem_ld32(tO + c * 32, o);
+                if (qr < p.w.n) {
+                    bf16 *out = p.o + ((long long)qr * p.w.Hq + h) * DH + c * 32;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint32_t wd[4];
+#pragma unroll
+                        for (int t = 0; t < 4; t++)
+                            wd[t] = pack_bf16(__uint_as_float(o[e + 2 * t]) * inv, __uint_as_float(o[e + 2 * t + 1]) * inv);
+                        *reinterpret_cast<uint4 *>(out + e) = make_uint4(wd[0], wd[1], wd[2], wd[3]);
+                    }
+                }
+            }
+            if (qr < p.w.n) p.lse[(long long)h * p.w.n + qr] = (m_used + log2f(l)) * kLn2;
+        }
+    }
+
+    __syncwarp();
+    leave(abort_flag);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, F::kCols);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// backward
+// ---------------------------------------------------------------------------------------------------------------
+struct BwdParams {
+    WindowShape w;
+    KeyWork<TILE> work;
+    const float *lse;     // [Hq, n]
+    const float *delta;   // [Hq, n]
+    void *dq, *dk, *dv;   // [n, Hq, DH], [q0 + n, Hkv, DH]
+    float *part;          // [sink item][Hkv][dK, dV][part_rows][DH]
+    int part_rows;
+    int mode;             // GradMode of dk, dv (dq: fp32 or bf16, always overwritten)
+    float scale, scale_log2;
+};
+
+template <int DH> struct Bwd {
+    static constexpr int kTile = TILE * DH * 2;
+    static constexpr int kQStages = 3, kKStages = 3;
+    static constexpr int kSlack = DH == 128 ? 768 : 1024;      // what the carve-out leaves for aligning the tiles to 1024 bytes
+    static constexpr int kSmemKV = (4 + kQStages) * kTile + 4 * TILE * 4 /* lse, delta x 2 stages */ + 256 + kSlack;
+    static constexpr int kSmemQ = (4 + kKStages) * kTile + 1024 + 256;
+    static constexpr int kSmem = kSmemKV > kSmemQ ? kSmemKV : kSmemQ;
+    static_assert(kSmem <= 232448, "backward roles exceed the shared memory of an SM");
+};
+constexpr int BWD_THREADS = 64 + 512;
+
+// 32 fp32 sums of one row to where the gradient goes
+__device__ __forceinline__ void put32(void *dst, long long at, const uint32_t (&r)[32], int mode) {
+    if (mode == GRAD_BF16_SET) {
+        bf16 *d = static_cast<bf16 *>(dst) + at;
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+            uint32_t wd[4];
+#pragma unroll
+            for (int t = 0; t < 4; t++) wd[t] = pack_bf16(__uint_as_float(r[e + 2 * t]), __uint_as_float(r[e + 2 * t + 1]));
+            *reinterpret_cast<uint4 *>(d + e) = make_uint4(wd[0], wd[1], wd[2], wd[3]);
+        }
+    } else {
+        float *d = static_cast<float *>(dst) + at;
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+            float4 a = make_float4(__uint_as_float(r[e]), __uint_as_float(r[e + 1]), __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
+            if (mode == GRAD_F32_ADD) {
+                const float4 b = *reinterpret_cast<const float4 *>(d + e);
+                a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+            }
+            *reinterpret_cast<float4 *>(d + e) = a;
+        }
+    }
+}
+
+template <int DH>
+__device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
+                                          const CUtensorMap &map_do, const BwdParams &p, uint8_t *smem_raw, int item, int g) {
+    typedef Bwd<DH> W;
+    constexpr int T = W::kTile, QS = W::kQStages;
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    const uint32_t sK = base, sV = sK + T, sQ = sV + T, sdO = sQ + QS * T;
+    uint8_t *tail = smem_raw + (base - raw) + (4 + QS) * T;
+    float *s_lse = reinterpret_cast<float *>(tail);           // [2][128], pre-multiplied by log2(e)
+    float *s_delta = s_lse + 2 * TILE;                        // [2][128], pre-multiplied by the score scale
+    uint8_t *aux = tail + 4 * TILE * 4;
+    const uint32_t bars = smem_u32(aux);
+    const uint32_t kv_full = bars, q_full = bars + 8, q_empty = bars + 32, do_full = bars + 56, do_empty = bars + 72,
+                   rows_empty = bars + 88, s_full = bars + 104, dp_full = bars + 112, loaded = bars + 120,
+                   p1_full = bars + 128, p2_full = bars + 136, acc_full = bars + 144;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(aux + 152);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(aux + 160);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int G = p.w.Hq / p.w.Hkv;
+    int kt, qt_begin, qt_end, seg;
+    p.work.item(p.w, item, kt, qt_begin, qt_end, seg);
+    const int k_abs0 = kt * TILE;
+    const int per_head = qt_end - qt_begin;
+    const int iters = G * per_head;
+
+    if (threadIdx.x == 0) {
+        mbar_init(kv_full, 1);
+        for (int s = 0; s < QS; s++) {
+            mbar_init(q_full + 8 * s, 1);
+            mbar_init(q_empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; s++) {
+            mbar_init(do_full + 8 * s, 1);
+            mbar_init(do_empty + 8 * s, 1);
+            mbar_init(rows_empty + 8 * s, 1);
+        }
+        mbar_init(s_full, 1);
+        mbar_init(dp_full, 1);
+        mbar_init(loaded, 16);
+        mbar_init(p1_full, 16);
+        mbar_init(p2_full, 16);
+        mbar_init(acc_full, 1);
+        // a base that needs more alignment than the carve-out leaves cannot be used
+        *abort_flag = (int)(base - raw) > W::kSlack ? 1 : 0;
+        if (*abort_flag) atomicExch(&g_tc_fault, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    // columns: S^T at 0; dP^T at 128, later P^T (packed) in the first and dS^T (packed) in the second 16 columns of
+    // every 32-column group; dV at 256, dK behind it
+    const uint32_t tST = tmem, tDPT = tmem + 128, tDV = tmem + 256, tDK = tmem + 256 + DH;
+    const bool usable = *abort_flag == 0;
+
+    if (!usable) {
+        // nothing was issued: fall through to the common exit
+    } else if (warp == 0) {
+        if (lane == 0 && iters > 0) {
+            mbar_expect_tx(kv_full, 2 * T);
+            load_tile<DH>(sK, &map_k, kv_full, g, k_abs0);
+            load_tile<DH>(sV, &map_v, kv_full, g, k_abs0);
+        }
+        uint32_t sq = 0, qph = 0;
+        int h = g * G, qt = qt_begin;
+        for (int it = 0; it < iters; it++) {
+            const int qt0 = qt * TILE;
+            const uint32_t sd = it & 1, dph = (it >> 1) & 1;
+            int ok = 1;
+            if (lane == 0) {
+                ok = mbar_wait(q_empty + 8 * sq, qph ^ 1u, abort_flag) ? 1 : 0;          // dK of the stage's last user
+                if (ok) {
+                    mbar_expect_tx(q_full + 8 * sq, T);
+                    load_tile<DH>(sQ + sq * T, &map_q, q_full + 8 * sq, h, qt0);
+                    ok = mbar_wait(do_empty + 8 * sd, dph ^ 1u, abort_flag) ? 1 : 0;     // dV of the stage's last user
+                }
+                if (ok) {
+                    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(do_full + 8 * sd), "r"(T) : "memory");
+                    load_tile<DH>(sdO + sd * T, &map_do, do_full + 8 * sd, h, qt0);
+                    ok = mbar_wait(rows_empty + 8 * sd, dph ^ 1u, abort_flag) ? 1 : 0;   // delta rows: read until dS^T is packed
+                }
+            }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            if (!ok) break;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int col = lane * 4 + e, r = qt0 + col;
+                s_lse[sd * TILE + col] = r < p.w.n ? p.lse[(long long)h * p.w.n + r] * kLog2e : 0.f;
+                s_delta[sd * TILE + col] = r < p.w.n ? p.delta[(long long)h * p.w.n + r] * p.scale : 0.f;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(do_full + 8 * sd);   // publishes the rows; the phase completes when dO has landed too
+            if (++sq == QS) { sq = 0; qph ^= 1u; }
+            if (++qt == qt_end) { qt = qt_begin; h++; }
+        }
+    } else if (warp == 1) {
+        // the whole warp runs the issue loop; each MMA / commit executes in one elected lane
+        constexpr uint32_t idesc_kk = make_idesc(TILE, TILE, false, false);     // both operands K-major
+        constexpr uint32_t idesc_acc = make_idesc(TILE, DH, false, true);       // B MN-major (N = head dims)
+        bool alive = iters == 0 || mbar_wait_warp(kv_full, 0, abort_flag);
+        const uint32_t k_lo = klo(sK), v_lo = klo(sV);
+        uint32_t sq_s = 0, qph_s = 0;      // Q stage / phase of the next S^T
+        uint32_t sq_k = 0;                 // Q stage of the next dK
+        auto issue_st = [&]() -> bool {    // S^T = K Q^T for the next iteration
+            if (!mbar_wait_warp(q_full + 8 * sq_s, qph_s, abort_flag)) return false;
+            tc_fence_after();
+            const uint32_t q_lo = klo(sQ + sq_s * T);
+#pragma unroll
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tST, k_lo + kstep(kk), q_lo + kstep(kk), idesc_kk, kk != 0);
+            umma_commit_w(s_full);
+            if (++sq_s == QS) { sq_s = 0; qph_s ^= 1u; }
+            return true;
+        };
+        auto issue_dpt = [&](int it) -> bool {     // dP^T = V dO^T of iteration `it`
+            if (!mbar_wait_warp(do_full + 8 * (it & 1), (it >> 1) & 1, abort_flag)) return false;
+            tc_fence_after();
+            const uint32_t do_lo = klo(sdO + (it & 1) * T);
+#pragma unroll
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tDPT, v_lo + kstep(kk), do_lo + kstep(kk), idesc_kk, kk != 0);
+            umma_commit_w(dp_full);
+            return true;
+        };
+        if (alive && iters > 0) alive = issue_st() && issue_dpt(0);
+        for (int it = 0; it < iters && alive; it++) {
+            const uint32_t sd = it & 1;
+            // the softmax warps hold S^T of this iteration in registers: its columns take the next one's at once
+            if (it + 1 < iters) {
+                if (!mbar_wait_warp(loaded, it & 1, abort_flag)) { alive = false; break; }
+                tc_fence_after();
+                if (!issue_st()) { alive = false; break; }
+            }
+            // dV += P^T dO as soon as P^T is packed (first 16 columns of each group of the dP^T region)
+            if (!mbar_wait_warp(p1_full, it & 1, abort_flag)) { alive = false; break; }
+            tc_fence_after();
+            const uint32_t do_mn = mnlo(sdO + sd * T);
+#pragma unroll
+            for (int kk = 0; kk < 8; kk++)
+                umma_ts_w(tDV, tDPT + (kk >> 1) * 32 + (kk & 1) * 8, do_mn + mnstep(kk), idesc_acc, (it | kk) != 0);
+            umma_commit_w(do_empty + 8 * sd);            // dO of this stage is consumed (dP^T was issued earlier)
+            // dK += dS^T Q (second 16 columns of each group)
+            if (!mbar_wait_warp(p2_full, it & 1, abort_flag)) { alive = false; break; }
+            tc_fence_after();
+            const uint32_t q_mn = mnlo(sQ + sq_k * T);
+#pragma unroll
+            for (int kk = 0; kk < 8; kk++)
+                umma_ts_w(tDK, tDPT + (kk >> 1) * 32 + 16 + (kk & 1) * 8, q_mn + mnstep(kk), idesc_acc, (it | kk) != 0);
+            umma_commit_w(q_empty + 8 * sq_k);           // Q of this stage is consumed
+            umma_commit_w(rows_empty + 8 * sd);          // and so are the lse / delta rows
+            if (++sq_k == QS) sq_k = 0;
+            // the dP^T region is free once dV and dK have read it (in order): next iteration's dP^T
+            if (it + 1 < iters && !issue_dpt(it + 1)) { alive = false; break; }
+        }
+        if (alive && iters > 0) umma_commit_w(acc_full);
+    } else {
+        const int quarter = warp & 3;
+        const int wg = (warp - 2) >> 2;                           // 0..3: 32-query group of the tile
+        const int col_base = wg * 32;
+        const int row = quarter * 32 + lane;                      // key row within the tile
+        const int k_abs = k_abs0 + row;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        // The group reads its 32 fp32 columns of S^T and of dP^T into registers, then writes the packed bf16 pairs of P^T
+        // over the first and of dS^T over the second 16 of ITS OWN dP^T columns; the MMA warp addresses each 16-query
+        // slice of those A operands separately.  S^T's columns are never written by these warps.
+        const uint32_t tS_g = tST + col_base + lane_base, tP_g = tDPT + col_base + lane_base;
+        bool alive = true;
+        int qt = qt_begin;
+        for (int it = 0; it < iters && alive; it++) {
+            const int q_abs0 = p.w.q0 + qt * TILE;
+            const uint32_t sd = it & 1;
+            if (!mbar_wait(s_full, it & 1, abort_flag)) { alive = false; break; }
+            tc_fence_after();
+            uint32_t rs[32];
+            tmem_ld32(tS_g, rs);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(loaded);
+            // the producer's lse / delta rows of this stage are published together with the dO tile
+            if (!mbar_wait(do_full + 8 * sd, (it >> 1) & 1, abort_flag)) { alive = false; break; }
+            const uint32_t see = mixed(p.w, q_abs0, k_abs0) ? visible_rows(p.w, k_abs, q_abs0, col_base) : 0xffffffffu;
+            const float *lse2 = s_lse + sd * TILE + col_base, *dl = s_delta + sd * TILE + col_base;
+            // phase 1: P^T = exp2(S^T * scale - lse), all the dV product needs
+            float pv[32];
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+                const float4 l4 = *reinterpret_cast<const float4 *>(lse2 + e);
+                const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                for (int t = 0; t < 4; t++) {
+                    float x = fmaf(__uint_as_float(rs[e + t]), p.scale_log2, -lv[t]);
+                    if (!(see >> (e + t) & 1u)) x = -INFINITY;
+                    pv[e + t] = fast_exp2(x);
+                }
+            }
+            // dP^T of this iteration was queued a whole iteration ago; its columns become P^T and dS^T
+            uint32_t pp[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) pp[e / 2] = pack_bf16(pv[e], pv[e + 1]);
+            if (!mbar_wait(dp_full, it & 1, abort_flag)) { alive = false; break; }
+            tc_fence_after();
+            uint32_t rp[32];
+            tmem_ld32(tP_g, rp);
+            {
+                tmem_st16(tP_g, pp);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p1_full);
+            }
+            // phase 2: dS^T = P^T * (dP^T * scale - delta * scale)
+            {
+                uint32_t ds[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const float4 d4 = *reinterpret_cast<const float4 *>(dl + e);
+                    const float dv[4] = {d4.x, d4.y, d4.z, d4.w};
+                    float dsv[4];
+#pragma unroll
+                    for (int t = 0; t < 4; t++) dsv[t] = pv[e + t] * fmaf(__uint_as_float(rp[e + t]), p.scale, -dv[t]);
+                    ds[e / 2] = pack_bf16(dsv[0], dsv[1]);
+                    ds[e / 2 + 1] = pack_bf16(dsv[2], dsv[3]);
+                }
+                tmem_st16(tP_g + 16, ds);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p2_full);
+            }
+            if (++qt == qt_end) qt = qt_begin;
+        }
+        if (alive && (iters == 0 || mbar_wait(acc_full, 0, abort_flag)) && wg < DH / 32) {
+            tc_fence_after();
+            // group wg writes head dims 32*wg .. 32*wg+31
+            uint32_t rv[32], rk[32];
+            if (iters > 0) {
+                tmem_ld32(tDV + lane_base + col_base, rv);
+                tmem_ld32(tDK + lane_base + col_base, rk);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 32; e++) rv[e] = rk[e] = 0u;
+            }
+            const bool joined = seg >= 0 && row < sink_rows<TILE>(p.w, kt);
+            if (joined) {                                         // this segment's share of a sink key's sums
+                float *part = p.part + (((long long)item * p.w.Hkv + g) * 2 * p.part_rows + row) * DH + col_base;
+                put32(part, 0, rk, GRAD_F32_SET);
+                put32(part, (long long)p.part_rows * DH, rv, GRAD_F32_SET);
+            } else if (seg <= 0 && k_abs < p.w.q0 + p.w.n) {      // segments behind the first have nothing for these rows
+                const long long at = ((long long)k_abs * p.w.Hkv + g) * DH + col_base;
+                put32(p.dv, at, rv, p.mode);
+                put32(p.dk, at, rk, p.mode);
+            }
+        }
+    }
+
+    __syncwarp();
+    leave(abort_flag);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+template <int DH>
+__device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
+                                        const CUtensorMap &map_do, const BwdParams &p, uint8_t *smem_raw, int block_x, int h) {
+    typedef Bwd<DH> W;
+    constexpr int T = W::kTile, KS = W::kKStages;
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    // K tiles live from S_j to dQ_j, so their ring has three stages; V tiles are released right after dP_j (two stages)
+    const uint32_t sQ = base, sdO = sQ + T, sK = sdO + T, sV = sK + KS * T;
+    uint8_t *aux = smem_raw + (base - raw) + (4 + KS) * T;
+    const uint32_t bars = smem_u32(aux);
+    const uint32_t q_full = bars, k_full = bars + 8, k_empty = bars + 32, v_full = bars + 56, v_empty = bars + 72,
+                   s_full = bars + 88, dp_full = bars + 96, s_free = bars + 104, p2_full = bars + 112,
+                   acc_full = bars + 120;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(aux + 128);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(aux + 136);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g = h / (p.w.Hq / p.w.Hkv);
+    const int qt0 = block_x * TILE;
+    const int q_abs0 = p.w.q0 + qt0;
+    const int rows_here = (p.w.n - qt0) < TILE ? (p.w.n - qt0) : TILE;
+    const KeySpan span = key_span<TILE>(p.w, q_abs0, q_abs0 + rows_here - 1);
+    const int nkv = span.count();
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        for (int s = 0; s < KS; s++) {
+            mbar_init(k_full + 8 * s, 1);
+            mbar_init(k_empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; s++) {
+            mbar_init(v_full + 8 * s, 1);
+            mbar_init(v_empty + 8 * s, 1);
+        }
+        mbar_init(s_full, 1);
+        mbar_init(dp_full, 1);
+        mbar_init(s_free, 16);
+        mbar_init(p2_full, 16);
+        mbar_init(acc_full, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    // columns: S at 0, dP at 128, dQ at 256
+    const uint32_t tS = tmem, tDP = tmem + 128, tDQ = tmem + 256;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            mbar_expect_tx(q_full, 2 * T);
+            load_tile<DH>(sQ, &map_q, q_full, h, qt0);
+            load_tile<DH>(sdO, &map_do, q_full, h, qt0);
+            uint32_t ks = 0, kph = 0;
+            for (int j = 0; j < nkv; j++) {
+                const int row = span.tile(j) * TILE;
+                if (!mbar_wait(k_empty + 8 * ks, kph ^ 1u, abort_flag)) break;
+                mbar_expect_tx(k_full + 8 * ks, T);
+                load_tile<DH>(sK + ks * T, &map_k, k_full + 8 * ks, g, row);
+                if (++ks == KS) { ks = 0; kph ^= 1u; }
+                const uint32_t vs = j & 1, vph = (j >> 1) & 1;
+                if (!mbar_wait(v_empty + 8 * vs, vph ^ 1u, abort_flag)) break;
+                mbar_expect_tx(v_full + 8 * vs, T);
+                load_tile<DH>(sV + vs * T, &map_v, v_full + 8 * vs, g, row);
+            }
+        }
+    } else if (warp == 1) {
+        // the whole warp runs the issue loop; each MMA / commit executes in one elected lane
+        constexpr uint32_t idesc_kk = make_idesc(TILE, TILE, false, false);
+        constexpr uint32_t idesc_acc = make_idesc(TILE, DH, false, true);
+        bool alive = mbar_wait_warp(q_full, 0, abort_flag);
+        const uint32_t q_lo = klo(sQ), do_lo = klo(sdO);
+        // K stage and phase of the tile whose S is issued next / whose dQ is issued next
+        uint32_t ks_s = 0, kph_s = 0, ks_q = 0;
+        auto issue_s = [&]() -> bool {             // S = Q K^T
+            if (!mbar_wait_warp(k_full + 8 * ks_s, kph_s, abort_flag)) return false;
+            tc_fence_after();
+            const uint32_t k_lo = klo(sK + ks_s * T);
+#pragma unroll
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tS, q_lo + kstep(kk), k_lo + kstep(kk), idesc_kk, kk != 0);
+            umma_commit_w(s_full);
+            if (++ks_s == KS) { ks_s = 0; kph_s ^= 1u; }
+            return true;
+        };
+        auto issue_dp = [&](int j) -> bool {       // dP = dO V^T
+            const uint32_t vs = j & 1;
+            if (!mbar_wait_warp(v_full + 8 * vs, (j >> 1) & 1, abort_flag)) return false;
+            tc_fence_after();
+            const uint32_t v_lo = klo(sV + vs * T);
+#pragma unroll
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tDP, do_lo + kstep(kk), v_lo + kstep(kk), idesc_kk, kk != 0);
+            umma_commit_w(v_empty + 8 * vs);             // V of this stage is consumed
+            umma_commit_w(dp_full);
+            return true;
+        };
+        if (alive) alive = issue_s() && issue_dp(0);
+        for (int j = 0; j < nkv && alive; j++) {
+            if (j + 1 < nkv) {
+                // next tile's S as soon as the softmax warps have read this tile's S into registers
+                if (!mbar_wait_warp(s_free, j & 1, abort_flag)) { alive = false; break; }
+                tc_fence_after();
+                if (!issue_s()) { alive = false; break; }
+            }
+            if (!mbar_wait_warp(p2_full, j & 1, abort_flag)) { alive = false; break; }
+            tc_fence_after();
+            const uint32_t k_mn = mnlo(sK + ks_q * T);
+#pragma unroll
+            for (int kk = 0; kk < 8; kk++)
+                umma_ts_w(tDQ, tDP + (kk >> 1) * 32 + (kk & 1) * 8, k_mn + mnstep(kk), idesc_acc, (j | kk) != 0);
+            umma_commit_w(k_empty + 8 * ks_q);           // K of this stage is consumed
+            if (++ks_q == KS) ks_q = 0;
+            // the dP columns are free once dQ has read dS (in order)
+            if (j + 1 < nkv && !issue_dp(j + 1)) { alive = false; break; }
+        }
+        if (alive) umma_commit_w(acc_full);
+    } else {
+        const int quarter = warp & 3;
+        const int wg = (warp - 2) >> 2;                           // 0..3: 32-key group of the tile
+        const int key_base = wg * 32;
+        const int row = quarter * 32 + lane;
+        const int qr = qt0 + row;
+        const int q_abs = q_abs0 + row;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t tS_g = tS + key_base + lane_base, tP_g = tDP + key_base + lane_base;
+        const float neg_lse2 = qr < p.w.n ? -p.lse[(long long)h * p.w.n + qr] * kLog2e : 0.f;
+        const float neg_delta_s = qr < p.w.n ? -p.delta[(long long)h * p.w.n + qr] * p.scale : 0.f;
+        bool alive = true;
+        for (int j = 0; j < nkv && alive; j++) {
+            const int k_abs0 = span.tile(j) * TILE;
+            if (!mbar_wait(s_full, j & 1, abort_flag)) { alive = false; break; }
+            tc_fence_after();
+            const uint32_t see = mixed(p.w, q_abs0, k_abs0) ? visible_keys(p.w, q_abs, k_abs0, key_base) : 0xffffffffu;
+            // phase 1: P from S; the S columns are handed back to the tensor pipe right after the load
+            float pv[32];
+            {
+                uint32_t rs[32];
+                tmem_ld32(tS_g, rs);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_free);
+#pragma unroll
+                for (int e = 0; e < 32; e++) {
+                    float x = fmaf(__uint_as_float(rs[e]), p.scale_log2, neg_lse2);
+                    if (!(see >> e & 1u)) x = -INFINITY;
+                    pv[e] = fast_exp2(x);
+                }
+            }
+            // phase 2: dS = P * (dP * scale - delta * scale), packed in place
+            if (!mbar_wait(dp_full, j & 1, abort_flag)) { alive = false; break; }
+            tc_fence_after();
+            {
+                uint32_t rp[32], ds[16];
+                tmem_ld32(tP_g, rp);
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    const float d0 = pv[e] * fmaf(__uint_as_float(rp[e]), p.scale, neg_delta_s);
+                    const float d1 = pv[e + 1] * fmaf(__uint_as_float(rp[e + 1]), p.scale, neg_delta_s);
+                    ds[e / 2] = pack_bf16(d0, d1);
+                }
+                tmem_st16(tP_g, ds);       // front of the group's own fp32 columns
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p2_full);
+            }
+        }
+        if (alive && mbar_wait(acc_full, 0, abort_flag) && wg < DH / 32) {
+            tc_fence_after();
+            uint32_t r[32];
+            tmem_ld32(tDQ + lane_base + key_base, r);
+            if (qr < p.w.n)
+                put32(p.dq, ((long long)qr * p.w.Hq + h) * DH + key_base, r, p.mode == GRAD_BF16_SET ? GRAD_BF16_SET : GRAD_F32_SET);
+        }
+    }
+
+    __syncwarp();
+    leave(abort_flag);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+template <int DH>
+__global__ void __launch_bounds__(BWD_THREADS, 1)
+    attn_window_bwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
+                           const BwdParams p, int n_dkdv, int n_dq_first) {
+    pdl_enter();
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    // dispatch order: n_dq_first dQ CTAs (all of them or none), then the dK/dV CTAs, then the rest
+    const int b = (int)blockIdx.x;
+    const bool dq_role = b < n_dq_first || b >= n_dq_first + n_dkdv;
+    if (!dq_role) {
+        const int c = b - n_dq_first;
+        dkdv_body<DH>(map_q, map_k, map_v, map_do, p, smem_raw, c / p.w.Hkv, c % p.w.Hkv);
+    } else {
+        const int c = b < n_dq_first ? b : b - n_dkdv;
+        dq_body<DH>(map_q, map_k, map_v, map_do, p, smem_raw, p.work.q_tiles - 1 - c % p.work.q_tiles, c / p.work.q_tiles);
+    }
+}
+
+// delta[h, i] = sum_j dO[i, h, j] O[i, h, j]: one 16-byte load of each per thread, DH / 8 threads to a row
+template <int DH>
+__global__ void __launch_bounds__(256) window_delta_kernel(const bf16 *o, const bf16 *dout, int n, int Hq, float *delta, WsHeader *hdr) {
+    pdl_enter();
+    if (blockIdx.x == 0 && threadIdx.x == 0) clear_status(hdr);
+    constexpr int kLanes = DH / 8;
+    const long long rows = (long long)n * Hq, step = (long long)gridDim.x * (256 / kLanes);
+    const int sub = threadIdx.x % kLanes;
+    for (long long r = (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes; r - threadIdx.x / kLanes < rows; r += step) {
+        float s = 0.f;
+        if (r < rows) {
+            Vec<bf16> a, b;
+            a.load(o + r * DH + sub * 8);
+            b.load(dout + r * DH + sub * 8);
+#pragma unroll
+            for (int e = 0; e < 8; e++) s = fmaf(a.v[e], b.v[e], s);
+        }
+#pragma unroll
+        for (int w = kLanes / 2; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
+        if (sub == 0 && r < rows) delta[(r % Hq) * n + r / Hq] = s;
+    }
+}
+
+template <typename K>
+bool opt_in_smem(K kernel, int bytes) {
+    return cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+}
+
+struct Maps { CUtensorMap q, k, v, d; };
+bool make_maps(Maps &m, const WindowShape &w, int DH, const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *dout) {
+    const int64_t kv = (int64_t)w.q0 + w.n;
+    return make_tensor_map(&m.q, q, w.n, (int64_t)w.Hq * DH, (int64_t)w.Hq * DH, 64, TILE, false) &&
+           make_tensor_map(&m.k, k, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, TILE, false) &&
+           make_tensor_map(&m.v, v, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, TILE, false) &&
+           (!dout || make_tensor_map(&m.d, dout, w.n, (int64_t)w.Hq * DH, (int64_t)w.Hq * DH, 64, TILE, false));
+}
+
+template <int DH, int TEAMS, int ST>
+int launch_fwd(const Maps &m, const FwdParams &p, cudaStream_t st) {
+    typedef Fwd<DH, TEAMS, ST> F;
+    static PerDevice configured;
+    if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, TEAMS, ST>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+    const int64_t tiles = ((int64_t)p.w.n + TEAMS * TILE - 1) / (TEAMS * TILE);
+    if (tiles > 65535) return STREAMBP_E_SHAPE;
+    SBP_LAUNCH((attn_window_fwd_kernel<DH, TEAMS, ST>), dim3(p.w.Hq, (unsigned)tiles), F::kThreads, F::kSmem, st, m.q, m.k, m.v, p);
+    return STREAMBP_OK;
+}
+
+template <int DH>
+int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, bf16 *o, float *lse, cudaStream_t st, int teams) {
+    Maps m;
+    if (!make_maps(m, w, DH, q, k, v, nullptr)) return STREAMBP_E_CUDA;
+    const FwdParams p{w, o, lse, kLog2e / sqrtf((float)DH)};
+    if (teams == 0) teams = 1;
+    if (teams == 2) return launch_fwd<DH, 2, 2>(m, p, st);
+    return launch_fwd<DH, 1, DH == 64 ? 2 : 1>(m, p, st);
+}
+
+template <int DH>
+int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf16 *dout, const float *lse, const WindowShape &w,
+            int mode, void *dq, void *dk, void *dv, float *delta, float *part, WsHeader *hdr, cudaStream_t st) {
+    Maps m;
+    if (!make_maps(m, w, DH, q, k, v, dout)) return STREAMBP_E_CUDA;
+    static PerDevice configured;
+    if (!configured.get([] { return opt_in_smem(attn_window_bwd_kernel<DH>, Bwd<DH>::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+    {
+        const int64_t blocks = ((int64_t)w.n * w.Hq * (DH / 8) + 255) / 256, most = (int64_t)sm_count() * 8;
+        SBP_LAUNCH(window_delta_kernel<DH>, (unsigned)(blocks < most ? blocks : most), 256, 0, st, o, dout, w.n, w.Hq, delta, hdr);
+    }
+    const float scale = 1.f / sqrtf((float)DH);
+    BwdParams p;
+    memset(&p, 0, sizeof(p));
+    p.w = w;
+    p.work = key_work<TILE>(w);
+    p.lse = lse; p.delta = delta;
+    p.dq = dq; p.dk = dk; p.dv = dv;
+    p.part = part;
+    p.part_rows = w.sinks < TILE ? w.sinks : TILE;
+    p.mode = mode;
+    p.scale = scale;
+    p.scale_log2 = scale * kLog2e;
+    const int64_t n_dkdv = (int64_t)p.work.items() * w.Hkv, n_dq = (int64_t)p.work.q_tiles * w.Hq;
+    if (n_dkdv + n_dq > 0x7fffffff) return STREAMBP_E_SHAPE;
+    // cost of the longest CTA of each role in tile pairs (a dK/dV pair takes ~1.25x a dQ pair: four products against three)
+    const int64_t dq_longest = 4 * (int64_t)(w.window / TILE + 2 + (w.sinks + TILE - 1) / TILE);
+    const int64_t dkdv_longest = 5 * (int64_t)(w.Hq / w.Hkv) * (p.work.len < p.work.q_tiles ? p.work.len : p.work.q_tiles);
+    const int n_dq_first = dq_longest > dkdv_longest ? (int)n_dq : 0;
+    SBP_LAUNCH(attn_window_bwd_kernel<DH>, (unsigned)(n_dkdv + n_dq), BWD_THREADS, Bwd<DH>::kSmem, st, m.q, m.k, m.v, m.d, p,
+               (int)n_dkdv, n_dq_first);
+    return STREAMBP_OK;
+}
+
+}  // namespace
+
+bool attention_window_tc_available() { return tensor_maps_available(); }
+
+int attention_window_fwd_tc(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, int dh, bf16 *o, float *lse,
+                            cudaStream_t st, int teams) {
+    return dh == 64 ? fwd_any<64>(q, k, v, w, o, lse, st, teams) : fwd_any<128>(q, k, v, w, o, lse, st, teams);
+}
+int attention_window_bwd_tc(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf16 *dout, const float *lse,
+                            const WindowShape &w, int dh, int mode, void *dq, void *dk, void *dv, float *delta, float *part,
+                            WsHeader *hdr, cudaStream_t st) {
+    return dh == 64 ? bwd_any<64>(q, k, v, o, dout, lse, w, mode, dq, dk, dv, delta, part, hdr, st)
+                    : bwd_any<128>(q, k, v, o, dout, lse, w, mode, dq, dk, dv, delta, part, hdr, st);
+}
+int attention_window_take_fault() { return take_fault_local(); }
+
+}  // namespace sbp

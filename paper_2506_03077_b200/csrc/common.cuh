@@ -237,6 +237,13 @@ __device__ __forceinline__ void set_status(WsHeader *h, int st, int detail) {
     if (atomicCAS(&h->status, 0, st) == 0) h->detail = detail;
 }
 
+// What a call writes into its workspace header when no kernel of it can report a condition of its own: one thread of one
+// of its kernels does it, which saves the memset the schedulers start with.
+__device__ __forceinline__ void clear_status(WsHeader *h) {
+    h->status = 0;
+    h->detail = 0;
+}
+
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Bump allocator over the caller's workspace; also used (with base == nullptr) to plan sizes.
@@ -345,7 +352,7 @@ int gemm_simt_epilogue(const GemmEpilogue<T> &g, cudaStream_t st);
 int gemm_epilogue_splits(int64_t M, int64_t N);
 template <typename T>
 int gemm_epilogue_bwd(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int act, int64_t M, int64_t N, T *dZ, int64_t ldz,
-                      float *dbias, bool accumulate, float *partials, cudaStream_t st);
+                      float *dbias, bool accumulate, float *partials, WsHeader *hdr, cudaStream_t st);
 
 // Reads and clears the flag a tensor-core kernel raises when one of its bounded waits expires.
 int gemm_tc_take_fault();
@@ -442,6 +449,27 @@ int attn_fwd(const T *q, const T *k, const T *v, int64_t n, int64_t q0, int Hq, 
 template <typename T>
 int attn_bwd(const T *q, const T *k, const T *v, const T *o, const T *dout, const float *lse, int64_t n, int64_t q0,
              int Hq, int Hkv, int dh, float *delta, float *dq, float *dk, float *dv, cudaStream_t st, int engine = -1);
+
+// Attention with a sliding window and sink keys (window.cuh).  mode: GradMode of dk, dv (dq is fp32, or bf16 with
+// GRAD_BF16_SET, and overwritten).  delta: [Hq, n] scratch; part: the sums of sink segments.  The backward calls leave the
+// rows of sink tiles whose work is cut (segs > 1) to attention_window_join.
+struct WindowShape;
+bool attention_window_tc_available();
+// teams: 128-query tiles per CTA, 1 or 2
+int attention_window_fwd_tc(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, int dh, bf16 *o, float *lse,
+                            cudaStream_t st, int teams);
+int attention_window_bwd_tc(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf16 *dout, const float *lse,
+                            const WindowShape &w, int dh, int mode, void *dq, void *dk, void *dv, float *delta, float *part,
+                            WsHeader *hdr, cudaStream_t st);
+int attention_window_take_fault();
+template <typename T>
+int attention_window_fwd_simt(const T *q, const T *k, const T *v, const WindowShape &w, int dh, T *o, float *lse, cudaStream_t st);
+template <typename T>
+int attention_window_bwd_simt(const T *q, const T *k, const T *v, const T *o, const T *dout, const float *lse, const WindowShape &w,
+                              int dh, int mode, void *dq, void *dk, void *dv, float *delta, float *part, WsHeader *hdr,
+                              cudaStream_t st);
+int attention_window_join(const float *part, int tile, int segs, const WindowShape &w, int dh, int mode, void *dk, void *dv,
+                          cudaStream_t st);
 
 // LM head pieces
 int count_valid_labels(const int64_t *labels, int64_t T, int64_t vocab, int64_t ignore, WsHeader *hdr,

@@ -124,8 +124,9 @@ __global__ void __launch_bounds__(256, 4)
     }
 }
 
-__global__ void __launch_bounds__(256) epilogue_sum_kernel(const float *partials, int splits, int N, float *dbias, int accumulate) {
+__global__ void __launch_bounds__(256) epilogue_sum_kernel(const float *partials, int splits, int N, float *dbias, int accumulate, WsHeader *hdr) {
     pdl_enter();
+    if (blockIdx.x == 0 && threadIdx.x == 0) clear_status(hdr);
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= N) return;
     float s = 0.f;
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(256) epilogue_sum_kernel(const float *partials
 
 template <typename T, int ACT>
 int launch(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int64_t N, T *dZ, int64_t ldz, float *dbias,
-           bool accumulate, float *partials, cudaStream_t st) {
+           bool accumulate, float *partials, WsHeader *hdr, cudaStream_t st) {
     auto rows16 = [](const void *q, int64_t ld) {
         return !q || ((reinterpret_cast<uintptr_t>(q) & 15u) == 0 && (ld * (int64_t)sizeof(T)) % 16 == 0);
     };
@@ -148,7 +149,7 @@ int launch(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int64
     else
         SBP_LAUNCH((epilogue_bwd_any_kernel<T, ACT>), grid, 256, 0, st, dC, ldd, pre, ldp, M, (int)N, per, dZ, ldz, sums);
     if (dbias)
-        SBP_LAUNCH(epilogue_sum_kernel, (unsigned)((N + 255) / 256), 256, 0, st, partials, splits, (int)N, dbias, accumulate ? 1 : 0);
+        SBP_LAUNCH(epilogue_sum_kernel, (unsigned)((N + 255) / 256), 256, 0, st, partials, splits, (int)N, dbias, accumulate ? 1 : 0, hdr);
     return STREAMBP_OK;
 }
 
@@ -165,20 +166,20 @@ int gemm_epilogue_splits(int64_t M, int64_t N) {
 
 template <typename T>
 int gemm_epilogue_bwd(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int act, int64_t M, int64_t N, T *dZ, int64_t ldz,
-                      float *dbias, bool accumulate, float *partials, cudaStream_t st) {
+                      float *dbias, bool accumulate, float *partials, WsHeader *hdr, cudaStream_t st) {
     switch (act) {
-        case STREAMBP_ACT_NONE: return launch<T, STREAMBP_ACT_NONE>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
-        case STREAMBP_ACT_RELU: return launch<T, STREAMBP_ACT_RELU>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
-        case STREAMBP_ACT_GELU: return launch<T, STREAMBP_ACT_GELU>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
+        case STREAMBP_ACT_NONE: return launch<T, STREAMBP_ACT_NONE>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, hdr, st);
+        case STREAMBP_ACT_RELU: return launch<T, STREAMBP_ACT_RELU>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, hdr, st);
+        case STREAMBP_ACT_GELU: return launch<T, STREAMBP_ACT_GELU>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, hdr, st);
         case STREAMBP_ACT_GELU_TANH:
-            return launch<T, STREAMBP_ACT_GELU_TANH>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
-        case STREAMBP_ACT_SILU: return launch<T, STREAMBP_ACT_SILU>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, st);
+            return launch<T, STREAMBP_ACT_GELU_TANH>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, hdr, st);
+        case STREAMBP_ACT_SILU: return launch<T, STREAMBP_ACT_SILU>(dC, ldd, pre, ldp, M, N, dZ, ldz, dbias, accumulate, partials, hdr, st);
         default: return STREAMBP_E_SHAPE;
     }
 }
 template int gemm_epilogue_bwd<float>(const float *, int64_t, const float *, int64_t, int, int64_t, int64_t, float *, int64_t,
-                                      float *, bool, float *, cudaStream_t);
+                                      float *, bool, float *, WsHeader *, cudaStream_t);
 template int gemm_epilogue_bwd<bf16>(const bf16 *, int64_t, const bf16 *, int64_t, int, int64_t, int64_t, bf16 *, int64_t,
-                                     float *, bool, float *, cudaStream_t);
+                                     float *, bool, float *, WsHeader *, cudaStream_t);
 
 }  // namespace sbp

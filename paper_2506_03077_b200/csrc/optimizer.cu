@@ -428,8 +428,9 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_consta
 }
 
 __global__ void __launch_bounds__(1024) grad_norm_finish_kernel(const double *partial, int n, float max_norm, float *norm,
-                                                                float *scale) {
+                                                                float *scale, WsHeader *hdr) {
     pdl_enter();
+    if (threadIdx.x == 0) clear_status(hdr);
     __shared__ double red[32];
     double v = 0.0;
     for (int i = threadIdx.x; i < n; i += blockDim.x) v += partial[i];
@@ -638,7 +639,7 @@ int streambp_grad_norm(const float *const *grads, const int64_t *counts, int32_t
     int used = 0;
     if (n <= 32) SBP_TRY(launch_norm<32>(grads, counts, n, partial, &used, st));
     else SBP_TRY(launch_norm<512>(grads, counts, n, partial, &used, st));
-    SBP_LAUNCH(grad_norm_finish_kernel, 1, 1024, 0, st, partial, used, max_norm, norm, scale);
+    SBP_LAUNCH(grad_norm_finish_kernel, 1, 1024, 0, st, partial, used, max_norm, norm, scale, static_cast<WsHeader *>(workspace));
     return STREAMBP_OK;
 }
 

@@ -235,7 +235,7 @@ def test_grad_norm(sizes):
         assert abs(scale.item() - want) <= 8 * E32 * want
     first = norm.clone()
     B.grad_norm(c.plan, 1.0, norm, None, ws[:-256])
-    assert torch.equal(first, norm) and bool((ws[-256:] == FENCE).all())
+    assert torch.equal(first, norm) and bool((ws[-256:] == FENCE).all()) and B.last_device_status(ws) == B.OK
 
 
 def test_grad_norm_of_huge_tiny_and_broken_gradients():

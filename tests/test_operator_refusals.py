@@ -107,3 +107,93 @@ def test_gemm_epilogue_backward_refusals(lib):
     assert call(ldd=31) == B.E_SHAPE and call(ldp=31) == B.E_SHAPE and call(ldz=31) == B.E_SHAPE
     assert call(dC=P + 1) == B.E_ALIGN and call(dZ=P + 1) == B.E_ALIGN and call(dbias=P + 2) == B.E_ALIGN and call(ws=P + 64) == B.E_ALIGN
     assert call(size=need - 1) == B.E_WORKSPACE and call(dZ=P, ldz=40) == B.E_SHAPE and call(dZ=P + 0x1000, ldz=40) == B.E_SHAPE
+
+
+def window_fwd(lib, **kw):
+    a = dict(q=P, k=P, v=P, n=16, q0=8, Hq=4, Hkv=2, dh=64, dtype=B.STREAMBP_BF16, window=4, sinks=1, o=P, lse=P, engine=0)
+    a.update(kw)
+    return lib.streambp_attention_window_forward(*a.values(), None)
+
+
+SIZES = [
+    (dict(n=0), B.E_SHAPE), (dict(n=-1), B.E_SHAPE), (dict(q0=-1), B.E_SHAPE), (dict(n=1 << 31), B.E_SHAPE),
+    (dict(q0=1 << 30), B.E_SHAPE), (dict(Hq=0), B.E_SHAPE), (dict(Hkv=3), B.E_SHAPE), (dict(Hkv=0), B.E_SHAPE), (dict(dh=96), B.E_SHAPE),
+    (dict(window=0), B.E_SHAPE), (dict(window=-5), B.E_SHAPE), (dict(sinks=-1), B.E_SHAPE), (dict(dtype=2), B.E_DTYPE),
+    (dict(Hq=1 << 17, Hkv=1 << 17), B.E_SHAPE),
+]
+
+
+@pytest.mark.parametrize("kw,status", SIZES + [
+    (dict(q=None), B.E_NULL), (dict(k=None), B.E_NULL), (dict(v=None), B.E_NULL), (dict(o=None), B.E_NULL), (dict(lse=None), B.E_NULL),
+    (dict(q=P + 8), B.E_ALIGN), (dict(k=P + 2), B.E_ALIGN), (dict(o=P + 4), B.E_ALIGN), (dict(lse=P + 2), B.E_ALIGN),
+    (dict(engine=5), B.E_SHAPE), (dict(engine=-1), B.E_SHAPE), (dict(dtype=B.STREAMBP_F32, engine=2), B.E_DTYPE)])
+def test_window_forward_refusals(lib, kw, status):
+    assert window_fwd(lib, **kw) == status
+
+
+@pytest.mark.parametrize("kw,status", SIZES + [
+    (dict(d_o=None), B.E_NULL), (dict(dq=None), B.E_NULL), (dict(ws=None), B.E_NULL), (dict(dk=P + 8), B.E_ALIGN),
+    (dict(ws=P + 16), B.E_ALIGN), (dict(size=100), B.E_WORKSPACE), (dict(grad=2), B.E_DTYPE), (dict(grad=1, acc=1), B.E_DTYPE),
+    (dict(dtype=0, grad=1), B.E_DTYPE), (dict(engine=3), B.E_SHAPE), (dict(dtype=0, engine=2), B.E_DTYPE)])
+def test_window_backward_refusals(lib, kw, status):
+    a = dict(q=P, k=P, v=P, o=P, d_o=P, lse=P, n=16, q0=8, Hq=4, Hkv=2, dh=64, dtype=B.STREAMBP_BF16, window=4, sinks=1, grad=0, acc=0,
+             dq=P, dk=P, dv=P, ws=P, size=1 << 20, engine=0)
+    a.update(kw)
+    assert lib.streambp_attention_window_backward(*a.values(), None) == status
+
+
+def test_window_workspace(lib):
+    size = lib.streambp_attention_window_workspace_bytes
+    assert size(16, 8, 4, 2, 64, 4, 1) > 0 and size(16, 8, 4, 2, 96, 4, 1) == 0 and size(16, 8, 4, 3, 64, 4, 1) == 0
+    assert size(0, 8, 4, 2, 64, 4, 1) == 0 and size(16, 8, 4, 2, 64, 0, 1) == 0
+    # what the sinks' segments take is bounded, however many sinks there are
+    assert all(size(32768, 0, 32, 8, 128, 128, s) < (200 << 20) for s in (0, 1, 4, 128, 1000, 16000, 32767, 1 << 20))
+
+
+def _key_work(n, q0, Hkv, window, sinks, T):
+    """The key tiles' work as window.cuh lays it out, restated: (key tile, query tiles, segment) of every item."""
+    kv, qt = q0 + n, -(-n // T)
+    lo = max(0, q0 - window + 1) // T
+    st = min(-(-sinks // T), -(-kv // T))
+    length = max(8, (window + 2 * T - 2) // T + 1)
+    segs = -(-qt // length) if st else 1
+    most = 592 // min(592, st * Hkv) if st else 1
+    if segs > most:
+        length = -(-qt // most)
+        segs = -(-qt // length)
+    first = lambda kt: (kt * T - q0) // T if kt * T > q0 else 0
+    items = []
+    for kt in range(st):
+        for s in range(segs):
+            b = first(kt) + s * length
+            items.append((kt, range(b, qt if segs == 1 else min(qt, b + length)), s if segs > 1 else -1))
+    for kt in range(max(st, lo), -(-kv // T)):
+        last = kt * T + T - 1 + window - 1 - q0
+        items.append((kt, range(first(kt), min(qt, last // T + 1) if last >= 0 else 0), -1))
+    return items
+
+
+def test_key_work_covers_every_visible_pair_once():
+    """Every visible (query, key) pair lies in exactly one item; behind the first segment of a sink tile only sinks are seen."""
+    import random
+    rng = random.Random(0)
+    for _ in range(300):
+        T = rng.choice((4, 8))
+        n, q0 = rng.randrange(1, 90), rng.choice((0, rng.randrange(0, 80)))
+        window, sinks = rng.randrange(1, 60), rng.choice((0, 1, 3, 5, 17, 40))
+        kv = q0 + n
+        window = min(window, kv)
+        sinks = min(sinks, kv)
+        if sinks == kv or window == kv:
+            window, sinks = kv, 0
+        seen = {}
+        for kt, tiles, seg in _key_work(n, q0, rng.choice((1, 8, 200)), window, sinks, T):
+            for qt in tiles:
+                assert 0 <= qt < -(-n // T)
+                for t in range(q0 + qt * T, min(q0 + n, q0 + qt * T + T)):
+                    for j in range(kt * T, min(kv, kt * T + T)):
+                        if j <= t and (t - j < window or j < sinks):
+                            seen[(t, j)] = seen.get((t, j), 0) + 1
+                            assert seg <= 0 or j < sinks
+        want = {(t, j) for t in range(q0, kv) for j in range(t + 1) if t - j < window or j < sinks}
+        assert set(seen) == want and set(seen.values()) <= {1}
