@@ -239,41 +239,23 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return s.cuda_stream
 
 
-def _shared_device(what: str, *tensors: Optional[torch.Tensor]) -> torch.device:
-    """The CUDA device that all the tensors lie on; refuses others, and tensors that are not contiguous."""
-    dev = None
+def _launch(what: str, device: int, stream: Optional[torch.cuda.Stream], fn, *args) -> int:
+    """fn(*args, stream) with the tensors' device current (it need not be the caller's), on the given stream, which must
+    belong to that device, or on that device's current stream."""
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"{what}: the stream belongs to cuda:{stream.device_index}, the tensors lie on cuda:{device}")
+    raw = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
+    if torch._C._cuda_getDevice() == device:
+        return fn(*args, raw)
+    with torch.cuda.device(device):
+        return fn(*args, raw)
+
+
+def _same(what: str, device: int, *tensors) -> None:
+    """All tensors contiguous and on that CUDA device."""
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda or not t.is_contiguous():
-            raise ValueError(f"{what}: tensors must be contiguous CUDA tensors")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError(f"{what}: tensors lie on {dev} and {t.device}")
-    return dev
-
-
-class _Launch:
-    """The tensors' device made current for a call (it need not be the caller's), and the stream the call goes to: the
-    given one, which must belong to that device, or that device's current stream."""
-
-    def __init__(self, what: str, device: torch.device, stream: Optional[torch.cuda.Stream]):
-        if stream is not None and stream.device != device:
-            raise ValueError(f"{what}: the stream belongs to {stream.device}, the tensors lie on {device}")
-        self.other = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-        self.device, self.stream = device, stream
-
-    def __enter__(self) -> int:
-        if self.other is not None:
-            self.other.__enter__()
-        if self.stream is not None:
-            return self.stream.cuda_stream
-        return torch._C._cuda_getCurrentRawStream(self.device.index)      # current_stream() without building an object
-
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
+        if t.get_device() != device or device < 0 or not t.is_contiguous():
+            raise ValueError(f"{what}: tensors must be contiguous CUDA tensors on one device")
 
 
 def _want(ok: bool, what: str, rule: str) -> None:
@@ -591,9 +573,9 @@ def gemm_epilogue(A, W, C_out, bias=None, activation: str = "none", residual=Non
     c, r, z = (_rows(what, dev, dt, (M, N), t) for t in (C_out, residual, pre))
     if bias is not None and (bias.get_device() != dev or bias.dtype != dt or tuple(bias.shape) != (N,) or not bias.is_contiguous()):
         raise ValueError(f"{what}: bias is a contiguous {dt} vector of {N} on cuda:{dev}")
-    with _Launch(what, A.device, stream) as s:
-        st = lib().streambp_gemm_epilogue(a[0], a[1], w[0], w[1], M, N, K, None if bias is None else bias.data_ptr(),
-                                          ACTIVATIONS[activation], r[0], r[1], c[0], c[1], z[0], z[1], _dtype_code(dt), s)
+    st = _launch(what, dev, stream, lib().streambp_gemm_epilogue, a[0], a[1], w[0], w[1], M, N, K,
+                 None if bias is None else bias.data_ptr(), ACTIVATIONS[activation], r[0], r[1], c[0], c[1], z[0], z[1],
+                 _dtype_code(dt))
     if check:
         _check(st, "streambp_gemm_epilogue")
     return st
@@ -615,11 +597,10 @@ def gemm_epilogue_backward(dC, pre, activation: str, dZ=None, dbias=None, worksp
         raise ValueError(f"{what}: dbias is a contiguous fp32 vector of {N} on cuda:{dev}")
     if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError(f"{what}: workspace is contiguous, on cuda:{dev}")
-    with _Launch(what, dC.device, stream) as s:
-        st = lib().streambp_gemm_epilogue_backward(d[0], d[1], z[0], z[1], ACTIVATIONS[activation], M, N, g[0], g[1],
-                                                   None if dbias is None else dbias.data_ptr(), 1 if accumulate else 0,
-                                                   _dtype_code(dt), None if workspace is None else workspace.data_ptr(),
-                                                   0 if workspace is None else workspace.numel() * workspace.element_size(), s)
+    st = _launch(what, dev, stream, lib().streambp_gemm_epilogue_backward, d[0], d[1], z[0], z[1], ACTIVATIONS[activation], M, N,
+                 g[0], g[1], None if dbias is None else dbias.data_ptr(), 1 if accumulate else 0, _dtype_code(dt),
+                 None if workspace is None else workspace.data_ptr(),
+                 0 if workspace is None else workspace.numel() * workspace.element_size())
     if check:
         _check(st, "streambp_gemm_epilogue_backward")
     return st
@@ -694,26 +675,29 @@ def attention_backward_static(q, k, v, o, d_o, lse, q0: int, dq, dk, dv, engine:
     return st
 
 
-def _window_args(what: str, q, k, v, q0: int, others) -> tuple:
-    """Checks of a windowed call: q [n, Hq, dh], k and v [q0 + n, Hkv, dh], `others` (tensor, shape, dtypes) each."""
-    _want(q.dim() == 3 and k.dim() == 3 and q0 >= 0, what, "q [n, Hq, dh] and k [q0 + n, Hkv, dh], q0 >= 0")
-    n, Hq, dh = q.shape
-    _want(tuple(k.shape) == (q0 + n, k.shape[1], dh) and k.shape == v.shape, what, f"k and v are [{q0 + n}, Hkv, {dh}]")
-    _want(k.dtype == q.dtype and v.dtype == q.dtype, what, "q, k and v share a type")
-    for t, shape, dtypes in others:
-        _want(tuple(t.shape) == shape and t.dtype in dtypes, what, f"expected {shape} {dtypes}, got {tuple(t.shape)} {t.dtype}")
-    return n, Hq, k.shape[1], dh
+def _window_args(what: str, q, k, v, q0: int) -> tuple:
+    """Sizes of a windowed call: q [n, Hq, dh], k and v [q0 + n, Hkv, dh]."""
+    if q.dim() != 3 or k.dim() != 3 or q0 < 0:
+        raise ValueError(f"{what}: q is [n, Hq, dh], k and v are [q0 + n, Hkv, dh], q0 >= 0")
+    shape, (n, Hq, dh), kv = q.shape, q.shape, k.shape
+    if kv[0] != q0 + n or kv[2] != dh or v.shape != kv:
+        raise ValueError(f"{what}: k and v are [{q0 + n}, Hkv, {dh}], got {tuple(kv)} and {tuple(v.shape)}")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError(f"{what}: q, k and v share a type")
+    return n, Hq, kv[1], dh, shape, kv
 
 
 def attention_window_forward(q, k, v, q0: int, window: int, sinks: int, o, lse, engine: int = 0, stream=None,
                              check: bool = True) -> int:
     """streambp_attention_window_forward; q, o: [n, Hq, dh], k, v: [q0+n, Hkv, dh], lse: [Hq, n] fp32."""
-    what, Hq_n = "attention_window_forward", (q.shape[1], q.shape[0])
-    n, Hq, Hkv, dh = _window_args(what, q, k, v, q0, ((o, tuple(q.shape), (q.dtype,)), (lse, Hq_n, (torch.float32,))))
-    dev = _shared_device(what, q, k, v, o, lse)
-    with _Launch(what, dev, stream) as s:
-        st = lib().streambp_attention_window_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), n, q0, Hq, Hkv, dh,
-                                                     _dtype_code(q.dtype), window, sinks, o.data_ptr(), lse.data_ptr(), engine, s)
+    what = "attention_window_forward"
+    n, Hq, Hkv, dh, shape, _ = _window_args(what, q, k, v, q0)
+    if o.shape != shape or o.dtype != q.dtype or lse.shape != (Hq, n) or lse.dtype != torch.float32:
+        raise ValueError(f"{what}: o is like q, lse is fp32 [{Hq}, {n}]")
+    dev = q.get_device()
+    _same(what, dev, q, k, v, o, lse)
+    st = _launch(what, dev, stream, lib().streambp_attention_window_forward, q.data_ptr(), k.data_ptr(), v.data_ptr(), n, q0, Hq,
+                 Hkv, dh, _dtype_code(q.dtype), window, sinks, o.data_ptr(), lse.data_ptr(), engine)
     if check:
         _check(st, "streambp_attention_window_forward")
     return st
@@ -728,18 +712,20 @@ def attention_window_backward(q, k, v, o, d_o, lse, q0: int, window: int, sinks:
                               accumulate: bool = False, engine: int = 0, stream=None, check: bool = True) -> int:
     """streambp_attention_window_backward; dq, dk, dv share a type (fp32, or bf16 for bf16 storage): overwritten, or with
     accumulate=True (fp32) dk and dv are added to."""
-    what, kv = "attention_window_backward", tuple(k.shape)
-    grads = (dq.dtype,)
-    _want(dq.dtype in (torch.float32, torch.bfloat16), what, "gradients are fp32 or bf16")
-    n, Hq, Hkv, dh = _window_args(what, q, k, v, q0, (
-        (o, tuple(q.shape), (q.dtype,)), (d_o, tuple(q.shape), (q.dtype,)), (lse, (q.shape[1], q.shape[0]), (torch.float32,)),
-        (dq, tuple(q.shape), grads), (dk, kv, grads), (dv, kv, grads)))
-    dev = _shared_device(what, q, k, v, o, d_o, lse, dq, dk, dv, workspace)
-    with _Launch(what, dev, stream) as s:
-        st = lib().streambp_attention_window_backward(
-            q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), d_o.data_ptr(), lse.data_ptr(), n, q0, Hq, Hkv, dh,
-            _dtype_code(q.dtype), window, sinks, _dtype_code(dq.dtype), 1 if accumulate else 0, dq.data_ptr(), dk.data_ptr(),
-            dv.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), engine, s)
+    what = "attention_window_backward"
+    n, Hq, Hkv, dh, shape, kv = _window_args(what, q, k, v, q0)
+    if (o.shape != shape or d_o.shape != shape or o.dtype != q.dtype or d_o.dtype != q.dtype or lse.shape != (Hq, n) or
+            lse.dtype != torch.float32):
+        raise ValueError(f"{what}: o and d_o are like q, lse is fp32 [{Hq}, {n}]")
+    grad = dq.dtype
+    if dq.shape != shape or dk.shape != kv or dv.shape != kv or dk.dtype != grad or dv.dtype != grad:
+        raise ValueError(f"{what}: dq, dk and dv have the shapes of q, k and v and share a type")
+    dev = q.get_device()
+    _same(what, dev, q, k, v, o, d_o, lse, dq, dk, dv, workspace)
+    st = _launch(what, dev, stream, lib().streambp_attention_window_backward, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                 o.data_ptr(), d_o.data_ptr(), lse.data_ptr(), n, q0, Hq, Hkv, dh, _dtype_code(q.dtype), window, sinks,
+                 _dtype_code(grad), 1 if accumulate else 0, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(),
+                 workspace.numel() * workspace.element_size(), engine)
     if check:
         _check(st, "streambp_attention_window_backward")
     return st
@@ -787,7 +773,8 @@ class AdamWPlan:
         _want(len(tensors) > 0, what, "needs at least one tensor")
         self.tensors = [dict(t) for t in tensors]
         p0, m0 = self.tensors[0]["param"], self.tensors[0]["m"]
-        self.device = _shared_device(what, p0)
+        _same(what, p0.get_device(), p0)
+        self.device = p0.device
         self.param_dtype, index, f32 = _dtype_code(p0.dtype), p0.get_device(), torch.float32
         _want(m0.dtype in (f32, torch.uint8), what, "m is fp32 or uint8 codes")
         mx8 = m0.dtype == torch.uint8
@@ -841,8 +828,8 @@ def adamw_step(plan: AdamWPlan, lr: float, beta1: float, beta2: float, eps: floa
         _want(grad_scale.dtype == torch.float32 and grad_scale.numel() == 1 and grad_scale.device == plan.device,
               "adamw_step", "grad_scale is one fp32 value on the tensors' device")
     c = AdamWCfgC(lr, beta1, beta2, eps, plan.param_dtype, plan.state_dtype, 0 if on_device else int(step))
-    with _Launch("adamw_step", plan.device, stream) as s:
-        st = lib().streambp_adamw_step(C.byref(c), plan.c, len(plan), _ptr(grad_scale), _ptr(step) if on_device else None, s)
+    st = _launch("adamw_step", plan.device.index, stream, lib().streambp_adamw_step, C.byref(c), plan.c, len(plan),
+                 None if grad_scale is None else grad_scale.data_ptr(), step.data_ptr() if on_device else None)
     if check:
         _check(st, "streambp_adamw_step")
     return st
@@ -857,10 +844,10 @@ def grad_norm(plan: AdamWPlan, max_norm: float, norm: torch.Tensor, scale: Optio
     """streambp_grad_norm over the gradients of a plan: norm and scale (or None) are fp32 CUDA tensors of one value."""
     for t in (norm, scale):
         _want(t is None or (t.dtype == torch.float32 and t.numel() == 1), "grad_norm", "norm and scale are one fp32 value each")
-    _want(_shared_device("grad_norm", norm, scale, workspace) == plan.device, "grad_norm", "outputs lie on another device")
-    with _Launch("grad_norm", plan.device, stream) as s:
-        st = lib().streambp_grad_norm(plan.grads, plan.counts, len(plan), max_norm, _ptr(norm), _ptr(scale),
-                                      _ptr(workspace), workspace.numel() * workspace.element_size(), s)
+    _same("grad_norm", plan.device.index, *((norm, workspace) if scale is None else (norm, workspace, scale)))
+    st = _launch("grad_norm", plan.device.index, stream, lib().streambp_grad_norm, plan.grads, plan.counts, len(plan), max_norm,
+                 norm.data_ptr(), None if scale is None else scale.data_ptr(), workspace.data_ptr(),
+                 workspace.numel() * workspace.element_size())
     if check:
         _check(st, "streambp_grad_norm")
     return st
@@ -873,9 +860,9 @@ def mx8_encode(values: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, 
     _want(values.dtype == torch.float32 and codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and
           codes.numel() == n and scales.numel() == (n + MX8_BLOCK - 1) // MX8_BLOCK, "mx8_encode",
           "fp32 values, uint8 codes of the same size, one uint8 scale per 32")
-    dev = _shared_device("mx8_encode", values, codes, scales)
-    with _Launch("mx8_encode", dev, stream) as s:
-        st = lib().streambp_mx8_encode(_ptr(values), n, 1 if keep_nonzero else 0, _ptr(codes), _ptr(scales), s)
+    _same("mx8_encode", values.get_device(), values, codes, scales)
+    st = _launch("mx8_encode", values.get_device(), stream, lib().streambp_mx8_encode, values.data_ptr(), n,
+                 1 if keep_nonzero else 0, codes.data_ptr(), scales.data_ptr())
     if check:
         _check(st, "streambp_mx8_encode")
     return st
@@ -887,9 +874,9 @@ def mx8_decode(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, str
     _want(codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and out.numel() == n and
           scales.numel() == (n + MX8_BLOCK - 1) // MX8_BLOCK, "mx8_decode",
           "uint8 codes, one uint8 scale per 32, as many values out")
-    dev = _shared_device("mx8_decode", codes, scales, out)
-    with _Launch("mx8_decode", dev, stream) as s:
-        st = lib().streambp_mx8_decode(_ptr(codes), _ptr(scales), n, _ptr(out), _dtype_code(out.dtype), s)
+    _same("mx8_decode", codes.get_device(), codes, scales, out)
+    st = _launch("mx8_decode", codes.get_device(), stream, lib().streambp_mx8_decode, codes.data_ptr(), scales.data_ptr(), n,
+                 out.data_ptr(), _dtype_code(out.dtype))
     if check:
         _check(st, "streambp_mx8_decode")
     return st
