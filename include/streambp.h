@@ -426,8 +426,7 @@ int streambp_attention_backward(const void *q, const void *k, const void *v, con
  * backward).  grad_dtype STREAMBP_BF16 (bf16 storage only, accumulate = 0): all three are overwritten, rounded once from
  * fp32 sums.  Overwritten dk and dv rows that no query sees become 0.  Every later query adds to the gradients of the
  * sinks; their sums are formed in segments through the workspace and joined in a fixed order, so all results are
- * reproducible bit by bit.  engine: 0 automatic, 1 CUDA cores, 2 tensor cores (bf16); the forward also takes 3 / 4 =
- * tensor cores with one / two 128-query tiles per CTA.
+ * reproducible bit by bit.  engine: 0 automatic, 1 CUDA cores, 2 tensor cores (bf16).
  */
 int streambp_attention_window_forward(const void *q, const void *k, const void *v, int64_t n, int64_t q0,
                                       int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,

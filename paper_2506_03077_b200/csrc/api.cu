@@ -732,7 +732,7 @@ int streambp_attention_window_forward(const void *q, const void *k, const void *
     if (dtype != STREAMBP_F32 && dtype != STREAMBP_BF16) return STREAMBP_E_DTYPE;
     WindowShape w;
     SBP_TRY(window_shape(n, q0, n_q_heads, n_kv_heads, head_dim, window, sinks, &w));
-    if (engine < 0 || engine > 4) return STREAMBP_E_SHAPE;
+    if (engine < 0 || engine > 2) return STREAMBP_E_SHAPE;
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || !aligned(lse, 4)) return STREAMBP_E_ALIGN;
     if (dtype == STREAMBP_F32 && engine >= 2) return STREAMBP_E_DTYPE;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -743,8 +743,7 @@ int streambp_attention_window_forward(const void *q, const void *k, const void *
     const bool tc = attention_window_tc_available();
     if (engine >= 2 && !tc) return STREAMBP_E_SHAPE;
     if (engine != 1 && tc)
-        return attention_window_fwd_tc((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, w, head_dim, (bf16 *)o, lse, st,
-                                       engine == 3 ? 1 : (engine == 4 ? 2 : 0));
+        return attention_window_fwd_tc((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, w, head_dim, (bf16 *)o, lse, st);
     return attention_window_fwd_simt<bf16>((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, w, head_dim, (bf16 *)o, lse, st);
 }
 

@@ -1,16 +1,20 @@
 // Attention with a sliding window and sink keys on tcgen05 tensor cores (bf16 operands, head_dim 64 or 128): the queries
 // of one chunk against the key tiles their window reaches and the tiles that hold sinks; nothing else is loaded.
 //
-// Forward (attn_window_fwd_kernel): a CTA owns TEAMS adjacent 128-query tiles of one head.
-//   warp 0      : TMA producer -- the query tiles once, then K and V tiles of 128 keys through rings
-//   warp 1      : MMA issuer (warp-uniform issue) -- per key tile and team S = Q K^T into tensor memory when the team has
-//                 handed over its previous P, then O += P V with P read from tensor memory (packed over the columns of S:
-//                 the product that reads P is queued before the one that overwrites S, one thread's MMAs run in order)
-//   other warps : softmax, four per team -- a thread owns a query row: 128 scores in registers, row maximum and sum private;
-//                 the running output is rescaled only when a row's maximum grows by more than 2^8 (exact: the final
-//                 division uses the same reference)
-// A row may see nothing of the first tiles of its CTA's list: its maximum stays -infinity and it adds exact zeros until it
-// sees a key.  Every query sees its own key, so no row ends empty.
+// Forward (attn_window_fwd_kernel): two persistent CTAs per SM, each walking (query tile, head) items.
+//   warp 0      : TMA producer -- query tiles, K and V tiles of 128 keys through rings; runs ahead into the next item
+//   warp 1      : MMA issuer (warp-uniform issue) -- S = Q K^T into tensor memory, O += P V with P read from tensor memory
+//                 (packed over the columns of S: the product that reads P is queued before the one that overwrites S, one
+//                 thread's MMAs run in order); behind an item's last P V comes the next item's first S
+//   warps 2..5  : softmax -- a thread owns a query row: 128 scores in registers, row maximum and sum private; the running
+//                 output is rescaled only when a row's maximum grows by more than 2^8 (exact: the final division uses the
+//                 same reference)
+// What two CTAs of one chain each buy: one's latencies (tensor-memory loads, hand-offs, the P V -> next S chain) fall into
+// the other's exponentials, and short windows -- a handful of key tiles between fetching queries and storing outputs -- pay
+// neither launch nor set-up nor first loads per tile.
+// A row may see nothing of the first tiles of its list: its maximum stays -infinity and it adds exact zeros until it sees
+// a key.  Every query sees its own key, so no row ends empty.  Groups of 32 columns that no row of a warp sees are skipped,
+// and the sink tile that the window does not reach is cut to its sinks (16 columns for up to 16 of them).
 //
 // Backward (attn_window_bwd_kernel): two CTA roles in one grid, both deterministic (no floating-point atomics).
 //   dK/dV: one CTA per (key tile, KV head) loops over the query heads of the group and the query tiles that see the tile;
@@ -89,238 +93,327 @@ struct FwdParams {
     bf16 *o;            // [n, Hq, DH]
     float *lse;         // [Hq, n]
     float scale_log2;   // log2(e) / sqrt(head_dim)
+    int q_tiles, items; // items = q_tiles * Hq, the last query tiles (longest spans) first, the heads of a tile side by side
+    int edge, edge_keys;// the sink tile that holds sinks in its first rows only (-1: none), and those rows rounded up to 16
 };
 
-template <int DH, int TEAMS, int ST> struct Fwd {       // ST: stages of the K and of the V ring
+template <int DH> struct Fwd {
     static constexpr int kTile = TILE * DH * 2;
-    static constexpr int kThreads = 64 + 128 * TEAMS;
-    static constexpr int kSmem = (TEAMS + 2 * ST) * kTile + 1024 + 256;
-    static constexpr uint32_t kCols = TEAMS == 2 ? 512 : 256;
-    static constexpr int kBlocks = TEAMS == 1 ? 2 : 1;
+    static constexpr int kRing = DH == 64 ? 2 : 1;         // stages of the Q, K and V rings: what leaves room for two CTAs
+    static constexpr int kThreads = 64 + 128;
+    static constexpr int kStaging = 4 * 2048;              // a 32 x 32 block of O per softmax warp
+    static constexpr int kSmem = 3 * kRing * kTile + kStaging + 1024 + 256;
+    static_assert(2 * (kSmem + 1024) <= 233472, "two CTAs share an SM");
+};
+struct RingAt {                                            // stage and phase of the next use of a ring of N stages
+    uint32_t st = 0, ph = 0;
+    template <int N> __device__ __forceinline__ void next() {
+        if (++st == N) { st = 0; ph ^= 1u; }
+    }
 };
 
-template <int DH, int TEAMS, int ST>
-__global__ void __launch_bounds__(Fwd<DH, TEAMS, ST>::kThreads, Fwd<DH, TEAMS, ST>::kBlocks)
+// The running maximum of a row takes in the maximum `mt` of a tile; O (at rest: S complete implies the product with the
+// previous P complete, same issuing thread, in order) and l are rescaled where it grew by more than 2^8.
+template <int DH>
+__device__ __forceinline__ void take_maximum(float mt, uint32_t tO, bool later, float &m_used, float &l) {
+    float factor = 1.f;
+    const bool grow = mt > m_used + 8.f;                  // also true on the first tile with a visible key
+    if (grow) {
+        factor = fast_exp2(m_used - mt);
+        m_used = mt;
+        l *= factor;
+    }
+    if (later && __any_sync(0xffffffffu, grow)) {
+#pragma unroll 1
+        for (int c = 0; c < DH / 32; c++) {
+            uint32_t o[32];
+            tmem_ld32(tO + c * 32, o);
+#pragma unroll
+            for (int e = 0; e < 32; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+            tmem_st32(tO + c * 32, o);
+        }
+    }
+}
+
+// A key tile that the row sees whole: 128 scores in registers, P packed over the first 64 columns of S.
+template <int DH>
+__device__ __forceinline__ void softmax_whole(float scale_log2, uint32_t tS, uint32_t tO, bool later, float &m_used, float &l) {
+    uint32_t r[128];
+#pragma unroll
+    for (int c = 0; c < 4; c++) tmem_ld32_async(tS + c * 32, r + c * 32);
+    tmem_wait_ld();
+    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int e = 0; e < 128; e++) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(r[e]));
+    take_maximum<DH>(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale_log2, tO, later, m_used, l);
+    const float neg_m = -m_used;
+    float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 8; c++) {                        // 16 scores -> 8 packed words per step
+        uint32_t pk[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float p0 = fast_exp2(fmaf(__uint_as_float(r[c * 16 + e]), scale_log2, neg_m));
+            const float p1 = fast_exp2(fmaf(__uint_as_float(r[c * 16 + e + 1]), scale_log2, neg_m));
+            l4[(e >> 1) & 3] += p0 + p1;
+            pk[e >> 1] = pack_bf16(p0, p1);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) r[c * 8 + e] = pk[e];  // packed P reuses the registers of consumed scores
+    }
+    l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        uint32_t wd[16];
+#pragma unroll
+        for (int e = 0; e < 16; e++) wd[e] = r[c * 16 + e];
+        tmem_st16(tS + c * 16, wd);
+    }
+}
+
+// A key tile that holds keys the row does not see, or an edge tile of `keys` columns: 32 columns at a time, once for the
+// maximum and once for P (columns 16 c .. of P lie over scores that have been read by then), groups that no row of the warp
+// sees left out.  With all 128 scores in registers under those conditions the compiler spilled a kilobyte and a half.
+template <int DH>
+__device__ __forceinline__ void softmax_hidden(const FwdParams &p, uint32_t tS, uint32_t tO, int q_abs, int k0, int keys, bool later,
+                                               float &m_used, float &l) {
+    uint32_t see[4], any = 0u;
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        see[c] = visible_keys(p.w, q_abs, k0, c * 32);
+        any |= __any_sync(0xffffffffu, see[c] != 0u) ? 1u << c : 0u;
+    }
+    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        if (!(any >> c & 1u)) continue;
+        uint32_t r[32];
+        tmem_ld32(tS + c * 32, r);
+#pragma unroll
+        for (int e = 0; e < 32; e++)
+            m4[e & 3] = fmaxf(m4[e & 3], (see[c] >> e & 1u) ? __uint_as_float(r[e]) : -INFINITY);
+    }
+    take_maximum<DH>(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2, tO, later, m_used, l);
+    const float neg_m = m_used == -INFINITY ? 0.f : -m_used;        // nothing seen so far: exact zeros
+    float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        if (c * 32 >= keys) continue;                               // the product does not read these
+        uint32_t pk[16];
+        if (any >> c & 1u) {
+            uint32_t r[32];
+            tmem_ld32(tS + c * 32, r);
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+                const float x0 = (see[c] >> e & 1u) ? __uint_as_float(r[e]) : -INFINITY;
+                const float x1 = (see[c] >> (e + 1) & 1u) ? __uint_as_float(r[e + 1]) : -INFINITY;
+                const float p0 = fast_exp2(fmaf(x0, p.scale_log2, neg_m)), p1 = fast_exp2(fmaf(x1, p.scale_log2, neg_m));
+                l4[(e >> 1) & 3] += p0 + p1;
+                pk[e >> 1] = pack_bf16(p0, p1);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; e++) pk[e] = 0u;
+        }
+        tmem_st16(tS + c * 16, pk);
+    }
+    l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+}
+
+template <int DH>
+__global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
     attn_window_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                           const __grid_constant__ CUtensorMap map_v, const FwdParams p) {
+                           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_ke,
+                           const __grid_constant__ CUtensorMap map_ve, const __grid_constant__ CUtensorMap map_o, const FwdParams p) {
     pdl_enter();
-    typedef Fwd<DH, TEAMS, ST> F;
+    typedef Fwd<DH> F;
+    constexpr int N = F::kRing;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
-    const uint32_t sQ = base, sK = sQ + TEAMS * F::kTile, sV = sK + ST * F::kTile;
-    uint8_t *aux = smem_raw + (base - raw) + (TEAMS + 2 * ST) * F::kTile;
+    const uint32_t sQ = base, sK = sQ + N * F::kTile, sV = sK + N * F::kTile, sO = sV + N * F::kTile;
+    uint8_t *aux = smem_raw + (base - raw) + 3 * N * F::kTile + F::kStaging;
     const uint32_t bars = smem_u32(aux);
-    const uint32_t q_full = bars, k_full = bars + 8, k_empty = k_full + 8 * ST, v_full = k_empty + 8 * ST,
-                   v_empty = v_full + 8 * ST, s_full = v_empty + 8 * ST, p_full = s_full + 16, o_done = p_full + 16;
+    const uint32_t q_full = bars, q_empty = q_full + 8 * N, k_full = q_empty + 8 * N, k_empty = k_full + 8 * N,
+                   v_full = k_empty + 8 * N, v_empty = v_full + 8 * N, s_full = v_empty + 8 * N, p_full = s_full + 8,
+                   o_done = p_full + 8;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(aux + 192);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(aux + 200);
-
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int h = blockIdx.x, g = h / (p.w.Hq / p.w.Hkv);
-    const int qt0 = (int)(gridDim.y - 1 - blockIdx.y) * TEAMS * TILE;     // the longest spans are dispatched first
-    // rows of team x (absolute): first[x] .. last[x], none if last < first
-    int first[TEAMS], last[TEAMS];
-#pragma unroll
-    for (int x = 0; x < TEAMS; x++) {
-        const int r = qt0 + x * TILE, rows = p.w.n - r < TILE ? p.w.n - r : TILE;
-        first[x] = p.w.q0 + r;
-        last[x] = rows > 0 ? first[x] + rows - 1 : first[x] - 1;
-    }
-    const int last_all = TEAMS == 2 && last[TEAMS - 1] >= first[TEAMS - 1] ? last[TEAMS - 1] : last[0];
-    const KeySpan span = key_span<TILE>(p.w, first[0], last_all);
-    const int count = span.count();
-    auto active = [&](int x, int kt) { return TEAMS == 1 || (last[x] >= first[x] && sees<TILE>(p.w, kt, first[x], last[x])); };
 
     if (threadIdx.x == 0) {
-        mbar_init(q_full, 1);
-        for (int s = 0; s < ST; s++) {
+        for (int s = 0; s < N; s++) {
+            mbar_init(q_full + 8 * s, 1);
+            mbar_init(q_empty + 8 * s, 1);
             mbar_init(k_full + 8 * s, 1);
             mbar_init(k_empty + 8 * s, 1);
             mbar_init(v_full + 8 * s, 1);
             mbar_init(v_empty + 8 * s, 1);
         }
-        for (int x = 0; x < 2; x++) {
-            mbar_init(s_full + 8 * x, 1);
-            mbar_init(p_full + 8 * x, 4);
-            mbar_init(o_done + 8 * x, 1);
-        }
+        mbar_init(s_full, 1);
+        mbar_init(p_full, 4);
+        mbar_init(o_done, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), F::kCols);
+    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 256);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;      // S of the teams (128 columns each), then their O (DH columns each)
+    const uint32_t tmem = *tmem_slot;      // S (128 columns), O (DH columns)
+
+    // an item: one query tile of one head
+    struct Item { int h, qt0, first, last; KeySpan span; };
+    auto item_at = [&](int i) {
+        Item t;
+        t.h = i % p.w.Hq;
+        t.qt0 = (p.q_tiles - 1 - i / p.w.Hq) * TILE;
+        const int rows = p.w.n - t.qt0 < TILE ? p.w.n - t.qt0 : TILE;
+        t.first = p.w.q0 + t.qt0;
+        t.last = t.first + rows - 1;
+        t.span = key_span<TILE>(p.w, t.first, t.last);
+        return t;
+    };
+    // keys of a tile that take part: all, or the sinks at the head of the edge tile where the window does not reach it
+    auto keys_of = [&](const Item &t, int j) { return j < t.span.ns && j == p.edge ? p.edge_keys : TILE; };
 
     if (warp == 0) {
         if (lane == 0) {
-            const int teams = TEAMS == 2 && last[TEAMS - 1] >= first[TEAMS - 1] ? 2 : 1;
-            mbar_expect_tx(q_full, teams * F::kTile);
-            for (int x = 0; x < teams; x++) load_tile<DH>(sQ + x * F::kTile, &map_q, q_full, h, qt0 + x * TILE);
-            for (int j = 0; j < count; j++) {
-                const uint32_t st = j % ST, ph = (j / ST) & 1;
-                const int row = span.tile(j) * TILE;
-                if (!mbar_wait(k_empty + 8 * st, ph ^ 1u, abort_flag)) break;
-                mbar_expect_tx(k_full + 8 * st, F::kTile);
-                load_tile<DH>(sK + st * F::kTile, &map_k, k_full + 8 * st, g, row);
-                if (!mbar_wait(v_empty + 8 * st, ph ^ 1u, abort_flag)) break;
-                mbar_expect_tx(v_full + 8 * st, F::kTile);
-                load_tile<DH>(sV + st * F::kTile, &map_v, v_full + 8 * st, g, row);
+            RingAt q, kv;
+            bool alive = true;
+            for (int i = blockIdx.x; i < p.items && alive; i += gridDim.x) {
+                const Item t = item_at(i);
+                const int g = t.h / (p.w.Hq / p.w.Hkv), count = t.span.count();
+                if (!mbar_wait(q_empty + 8 * q.st, q.ph ^ 1u, abort_flag)) break;
+                mbar_expect_tx(q_full + 8 * q.st, F::kTile);
+                load_tile<DH>(sQ + q.st * F::kTile, &map_q, q_full + 8 * q.st, t.h, t.qt0);
+                q.next<N>();
+                for (int j = 0; j < count; j++) {
+                    const int row = t.span.tile(j) * TILE, keys = keys_of(t, j);
+                    const bool part = keys < TILE;
+                    const uint32_t bytes = (uint32_t)keys * DH * 2u;
+                    if (!mbar_wait(k_empty + 8 * kv.st, kv.ph ^ 1u, abort_flag)) { alive = false; break; }
+                    mbar_expect_tx(k_full + 8 * kv.st, bytes);
+                    load_tile<DH>(sK + kv.st * F::kTile, part ? &map_ke : &map_k, k_full + 8 * kv.st, g, row);
+                    if (!mbar_wait(v_empty + 8 * kv.st, kv.ph ^ 1u, abort_flag)) { alive = false; break; }
+                    mbar_expect_tx(v_full + 8 * kv.st, bytes);
+                    load_tile<DH>(sV + kv.st * F::kTile, part ? &map_ve : &map_v, v_full + 8 * kv.st, g, row);
+                    kv.next<N>();
+                }
             }
         }
     } else if (warp == 1) {
-        constexpr uint32_t idesc_s = make_idesc(TILE, TILE, false, false);
         constexpr uint32_t idesc_pv = make_idesc(TILE, DH, false, true);
-        bool alive = mbar_wait_warp(q_full, 0, abort_flag);
-        uint32_t used[TEAMS] = {};                      // P tiles taken from each team
-        auto issue_s = [&](int x, int j) {              // S_x = Q_x K_j^T (K_j is in shared memory)
-            const uint32_t q_lo = klo(sQ + x * F::kTile), k_lo = klo(sK + (j % ST) * F::kTile);
-#pragma unroll
-            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tmem + x * TILE, q_lo + kstep(kk), k_lo + kstep(kk), idesc_s, kk != 0);
-            umma_commit_w(s_full + 8 * x);
-        };
-        auto issue_pv = [&](int x, int j) -> bool {     // O_x += P_x V_j once the team has stored P_x
-            if (!mbar_wait_warp(p_full + 8 * x, used[x] & 1, abort_flag)) return false;
+        RingAt q, k, v;                                 // next use by S, by S, by P V
+        uint32_t steps = 0;                             // P tiles taken
+        bool alive = true;
+        // S = Q K_j^T of item t; the last of an item hands the query tile back
+        auto issue_s = [&](const Item &t, int j) -> bool {
+            if (j == 0 && !mbar_wait_warp(q_full + 8 * q.st, q.ph, abort_flag)) return false;
+            if (!mbar_wait_warp(k_full + 8 * k.st, k.ph, abort_flag)) return false;
             tc_fence_after();
-            const uint32_t v_lo = mnlo(sV + (j % ST) * F::kTile);
+            const uint32_t q_lo = klo(sQ + q.st * F::kTile), k_lo = klo(sK + k.st * F::kTile);
+            const uint32_t idesc_s = make_idesc(TILE, keys_of(t, j), false, false);
 #pragma unroll
-            for (int kk = 0; kk < 8; kk++)
-                umma_ts_w(tmem + TEAMS * TILE + x * DH, tmem + x * TILE + kk * 8, v_lo + mnstep(kk), idesc_pv, used[x] | (uint32_t)kk);
-            used[x]++;
-            if (span.tile(j) == last[x] / TILE) umma_commit_w(o_done + 8 * x);
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tmem, q_lo + kstep(kk), k_lo + kstep(kk), idesc_s, kk != 0);
+            umma_commit_w(s_full);
+            umma_commit_w(k_empty + 8 * k.st);
+            k.next<N>();
+            if (j == t.span.count() - 1) {
+                umma_commit_w(q_empty + 8 * q.st);
+                q.next<N>();
+            }
             return true;
         };
-        if (alive) alive = mbar_wait_warp(k_full, 0, abort_flag);
-        if (alive) {
-            tc_fence_after();
-#pragma unroll
-            for (int x = 0; x < TEAMS; x++)
-                if (active(x, span.tile(0))) issue_s(x, 0);
-            umma_commit_w(k_empty);
+        Item t;
+        if ((int)blockIdx.x < p.items) {
+            t = item_at(blockIdx.x);
+            alive = issue_s(t, 0);
         }
-        for (int j = 0; j < count && alive; j++) {
-            const uint32_t st = j % ST, ph = (j / ST) & 1;
-            const int n = j + 1;
-            if (!mbar_wait_warp(v_full + 8 * st, ph, abort_flag)) { alive = false; break; }
-            if (n < count && !mbar_wait_warp(k_full + 8 * (n % ST), (n / ST) & 1, abort_flag)) { alive = false; break; }
-            tc_fence_after();
+        for (int i = blockIdx.x; i < p.items && alive; i += gridDim.x) {
+            const int count = t.span.count();
+            for (int j = 0; j < count; j++) {
+                // O += P V_j once P is stored; then S of the next tile (of the next item behind the last) over P's columns
+                if (!mbar_wait_warp(p_full, steps & 1, abort_flag) || !mbar_wait_warp(v_full + 8 * v.st, v.ph, abort_flag)) { alive = false; break; }
+                tc_fence_after();
+                const uint32_t v_lo = mnlo(sV + v.st * F::kTile);
+                const int slices = keys_of(t, j) / 16;
+                if (slices == 8) {
 #pragma unroll
-            for (int x = 0; x < TEAMS; x++) {
-                if (alive && active(x, span.tile(j))) alive = issue_pv(x, j);
-                if (alive && n < count && active(x, span.tile(n))) issue_s(x, n);
+                    for (int kk = 0; kk < 8; kk++)
+                        umma_ts_w(tmem + TILE, tmem + kk * 8, v_lo + mnstep(kk), idesc_pv, (j | kk) != 0);
+                } else {
+                    for (int kk = 0; kk < slices; kk++)
+                        umma_ts_w(tmem + TILE, tmem + kk * 8, v_lo + mnstep(kk), idesc_pv, (j | kk) != 0);
+                }
+                umma_commit_w(v_empty + 8 * v.st);
+                v.next<N>();
+                steps++;
+                if (j + 1 < count) {
+                    alive = issue_s(t, j + 1);
+                } else {
+                    umma_commit_w(o_done);
+                    if (i + (int)gridDim.x < p.items) {
+                        t = item_at(i + gridDim.x);
+                        alive = issue_s(t, 0);
+                    }
+                }
+                if (!alive) break;
             }
-            if (!alive) break;
-            umma_commit_w(v_empty + 8 * st);
-            if (n < count) umma_commit_w(k_empty + 8 * (n % ST));
         }
     } else {
-        const int x = TEAMS == 2 ? (warp - 2) >> 2 : 0;
         const int quarter = warp & 3;
         const int row = quarter * 32 + lane;
-        const int q_first = x == 0 ? first[0] : first[TEAMS - 1], q_last = x == 0 ? last[0] : last[TEAMS - 1];
-        const int q_abs = q_first + row;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-        const uint32_t tS = tmem + x * TILE + lane_base, tO = tmem + TEAMS * TILE + x * DH + lane_base;
-        float m_used = -INFINITY, l = 0.f;
-        uint32_t done = 0;                                        // key tiles this team has taken
+        const uint32_t tS = tmem + lane_base, tO = tmem + TILE + lane_base;
+        const uint32_t stage = sO + quarter * 2048u;
+        uint32_t steps = 0, done = 0;
         bool alive = true;
-        for (int j = 0; j < count && alive; j++) {
-            const int kt = span.tile(j);
-            if (TEAMS == 2 && !(q_last >= q_first && sees<TILE>(p.w, kt, q_first, q_last))) continue;
-            if (!mbar_wait(s_full + 8 * x, done & 1, abort_flag)) { alive = false; break; }
+        for (int i = blockIdx.x; i < p.items && alive; i += gridDim.x, done++) {
+            const Item t = item_at(i);
+            const int count = t.span.count(), q_abs = t.first + row;
+            float m_used = -INFINITY, l = 0.f;
+            for (int j = 0; j < count; j++, steps++) {
+                const int k0 = t.span.tile(j) * TILE, keys = keys_of(t, j);
+                if (!mbar_wait(s_full, steps & 1, abort_flag)) { alive = false; break; }
+                tc_fence_after();
+                if (keys < TILE || mixed(p.w, t.first, k0)) softmax_hidden<DH>(p, tS, tO, q_abs, k0, keys, j > 0, m_used, l);
+                else softmax_whole<DH>(p.scale_log2, tS, tO, j > 0, m_used, l);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
+            }
+            if (!alive || !mbar_wait(o_done, done & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
-            uint32_t r[128];
-#pragma unroll
-            for (int c = 0; c < 4; c++) tmem_ld32_async(tS + c * 32, r + c * 32);
-            tmem_wait_ld();
-            if (mixed(p.w, q_first, kt * TILE)) {
-#pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    const uint32_t see = visible_keys(p.w, q_abs, kt * TILE, c * 32);
-#pragma unroll
-                    for (int e = 0; e < 32; e++)
-                        if (!(see >> e & 1u)) r[c * 32 + e] = 0xff800000u;              // -inf
-                }
-            }
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int e = 0; e < 128; e += 4) {
-#pragma unroll
-                for (int t = 0; t < 4; t++) m4[t] = fmaxf(m4[t], __uint_as_float(r[e + t]));
-            }
-            const float mt = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2;
-            float factor = 1.f;
-            const bool grow = mt > m_used + 8.f;                  // also true on the first tile with a visible key
-            if (grow) {
-                factor = fast_exp2(m_used - mt);
-                m_used = mt;
-                l *= factor;
-            }
-            // S complete implies the product with the previous P complete (same issuing thread, in order): O is at rest
-            if (done > 0 && __any_sync(0xffffffffu, grow)) {
-#pragma unroll 1
-                for (int c = 0; c < DH / 32; c++) {
-                    uint32_t o[32];
-                    tmem_ld32(tO + c * 32, o);
-#pragma unroll
-                    for (int e = 0; e < 32; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                    tmem_st32(tO + c * 32, o);
-                }
-            }
-            const float neg_m = m_used == -INFINITY ? 0.f : -m_used;        // nothing seen so far: exact zeros
-            float l4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < 8; c++) {                        // 16 scores -> 8 packed words per step
-                uint32_t pk[8];
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const float p0 = fast_exp2(fmaf(__uint_as_float(r[c * 16 + e]), p.scale_log2, neg_m));
-                    const float p1 = fast_exp2(fmaf(__uint_as_float(r[c * 16 + e + 1]), p.scale_log2, neg_m));
-                    l4[(e >> 1) & 3] += p0 + p1;
-                    pk[e >> 1] = pack_bf16(p0, p1);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; e++) r[c * 8 + e] = pk[e];  // packed P reuses the registers of consumed scores
-            }
-            l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-            // P overwrites the first 64 columns of S (this thread's own lane)
-#pragma unroll
-            for (int c = 0; c < 4; c++) {
-                uint32_t wd[16];
-#pragma unroll
-                for (int e = 0; e < 16; e++) wd[e] = r[c * 16 + e];
-                tmem_st16(tS + c * 16, wd);
-            }
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 8 * x);
-            done++;
-        }
-        if (alive && done > 0 && mbar_wait(o_done + 8 * x, 0, abort_flag)) {
-            tc_fence_after();
+            // O / l through a 32 x 32 block in shared memory (rows of 64 bytes, 64-byte swizzle) and TMA stores, which clip
+            // the rows behind the last query; the warp's next P is handed over only after its O has been read
             const float inv = 1.f / l;
-            const int qr = qt0 + x * TILE + row;
 #pragma unroll 1
             for (int c = 0; c < DH / 32; c++) {
                 uint32_t o[32];
                 tmem_ld32(tO + c * 32, o);
-                if (qr < p.w.n) {
-                    bf16 *out = p.o + ((long long)qr * p.w.Hq + h) * DH + c * 32;
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                __syncwarp();
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint32_t wd[4];
+                for (int e = 0; e < 32; e += 8) {
+                    uint32_t wd[4];
 #pragma unroll
-                        for (int t = 0; t < 4; t++)
-                            wd[t] = pack_bf16(__uint_as_float(o[e + 2 * t]) * inv, __uint_as_float(o[e + 2 * t + 1]) * inv);
-                        *reinterpret_cast<uint4 *>(out + e) = make_uint4(wd[0], wd[1], wd[2], wd[3]);
-                    }
+                    for (int u = 0; u < 4; u++)
+                        wd[u] = pack_bf16(__uint_as_float(o[e + 2 * u]) * inv, __uint_as_float(o[e + 2 * u + 1]) * inv);
+                    const uint32_t at = stage + (uint32_t)lane * 64u + ((uint32_t)((e >> 3) ^ ((lane >> 1) & 3)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(wd[0]), "r"(wd[1]), "r"(wd[2]), "r"(wd[3]) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_2d(&map_o, stage, t.h * DH + c * 32, t.qt0 + quarter * 32);
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
             }
-            if (qr < p.w.n) p.lse[(long long)h * p.w.n + qr] = (m_used + log2f(l)) * kLn2;
+            if (t.qt0 + row < p.w.n) p.lse[(long long)t.h * p.w.n + t.qt0 + row] = (m_used + log2f(l)) * kLn2;
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
 
     __syncwarp();
@@ -329,7 +422,7 @@ __global__ void __launch_bounds__(Fwd<DH, TEAMS, ST>::kThreads, Fwd<DH, TEAMS, S
     __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, F::kCols);
+        tmem_dealloc(tmem, 256);
     }
 }
 
@@ -895,25 +988,37 @@ bool make_maps(Maps &m, const WindowShape &w, int DH, const bf16 *q, const bf16 
            (!dout || make_tensor_map(&m.d, dout, w.n, (int64_t)w.Hq * DH, (int64_t)w.Hq * DH, 64, TILE, false));
 }
 
-template <int DH, int TEAMS, int ST>
-int launch_fwd(const Maps &m, const FwdParams &p, cudaStream_t st) {
-    typedef Fwd<DH, TEAMS, ST> F;
-    static PerDevice configured;
-    if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, TEAMS, ST>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
-    const int64_t tiles = ((int64_t)p.w.n + TEAMS * TILE - 1) / (TEAMS * TILE);
-    if (tiles > 65535) return STREAMBP_E_SHAPE;
-    SBP_LAUNCH((attn_window_fwd_kernel<DH, TEAMS, ST>), dim3(p.w.Hq, (unsigned)tiles), F::kThreads, F::kSmem, st, m.q, m.k, m.v, p);
-    return STREAMBP_OK;
-}
-
 template <int DH>
-int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, bf16 *o, float *lse, cudaStream_t st, int teams) {
+int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, bf16 *o, float *lse, cudaStream_t st) {
+    typedef Fwd<DH> F;
     Maps m;
     if (!make_maps(m, w, DH, q, k, v, nullptr)) return STREAMBP_E_CUDA;
-    const FwdParams p{w, o, lse, kLog2e / sqrtf((float)DH)};
-    if (teams == 0) teams = 1;
-    if (teams == 2) return launch_fwd<DH, 2, 2>(m, p, st);
-    return launch_fwd<DH, 1, DH == 64 ? 2 : 1>(m, p, st);
+    FwdParams p;
+    memset(&p, 0, sizeof(p));
+    p.w = w;
+    p.o = o;
+    p.lse = lse;
+    p.scale_log2 = kLog2e / sqrtf((float)DH);
+    p.q_tiles = (w.n + TILE - 1) / TILE;
+    const int64_t items = (int64_t)p.q_tiles * w.Hq;
+    if (items > 0x7fffffff / 2) return STREAMBP_E_SHAPE;
+    p.items = (int)items;
+    // the sink tile whose last rows are no sinks is read, multiplied and exponentiated only as far as its sinks go
+    p.edge = w.sinks % TILE ? w.sinks / TILE : -1;
+    p.edge_keys = (w.sinks % TILE + 15) / 16 * 16;
+    if (p.edge_keys == TILE) p.edge = -1;
+    const int64_t kv = (int64_t)w.q0 + w.n;
+    const uint32_t box = p.edge >= 0 ? (uint32_t)p.edge_keys : 16u;
+    CUtensorMap ke, ve, mo;
+    if (!make_tensor_map(&ke, k, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, box, false) ||
+        !make_tensor_map(&ve, v, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, box, false) ||
+        !make_tensor_map(&mo, o, w.n, (int64_t)w.Hq * DH, (int64_t)w.Hq * DH, 32, 32, false, CU_TENSOR_MAP_SWIZZLE_64B))
+        return STREAMBP_E_CUDA;
+    static PerDevice configured;
+    if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+    const int slots = 2 * sm_count();
+    SBP_LAUNCH(attn_window_fwd_kernel<DH>, p.items < slots ? p.items : slots, F::kThreads, F::kSmem, st, m.q, m.k, m.v, ke, ve, mo, p);
+    return STREAMBP_OK;
 }
 
 template <int DH>
@@ -955,8 +1060,8 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
 bool attention_window_tc_available() { return tensor_maps_available(); }
 
 int attention_window_fwd_tc(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, int dh, bf16 *o, float *lse,
-                            cudaStream_t st, int teams) {
-    return dh == 64 ? fwd_any<64>(q, k, v, w, o, lse, st, teams) : fwd_any<128>(q, k, v, w, o, lse, st, teams);
+                            cudaStream_t st) {
+    return dh == 64 ? fwd_any<64>(q, k, v, w, o, lse, st) : fwd_any<128>(q, k, v, w, o, lse, st);
 }
 int attention_window_bwd_tc(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf16 *dout, const float *lse,
                             const WindowShape &w, int dh, int mode, void *dq, void *dk, void *dv, float *delta, float *part,

@@ -455,9 +455,8 @@ int attn_bwd(const T *q, const T *k, const T *v, const T *o, const T *dout, cons
 // rows of sink tiles whose work is cut (segs > 1) to attention_window_join.
 struct WindowShape;
 bool attention_window_tc_available();
-// teams: 128-query tiles per CTA, 1 or 2
 int attention_window_fwd_tc(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, int dh, bf16 *o, float *lse,
-                            cudaStream_t st, int teams);
+                            cudaStream_t st);
 int attention_window_bwd_tc(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf16 *dout, const float *lse,
                             const WindowShape &w, int dh, int mode, void *dq, void *dk, void *dv, float *delta, float *part,
                             WsHeader *hdr, cudaStream_t st);

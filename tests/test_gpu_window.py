@@ -107,12 +107,11 @@ def run(case, engines=(0,), grads=(F32,)):
         o, lse = case.forward(engine)
         case.check("o", o, ref["o"], err["o"])
         case.check("lse", lse, ref["lse"], err["lse"])
-        bwd = engine if engine <= 2 else 2
         for gd in grads:
-            for name, x in zip(("dq", "dk", "dv"), case.backward(o, lse, gd, engine=bwd)):
+            for name, x in zip(("dq", "dk", "dv"), case.backward(o, lse, gd, engine=engine)):
                 case.check(f"{name} engine {engine} {gd}", x, ref[name], err[name])
         # adding: to what the accumulators hold (dq is overwritten)
-        dq, dk, dv = case.backward(o, lse, F32, accumulate=True, fill=0.25, engine=bwd)
+        dq, dk, dv = case.backward(o, lse, F32, accumulate=True, fill=0.25, engine=engine)
         case.check("dq", dq, ref["dq"], err["dq"])
         case.check("dk +=", dk, ref["dk"] + 0.25, err["dk"], 2.0 ** -24)
         case.check("dv +=", dv, ref["dv"] + 0.25, err["dv"], 2.0 ** -24)
@@ -122,20 +121,20 @@ SHAPES = [
     # n, q0, window, sinks
     (1, 0, 1, 0), (1, 500, 100, 3), (2, 0, 2, 1), (5, 300, 64, 0), (127, 0, 20, 0), (128, 0, 128, 4), (129, 0, 129, 0),
     (130, 126, 1, 0), (200, 56, 127, 130), (256, 128, 128, 1), (300, 0, 1000, 4), (333, 700, 200, 0), (333, 700, 200, 5),
-    (511, 513, 300, 129), (700, 0, 33, 17), (700, 100, 255, 256), (640, 0, 640, 640), (640, 0, 5, 10000),
+    (511, 513, 300, 129), (600, 0, 40, 128), (600, 0, 40, 113), (600, 0, 40, 16), (600, 300, 70, 290), (700, 0, 33, 17), (700, 100, 255, 256), (640, 0, 640, 640), (640, 0, 5, 10000),
 ]
 
 
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("n,q0,window,sinks", SHAPES)
 def test_tensor_core_shapes(n, q0, window, sinks, dh):
-    run(Case(n, q0, 4, 2, dh, window, sinks), engines=(0, 3, 4), grads=(F32, BF))
+    run(Case(n, q0, 4, 2, dh, window, sinks), engines=(0,), grads=(F32, BF))
 
 
 @pytest.mark.parametrize("Hq,Hkv", [(1, 1), (7, 1), (6, 6), (14, 2), (3, 3)])
 def test_head_layouts(Hq, Hkv):
-    run(Case(300, 150, Hq, Hkv, 64, 100, 2), engines=(0, 4), grads=(BF,))
-    run(Case(270, 0, Hq, Hkv, 128, 130, 0), engines=(0, 4), grads=(BF,))
+    run(Case(300, 150, Hq, Hkv, 64, 100, 2), engines=(0, 2), grads=(BF,))
+    run(Case(270, 0, Hq, Hkv, 128, 130, 0), engines=(0, 2), grads=(BF,))
 
 
 @pytest.mark.parametrize("dh", [64, 128])

@@ -126,7 +126,7 @@ SIZES = [
 @pytest.mark.parametrize("kw,status", SIZES + [
     (dict(q=None), B.E_NULL), (dict(k=None), B.E_NULL), (dict(v=None), B.E_NULL), (dict(o=None), B.E_NULL), (dict(lse=None), B.E_NULL),
     (dict(q=P + 8), B.E_ALIGN), (dict(k=P + 2), B.E_ALIGN), (dict(o=P + 4), B.E_ALIGN), (dict(lse=P + 2), B.E_ALIGN),
-    (dict(engine=5), B.E_SHAPE), (dict(engine=-1), B.E_SHAPE), (dict(dtype=B.STREAMBP_F32, engine=2), B.E_DTYPE)])
+    (dict(engine=3), B.E_SHAPE), (dict(engine=-1), B.E_SHAPE), (dict(dtype=B.STREAMBP_F32, engine=2), B.E_DTYPE)])
 def test_window_forward_refusals(lib, kw, status):
     assert window_fwd(lib, **kw) == status
 
