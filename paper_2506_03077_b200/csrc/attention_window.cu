@@ -88,9 +88,9 @@ __device__ __forceinline__ void leave(volatile int *abort_flag) {
 // ---------------------------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------------------------
+constexpr int KT = 64;                    // keys per tile of the forward: two S tiles fit beside O in half of tensor memory
 struct FwdParams {
     WindowShape w;
-    bf16 *o;            // [n, Hq, DH]
     float *lse;         // [Hq, n]
     float scale_log2;   // log2(e) / sqrt(head_dim)
     int q_tiles, items; // items = q_tiles * Hq, the last query tiles (longest spans) first, the heads of a tile side by side
@@ -98,13 +98,18 @@ struct FwdParams {
 };
 
 template <int DH> struct Fwd {
-    static constexpr int kTile = TILE * DH * 2;
-    static constexpr int kRing = DH == 64 ? 2 : 1;         // stages of the Q, K and V rings: what leaves room for two CTAs
+    static constexpr int kQ = TILE * DH * 2, kKV = KT * DH * 2;
+    static constexpr int kQRing = DH == 64 ? 2 : 1, kRing = DH == 64 ? 4 : 2;      // what leaves room for two CTAs
+    static constexpr int kS = (256 - DH) / KT;             // S tiles in tensor memory: 3 or 2
     static constexpr int kThreads = 64 + 128;
     static constexpr int kStaging = 4 * 2048;              // a 32 x 32 block of O per softmax warp
-    static constexpr int kSmem = 3 * kRing * kTile + kStaging + 1024 + 256;
+    static constexpr int kSmem = kQRing * kQ + 2 * kRing * kKV + kStaging + 1024 + 256;
     static_assert(2 * (kSmem + 1024) <= 233472, "two CTAs share an SM");
+    static_assert((2 * kQRing + 4 * kRing + 3 * kS) * 8 <= 232, "barriers");
 };
+constexpr int KSUB = KT * 64 * 2;         // one [64 keys][64 columns] swizzled sub-tile
+__host__ __device__ constexpr uint32_t kvstep(int kk) { return (uint32_t)((kk >> 2) * (KSUB >> 4) + (kk & 3) * 2); }
+
 struct RingAt {                                            // stage and phase of the next use of a ring of N stages
     uint32_t st = 0, ph = 0;
     template <int N> __device__ __forceinline__ void next() {
@@ -112,10 +117,10 @@ struct RingAt {                                            // stage and phase of
     }
 };
 
-// The running maximum of a row takes in the maximum `mt` of a tile; O (at rest: S complete implies the product with the
-// previous P complete, same issuing thread, in order) and l are rescaled where it grew by more than 2^8.
-template <int DH>
-__device__ __forceinline__ void take_maximum(float mt, uint32_t tO, bool later, float &m_used, float &l) {
+// The running maximum of a row takes in the maximum `mt` of a tile; O and l are rescaled where it grew by more than 2^8
+// (the product with the previous P has to have completed: `rest` waits for it).
+template <int DH, typename F>
+__device__ __forceinline__ bool take_maximum(float mt, uint32_t tO, bool later, float &m_used, float &l, F rest) {
     float factor = 1.f;
     const bool grow = mt > m_used + 8.f;                  // also true on the first tile with a visible key
     if (grow) {
@@ -124,6 +129,8 @@ __device__ __forceinline__ void take_maximum(float mt, uint32_t tO, bool later, 
         l *= factor;
     }
     if (later && __any_sync(0xffffffffu, grow)) {
+        if (!rest()) return false;
+        tc_fence_after();
 #pragma unroll 1
         for (int c = 0; c < DH / 32; c++) {
             uint32_t o[32];
@@ -133,91 +140,43 @@ __device__ __forceinline__ void take_maximum(float mt, uint32_t tO, bool later, 
             tmem_st32(tO + c * 32, o);
         }
     }
+    return true;
 }
 
-// A key tile that the row sees whole: 128 scores in registers, P packed over the first 64 columns of S.
-template <int DH>
-__device__ __forceinline__ void softmax_whole(float scale_log2, uint32_t tS, uint32_t tO, bool later, float &m_used, float &l) {
-    uint32_t r[128];
-#pragma unroll
-    for (int c = 0; c < 4; c++) tmem_ld32_async(tS + c * 32, r + c * 32);
+// One key tile of a query row: scores from tensor memory, P packed over the first 32 of their 64 columns.  HIDDEN: the tile
+// holds keys the row does not see (see[]: the ones it does).
+template <bool HIDDEN, int DH, typename F>
+__device__ __forceinline__ bool softmax_tile(float scale_log2, uint32_t tS, uint32_t tO, const uint32_t (&see)[2], bool later,
+                                             float &m_used, float &l, F rest) {
+    uint32_t r[KT];
+    tmem_ld32_async(tS, r);
+    tmem_ld32_async(tS + 32, r + 32);
     tmem_wait_ld();
+    if (HIDDEN) {
+#pragma unroll
+        for (int e = 0; e < KT; e++)
+            if (!(see[e >> 5] >> (e & 31) & 1u)) r[e] = 0xff800000u;              // -inf
+    }
     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int e = 0; e < 128; e++) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(r[e]));
-    take_maximum<DH>(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale_log2, tO, later, m_used, l);
-    const float neg_m = -m_used;
+    for (int e = 0; e < KT; e++) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(r[e]));
+    if (!take_maximum<DH>(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale_log2, tO, later, m_used, l, rest)) return false;
+    const float neg_m = HIDDEN && m_used == -INFINITY ? 0.f : -m_used;        // nothing seen so far: exact zeros
     float l4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < 8; c++) {                        // 16 scores -> 8 packed words per step
-        uint32_t pk[8];
+    for (int c = 0; c < 2; c++) {
+        uint32_t pk[16];
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            const float p0 = fast_exp2(fmaf(__uint_as_float(r[c * 16 + e]), scale_log2, neg_m));
-            const float p1 = fast_exp2(fmaf(__uint_as_float(r[c * 16 + e + 1]), scale_log2, neg_m));
+        for (int e = 0; e < 32; e += 2) {
+            const float p0 = fast_exp2(fmaf(__uint_as_float(r[c * 32 + e]), scale_log2, neg_m));
+            const float p1 = fast_exp2(fmaf(__uint_as_float(r[c * 32 + e + 1]), scale_log2, neg_m));
             l4[(e >> 1) & 3] += p0 + p1;
             pk[e >> 1] = pack_bf16(p0, p1);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; e++) r[c * 8 + e] = pk[e];  // packed P reuses the registers of consumed scores
-    }
-    l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-#pragma unroll
-    for (int c = 0; c < 4; c++) {
-        uint32_t wd[16];
-#pragma unroll
-        for (int e = 0; e < 16; e++) wd[e] = r[c * 16 + e];
-        tmem_st16(tS + c * 16, wd);
-    }
-}
-
-// A key tile that holds keys the row does not see, or an edge tile of `keys` columns: 32 columns at a time, once for the
-// maximum and once for P (columns 16 c .. of P lie over scores that have been read by then), groups that no row of the warp
-// sees left out.  With all 128 scores in registers under those conditions the compiler spilled a kilobyte and a half.
-template <int DH>
-__device__ __forceinline__ void softmax_hidden(const FwdParams &p, uint32_t tS, uint32_t tO, int q_abs, int k0, int keys, bool later,
-                                               float &m_used, float &l) {
-    uint32_t see[4], any = 0u;
-#pragma unroll
-    for (int c = 0; c < 4; c++) {
-        see[c] = visible_keys(p.w, q_abs, k0, c * 32);
-        any |= __any_sync(0xffffffffu, see[c] != 0u) ? 1u << c : 0u;
-    }
-    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-    for (int c = 0; c < 4; c++) {
-        if (!(any >> c & 1u)) continue;
-        uint32_t r[32];
-        tmem_ld32(tS + c * 32, r);
-#pragma unroll
-        for (int e = 0; e < 32; e++)
-            m4[e & 3] = fmaxf(m4[e & 3], (see[c] >> e & 1u) ? __uint_as_float(r[e]) : -INFINITY);
-    }
-    take_maximum<DH>(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2, tO, later, m_used, l);
-    const float neg_m = m_used == -INFINITY ? 0.f : -m_used;        // nothing seen so far: exact zeros
-    float l4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < 4; c++) {
-        if (c * 32 >= keys) continue;                               // the product does not read these
-        uint32_t pk[16];
-        if (any >> c & 1u) {
-            uint32_t r[32];
-            tmem_ld32(tS + c * 32, r);
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-                const float x0 = (see[c] >> e & 1u) ? __uint_as_float(r[e]) : -INFINITY;
-                const float x1 = (see[c] >> (e + 1) & 1u) ? __uint_as_float(r[e + 1]) : -INFINITY;
-                const float p0 = fast_exp2(fmaf(x0, p.scale_log2, neg_m)), p1 = fast_exp2(fmaf(x1, p.scale_log2, neg_m));
-                l4[(e >> 1) & 3] += p0 + p1;
-                pk[e >> 1] = pack_bf16(p0, p1);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; e++) pk[e] = 0u;
         }
         tmem_st16(tS + c * 16, pk);
     }
     l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+    return true;
 }
 
 template <int DH>
@@ -227,32 +186,36 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
                            const __grid_constant__ CUtensorMap map_ve, const __grid_constant__ CUtensorMap map_o, const FwdParams p) {
     pdl_enter();
     typedef Fwd<DH> F;
-    constexpr int N = F::kRing;
+    constexpr int N = F::kRing, NQ = F::kQRing, NS = F::kS;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
-    const uint32_t sQ = base, sK = sQ + N * F::kTile, sV = sK + N * F::kTile, sO = sV + N * F::kTile;
-    uint8_t *aux = smem_raw + (base - raw) + 3 * N * F::kTile + F::kStaging;
+    const uint32_t sQ = base, sK = sQ + NQ * F::kQ, sV = sK + N * F::kKV, sO = sV + N * F::kKV;
+    uint8_t *aux = smem_raw + (base - raw) + NQ * F::kQ + 2 * N * F::kKV + F::kStaging;
     const uint32_t bars = smem_u32(aux);
-    const uint32_t q_full = bars, q_empty = q_full + 8 * N, k_full = q_empty + 8 * N, k_empty = k_full + 8 * N,
-                   v_full = k_empty + 8 * N, v_empty = v_full + 8 * N, s_full = v_empty + 8 * N, p_full = s_full + 8,
-                   o_done = p_full + 8;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(aux + 192);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(aux + 200);
+    const uint32_t q_full = bars, q_empty = q_full + 8 * NQ, k_full = q_empty + 8 * NQ, k_empty = k_full + 8 * N,
+                   v_full = k_empty + 8 * N, v_empty = v_full + 8 * N, s_full = v_empty + 8 * N, p_full = s_full + 8 * NS,
+                   pv_done = p_full + 8 * NS;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(aux + 232);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(aux + 240);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < N; s++) {
+        for (int s = 0; s < NQ; s++) {
             mbar_init(q_full + 8 * s, 1);
             mbar_init(q_empty + 8 * s, 1);
+        }
+        for (int s = 0; s < N; s++) {
             mbar_init(k_full + 8 * s, 1);
             mbar_init(k_empty + 8 * s, 1);
             mbar_init(v_full + 8 * s, 1);
             mbar_init(v_empty + 8 * s, 1);
         }
-        mbar_init(s_full, 1);
-        mbar_init(p_full, 4);
-        mbar_init(o_done, 1);
+        for (int s = 0; s < NS; s++) {
+            mbar_init(s_full + 8 * s, 1);
+            mbar_init(p_full + 8 * s, 4);
+            mbar_init(pv_done + 8 * s, 1);
+        }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -260,22 +223,22 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;      // S (128 columns), O (DH columns)
+    const uint32_t tmem = *tmem_slot;      // O (DH columns), then the S tiles (64 columns each)
 
     // an item: one query tile of one head
-    struct Item { int h, qt0, first, last; KeySpan span; };
+    struct Item { int h, qt0, first, count; KeySpan span; };
     auto item_at = [&](int i) {
         Item t;
         t.h = i % p.w.Hq;
         t.qt0 = (p.q_tiles - 1 - i / p.w.Hq) * TILE;
         const int rows = p.w.n - t.qt0 < TILE ? p.w.n - t.qt0 : TILE;
         t.first = p.w.q0 + t.qt0;
-        t.last = t.first + rows - 1;
-        t.span = key_span<TILE>(p.w, t.first, t.last);
+        t.span = key_span<KT>(p.w, t.first, t.first + rows - 1);
+        t.count = t.span.count();
         return t;
     };
     // keys of a tile that take part: all, or the sinks at the head of the edge tile where the window does not reach it
-    auto keys_of = [&](const Item &t, int j) { return j < t.span.ns && j == p.edge ? p.edge_keys : TILE; };
+    auto keys_of = [&](const Item &t, int j) { return j < t.span.ns && j == p.edge ? p.edge_keys : KT; };
 
     if (warp == 0) {
         if (lane == 0) {
@@ -283,108 +246,118 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
             bool alive = true;
             for (int i = blockIdx.x; i < p.items && alive; i += gridDim.x) {
                 const Item t = item_at(i);
-                const int g = t.h / (p.w.Hq / p.w.Hkv), count = t.span.count();
+                const int g = t.h / (p.w.Hq / p.w.Hkv);
                 if (!mbar_wait(q_empty + 8 * q.st, q.ph ^ 1u, abort_flag)) break;
-                mbar_expect_tx(q_full + 8 * q.st, F::kTile);
-                load_tile<DH>(sQ + q.st * F::kTile, &map_q, q_full + 8 * q.st, t.h, t.qt0);
-                q.next<N>();
-                for (int j = 0; j < count; j++) {
-                    const int row = t.span.tile(j) * TILE, keys = keys_of(t, j);
-                    const bool part = keys < TILE;
+                mbar_expect_tx(q_full + 8 * q.st, F::kQ);
+                load_tile<DH>(sQ + q.st * F::kQ, &map_q, q_full + 8 * q.st, t.h, t.qt0);
+                q.next<NQ>();
+                for (int j = 0; j < t.count; j++) {
+                    const int row = t.span.tile(j) * KT, keys = keys_of(t, j);
+                    const bool part = keys < KT;
                     const uint32_t bytes = (uint32_t)keys * DH * 2u;
                     if (!mbar_wait(k_empty + 8 * kv.st, kv.ph ^ 1u, abort_flag)) { alive = false; break; }
                     mbar_expect_tx(k_full + 8 * kv.st, bytes);
-                    load_tile<DH>(sK + kv.st * F::kTile, part ? &map_ke : &map_k, k_full + 8 * kv.st, g, row);
+#pragma unroll
+                    for (int c = 0; c < DH / 64; c++)
+                        tma_load_2d(sK + kv.st * F::kKV + c * KSUB, part ? &map_ke : &map_k, k_full + 8 * kv.st, g * DH + c * 64, row);
                     if (!mbar_wait(v_empty + 8 * kv.st, kv.ph ^ 1u, abort_flag)) { alive = false; break; }
                     mbar_expect_tx(v_full + 8 * kv.st, bytes);
-                    load_tile<DH>(sV + kv.st * F::kTile, part ? &map_ve : &map_v, v_full + 8 * kv.st, g, row);
+#pragma unroll
+                    for (int c = 0; c < DH / 64; c++)
+                        tma_load_2d(sV + kv.st * F::kKV + c * KSUB, part ? &map_ve : &map_v, v_full + 8 * kv.st, g * DH + c * 64, row);
                     kv.next<N>();
                 }
             }
         }
     } else if (warp == 1) {
         constexpr uint32_t idesc_pv = make_idesc(TILE, DH, false, true);
-        RingAt q, k, v;                                 // next use by S, by S, by P V
-        uint32_t steps = 0;                             // P tiles taken
+        // two cursors over the same sequence of (item, tile): S runs up to NS tiles ahead of P V
+        RingAt q, k, v, bs, bp;                         // rings: Q and K (by S), V (by P V), S tiles (by S and by P V)
+        int is = blockIdx.x, js = 0, ip = blockIdx.x, jp = 0;
+        Item ts, tp;
+        if (is < p.items) ts = tp = item_at(is);
         bool alive = true;
-        // S = Q K_j^T of item t; the last of an item hands the query tile back
-        auto issue_s = [&](const Item &t, int j) -> bool {
-            if (j == 0 && !mbar_wait_warp(q_full + 8 * q.st, q.ph, abort_flag)) return false;
+        auto issue_s = [&]() -> bool {                  // S = Q K^T of the next tile; the last of an item hands Q back
+            if (is >= p.items) return true;
+            if (js == 0 && !mbar_wait_warp(q_full + 8 * q.st, q.ph, abort_flag)) return false;
             if (!mbar_wait_warp(k_full + 8 * k.st, k.ph, abort_flag)) return false;
             tc_fence_after();
-            const uint32_t q_lo = klo(sQ + q.st * F::kTile), k_lo = klo(sK + k.st * F::kTile);
-            const uint32_t idesc_s = make_idesc(TILE, keys_of(t, j), false, false);
+            const uint32_t q_lo = klo(sQ + q.st * F::kQ), k_lo = klo(sK + k.st * F::kKV);
+            const uint32_t idesc_s = make_idesc(TILE, keys_of(ts, js), false, false), d = tmem + DH + bs.st * KT;
 #pragma unroll
-            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tmem, q_lo + kstep(kk), k_lo + kstep(kk), idesc_s, kk != 0);
-            umma_commit_w(s_full);
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(d, q_lo + kstep(kk), k_lo + kvstep(kk), idesc_s, kk != 0);
+            umma_commit_w(s_full + 8 * bs.st);
             umma_commit_w(k_empty + 8 * k.st);
             k.next<N>();
-            if (j == t.span.count() - 1) {
+            bs.next<NS>();
+            if (++js == ts.count) {
                 umma_commit_w(q_empty + 8 * q.st);
-                q.next<N>();
+                q.next<NQ>();
+                js = 0;
+                is += gridDim.x;
+                if (is < p.items) ts = item_at(is);
             }
             return true;
         };
-        Item t;
-        if ((int)blockIdx.x < p.items) {
-            t = item_at(blockIdx.x);
-            alive = issue_s(t, 0);
-        }
-        for (int i = blockIdx.x; i < p.items && alive; i += gridDim.x) {
-            const int count = t.span.count();
-            for (int j = 0; j < count; j++) {
-                // O += P V_j once P is stored; then S of the next tile (of the next item behind the last) over P's columns
-                if (!mbar_wait_warp(p_full, steps & 1, abort_flag) || !mbar_wait_warp(v_full + 8 * v.st, v.ph, abort_flag)) { alive = false; break; }
-                tc_fence_after();
-                const uint32_t v_lo = mnlo(sV + v.st * F::kTile);
-                const int slices = keys_of(t, j) / 16;
-                if (slices == 8) {
+        for (int s = 0; s < NS && alive; s++) alive = issue_s();
+        while (alive && ip < p.items) {
+            // O += P V once P is stored; the S tile that P lay in then takes the scores NS tiles further on
+            if (!mbar_wait_warp(v_full + 8 * v.st, v.ph, abort_flag) || !mbar_wait_warp(p_full + 8 * bp.st, bp.ph, abort_flag)) break;
+            tc_fence_after();
+            const uint32_t v_lo = desc_lo(sV + v.st * F::kKV, KSUB), a = tmem + DH + bp.st * KT;
+            const int slices = keys_of(tp, jp) / 16;
 #pragma unroll
-                    for (int kk = 0; kk < 8; kk++)
-                        umma_ts_w(tmem + TILE, tmem + kk * 8, v_lo + mnstep(kk), idesc_pv, (j | kk) != 0);
-                } else {
-                    for (int kk = 0; kk < slices; kk++)
-                        umma_ts_w(tmem + TILE, tmem + kk * 8, v_lo + mnstep(kk), idesc_pv, (j | kk) != 0);
-                }
-                umma_commit_w(v_empty + 8 * v.st);
-                v.next<N>();
-                steps++;
-                if (j + 1 < count) {
-                    alive = issue_s(t, j + 1);
-                } else {
-                    umma_commit_w(o_done);
-                    if (i + (int)gridDim.x < p.items) {
-                        t = item_at(i + gridDim.x);
-                        alive = issue_s(t, 0);
-                    }
-                }
-                if (!alive) break;
+            for (int kk = 0; kk < KT / 16; kk++)
+                if (kk < slices) umma_ts_w(tmem, a + kk * 8, v_lo + mnstep(kk), idesc_pv, (jp | kk) != 0);
+            umma_commit_w(v_empty + 8 * v.st);
+            umma_commit_w(pv_done + 8 * bp.st);
+            v.next<N>();
+            bp.next<NS>();
+            alive = issue_s();
+            if (++jp == tp.count) {
+                jp = 0;
+                ip += gridDim.x;
+                if (ip < p.items) tp = item_at(ip);
             }
         }
     } else {
         const int quarter = warp & 3;
         const int row = quarter * 32 + lane;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-        const uint32_t tS = tmem + lane_base, tO = tmem + TILE + lane_base;
+        const uint32_t tO = tmem + lane_base;
         const uint32_t stage = sO + quarter * 2048u;
-        uint32_t steps = 0, done = 0;
+        RingAt b, before;                                // S tile of this step and of the one before
         bool alive = true;
-        for (int i = blockIdx.x; i < p.items && alive; i += gridDim.x, done++) {
+        // P V of the step before has completed.  One barrier per S tile: a warp may be a tile or two ahead of the others,
+        // and S of a tile, which it has seen, was issued behind the last use of that tile's barrier -- a single barrier
+        // could still be two phases back and pass for done.
+        auto rest = [&]() -> bool { return mbar_wait(pv_done + 8 * before.st, before.ph, abort_flag); };
+        for (int i = blockIdx.x; i < p.items && alive; i += gridDim.x) {
             const Item t = item_at(i);
-            const int count = t.span.count(), q_abs = t.first + row;
+            const int q_abs = t.first + row;
             float m_used = -INFINITY, l = 0.f;
-            for (int j = 0; j < count; j++, steps++) {
-                const int k0 = t.span.tile(j) * TILE, keys = keys_of(t, j);
-                if (!mbar_wait(s_full, steps & 1, abort_flag)) { alive = false; break; }
+            for (int j = 0; j < t.count; j++) {
+                const int k0 = t.span.tile(j) * KT;
+                const uint32_t tS = tmem + DH + b.st * KT + lane_base;
+                const bool hidden = k0 + KT - 1 > t.first || (t.first + TILE - 1 - k0 >= p.w.window && k0 + KT > p.w.sinks);
+                uint32_t see[2];
+                if (hidden) {
+                    see[0] = visible_keys(p.w, q_abs, k0, 0);
+                    see[1] = visible_keys(p.w, q_abs, k0, 32);
+                }
+                if (!mbar_wait(s_full + 8 * b.st, b.ph, abort_flag)) { alive = false; break; }
                 tc_fence_after();
-                if (keys < TILE || mixed(p.w, t.first, k0)) softmax_hidden<DH>(p, tS, tO, q_abs, k0, keys, j > 0, m_used, l);
-                else softmax_whole<DH>(p.scale_log2, tS, tO, j > 0, m_used, l);
+                alive = hidden ? softmax_tile<true, DH>(p.scale_log2, tS, tO, see, j > 0, m_used, l, rest)
+                               : softmax_tile<false, DH>(p.scale_log2, tS, tO, see, j > 0, m_used, l, rest);
+                if (!alive) break;
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full);
+                if (lane == 0) mbar_arrive(p_full + 8 * b.st);
+                before = b;
+                b.next<NS>();
             }
-            if (!alive || !mbar_wait(o_done, done & 1, abort_flag)) { alive = false; break; }
+            if (!alive || !rest()) { alive = false; break; }
             tc_fence_after();
             // O / l through a 32 x 32 block in shared memory (rows of 64 bytes, 64-byte swizzle) and TMA stores, which clip
             // the rows behind the last query; the warp's next P is handed over only after its O has been read
@@ -996,7 +969,6 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
     FwdParams p;
     memset(&p, 0, sizeof(p));
     p.w = w;
-    p.o = o;
     p.lse = lse;
     p.scale_log2 = kLog2e / sqrtf((float)DH);
     p.q_tiles = (w.n + TILE - 1) / TILE;
@@ -1004,13 +976,15 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
     if (items > 0x7fffffff / 2) return STREAMBP_E_SHAPE;
     p.items = (int)items;
     // the sink tile whose last rows are no sinks is read, multiplied and exponentiated only as far as its sinks go
-    p.edge = w.sinks % TILE ? w.sinks / TILE : -1;
-    p.edge_keys = (w.sinks % TILE + 15) / 16 * 16;
-    if (p.edge_keys == TILE) p.edge = -1;
+    p.edge = w.sinks % KT ? w.sinks / KT : -1;
+    p.edge_keys = (w.sinks % KT + 15) / 16 * 16;
+    if (p.edge_keys == KT) p.edge = -1;
     const int64_t kv = (int64_t)w.q0 + w.n;
     const uint32_t box = p.edge >= 0 ? (uint32_t)p.edge_keys : 16u;
     CUtensorMap ke, ve, mo;
-    if (!make_tensor_map(&ke, k, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, box, false) ||
+    if (!make_tensor_map(&m.k, k, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, KT, false) ||
+        !make_tensor_map(&m.v, v, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, KT, false) ||
+        !make_tensor_map(&ke, k, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, box, false) ||
         !make_tensor_map(&ve, v, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, box, false) ||
         !make_tensor_map(&mo, o, w.n, (int64_t)w.Hq * DH, (int64_t)w.Hq * DH, 32, 32, false, CU_TENSOR_MAP_SWIZZLE_64B))
         return STREAMBP_E_CUDA;

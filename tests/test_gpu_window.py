@@ -156,9 +156,12 @@ def test_a_window_over_everything_is_causal_attention():
     o, lse = c.forward()
     want, want_lse = torch.empty_like(o), torch.empty_like(lse)
     B.attention_forward(c.q, c.k, c.v, c.q0, want, want_lse)
-    # the same products and exponentials in the same order of keys; the output is rounded once on each side
-    assert bool(((o.float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 1e-6).all())
-    assert bool(((lse - want_lse).abs() <= 1e-5 * (1 + want_lse.abs())).all())
+    # The two kernels take their maxima over 64 and over 128 keys at a time, so their P are rounded against different
+    # references: each is within its own bound of the exact result (P to 2^-8 of sum p |v|), not of the other's bits.
+    ref, err = c.reference()
+    for x, y in ((o, lse), (want, want_lse)):
+        c.check("o", x, ref["o"], err["o"])
+        c.check("lse", y, ref["lse"], err["lse"])
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
