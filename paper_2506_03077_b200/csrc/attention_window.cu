@@ -151,27 +151,43 @@ __device__ __forceinline__ bool softmax_tile(float scale_log2, uint32_t tS, uint
     uint32_t r[KT];
     tmem_ld32_async(tS, r);
     tmem_ld32_async(tS + 32, r + 32);
-    tmem_wait_ld();
+    // of each group of 32 columns: whether some row of the warp sees one (else its P is zero without an exponential), and
+    // whether every row sees all (else the hidden scores are struck out)
+    bool some[2] = {true, true};
     if (HIDDEN) {
-#pragma unroll
-        for (int e = 0; e < KT; e++)
-            if (!(see[e >> 5] >> (e & 31) & 1u)) r[e] = 0xff800000u;              // -inf
+        some[0] = __any_sync(0xffffffffu, see[0] != 0u);
+        some[1] = __any_sync(0xffffffffu, see[1] != 0u);
     }
+    tmem_wait_ld();
     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int e = 0; e < KT; e++) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(r[e]));
+    for (int c = 0; c < 2; c++) {
+        if (HIDDEN && !__all_sync(0xffffffffu, see[c] == 0xffffffffu)) {
+            if (!some[c]) continue;
+#pragma unroll
+            for (int e = 0; e < 32; e++)
+                if (!(see[c] >> e & 1u)) r[c * 32 + e] = 0xff800000u;              // -inf
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e++) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(r[c * 32 + e]));
+    }
     if (!take_maximum<DH>(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale_log2, tO, later, m_used, l, rest)) return false;
     const float neg_m = HIDDEN && m_used == -INFINITY ? 0.f : -m_used;        // nothing seen so far: exact zeros
     float l4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < 2; c++) {
         uint32_t pk[16];
+        if (!HIDDEN || some[c]) {
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-            const float p0 = fast_exp2(fmaf(__uint_as_float(r[c * 32 + e]), scale_log2, neg_m));
-            const float p1 = fast_exp2(fmaf(__uint_as_float(r[c * 32 + e + 1]), scale_log2, neg_m));
-            l4[(e >> 1) & 3] += p0 + p1;
-            pk[e >> 1] = pack_bf16(p0, p1);
+            for (int e = 0; e < 32; e += 2) {
+                const float p0 = fast_exp2(fmaf(__uint_as_float(r[c * 32 + e]), scale_log2, neg_m));
+                const float p1 = fast_exp2(fmaf(__uint_as_float(r[c * 32 + e + 1]), scale_log2, neg_m));
+                l4[(e >> 1) & 3] += p0 + p1;
+                pk[e >> 1] = pack_bf16(p0, p1);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; e++) pk[e] = 0u;
         }
         tmem_st16(tS + c * 16, pk);
     }
