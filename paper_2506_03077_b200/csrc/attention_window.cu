@@ -99,11 +99,12 @@ struct FwdParams {
 
 template <int DH> struct Fwd {
     static constexpr int kQ = TILE * DH * 2, kKV = KT * DH * 2;
-    static constexpr int kQRing = DH == 64 ? 2 : 1, kRing = DH == 64 ? 4 : 2;      // what leaves room for two CTAs
+    static constexpr int kQRing = DH == 64 ? 2 : 1, kRing = DH == 64 ? 3 : 2;      // what leaves room for two CTAs
     static constexpr int kS = (256 - DH) / KT;             // S tiles in tensor memory: 3 or 2
     static constexpr int kThreads = 64 + 128;
-    static constexpr int kStaging = 4 * 2048;              // a 32 x 32 block of O per softmax warp
-    static constexpr int kSmem = kQRing * kQ + 2 * kRing * kKV + kStaging + 1024 + 256;
+    static constexpr int kStaging = 4 * 2 * 2048;          // two 32 x 32 blocks of O per softmax warp
+    static constexpr int kSlack = 768;                     // what two CTAs leave for aligning the tiles to 1024 bytes
+    static constexpr int kSmem = kQRing * kQ + 2 * kRing * kKV + kStaging + kSlack + 256;
     static_assert(2 * (kSmem + 1024) <= 233472, "two CTAs share an SM");
     static_assert((2 * kQRing + 4 * kRing + 3 * kS) * 8 <= 232, "barriers");
 };
@@ -122,13 +123,14 @@ struct RingAt {                                            // stage and phase of
 template <int DH, typename F>
 __device__ __forceinline__ bool take_maximum(float mt, uint32_t tO, bool later, float &m_used, float &l, F rest) {
     float factor = 1.f;
-    const bool grow = mt > m_used + 8.f;                  // also true on the first tile with a visible key
-    if (grow) {
-        factor = fast_exp2(m_used - mt);
+    bool rescale = false;
+    if (mt > m_used + 8.f) {                              // also true on the first tile with a visible key:
+        rescale = m_used != -INFINITY;                    // nothing to rescale then, the row's O is zero or not yet written
+        if (rescale) factor = fast_exp2(m_used - mt);
         m_used = mt;
         l *= factor;
     }
-    if (later && __any_sync(0xffffffffu, grow)) {
+    if (later && __any_sync(0xffffffffu, rescale)) {
         if (!rest()) return false;
         tc_fence_after();
 #pragma unroll 1
@@ -232,7 +234,9 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
             mbar_init(p_full + 8 * s, 4);
             mbar_init(pv_done + 8 * s, 1);
         }
-        *abort_flag = 0;
+        // a base that needs more alignment than the carve-out leaves cannot be used
+        *abort_flag = (int)(base - raw) > F::kSlack ? 1 : 0;
+        if (*abort_flag) atomicExch(&g_tc_fault, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 256);
@@ -240,6 +244,7 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;      // O (DH columns), then the S tiles (64 columns each)
+    const bool usable = *abort_flag == 0;
 
     // an item: one query tile of one head
     struct Item { int h, qt0, first, count; KeySpan span; };
@@ -256,7 +261,9 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
     // keys of a tile that take part: all, or the sinks at the head of the edge tile where the window does not reach it
     auto keys_of = [&](const Item &t, int j) { return j < t.span.ns && j == p.edge ? p.edge_keys : KT; };
 
-    if (warp == 0) {
+    if (!usable) {
+        // nothing was issued: fall through to the common exit
+    } else if (warp == 0) {
         if (lane == 0) {
             RingAt q, kv;
             bool alive = true;
@@ -341,7 +348,7 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
         const int row = quarter * 32 + lane;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t tO = tmem + lane_base;
-        const uint32_t stage = sO + quarter * 2048u;
+        const uint32_t stage0 = sO + quarter * 4096u;
         RingAt b, before;                                // S tile of this step and of the one before
         bool alive = true;
         // P V of the step before has completed.  One barrier per S tile: a warp may be a tile or two ahead of the others,
@@ -375,14 +382,15 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
             }
             if (!alive || !rest()) { alive = false; break; }
             tc_fence_after();
-            // O / l through a 32 x 32 block in shared memory (rows of 64 bytes, 64-byte swizzle) and TMA stores, which clip
+            // O / l through 32 x 32 blocks in shared memory (rows of 64 bytes, 64-byte swizzle) and TMA stores, which clip
             // the rows behind the last query; the warp's next P is handed over only after its O has been read
             const float inv = 1.f / l;
 #pragma unroll 1
             for (int c = 0; c < DH / 32; c++) {
                 uint32_t o[32];
                 tmem_ld32(tO + c * 32, o);
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                const uint32_t stage = stage0 + (c & 1) * 2048u;
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");    // the block before last
                 __syncwarp();
 #pragma unroll
                 for (int e = 0; e < 32; e += 8) {
