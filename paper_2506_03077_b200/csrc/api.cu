@@ -361,16 +361,17 @@ int window_shape(int64_t n, int64_t q0, int32_t Hq, int32_t Hkv, int32_t dh, int
 }
 // scratch of the windowed backward: delta, then the sums of the sink segments (the larger of the two engines' needs)
 struct WindowScratch { float *delta, *part; };
-template <int TILE_>
+template <int TK, int TQ>
 size_t window_part_floats(const WindowShape &w, int dh) {
-    const KeyWork<TILE_> k = key_work<TILE_>(w);
-    return k.segs > 1 ? (size_t)k.st * k.segs * w.Hkv * 2 * (w.sinks < TILE_ ? w.sinks : TILE_) * dh : 0;
+    const KeyWork<TK, TQ> k = key_work<TK, TQ>(w);
+    return k.segs > 1 ? (size_t)k.st * k.segs * w.Hkv * 2 * (w.sinks < TK ? w.sinks : TK) * dh : 0;
 }
 size_t window_scratch(const WindowShape &w, int dh, void *base, WindowScratch *out) {
     Arena a(base);
     a.take_bytes(kHeaderBytes);
     out->delta = a.take<float>((size_t)w.Hq * w.n);
-    const size_t x = window_part_floats<128>(w, dh), y = window_part_floats<32>(w, dh);
+    const size_t x = dh == 64 ? window_part_floats<128, kBwdRows64>(w, dh) : window_part_floats<128, kBwdRows128>(w, dh),
+                 y = window_part_floats<32, 32>(w, dh);
     out->part = a.take<float>(x > y ? x : y);
     return a.size();
 }
@@ -778,14 +779,7 @@ int streambp_attention_window_backward(const void *q, const void *k, const void 
     call_state().launches = 0;
     WsHeader *hdr = static_cast<WsHeader *>(workspace);
     const int mode = grad_dtype == STREAMBP_BF16 ? GRAD_BF16_SET : (accumulate ? GRAD_F32_ADD : GRAD_F32_SET);
-    // keys that no query of the chunk sees have no owner among the key tiles: their gradients are zero
     const int tile = tc ? 128 : 32;
-    const int64_t unseen = tc ? (int64_t)key_work<128>(w).lo * 128 : (int64_t)key_work<32>(w).lo * 32;
-    if (mode != GRAD_F32_ADD && unseen > 0) {
-        const size_t bytes = (size_t)unseen * n_kv_heads * head_dim * (grad_dtype == STREAMBP_BF16 ? 2 : 4);
-        SBP_TRY(fill_zero(dk, bytes, st));
-        SBP_TRY(fill_zero(dv, bytes, st));
-    }
     int rc;
     if (tc)
         rc = attention_window_bwd_tc((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o, lse, w,
@@ -797,7 +791,8 @@ int streambp_attention_window_backward(const void *q, const void *k, const void 
         rc = attention_window_bwd_simt<float>((const float *)q, (const float *)k, (const float *)v, (const float *)o,
                                               (const float *)d_o, lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
     SBP_TRY(rc);
-    const int segs = tc ? key_work<128>(w).segs : key_work<32>(w).segs;
+    const int segs = !tc ? key_work<32>(w).segs
+                         : (head_dim == 64 ? key_work<128, kBwdRows64>(w).segs : key_work<128, kBwdRows128>(w).segs);
     if (segs > 1) return attention_window_join(s.part, tile, segs, w, head_dim, mode, dk, dv, st);
     return STREAMBP_OK;
 }

@@ -45,10 +45,15 @@ __host__ __device__ constexpr uint32_t kstep(int kk) { return (uint32_t)((kk >> 
 __device__ __forceinline__ uint32_t mnlo(uint32_t tile) { return desc_lo(tile, SUB_BYTES); }
 __host__ __device__ constexpr uint32_t mnstep(int kk) { return (uint32_t)(kk * 128); }
 
-template <int DH>
+template <int DH, int SUB = SUB_BYTES>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int head, int row) {
 #pragma unroll
-    for (int c = 0; c < DH / 64; c++) tma_load_2d(dst + c * SUB_BYTES, map, bar, head * DH + c * 64, row);
+    for (int c = 0; c < DH / 64; c++) tma_load_2d(dst + c * SUB, map, bar, head * DH + c * 64, row);
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+    return v;
 }
 
 __device__ __forceinline__ float fast_exp2(float x) {
@@ -74,8 +79,9 @@ __device__ __forceinline__ uint32_t visible_rows(const WindowShape &w, int key, 
     return key < w.sinks ? behind : behind & below(key + w.window - at);
 }
 // Whether a (query tile, key tile) pair holds hidden pairs: the diagonal or the window's far edge crosses it.
+template <int ROWS, int KEYS>
 __device__ __forceinline__ bool mixed(const WindowShape &w, int q0, int k0) {
-    return k0 + TILE - 1 > q0 || (q0 + TILE - 1 - k0 >= w.window && k0 + TILE > w.sinks);
+    return k0 + KEYS - 1 > q0 || (q0 + ROWS - 1 - k0 >= w.window && k0 + KEYS > w.sinks);
 }
 
 __device__ __forceinline__ void leave(volatile int *abort_flag) {
@@ -362,7 +368,7 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
             for (int j = 0; j < t.count; j++) {
                 const int k0 = t.span.tile(j) * KT;
                 const uint32_t tS = tmem + DH + b.st * KT + lane_base;
-                const bool hidden = k0 + KT - 1 > t.first || (t.first + TILE - 1 - k0 >= p.w.window && k0 + KT > p.w.sinks);
+                const bool hidden = mixed<TILE, KT>(p.w, t.first, k0);
                 uint32_t see[2];
                 if (hidden) {
                     see[0] = visible_keys(p.w, q_abs, k0, 0);
@@ -426,28 +432,42 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
 // ---------------------------------------------------------------------------------------------------------------
 // backward
 // ---------------------------------------------------------------------------------------------------------------
+// What the two head sizes need of an SM decides their shape.  Heads of 128: inner tiles of 128 (every product a full one),
+// all of tensor memory, one CTA of sixteen softmax warps per SM.  Heads of 64: the products are short and what bounds an
+// iteration is its chain of loads, exponentials and hand-offs, so inner tiles of 64 and half of tensor memory let two
+// independent CTAs of eight softmax warps share an SM, each in the other's latencies.
+template <int DH> struct Bwd {
+    static constexpr int IT = DH == 64 ? kBwdRows64 : kBwdRows128;   // query rows (dK/dV role) or keys (dQ role) of an inner tile
+    static constexpr int kGroups = IT / 32;                          // softmax warpgroups, 32 columns of a row each
+    static constexpr int kThreads = 64 + 128 * kGroups;
+    static constexpr int kBlocks = DH == 64 ? 2 : 1;
+    static constexpr uint32_t kCols = DH == 64 ? 256 : 512;
+    static constexpr int kOut = TILE * DH * 2, kIn = IT * DH * 2;    // bytes of a resident and of an inner tile
+    static constexpr int kInSub = IT * 64 * 2;
+    static constexpr int kQStages = 3, kKStages = 3;
+    static constexpr int kSlack = 768;                               // what is left for aligning the tiles to 1024 bytes
+    static constexpr int kTiles = 2 * kOut + 5 * kIn;
+    static constexpr int kSmem = kTiles + 4 * IT * 4 /* lse, delta x 2 stages */ + 256 + kSlack;
+    static constexpr int kSums = 2 * DH * TILE * 4;                  // fp32 sums of a CTA that hands them to another
+    static_assert(kBlocks * (kSmem + 1024) <= 233472 && kSums <= kTiles, "backward roles exceed the shared memory of an SM");
+    typedef KeyWork<TILE, IT> Work;
+    __host__ __device__ static constexpr uint32_t step(int kk) { return (uint32_t)((kk >> 2) * (kInSub >> 4) + (kk & 3) * 2); }
+};
+template <int DH>
 struct BwdParams {
     WindowShape w;
-    KeyWork<TILE> work;
+    typename Bwd<DH>::Work work;
     const float *lse;     // [Hq, n]
     const float *delta;   // [Hq, n]
     void *dq, *dk, *dv;   // [n, Hq, DH], [q0 + n, Hkv, DH]
     float *part;          // [sink item][Hkv][dK, dV][part_rows][DH]
     int part_rows;
     int mode;             // GradMode of dk, dv (dq: fp32 or bf16, always overwritten)
+    int edge, edge_keys;  // dQ role: the sink tile that holds sinks in its first rows only (-1: none), those rows rounded up to 32
+    int cluster;          // CTAs that share the query heads of a dK/dV item
+    int n_dkdv, n_dq, n_dq_first;   // CTAs of the roles (multiples of the cluster); dQ CTAs that are dispatched first
     float scale, scale_log2;
 };
-
-template <int DH> struct Bwd {
-    static constexpr int kTile = TILE * DH * 2;
-    static constexpr int kQStages = 3, kKStages = 3;
-    static constexpr int kSlack = DH == 128 ? 768 : 1024;      // what the carve-out leaves for aligning the tiles to 1024 bytes
-    static constexpr int kSmemKV = (4 + kQStages) * kTile + 4 * TILE * 4 /* lse, delta x 2 stages */ + 256 + kSlack;
-    static constexpr int kSmemQ = (4 + kKStages) * kTile + 1024 + 256;
-    static constexpr int kSmem = kSmemKV > kSmemQ ? kSmemKV : kSmemQ;
-    static_assert(kSmem <= 232448, "backward roles exceed the shared memory of an SM");
-};
-constexpr int BWD_THREADS = 64 + 512;
 
 // 32 fp32 sums of one row to where the gradient goes
 __device__ __forceinline__ void put32(void *dst, long long at, const uint32_t (&r)[32], int mode) {
@@ -476,16 +496,16 @@ __device__ __forceinline__ void put32(void *dst, long long at, const uint32_t (&
 
 template <int DH>
 __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
-                                          const CUtensorMap &map_do, const BwdParams &p, uint8_t *smem_raw, int item, int g) {
+                                          const CUtensorMap &map_do, const BwdParams<DH> &p, uint8_t *smem_raw, int item, int g, int rank) {
     typedef Bwd<DH> W;
-    constexpr int T = W::kTile, QS = W::kQStages;
+    constexpr int T = W::kIn, QS = W::kQStages, IT = W::IT;
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
-    const uint32_t sK = base, sV = sK + T, sQ = sV + T, sdO = sQ + QS * T;
-    uint8_t *tail = smem_raw + (base - raw) + (4 + QS) * T;
-    float *s_lse = reinterpret_cast<float *>(tail);           // [2][128], pre-multiplied by log2(e)
-    float *s_delta = s_lse + 2 * TILE;                        // [2][128], pre-multiplied by the score scale
-    uint8_t *aux = tail + 4 * TILE * 4;
+    const uint32_t sK = base, sV = sK + W::kOut, sQ = sV + W::kOut, sdO = sQ + QS * T;
+    uint8_t *tail = smem_raw + (base - raw) + W::kTiles;
+    float *s_lse = reinterpret_cast<float *>(tail);           // [2][IT], pre-multiplied by log2(e)
+    float *s_delta = s_lse + 2 * IT;                          // [2][IT], pre-multiplied by the score scale
+    uint8_t *aux = tail + 4 * IT * 4;
     const uint32_t bars = smem_u32(aux);
     const uint32_t kv_full = bars, q_full = bars + 8, q_empty = bars + 32, do_full = bars + 56, do_empty = bars + 72,
                    rows_empty = bars + 88, s_full = bars + 104, dp_full = bars + 112, loaded = bars + 120,
@@ -498,8 +518,9 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
     int kt, qt_begin, qt_end, seg;
     p.work.item(p.w, item, kt, qt_begin, qt_end, seg);
     const int k_abs0 = kt * TILE;
-    const int per_head = qt_end - qt_begin;
-    const int iters = G * per_head;
+    // this CTA's query heads of the group, each over the item's query tiles
+    const int h_begin = g * G + G * rank / p.cluster, h_end = g * G + G * (rank + 1) / p.cluster;
+    const int iters = (h_end - h_begin) * (qt_end - qt_begin);
 
     if (threadIdx.x == 0) {
         mbar_init(kv_full, 1);
@@ -514,59 +535,60 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
         }
         mbar_init(s_full, 1);
         mbar_init(dp_full, 1);
-        mbar_init(loaded, 16);
-        mbar_init(p1_full, 16);
-        mbar_init(p2_full, 16);
+        mbar_init(loaded, 4 * W::kGroups);
+        mbar_init(p1_full, 4 * W::kGroups);
+        mbar_init(p2_full, 4 * W::kGroups);
         mbar_init(acc_full, 1);
         // a base that needs more alignment than the carve-out leaves cannot be used
         *abort_flag = (int)(base - raw) > W::kSlack ? 1 : 0;
         if (*abort_flag) atomicExch(&g_tc_fault, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), W::kCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    // columns: S^T at 0; dP^T at 128, later P^T (packed) in the first and dS^T (packed) in the second 16 columns of
-    // every 32-column group; dV at 256, dK behind it
-    const uint32_t tST = tmem, tDPT = tmem + 128, tDV = tmem + 256, tDK = tmem + 256 + DH;
+    // columns: S^T; dP^T, later P^T (packed) in the first and dS^T (packed) in the second 16 columns of every 32-column
+    // group; dV; dK
+    const uint32_t tST = tmem, tDPT = tST + IT, tDV = tDPT + IT, tDK = tDV + DH;
     const bool usable = *abort_flag == 0;
+    bool done = false;                     // softmax warps: the sums of this CTA are complete
 
     if (!usable) {
         // nothing was issued: fall through to the common exit
     } else if (warp == 0) {
         if (lane == 0 && iters > 0) {
-            mbar_expect_tx(kv_full, 2 * T);
+            mbar_expect_tx(kv_full, 2 * W::kOut);
             load_tile<DH>(sK, &map_k, kv_full, g, k_abs0);
             load_tile<DH>(sV, &map_v, kv_full, g, k_abs0);
         }
         uint32_t sq = 0, qph = 0;
-        int h = g * G, qt = qt_begin;
+        int h = h_begin, qt = qt_begin;
         for (int it = 0; it < iters; it++) {
-            const int qt0 = qt * TILE;
+            const int qt0 = qt * IT;
             const uint32_t sd = it & 1, dph = (it >> 1) & 1;
             int ok = 1;
             if (lane == 0) {
                 ok = mbar_wait(q_empty + 8 * sq, qph ^ 1u, abort_flag) ? 1 : 0;          // dK of the stage's last user
                 if (ok) {
                     mbar_expect_tx(q_full + 8 * sq, T);
-                    load_tile<DH>(sQ + sq * T, &map_q, q_full + 8 * sq, h, qt0);
+                    load_tile<DH, W::kInSub>(sQ + sq * T, &map_q, q_full + 8 * sq, h, qt0);
                     ok = mbar_wait(do_empty + 8 * sd, dph ^ 1u, abort_flag) ? 1 : 0;     // dV of the stage's last user
                 }
                 if (ok) {
                     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(do_full + 8 * sd), "r"(T) : "memory");
-                    load_tile<DH>(sdO + sd * T, &map_do, do_full + 8 * sd, h, qt0);
+                    load_tile<DH, W::kInSub>(sdO + sd * T, &map_do, do_full + 8 * sd, h, qt0);
                     ok = mbar_wait(rows_empty + 8 * sd, dph ^ 1u, abort_flag) ? 1 : 0;   // delta rows: read until dS^T is packed
                 }
             }
             ok = __shfl_sync(0xffffffffu, ok, 0);
             if (!ok) break;
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const int col = lane * 4 + e, r = qt0 + col;
-                s_lse[sd * TILE + col] = r < p.w.n ? p.lse[(long long)h * p.w.n + r] * kLog2e : 0.f;
-                s_delta[sd * TILE + col] = r < p.w.n ? p.delta[(long long)h * p.w.n + r] * p.scale : 0.f;
+            for (int e = 0; e < IT / 32; e++) {
+                const int col = lane * (IT / 32) + e, r = qt0 + col;
+                s_lse[sd * IT + col] = r < p.w.n ? p.lse[(long long)h * p.w.n + r] * kLog2e : 0.f;
+                s_delta[sd * IT + col] = r < p.w.n ? p.delta[(long long)h * p.w.n + r] * p.scale : 0.f;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(do_full + 8 * sd);   // publishes the rows; the phase completes when dO has landed too
@@ -575,7 +597,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
         }
     } else if (warp == 1) {
         // the whole warp runs the issue loop; each MMA / commit executes in one elected lane
-        constexpr uint32_t idesc_kk = make_idesc(TILE, TILE, false, false);     // both operands K-major
+        constexpr uint32_t idesc_kk = make_idesc(TILE, IT, false, false);       // both operands K-major
         constexpr uint32_t idesc_acc = make_idesc(TILE, DH, false, true);       // B MN-major (N = head dims)
         bool alive = iters == 0 || mbar_wait_warp(kv_full, 0, abort_flag);
         const uint32_t k_lo = klo(sK), v_lo = klo(sV);
@@ -586,7 +608,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             tc_fence_after();
             const uint32_t q_lo = klo(sQ + sq_s * T);
 #pragma unroll
-            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tST, k_lo + kstep(kk), q_lo + kstep(kk), idesc_kk, kk != 0);
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tST, k_lo + kstep(kk), q_lo + W::step(kk), idesc_kk, kk != 0);
             umma_commit_w(s_full);
             if (++sq_s == QS) { sq_s = 0; qph_s ^= 1u; }
             return true;
@@ -596,7 +618,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             tc_fence_after();
             const uint32_t do_lo = klo(sdO + (it & 1) * T);
 #pragma unroll
-            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tDPT, v_lo + kstep(kk), do_lo + kstep(kk), idesc_kk, kk != 0);
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tDPT, v_lo + kstep(kk), do_lo + W::step(kk), idesc_kk, kk != 0);
             umma_commit_w(dp_full);
             return true;
         };
@@ -612,17 +634,17 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             // dV += P^T dO as soon as P^T is packed (first 16 columns of each group of the dP^T region)
             if (!mbar_wait_warp(p1_full, it & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
-            const uint32_t do_mn = mnlo(sdO + sd * T);
+            const uint32_t do_mn = desc_lo(sdO + sd * T, W::kInSub);
 #pragma unroll
-            for (int kk = 0; kk < 8; kk++)
+            for (int kk = 0; kk < IT / 16; kk++)
                 umma_ts_w(tDV, tDPT + (kk >> 1) * 32 + (kk & 1) * 8, do_mn + mnstep(kk), idesc_acc, (it | kk) != 0);
             umma_commit_w(do_empty + 8 * sd);            // dO of this stage is consumed (dP^T was issued earlier)
             // dK += dS^T Q (second 16 columns of each group)
             if (!mbar_wait_warp(p2_full, it & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
-            const uint32_t q_mn = mnlo(sQ + sq_k * T);
+            const uint32_t q_mn = desc_lo(sQ + sq_k * T, W::kInSub);
 #pragma unroll
-            for (int kk = 0; kk < 8; kk++)
+            for (int kk = 0; kk < IT / 16; kk++)
                 umma_ts_w(tDK, tDPT + (kk >> 1) * 32 + 16 + (kk & 1) * 8, q_mn + mnstep(kk), idesc_acc, (it | kk) != 0);
             umma_commit_w(q_empty + 8 * sq_k);           // Q of this stage is consumed
             umma_commit_w(rows_empty + 8 * sd);          // and so are the lse / delta rows
@@ -633,7 +655,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
         if (alive && iters > 0) umma_commit_w(acc_full);
     } else {
         const int quarter = warp & 3;
-        const int wg = (warp - 2) >> 2;                           // 0..3: 32-query group of the tile
+        const int wg = (warp - 2) >> 2;                           // 32-query group of the tile
         const int col_base = wg * 32;
         const int row = quarter * 32 + lane;                      // key row within the tile
         const int k_abs = k_abs0 + row;
@@ -645,7 +667,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
         bool alive = true;
         int qt = qt_begin;
         for (int it = 0; it < iters && alive; it++) {
-            const int q_abs0 = p.w.q0 + qt * TILE;
+            const int q_abs0 = p.w.q0 + qt * IT;
             const uint32_t sd = it & 1;
             if (!mbar_wait(s_full, it & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
@@ -656,8 +678,26 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             if (lane == 0) mbar_arrive(loaded);
             // the producer's lse / delta rows of this stage are published together with the dO tile
             if (!mbar_wait(do_full + 8 * sd, (it >> 1) & 1, abort_flag)) { alive = false; break; }
-            const uint32_t see = mixed(p.w, q_abs0, k_abs0) ? visible_rows(p.w, k_abs, q_abs0, col_base) : 0xffffffffu;
-            const float *lse2 = s_lse + sd * TILE + col_base, *dl = s_delta + sd * TILE + col_base;
+            const uint32_t see = mixed<IT, TILE>(p.w, q_abs0, k_abs0) ? visible_rows(p.w, k_abs, q_abs0, col_base) : 0xffffffffu;
+            if (!__any_sync(0xffffffffu, see != 0u)) {     // P and dS of all of the warp's pairs are zero
+                if (!mbar_wait(dp_full, it & 1, abort_flag)) { alive = false; break; }
+                tc_fence_after();
+                uint32_t zero[16];
+#pragma unroll
+                for (int e = 0; e < 16; e++) zero[e] = 0u;
+                tmem_st16(tP_g, zero);
+                tmem_st16(tP_g + 16, zero);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(p1_full);
+                    mbar_arrive(p2_full);
+                }
+                if (++qt == qt_end) qt = qt_begin;
+                continue;
+            }
+            const float *lse2 = s_lse + sd * IT + col_base, *dl = s_delta + sd * IT + col_base;
             // phase 1: P^T = exp2(S^T * scale - lse), all the dV product needs
             float pv[32];
 #pragma unroll
@@ -707,27 +747,59 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             }
             if (++qt == qt_end) qt = qt_begin;
         }
-        if (alive && (iters == 0 || mbar_wait(acc_full, 0, abort_flag)) && wg < DH / 32) {
-            tc_fence_after();
-            // group wg writes head dims 32*wg .. 32*wg+31
-            uint32_t rv[32], rk[32];
-            if (iters > 0) {
-                tmem_ld32(tDV + lane_base + col_base, rv);
-                tmem_ld32(tDK + lane_base + col_base, rk);
-            } else {
+        done = alive && (iters == 0 || mbar_wait(acc_full, 0, abort_flag));
+    }
+
+    // The CTAs of a cluster hold sums over different heads of the group: the others leave theirs in their shared memory (all
+    // copies and products are done there), the first adds them to its own in the order of the ranks.
+    __syncwarp();
+    const int wg = (warp - 2) >> 2, row = (warp & 3) * 32 + lane, col_base = wg * 32, k_abs = k_abs0 + row;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const bool writes = warp >= 2 && wg < DH / 32;       // group wg holds head dims 32 * wg ..
+    uint32_t rv[32], rk[32];
+    if (writes && done) {
+        tc_fence_after();
+        if (iters > 0) {
+            tmem_ld32(tDV + lane_base + col_base, rv);
+            tmem_ld32(tDK + lane_base + col_base, rk);
+        } else {
 #pragma unroll
-                for (int e = 0; e < 32; e++) rv[e] = rk[e] = 0u;
+            for (int e = 0; e < 32; e++) rv[e] = rk[e] = 0u;
+        }
+    }
+    if (p.cluster > 1) {
+        float *sums = reinterpret_cast<float *>(smem_raw + (base - raw));      // [dV, dK][DH][128 rows]
+        __syncthreads();                                  // every role of this CTA is through with the tiles
+        if (rank > 0 && writes && done) {
+#pragma unroll
+            for (int e = 0; e < 32; e++) {
+                sums[(col_base + e) * TILE + row] = __uint_as_float(rv[e]);
+                sums[(DH + col_base + e) * TILE + row] = __uint_as_float(rk[e]);
             }
-            const bool joined = seg >= 0 && row < sink_rows<TILE>(p.w, kt);
-            if (joined) {                                         // this segment's share of a sink key's sums
-                float *part = p.part + (((long long)item * p.w.Hkv + g) * 2 * p.part_rows + row) * DH + col_base;
-                put32(part, 0, rk, GRAD_F32_SET);
-                put32(part, (long long)p.part_rows * DH, rv, GRAD_F32_SET);
-            } else if (seg <= 0 && k_abs < p.w.q0 + p.w.n) {      // segments behind the first have nothing for these rows
-                const long long at = ((long long)k_abs * p.w.Hkv + g) * DH + col_base;
-                put32(p.dv, at, rv, p.mode);
-                put32(p.dk, at, rk, p.mode);
+        }
+        cluster_sync_all();
+        if (rank == 0 && writes && done) {
+            const uint32_t own = smem_u32(sums) + (uint32_t)(col_base * TILE + row) * 4u;
+            for (int r = 1; r < p.cluster; r++) {
+                const uint32_t from = map_to_cta(own, (uint32_t)r);
+#pragma unroll
+                for (int e = 0; e < 32; e++) {
+                    rv[e] = __float_as_uint(__uint_as_float(rv[e]) + ld_cluster_f32(from + (uint32_t)e * TILE * 4u));
+                    rk[e] = __float_as_uint(__uint_as_float(rk[e]) + ld_cluster_f32(from + (uint32_t)(DH + e) * TILE * 4u));
+                }
             }
+        }
+    }
+    if (rank == 0 && writes && done) {
+        const bool joined = seg >= 0 && row < sink_rows<TILE>(p.w, kt);
+        if (joined) {                                     // this segment's share of a sink key's sums
+            float *part = p.part + (((long long)item * p.w.Hkv + g) * 2 * p.part_rows + row) * DH + col_base;
+            put32(part, 0, rk, GRAD_F32_SET);
+            put32(part, (long long)p.part_rows * DH, rv, GRAD_F32_SET);
+        } else if (seg <= 0 && k_abs < p.w.q0 + p.w.n) {  // segments behind the first have nothing for these rows
+            const long long at = ((long long)k_abs * p.w.Hkv + g) * DH + col_base;
+            put32(p.dv, at, rv, p.mode);
+            put32(p.dk, at, rk, p.mode);
         }
     }
 
@@ -735,22 +807,24 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
     leave(abort_flag);
     tc_fence_before();
     __syncthreads();
+    if (p.cluster > 1) cluster_sync_all();                // no CTA leaves while another may read its sums
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc(tmem, W::kCols);
     }
 }
 
 template <int DH>
 __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
-                                        const CUtensorMap &map_do, const BwdParams &p, uint8_t *smem_raw, int block_x, int h) {
+                                        const CUtensorMap &map_do, const CUtensorMap &map_ke, const CUtensorMap &map_ve,
+                                        const BwdParams<DH> &p, uint8_t *smem_raw, int block_x, int h) {
     typedef Bwd<DH> W;
-    constexpr int T = W::kTile, KS = W::kKStages;
+    constexpr int T = W::kIn, KS = W::kKStages, IT = W::IT;
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
     // K tiles live from S_j to dQ_j, so their ring has three stages; V tiles are released right after dP_j (two stages)
-    const uint32_t sQ = base, sdO = sQ + T, sK = sdO + T, sV = sK + KS * T;
-    uint8_t *aux = smem_raw + (base - raw) + (4 + KS) * T;
+    const uint32_t sQ = base, sdO = sQ + W::kOut, sK = sdO + W::kOut, sV = sK + KS * T;
+    uint8_t *aux = smem_raw + (base - raw) + W::kTiles + 4 * IT * 4;
     const uint32_t bars = smem_u32(aux);
     const uint32_t q_full = bars, k_full = bars + 8, k_empty = bars + 32, v_full = bars + 56, v_empty = bars + 72,
                    s_full = bars + 88, dp_full = bars + 96, s_free = bars + 104, p2_full = bars + 112,
@@ -763,8 +837,9 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
     const int qt0 = block_x * TILE;
     const int q_abs0 = p.w.q0 + qt0;
     const int rows_here = (p.w.n - qt0) < TILE ? (p.w.n - qt0) : TILE;
-    const KeySpan span = key_span<TILE>(p.w, q_abs0, q_abs0 + rows_here - 1);
+    const KeySpan span = key_span<IT>(p.w, q_abs0, q_abs0 + rows_here - 1);
     const int nkv = span.count();
+    auto keys_of = [&](int j) { return j < span.ns && j == p.edge ? p.edge_keys : IT; };
 
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
@@ -778,52 +853,57 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
         }
         mbar_init(s_full, 1);
         mbar_init(dp_full, 1);
-        mbar_init(s_free, 16);
-        mbar_init(p2_full, 16);
+        mbar_init(s_free, 4 * W::kGroups);
+        mbar_init(p2_full, 4 * W::kGroups);
         mbar_init(acc_full, 1);
-        *abort_flag = 0;
+        // a base that needs more alignment than the carve-out leaves cannot be used
+        *abort_flag = (int)(base - raw) > W::kSlack ? 1 : 0;
+        if (*abort_flag) atomicExch(&g_tc_fault, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), W::kCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    // columns: S at 0, dP at 128, dQ at 256
-    const uint32_t tS = tmem, tDP = tmem + 128, tDQ = tmem + 256;
+    // columns: S, dP, dQ
+    const uint32_t tS = tmem, tDP = tS + IT, tDQ = tDP + IT;
+    const bool usable = *abort_flag == 0;
 
-    if (warp == 0) {
+    if (!usable) {
+        // nothing was issued: fall through to the common exit
+    } else if (warp == 0) {
         if (lane == 0) {
-            mbar_expect_tx(q_full, 2 * T);
+            mbar_expect_tx(q_full, 2 * W::kOut);
             load_tile<DH>(sQ, &map_q, q_full, h, qt0);
             load_tile<DH>(sdO, &map_do, q_full, h, qt0);
             uint32_t ks = 0, kph = 0;
             for (int j = 0; j < nkv; j++) {
-                const int row = span.tile(j) * TILE;
+                const int row = span.tile(j) * IT, keys = keys_of(j);
+                const uint32_t bytes = (uint32_t)keys * DH * 2u;
                 if (!mbar_wait(k_empty + 8 * ks, kph ^ 1u, abort_flag)) break;
-                mbar_expect_tx(k_full + 8 * ks, T);
-                load_tile<DH>(sK + ks * T, &map_k, k_full + 8 * ks, g, row);
+                mbar_expect_tx(k_full + 8 * ks, bytes);
+                load_tile<DH, W::kInSub>(sK + ks * T, keys < IT ? &map_ke : &map_k, k_full + 8 * ks, g, row);
                 if (++ks == KS) { ks = 0; kph ^= 1u; }
                 const uint32_t vs = j & 1, vph = (j >> 1) & 1;
                 if (!mbar_wait(v_empty + 8 * vs, vph ^ 1u, abort_flag)) break;
-                mbar_expect_tx(v_full + 8 * vs, T);
-                load_tile<DH>(sV + vs * T, &map_v, v_full + 8 * vs, g, row);
+                mbar_expect_tx(v_full + 8 * vs, bytes);
+                load_tile<DH, W::kInSub>(sV + vs * T, keys < IT ? &map_ve : &map_v, v_full + 8 * vs, g, row);
             }
         }
     } else if (warp == 1) {
         // the whole warp runs the issue loop; each MMA / commit executes in one elected lane
-        constexpr uint32_t idesc_kk = make_idesc(TILE, TILE, false, false);
         constexpr uint32_t idesc_acc = make_idesc(TILE, DH, false, true);
         bool alive = mbar_wait_warp(q_full, 0, abort_flag);
         const uint32_t q_lo = klo(sQ), do_lo = klo(sdO);
         // K stage and phase of the tile whose S is issued next / whose dQ is issued next
         uint32_t ks_s = 0, kph_s = 0, ks_q = 0;
-        auto issue_s = [&]() -> bool {             // S = Q K^T
+        auto issue_s = [&](int j) -> bool {        // S = Q K^T
             if (!mbar_wait_warp(k_full + 8 * ks_s, kph_s, abort_flag)) return false;
             tc_fence_after();
             const uint32_t k_lo = klo(sK + ks_s * T);
 #pragma unroll
-            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tS, q_lo + kstep(kk), k_lo + kstep(kk), idesc_kk, kk != 0);
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tS, q_lo + kstep(kk), k_lo + W::step(kk), make_idesc(TILE, keys_of(j), false, false), kk != 0);
             umma_commit_w(s_full);
             if (++ks_s == KS) { ks_s = 0; kph_s ^= 1u; }
             return true;
@@ -834,25 +914,26 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
             tc_fence_after();
             const uint32_t v_lo = klo(sV + vs * T);
 #pragma unroll
-            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tDP, do_lo + kstep(kk), v_lo + kstep(kk), idesc_kk, kk != 0);
+            for (int kk = 0; kk < DH / 16; kk++) umma_ss_w(tDP, do_lo + kstep(kk), v_lo + W::step(kk), make_idesc(TILE, keys_of(j), false, false), kk != 0);
             umma_commit_w(v_empty + 8 * vs);             // V of this stage is consumed
             umma_commit_w(dp_full);
             return true;
         };
-        if (alive) alive = issue_s() && issue_dp(0);
+        if (alive) alive = issue_s(0) && issue_dp(0);
         for (int j = 0; j < nkv && alive; j++) {
             if (j + 1 < nkv) {
                 // next tile's S as soon as the softmax warps have read this tile's S into registers
                 if (!mbar_wait_warp(s_free, j & 1, abort_flag)) { alive = false; break; }
                 tc_fence_after();
-                if (!issue_s()) { alive = false; break; }
+                if (!issue_s(j + 1)) { alive = false; break; }
             }
             if (!mbar_wait_warp(p2_full, j & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
-            const uint32_t k_mn = mnlo(sK + ks_q * T);
+            const uint32_t k_mn = desc_lo(sK + ks_q * T, W::kInSub);
+            const int slices = keys_of(j) / 16;
 #pragma unroll
-            for (int kk = 0; kk < 8; kk++)
-                umma_ts_w(tDQ, tDP + (kk >> 1) * 32 + (kk & 1) * 8, k_mn + mnstep(kk), idesc_acc, (j | kk) != 0);
+            for (int kk = 0; kk < IT / 16; kk++)
+                if (kk < slices) umma_ts_w(tDQ, tDP + (kk >> 1) * 32 + (kk & 1) * 8, k_mn + mnstep(kk), idesc_acc, (j | kk) != 0);
             umma_commit_w(k_empty + 8 * ks_q);           // K of this stage is consumed
             if (++ks_q == KS) ks_q = 0;
             // the dP columns are free once dQ has read dS (in order)
@@ -861,7 +942,7 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
         if (alive) umma_commit_w(acc_full);
     } else {
         const int quarter = warp & 3;
-        const int wg = (warp - 2) >> 2;                           // 0..3: 32-key group of the tile
+        const int wg = (warp - 2) >> 2;                           // 32-key group of the tile
         const int key_base = wg * 32;
         const int row = quarter * 32 + lane;
         const int qr = qt0 + row;
@@ -872,10 +953,25 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
         const float neg_delta_s = qr < p.w.n ? -p.delta[(long long)h * p.w.n + qr] * p.scale : 0.f;
         bool alive = true;
         for (int j = 0; j < nkv && alive; j++) {
-            const int k_abs0 = span.tile(j) * TILE;
+            const int k_abs0 = span.tile(j) * IT;
             if (!mbar_wait(s_full, j & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
-            const uint32_t see = mixed(p.w, q_abs0, k_abs0) ? visible_keys(p.w, q_abs, k_abs0, key_base) : 0xffffffffu;
+            const uint32_t see = mixed<TILE, IT>(p.w, q_abs0, k_abs0) ? visible_keys(p.w, q_abs, k_abs0, key_base) : 0xffffffffu;
+            if (!__any_sync(0xffffffffu, see != 0u)) {     // dS of all of the warp's pairs is zero
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_free);
+                if (!mbar_wait(dp_full, j & 1, abort_flag)) { alive = false; break; }
+                tc_fence_after();
+                uint32_t zero[16];
+#pragma unroll
+                for (int e = 0; e < 16; e++) zero[e] = 0u;
+                tmem_st16(tP_g, zero);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p2_full);
+                continue;
+            }
             // phase 1: P from S; the S columns are handed back to the tensor pipe right after the load
             float pv[32];
             {
@@ -925,34 +1021,45 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
     __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc(tmem, W::kCols);
     }
 }
 
 template <int DH>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
+__global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
     attn_window_bwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                            const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
-                           const BwdParams p, int n_dkdv, int n_dq_first) {
+                           const __grid_constant__ CUtensorMap map_qi, const __grid_constant__ CUtensorMap map_ki,
+                           const __grid_constant__ CUtensorMap map_vi, const __grid_constant__ CUtensorMap map_doi,
+                           const __grid_constant__ CUtensorMap map_ke, const __grid_constant__ CUtensorMap map_ve,
+                           const __grid_constant__ BwdParams<DH> p) {
     pdl_enter();
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // dispatch order: n_dq_first dQ CTAs (all of them or none), then the dK/dV CTAs, then the rest
     const int b = (int)blockIdx.x;
-    const bool dq_role = b < n_dq_first || b >= n_dq_first + n_dkdv;
+    const bool dq_role = b < p.n_dq_first || b >= p.n_dq_first + p.n_dkdv;
     if (!dq_role) {
-        const int c = b - n_dq_first;
-        dkdv_body<DH>(map_q, map_k, map_v, map_do, p, smem_raw, c / p.w.Hkv, c % p.w.Hkv);
+        const int c = b - p.n_dq_first, unit = c / p.cluster;
+        dkdv_body<DH>(map_qi, map_k, map_v, map_doi, p, smem_raw, unit / p.w.Hkv, unit % p.w.Hkv, c % p.cluster);
     } else {
-        const int c = b < n_dq_first ? b : b - n_dkdv;
-        dq_body<DH>(map_q, map_k, map_v, map_do, p, smem_raw, p.work.q_tiles - 1 - c % p.work.q_tiles, c / p.work.q_tiles);
+        const int c = b < p.n_dq_first ? b : b - p.n_dkdv, tiles = (p.w.n + TILE - 1) / TILE;
+        if (c < tiles * p.w.Hq)                           // the role is padded to whole clusters
+            dq_body<DH>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, p, smem_raw, tiles - 1 - c % tiles, c / tiles);
     }
 }
 
 // delta[h, i] = sum_j dO[i, h, j] O[i, h, j]: one 16-byte load of each per thread, DH / 8 threads to a row
 template <int DH>
-__global__ void __launch_bounds__(256) window_delta_kernel(const bf16 *o, const bf16 *dout, int n, int Hq, float *delta, WsHeader *hdr) {
+__global__ void __launch_bounds__(256) window_delta_kernel(const bf16 *o, const bf16 *dout, int n, int Hq, float *delta, WsHeader *hdr,
+                                                           void *dk, void *dv, long long unseen16) {
     pdl_enter();
     if (blockIdx.x == 0 && threadIdx.x == 0) clear_status(hdr);
+    // rows of dk and dv that no query of the chunk sees have no owner among the key tiles: their gradients are zero (sink rows
+    // among them are written later in the stream)
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < unseen16; i += (long long)gridDim.x * 256) {
+        static_cast<uint4 *>(dk)[i] = make_uint4(0u, 0u, 0u, 0u);
+        static_cast<uint4 *>(dv)[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
     constexpr int kLanes = DH / 8;
     const long long rows = (long long)n * Hq, step = (long long)gridDim.x * (256 / kLanes);
     const int sub = threadIdx.x % kLanes;
@@ -971,70 +1078,85 @@ __global__ void __launch_bounds__(256) window_delta_kernel(const bf16 *o, const 
     }
 }
 
+#ifndef CMAX
+#define CMAX 4
+#endif
+#ifndef CNUM
+#define CNUM 4
+#endif
 template <typename K>
 bool opt_in_smem(K kernel, int bytes) {
     return cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
 }
 
-struct Maps { CUtensorMap q, k, v, d; };
-bool make_maps(Maps &m, const WindowShape &w, int DH, const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *dout) {
-    const int64_t kv = (int64_t)w.q0 + w.n;
-    return make_tensor_map(&m.q, q, w.n, (int64_t)w.Hq * DH, (int64_t)w.Hq * DH, 64, TILE, false) &&
-           make_tensor_map(&m.k, k, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, TILE, false) &&
-           make_tensor_map(&m.v, v, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, TILE, false) &&
-           (!dout || make_tensor_map(&m.d, dout, w.n, (int64_t)w.Hq * DH, (int64_t)w.Hq * DH, 64, TILE, false));
+// [rows, heads, DH] as tiles of `box` rows and 64 columns
+template <int DH>
+bool tile_map(CUtensorMap *m, const bf16 *p, int64_t rows, int heads, uint32_t box) {
+    return make_tensor_map(m, p, rows, (int64_t)heads * DH, (int64_t)heads * DH, 64, box, false);
+}
+// The sink tile (of T keys) whose last rows are no sinks is read, multiplied and exponentiated only as far as its sinks go.
+// `unit`: 16, or 32 where a warp reads all of the 32 columns that it sees some of.
+template <int T>
+void edge_of(const WindowShape &w, int unit, int &edge, int &keys) {
+    edge = w.sinks % T ? w.sinks / T : -1;
+    keys = (w.sinks % T + unit - 1) / unit * unit;
+    if (keys == T) edge = -1;
+    if (edge < 0) keys = unit;
 }
 
 template <int DH>
 int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, bf16 *o, float *lse, cudaStream_t st) {
     typedef Fwd<DH> F;
-    Maps m;
-    if (!make_maps(m, w, DH, q, k, v, nullptr)) return STREAMBP_E_CUDA;
     FwdParams p;
     memset(&p, 0, sizeof(p));
     p.w = w;
     p.lse = lse;
     p.scale_log2 = kLog2e / sqrtf((float)DH);
     p.q_tiles = (w.n + TILE - 1) / TILE;
-    const int64_t items = (int64_t)p.q_tiles * w.Hq;
+    const int64_t items = (int64_t)p.q_tiles * w.Hq, kv = (int64_t)w.q0 + w.n;
     if (items > 0x7fffffff / 2) return STREAMBP_E_SHAPE;
     p.items = (int)items;
-    // the sink tile whose last rows are no sinks is read, multiplied and exponentiated only as far as its sinks go
-    p.edge = w.sinks % KT ? w.sinks / KT : -1;
-    p.edge_keys = (w.sinks % KT + 15) / 16 * 16;
-    if (p.edge_keys == KT) p.edge = -1;
-    const int64_t kv = (int64_t)w.q0 + w.n;
-    const uint32_t box = p.edge >= 0 ? (uint32_t)p.edge_keys : 16u;
-    CUtensorMap ke, ve, mo;
-    if (!make_tensor_map(&m.k, k, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, KT, false) ||
-        !make_tensor_map(&m.v, v, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, KT, false) ||
-        !make_tensor_map(&ke, k, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, box, false) ||
-        !make_tensor_map(&ve, v, kv, (int64_t)w.Hkv * DH, (int64_t)w.Hkv * DH, 64, box, false) ||
+    edge_of<KT>(w, 16, p.edge, p.edge_keys);
+    CUtensorMap mq, mk, mv, ke, ve, mo;
+    if (!tile_map<DH>(&mq, q, w.n, w.Hq, TILE) || !tile_map<DH>(&mk, k, kv, w.Hkv, KT) || !tile_map<DH>(&mv, v, kv, w.Hkv, KT) ||
+        !tile_map<DH>(&ke, k, kv, w.Hkv, (uint32_t)p.edge_keys) || !tile_map<DH>(&ve, v, kv, w.Hkv, (uint32_t)p.edge_keys) ||
         !make_tensor_map(&mo, o, w.n, (int64_t)w.Hq * DH, (int64_t)w.Hq * DH, 32, 32, false, CU_TENSOR_MAP_SWIZZLE_64B))
         return STREAMBP_E_CUDA;
     static PerDevice configured;
     if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
     const int slots = 2 * sm_count();
-    SBP_LAUNCH(attn_window_fwd_kernel<DH>, p.items < slots ? p.items : slots, F::kThreads, F::kSmem, st, m.q, m.k, m.v, ke, ve, mo, p);
+    SBP_LAUNCH(attn_window_fwd_kernel<DH>, p.items < slots ? p.items : slots, F::kThreads, F::kSmem, st, mq, mk, mv, ke, ve, mo, p);
     return STREAMBP_OK;
 }
 
 template <int DH>
 int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf16 *dout, const float *lse, const WindowShape &w,
             int mode, void *dq, void *dk, void *dv, float *delta, float *part, WsHeader *hdr, cudaStream_t st) {
-    Maps m;
-    if (!make_maps(m, w, DH, q, k, v, dout)) return STREAMBP_E_CUDA;
-    static PerDevice configured;
-    if (!configured.get([] { return opt_in_smem(attn_window_bwd_kernel<DH>, Bwd<DH>::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
-    {
-        const int64_t blocks = ((int64_t)w.n * w.Hq * (DH / 8) + 255) / 256, most = (int64_t)sm_count() * 8;
-        SBP_LAUNCH(window_delta_kernel<DH>, (unsigned)(blocks < most ? blocks : most), 256, 0, st, o, dout, w.n, w.Hq, delta, hdr);
-    }
-    const float scale = 1.f / sqrtf((float)DH);
-    BwdParams p;
+    typedef Bwd<DH> W;
+    constexpr int IT = W::IT;
+    BwdParams<DH> p;
     memset(&p, 0, sizeof(p));
     p.w = w;
-    p.work = key_work<TILE>(w);
+    p.work = key_work<TILE, IT>(w);
+    edge_of<IT>(w, 32, p.edge, p.edge_keys);
+    const int64_t kv = (int64_t)w.q0 + w.n;
+    const uint32_t edge = (uint32_t)p.edge_keys;
+    CUtensorMap m[10];       // resident tiles of q, k, v, dO; inner tiles of the same; edge tiles of k, v
+    if (!tile_map<DH>(&m[0], q, w.n, w.Hq, TILE) || !tile_map<DH>(&m[1], k, kv, w.Hkv, TILE) || !tile_map<DH>(&m[2], v, kv, w.Hkv, TILE) ||
+        !tile_map<DH>(&m[3], dout, w.n, w.Hq, TILE) || !tile_map<DH>(&m[4], q, w.n, w.Hq, IT) || !tile_map<DH>(&m[5], k, kv, w.Hkv, IT) ||
+        !tile_map<DH>(&m[6], v, kv, w.Hkv, IT) || !tile_map<DH>(&m[7], dout, w.n, w.Hq, IT) || !tile_map<DH>(&m[8], k, kv, w.Hkv, edge) ||
+        !tile_map<DH>(&m[9], v, kv, w.Hkv, edge))
+        return STREAMBP_E_CUDA;
+    static PerDevice configured;
+    if (!configured.get([] { return opt_in_smem(attn_window_bwd_kernel<DH>, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+    {
+        const int64_t unseen16 = mode == GRAD_F32_ADD ? 0 : (int64_t)p.work.lo * TILE * w.Hkv * DH * (mode == GRAD_BF16_SET ? 2 : 4) / 16;
+        const int64_t rows = (int64_t)w.n * w.Hq * (DH / 8), work = rows > unseen16 ? rows : unseen16;
+        const int64_t blocks = (work + 255) / 256, most = (int64_t)sm_count() * 8;
+        SBP_LAUNCH(window_delta_kernel<DH>, (unsigned)(blocks < most ? blocks : most), 256, 0, st, o, dout, w.n, w.Hq, delta, hdr, dk, dv,
+                   (long long)unseen16);
+    }
+    const float scale = 1.f / sqrtf((float)DH);
     p.lse = lse; p.delta = delta;
     p.dq = dq; p.dk = dk; p.dv = dv;
     p.part = part;
@@ -1042,15 +1164,39 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     p.mode = mode;
     p.scale = scale;
     p.scale_log2 = scale * kLog2e;
-    const int64_t n_dkdv = (int64_t)p.work.items() * w.Hkv, n_dq = (int64_t)p.work.q_tiles * w.Hq;
+    // Costs in units of a quarter of a dQ inner tile (a dK/dV one takes ~1.25x: four products against three).
+    const int G = w.Hq / w.Hkv, q_tiles = (w.n + TILE - 1) / TILE;
+    const int64_t span = w.window / IT + 2 + (w.sinks + IT - 1) / IT, most_keys = (kv + IT - 1) / IT;
+    const int64_t dq_longest = 4 * (span < most_keys ? span : most_keys);
+    const int64_t walk = p.work.len < p.work.q_tiles ? p.work.len : p.work.q_tiles;
+    const int64_t n_units = (int64_t)p.work.items() * w.Hkv, slots = (int64_t)W::kBlocks * sm_count();
+    const int64_t total = n_units * 5 * G * walk + (int64_t)q_tiles * w.Hq * dq_longest;
+    // A dK/dV item whose walk is a good part of the whole launch's time on a slot is shared by a cluster of two or four CTAs
+    p.cluster = 1;
+    while (p.cluster < CMAX && 2 * p.cluster <= G && 5 * G * walk * slots * CNUM > total * p.cluster * 4) p.cluster *= 2;
+    const int64_t n_dkdv = n_units * p.cluster, n_dq = ((int64_t)q_tiles * w.Hq + p.cluster - 1) / p.cluster * p.cluster;
     if (n_dkdv + n_dq > 0x7fffffff) return STREAMBP_E_SHAPE;
-    // cost of the longest CTA of each role in tile pairs (a dK/dV pair takes ~1.25x a dQ pair: four products against three)
-    const int64_t dq_longest = 4 * (int64_t)(w.window / TILE + 2 + (w.sinks + TILE - 1) / TILE);
-    const int64_t dkdv_longest = 5 * (int64_t)(w.Hq / w.Hkv) * (p.work.len < p.work.q_tiles ? p.work.len : p.work.q_tiles);
-    const int n_dq_first = dq_longest > dkdv_longest ? (int)n_dq : 0;
-    SBP_LAUNCH(attn_window_bwd_kernel<DH>, (unsigned)(n_dkdv + n_dq), BWD_THREADS, Bwd<DH>::kSmem, st, m.q, m.k, m.v, m.d, p,
-               (int)n_dkdv, n_dq_first);
-    return STREAMBP_OK;
+    p.n_dkdv = (int)n_dkdv;
+    p.n_dq = (int)n_dq;
+    p.n_dq_first = dq_longest > 5 * G * walk / p.cluster ? (int)n_dq : 0;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)(n_dkdv + n_dq));
+    cfg.blockDim = dim3(W::kThreads);
+    cfg.dynamicSmemBytes = W::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    memset(attr, 0, sizeof(attr));
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)p.cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.cluster > 1 ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, attn_window_bwd_kernel<DH>, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7], m[8], m[9], p);
+    call_state().launches++;
+    return cuda_ok(e) && cuda_ok(cudaGetLastError()) ? STREAMBP_OK : STREAMBP_E_CUDA;
 }
 
 }  // namespace

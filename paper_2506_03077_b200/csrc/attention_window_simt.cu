@@ -104,10 +104,20 @@ __global__ void __launch_bounds__(256)
     }
 }
 
+// Rows of dk and dv that no query of the chunk sees have no owner among the key tiles: their gradients are zero (`count`
+// 16-byte pieces of each; sink rows among them are written later in the stream).
+__device__ __forceinline__ void clear_unseen(void *dk, void *dv, int64_t count) {
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < count; i += (int64_t)gridDim.x * blockDim.x) {
+        static_cast<uint4 *>(dk)[i] = make_uint4(0u, 0u, 0u, 0u);
+        static_cast<uint4 *>(dv)[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
 template <typename T>
-__global__ void __launch_bounds__(256) window_delta_any_kernel(const T *o, const T *dout, int n, int Hq, int dh, float *delta, WsHeader *hdr) {
+__global__ void __launch_bounds__(256) window_delta_any_kernel(const T *o, const T *dout, int n, int Hq, int dh, float *delta, WsHeader *hdr,
+                                                               void *dk, void *dv, int64_t unseen16) {
     pdl_enter();
     if (blockIdx.x == 0 && threadIdx.x == 0) clear_status(hdr);
+    clear_unseen(dk, dv, unseen16);
     const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
     const int lane = threadIdx.x & 31;
     if (r >= (int64_t)n * Hq) return;
@@ -311,8 +321,10 @@ int bwd(const T *q, const T *k, const T *v, const T *o, const T *dout, const flo
     if (!configured.get([&] { return set_smem(window_dkdv_kernel<T, DH>, smem) && set_smem(window_dq_kernel<T, DH>, smem) ? 1 : 0; }))
         return STREAMBP_E_CUDA;
     const int64_t rows = (int64_t)w.n * w.Hq;
-    SBP_LAUNCH(window_delta_any_kernel<T>, (unsigned)((rows * 32 + 255) / 256), 256, 0, st, o, dout, w.n, w.Hq, DH, delta, hdr);
     const KeyWork<TILE> work = key_work<TILE>(w);
+    const int64_t unseen16 = mode == GRAD_F32_ADD ? 0 : (int64_t)work.lo * TILE * w.Hkv * DH * (mode == GRAD_BF16_SET ? 2 : 4) / 16;
+    SBP_LAUNCH(window_delta_any_kernel<T>, (unsigned)((rows * 32 + 255) / 256), 256, 0, st, o, dout, w.n, w.Hq, DH, delta, hdr, dk, dv,
+               unseen16);
     const int part_rows = w.sinks < TILE ? w.sinks : TILE;
     SBP_LAUNCH((window_dkdv_kernel<T, DH>), dim3(work.items(), w.Hkv), 256, smem, st, q, k, v, dout, lse, (const float *)delta, w,
                work, dk, dv, mode, part, part_rows);

@@ -44,11 +44,12 @@ SBP_HD bool sees(const WindowShape &w, int kt, int first, int last) {
     return kt <= last / T && (kt >= (from > 0 ? from / T : 0) || kt * T < w.sinks);
 }
 
-// The work of the key-tile owners (dK, dV).  Tiles below `lo` hold sinks only, or nothing that a query of the chunk sees.
+// The work of the key-tile owners (dK, dV): key tiles of TK keys against query tiles of TQ rows.  Tiles below `lo` hold
+// sinks only, or nothing that a query of the chunk sees.
 //   sink tiles 0 .. st - 1 : every later query adds to them; their query tiles are cut into `segs` segments of `len`
 //                            tiles, one owner each, whose sums are joined afterwards in the order of the segments
 //   window tiles wt0 .. kv_tiles - 1 : one owner each, over the query tiles the window reaches
-template <int T> struct KeyWork {
+template <int TK, int TQ = TK> struct KeyWork {
     int kv_tiles, q_tiles, lo, st, segs, len, wt0;
     SBP_HD int items() const { return st * segs + (kv_tiles - wt0); }
     // item -> key tile, query tiles [begin, end), segment (-1: the item writes its result itself)
@@ -64,34 +65,33 @@ template <int T> struct KeyWork {
             kt = wt0 + i - st * segs;
             seg = -1;
             begin = first(w, kt);
-            // the last query that sees key kt * T + T - 1 through the window
-            const long long last = (long long)kt * T + T - 1 + w.window - 1 - w.q0;
-            end = last < 0 ? 0 : (last / T + 1 < q_tiles ? (int)(last / T) + 1 : q_tiles);
+            // the last query that sees the tile's last key through the window
+            const long long last = (long long)kt * TK + TK - 1 + w.window - 1 - w.q0;
+            end = last < 0 ? 0 : (last / TQ + 1 < q_tiles ? (int)(last / TQ) + 1 : q_tiles);
         }
         if (end < begin) end = begin;
     }
     // first query tile that holds a row at or behind the tile's first key
     SBP_HD static int first(const WindowShape &w, int kt) {
-        const long long k0 = (long long)kt * T;
-        return k0 > w.q0 ? (int)((k0 - w.q0) / T) : 0;
+        const long long k0 = (long long)kt * TK;
+        return k0 > w.q0 ? (int)((k0 - w.q0) / TQ) : 0;
     }
 };
-template <int T>
-inline KeyWork<T> key_work(const WindowShape &w) {
-    KeyWork<T> k;
+template <int TK, int TQ = TK>
+inline KeyWork<TK, TQ> key_work(const WindowShape &w) {
+    KeyWork<TK, TQ> k;
     const int kv = w.q0 + w.n;
-    k.kv_tiles = (kv + T - 1) / T;
-    k.q_tiles = (w.n + T - 1) / T;
+    k.kv_tiles = (kv + TK - 1) / TK;
+    k.q_tiles = (w.n + TQ - 1) / TQ;
     const int from = w.q0 - w.window + 1;
-    k.lo = from > 0 ? from / T : 0;
-    const int sink_tiles = (w.sinks + T - 1) / T;
+    k.lo = from > 0 ? from / TK : 0;
+    const int sink_tiles = (w.sinks + TK - 1) / TK;
     k.st = sink_tiles < k.kv_tiles ? sink_tiles : k.kv_tiles;
     k.wt0 = k.st > k.lo ? k.st : k.lo;
     // a segment is as long as a window tile's walk, and the first one covers every query that sees a key of the tile
     // through the window: in the later ones only the sinks have anything to add
-    k.len = (w.window + 2 * T - 2) / T + 1;
-    const int len0 = 8;
-    if (k.len < len0) k.len = len0;
+    k.len = (w.window + TK + 2 * TQ - 2) / TQ;
+    if (k.len < 8) k.len = 8;
     k.segs = k.st > 0 ? (k.q_tiles + k.len - 1) / k.len : 1;
     // no more owners of sink tiles than four for each of 148 SMs: that many keep the GPU busy, and they bound the workspace
     // (many sinks need no segments at all)
@@ -103,6 +103,9 @@ inline KeyWork<T> key_work(const WindowShape &w) {
     if (k.segs < 1) k.segs = 1;
     return k;
 }
+// query rows to a tile of the tensor-core backward's key-tile owners, by head_dim
+constexpr int kBwdRows64 = 64, kBwdRows128 = 128;
+
 // rows of a sink tile whose sums go through the workspace
 template <int T>
 SBP_HD int sink_rows(const WindowShape &w, int kt) {

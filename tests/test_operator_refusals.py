@@ -150,26 +150,26 @@ def test_window_workspace(lib):
     assert all(size(32768, 0, 32, 8, 128, 128, s) < (200 << 20) for s in (0, 1, 4, 128, 1000, 16000, 32767, 1 << 20))
 
 
-def _key_work(n, q0, Hkv, window, sinks, T):
+def _key_work(n, q0, Hkv, window, sinks, TK, TQ):
     """The key tiles' work as window.cuh lays it out, restated: (key tile, query tiles, segment) of every item."""
-    kv, qt = q0 + n, -(-n // T)
-    lo = max(0, q0 - window + 1) // T
-    st = min(-(-sinks // T), -(-kv // T))
-    length = max(8, (window + 2 * T - 2) // T + 1)
+    kv, qt = q0 + n, -(-n // TQ)
+    lo = max(0, q0 - window + 1) // TK
+    st = min(-(-sinks // TK), -(-kv // TK))
+    length = max(8, (window + TK + 2 * TQ - 2) // TQ)
     segs = -(-qt // length) if st else 1
     most = 592 // min(592, st * Hkv) if st else 1
     if segs > most:
         length = -(-qt // most)
         segs = -(-qt // length)
-    first = lambda kt: (kt * T - q0) // T if kt * T > q0 else 0
+    first = lambda kt: (kt * TK - q0) // TQ if kt * TK > q0 else 0
     items = []
     for kt in range(st):
         for s in range(segs):
             b = first(kt) + s * length
             items.append((kt, range(b, qt if segs == 1 else min(qt, b + length)), s if segs > 1 else -1))
-    for kt in range(max(st, lo), -(-kv // T)):
-        last = kt * T + T - 1 + window - 1 - q0
-        items.append((kt, range(first(kt), min(qt, last // T + 1) if last >= 0 else 0), -1))
+    for kt in range(max(st, lo), -(-kv // TK)):
+        last = kt * TK + TK - 1 + window - 1 - q0
+        items.append((kt, range(first(kt), min(qt, last // TQ + 1) if last >= 0 else 0), -1))
     return items
 
 
@@ -177,9 +177,9 @@ def test_key_work_covers_every_visible_pair_once():
     """Every visible (query, key) pair lies in exactly one item; behind the first segment of a sink tile only sinks are seen."""
     import random
     rng = random.Random(0)
-    for _ in range(300):
-        T = rng.choice((4, 8))
-        n, q0 = rng.randrange(1, 90), rng.choice((0, rng.randrange(0, 80)))
+    for _ in range(400):
+        TK, TQ = rng.choice(((4, 4), (8, 8), (8, 4), (16, 4)))
+        n, q0 = rng.randrange(1, 120), rng.choice((0, rng.randrange(0, 80)))
         window, sinks = rng.randrange(1, 60), rng.choice((0, 1, 3, 5, 17, 40))
         kv = q0 + n
         window = min(window, kv)
@@ -187,11 +187,11 @@ def test_key_work_covers_every_visible_pair_once():
         if sinks == kv or window == kv:
             window, sinks = kv, 0
         seen = {}
-        for kt, tiles, seg in _key_work(n, q0, rng.choice((1, 8, 200)), window, sinks, T):
+        for kt, tiles, seg in _key_work(n, q0, rng.choice((1, 8, 200)), window, sinks, TK, TQ):
             for qt in tiles:
-                assert 0 <= qt < -(-n // T)
-                for t in range(q0 + qt * T, min(q0 + n, q0 + qt * T + T)):
-                    for j in range(kt * T, min(kv, kt * T + T)):
+                assert 0 <= qt < -(-n // TQ)
+                for t in range(q0 + qt * TQ, min(q0 + n, q0 + qt * TQ + TQ)):
+                    for j in range(kt * TK, min(kv, kt * TK + TK)):
                         if j <= t and (t - j < window or j < sinks):
                             seen[(t, j)] = seen.get((t, j), 0) + 1
                             assert seg <= 0 or j < sinks
