@@ -65,6 +65,48 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t *>(&h);
 }
+// Two fp32 values in one 64-bit register: sm_100 multiplies and adds them with one instruction.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split(f32x2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// P of 32 scores of a row: 2^(s * scale + shift), shift of each pair from `shift(e)`.  HIDDEN: pairs that are not seen get 0.
+// (Every fourth to every second pair through a polynomial on the fma units instead of ex2 changed no time by more than the
+// noise, here and in the forward: the kernels are not bound by the special-function unit.)
+template <bool HIDDEN, typename F>
+__device__ __forceinline__ void exponentials(const uint32_t (&rs)[32], float scale, uint32_t see, F shift, f32x2 (&pv)[16]) {
+    const f32x2 sc = pair(scale, scale);
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+        const f32x2 x = fma2(pair(__uint_as_float(rs[2 * e]), __uint_as_float(rs[2 * e + 1])), sc, shift(e));
+        float a, b;
+        split(x, a, b);
+        if (HIDDEN) {
+            if (!(see >> (2 * e) & 1u)) a = -INFINITY;
+            if (!(see >> (2 * e + 1) & 1u)) b = -INFINITY;
+        }
+        pv[e] = pair(fast_exp2(a), fast_exp2(b));
+    }
+}
+__device__ __forceinline__ uint32_t pack_pair(f32x2 v) {
+    float a, b;
+    split(v, a, b);
+    return pack_bf16(a, b);
+}
+
 // bits [0, n) of 32, n clamped
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
 // Which of the keys k0 + base .. + 31 the query row sees, as bits.
@@ -449,7 +491,7 @@ template <int DH> struct Bwd {
     static constexpr int kTiles = 2 * kOut + 5 * kIn;
     static constexpr int kSmem = kTiles + 4 * IT * 4 /* lse, delta x 2 stages */ + 256 + kSlack;
     static constexpr int kSums = 2 * DH * TILE * 4;                  // fp32 sums of a CTA that hands them to another
-    static_assert(kBlocks * (kSmem + 1024) <= 233472 && kSums <= kTiles, "backward roles exceed the shared memory of an SM");
+    static_assert(kBlocks * (kSmem + 1024) <= 233472 && kSums <= kTiles && 4 * kGroups * 8192 <= kTiles, "backward roles exceed the shared memory of an SM");
     typedef KeyWork<TILE, IT> Work;
     __host__ __device__ static constexpr uint32_t step(int kk) { return (uint32_t)((kk >> 2) * (kInSub >> 4) + (kk & 3) * 2); }
 };
@@ -494,17 +536,45 @@ __device__ __forceinline__ void put32(void *dst, long long at, const uint32_t (&
     }
 }
 
+// The same for a warp's 32 rows through a block of shared memory and a TMA store (or add), which clips the rows behind the
+// last.  Written by the lanes themselves, 16 bytes of 32 rows at a time, the epilogue of a CTA took 4000 - 8000 cycles.
+__device__ __forceinline__ void put_block(const CUtensorMap *map, uint32_t at, const uint32_t (&r)[32], int lane, int col, int row0, int mode) {
+    if (mode == GRAD_BF16_SET) {                            // rows of 64 bytes, 64-byte swizzle
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            uint32_t wd[4];
+#pragma unroll
+            for (int t = 0; t < 4; t++) wd[t] = pack_bf16(__uint_as_float(r[8 * j + 2 * t]), __uint_as_float(r[8 * j + 2 * t + 1]));
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)), "r"(wd[0]),
+                         "r"(wd[1]), "r"(wd[2]), "r"(wd[3]) : "memory");
+        }
+    } else {                                                // rows of 128 bytes, 128-byte swizzle
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(r[4 * j]),
+                         "r"(r[4 * j + 1]), "r"(r[4 * j + 2]), "r"(r[4 * j + 3]) : "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        if (mode == GRAD_F32_ADD) tma_reduce_add_2d(map, at, col, row0);
+        else tma_store_2d(map, at, col, row0);
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
+
 template <int DH>
 __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
-                                          const CUtensorMap &map_do, const BwdParams<DH> &p, uint8_t *smem_raw, int item, int g, int rank) {
+                                          const CUtensorMap &map_do, const CUtensorMap &map_dk, const CUtensorMap &map_dv,
+                                          const BwdParams<DH> &p, uint8_t *smem_raw, int item, int g, int rank) {
     typedef Bwd<DH> W;
     constexpr int T = W::kIn, QS = W::kQStages, IT = W::IT;
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
     const uint32_t sK = base, sV = sK + W::kOut, sQ = sV + W::kOut, sdO = sQ + QS * T;
     uint8_t *tail = smem_raw + (base - raw) + W::kTiles;
-    float *s_lse = reinterpret_cast<float *>(tail);           // [2][IT], pre-multiplied by log2(e)
-    float *s_delta = s_lse + 2 * IT;                          // [2][IT], pre-multiplied by the score scale
+    float *s_lse = reinterpret_cast<float *>(tail);           // [2][IT], -lse * log2(e)
+    float *s_delta = s_lse + 2 * IT;                          // [2][IT], -delta * scale
     uint8_t *aux = tail + 4 * IT * 4;
     const uint32_t bars = smem_u32(aux);
     const uint32_t kv_full = bars, q_full = bars + 8, q_empty = bars + 32, do_full = bars + 56, do_empty = bars + 72,
@@ -587,8 +657,8 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
 #pragma unroll
             for (int e = 0; e < IT / 32; e++) {
                 const int col = lane * (IT / 32) + e, r = qt0 + col;
-                s_lse[sd * IT + col] = r < p.w.n ? p.lse[(long long)h * p.w.n + r] * kLog2e : 0.f;
-                s_delta[sd * IT + col] = r < p.w.n ? p.delta[(long long)h * p.w.n + r] * p.scale : 0.f;
+                s_lse[sd * IT + col] = r < p.w.n ? -p.lse[(long long)h * p.w.n + r] * kLog2e : 0.f;
+                s_delta[sd * IT + col] = r < p.w.n ? -p.delta[(long long)h * p.w.n + r] * p.scale : 0.f;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(do_full + 8 * sd);   // publishes the rows; the phase completes when dO has landed too
@@ -697,24 +767,17 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
                 if (++qt == qt_end) qt = qt_begin;
                 continue;
             }
-            const float *lse2 = s_lse + sd * IT + col_base, *dl = s_delta + sd * IT + col_base;
+            const f32x2 *lse2 = reinterpret_cast<const f32x2 *>(s_lse + sd * IT + col_base);
+            const f32x2 *dl = reinterpret_cast<const f32x2 *>(s_delta + sd * IT + col_base);
             // phase 1: P^T = exp2(S^T * scale - lse), all the dV product needs
-            float pv[32];
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-                const float4 l4 = *reinterpret_cast<const float4 *>(lse2 + e);
-                const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-                for (int t = 0; t < 4; t++) {
-                    float x = fmaf(__uint_as_float(rs[e + t]), p.scale_log2, -lv[t]);
-                    if (!(see >> (e + t) & 1u)) x = -INFINITY;
-                    pv[e + t] = fast_exp2(x);
-                }
-            }
+            f32x2 pv[16];
+            auto shift = [&](int e) { return lse2[e]; };
+            if (see == 0xffffffffu) exponentials<false>(rs, p.scale_log2, see, shift, pv);
+            else exponentials<true>(rs, p.scale_log2, see, shift, pv);
             // dP^T of this iteration was queued a whole iteration ago; its columns become P^T and dS^T
             uint32_t pp[16];
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) pp[e / 2] = pack_bf16(pv[e], pv[e + 1]);
+            for (int e = 0; e < 16; e++) pp[e] = pack_pair(pv[e]);
             if (!mbar_wait(dp_full, it & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
             uint32_t rp[32];
@@ -729,16 +792,10 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             // phase 2: dS^T = P^T * (dP^T * scale - delta * scale)
             {
                 uint32_t ds[16];
+                const f32x2 sc = pair(p.scale, p.scale);
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const float4 d4 = *reinterpret_cast<const float4 *>(dl + e);
-                    const float dv[4] = {d4.x, d4.y, d4.z, d4.w};
-                    float dsv[4];
-#pragma unroll
-                    for (int t = 0; t < 4; t++) dsv[t] = pv[e + t] * fmaf(__uint_as_float(rp[e + t]), p.scale, -dv[t]);
-                    ds[e / 2] = pack_bf16(dsv[0], dsv[1]);
-                    ds[e / 2 + 1] = pack_bf16(dsv[2], dsv[3]);
-                }
+                for (int e = 0; e < 16; e++)
+                    ds[e] = pack_pair(mul2(pv[e], fma2(pair(__uint_as_float(rp[2 * e]), __uint_as_float(rp[2 * e + 1])), sc, dl[e])));
                 tmem_st16(tP_g + 16, ds);
                 tmem_wait_st();
                 tc_fence_before();
@@ -791,12 +848,20 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
         }
     }
     if (rank == 0 && writes && done) {
-        const bool joined = seg >= 0 && row < sink_rows<TILE>(p.w, kt);
-        if (joined) {                                     // this segment's share of a sink key's sums
+        if (seg < 0) {
+            // the tiles are through with their products, and peers' sums are not in this CTA: each warp stages its two blocks
+            const uint32_t at = base + (uint32_t)(warp - 2) * 8192u;
+            const int row0 = k_abs0 + (warp & 3) * 32;
+            if (row0 < p.w.q0 + p.w.n) {
+                put_block(&map_dv, at, rv, lane, g * DH + col_base, row0, p.mode);
+                put_block(&map_dk, at + 4096u, rk, lane, g * DH + col_base, row0, p.mode);
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            }
+        } else if (row < sink_rows<TILE>(p.w, kt)) {       // this segment's share of a sink key's sums
             float *part = p.part + (((long long)item * p.w.Hkv + g) * 2 * p.part_rows + row) * DH + col_base;
             put32(part, 0, rk, GRAD_F32_SET);
             put32(part, (long long)p.part_rows * DH, rv, GRAD_F32_SET);
-        } else if (seg <= 0 && k_abs < p.w.q0 + p.w.n) {  // segments behind the first have nothing for these rows
+        } else if (seg == 0 && k_abs < p.w.q0 + p.w.n) {   // segments behind the first have nothing for these rows
             const long long at = ((long long)k_abs * p.w.Hkv + g) * DH + col_base;
             put32(p.dv, at, rv, p.mode);
             put32(p.dk, at, rk, p.mode);
@@ -817,7 +882,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
 template <int DH>
 __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
                                         const CUtensorMap &map_do, const CUtensorMap &map_ke, const CUtensorMap &map_ve,
-                                        const BwdParams<DH> &p, uint8_t *smem_raw, int block_x, int h) {
+                                        const CUtensorMap &map_dq, const BwdParams<DH> &p, uint8_t *smem_raw, int block_x, int h) {
     typedef Bwd<DH> W;
     constexpr int T = W::kIn, KS = W::kKStages, IT = W::IT;
     const uint32_t raw = smem_u32(smem_raw);
@@ -973,19 +1038,16 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
                 continue;
             }
             // phase 1: P from S; the S columns are handed back to the tensor pipe right after the load
-            float pv[32];
+            f32x2 pv[16];
             {
                 uint32_t rs[32];
                 tmem_ld32(tS_g, rs);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(s_free);
-#pragma unroll
-                for (int e = 0; e < 32; e++) {
-                    float x = fmaf(__uint_as_float(rs[e]), p.scale_log2, neg_lse2);
-                    if (!(see >> e & 1u)) x = -INFINITY;
-                    pv[e] = fast_exp2(x);
-                }
+                auto shift = [&](int) { return pair(neg_lse2, neg_lse2); };
+                if (see == 0xffffffffu) exponentials<false>(rs, p.scale_log2, see, shift, pv);
+                else exponentials<true>(rs, p.scale_log2, see, shift, pv);
             }
             // phase 2: dS = P * (dP * scale - delta * scale), packed in place
             if (!mbar_wait(dp_full, j & 1, abort_flag)) { alive = false; break; }
@@ -993,12 +1055,10 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
             {
                 uint32_t rp[32], ds[16];
                 tmem_ld32(tP_g, rp);
+                const f32x2 sc = pair(p.scale, p.scale), dl = pair(neg_delta_s, neg_delta_s);
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    const float d0 = pv[e] * fmaf(__uint_as_float(rp[e]), p.scale, neg_delta_s);
-                    const float d1 = pv[e + 1] * fmaf(__uint_as_float(rp[e + 1]), p.scale, neg_delta_s);
-                    ds[e / 2] = pack_bf16(d0, d1);
-                }
+                for (int e = 0; e < 16; e++)
+                    ds[e] = pack_pair(mul2(pv[e], fma2(pair(__uint_as_float(rp[2 * e]), __uint_as_float(rp[2 * e + 1])), sc, dl)));
                 tmem_st16(tP_g, ds);       // front of the group's own fp32 columns
                 tmem_wait_st();
                 tc_fence_before();
@@ -1010,8 +1070,12 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
             tc_fence_after();
             uint32_t r[32];
             tmem_ld32(tDQ + lane_base + key_base, r);
-            if (qr < p.w.n)
-                put32(p.dq, ((long long)qr * p.w.Hq + h) * DH + key_base, r, p.mode == GRAD_BF16_SET ? GRAD_BF16_SET : GRAD_F32_SET);
+            const int row0 = qt0 + quarter * 32;
+            if (row0 < p.w.n) {                               // the tiles are through with their products
+                put_block(&map_dq, base + (uint32_t)(warp - 2) * 4096u, r, lane, h * DH + key_base, row0,
+                          p.mode == GRAD_BF16_SET ? GRAD_BF16_SET : GRAD_F32_SET);
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            }
         }
     }
 
@@ -1032,7 +1096,8 @@ __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
                            const __grid_constant__ CUtensorMap map_qi, const __grid_constant__ CUtensorMap map_ki,
                            const __grid_constant__ CUtensorMap map_vi, const __grid_constant__ CUtensorMap map_doi,
                            const __grid_constant__ CUtensorMap map_ke, const __grid_constant__ CUtensorMap map_ve,
-                           const __grid_constant__ BwdParams<DH> p) {
+                           const __grid_constant__ CUtensorMap map_dq, const __grid_constant__ CUtensorMap map_dk,
+                           const __grid_constant__ CUtensorMap map_dv, const __grid_constant__ BwdParams<DH> p) {
     pdl_enter();
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // dispatch order: n_dq_first dQ CTAs (all of them or none), then the dK/dV CTAs, then the rest
@@ -1040,11 +1105,11 @@ __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
     const bool dq_role = b < p.n_dq_first || b >= p.n_dq_first + p.n_dkdv;
     if (!dq_role) {
         const int c = b - p.n_dq_first, unit = c / p.cluster;
-        dkdv_body<DH>(map_qi, map_k, map_v, map_doi, p, smem_raw, unit / p.w.Hkv, unit % p.w.Hkv, c % p.cluster);
+        dkdv_body<DH>(map_qi, map_k, map_v, map_doi, map_dk, map_dv, p, smem_raw, unit / p.w.Hkv, unit % p.w.Hkv, c % p.cluster);
     } else {
         const int c = b < p.n_dq_first ? b : b - p.n_dkdv, tiles = (p.w.n + TILE - 1) / TILE;
         if (c < tiles * p.w.Hq)                           // the role is padded to whole clusters
-            dq_body<DH>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, p, smem_raw, tiles - 1 - c % tiles, c / tiles);
+            dq_body<DH>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, map_dq, p, smem_raw, tiles - 1 - c % tiles, c / tiles);
     }
 }
 
@@ -1141,12 +1206,18 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     edge_of<IT>(w, 32, p.edge, p.edge_keys);
     const int64_t kv = (int64_t)w.q0 + w.n;
     const uint32_t edge = (uint32_t)p.edge_keys;
-    CUtensorMap m[10];       // resident tiles of q, k, v, dO; inner tiles of the same; edge tiles of k, v
+    CUtensorMap m[13];       // resident tiles of q, k, v, dO; inner tiles of the same; edge tiles of k, v; blocks of dq, dk, dv
     if (!tile_map<DH>(&m[0], q, w.n, w.Hq, TILE) || !tile_map<DH>(&m[1], k, kv, w.Hkv, TILE) || !tile_map<DH>(&m[2], v, kv, w.Hkv, TILE) ||
         !tile_map<DH>(&m[3], dout, w.n, w.Hq, TILE) || !tile_map<DH>(&m[4], q, w.n, w.Hq, IT) || !tile_map<DH>(&m[5], k, kv, w.Hkv, IT) ||
         !tile_map<DH>(&m[6], v, kv, w.Hkv, IT) || !tile_map<DH>(&m[7], dout, w.n, w.Hq, IT) || !tile_map<DH>(&m[8], k, kv, w.Hkv, edge) ||
         !tile_map<DH>(&m[9], v, kv, w.Hkv, edge))
         return STREAMBP_E_CUDA;
+    const bool f32 = mode != GRAD_BF16_SET;
+    const CUtensorMapSwizzle swizzle = f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+    auto block_map = [&](CUtensorMap *x, void *g, int64_t rows, int heads) {
+        return make_tensor_map(x, g, rows, (int64_t)heads * DH, (int64_t)heads * DH, 32, 32, f32, swizzle);
+    };
+    if (!block_map(&m[10], dq, w.n, w.Hq) || !block_map(&m[11], dk, kv, w.Hkv) || !block_map(&m[12], dv, kv, w.Hkv)) return STREAMBP_E_CUDA;
     static PerDevice configured;
     if (!configured.get([] { return opt_in_smem(attn_window_bwd_kernel<DH>, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
     {
@@ -1194,7 +1265,8 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = p.cluster > 1 ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, attn_window_bwd_kernel<DH>, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7], m[8], m[9], p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, attn_window_bwd_kernel<DH>, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7], m[8], m[9], m[10],
+                                             m[11], m[12], p);
     call_state().launches++;
     return cuda_ok(e) && cuda_ok(cudaGetLastError()) ? STREAMBP_OK : STREAMBP_E_CUDA;
 }
