@@ -361,17 +361,13 @@ int window_shape(int64_t n, int64_t q0, int32_t Hq, int32_t Hkv, int32_t dh, int
 }
 // scratch of the windowed backward: delta, then the sums of the sink segments (the larger of the two engines' needs)
 struct WindowScratch { float *delta, *part; };
-template <int TK, int TQ>
-size_t window_part_floats(const WindowShape &w, int dh) {
-    const KeyWork<TK, TQ> k = key_work<TK, TQ>(w);
-    return k.segs > 1 ? (size_t)k.st * k.segs * w.Hkv * 2 * (w.sinks < TK ? w.sinks : TK) * dh : 0;
-}
 size_t window_scratch(const WindowShape &w, int dh, void *base, WindowScratch *out) {
     Arena a(base);
     a.take_bytes(kHeaderBytes);
     out->delta = a.take<float>((size_t)w.Hq * w.n);
-    const size_t x = dh == 64 ? window_part_floats<128, kBwdRows64>(w, dh) : window_part_floats<128, kBwdRows128>(w, dh),
-                 y = window_part_floats<32, 32>(w, dh);
+    const size_t x = dh == 64 ? key_work<128, kBwdRows64>(w, kBwdSlots64).part_floats(w, dh)
+                              : key_work<128, kBwdRows128>(w, kBwdSlots128).part_floats(w, dh),
+                 y = key_work<32>(w, 0).part_floats(w, dh);
     out->part = a.take<float>(x > y ? x : y);
     return a.size();
 }
@@ -779,22 +775,14 @@ int streambp_attention_window_backward(const void *q, const void *k, const void 
     call_state().launches = 0;
     WsHeader *hdr = static_cast<WsHeader *>(workspace);
     const int mode = grad_dtype == STREAMBP_BF16 ? GRAD_BF16_SET : (accumulate ? GRAD_F32_ADD : GRAD_F32_SET);
-    const int tile = tc ? 128 : 32;
-    int rc;
     if (tc)
-        rc = attention_window_bwd_tc((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o, lse, w,
-                                     head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
-    else if (dtype == STREAMBP_BF16)
-        rc = attention_window_bwd_simt<bf16>((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o,
-                                             lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
-    else
-        rc = attention_window_bwd_simt<float>((const float *)q, (const float *)k, (const float *)v, (const float *)o,
-                                              (const float *)d_o, lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
-    SBP_TRY(rc);
-    const int segs = !tc ? key_work<32>(w).segs
-                         : (head_dim == 64 ? key_work<128, kBwdRows64>(w).segs : key_work<128, kBwdRows128>(w).segs);
-    if (segs > 1) return attention_window_join(s.part, tile, segs, w, head_dim, mode, dk, dv, st);
-    return STREAMBP_OK;
+        return attention_window_bwd_tc((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o, lse, w,
+                                       head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
+    if (dtype == STREAMBP_BF16)
+        return attention_window_bwd_simt<bf16>((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o,
+                                               lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
+    return attention_window_bwd_simt<float>((const float *)q, (const float *)k, (const float *)v, (const float *)o,
+                                            (const float *)d_o, lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
 }
 
 int streambp_product_kernel(void) { return gemm_tc_variant(); }

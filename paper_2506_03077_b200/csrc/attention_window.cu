@@ -1,28 +1,34 @@
 // Attention with a sliding window and sink keys on tcgen05 tensor cores (bf16 operands, head_dim 64 or 128): the queries
 // of one chunk against the key tiles their window reaches and the tiles that hold sinks; nothing else is loaded.
 //
-// Forward (attn_window_fwd_kernel): two persistent CTAs per SM, each walking (query tile, head) items.
-//   warp 0      : TMA producer -- query tiles, K and V tiles of 128 keys through rings; runs ahead into the next item
-//   warp 1      : MMA issuer (warp-uniform issue) -- S = Q K^T into tensor memory, O += P V with P read from tensor memory
-//                 (packed over the columns of S: the product that reads P is queued before the one that overwrites S, one
-//                 thread's MMAs run in order); behind an item's last P V comes the next item's first S
-//   warps 2..5  : softmax -- a thread owns a query row: 128 scores in registers, row maximum and sum private; the running
+// Forward (attn_window_fwd_kernel): two persistent CTAs per SM, each walking (query tile of 128, head) items.
+//   warp 0      : TMA producer -- query tiles, K and V tiles of 64 keys through rings; runs ahead into the next item
+//   warp 1      : MMA issuer (warp-uniform issue) -- S = Q K^T into tensor memory two or three tiles ahead, O += P V with P
+//                 read from tensor memory (packed over the columns of its S: the product that reads P is queued before the
+//                 one that overwrites S, one thread's MMAs run in order)
+//   warps 2..5  : softmax -- a thread owns a query row: its scores in registers, row maximum and sum private; the running
 //                 output is rescaled only when a row's maximum grows by more than 2^8 (exact: the final division uses the
 //                 same reference)
-// What two CTAs of one chain each buy: one's latencies (tensor-memory loads, hand-offs, the P V -> next S chain) fall into
-// the other's exponentials, and short windows -- a handful of key tiles between fetching queries and storing outputs -- pay
-// neither launch nor set-up nor first loads per tile.
+// What two CTAs of one chain each buy: one's latencies (tensor-memory loads, hand-offs) fall into the other's exponentials,
+// and short windows -- a handful of key tiles between fetching queries and storing outputs -- pay neither launch nor set-up
+// nor first loads per tile.  Key tiles of 64 rather than 128 waste less at the two ends of a window and leave tensor memory
+// for scores ahead (16384 rows, window 128, heads of 64: 125 -> 107 us; window 1024, heads of 128: 350 -> 305 us).
 // A row may see nothing of the first tiles of its list: its maximum stays -infinity and it adds exact zeros until it sees
 // a key.  Every query sees its own key, so no row ends empty.  Groups of 32 columns that no row of a warp sees are skipped,
 // and the sink tile that the window does not reach is cut to its sinks (16 columns for up to 16 of them).
+// What bounds it: the exponentials and the conversions around them, ~770 of the ~1600 cycles of a CTA's step of 128 x 64
+// scores, and the latencies that two chains do not hide.
 //
 // Backward (attn_window_bwd_kernel): two CTA roles in one grid, both deterministic (no floating-point atomics).
 //   dK/dV: one CTA per (key tile, KV head) loops over the query heads of the group and the query tiles that see the tile;
-//          a sink tile, which every later query sees, is cut into segments of query tiles that are joined in order by
-//          window_join_kernel (fp32 sums in the workspace, only the sinks' rows)
+//          a sink tile, which every later query sees, and all tiles where there are few, are cut into segments of query
+//          tiles whose fp32 sums meet in the workspace and are joined in order by window_join_kernel
 //   dQ   : one CTA per (query tile, head) loops over the key tiles of its span
-// The pipelines of both are those of the causal backward (attention_tc.cu): softmax work split in time (P for dV first,
-// then dS), packed operands in tensor memory, every product a full tile.
+// Softmax work is split in time (P for dV first, then dS), packed operands stay in tensor memory, every product is a full
+// tile; gradients leave through blocks of shared memory and TMA stores or adds, fp32 sums rounded once.
+// What bounds it: one iteration's chain of products and exponentials, ~2900 (dK/dV) and ~2500 cycles (dQ) for 128 x 128
+// scores at heads of 128, of which the products are ~1300.  Heads of 64 run two CTAs with inner tiles of 64 per SM.
+//
 //
 // All mbarrier waits are bounded (sm100.cuh).
 #include <cstring>
@@ -33,7 +39,7 @@
 namespace sbp {
 namespace {
 
-constexpr int TILE = 128;                 // queries per team, keys per tile
+constexpr int TILE = 128;                 // queries to a tile; keys to a tile of the backward
 constexpr int SUB_BYTES = TILE * 64 * 2;  // one [128 rows][64 columns] swizzled sub-tile
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -42,18 +48,12 @@ constexpr float kLn2 = 0.6931471805599453f;
 // step) and MN-major (contraction along the rows, 16 a step).
 __device__ __forceinline__ uint32_t klo(uint32_t tile) { return desc_lo(tile, 16); }
 __host__ __device__ constexpr uint32_t kstep(int kk) { return (uint32_t)((kk >> 2) * (SUB_BYTES >> 4) + (kk & 3) * 2); }
-__device__ __forceinline__ uint32_t mnlo(uint32_t tile) { return desc_lo(tile, SUB_BYTES); }
 __host__ __device__ constexpr uint32_t mnstep(int kk) { return (uint32_t)(kk * 128); }
 
 template <int DH, int SUB = SUB_BYTES>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int head, int row) {
 #pragma unroll
     for (int c = 0; c < DH / 64; c++) tma_load_2d(dst + c * SUB, map, bar, head * DH + c * 64, row);
-}
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
-    return v;
 }
 
 __device__ __forceinline__ float fast_exp2(float x) {
@@ -490,8 +490,7 @@ template <int DH> struct Bwd {
     static constexpr int kSlack = 768;                               // what is left for aligning the tiles to 1024 bytes
     static constexpr int kTiles = 2 * kOut + 5 * kIn;
     static constexpr int kSmem = kTiles + 4 * IT * 4 /* lse, delta x 2 stages */ + 256 + kSlack;
-    static constexpr int kSums = 2 * DH * TILE * 4;                  // fp32 sums of a CTA that hands them to another
-    static_assert(kBlocks * (kSmem + 1024) <= 233472 && kSums <= kTiles && 4 * kGroups * 8192 <= kTiles, "backward roles exceed the shared memory of an SM");
+    static_assert(kBlocks * (kSmem + 1024) <= 233472 && 4 * kGroups * 8192 <= kTiles, "backward roles exceed the shared memory of an SM");
     typedef KeyWork<TILE, IT> Work;
     __host__ __device__ static constexpr uint32_t step(int kk) { return (uint32_t)((kk >> 2) * (kInSub >> 4) + (kk & 3) * 2); }
 };
@@ -502,12 +501,11 @@ struct BwdParams {
     const float *lse;     // [Hq, n]
     const float *delta;   // [Hq, n]
     void *dq, *dk, *dv;   // [n, Hq, DH], [q0 + n, Hkv, DH]
-    float *part;          // [sink item][Hkv][dK, dV][part_rows][DH]
+    float *part;          // sums of segments: [item][Hkv][dK, dV][part_rows][DH]
     int part_rows;
     int mode;             // GradMode of dk, dv (dq: fp32 or bf16, always overwritten)
     int edge, edge_keys;  // dQ role: the sink tile that holds sinks in its first rows only (-1: none), those rows rounded up to 32
-    int cluster;          // CTAs that share the query heads of a dK/dV item
-    int n_dkdv, n_dq, n_dq_first;   // CTAs of the roles (multiples of the cluster); dQ CTAs that are dispatched first
+    int n_dkdv, n_dq_first;         // dK/dV CTAs; dQ CTAs that are dispatched before them (all or none)
     float scale, scale_log2;
 };
 
@@ -566,7 +564,7 @@ __device__ __forceinline__ void put_block(const CUtensorMap *map, uint32_t at, c
 template <int DH>
 __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
                                           const CUtensorMap &map_do, const CUtensorMap &map_dk, const CUtensorMap &map_dv,
-                                          const BwdParams<DH> &p, uint8_t *smem_raw, int item, int g, int rank) {
+                                          const CUtensorMap &map_part, const BwdParams<DH> &p, uint8_t *smem_raw, int item, int g) {
     typedef Bwd<DH> W;
     constexpr int T = W::kIn, QS = W::kQStages, IT = W::IT;
     const uint32_t raw = smem_u32(smem_raw);
@@ -588,9 +586,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
     int kt, qt_begin, qt_end, seg;
     p.work.item(p.w, item, kt, qt_begin, qt_end, seg);
     const int k_abs0 = kt * TILE;
-    // this CTA's query heads of the group, each over the item's query tiles
-    const int h_begin = g * G + G * rank / p.cluster, h_end = g * G + G * (rank + 1) / p.cluster;
-    const int iters = (h_end - h_begin) * (qt_end - qt_begin);
+    const int iters = G * (qt_end - qt_begin);        // the query heads of the group, each over the item's query tiles
 
     if (threadIdx.x == 0) {
         mbar_init(kv_full, 1);
@@ -634,7 +630,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             load_tile<DH>(sV, &map_v, kv_full, g, k_abs0);
         }
         uint32_t sq = 0, qph = 0;
-        int h = h_begin, qt = qt_begin;
+        int h = g * G, qt = qt_begin;
         for (int it = 0; it < iters; it++) {
             const int qt0 = qt * IT;
             const uint32_t sd = it & 1, dph = (it >> 1) & 1;
@@ -807,15 +803,12 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
         done = alive && (iters == 0 || mbar_wait(acc_full, 0, abort_flag));
     }
 
-    // The CTAs of a cluster hold sums over different heads of the group: the others leave theirs in their shared memory (all
-    // copies and products are done there), the first adds them to its own in the order of the ranks.
     __syncwarp();
-    const int wg = (warp - 2) >> 2, row = (warp & 3) * 32 + lane, col_base = wg * 32, k_abs = k_abs0 + row;
-    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const bool writes = warp >= 2 && wg < DH / 32;       // group wg holds head dims 32 * wg ..
-    uint32_t rv[32], rk[32];
-    if (writes && done) {
+    const int wg = (warp - 2) >> 2, row = (warp & 3) * 32 + lane, col_base = wg * 32;
+    if (done && wg < DH / 32) {                          // group wg holds head dims 32 * wg .. of every key
         tc_fence_after();
+        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+        uint32_t rv[32], rk[32];
         if (iters > 0) {
             tmem_ld32(tDV + lane_base + col_base, rv);
             tmem_ld32(tDK + lane_base + col_base, rk);
@@ -823,33 +816,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
 #pragma unroll
             for (int e = 0; e < 32; e++) rv[e] = rk[e] = 0u;
         }
-    }
-    if (p.cluster > 1) {
-        float *sums = reinterpret_cast<float *>(smem_raw + (base - raw));      // [dV, dK][DH][128 rows]
-        __syncthreads();                                  // every role of this CTA is through with the tiles
-        if (rank > 0 && writes && done) {
-#pragma unroll
-            for (int e = 0; e < 32; e++) {
-                sums[(col_base + e) * TILE + row] = __uint_as_float(rv[e]);
-                sums[(DH + col_base + e) * TILE + row] = __uint_as_float(rk[e]);
-            }
-        }
-        cluster_sync_all();
-        if (rank == 0 && writes && done) {
-            const uint32_t own = smem_u32(sums) + (uint32_t)(col_base * TILE + row) * 4u;
-            for (int r = 1; r < p.cluster; r++) {
-                const uint32_t from = map_to_cta(own, (uint32_t)r);
-#pragma unroll
-                for (int e = 0; e < 32; e++) {
-                    rv[e] = __float_as_uint(__uint_as_float(rv[e]) + ld_cluster_f32(from + (uint32_t)e * TILE * 4u));
-                    rk[e] = __float_as_uint(__uint_as_float(rk[e]) + ld_cluster_f32(from + (uint32_t)(DH + e) * TILE * 4u));
-                }
-            }
-        }
-    }
-    if (rank == 0 && writes && done) {
-        if (seg < 0) {
-            // the tiles are through with their products, and peers' sums are not in this CTA: each warp stages its two blocks
+        if (seg < 0) {                                    // the tiles are through with their products: room for two blocks a warp
             const uint32_t at = base + (uint32_t)(warp - 2) * 8192u;
             const int row0 = k_abs0 + (warp & 3) * 32;
             if (row0 < p.w.q0 + p.w.n) {
@@ -857,12 +824,18 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
                 put_block(&map_dk, at + 4096u, rk, lane, g * DH + col_base, row0, p.mode);
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             }
-        } else if (row < sink_rows<TILE>(p.w, kt)) {       // this segment's share of a sink key's sums
+        } else if (p.work.full()) {                       // this segment's share of the sums, all rows of the tile
+            const uint32_t at = base + (uint32_t)(warp - 2) * 8192u;
+            const int row0 = ((item * p.w.Hkv + g) * 2) * TILE + (warp & 3) * 32;
+            put_block(&map_part, at, rk, lane, col_base, row0, GRAD_F32_SET);
+            put_block(&map_part, at + 4096u, rv, lane, col_base, row0 + TILE, GRAD_F32_SET);
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        } else if (row < p.work.joined_rows(p.w, kt)) {   // the same of a sink tile's sinks
             float *part = p.part + (((long long)item * p.w.Hkv + g) * 2 * p.part_rows + row) * DH + col_base;
             put32(part, 0, rk, GRAD_F32_SET);
             put32(part, (long long)p.part_rows * DH, rv, GRAD_F32_SET);
-        } else if (seg == 0 && k_abs < p.w.q0 + p.w.n) {   // segments behind the first have nothing for these rows
-            const long long at = ((long long)k_abs * p.w.Hkv + g) * DH + col_base;
+        } else if (seg == 0 && k_abs0 + row < p.w.q0 + p.w.n) {   // segments behind the first have nothing for these rows
+            const long long at = ((long long)(k_abs0 + row) * p.w.Hkv + g) * DH + col_base;
             put32(p.dv, at, rv, p.mode);
             put32(p.dk, at, rk, p.mode);
         }
@@ -872,7 +845,6 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
     leave(abort_flag);
     tc_fence_before();
     __syncthreads();
-    if (p.cluster > 1) cluster_sync_all();                // no CTA leaves while another may read its sums
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, W::kCols);
@@ -1097,19 +1069,19 @@ __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
                            const __grid_constant__ CUtensorMap map_vi, const __grid_constant__ CUtensorMap map_doi,
                            const __grid_constant__ CUtensorMap map_ke, const __grid_constant__ CUtensorMap map_ve,
                            const __grid_constant__ CUtensorMap map_dq, const __grid_constant__ CUtensorMap map_dk,
-                           const __grid_constant__ CUtensorMap map_dv, const __grid_constant__ BwdParams<DH> p) {
+                           const __grid_constant__ CUtensorMap map_dv, const __grid_constant__ CUtensorMap map_part,
+                           const __grid_constant__ BwdParams<DH> p) {
     pdl_enter();
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // dispatch order: n_dq_first dQ CTAs (all of them or none), then the dK/dV CTAs, then the rest
     const int b = (int)blockIdx.x;
     const bool dq_role = b < p.n_dq_first || b >= p.n_dq_first + p.n_dkdv;
     if (!dq_role) {
-        const int c = b - p.n_dq_first, unit = c / p.cluster;
-        dkdv_body<DH>(map_qi, map_k, map_v, map_doi, map_dk, map_dv, p, smem_raw, unit / p.w.Hkv, unit % p.w.Hkv, c % p.cluster);
+        const int c = b - p.n_dq_first;
+        dkdv_body<DH>(map_qi, map_k, map_v, map_doi, map_dk, map_dv, map_part, p, smem_raw, c / p.w.Hkv, c % p.w.Hkv);
     } else {
         const int c = b < p.n_dq_first ? b : b - p.n_dkdv, tiles = (p.w.n + TILE - 1) / TILE;
-        if (c < tiles * p.w.Hq)                           // the role is padded to whole clusters
-            dq_body<DH>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, map_dq, p, smem_raw, tiles - 1 - c % tiles, c / tiles);
+        dq_body<DH>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, map_dq, p, smem_raw, tiles - 1 - c % tiles, c / tiles);
     }
 }
 
@@ -1143,12 +1115,6 @@ __global__ void __launch_bounds__(256) window_delta_kernel(const bf16 *o, const 
     }
 }
 
-#ifndef CMAX
-#define CMAX 4
-#endif
-#ifndef CNUM
-#define CNUM 4
-#endif
 template <typename K>
 bool opt_in_smem(K kernel, int bytes) {
     return cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
@@ -1202,11 +1168,11 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     BwdParams<DH> p;
     memset(&p, 0, sizeof(p));
     p.w = w;
-    p.work = key_work<TILE, IT>(w);
+    p.work = key_work<TILE, IT>(w, DH == 64 ? kBwdSlots64 : kBwdSlots128);
     edge_of<IT>(w, 32, p.edge, p.edge_keys);
     const int64_t kv = (int64_t)w.q0 + w.n;
     const uint32_t edge = (uint32_t)p.edge_keys;
-    CUtensorMap m[13];       // resident tiles of q, k, v, dO; inner tiles of the same; edge tiles of k, v; blocks of dq, dk, dv
+    CUtensorMap m[14];       // resident tiles of q, k, v, dO; inner tiles of the same; edge tiles of k, v; blocks of dq, dk, dv, part
     if (!tile_map<DH>(&m[0], q, w.n, w.Hq, TILE) || !tile_map<DH>(&m[1], k, kv, w.Hkv, TILE) || !tile_map<DH>(&m[2], v, kv, w.Hkv, TILE) ||
         !tile_map<DH>(&m[3], dout, w.n, w.Hq, TILE) || !tile_map<DH>(&m[4], q, w.n, w.Hq, IT) || !tile_map<DH>(&m[5], k, kv, w.Hkv, IT) ||
         !tile_map<DH>(&m[6], v, kv, w.Hkv, IT) || !tile_map<DH>(&m[7], dout, w.n, w.Hq, IT) || !tile_map<DH>(&m[8], k, kv, w.Hkv, edge) ||
@@ -1218,6 +1184,8 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
         return make_tensor_map(x, g, rows, (int64_t)heads * DH, (int64_t)heads * DH, 32, 32, f32, swizzle);
     };
     if (!block_map(&m[10], dq, w.n, w.Hq) || !block_map(&m[11], dk, kv, w.Hkv) || !block_map(&m[12], dv, kv, w.Hkv)) return STREAMBP_E_CUDA;
+    m[13] = m[12];
+    if (p.work.full() && !make_tensor_map(&m[13], part, (int64_t)p.work.items() * w.Hkv * 2 * TILE, DH, DH, 32, 32, true)) return STREAMBP_E_CUDA;
     static PerDevice configured;
     if (!configured.get([] { return opt_in_smem(attn_window_bwd_kernel<DH>, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
     {
@@ -1231,44 +1199,24 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     p.lse = lse; p.delta = delta;
     p.dq = dq; p.dk = dk; p.dv = dv;
     p.part = part;
-    p.part_rows = w.sinks < TILE ? w.sinks : TILE;
+    p.part_rows = p.work.slot_rows(w);
     p.mode = mode;
     p.scale = scale;
     p.scale_log2 = scale * kLog2e;
-    // Costs in units of a quarter of a dQ inner tile (a dK/dV one takes ~1.25x: four products against three).
-    const int G = w.Hq / w.Hkv, q_tiles = (w.n + TILE - 1) / TILE;
-    const int64_t span = w.window / IT + 2 + (w.sinks + IT - 1) / IT, most_keys = (kv + IT - 1) / IT;
-    const int64_t dq_longest = 4 * (span < most_keys ? span : most_keys);
-    const int64_t walk = p.work.len < p.work.q_tiles ? p.work.len : p.work.q_tiles;
-    const int64_t n_units = (int64_t)p.work.items() * w.Hkv, slots = (int64_t)W::kBlocks * sm_count();
-    const int64_t total = n_units * 5 * G * walk + (int64_t)q_tiles * w.Hq * dq_longest;
-    // A dK/dV item whose walk is a good part of the whole launch's time on a slot is shared by a cluster of two or four CTAs
-    p.cluster = 1;
-    while (p.cluster < CMAX && 2 * p.cluster <= G && 5 * G * walk * slots * CNUM > total * p.cluster * 4) p.cluster *= 2;
-    const int64_t n_dkdv = n_units * p.cluster, n_dq = ((int64_t)q_tiles * w.Hq + p.cluster - 1) / p.cluster * p.cluster;
+    // The role with the longer walks is dispatched first (a dK/dV tile takes ~1.25x a dQ tile: four products against three)
+    const int q_tiles = (w.n + TILE - 1) / TILE;
+    const int64_t span = ((w.window < kv ? w.window : kv) + IT - 1) / IT + 1 + (w.sinks + IT - 1) / IT;
+    const int64_t walk = p.work.wlen < p.work.q_tiles ? p.work.wlen : p.work.q_tiles;
+    const int64_t n_dkdv = (int64_t)p.work.items() * w.Hkv, n_dq = (int64_t)q_tiles * w.Hq;
     if (n_dkdv + n_dq > 0x7fffffff) return STREAMBP_E_SHAPE;
     p.n_dkdv = (int)n_dkdv;
-    p.n_dq = (int)n_dq;
-    p.n_dq_first = dq_longest > 5 * G * walk / p.cluster ? (int)n_dq : 0;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3((unsigned)(n_dkdv + n_dq));
-    cfg.blockDim = dim3(W::kThreads);
-    cfg.dynamicSmemBytes = W::kSmem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    memset(attr, 0, sizeof(attr));
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)p.cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = p.cluster > 1 ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, attn_window_bwd_kernel<DH>, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7], m[8], m[9], m[10],
-                                             m[11], m[12], p);
-    call_state().launches++;
-    return cuda_ok(e) && cuda_ok(cudaGetLastError()) ? STREAMBP_OK : STREAMBP_E_CUDA;
+    p.n_dq_first = 4 * span > 5 * (w.Hq / w.Hkv) * walk ? (int)n_dq : 0;
+    SBP_LAUNCH(attn_window_bwd_kernel<DH>, (unsigned)(n_dkdv + n_dq), W::kThreads, W::kSmem, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6],
+               m[7], m[8], m[9], m[10], m[11], m[12], m[13], p);
+    const auto &k_ = p.work;
+    if (k_.segs > 1 || k_.wsegs > 1)
+        return attention_window_join(part, TILE, k_.st, k_.segs, k_.wt0, k_.wsegs, p.part_rows, w, DH, mode, dk, dv, st);
+    return STREAMBP_OK;
 }
 
 }  // namespace

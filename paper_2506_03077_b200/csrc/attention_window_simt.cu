@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(256)
             }
         }
     }
-    const bool joined = seg >= 0 && kr < sink_rows<TILE>(w, kt);
+    const bool joined = seg >= 0 && kr < work.joined_rows(w, kt);
 #pragma unroll
     for (int e = 0; e < NE; e++) {
         if (joined) {
@@ -283,18 +283,26 @@ __global__ void __launch_bounds__(256)
             put4(dq, ((int64_t)(r0 + qr) * w.Hq + h) * DH + e * 32 + sub * 4, aq[e], mode == GRAD_BF16_SET ? mode : GRAD_F32_SET);
 }
 
-// The sums of the sink keys: segment shares added in the order of the segments, then to where the gradient goes.
-// grid (sink keys x Hkv), DH / 4 threads for dK and as many for dV
-__global__ void window_join_kernel(const float *part, int tile, int segs, int part_rows, int Hkv, int dh, void *dk, void *dv, int mode) {
+// A thread per four values of (key, KV head, dK or dV); the keys are those of the first st tiles, `lead` of them, then those of
+// the tiles from wt0 on.
+__global__ void __launch_bounds__(256)
+    window_join_kernel(const float *part, int tile, int st, int segs, int wt0, int wsegs, int lead, int rows, int Hkv, int dh, int64_t count,
+                       void *dk, void *dv, int mode) {
     pdl_enter();
-    const int key = blockIdx.x / Hkv, g = blockIdx.x % Hkv, kt = key / tile, row = key - kt * tile;
-    const int half = dh / 4, which = threadIdx.x / half, d = (threadIdx.x % half) * 4;      // 0: dK, 1: dV
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (t >= count) return;
+    const int per = dh / 4, d = (int)(t % per) * 4, which = (int)(t / per) & 1;
+    const int64_t unit = t / (2 * per);
+    const int i = (int)(unit / Hkv), g = (int)(unit % Hkv);
+    const bool head = i < lead;
+    const int key = head ? i : wt0 * tile + i - lead, kt = key / tile, row = key - kt * tile;
+    const int n = head ? segs : wsegs, item0 = head ? kt * segs : st * segs + (kt - wt0) * wsegs;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    const float *p = part + ((((int64_t)kt * segs * Hkv + g) * 2 + which) * part_rows + row) * dh + d;
-    const int64_t step = (int64_t)Hkv * 2 * part_rows * dh;
+    const float *p = part + ((((int64_t)item0 * Hkv + g) * 2 + which) * rows + row) * dh + d;
+    const int64_t step = (int64_t)Hkv * 2 * rows * dh;
 #pragma unroll 4
-    for (int i = 0; i < segs; i++) {
-        const float4 a = *reinterpret_cast<const float4 *>(p + i * step);
+    for (int k = 0; k < n; k++) {
+        const float4 a = *reinterpret_cast<const float4 *>(p + k * step);
         s[0] += a.x; s[1] += a.y; s[2] += a.z; s[3] += a.w;
     }
     put4(which ? dv : dk, ((int64_t)key * Hkv + g) * dh + d, s, mode);
@@ -321,25 +329,32 @@ int bwd(const T *q, const T *k, const T *v, const T *o, const T *dout, const flo
     if (!configured.get([&] { return set_smem(window_dkdv_kernel<T, DH>, smem) && set_smem(window_dq_kernel<T, DH>, smem) ? 1 : 0; }))
         return STREAMBP_E_CUDA;
     const int64_t rows = (int64_t)w.n * w.Hq;
-    const KeyWork<TILE> work = key_work<TILE>(w);
+    const KeyWork<TILE> work = key_work<TILE>(w, 0);
     const int64_t unseen16 = mode == GRAD_F32_ADD ? 0 : (int64_t)work.lo * TILE * w.Hkv * DH * (mode == GRAD_BF16_SET ? 2 : 4) / 16;
     SBP_LAUNCH(window_delta_any_kernel<T>, (unsigned)((rows * 32 + 255) / 256), 256, 0, st, o, dout, w.n, w.Hq, DH, delta, hdr, dk, dv,
                unseen16);
-    const int part_rows = w.sinks < TILE ? w.sinks : TILE;
+    const int part_rows = work.slot_rows(w);
     SBP_LAUNCH((window_dkdv_kernel<T, DH>), dim3(work.items(), w.Hkv), 256, smem, st, q, k, v, dout, lse, (const float *)delta, w,
                work, dk, dv, mode, part, part_rows);
     SBP_LAUNCH((window_dq_kernel<T, DH>), dim3((w.n + TILE - 1) / TILE, w.Hq), 256, smem, st, q, k, v, dout, lse,
                (const float *)delta, w, dq, mode);
+    if (work.segs > 1)
+        return attention_window_join(part, TILE, work.st, work.segs, work.wt0, work.wsegs, part_rows, w, DH, mode, dk, dv, st);
     return STREAMBP_OK;
 }
 
 }  // namespace
 
-// after either backward: the sink keys of tiles whose work was cut
-int attention_window_join(const float *part, int tile, int segs, const WindowShape &w, int dh, int mode, void *dk, void *dv,
-                          cudaStream_t st) {
-    const int rows = w.sinks < tile ? w.sinks : tile;
-    SBP_LAUNCH(window_join_kernel, (unsigned)w.sinks * (unsigned)w.Hkv, dh / 2, 0, st, part, tile, segs, rows, w.Hkv, dh, dk, dv, mode);
+int attention_window_join(const float *part, int tile, int st, int segs, int wt0, int wsegs, int rows, const WindowShape &w, int dh,
+                          int mode, void *dk, void *dv, cudaStream_t stream) {
+    // keys of the leading tiles: all of them where every row is joined, else the sinks
+    const int64_t kv = (int64_t)w.q0 + w.n, whole = (int64_t)st * tile < kv ? (int64_t)st * tile : kv;
+    const int64_t lead = segs > 1 ? (wsegs > 1 ? whole : w.sinks) : 0, behind = wsegs > 1 ? kv - (int64_t)wt0 * tile : 0;
+    const int64_t count = (lead + behind) * w.Hkv * (dh / 2), blocks = (count + 255) / 256;
+    if (blocks > 0x7fffffff) return STREAMBP_E_SHAPE;
+    if (count == 0) return STREAMBP_OK;
+    SBP_LAUNCH(window_join_kernel, (unsigned)blocks, 256, 0, stream, part, tile, st, segs, wt0, wsegs, (int)lead, rows, w.Hkv, dh, count, dk,
+               dv, mode);
     return STREAMBP_OK;
 }
 

@@ -451,8 +451,7 @@ int attn_bwd(const T *q, const T *k, const T *v, const T *o, const T *dout, cons
              int Hq, int Hkv, int dh, float *delta, float *dq, float *dk, float *dv, cudaStream_t st, int engine = -1);
 
 // Attention with a sliding window and sink keys (window.cuh).  mode: GradMode of dk, dv (dq is fp32, or bf16 with
-// GRAD_BF16_SET, and overwritten).  delta: [Hq, n] scratch; part: the sums of sink segments.  The backward calls leave the
-// rows of sink tiles whose work is cut (segs > 1) to attention_window_join.
+// GRAD_BF16_SET, and overwritten).  delta: [Hq, n] scratch; part: the sums of sink segments. 
 struct WindowShape;
 bool attention_window_tc_available();
 int attention_window_fwd_tc(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, int dh, bf16 *o, float *lse,
@@ -467,8 +466,10 @@ template <typename T>
 int attention_window_bwd_simt(const T *q, const T *k, const T *v, const T *o, const T *dout, const float *lse, const WindowShape &w,
                               int dh, int mode, void *dq, void *dk, void *dv, float *delta, float *part, WsHeader *hdr,
                               cudaStream_t st);
-int attention_window_join(const float *part, int tile, int segs, const WindowShape &w, int dh, int mode, void *dk, void *dv,
-                          cudaStream_t st);
+// Sums of key tiles whose work is cut: segments added in their order, then to where the gradients go.  Tiles are `tile` keys,
+// the first `st` with `segs` segments, the others, from `wt0`, with `wsegs`; `rows` rows to a workspace slot.
+int attention_window_join(const float *part, int tile, int st, int segs, int wt0, int wsegs, int rows, const WindowShape &w, int dh,
+                          int mode, void *dk, void *dv, cudaStream_t stream);
 
 // LM head pieces
 int count_valid_labels(const int64_t *labels, int64_t T, int64_t vocab, int64_t ignore, WsHeader *hdr,

@@ -4,6 +4,7 @@
 // All rows are below 2^31 (checked at the entry), so positions are ints; element offsets are 64-bit.
 #pragma once
 
+#include <cstddef>
 #include <cstdint>
 
 namespace sbp {
@@ -37,50 +38,56 @@ SBP_HD KeySpan key_span(const WindowShape &w, int first, int last) {
     s.ns = st < s.lo ? st : s.lo;
     return s;
 }
-// Whether rows first .. last see anything of tile kt <= their own (the span of two row tiles may hold tiles only one sees).
-template <int T>
-SBP_HD bool sees(const WindowShape &w, int kt, int first, int last) {
-    const int from = first - w.window + 1;
-    return kt <= last / T && (kt >= (from > 0 ? from / T : 0) || kt * T < w.sinks);
-}
 
 // The work of the key-tile owners (dK, dV): key tiles of TK keys against query tiles of TQ rows.  Tiles below `lo` hold
 // sinks only, or nothing that a query of the chunk sees.
-//   sink tiles 0 .. st - 1 : every later query adds to them; their query tiles are cut into `segs` segments of `len`
-//                            tiles, one owner each, whose sums are joined afterwards in the order of the segments
-//   window tiles wt0 .. kv_tiles - 1 : one owner each, over the query tiles the window reaches
+//   sink tiles 0 .. st - 1 : every later query adds to them; their query tiles are cut into `segs` segments of `len` tiles
+//   window tiles wt0 .. kv_tiles - 1 : over the query tiles the window reaches, cut into `wsegs` segments of `wlen`
+// One owner per segment; where there are several, fp32 sums meet in a workspace and are joined in the order of the
+// segments.  wsegs > 1 (a short chunk: few owners, each with a long walk over its group's heads): all rows of every tile go
+// through the workspace (`full`).  Else a sink tile's first segment covers every query that sees a key of the tile
+// through the window, and only the sinks' rows do.
 template <int TK, int TQ = TK> struct KeyWork {
-    int kv_tiles, q_tiles, lo, st, segs, len, wt0;
-    SBP_HD int items() const { return st * segs + (kv_tiles - wt0); }
+    int kv_tiles, q_tiles, lo, st, segs, len, wt0, wsegs, wlen;
+    SBP_HD int items() const { return st * segs + (kv_tiles - wt0) * wsegs; }
+    SBP_HD bool full() const { return wsegs > 1; }
     // item -> key tile, query tiles [begin, end), segment (-1: the item writes its result itself)
     SBP_HD void item(const WindowShape &w, int i, int &kt, int &begin, int &end, int &seg) const {
-        if (i < st * segs) {
-            kt = i / segs;
-            seg = i - kt * segs;
-            const int f = first(w, kt);
-            begin = f + seg * len;
-            end = begin + len < q_tiles ? begin + len : q_tiles;
-            if (segs == 1) { seg = -1; end = q_tiles; }
-        } else {
-            kt = wt0 + i - st * segs;
-            seg = -1;
-            begin = first(w, kt);
-            // the last query that sees the tile's last key through the window
-            const long long last = (long long)kt * TK + TK - 1 + w.window - 1 - w.q0;
-            end = last < 0 ? 0 : (last / TQ + 1 < q_tiles ? (int)(last / TQ) + 1 : q_tiles);
-        }
+        const bool sink = i < st * segs;
+        const int n = sink ? segs : wsegs, j = sink ? i : i - st * segs, step = sink ? len : wlen;
+        kt = (sink ? 0 : wt0) + j / n;
+        const int s = j % n;
+        // the last query that sees the tile's last key: any for a sink, else through the window
+        const long long last = (long long)kt * TK + TK - 1 + w.window - 1 - w.q0;
+        const int all = sink ? q_tiles : (last < 0 ? 0 : (last / TQ + 1 < q_tiles ? (int)(last / TQ) + 1 : q_tiles));
+        begin = first(w, kt) + s * step;
+        end = n == 1 || begin + step > all ? all : begin + step;
         if (end < begin) end = begin;
+        seg = n > 1 ? s : -1;
     }
     // first query tile that holds a row at or behind the tile's first key
     SBP_HD static int first(const WindowShape &w, int kt) {
         const long long k0 = (long long)kt * TK;
         return k0 > w.q0 ? (int)((k0 - w.q0) / TQ) : 0;
     }
+    // rows of tile kt whose sums go through the workspace where its work is cut, and the rows of a workspace slot
+    SBP_HD int joined_rows(const WindowShape &w, int kt) const {
+        const int r = full() ? TK : w.sinks - kt * TK;
+        return r < TK ? (r > 0 ? r : 0) : TK;
+    }
+    SBP_HD int slot_rows(const WindowShape &w) const { return full() || w.sinks > TK ? TK : w.sinks; }
+    // floats of the workspace: [item][Hkv][dK, dV][slot_rows][dh]
+    size_t part_floats(const WindowShape &w, int dh) const {
+        if (segs == 1 && wsegs == 1) return 0;
+        return (size_t)(full() ? items() : st * segs) * w.Hkv * 2 * slot_rows(w) * dh;
+    }
 };
+// `slots`: CTAs of the kernel that the 148 SMs hold at a time (0: windows are not cut).  A function of the sizes alone, so
+// that workspace queries need no GPU and the order of the sums is the same everywhere.
 template <int TK, int TQ = TK>
-inline KeyWork<TK, TQ> key_work(const WindowShape &w) {
+inline KeyWork<TK, TQ> key_work(const WindowShape &w, int slots) {
     KeyWork<TK, TQ> k;
-    const int kv = w.q0 + w.n;
+    const int kv = w.q0 + w.n, G = w.Hq / w.Hkv;
     k.kv_tiles = (kv + TK - 1) / TK;
     k.q_tiles = (w.n + TQ - 1) / TQ;
     const int from = w.q0 - w.window + 1;
@@ -88,10 +95,24 @@ inline KeyWork<TK, TQ> key_work(const WindowShape &w) {
     const int sink_tiles = (w.sinks + TK - 1) / TK;
     k.st = sink_tiles < k.kv_tiles ? sink_tiles : k.kv_tiles;
     k.wt0 = k.st > k.lo ? k.st : k.lo;
-    // a segment is as long as a window tile's walk, and the first one covers every query that sees a key of the tile
-    // through the window: in the later ones only the sinks have anything to add
+    // walk of a window tile; as a sink segment's length it covers the window's part of a sink tile
     k.len = (w.window + TK + 2 * TQ - 2) / TQ;
-    if (k.len < 8) k.len = 8;
+    const int walk = k.len < k.q_tiles ? k.len : k.q_tiles;
+    k.wsegs = 1;
+    k.wlen = k.len;
+    if (slots > 0) {
+        // costs in units of a quarter of a dQ tile of the same launch (TQ keys; a dK/dV one takes ~1.25x: four products
+        // against three): what a slot has to do on average, and the longest owner's walk
+        const long long span = ((w.window < kv ? w.window : kv) + TQ - 1) / TQ + 1 + (w.sinks + TQ - 1) / TQ;
+        const long long owners = (long long)(k.kv_tiles - k.wt0 + k.st) * w.Hkv, longest = 5ll * G * walk;
+        const long long each = (owners * longest + 4 * span * ((w.n + 127) / 128) * w.Hq) / slots;
+        // cut while the longest owner has more to do than a slot has on average (2000 rows, 16 heads to one key head, 128:
+        // 381 us uncut, 82 us; 4000 rows at heads of 64, window 300: 176 and 74), unless the owners are many already
+        while (k.wsegs < 16 && 2 * k.wsegs <= walk && longest > each * k.wsegs && owners * k.wsegs <= 2 * slots) k.wsegs *= 2;
+        k.wlen = (walk + k.wsegs - 1) / k.wsegs;
+    }
+    if (k.full()) k.len = k.wlen;
+    else if (k.len < 8) k.len = 8;
     k.segs = k.st > 0 ? (k.q_tiles + k.len - 1) / k.len : 1;
     // no more owners of sink tiles than four for each of 148 SMs: that many keep the GPU busy, and they bound the workspace
     // (many sinks need no segments at all)
@@ -105,13 +126,8 @@ inline KeyWork<TK, TQ> key_work(const WindowShape &w) {
 }
 // query rows to a tile of the tensor-core backward's key-tile owners, by head_dim
 constexpr int kBwdRows64 = 64, kBwdRows128 = 128;
-
-// rows of a sink tile whose sums go through the workspace
-template <int T>
-SBP_HD int sink_rows(const WindowShape &w, int kt) {
-    const int r = w.sinks - kt * T;
-    return r < T ? (r > 0 ? r : 0) : T;
-}
+// its CTAs on 148 SMs
+constexpr int kBwdSlots64 = 296, kBwdSlots128 = 148;
 
 // Where gradients go: fp32 added to or overwritten, or bf16 overwritten.
 enum GradMode { GRAD_F32_ADD = 0, GRAD_F32_SET = 1, GRAD_BF16_SET = 2 };

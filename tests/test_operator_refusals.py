@@ -150,12 +150,15 @@ def test_window_workspace(lib):
     assert all(size(32768, 0, 32, 8, 128, 128, s) < (200 << 20) for s in (0, 1, 4, 128, 1000, 16000, 32767, 1 << 20))
 
 
-def _key_work(n, q0, Hkv, window, sinks, TK, TQ):
+def _key_work(n, q0, Hkv, window, sinks, TK, TQ, wsegs):
     """The key tiles' work as window.cuh lays it out, restated: (key tile, query tiles, segment) of every item."""
     kv, qt = q0 + n, -(-n // TQ)
     lo = max(0, q0 - window + 1) // TK
     st = min(-(-sinks // TK), -(-kv // TK))
-    length = max(8, (window + TK + 2 * TQ - 2) // TQ)
+    length = (window + TK + 2 * TQ - 2) // TQ
+    walk = min(length, qt)
+    wlen = -(-walk // wsegs) if wsegs > 1 else length
+    length = wlen if wsegs > 1 else max(8, length)
     segs = -(-qt // length) if st else 1
     most = 592 // min(592, st * Hkv) if st else 1
     if segs > most:
@@ -163,21 +166,22 @@ def _key_work(n, q0, Hkv, window, sinks, TK, TQ):
         segs = -(-qt // length)
     first = lambda kt: (kt * TK - q0) // TQ if kt * TK > q0 else 0
     items = []
-    for kt in range(st):
-        for s in range(segs):
-            b = first(kt) + s * length
-            items.append((kt, range(b, qt if segs == 1 else min(qt, b + length)), s if segs > 1 else -1))
-    for kt in range(max(st, lo), -(-kv // TK)):
+    for kt in list(range(st)) + list(range(max(st, lo), -(-kv // TK))):
         last = kt * TK + TK - 1 + window - 1 - q0
-        items.append((kt, range(first(kt), min(qt, last // TQ + 1) if last >= 0 else 0), -1))
+        n_seg, step = (segs, length) if kt < st else (wsegs, wlen)
+        end = qt if kt < st else (min(qt, last // TQ + 1) if last >= 0 else 0)
+        for s in range(n_seg):
+            b = first(kt) + s * step
+            items.append((kt, range(b, end if n_seg == 1 else min(end, b + step)), s if n_seg > 1 else -1))
     return items
 
 
 def test_key_work_covers_every_visible_pair_once():
-    """Every visible (query, key) pair lies in exactly one item; behind the first segment of a sink tile only sinks are seen."""
+    """Every visible (query, key) pair lies in exactly one item; where windows are not cut, only sinks are seen behind the
+    first segment of a sink tile."""
     import random
     rng = random.Random(0)
-    for _ in range(400):
+    for _ in range(500):
         TK, TQ = rng.choice(((4, 4), (8, 8), (8, 4), (16, 4)))
         n, q0 = rng.randrange(1, 120), rng.choice((0, rng.randrange(0, 80)))
         window, sinks = rng.randrange(1, 60), rng.choice((0, 1, 3, 5, 17, 40))
@@ -186,14 +190,16 @@ def test_key_work_covers_every_visible_pair_once():
         sinks = min(sinks, kv)
         if sinks == kv or window == kv:
             window, sinks = kv, 0
+        walk = min((window + TK + 2 * TQ - 2) // TQ, -(-n // TQ))
+        wsegs = rng.choice([s for s in (1, 1, 2, 4, 8) if s <= walk])
         seen = {}
-        for kt, tiles, seg in _key_work(n, q0, rng.choice((1, 8, 200)), window, sinks, TK, TQ):
+        for kt, tiles, seg in _key_work(n, q0, rng.choice((1, 8, 200)), window, sinks, TK, TQ, wsegs):
             for qt in tiles:
                 assert 0 <= qt < -(-n // TQ)
                 for t in range(q0 + qt * TQ, min(q0 + n, q0 + qt * TQ + TQ)):
                     for j in range(kt * TK, min(kv, kt * TK + TK)):
                         if j <= t and (t - j < window or j < sinks):
                             seen[(t, j)] = seen.get((t, j), 0) + 1
-                            assert seg <= 0 or j < sinks
+                            assert seg <= 0 or wsegs > 1 or j < sinks
         want = {(t, j) for t in range(q0, kv) for j in range(t + 1) if t - j < window or j < sinks}
         assert set(seen) == want and set(seen.values()) <= {1}
