@@ -138,3 +138,89 @@ def gather_full_gradients(bucket: GradBucket, shard: torch.Tensor, group=None) -
     else:
         flat = shard
     return {k: flat[o:o + n].view(bucket.shapes[k]).clone() for k, (o, n) in bucket.table.items()}
+
+
+class ParamBucket:
+    """Flat parameters of one layer in the layout of its GradBucket (storage dtype), with named views: what the backward
+    reads as weights, and what a sharded optimizer writes one slice of per rank."""
+
+    def __init__(self, grads: GradBucket, values: Dict[str, torch.Tensor]):
+        dtype = next(iter(values.values())).dtype
+        self.flat = torch.zeros(grads.total, dtype=dtype, device=grads.flat.device)
+        self.views = {k: self.flat[o:o + n].view(grads.shapes[k]) for k, (o, n) in grads.table.items()}
+        for k, v in self.views.items():
+            v.copy_(values[k])
+
+
+def shard_slices(bucket: GradBucket, rank: int) -> List[Tuple[str, int, int]]:
+    """(name, begin, end) of every piece of a tensor inside a rank's shard, as offsets into the shard.  Tensors and shards
+    start on ALIGN_ELEMS boundaries, so every piece does too: aligned for the kernels, and a whole number of blocks of
+    8-bit moments before it."""
+    lo, _ = bucket.shard_range(rank)
+    out = []
+    for name, (a, b) in bucket.owner_slices(rank).items():
+        at = bucket.table[name][0] + a - lo
+        out.append((name, at, at + b - a))
+    return out
+
+
+class ShardedAdamW:
+    """One AdamW step of a layer's parameters, each rank on its shard of the summed gradients: the moments and the fp32
+    master copy exist once over all ranks.  `shard` is what DataParallelLayerBackward.exchange leaves (wait() first).
+    step() clips by the norm over the whole layer (an all-reduce of one number), updates this rank's slice on the library's
+    kernels and gathers the rounded parameters of all ranks.  A norm that is not finite leaves every rank's slice as it was.
+
+    weight_decay: per tensor name (missing: 0).  bits: 32, or 8 for moments in blocks of 32 e4m3 codes."""
+
+    def __init__(self, params: ParamBucket, grads: GradBucket, shard: torch.Tensor, weight_decay: Dict[str, float],
+                 bits: int = 8, group=None, rank: int = None, world: int = None):
+        from . import binding as B
+        if bits not in (8, 32):
+            raise ValueError("moments have 8 or 32 bits")
+        ready = dist.is_initialized()
+        self.rank = rank if rank is not None else (dist.get_rank(group) if ready else 0)
+        self.world = world if world is not None else (dist.get_world_size(group) if ready else 1)
+        if grads.world != self.world or shard.numel() != grads.shard_elems:
+            raise ValueError(f"the bucket is laid out for {grads.world} ranks, the group has {self.world}")
+        self.B, self.params, self.shard, self.group = B, params, shard, group
+        lo, hi = grads.shard_range(self.rank)
+        self.param = params.flat[lo:hi]
+        f32, dev, n = self.param.dtype == torch.float32, shard.device, hi - lo
+        self.master = None if f32 else self.param.float()
+        self.m, self.v = (torch.zeros(n, dtype=torch.uint8 if bits == 8 else torch.float32, device=dev) for _ in range(2))
+        self.scales = [torch.ones(n // B.MX8_BLOCK, dtype=torch.uint8, device=dev) for _ in range(2)] if bits == 8 else None
+        tensors = []
+        for name, a, b in shard_slices(grads, self.rank):
+            t = {"param": self.param[a:b], "grad": shard[a:b], "m": self.m[a:b], "v": self.v[a:b],
+                 "weight_decay": weight_decay.get(name, 0.0)}
+            if self.master is not None:
+                t["master"] = self.master[a:b]
+            if bits == 8:
+                s = slice(a // B.MX8_BLOCK, (b + B.MX8_BLOCK - 1) // B.MX8_BLOCK)
+                t["m_scale"], t["v_scale"] = self.scales[0][s], self.scales[1][s]
+            tensors.append(t)
+        self.plan = B.AdamWPlan(tensors) if tensors else None      # a short last shard may hold padding only
+        self.norm, self.scale = torch.zeros(1, device=dev), torch.ones(1, device=dev)
+        self.steps = torch.zeros(1, dtype=torch.int64, device=dev)
+        self.ws = B.alloc_workspace(B.grad_norm_workspace_bytes(), dev)
+
+    def step(self, lr: float, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, max_norm: float = 1.0) -> None:
+        """On the current stream."""
+        if self.plan is not None:
+            self.B.grad_norm(self.plan, max_norm, self.norm, self.scale, self.ws)
+        if self.world > 1:
+            total = self.norm.double().square_()
+            dist.all_reduce(total, group=self.group)
+            self.norm.copy_(total.sqrt_())
+            # what grad_norm writes for one rank; norm - norm is NaN where the norm is not finite
+            self.scale.copy_((max_norm / (self.norm + 1e-6)).clamp_(max=1.0) + (self.norm - self.norm))
+        self.steps += 1
+        if self.plan is not None:
+            self.B.adamw_step(self.plan, lr, beta1, beta2, eps, self.steps, grad_scale=self.scale)
+        if self.world > 1:
+            if dist.get_backend(self.group) == "nccl":
+                dist.all_gather_into_tensor(self.params.flat, self.param.clone(), group=self.group)
+            else:
+                parts = [torch.empty_like(self.param) for _ in range(self.world)]
+                dist.all_gather(parts, self.param, group=self.group)
+                self.params.flat.copy_(torch.cat(parts))
