@@ -1,7 +1,9 @@
 // Attention with a sliding window and sink keys on tcgen05 tensor cores (bf16 operands, head_dim 64 or 128): the queries
 // of one chunk against the key tiles their window reaches and the tiles that hold sinks; nothing else is loaded.
 //
-// Forward (attn_window_fwd_kernel): two persistent CTAs per SM, each walking (query tile of 128, head) items.
+// Forward (attn_window_fwd_kernel): two persistent CTAs per SM, each walking items: 128 rows of queries, which are the rows
+// of as many heads of one group as divide up, against the key tiles they see.  Few items: a cluster to each, which shares
+// its key tiles and joins the sums.
 //   warp 0      : TMA producer -- query tiles, K and V tiles of 64 keys through rings; runs ahead into the next item
 //   warp 1      : MMA issuer (warp-uniform issue) -- S = Q K^T into tensor memory two or three tiles ahead, O += P V with P
 //                 read from tensor memory (packed over the columns of its S: the product that reads P is queued before the
@@ -15,7 +17,8 @@
 // for scores ahead (16384 rows, window 128, heads of 64: 125 -> 107 us; window 1024, heads of 128: 350 -> 305 us).
 // A row may see nothing of the first tiles of its list: its maximum stays -infinity and it adds exact zeros until it sees
 // a key.  Every query sees its own key, so no row ends empty.  Groups of 32 columns that no row of a warp sees are skipped,
-// and the sink tile that the window does not reach is cut to its sinks (16 columns for up to 16 of them).
+// and the sink tile that the window does not reach is cut to its sinks (16 columns for up to 16 of them).  32 rows of four
+// heads span 96 keys fewer than 128 rows of one (16384 rows, window 128, heads of 64: 96 -> 86 us).
 // What bounds it: the exponentials and the conversions around them, ~770 of the ~1600 cycles of a CTA's step of 128 x 64
 // scores, and the latencies that two chains do not hide.
 //
@@ -121,9 +124,8 @@ __device__ __forceinline__ uint32_t visible_rows(const WindowShape &w, int key, 
     return key < w.sinks ? behind : behind & below(key + w.window - at);
 }
 // Whether a (query tile, key tile) pair holds hidden pairs: the diagonal or the window's far edge crosses it.
-template <int ROWS, int KEYS>
-__device__ __forceinline__ bool mixed(const WindowShape &w, int q0, int k0) {
-    return k0 + KEYS - 1 > q0 || (q0 + ROWS - 1 - k0 >= w.window && k0 + KEYS > w.sinks);
+__device__ __forceinline__ bool mixed(const WindowShape &w, int q0, int rows, int k0, int keys) {
+    return k0 + keys - 1 > q0 || (q0 + rows - 1 - k0 >= w.window && k0 + keys > w.sinks);
 }
 
 __device__ __forceinline__ void leave(volatile int *abort_flag) {
@@ -141,7 +143,10 @@ struct FwdParams {
     WindowShape w;
     float *lse;         // [Hq, n]
     float scale_log2;   // log2(e) / sqrt(head_dim)
-    int q_tiles, items; // items = q_tiles * Hq, the last query tiles (longest spans) first, the heads of a tile side by side
+    int heads, tokens;  // rows of a tile: `tokens` query rows of `heads` heads of one group, the heads of a row side by side
+    int q_tiles, items; // items = q_tiles * Hq / heads, the last query tiles (longest spans) first, heads side by side
+    int split;          // CTAs that share an item's key tiles, a cluster (SPLIT kernel)
+    bf16 *o;            // SPLIT kernel
     int edge, edge_keys;// the sink tile that holds sinks in its first rows only (-1: none), and those rows rounded up to 16
 };
 
@@ -245,7 +250,21 @@ __device__ __forceinline__ bool softmax_tile(float scale_log2, uint32_t tS, uint
     return true;
 }
 
-template <int DH>
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+    return v;
+}
+template <int N>
+__device__ __forceinline__ void ld_cluster(uint32_t addr, float (&v)[N]) {
+    static_assert(N == 2 || N == 4, "8 or 16 bytes");
+    if (N == 4) asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[N - 2]), "=f"(v[N - 1]) : "r"(addr));
+    else asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(addr));
+}
+
+// SPLIT: one item to a cluster, its key tiles dealt to the CTAs in order; each leaves O, the reference of its exponentials
+// and their sum in its shared memory, and the rows are joined from there, dealt to the warps of all.
+template <int DH, bool SPLIT>
 __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
     attn_window_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                            const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_ke,
@@ -265,6 +284,7 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(aux + 232);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(aux + 240);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = SPLIT ? (int)cluster_cta_rank() : 0;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < NQ; s++) {
@@ -294,18 +314,26 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
     const uint32_t tmem = *tmem_slot;      // O (DH columns), then the S tiles (64 columns each)
     const bool usable = *abort_flag == 0;
 
-    // an item: one query tile of one head
-    struct Item { int h, qt0, first, count; KeySpan span; };
+    // an item: the query tile's rows of some heads of a group against key tiles begin .. end - 1 of its span
+    struct Item { int h0, t0, first, begin, end; KeySpan span; };
+    const int groups = p.w.Hq / p.heads;
     auto item_at = [&](int i) {
         Item t;
-        t.h = i % p.w.Hq;
-        t.qt0 = (p.q_tiles - 1 - i / p.w.Hq) * TILE;
-        const int rows = p.w.n - t.qt0 < TILE ? p.w.n - t.qt0 : TILE;
-        t.first = p.w.q0 + t.qt0;
+        t.h0 = i % groups * p.heads;
+        t.t0 = (p.q_tiles - 1 - i / groups) * p.tokens;
+        const int rows = p.w.n - t.t0 < p.tokens ? p.w.n - t.t0 : p.tokens;
+        t.first = p.w.q0 + t.t0;
         t.span = key_span<KT>(p.w, t.first, t.first + rows - 1);
-        t.count = t.span.count();
+        const int count = t.span.count();
+        t.begin = SPLIT ? (int)((long long)count * rank / p.split) : 0;
+        t.end = SPLIT ? (int)((long long)count * (rank + 1) / p.split) : count;
         return t;
     };
+    // the items of this CTA: SPLIT, the cluster's one, or none where there are fewer key tiles than CTAs
+    const Item mine = item_at(SPLIT ? (int)blockIdx.x / p.split : 0);
+    auto first_item = [&] { return SPLIT ? (int)blockIdx.x / p.split : (int)blockIdx.x; };
+    auto next_item = [&](int i) { return SPLIT ? p.items : i + (int)gridDim.x; };
+    auto is_item = [&](int i) { return i < p.items && (!SPLIT || mine.begin < mine.end); };
     // keys of a tile that take part: all, or the sinks at the head of the edge tile where the window does not reach it
     auto keys_of = [&](const Item &t, int j) { return j < t.span.ns && j == p.edge ? p.edge_keys : KT; };
 
@@ -315,14 +343,16 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
         if (lane == 0) {
             RingAt q, kv;
             bool alive = true;
-            for (int i = blockIdx.x; i < p.items && alive; i += gridDim.x) {
+            for (int i = first_item(); is_item(i) && alive; i = next_item(i)) {
                 const Item t = item_at(i);
-                const int g = t.h / (p.w.Hq / p.w.Hkv);
+                const int g = t.h0 / (p.w.Hq / p.w.Hkv);
                 if (!mbar_wait(q_empty + 8 * q.st, q.ph ^ 1u, abort_flag)) break;
-                mbar_expect_tx(q_full + 8 * q.st, F::kQ);
-                load_tile<DH>(sQ + q.st * F::kQ, &map_q, q_full + 8 * q.st, t.h, t.qt0);
+                mbar_expect_tx(q_full + 8 * q.st, (uint32_t)(p.heads * p.tokens * DH * 2));
+#pragma unroll
+                for (int c = 0; c < DH / 64; c++)
+                    tma_load_3d(sQ + q.st * F::kQ + c * SUB_BYTES, &map_q, q_full + 8 * q.st, c * 64, t.h0, t.t0);
                 q.next<NQ>();
-                for (int j = 0; j < t.count; j++) {
+                for (int j = t.begin; j < t.end; j++) {
                     const int row = t.span.tile(j) * KT, keys = keys_of(t, j);
                     const bool part = keys < KT;
                     const uint32_t bytes = (uint32_t)keys * DH * 2u;
@@ -344,13 +374,16 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
         constexpr uint32_t idesc_pv = make_idesc(TILE, DH, false, true);
         // two cursors over the same sequence of (item, tile): S runs up to NS tiles ahead of P V
         RingAt q, k, v, bs, bp;                         // rings: Q and K (by S), V (by P V), S tiles (by S and by P V)
-        int is = blockIdx.x, js = 0, ip = blockIdx.x, jp = 0;
+        int is = first_item(), js = 0, ip = is, jp = 0;
         Item ts, tp;
-        if (is < p.items) ts = tp = item_at(is);
+        if (is_item(is)) {
+            ts = tp = item_at(is);
+            js = jp = ts.begin;
+        }
         bool alive = true;
         auto issue_s = [&]() -> bool {                  // S = Q K^T of the next tile; the last of an item hands Q back
-            if (is >= p.items) return true;
-            if (js == 0 && !mbar_wait_warp(q_full + 8 * q.st, q.ph, abort_flag)) return false;
+            if (!is_item(is)) return true;
+            if (js == ts.begin && !mbar_wait_warp(q_full + 8 * q.st, q.ph, abort_flag)) return false;
             if (!mbar_wait_warp(k_full + 8 * k.st, k.ph, abort_flag)) return false;
             tc_fence_after();
             const uint32_t q_lo = klo(sQ + q.st * F::kQ), k_lo = klo(sK + k.st * F::kKV);
@@ -361,17 +394,19 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
             umma_commit_w(k_empty + 8 * k.st);
             k.next<N>();
             bs.next<NS>();
-            if (++js == ts.count) {
+            if (++js == ts.end) {
                 umma_commit_w(q_empty + 8 * q.st);
                 q.next<NQ>();
-                js = 0;
-                is += gridDim.x;
-                if (is < p.items) ts = item_at(is);
+                is = next_item(is);
+                if (is_item(is)) {
+                    ts = item_at(is);
+                    js = ts.begin;
+                }
             }
             return true;
         };
         for (int s = 0; s < NS && alive; s++) alive = issue_s();
-        while (alive && ip < p.items) {
+        while (alive && is_item(ip)) {
             // O += P V once P is stored; the S tile that P lay in then takes the scores NS tiles further on
             if (!mbar_wait_warp(v_full + 8 * v.st, v.ph, abort_flag) || !mbar_wait_warp(p_full + 8 * bp.st, bp.ph, abort_flag)) break;
             tc_fence_after();
@@ -379,21 +414,24 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
             const int slices = keys_of(tp, jp) / 16;
 #pragma unroll
             for (int kk = 0; kk < KT / 16; kk++)
-                if (kk < slices) umma_ts_w(tmem, a + kk * 8, v_lo + mnstep(kk), idesc_pv, (jp | kk) != 0);
+                if (kk < slices) umma_ts_w(tmem, a + kk * 8, v_lo + mnstep(kk), idesc_pv, jp != tp.begin || kk != 0);
             umma_commit_w(v_empty + 8 * v.st);
             umma_commit_w(pv_done + 8 * bp.st);
             v.next<N>();
             bp.next<NS>();
             alive = issue_s();
-            if (++jp == tp.count) {
-                jp = 0;
-                ip += gridDim.x;
-                if (ip < p.items) tp = item_at(ip);
+            if (++jp == tp.end) {
+                ip = next_item(ip);
+                if (is_item(ip)) {
+                    tp = item_at(ip);
+                    jp = tp.begin;
+                }
             }
         }
     } else {
         const int quarter = warp & 3;
-        const int row = quarter * 32 + lane;
+        const int row = quarter * 32 + lane, token = row / p.heads, head = row % p.heads;
+        const int seen_as = token < p.tokens ? token : p.tokens - 1;       // rows that are none of the tile's see as its last
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t tO = tmem + lane_base;
         const uint32_t stage0 = sO + quarter * 4096u;
@@ -403,14 +441,14 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
         // and S of a tile, which it has seen, was issued behind the last use of that tile's barrier -- a single barrier
         // could still be two phases back and pass for done.
         auto rest = [&]() -> bool { return mbar_wait(pv_done + 8 * before.st, before.ph, abort_flag); };
-        for (int i = blockIdx.x; i < p.items && alive; i += gridDim.x) {
+        for (int i = first_item(); is_item(i) && alive; i = next_item(i)) {
             const Item t = item_at(i);
-            const int q_abs = t.first + row;
+            const int q_abs = t.first + seen_as;
             float m_used = -INFINITY, l = 0.f;
-            for (int j = 0; j < t.count; j++) {
+            for (int j = t.begin; j < t.end; j++) {
                 const int k0 = t.span.tile(j) * KT;
                 const uint32_t tS = tmem + DH + b.st * KT + lane_base;
-                const bool hidden = mixed<TILE, KT>(p.w, t.first, k0);
+                const bool hidden = mixed(p.w, t.first, p.tokens, k0, KT);
                 uint32_t see[2];
                 if (hidden) {
                     see[0] = visible_keys(p.w, q_abs, k0, 0);
@@ -418,8 +456,8 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
                 }
                 if (!mbar_wait(s_full + 8 * b.st, b.ph, abort_flag)) { alive = false; break; }
                 tc_fence_after();
-                alive = hidden ? softmax_tile<true, DH>(p.scale_log2, tS, tO, see, j > 0, m_used, l, rest)
-                               : softmax_tile<false, DH>(p.scale_log2, tS, tO, see, j > 0, m_used, l, rest);
+                alive = hidden ? softmax_tile<true, DH>(p.scale_log2, tS, tO, see, j > t.begin, m_used, l, rest)
+                               : softmax_tile<false, DH>(p.scale_log2, tS, tO, see, j > t.begin, m_used, l, rest);
                 if (!alive) break;
                 tmem_wait_st();
                 tc_fence_before();
@@ -430,6 +468,22 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
             }
             if (!alive || !rest()) { alive = false; break; }
             tc_fence_after();
+            if (SPLIT) {       // the rings of K and V are done with: O there, 16-byte groups of eight rows on different banks
+                if (quarter * 32 < p.heads * p.tokens) {
+#pragma unroll 1
+                    for (int c = 0; c < DH / 32; c++) {
+                        uint32_t o[32];
+                        tmem_ld32(tO + c * 32, o);
+#pragma unroll
+                        for (int e = 0; e < 8; e++)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                         ::"r"(sK + (uint32_t)(row * DH * 4 + (((c * 8 + e) ^ (row & 7)) << 4))), "r"(o[4 * e]),
+                                         "r"(o[4 * e + 1]), "r"(o[4 * e + 2]), "r"(o[4 * e + 3]) : "memory");
+                    }
+                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(sO + row * 8u), "f"(m_used), "f"(l) : "memory");
+                }
+                continue;
+            }
             // O / l through 32 x 32 blocks in shared memory (rows of 64 bytes, 64-byte swizzle) and TMA stores, which clip
             // the rows behind the last query; the warp's next P is handed over only after its O has been read
             const float inv = 1.f / l;
@@ -452,19 +506,81 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    tma_store_2d(&map_o, stage, t.h * DH + c * 32, t.qt0 + quarter * 32);
+                    tma_store_3d(&map_o, stage, c * 32, t.h0, t.t0 + quarter * (32 / p.heads));
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
             }
-            if (t.qt0 + row < p.w.n) p.lse[(long long)t.h * p.w.n + t.qt0 + row] = (m_used + log2f(l)) * kLn2;
+            if (t.t0 + token < p.w.n) p.lse[(long long)(t.h0 + head) * p.w.n + t.t0 + token] = (m_used + log2f(l)) * kLn2;
         }
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (SPLIT && mine.begin == mine.end) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(sO + row * 8u), "f"(-INFINITY), "f"(0.f) : "memory");
+        if (!SPLIT && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
 
     __syncwarp();
+    if (SPLIT) {
+        cluster_sync_all();
+        // out = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c over the CTAs c; four rows to a warp at a time, a lane has DH / 32
+        // columns of each
+        if (!*abort_flag) {
+            constexpr int NC = DH / 32;
+            const Item &t = mine;
+            const int rows = (p.w.n - t.t0 < p.tokens ? p.w.n - t.t0 : p.tokens) * p.heads, warps = p.split * (F::kThreads / 32);
+            for (int r0 = rank * (F::kThreads / 32) + warp; r0 < rows; r0 += 4 * warps) {
+                // lane (row i, CTA c): their reference, sum and weight
+                const int c_l = lane & 7, r_l = r0 + (lane >> 3) * warps;
+                float m = -INFINITY, l = 0.f;
+                if (c_l < p.split && r_l < rows) {
+                    const uint32_t at = map_to_cta(sO, (uint32_t)c_l) + r_l * 8u;
+                    m = ld_cluster_f32(at);
+                    l = ld_cluster_f32(at + 4u);
+                }
+                float top = m;
+#pragma unroll
+                for (int x = 1; x < 8; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                const float f = m == -INFINITY ? 0.f : fast_exp2(m - top);
+                float sum = l * f;
+#pragma unroll
+                for (int x = 1; x < 8; x *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+                const float weight = f / sum;
+                float acc[4][NC];
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int e = 0; e < NC; e++) acc[i][e] = 0.f;
+#pragma unroll 2
+                for (int c = 0; c < p.split; c++) {
+                    const uint32_t from = map_to_cta(sK, (uint32_t)c);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int r = r0 + i * warps;
+                        const float wt = __shfl_sync(0xffffffffu, weight, i * 8 + c);
+                        float o[NC];
+                        if (r >= rows) continue;
+                        ld_cluster<NC>(from + (uint32_t)(r * DH * 4 + (((lane * NC >> 2) ^ (r & 7)) << 4) + (lane * NC & 3) * 4), o);
+#pragma unroll
+                        for (int e = 0; e < NC; e++)
+                            if (wt != 0.f) acc[i][e] = fmaf(o[e], wt, acc[i][e]);      // nothing seen there: O may never have been written
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int r = r0 + i * warps;
+                    if (r >= rows) break;
+                    const int h = t.h0 + r % p.heads, at = t.t0 + r / p.heads;
+                    bf16 *out = p.o + ((long long)at * p.w.Hq + h) * DH + lane * NC;
+#pragma unroll
+                    for (int e = 0; e < NC; e += 2) *reinterpret_cast<uint32_t *>(out + e) = pack_bf16(acc[i][e], acc[i][e + 1]);
+                }
+                if (c_l == 0 && r_l < rows)
+                    p.lse[(long long)(t.h0 + r_l % p.heads) * p.w.n + t.t0 + r_l / p.heads] = (top + log2f(sum)) * kLn2;
+            }
+        }
+        __syncwarp();
+    }
     leave(abort_flag);
     tc_fence_before();
     __syncthreads();
+    if (SPLIT) cluster_sync_all();          // no CTA leaves while another may read its sums
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, 256);
@@ -744,7 +860,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             if (lane == 0) mbar_arrive(loaded);
             // the producer's lse / delta rows of this stage are published together with the dO tile
             if (!mbar_wait(do_full + 8 * sd, (it >> 1) & 1, abort_flag)) { alive = false; break; }
-            const uint32_t see = mixed<IT, TILE>(p.w, q_abs0, k_abs0) ? visible_rows(p.w, k_abs, q_abs0, col_base) : 0xffffffffu;
+            const uint32_t see = mixed(p.w, q_abs0, IT, k_abs0, TILE) ? visible_rows(p.w, k_abs, q_abs0, col_base) : 0xffffffffu;
             if (!__any_sync(0xffffffffu, see != 0u)) {     // P and dS of all of the warp's pairs are zero
                 if (!mbar_wait(dp_full, it & 1, abort_flag)) { alive = false; break; }
                 tc_fence_after();
@@ -993,7 +1109,7 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
             const int k_abs0 = span.tile(j) * IT;
             if (!mbar_wait(s_full, j & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
-            const uint32_t see = mixed<TILE, IT>(p.w, q_abs0, k_abs0) ? visible_keys(p.w, q_abs, k_abs0, key_base) : 0xffffffffu;
+            const uint32_t see = mixed(p.w, q_abs0, TILE, k_abs0, IT) ? visible_keys(p.w, q_abs, k_abs0, key_base) : 0xffffffffu;
             if (!__any_sync(0xffffffffu, see != 0u)) {     // dS of all of the warp's pairs is zero
                 __syncwarp();
                 if (lane == 0) mbar_arrive(s_free);
@@ -1143,20 +1259,77 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
     p.w = w;
     p.lse = lse;
     p.scale_log2 = kLog2e / sqrtf((float)DH);
-    p.q_tiles = (w.n + TILE - 1) / TILE;
-    const int64_t items = (int64_t)p.q_tiles * w.Hq, kv = (int64_t)w.q0 + w.n;
+    p.o = o;
+    const int64_t kv = (int64_t)w.q0 + w.n;
+    const int G = w.Hq / w.Hkv, slots = 2 * sm_count();
+    // Rows of a tile come from all heads of a group, as far as that divides up: the fewer query rows in a tile, the fewer key
+    // tiles it spans, and a handful of rows fills tiles that would be read for each head by itself.
+    auto tile_of = [&](int heads) {
+        p.heads = heads;
+        p.tokens = TILE / heads;
+        p.q_tiles = (w.n + p.tokens - 1) / p.tokens;
+        return (int64_t)p.q_tiles * (w.Hq / heads);
+    };
+    int heads = 1;
+    while (heads < 32 && G % (2 * heads) == 0) heads *= 2;          // whole rows to a warp, which stores its 32 by itself
+    int64_t items = tile_of(heads);
+    p.split = 1;
+    if (2 * items <= slots) {
+        // few rows: any divisor of the group, and clusters that share an item's key tiles
+        int best = 1;
+        for (int d = 2; d <= G && d <= TILE; d++)
+            if (G % d == 0 && tile_of(d) <= tile_of(best)) best = d;
+        const int64_t few = tile_of(best);
+        const int count = key_span<KT>(w, w.q0 + (p.q_tiles - 1) * p.tokens, w.q0 + w.n - 1).count();
+        int64_t split = slots / few < 8 ? slots / few : 8;
+        if (split > count) split = count;
+        // Joining costs as much as 2 steps of a CTA (128 x 64 scores, 0.76 us) and one more for each 16 rows.  At heads of 128,
+        // split against one CTA an item: one row of 28:4 heads, window 1024: 8.9 us against 17.6, window 64: 6.2 and 6.1; 32
+        // rows of 32:8 heads, window 1024: 13.1 and 17.2, window 512: 12.5 and 11.1.
+        const int joined = (w.n < p.tokens ? w.n : p.tokens) * best;
+        if (split > 1 && count - (count + split - 1) / split > 2 + joined / 16) {
+            items = few;
+            p.split = (int)split;
+        } else {
+            tile_of(heads);
+        }
+    }
     if (items > 0x7fffffff / 2) return STREAMBP_E_SHAPE;
     p.items = (int)items;
     edge_of<KT>(w, 16, p.edge, p.edge_keys);
     CUtensorMap mq, mk, mv, ke, ve, mo;
-    if (!tile_map<DH>(&mq, q, w.n, w.Hq, TILE) || !tile_map<DH>(&mk, k, kv, w.Hkv, KT) || !tile_map<DH>(&mv, v, kv, w.Hkv, KT) ||
-        !tile_map<DH>(&ke, k, kv, w.Hkv, (uint32_t)p.edge_keys) || !tile_map<DH>(&ve, v, kv, w.Hkv, (uint32_t)p.edge_keys) ||
-        !make_tensor_map(&mo, o, w.n, (int64_t)w.Hq * DH, (int64_t)w.Hq * DH, 32, 32, false, CU_TENSOR_MAP_SWIZZLE_64B))
+    if (!make_heads_map(&mq, q, w.n, w.Hq, DH, 64, (uint32_t)p.heads, (uint32_t)p.tokens) || !tile_map<DH>(&mk, k, kv, w.Hkv, KT) ||
+        !tile_map<DH>(&mv, v, kv, w.Hkv, KT) || !tile_map<DH>(&ke, k, kv, w.Hkv, (uint32_t)p.edge_keys) ||
+        !tile_map<DH>(&ve, v, kv, w.Hkv, (uint32_t)p.edge_keys))
         return STREAMBP_E_CUDA;
+    if (p.split > 1) {
+        static PerDevice configured;
+        if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, true>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cfg.gridDim = dim3((unsigned)(p.items * p.split));
+        cfg.blockDim = dim3(F::kThreads);
+        cfg.dynamicSmemBytes = F::kSmem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[2];
+        memset(attr, 0, sizeof(attr));
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)p.split;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, attn_window_fwd_kernel<DH, true>, mq, mk, mv, ke, ve, mk, p);
+        call_state().launches++;
+        return cuda_ok(e) && cuda_ok(cudaGetLastError()) ? STREAMBP_OK : STREAMBP_E_CUDA;
+    }
+    if (!make_heads_map(&mo, o, w.n, w.Hq, DH, 32, (uint32_t)p.heads, 32u / (uint32_t)p.heads, CU_TENSOR_MAP_SWIZZLE_64B)) return STREAMBP_E_CUDA;
     static PerDevice configured;
-    if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
-    const int slots = 2 * sm_count();
-    SBP_LAUNCH(attn_window_fwd_kernel<DH>, p.items < slots ? p.items : slots, F::kThreads, F::kSmem, st, mq, mk, mv, ke, ve, mo, p);
+    if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, false>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+    void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
+                   const FwdParams) = attn_window_fwd_kernel<DH, false>;
+    SBP_LAUNCH(kernel, p.items < slots ? p.items : slots, F::kThreads, F::kSmem, st, mq, mk, mv, ke, ve, mo, p);
     return STREAMBP_OK;
 }
 

@@ -131,6 +131,32 @@ def test_tensor_core_shapes(n, q0, window, sinks, dh):
     run(Case(n, q0, 4, 2, dh, window, sinks), engines=(0,), grads=(F32, BF))
 
 
+# (rows, heads): more (128-row tile, head) items than the GPU holds at half load, so that the forward walks them with persistent
+# CTAs; tiles of 1, 2, 4, 16 and 32 heads of a group
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(32, 32), (28, 4), (24, 12), (32, 8), (32, 2), (64, 1)])
+def test_many_items(Hq, Hkv, dh):
+    for n, q0, window, sinks in ((777, 100, 90, 3), (801, 0, 300, 70)):
+        case = Case(n, q0, Hq, Hkv, dh, window, sinks)
+        ref, err = case.reference()
+        o, lse = case.forward()
+        case.check("o", o, ref["o"], err["o"])
+        case.check("lse", lse, ref["lse"], err["lse"])
+
+
+# few rows: all heads of a group in one tile (47 does not divide into 128 rows), key tiles dealt to a cluster, some of whose
+# CTAs see nothing of a row
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(28, 4), (16, 1), (47, 1), (150, 1), (6, 2), (8, 8)])
+def test_few_rows(Hq, Hkv, dh):
+    for n, q0, window, sinks in ((1, 0, 1, 0), (1, 999, 1000, 0), (1, 777, 100, 400), (3, 1500, 640, 1), (9, 1000, 3, 700), (20, 1, 20, 0)):
+        case = Case(n, q0, Hq, Hkv, dh, window, sinks)
+        ref, err = case.reference()
+        o, lse = case.forward()
+        case.check("o", o, ref["o"], err["o"])
+        case.check("lse", lse, ref["lse"], err["lse"])
+
+
 @pytest.mark.parametrize("Hq,Hkv", [(1, 1), (7, 1), (6, 6), (14, 2), (3, 3)])
 def test_head_layouts(Hq, Hkv):
     run(Case(300, 150, Hq, Hkv, 64, 100, 2), engines=(0, 2), grads=(BF,))
