@@ -365,9 +365,9 @@ size_t window_scratch(const WindowShape &w, int dh, void *base, WindowScratch *o
     Arena a(base);
     a.take_bytes(kHeaderBytes);
     out->delta = a.take<float>((size_t)w.Hq * w.n);
-    const size_t x = dh == 64 ? key_work<128, kBwdRows64>(w, kBwdSlots64).part_floats(w, dh)
-                              : key_work<128, kBwdRows128>(w, kBwdSlots128).part_floats(w, dh),
-                 y = key_work<32>(w, 0).part_floats(w, dh);
+    const size_t x = dh == 64 ? key_work<128>(w, kBwdRows64, bwd_heads(w, kBwdRows64), kBwdSlots64).part_floats(w, dh)
+                              : key_work<128>(w, kBwdRows128, bwd_heads(w, kBwdRows128), kBwdSlots128).part_floats(w, dh),
+                 y = key_work<32>(w, 32, 1, 0).part_floats(w, dh);
     out->part = a.take<float>(x > y ? x : y);
     return a.size();
 }

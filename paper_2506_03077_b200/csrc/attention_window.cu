@@ -117,11 +117,12 @@ __device__ __forceinline__ uint32_t visible_keys(const WindowShape &w, int row, 
     const int at = k0 + base;
     return below(row + 1 - at) & (~below(row - w.window + 1 - at) | below(w.sinks - at));
 }
-// Which of the query rows q0 + base .. + 31 see the key, as bits.
-__device__ __forceinline__ uint32_t visible_rows(const WindowShape &w, int key, int q0, int base) {
-    const int at = q0 + base;
-    const uint32_t behind = ~below(key - at);
-    return key < w.sinks ? behind : behind & below(key + w.window - at);
+// Which of a tile's columns base .. + 31 see the key, as bits: columns are query rows q0 .. of `heads` heads each, the heads
+// of a row side by side; `cols` are used.
+__device__ __forceinline__ uint32_t visible_columns(const WindowShape &w, int key, int q0, int heads, int cols, int base) {
+    auto before = [&](int row) { return below(min(max(row - q0, 0), 128) * heads - base); };     // the columns of rows q0 .. row - 1
+    const uint32_t behind = below(cols - base) & ~before(key);
+    return key < w.sinks ? behind : behind & before(key + w.window);
 }
 // Whether a (query tile, key tile) pair holds hidden pairs: the diagonal or the window's far edge crosses it.
 __device__ __forceinline__ bool mixed(const WindowShape &w, int q0, int rows, int k0, int keys) {
@@ -607,7 +608,7 @@ template <int DH> struct Bwd {
     static constexpr int kTiles = 2 * kOut + 5 * kIn;
     static constexpr int kSmem = kTiles + 4 * IT * 4 /* lse, delta x 2 stages */ + 256 + kSlack;
     static_assert(kBlocks * (kSmem + 1024) <= 233472 && 4 * kGroups * 8192 <= kTiles, "backward roles exceed the shared memory of an SM");
-    typedef KeyWork<TILE, IT> Work;
+    typedef KeyWork<TILE> Work;
     __host__ __device__ static constexpr uint32_t step(int kk) { return (uint32_t)((kk >> 2) * (kInSub >> 4) + (kk & 3) * 2); }
 };
 template <int DH>
@@ -623,6 +624,12 @@ struct BwdParams {
     int edge, edge_keys;  // dQ role: the sink tile that holds sinks in its first rows only (-1: none), those rows rounded up to 32
     int n_dkdv, n_dq_first;         // dK/dV CTAs; dQ CTAs that are dispatched before them (all or none)
     float scale, scale_log2;
+    // PACKED: several heads of a group share a tile.  Heads of a query row, query rows of an inner tile (dK/dV role), the rows
+    // that these make, query rows of a resident tile (dQ role).
+    template <bool PACKED> __host__ __device__ int heads() const { return PACKED ? work.heads : 1; }
+    template <bool PACKED> __host__ __device__ int rows() const { return PACKED ? work.tq : Bwd<DH>::IT; }
+    template <bool PACKED> __host__ __device__ int used() const { return PACKED ? work.heads * work.tq : Bwd<DH>::IT; }
+    template <bool PACKED> __host__ __device__ int tokens() const { return PACKED ? TILE / work.heads : TILE; }
 };
 
 // 32 fp32 sums of one row to where the gradient goes
@@ -652,7 +659,8 @@ __device__ __forceinline__ void put32(void *dst, long long at, const uint32_t (&
 
 // The same for a warp's 32 rows through a block of shared memory and a TMA store (or add), which clips the rows behind the
 // last.  Written by the lanes themselves, 16 bytes of 32 rows at a time, the epilogue of a CTA took 4000 - 8000 cycles.
-__device__ __forceinline__ void put_block(const CUtensorMap *map, uint32_t at, const uint32_t (&r)[32], int lane, int col, int row0, int mode) {
+template <typename Store>
+__device__ __forceinline__ void put_block(uint32_t at, const uint32_t (&r)[32], int lane, int mode, Store store) {
     if (mode == GRAD_BF16_SET) {                            // rows of 64 bytes, 64-byte swizzle
 #pragma unroll
         for (int j = 0; j < 4; j++) {
@@ -671,13 +679,24 @@ __device__ __forceinline__ void put_block(const CUtensorMap *map, uint32_t at, c
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) {
-        if (mode == GRAD_F32_ADD) tma_reduce_add_2d(map, at, col, row0);
-        else tma_store_2d(map, at, col, row0);
+        store();
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
 }
+__device__ __forceinline__ void put_block(const CUtensorMap *map, uint32_t at, const uint32_t (&r)[32], int lane, int col, int row0, int mode) {
+    put_block(at, r, lane, mode, [&] {
+        if (mode == GRAD_F32_ADD) tma_reduce_add_2d(map, at, col, row0);
+        else tma_store_2d(map, at, col, row0);
+    });
+}
+// rows [rows][heads] of a tile of DH columns
+template <int DH, int SUB>
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap *map, uint32_t bar, int head, int row) {
+#pragma unroll
+    for (int c = 0; c < DH / 64; c++) tma_load_3d(dst + c * SUB, map, bar, c * 64, head, row);
+}
 
-template <int DH>
+template <int DH, bool PACKED>
 __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
                                           const CUtensorMap &map_do, const CUtensorMap &map_dk, const CUtensorMap &map_dv,
                                           const CUtensorMap &map_part, const BwdParams<DH> &p, uint8_t *smem_raw, int item, int g) {
@@ -702,7 +721,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
     int kt, qt_begin, qt_end, seg;
     p.work.item(p.w, item, kt, qt_begin, qt_end, seg);
     const int k_abs0 = kt * TILE;
-    const int iters = G * (qt_end - qt_begin);        // the query heads of the group, each over the item's query tiles
+    const int iters = G / p.template heads<PACKED>() * (qt_end - qt_begin);     // the query heads of the group, `heads` at a time, over the item's query tiles
 
     if (threadIdx.x == 0) {
         mbar_init(kv_full, 1);
@@ -726,6 +745,13 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
         if (*abort_flag) atomicExch(&g_tc_fault, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (p.template used<PACKED>() < IT) {       // rows that no copy reaches are factors of the products: zeros
+        for (int i = threadIdx.x; i < (QS + 2) * (DH / 64) * (IT - p.template used<PACKED>()) * 8; i += W::kThreads) {
+            const int sub = i / ((IT - p.template used<PACKED>()) * 8), at = i % ((IT - p.template used<PACKED>()) * 8);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sQ + sub * W::kInSub + p.template used<PACKED>() * 128 + at * 16), "r"(0) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     if (warp == 1) tmem_alloc(smem_u32(tmem_slot), W::kCols);
     tc_fence_before();
     __syncthreads();
@@ -747,20 +773,27 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
         }
         uint32_t sq = 0, qph = 0;
         int h = g * G, qt = qt_begin;
+        const uint32_t bytes = (uint32_t)(p.template used<PACKED>() * DH * 2);
+        int col_row[IT / 32], col_head[IT / 32];
+#pragma unroll
+        for (int e = 0; e < IT / 32; e++) {
+            col_row[e] = (lane * (IT / 32) + e) / p.template heads<PACKED>();
+            col_head[e] = (lane * (IT / 32) + e) % p.template heads<PACKED>();
+        }
         for (int it = 0; it < iters; it++) {
-            const int qt0 = qt * IT;
+            const int qt0 = qt * p.template rows<PACKED>();
             const uint32_t sd = it & 1, dph = (it >> 1) & 1;
             int ok = 1;
             if (lane == 0) {
                 ok = mbar_wait(q_empty + 8 * sq, qph ^ 1u, abort_flag) ? 1 : 0;          // dK of the stage's last user
                 if (ok) {
-                    mbar_expect_tx(q_full + 8 * sq, T);
-                    load_tile<DH, W::kInSub>(sQ + sq * T, &map_q, q_full + 8 * sq, h, qt0);
+                    mbar_expect_tx(q_full + 8 * sq, bytes);
+                    load_rows<DH, W::kInSub>(sQ + sq * T, &map_q, q_full + 8 * sq, h, qt0);
                     ok = mbar_wait(do_empty + 8 * sd, dph ^ 1u, abort_flag) ? 1 : 0;     // dV of the stage's last user
                 }
                 if (ok) {
-                    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(do_full + 8 * sd), "r"(T) : "memory");
-                    load_tile<DH, W::kInSub>(sdO + sd * T, &map_do, do_full + 8 * sd, h, qt0);
+                    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(do_full + 8 * sd), "r"(bytes) : "memory");
+                    load_rows<DH, W::kInSub>(sdO + sd * T, &map_do, do_full + 8 * sd, h, qt0);
                     ok = mbar_wait(rows_empty + 8 * sd, dph ^ 1u, abort_flag) ? 1 : 0;   // delta rows: read until dS^T is packed
                 }
             }
@@ -768,14 +801,16 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             if (!ok) break;
 #pragma unroll
             for (int e = 0; e < IT / 32; e++) {
-                const int col = lane * (IT / 32) + e, r = qt0 + col;
-                s_lse[sd * IT + col] = r < p.w.n ? -p.lse[(long long)h * p.w.n + r] * kLog2e : 0.f;
-                s_delta[sd * IT + col] = r < p.w.n ? -p.delta[(long long)h * p.w.n + r] * p.scale : 0.f;
+                const int col = lane * (IT / 32) + e, r = qt0 + col_row[e];
+                const bool used = col < p.template used<PACKED>() && r < p.w.n;
+                const long long at = (long long)(h + col_head[e]) * p.w.n + r;
+                s_lse[sd * IT + col] = used ? -p.lse[at] * kLog2e : 0.f;
+                s_delta[sd * IT + col] = used ? -p.delta[at] * p.scale : 0.f;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(do_full + 8 * sd);   // publishes the rows; the phase completes when dO has landed too
             if (++sq == QS) { sq = 0; qph ^= 1u; }
-            if (++qt == qt_end) { qt = qt_begin; h++; }
+            if (++qt == qt_end) { qt = qt_begin; h += p.template heads<PACKED>(); }
         }
     } else if (warp == 1) {
         // the whole warp runs the issue loop; each MMA / commit executes in one elected lane
@@ -849,7 +884,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
         bool alive = true;
         int qt = qt_begin;
         for (int it = 0; it < iters && alive; it++) {
-            const int q_abs0 = p.w.q0 + qt * IT;
+            const int q_abs0 = p.w.q0 + qt * p.template rows<PACKED>();
             const uint32_t sd = it & 1;
             if (!mbar_wait(s_full, it & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
@@ -860,7 +895,7 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
             if (lane == 0) mbar_arrive(loaded);
             // the producer's lse / delta rows of this stage are published together with the dO tile
             if (!mbar_wait(do_full + 8 * sd, (it >> 1) & 1, abort_flag)) { alive = false; break; }
-            const uint32_t see = mixed(p.w, q_abs0, IT, k_abs0, TILE) ? visible_rows(p.w, k_abs, q_abs0, col_base) : 0xffffffffu;
+            const uint32_t see = p.template used<PACKED>() < IT || mixed(p.w, q_abs0, p.template rows<PACKED>(), k_abs0, TILE) ? visible_columns(p.w, k_abs, q_abs0, p.template heads<PACKED>(), p.template used<PACKED>(), col_base) : 0xffffffffu;
             if (!__any_sync(0xffffffffu, see != 0u)) {     // P and dS of all of the warp's pairs are zero
                 if (!mbar_wait(dp_full, it & 1, abort_flag)) { alive = false; break; }
                 tc_fence_after();
@@ -967,10 +1002,10 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
     }
 }
 
-template <int DH>
+template <int DH, bool PACKED>
 __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
                                         const CUtensorMap &map_do, const CUtensorMap &map_ke, const CUtensorMap &map_ve,
-                                        const CUtensorMap &map_dq, const BwdParams<DH> &p, uint8_t *smem_raw, int block_x, int h) {
+                                        const CUtensorMap &map_dq, const BwdParams<DH> &p, uint8_t *smem_raw, int block_x, int h0) {
     typedef Bwd<DH> W;
     constexpr int T = W::kIn, KS = W::kKStages, IT = W::IT;
     const uint32_t raw = smem_u32(smem_raw);
@@ -986,10 +1021,10 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
     volatile int *abort_flag = reinterpret_cast<volatile int *>(aux + 136);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int g = h / (p.w.Hq / p.w.Hkv);
-    const int qt0 = block_x * TILE;
+    const int g = h0 / (p.w.Hq / p.w.Hkv);
+    const int qt0 = block_x * p.template tokens<PACKED>();
     const int q_abs0 = p.w.q0 + qt0;
-    const int rows_here = (p.w.n - qt0) < TILE ? (p.w.n - qt0) : TILE;
+    const int rows_here = (p.w.n - qt0) < p.template tokens<PACKED>() ? (p.w.n - qt0) : p.template tokens<PACKED>();
     const KeySpan span = key_span<IT>(p.w, q_abs0, q_abs0 + rows_here - 1);
     const int nkv = span.count();
     auto keys_of = [&](int j) { return j < span.ns && j == p.edge ? p.edge_keys : IT; };
@@ -1027,9 +1062,9 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
         // nothing was issued: fall through to the common exit
     } else if (warp == 0) {
         if (lane == 0) {
-            mbar_expect_tx(q_full, 2 * W::kOut);
-            load_tile<DH>(sQ, &map_q, q_full, h, qt0);
-            load_tile<DH>(sdO, &map_do, q_full, h, qt0);
+            mbar_expect_tx(q_full, (uint32_t)(2 * p.template heads<PACKED>() * p.template tokens<PACKED>() * DH * 2));
+            load_rows<DH, SUB_BYTES>(sQ, &map_q, q_full, h0, qt0);
+            load_rows<DH, SUB_BYTES>(sdO, &map_do, q_full, h0, qt0);
             uint32_t ks = 0, kph = 0;
             for (int j = 0; j < nkv; j++) {
                 const int row = span.tile(j) * IT, keys = keys_of(j);
@@ -1098,18 +1133,20 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
         const int wg = (warp - 2) >> 2;                           // 32-key group of the tile
         const int key_base = wg * 32;
         const int row = quarter * 32 + lane;
-        const int qr = qt0 + row;
-        const int q_abs = q_abs0 + row;
+        const int token = row / p.template heads<PACKED>(), h = h0 + row % p.template heads<PACKED>();
+        const int qr = qt0 + token;
+        const int q_abs = q_abs0 + (token < p.template tokens<PACKED>() ? token : p.template tokens<PACKED>() - 1);    // rows that are none of the tile's see as its last
+        const bool used = token < p.template tokens<PACKED>() && qr < p.w.n;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t tS_g = tS + key_base + lane_base, tP_g = tDP + key_base + lane_base;
-        const float neg_lse2 = qr < p.w.n ? -p.lse[(long long)h * p.w.n + qr] * kLog2e : 0.f;
-        const float neg_delta_s = qr < p.w.n ? -p.delta[(long long)h * p.w.n + qr] * p.scale : 0.f;
+        const float neg_lse2 = used ? -p.lse[(long long)h * p.w.n + qr] * kLog2e : 0.f;
+        const float neg_delta_s = used ? -p.delta[(long long)h * p.w.n + qr] * p.scale : 0.f;
         bool alive = true;
         for (int j = 0; j < nkv && alive; j++) {
             const int k_abs0 = span.tile(j) * IT;
             if (!mbar_wait(s_full, j & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
-            const uint32_t see = mixed(p.w, q_abs0, TILE, k_abs0, IT) ? visible_keys(p.w, q_abs, k_abs0, key_base) : 0xffffffffu;
+            const uint32_t see = mixed(p.w, q_abs0, p.template tokens<PACKED>(), k_abs0, IT) ? visible_keys(p.w, q_abs, k_abs0, key_base) : 0xffffffffu;
             if (!__any_sync(0xffffffffu, see != 0u)) {     // dS of all of the warp's pairs is zero
                 __syncwarp();
                 if (lane == 0) mbar_arrive(s_free);
@@ -1158,11 +1195,16 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
             tc_fence_after();
             uint32_t r[32];
             tmem_ld32(tDQ + lane_base + key_base, r);
-            const int row0 = qt0 + quarter * 32;
-            if (row0 < p.w.n) {                               // the tiles are through with their products
-                put_block(&map_dq, base + (uint32_t)(warp - 2) * 4096u, r, lane, h * DH + key_base, row0,
-                          p.mode == GRAD_BF16_SET ? GRAD_BF16_SET : GRAD_F32_SET);
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            const int mode = p.mode == GRAD_BF16_SET ? GRAD_BF16_SET : GRAD_F32_SET;
+            if (32 % p.template heads<PACKED>() == 0) {                            // whole rows to a warp
+                const int row0 = qt0 + quarter * (32 / p.template heads<PACKED>());
+                if (row0 < p.w.n) {                           // the tiles are through with their products
+                    const uint32_t at = base + (uint32_t)(warp - 2) * 4096u;
+                    put_block(at, r, lane, mode, [&] { tma_store_3d(&map_dq, at, key_base, h0, row0); });
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+                }
+            } else if (used) {                                // few rows
+                put32(p.dq, ((long long)qr * p.w.Hq + h) * DH + key_base, r, mode);
             }
         }
     }
@@ -1177,7 +1219,7 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
     }
 }
 
-template <int DH>
+template <int DH, bool PACKED>
 __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
     attn_window_bwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                            const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
@@ -1194,10 +1236,10 @@ __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
     const bool dq_role = b < p.n_dq_first || b >= p.n_dq_first + p.n_dkdv;
     if (!dq_role) {
         const int c = b - p.n_dq_first;
-        dkdv_body<DH>(map_qi, map_k, map_v, map_doi, map_dk, map_dv, map_part, p, smem_raw, c / p.w.Hkv, c % p.w.Hkv);
+        dkdv_body<DH, PACKED>(map_qi, map_k, map_v, map_doi, map_dk, map_dv, map_part, p, smem_raw, c / p.w.Hkv, c % p.w.Hkv);
     } else {
-        const int c = b < p.n_dq_first ? b : b - p.n_dkdv, tiles = (p.w.n + TILE - 1) / TILE;
-        dq_body<DH>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, map_dq, p, smem_raw, tiles - 1 - c % tiles, c / tiles);
+        const int c = b < p.n_dq_first ? b : b - p.n_dkdv, tiles = (p.w.n + p.template tokens<PACKED>() - 1) / p.template tokens<PACKED>();
+        dq_body<DH, PACKED>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, map_dq, p, smem_raw, tiles - 1 - c % tiles, c / tiles * p.template heads<PACKED>());
     }
 }
 
@@ -1298,7 +1340,7 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
     p.items = (int)items;
     edge_of<KT>(w, 16, p.edge, p.edge_keys);
     CUtensorMap mq, mk, mv, ke, ve, mo;
-    if (!make_heads_map(&mq, q, w.n, w.Hq, DH, 64, (uint32_t)p.heads, (uint32_t)p.tokens) || !tile_map<DH>(&mk, k, kv, w.Hkv, KT) ||
+    if (!make_heads_map(&mq, q, w.n, w.Hq, DH, 64, (uint32_t)p.heads, (uint32_t)p.tokens, false) || !tile_map<DH>(&mk, k, kv, w.Hkv, KT) ||
         !tile_map<DH>(&mv, v, kv, w.Hkv, KT) || !tile_map<DH>(&ke, k, kv, w.Hkv, (uint32_t)p.edge_keys) ||
         !tile_map<DH>(&ve, v, kv, w.Hkv, (uint32_t)p.edge_keys))
         return STREAMBP_E_CUDA;
@@ -1324,7 +1366,7 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
         call_state().launches++;
         return cuda_ok(e) && cuda_ok(cudaGetLastError()) ? STREAMBP_OK : STREAMBP_E_CUDA;
     }
-    if (!make_heads_map(&mo, o, w.n, w.Hq, DH, 32, (uint32_t)p.heads, 32u / (uint32_t)p.heads, CU_TENSOR_MAP_SWIZZLE_64B)) return STREAMBP_E_CUDA;
+    if (!make_heads_map(&mo, o, w.n, w.Hq, DH, 32, (uint32_t)p.heads, 32u / (uint32_t)p.heads, false, CU_TENSOR_MAP_SWIZZLE_64B)) return STREAMBP_E_CUDA;
     static PerDevice configured;
     if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, false>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
     void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
@@ -1341,14 +1383,16 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     BwdParams<DH> p;
     memset(&p, 0, sizeof(p));
     p.w = w;
-    p.work = key_work<TILE, IT>(w, DH == 64 ? kBwdSlots64 : kBwdSlots128);
+    p.work = key_work<TILE>(w, IT, bwd_heads(w, IT), DH == 64 ? kBwdSlots64 : kBwdSlots128);
+    const uint32_t heads = (uint32_t)p.work.heads, tokens = TILE / heads;
     edge_of<IT>(w, 32, p.edge, p.edge_keys);
     const int64_t kv = (int64_t)w.q0 + w.n;
     const uint32_t edge = (uint32_t)p.edge_keys;
     CUtensorMap m[14];       // resident tiles of q, k, v, dO; inner tiles of the same; edge tiles of k, v; blocks of dq, dk, dv, part
-    if (!tile_map<DH>(&m[0], q, w.n, w.Hq, TILE) || !tile_map<DH>(&m[1], k, kv, w.Hkv, TILE) || !tile_map<DH>(&m[2], v, kv, w.Hkv, TILE) ||
-        !tile_map<DH>(&m[3], dout, w.n, w.Hq, TILE) || !tile_map<DH>(&m[4], q, w.n, w.Hq, IT) || !tile_map<DH>(&m[5], k, kv, w.Hkv, IT) ||
-        !tile_map<DH>(&m[6], v, kv, w.Hkv, IT) || !tile_map<DH>(&m[7], dout, w.n, w.Hq, IT) || !tile_map<DH>(&m[8], k, kv, w.Hkv, edge) ||
+    auto rows_map = [&](CUtensorMap *x, const bf16 *a, uint32_t rows) { return make_heads_map(x, a, w.n, w.Hq, DH, 64, heads, rows, false); };
+    if (!rows_map(&m[0], q, tokens) || !tile_map<DH>(&m[1], k, kv, w.Hkv, TILE) || !tile_map<DH>(&m[2], v, kv, w.Hkv, TILE) ||
+        !rows_map(&m[3], dout, tokens) || !rows_map(&m[4], q, (uint32_t)p.work.tq) || !tile_map<DH>(&m[5], k, kv, w.Hkv, IT) ||
+        !tile_map<DH>(&m[6], v, kv, w.Hkv, IT) || !rows_map(&m[7], dout, (uint32_t)p.work.tq) || !tile_map<DH>(&m[8], k, kv, w.Hkv, edge) ||
         !tile_map<DH>(&m[9], v, kv, w.Hkv, edge))
         return STREAMBP_E_CUDA;
     const bool f32 = mode != GRAD_BF16_SET;
@@ -1356,11 +1400,16 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     auto block_map = [&](CUtensorMap *x, void *g, int64_t rows, int heads) {
         return make_tensor_map(x, g, rows, (int64_t)heads * DH, (int64_t)heads * DH, 32, 32, f32, swizzle);
     };
-    if (!block_map(&m[10], dq, w.n, w.Hq) || !block_map(&m[11], dk, kv, w.Hkv) || !block_map(&m[12], dv, kv, w.Hkv)) return STREAMBP_E_CUDA;
+    if (!block_map(&m[11], dk, kv, w.Hkv) || !block_map(&m[12], dv, kv, w.Hkv)) return STREAMBP_E_CUDA;
+    m[10] = m[11];           // unused where a row's heads straddle warps
+    if (32 % heads == 0 && !make_heads_map(&m[10], dq, w.n, w.Hq, DH, 32, heads, 32 / heads, f32, swizzle)) return STREAMBP_E_CUDA;
     m[13] = m[12];
     if (p.work.full() && !make_tensor_map(&m[13], part, (int64_t)p.work.items() * w.Hkv * 2 * TILE, DH, DH, 32, 32, true)) return STREAMBP_E_CUDA;
-    static PerDevice configured;
-    if (!configured.get([] { return opt_in_smem(attn_window_bwd_kernel<DH>, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+    void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
+                   const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
+                   const CUtensorMap, const CUtensorMap, const BwdParams<DH>) = heads > 1 ? attn_window_bwd_kernel<DH, true> : attn_window_bwd_kernel<DH, false>;
+    static PerDevice configured[2];
+    if (!configured[heads > 1].get([&] { return opt_in_smem(kernel, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
     {
         const int64_t unseen16 = mode == GRAD_F32_ADD ? 0 : (int64_t)p.work.lo * TILE * w.Hkv * DH * (mode == GRAD_BF16_SET ? 2 : 4) / 16;
         const int64_t rows = (int64_t)w.n * w.Hq * (DH / 8), work = rows > unseen16 ? rows : unseen16;
@@ -1377,14 +1426,14 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     p.scale = scale;
     p.scale_log2 = scale * kLog2e;
     // The role with the longer walks is dispatched first (a dK/dV tile takes ~1.25x a dQ tile: four products against three)
-    const int q_tiles = (w.n + TILE - 1) / TILE;
+    const int q_tiles = (w.n + (int)tokens - 1) / (int)tokens;
     const int64_t span = ((w.window < kv ? w.window : kv) + IT - 1) / IT + 1 + (w.sinks + IT - 1) / IT;
     const int64_t walk = p.work.wlen < p.work.q_tiles ? p.work.wlen : p.work.q_tiles;
-    const int64_t n_dkdv = (int64_t)p.work.items() * w.Hkv, n_dq = (int64_t)q_tiles * w.Hq;
+    const int64_t n_dkdv = (int64_t)p.work.items() * w.Hkv, n_dq = (int64_t)q_tiles * (w.Hq / p.work.heads);
     if (n_dkdv + n_dq > 0x7fffffff) return STREAMBP_E_SHAPE;
     p.n_dkdv = (int)n_dkdv;
-    p.n_dq_first = 4 * span > 5 * (w.Hq / w.Hkv) * walk ? (int)n_dq : 0;
-    SBP_LAUNCH(attn_window_bwd_kernel<DH>, (unsigned)(n_dkdv + n_dq), W::kThreads, W::kSmem, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6],
+    p.n_dq_first = 4 * span > 5 * (w.Hq / w.Hkv / p.work.heads) * walk ? (int)n_dq : 0;
+    SBP_LAUNCH(kernel, (unsigned)(n_dkdv + n_dq), W::kThreads, W::kSmem, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6],
                m[7], m[8], m[9], m[10], m[11], m[12], m[13], p);
     const auto &k_ = p.work;
     if (k_.segs > 1 || k_.wsegs > 1)

@@ -329,7 +329,7 @@ int bwd(const T *q, const T *k, const T *v, const T *o, const T *dout, const flo
     if (!configured.get([&] { return set_smem(window_dkdv_kernel<T, DH>, smem) && set_smem(window_dq_kernel<T, DH>, smem) ? 1 : 0; }))
         return STREAMBP_E_CUDA;
     const int64_t rows = (int64_t)w.n * w.Hq;
-    const KeyWork<TILE> work = key_work<TILE>(w, 0);
+    const KeyWork<TILE> work = key_work<TILE>(w, TILE, 1, 0);
     const int64_t unseen16 = mode == GRAD_F32_ADD ? 0 : (int64_t)work.lo * TILE * w.Hkv * DH * (mode == GRAD_BF16_SET ? 2 : 4) / 16;
     SBP_LAUNCH(window_delta_any_kernel<T>, (unsigned)((rows * 32 + 255) / 256), 256, 0, st, o, dout, w.n, w.Hq, DH, delta, hdr, dk, dv,
                unseen16);

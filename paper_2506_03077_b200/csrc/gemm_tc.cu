@@ -95,16 +95,16 @@ bool make_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t c
     return true;
 }
 
-// 3-D map over bf16 [rows, heads, dim] without gaps: boxes of `box_rows` rows of `box_heads` heads.
+// 3-D map over [rows, heads, dim] without gaps: boxes of `box_rows` rows of `box_heads` heads.
 bool make_heads_map(CUtensorMap *map, const void *base, int64_t rows, int64_t heads, int64_t dim, uint32_t box_cols,
-                    uint32_t box_heads, uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+                    uint32_t box_heads, uint32_t box_rows, bool f32, CUtensorMapSwizzle swizzle) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)rows};
-    const cuuint64_t strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)(heads * dim) * 2};
+    const cuuint64_t strides[2] = {(cuuint64_t)dim * (f32 ? 4 : 2), (cuuint64_t)(heads * dim) * (f32 ? 4 : 2)};
     const cuuint32_t box[3] = {box_cols, box_heads, box_rows};
     const cuuint32_t estr[3] = {1, 1, 1};
-    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
+    const CUresult r = fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {

@@ -375,7 +375,7 @@ __device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t cols)
 bool make_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, uint32_t box_cols,
                      uint32_t box_rows, bool f32, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B);
 bool make_heads_map(CUtensorMap *map, const void *base, int64_t rows, int64_t heads, int64_t dim, uint32_t box_cols,
-                    uint32_t box_heads, uint32_t box_rows, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B);
+                    uint32_t box_heads, uint32_t box_rows, bool f32, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B);
 bool tensor_maps_available();
 int sm_count();
 

@@ -39,7 +39,7 @@ SBP_HD KeySpan key_span(const WindowShape &w, int first, int last) {
     return s;
 }
 
-// The work of the key-tile owners (dK, dV): key tiles of TK keys against query tiles of TQ rows.  Tiles below `lo` hold
+// The work of the key-tile owners (dK, dV): key tiles of TK keys against query tiles of `tq` rows (of `heads` heads each).  Tiles below `lo` hold
 // sinks only, or nothing that a query of the chunk sees.
 //   sink tiles 0 .. st - 1 : every later query adds to them; their query tiles are cut into `segs` segments of `len` tiles
 //   window tiles wt0 .. kv_tiles - 1 : over the query tiles the window reaches, cut into `wsegs` segments of `wlen`
@@ -47,8 +47,8 @@ SBP_HD KeySpan key_span(const WindowShape &w, int first, int last) {
 // segments.  wsegs > 1 (a short chunk: few owners, each with a long walk over its group's heads): all rows of every tile go
 // through the workspace (`full`).  Else a sink tile's first segment covers every query that sees a key of the tile
 // through the window, and only the sinks' rows do.
-template <int TK, int TQ = TK> struct KeyWork {
-    int kv_tiles, q_tiles, lo, st, segs, len, wt0, wsegs, wlen;
+template <int TK> struct KeyWork {
+    int tq, heads, kv_tiles, q_tiles, lo, st, segs, len, wt0, wsegs, wlen;
     SBP_HD int items() const { return st * segs + (kv_tiles - wt0) * wsegs; }
     SBP_HD bool full() const { return wsegs > 1; }
     // item -> key tile, query tiles [begin, end), segment (-1: the item writes its result itself)
@@ -59,16 +59,16 @@ template <int TK, int TQ = TK> struct KeyWork {
         const int s = j % n;
         // the last query that sees the tile's last key: any for a sink, else through the window
         const long long last = (long long)kt * TK + TK - 1 + w.window - 1 - w.q0;
-        const int all = sink ? q_tiles : (last < 0 ? 0 : (last / TQ + 1 < q_tiles ? (int)(last / TQ) + 1 : q_tiles));
+        const int all = sink ? q_tiles : (last < 0 ? 0 : (last / tq + 1 < q_tiles ? (int)(last / tq) + 1 : q_tiles));
         begin = first(w, kt) + s * step;
         end = n == 1 || begin + step > all ? all : begin + step;
         if (end < begin) end = begin;
         seg = n > 1 ? s : -1;
     }
     // first query tile that holds a row at or behind the tile's first key
-    SBP_HD static int first(const WindowShape &w, int kt) {
+    SBP_HD int first(const WindowShape &w, int kt) const {
         const long long k0 = (long long)kt * TK;
-        return k0 > w.q0 ? (int)((k0 - w.q0) / TQ) : 0;
+        return k0 > w.q0 ? (int)((k0 - w.q0) / tq) : 0;
     }
     // rows of tile kt whose sums go through the workspace where its work is cut, and the rows of a workspace slot
     SBP_HD int joined_rows(const WindowShape &w, int kt) const {
@@ -82,12 +82,15 @@ template <int TK, int TQ = TK> struct KeyWork {
         return (size_t)(full() ? items() : st * segs) * w.Hkv * 2 * slot_rows(w) * dh;
     }
 };
+// Inner tiles hold `it` rows: it / heads query rows of `heads` heads of a group, or `it` keys of the dQ role's walk.
 // `slots`: CTAs of the kernel that the 148 SMs hold at a time (0: windows are not cut).  A function of the sizes alone, so
 // that workspace queries need no GPU and the order of the sums is the same everywhere.
-template <int TK, int TQ = TK>
-inline KeyWork<TK, TQ> key_work(const WindowShape &w, int slots) {
-    KeyWork<TK, TQ> k;
-    const int kv = w.q0 + w.n, G = w.Hq / w.Hkv;
+template <int TK>
+inline KeyWork<TK> key_work(const WindowShape &w, int it, int heads, int slots) {
+    KeyWork<TK> k;
+    const int kv = w.q0 + w.n, turns = w.Hq / w.Hkv / heads, TQ = it / heads;
+    k.tq = TQ;
+    k.heads = heads;
     k.kv_tiles = (kv + TK - 1) / TK;
     k.q_tiles = (w.n + TQ - 1) / TQ;
     const int from = w.q0 - w.window + 1;
@@ -101,18 +104,18 @@ inline KeyWork<TK, TQ> key_work(const WindowShape &w, int slots) {
     k.wsegs = 1;
     k.wlen = k.len;
     if (slots > 0) {
-        // costs in units of a quarter of a dQ tile of the same launch (TQ keys; a dK/dV one takes ~1.25x: four products
+        // costs in units of a quarter of a dQ tile of the same launch (`it` keys; a dK/dV one takes ~1.25x: four products
         // against three): what a slot has to do on average, and the longest owner's walk
-        const long long span = ((w.window < kv ? w.window : kv) + TQ - 1) / TQ + 1 + (w.sinks + TQ - 1) / TQ;
-        const long long owners = (long long)(k.kv_tiles - k.wt0 + k.st) * w.Hkv, longest = 5ll * G * walk;
-        const long long each = (owners * longest + 4 * span * ((w.n + 127) / 128) * w.Hq) / slots;
+        const long long span = ((w.window < kv ? w.window : kv) + it - 1) / it + 1 + (w.sinks + it - 1) / it;
+        const long long owners = (long long)(k.kv_tiles - k.wt0 + k.st) * w.Hkv, longest = 5ll * turns * walk;
+        const long long each = (owners * longest + 4 * span * ((w.n + 128 / heads - 1) / (128 / heads)) * (w.Hq / heads)) / slots;
         // cut while the longest owner has more to do than a slot has on average (2000 rows, 16 heads to one key head, 128:
         // 381 us uncut, 82 us; 4000 rows at heads of 64, window 300: 176 and 74), unless the owners are many already
         while (k.wsegs < 16 && 2 * k.wsegs <= walk && longest > each * k.wsegs && owners * k.wsegs <= 2 * slots) k.wsegs *= 2;
         k.wlen = (walk + k.wsegs - 1) / k.wsegs;
     }
     if (k.full()) k.len = k.wlen;
-    else if (k.len < 8) k.len = 8;
+    else if (k.len < 8 * heads) k.len = 8 * heads;
     k.segs = k.st > 0 ? (k.q_tiles + k.len - 1) / k.len : 1;
     // no more owners of sink tiles than four for each of 148 SMs: that many keep the GPU busy, and they bound the workspace
     // (many sinks need no segments at all)
@@ -124,10 +127,28 @@ inline KeyWork<TK, TQ> key_work(const WindowShape &w, int slots) {
     if (k.segs < 1) k.segs = 1;
     return k;
 }
-// query rows to a tile of the tensor-core backward's key-tile owners, by head_dim
+// rows of an inner tile of the tensor-core backward, by head_dim
 constexpr int kBwdRows64 = 64, kBwdRows128 = 128;
 // its CTAs on 148 SMs
 constexpr int kBwdSlots64 = 296, kBwdSlots128 = 148;
+
+// Heads of a group that share the rows of a tile: the fewer query rows a tile has, the fewer key tiles it spans.  As many as
+// divide up into whole rows of 32, or for few rows, that one tile holds, all that it holds; but one where that saves less
+// than a fifth of the (query tile, key tile) pairs: the rows' bookkeeping costs more then (8191 rows, window 512, heads of
+// 64, 4 to a group: 223 us with one, 226 with 4; 180 rows behind 900, window 300, heads of 128: 28.3 and 21.8; 30 rows, 16
+// heads to a group: 19 and 9.4).
+inline int bwd_heads(const WindowShape &w, int it) {
+    const int G = w.Hq / w.Hkv, kv = w.q0 + w.n;
+    int p = 1;
+    while (p < 32 && G % (2 * p) == 0) p *= 2;
+    for (int d = p + 1; d <= G && d <= it; d++)
+        if (G % d == 0 && w.n <= it / d) p = d;
+    auto pairs = [&](int heads) {            // in keys, the partly used tiles at the ends of a span counted half
+        const long long rows = 128 / heads;
+        return ((w.n + rows - 1) / rows) * (G / heads) * ((w.window < kv ? w.window : kv) + rows + it / 2);
+    };
+    return 5 * pairs(p) <= 4 * pairs(1) ? p : 1;
+}
 
 // Where gradients go: fp32 added to or overwritten, or bf16 overwritten.
 enum GradMode { GRAD_F32_ADD = 0, GRAD_F32_SET = 1, GRAD_BF16_SET = 2 };
