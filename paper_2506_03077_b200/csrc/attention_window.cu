@@ -26,7 +26,9 @@
 //   dK/dV: one CTA per (key tile, KV head) loops over the query heads of the group and the query tiles that see the tile;
 //          a sink tile, which every later query sees, and all tiles where there are few, are cut into segments of query
 //          tiles whose fp32 sums meet in the workspace and are joined in order by window_join_kernel
-//   dQ   : one CTA per (query tile, head) loops over the key tiles of its span
+//   dQ   : one CTA per (query tile, head) loops over the key tiles of its span; few of them: a cluster to each, which shares
+//          the key tiles and adds the sums in order
+// A tile's rows are those of one head, or of several of a group where that saves tile pairs (bwd_heads; PACKED kernels).
 // Softmax work is split in time (P for dV first, then dS), packed operands stay in tensor memory, every product is a full
 // tile; gradients leave through blocks of shared memory and TMA stores or adds, fp32 sums rounded once.
 // What bounds it: one iteration's chain of products and exponentials, ~2900 (dK/dV) and ~2500 cycles (dQ) for 128 x 128
@@ -622,6 +624,7 @@ struct BwdParams {
     int part_rows;
     int mode;             // GradMode of dk, dv (dq: fp32 or bf16, always overwritten)
     int edge, edge_keys;  // dQ role: the sink tile that holds sinks in its first rows only (-1: none), those rows rounded up to 32
+    int split;                      // PACKED: CTAs that share a dQ item's key tiles, a cluster (1: none)
     int n_dkdv, n_dq_first;         // dK/dV CTAs; dQ CTAs that are dispatched before them (all or none)
     float scale, scale_log2;
     // PACKED: several heads of a group share a tile.  Heads of a query row, query rows of an inner tile (dK/dV role), the rows
@@ -1026,8 +1029,11 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
     const int q_abs0 = p.w.q0 + qt0;
     const int rows_here = (p.w.n - qt0) < p.template tokens<PACKED>() ? (p.w.n - qt0) : p.template tokens<PACKED>();
     const KeySpan span = key_span<IT>(p.w, q_abs0, q_abs0 + rows_here - 1);
-    const int nkv = span.count();
-    auto keys_of = [&](int j) { return j < span.ns && j == p.edge ? p.edge_keys : IT; };
+    // the key tiles of this CTA: all of the span, or its share of them
+    const int count = span.count(), rank = PACKED && p.split > 1 ? (int)cluster_cta_rank() : 0;
+    const int j0 = PACKED ? (int)((long long)count * rank / p.split) : 0;
+    const int nkv = PACKED ? (int)((long long)count * (rank + 1) / p.split) - j0 : count;
+    auto keys_of = [&](int j) { return j0 + j < span.ns && j0 + j == p.edge ? p.edge_keys : IT; };
 
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
@@ -1061,13 +1067,13 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
     if (!usable) {
         // nothing was issued: fall through to the common exit
     } else if (warp == 0) {
-        if (lane == 0) {
+        if (lane == 0 && nkv > 0) {
             mbar_expect_tx(q_full, (uint32_t)(2 * p.template heads<PACKED>() * p.template tokens<PACKED>() * DH * 2));
             load_rows<DH, SUB_BYTES>(sQ, &map_q, q_full, h0, qt0);
             load_rows<DH, SUB_BYTES>(sdO, &map_do, q_full, h0, qt0);
             uint32_t ks = 0, kph = 0;
             for (int j = 0; j < nkv; j++) {
-                const int row = span.tile(j) * IT, keys = keys_of(j);
+                const int row = span.tile(j0 + j) * IT, keys = keys_of(j);
                 const uint32_t bytes = (uint32_t)keys * DH * 2u;
                 if (!mbar_wait(k_empty + 8 * ks, kph ^ 1u, abort_flag)) break;
                 mbar_expect_tx(k_full + 8 * ks, bytes);
@@ -1082,7 +1088,7 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
     } else if (warp == 1) {
         // the whole warp runs the issue loop; each MMA / commit executes in one elected lane
         constexpr uint32_t idesc_acc = make_idesc(TILE, DH, false, true);
-        bool alive = mbar_wait_warp(q_full, 0, abort_flag);
+        bool alive = nkv > 0 && mbar_wait_warp(q_full, 0, abort_flag);
         const uint32_t q_lo = klo(sQ), do_lo = klo(sdO);
         // K stage and phase of the tile whose S is issued next / whose dQ is issued next
         uint32_t ks_s = 0, kph_s = 0, ks_q = 0;
@@ -1143,7 +1149,7 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
         const float neg_delta_s = used ? -p.delta[(long long)h * p.w.n + qr] * p.scale : 0.f;
         bool alive = true;
         for (int j = 0; j < nkv && alive; j++) {
-            const int k_abs0 = span.tile(j) * IT;
+            const int k_abs0 = span.tile(j0 + j) * IT;
             if (!mbar_wait(s_full, j & 1, abort_flag)) { alive = false; break; }
             tc_fence_after();
             const uint32_t see = mixed(p.w, q_abs0, p.template tokens<PACKED>(), k_abs0, IT) ? visible_keys(p.w, q_abs, k_abs0, key_base) : 0xffffffffu;
@@ -1191,12 +1197,18 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
                 if (lane == 0) mbar_arrive(p2_full);
             }
         }
-        if (alive && mbar_wait(acc_full, 0, abort_flag) && wg < DH / 32) {
+        if (alive && nkv > 0 && mbar_wait(acc_full, 0, abort_flag) && wg < DH / 32) {
             tc_fence_after();
             uint32_t r[32];
             tmem_ld32(tDQ + lane_base + key_base, r);
             const int mode = p.mode == GRAD_BF16_SET ? GRAD_BF16_SET : GRAD_F32_SET;
-            if (32 % p.template heads<PACKED>() == 0) {                            // whole rows to a warp
+            if (PACKED && p.split > 1) {                      // this CTA's sum, 16-byte groups of eight rows on different banks
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                 ::"r"(sK + (uint32_t)(row * DH * 4 + (((wg * 8 + e) ^ (row & 7)) << 4))), "r"(r[4 * e]), "r"(r[4 * e + 1]),
+                                 "r"(r[4 * e + 2]), "r"(r[4 * e + 3]) : "memory");
+            } else if (32 % p.template heads<PACKED>() == 0) {                            // whole rows to a warp
                 const int row0 = qt0 + quarter * (32 / p.template heads<PACKED>());
                 if (row0 < p.w.n) {                           // the tiles are through with their products
                     const uint32_t at = base + (uint32_t)(warp - 2) * 4096u;
@@ -1209,6 +1221,33 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
         }
     }
 
+    if (PACKED && p.split > 1) {
+        __syncwarp();
+        cluster_sync_all();
+        if (!*abort_flag) {                                   // the sums of the CTAs in order, rows dealt to the warps of all
+            constexpr int NC = DH / 32, WARPS = W::kThreads / 32;
+            const int rows = rows_here * p.work.heads;
+            for (int r = rank * WARPS + warp; r < rows; r += p.split * WARPS) {
+                float acc[NC];
+#pragma unroll
+                for (int e = 0; e < NC; e++) acc[e] = 0.f;
+#pragma unroll
+                for (int c = 0; c < 8; c++) {
+                    if (c >= p.split || (long long)count * c / p.split == (long long)count * (c + 1) / p.split) continue;   // had none
+                    float x[NC];
+                    ld_cluster<NC>(map_to_cta(sK, (uint32_t)c) + (uint32_t)(r * DH * 4 + (((lane * NC >> 2) ^ (r & 7)) << 4) + (lane * NC & 3) * 4), x);
+#pragma unroll
+                    for (int e = 0; e < NC; e++) acc[e] += x[e];
+                }
+                const long long at = ((long long)(qt0 + r / p.work.heads) * p.w.Hq + h0 + r % p.work.heads) * DH + lane * NC;
+#pragma unroll
+                for (int e = 0; e < NC; e += 2) {
+                    if (p.mode == GRAD_BF16_SET) *reinterpret_cast<uint32_t *>(static_cast<bf16 *>(p.dq) + at + e) = pack_bf16(acc[e], acc[e + 1]);
+                    else *reinterpret_cast<float2 *>(static_cast<float *>(p.dq) + at + e) = make_float2(acc[e], acc[e + 1]);
+                }
+            }
+        }
+    }
     __syncwarp();
     leave(abort_flag);
     tc_fence_before();
@@ -1216,6 +1255,10 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, W::kCols);
+    }
+    if (PACKED && p.split > 1) {
+        __syncwarp();
+        cluster_sync_all();                                   // no CTA leaves while another may read its sums
     }
 }
 
@@ -1231,14 +1274,22 @@ __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
                            const __grid_constant__ BwdParams<DH> p) {
     pdl_enter();
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    // dispatch order: n_dq_first dQ CTAs (all of them or none), then the dK/dV CTAs, then the rest
+    // dispatch order: n_dq_first dQ CTAs (all of them or none), then the dK/dV CTAs, then the rest.  Where clusters share a dQ
+    // item: the dQ CTAs, then the dK/dV CTAs, and as many more as fill the last cluster
     const int b = (int)blockIdx.x;
-    const bool dq_role = b < p.n_dq_first || b >= p.n_dq_first + p.n_dkdv;
+    const bool dq_role = b < p.n_dq_first || b >= p.n_dq_first + p.n_dkdv && !(PACKED && p.split > 1);
     if (!dq_role) {
         const int c = b - p.n_dq_first;
-        dkdv_body<DH, PACKED>(map_qi, map_k, map_v, map_doi, map_dk, map_dv, map_part, p, smem_raw, c / p.w.Hkv, c % p.w.Hkv);
+        if (!PACKED || c < p.n_dkdv)
+            dkdv_body<DH, PACKED>(map_qi, map_k, map_v, map_doi, map_dk, map_dv, map_part, p, smem_raw, c / p.w.Hkv, c % p.w.Hkv);
+        if (PACKED && p.split > 1) {                          // the two barriers of a cluster whose last CTAs have the dQ role
+            __syncwarp();
+            cluster_sync_all();
+            cluster_sync_all();
+        }
     } else {
-        const int c = b < p.n_dq_first ? b : b - p.n_dkdv, tiles = (p.w.n + p.template tokens<PACKED>() - 1) / p.template tokens<PACKED>();
+        const int i = b < p.n_dq_first ? b : b - p.n_dkdv, tiles = (p.w.n + p.template tokens<PACKED>() - 1) / p.template tokens<PACKED>();
+        const int c = PACKED ? i / p.split : i;
         dq_body<DH, PACKED>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, map_dq, p, smem_raw, tiles - 1 - c % tiles, c / tiles * p.template heads<PACKED>());
     }
 }
@@ -1276,6 +1327,29 @@ __global__ void __launch_bounds__(256) window_delta_kernel(const bf16 *o, const 
 template <typename K>
 bool opt_in_smem(K kernel, int bytes) {
     return cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+}
+
+// A launch of clusters of `size` CTAs.
+template <typename... Args>
+int launch_clusters(void (*kernel)(Args...), unsigned ctas, int threads, int smem, int size, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    memset(attr, 0, sizeof(attr));
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)size;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    call_state().launches++;
+    return cuda_ok(e) && cuda_ok(cudaGetLastError()) ? STREAMBP_OK : STREAMBP_E_CUDA;
 }
 
 // [rows, heads, DH] as tiles of `box` rows and 64 columns
@@ -1347,24 +1421,8 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
     if (p.split > 1) {
         static PerDevice configured;
         if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, true>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
-        cudaLaunchConfig_t cfg;
-        memset(&cfg, 0, sizeof(cfg));
-        cfg.gridDim = dim3((unsigned)(p.items * p.split));
-        cfg.blockDim = dim3(F::kThreads);
-        cfg.dynamicSmemBytes = F::kSmem;
-        cfg.stream = st;
-        cudaLaunchAttribute attr[2];
-        memset(attr, 0, sizeof(attr));
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = (unsigned)p.split;
-        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 2;
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, attn_window_fwd_kernel<DH, true>, mq, mk, mv, ke, ve, mk, p);
-        call_state().launches++;
-        return cuda_ok(e) && cuda_ok(cudaGetLastError()) ? STREAMBP_OK : STREAMBP_E_CUDA;
+        return launch_clusters(attn_window_fwd_kernel<DH, true>, (unsigned)(p.items * p.split), F::kThreads, F::kSmem, p.split, st, mq, mk, mv,
+                               ke, ve, mk, p);
     }
     if (!make_heads_map(&mo, o, w.n, w.Hq, DH, 32, (uint32_t)p.heads, 32u / (uint32_t)p.heads, false, CU_TENSOR_MAP_SWIZZLE_64B)) return STREAMBP_E_CUDA;
     static PerDevice configured;
@@ -1405,11 +1463,6 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     if (32 % heads == 0 && !make_heads_map(&m[10], dq, w.n, w.Hq, DH, 32, heads, 32 / heads, f32, swizzle)) return STREAMBP_E_CUDA;
     m[13] = m[12];
     if (p.work.full() && !make_tensor_map(&m[13], part, (int64_t)p.work.items() * w.Hkv * 2 * TILE, DH, DH, 32, 32, true)) return STREAMBP_E_CUDA;
-    void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
-                   const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
-                   const CUtensorMap, const CUtensorMap, const BwdParams<DH>) = heads > 1 ? attn_window_bwd_kernel<DH, true> : attn_window_bwd_kernel<DH, false>;
-    static PerDevice configured[2];
-    if (!configured[heads > 1].get([&] { return opt_in_smem(kernel, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
     {
         const int64_t unseen16 = mode == GRAD_F32_ADD ? 0 : (int64_t)p.work.lo * TILE * w.Hkv * DH * (mode == GRAD_BF16_SET ? 2 : 4) / 16;
         const int64_t rows = (int64_t)w.n * w.Hq * (DH / 8), work = rows > unseen16 ? rows : unseen16;
@@ -1430,11 +1483,35 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     const int64_t span = ((w.window < kv ? w.window : kv) + IT - 1) / IT + 1 + (w.sinks + IT - 1) / IT;
     const int64_t walk = p.work.wlen < p.work.q_tiles ? p.work.wlen : p.work.q_tiles;
     const int64_t n_dkdv = (int64_t)p.work.items() * w.Hkv, n_dq = (int64_t)q_tiles * (w.Hq / p.work.heads);
-    if (n_dkdv + n_dq > 0x7fffffff) return STREAMBP_E_SHAPE;
+    if (n_dkdv + n_dq > 0x7fffffff / 8) return STREAMBP_E_SHAPE;
+    // Few dQ items: clusters that share their key tiles, on the SMs that the dK/dV CTAs leave free or on a quarter of them.  Joining
+    // costs as much as two iterations, and one for each 16 rows; what is gained ends where the dK/dV walks do (28:4 heads of 128, window 1024, 5 rows: 20.1 us with one
+    // CTA an item, 14.0; 20 rows of 16:1 heads of 64, window 4000: 62 and 22).
+    const int64_t count = key_span<IT>(w, w.q0 + (q_tiles - 1) * (int)tokens, w.q0 + w.n - 1).count(), slots = W::kBlocks * sm_count();
+    const int64_t joined = (w.n < (int)tokens ? w.n : (int)tokens) * p.work.heads;
+    const int64_t room = slots - n_dkdv > slots / 4 ? slots - n_dkdv : slots / 4;
+    int64_t split = room / n_dq < 8 ? room / n_dq : 8;
+    if (split > count) split = count;
+    const int64_t other = 5 * (w.Hq / w.Hkv / p.work.heads) * walk / 4;
+    const int64_t left = split > 1 && (count + split - 1) / split > other ? (count + split - 1) / split : other;
+    p.split = split > 1 && count - left > 2 + joined / 16 ? (int)split : 1;
     p.n_dkdv = (int)n_dkdv;
-    p.n_dq_first = 4 * span > 5 * (w.Hq / w.Hkv / p.work.heads) * walk ? (int)n_dq : 0;
-    SBP_LAUNCH(kernel, (unsigned)(n_dkdv + n_dq), W::kThreads, W::kSmem, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6],
-               m[7], m[8], m[9], m[10], m[11], m[12], m[13], p);
+    p.n_dq_first = p.split > 1 ? (int)n_dq * p.split : 4 * span > 5 * (w.Hq / w.Hkv / p.work.heads) * walk ? (int)n_dq : 0;
+    const bool packed = heads > 1 || p.split > 1;
+    void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
+                   const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
+                   const CUtensorMap, const CUtensorMap, const BwdParams<DH>) = packed ? attn_window_bwd_kernel<DH, true> : attn_window_bwd_kernel<DH, false>;
+    static PerDevice configured[2];
+    if (!configured[packed].get([&] { return opt_in_smem(kernel, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+    if (p.split > 1) {
+        const int64_t ctas = (n_dkdv + n_dq * p.split + p.split - 1) / p.split * p.split;
+        const int st_ = launch_clusters(kernel, (unsigned)ctas, W::kThreads, W::kSmem, p.split, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7],
+                                        m[8], m[9], m[10], m[11], m[12], m[13], p);
+        if (st_ != STREAMBP_OK) return st_;
+    } else {
+        SBP_LAUNCH(kernel, (unsigned)(n_dkdv + n_dq), W::kThreads, W::kSmem, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7], m[8], m[9],
+                   m[10], m[11], m[12], m[13], p);
+    }
     const auto &k_ = p.work;
     if (k_.segs > 1 || k_.wsegs > 1)
         return attention_window_join(part, TILE, k_.st, k_.segs, k_.wt0, k_.wsegs, p.part_rows, w, DH, mode, dk, dv, st);

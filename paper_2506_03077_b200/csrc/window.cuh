@@ -110,8 +110,9 @@ inline KeyWork<TK> key_work(const WindowShape &w, int it, int heads, int slots) 
         const long long owners = (long long)(k.kv_tiles - k.wt0 + k.st) * w.Hkv, longest = 5ll * turns * walk;
         const long long each = (owners * longest + 4 * span * ((w.n + 128 / heads - 1) / (128 / heads)) * (w.Hq / heads)) / slots;
         // cut while the longest owner has more to do than a slot has on average (2000 rows, 16 heads to one key head, 128:
-        // 381 us uncut, 82 us; 4000 rows at heads of 64, window 300: 176 and 74), unless the owners are many already
-        while (k.wsegs < 16 && 2 * k.wsegs <= walk && longest > each * k.wsegs && owners * k.wsegs <= 2 * slots) k.wsegs *= 2;
+        // 381 us uncut, 82 us; 4000 rows at heads of 64, window 300: 176 and 74), unless the owners are many already or the
+        // walk is too short to pay for the join (3 us, or two to three iterations)
+        while (k.wsegs < 16 && 2 * k.wsegs <= walk && (k.wsegs > 1 || turns * walk > 4) && longest > each * k.wsegs && owners * k.wsegs <= 2 * slots) k.wsegs *= 2;
         k.wlen = (walk + k.wsegs - 1) / k.wsegs;
     }
     if (k.full()) k.len = k.wlen;

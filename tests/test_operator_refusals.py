@@ -181,8 +181,8 @@ def test_key_work_covers_every_visible_pair_once():
     first segment of a sink tile."""
     import random
     rng = random.Random(0)
-    for _ in range(500):
-        TK, TQ = rng.choice(((4, 4), (8, 8), (8, 4), (16, 4)))
+    for _ in range(700):
+        TK, TQ = rng.choice(((4, 4), (8, 8), (8, 4), (16, 4), (16, 3), (8, 1)))
         n, q0 = rng.randrange(1, 120), rng.choice((0, rng.randrange(0, 80)))
         window, sinks = rng.randrange(1, 60), rng.choice((0, 1, 3, 5, 17, 40))
         kv = q0 + n
