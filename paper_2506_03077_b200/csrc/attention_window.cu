@@ -253,11 +253,6 @@ __device__ __forceinline__ bool softmax_tile(float scale_log2, uint32_t tS, uint
     return true;
 }
 
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
-    return v;
-}
 template <int N>
 __device__ __forceinline__ void ld_cluster(uint32_t addr, float (&v)[N]) {
     static_assert(N == 2 || N == 4, "8 or 16 bytes");
@@ -1329,29 +1324,6 @@ bool opt_in_smem(K kernel, int bytes) {
     return cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
 }
 
-// A launch of clusters of `size` CTAs.
-template <typename... Args>
-int launch_clusters(void (*kernel)(Args...), unsigned ctas, int threads, int smem, int size, cudaStream_t st, Args... args) {
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (size_t)smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    memset(attr, 0, sizeof(attr));
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)size;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
-    call_state().launches++;
-    return cuda_ok(e) && cuda_ok(cudaGetLastError()) ? STREAMBP_OK : STREAMBP_E_CUDA;
-}
-
 // [rows, heads, DH] as tiles of `box` rows and 64 columns
 template <int DH>
 bool tile_map(CUtensorMap *m, const bf16 *p, int64_t rows, int heads, uint32_t box) {
@@ -1421,7 +1393,7 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
     if (p.split > 1) {
         static PerDevice configured;
         if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, true>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
-        return launch_clusters(attn_window_fwd_kernel<DH, true>, (unsigned)(p.items * p.split), F::kThreads, F::kSmem, p.split, st, mq, mk, mv,
+        return launch_clusters(attn_window_fwd_kernel<DH, true>, dim3((unsigned)(p.items * p.split)), F::kThreads, F::kSmem, p.split, 1, st, mq, mk, mv,
                                ke, ve, mk, p);
     }
     if (!make_heads_map(&mo, o, w.n, w.Hq, DH, 32, (uint32_t)p.heads, 32u / (uint32_t)p.heads, false, CU_TENSOR_MAP_SWIZZLE_64B)) return STREAMBP_E_CUDA;
@@ -1505,7 +1477,7 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     if (!configured[packed].get([&] { return opt_in_smem(kernel, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
     if (p.split > 1) {
         const int64_t ctas = (n_dkdv + n_dq * p.split + p.split - 1) / p.split * p.split;
-        const int st_ = launch_clusters(kernel, (unsigned)ctas, W::kThreads, W::kSmem, p.split, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7],
+        const int st_ = launch_clusters(kernel, dim3((unsigned)ctas), W::kThreads, W::kSmem, p.split, 1, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7],
                                         m[8], m[9], m[10], m[11], m[12], m[13], p);
         if (st_ != STREAMBP_OK) return st_;
     } else {

@@ -3,8 +3,9 @@
 //
 // HBM-bound: dC and z are read once, dz is written once.  A block owns a strip of 64 columns (a 128-byte row segment in
 // bf16, eight threads of one 16-byte load each) and walks its rows 32 at a time, keeping the sums of its columns in
-// registers; a grid of (strips, row splits) fills the GPU, each split leaves its sums in `partials`, and a second small
-// kernel adds the splits in their order: no atomics, the same inputs give the same bits.  What bounds it: four rows in
+// registers; a grid of (strips, row splits) fills the GPU.  The splits of a strip, up to eight of them, are a cluster that adds
+// its sums in their order; more of them leave their sums in `partials`, which a second small kernel adds in the same order:
+// no atomics, the same inputs give the same bits.  What bounds it: four rows in
 // flight a thread as raw 16-byte words and four blocks an SM read at 4.2 - 4.7 TB/s (2048 x 14336 with GELU: 42 us for
 // 176 MB; 8192 x 4096 with SiLU: 43 us for 201 MB); unpacked as they arrive they cost twice the registers and half the blocks.
 #include <type_traits>
@@ -15,16 +16,40 @@
 namespace sbp {
 namespace {
 
-constexpr int kStrip = 64, kRowsAtOnce = 32;
+constexpr int kStrip = 64, kRowsAtOnce = 32, kClusterSplits = 8;
 
 // rows and strips of any alignment: a lane per column (consecutive addresses), four rows at a time, eight in flight
+// Where a block's sums of its 64 columns go (threads 0 .. 63): the workspace, or through the cluster to dbias.
+struct Sums {
+    float *partials;          // [splits][N]; null: no sums are wanted, or a cluster joins them
+    float *dbias;             // cluster
+    int accumulate;
+    WsHeader *hdr;
+};
+__device__ __forceinline__ void put_sums(const Sums &to, float s, int col, int N, float *joined) {
+    if (!to.dbias) {
+        if (threadIdx.x < kStrip && col < N) to.partials[(int64_t)blockIdx.y * N + col] = s;
+        return;
+    }
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) clear_status(to.hdr);
+    if (threadIdx.x < kStrip) joined[threadIdx.x] = s;
+    __syncthreads();
+    cluster_sync_all();
+    if (blockIdx.y == 0 && threadIdx.x < kStrip && col < N) {
+        float t = 0.f;
+        for (unsigned i = 0; i < gridDim.y; i++) t += ld_cluster_f32(map_to_cta(smem_u32(joined + threadIdx.x), i));
+        to.dbias[col] = to.accumulate ? to.dbias[col] + t : t;
+    }
+    cluster_sync_all();                       // no block leaves while another may read its sums
+}
+
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
     epilogue_bwd_any_kernel(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int N, int64_t rows_per_split, T *dZ,
-                            int64_t ldz, float *partials) {
+                            int64_t ldz, Sums to) {
     pdl_enter();
     constexpr bool FAST = sizeof(T) == 2;
-    __shared__ float s_sum[4][kStrip];
+    __shared__ float s_sum[4][kStrip], joined[kStrip];
     const int tc = threadIdx.x & 63, tr = threadIdx.x >> 6, col = blockIdx.x * kStrip + tc;
     const int64_t first = blockIdx.y * rows_per_split, end = first + rows_per_split < M ? first + rows_per_split : M;
     float sum = 0.f;
@@ -50,20 +75,19 @@ __global__ void __launch_bounds__(256)
             }
         }
     }
-    if (!partials) return;
+    if (!to.partials && !to.dbias) return;
     s_sum[tr][tc] = sum;
     __syncthreads();
-    if (threadIdx.x < kStrip && col < N)
-        partials[(int64_t)blockIdx.y * N + col] = (s_sum[0][tc] + s_sum[1][tc]) + (s_sum[2][tc] + s_sum[3][tc]);
+    put_sums(to, (s_sum[0][tc] + s_sum[1][tc]) + (s_sum[2][tc] + s_sum[3][tc]), col, N, joined);
 }
 
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256, 4)
     epilogue_bwd_kernel(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int N, int64_t rows_per_split, T *dZ,
-                        int64_t ldz, float *partials) {
+                        int64_t ldz, Sums to) {
     pdl_enter();
     constexpr bool FAST = sizeof(T) == 2;
-    __shared__ float s_sum[8][kStrip + 1];
+    __shared__ float s_sum[8][kStrip + 1], joined[kStrip];
     const int tc = threadIdx.x & 7, tr = threadIdx.x >> 3;
     const int col0 = blockIdx.x * kStrip + tc * 8;
     const int64_t first = blockIdx.y * rows_per_split, end = first + rows_per_split < M ? first + rows_per_split : M;
@@ -103,7 +127,7 @@ __global__ void __launch_bounds__(256, 4)
         for (; r + (kAhead - 1) * kRowsAtOnce < end; r += kAhead * kRowsAtOnce) some(r, std::integral_constant<int, kAhead>());
         for (; r < end; r += kRowsAtOnce) some(r, std::integral_constant<int, 1>());
     }
-    if (!partials) return;
+    if (!to.partials && !to.dbias) return;
     // the 32 row threads of a column: four of a warp by shuffles (lanes 8 apart), then the eight warps
 #pragma unroll
     for (int e = 0; e < 8; e++) {
@@ -116,12 +140,12 @@ __global__ void __launch_bounds__(256, 4)
     }
     __syncthreads();
     const int c = blockIdx.x * kStrip + threadIdx.x;
-    if (threadIdx.x < kStrip && c < N) {
-        float s = 0.f;
+    float s = 0.f;
+    if (threadIdx.x < kStrip) {
 #pragma unroll
         for (int w = 0; w < 8; w++) s += s_sum[w][threadIdx.x];
-        partials[(int64_t)blockIdx.y * N + c] = s;
     }
+    put_sums(to, s, c, N, joined);
 }
 
 __global__ void __launch_bounds__(256) epilogue_sum_kernel(const float *partials, int splits, int N, float *dbias, int accumulate, WsHeader *hdr) {
@@ -134,6 +158,10 @@ __global__ void __launch_bounds__(256) epilogue_sum_kernel(const float *partials
     dbias[c] = accumulate ? dbias[c] + s : s;
 }
 
+// One launch, the splits of a strip a cluster: where the second launch would cost more than blocks that wait for one another
+// do (333 x 2731: 8.3 -> 7.1 us, and 4 us less of the host's time; 1500 x 2000: 11.8 -> 8.5; 2048 x 14336: 43 -> 49, left).
+bool small_product(int64_t M, int64_t N) { return M <= 2048 && M * N <= (4 << 20); }
+
 template <typename T, int ACT>
 int launch(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int64_t N, T *dZ, int64_t ldz, float *dbias,
            bool accumulate, float *partials, WsHeader *hdr, cudaStream_t st) {
@@ -143,11 +171,16 @@ int launch(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int64
     const int splits = gemm_epilogue_splits(M, N);
     const int64_t per = (M + splits - 1) / splits;
     const dim3 grid((unsigned)((N + kStrip - 1) / kStrip), (unsigned)splits);
-    float *sums = dbias ? partials : nullptr;
-    if (N % 8 == 0 && rows16(dC, ldd) && rows16(ACT != STREAMBP_ACT_NONE ? pre : nullptr, ldp) && rows16(dZ, ldz))
-        SBP_LAUNCH((epilogue_bwd_kernel<T, ACT>), grid, 256, 0, st, dC, ldd, pre, ldp, M, (int)N, per, dZ, ldz, sums);
-    else
-        SBP_LAUNCH((epilogue_bwd_any_kernel<T, ACT>), grid, 256, 0, st, dC, ldd, pre, ldp, M, (int)N, per, dZ, ldz, sums);
+    const bool vec = N % 8 == 0 && rows16(dC, ldd) && rows16(ACT != STREAMBP_ACT_NONE ? pre : nullptr, ldp) && rows16(dZ, ldz);
+    void (*kernel)(const T *, int64_t, const T *, int64_t, int64_t, int, int64_t, T *, int64_t, Sums) =
+        vec ? epilogue_bwd_kernel<T, ACT> : epilogue_bwd_any_kernel<T, ACT>;
+    Sums to = {nullptr, nullptr, accumulate ? 1 : 0, hdr};
+    if (dbias && small_product(M, N)) {
+        to.dbias = dbias;
+        return launch_clusters(kernel, grid, 256, 0, 1, splits, st, dC, ldd, pre, ldp, M, (int)N, per, dZ, ldz, to);
+    }
+    if (dbias) to.partials = partials;
+    SBP_LAUNCH(kernel, grid, 256, 0, st, dC, ldd, pre, ldp, M, (int)N, per, dZ, ldz, to);
     if (dbias)
         SBP_LAUNCH(epilogue_sum_kernel, (unsigned)((N + 255) / 256), 256, 0, st, partials, splits, (int)N, dbias, accumulate ? 1 : 0, hdr);
     return STREAMBP_OK;
@@ -155,12 +188,14 @@ int launch(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int64
 
 }  // namespace
 
-// Row splits: about twelve blocks (three waves of four) for each of the 148 SMs, at least 32 rows each.  A function of the sizes alone, so that
-// the workspace query needs no GPU and the order of the sums is the same everywhere.
+// Row splits: about twelve blocks (three waves of four) for each of the 148 SMs, at least 32 rows each; small products no
+// more than a cluster holds.  A function of the sizes alone, so that the workspace query needs no GPU and the order of the
+// sums is the same everywhere.
 int gemm_epilogue_splits(int64_t M, int64_t N) {
     const int64_t strips = (N + kStrip - 1) / kStrip, rows = (M + kRowsAtOnce - 1) / kRowsAtOnce;
     int64_t s = (148 * 12 + strips - 1) / strips;
     if (s > rows) s = rows;
+    if (s > kClusterSplits && small_product(M, N)) s = kClusterSplits;
     return s < 1 ? 1 : (int)s;
 }
 

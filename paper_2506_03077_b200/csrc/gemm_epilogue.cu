@@ -298,12 +298,6 @@ template <int NP> struct Rows {                          // NP: rows of A per ti
     static_assert(kSmem <= 232448 && NP * 512 <= kStages * kStage, "stages hold the sums of a tile after the products");
 };
 
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
-    return v;
-}
-
 // grid (n tiles x S, m tiles), clusters of S along x: CTA `rank` of a cluster sums its share of the K blocks
 template <int ACT, int NP>
 __global__ void __launch_bounds__(R_THREADS, 1) gemm_act_rows_kernel(const __grid_constant__ EpiParams p, int S) {
@@ -449,24 +443,7 @@ int launch_rows(EpiParams p, const GemmEpilogue<bf16> &g, cudaStream_t st) {
     // as many CTAs to a cluster as the SMs allow, each with at least four K blocks to stream
     int S = 1;
     while (S < 8 && nt * mt * S * 2 <= sm_count() && p.nkb >= 8 * S) S *= 2;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3((unsigned)(nt * S), (unsigned)mt);
-    cfg.blockDim = dim3(R_THREADS);
-    cfg.dynamicSmemBytes = R::kSmem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    memset(attr, 0, sizeof(attr));
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)S;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = S > 1 ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, gemm_act_rows_kernel<ACT, NP>, p, S);
-    call_state().launches++;
-    return cuda_ok(e) && cuda_ok(cudaGetLastError()) ? STREAMBP_OK : STREAMBP_E_CUDA;
+    return launch_clusters(gemm_act_rows_kernel<ACT, NP>, dim3((unsigned)(nt * S), (unsigned)mt), R_THREADS, R::kSmem, S, 1, st, p, S);
 }
 
 // 32 x 32 blocks of a bf16 matrix, rows of 64 bytes swizzled in shared memory
