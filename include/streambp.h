@@ -418,8 +418,8 @@ int streambp_attention_backward(const void *q, const void *k, const void *v, con
  * (window >= 1 counts the row's own key; a window of q0 + n or more is the attention above).  Arguments, layouts, lse and
  * the chunk (rows q0 .. q0+n-1, keys 0 .. q0+n-1) as above; head_dim 64 or 128, both on tensor cores for bf16; q0 + n <= 2^30.
  * Only key tiles that some query sees are read, so a chunk costs what its window holds however long the prefix is; rows of
- * k and v that no query sees may hold anything.  Values that a query tile's key tiles do hold must be finite: a hidden key
- * has weight 0 there, and 0 times an infinity is NaN.
+ * k and v that no query of the call sees may hold anything.  Rows that some query sees must be finite: to another query of
+ * the same tile such a key has weight 0, and 0 times an infinity is NaN.
  *
  * Backward: lse and o are those of the forward call.  grad_dtype STREAMBP_F32: dq is overwritten, dk and dv [q0+n,
  * n_kv_heads, head_dim] are overwritten (accumulate = 0) or added to (1: the key-prefix accumulators of a streamed

@@ -112,6 +112,32 @@ __device__ __forceinline__ uint32_t pack_pair(f32x2 v) {
     return pack_bf16(a, b);
 }
 
+// Rows of K and V that no query of the chunk sees may hold anything, and 0 times that need not be 0.  They are the zeros that a
+// copy puts where its tensor ends: sinks are read from a tensor that ends with them (edge tile), the first tile of the windows
+// from one that begins with their first row (Gap).  Where one tile holds both the last sinks and the first row of the windows
+// (CLEAR kernels), the warp that issues its products overwrites the rows between them.
+struct Gap {
+    int tile, from;       // the first tile of the windows where no query sees its first rows (-1: none); the windows' first row
+};
+template <int T>
+Gap gap_of(const WindowShape &w, bool &clear) {
+    Gap g = {-1, w.seen_from()};
+    clear = false;
+    if (g.from <= w.sinks || g.from % T == 0) return g;          // nothing between the sinks and the windows; a whole tile
+    if (w.sinks > g.from / T * T) clear = true;
+    else g.tile = g.from / T;
+    return g;
+}
+template <int DH, int ROWS, int SUB>
+__device__ __forceinline__ void clear_unseen(const WindowShape &w, uint32_t tile, int k0, int lane) {
+    if (k0 >= w.seen_from() || k0 + ROWS <= w.sinks) return;
+    for (int r = lane; r < ROWS; r += 32)
+        if (w.unseen(k0 + r))
+            for (int e = 0; e < DH / 8; e++)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + (e >> 3) * SUB + r * 128 + (e & 7) * 16), "r"(0) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
 // bits [0, n) of 32, n clamped
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
 // Which of the keys k0 + base .. + 31 the query row sees, as bits.
@@ -151,6 +177,7 @@ struct FwdParams {
     int split;          // CTAs that share an item's key tiles, a cluster (SPLIT kernel)
     bf16 *o;            // SPLIT kernel
     int edge, edge_keys;// the sink tile that holds sinks in its first rows only (-1: none), and those rows rounded up to 16
+    Gap gap;
 };
 
 template <int DH> struct Fwd {
@@ -262,11 +289,12 @@ __device__ __forceinline__ void ld_cluster(uint32_t addr, float (&v)[N]) {
 
 // SPLIT: one item to a cluster, its key tiles dealt to the CTAs in order; each leaves O, the reference of its exponentials
 // and their sum in its shared memory, and the rows are joined from there, dealt to the warps of all.
-template <int DH, bool SPLIT>
+template <int DH, bool SPLIT, bool CLEAR>
 __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
     attn_window_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                            const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_ke,
-                           const __grid_constant__ CUtensorMap map_ve, const __grid_constant__ CUtensorMap map_o, const FwdParams p) {
+                           const __grid_constant__ CUtensorMap map_ve, const __grid_constant__ CUtensorMap map_kg,
+                           const __grid_constant__ CUtensorMap map_vg, const __grid_constant__ CUtensorMap map_o, const FwdParams p) {
     pdl_enter();
     typedef Fwd<DH> F;
     constexpr int N = F::kRing, NQ = F::kQRing, NS = F::kS;
@@ -351,19 +379,20 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
                     tma_load_3d(sQ + q.st * F::kQ + c * SUB_BYTES, &map_q, q_full + 8 * q.st, c * 64, t.h0, t.t0);
                 q.next<NQ>();
                 for (int j = t.begin; j < t.end; j++) {
-                    const int row = t.span.tile(j) * KT, keys = keys_of(t, j);
-                    const bool part = keys < KT;
+                    const int tile = t.span.tile(j), keys = keys_of(t, j);
+                    const bool part = j < t.span.ns && j == p.edge, gap = tile == p.gap.tile;
+                    const int row = tile * KT - (gap ? p.gap.from : 0);
                     const uint32_t bytes = (uint32_t)keys * DH * 2u;
                     if (!mbar_wait(k_empty + 8 * kv.st, kv.ph ^ 1u, abort_flag)) { alive = false; break; }
                     mbar_expect_tx(k_full + 8 * kv.st, bytes);
 #pragma unroll
                     for (int c = 0; c < DH / 64; c++)
-                        tma_load_2d(sK + kv.st * F::kKV + c * KSUB, part ? &map_ke : &map_k, k_full + 8 * kv.st, g * DH + c * 64, row);
+                        tma_load_2d(sK + kv.st * F::kKV + c * KSUB, part ? &map_ke : gap ? &map_kg : &map_k, k_full + 8 * kv.st, g * DH + c * 64, row);
                     if (!mbar_wait(v_empty + 8 * kv.st, kv.ph ^ 1u, abort_flag)) { alive = false; break; }
                     mbar_expect_tx(v_full + 8 * kv.st, bytes);
 #pragma unroll
                     for (int c = 0; c < DH / 64; c++)
-                        tma_load_2d(sV + kv.st * F::kKV + c * KSUB, part ? &map_ve : &map_v, v_full + 8 * kv.st, g * DH + c * 64, row);
+                        tma_load_2d(sV + kv.st * F::kKV + c * KSUB, part ? &map_ve : gap ? &map_vg : &map_v, v_full + 8 * kv.st, g * DH + c * 64, row);
                     kv.next<N>();
                 }
             }
@@ -406,7 +435,9 @@ __global__ void __launch_bounds__(Fwd<DH>::kThreads, 2)
         for (int s = 0; s < NS && alive; s++) alive = issue_s();
         while (alive && is_item(ip)) {
             // O += P V once P is stored; the S tile that P lay in then takes the scores NS tiles further on
-            if (!mbar_wait_warp(v_full + 8 * v.st, v.ph, abort_flag) || !mbar_wait_warp(p_full + 8 * bp.st, bp.ph, abort_flag)) break;
+            if (!mbar_wait_warp(v_full + 8 * v.st, v.ph, abort_flag)) break;
+            if (CLEAR) clear_unseen<DH, KT, KSUB>(p.w, sV + v.st * F::kKV, tp.span.tile(jp) * KT, lane);
+            if (!mbar_wait_warp(p_full + 8 * bp.st, bp.ph, abort_flag)) break;
             tc_fence_after();
             const uint32_t v_lo = desc_lo(sV + v.st * F::kKV, KSUB), a = tmem + DH + bp.st * KT;
             const int slices = keys_of(tp, jp) / 16;
@@ -618,6 +649,7 @@ struct BwdParams {
     float *part;          // sums of segments: [item][Hkv][dK, dV][part_rows][DH]
     int part_rows;
     int mode;             // GradMode of dk, dv (dq: fp32 or bf16, always overwritten)
+    Gap gap;              // dQ role, like
     int edge, edge_keys;  // dQ role: the sink tile that holds sinks in its first rows only (-1: none), those rows rounded up to 32
     int split;                      // PACKED: CTAs that share a dQ item's key tiles, a cluster (1: none)
     int n_dkdv, n_dq_first;         // dK/dV CTAs; dQ CTAs that are dispatched before them (all or none)
@@ -965,6 +997,10 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
 #pragma unroll
             for (int e = 0; e < 32; e++) rv[e] = rk[e] = 0u;
         }
+        if (p.w.unseen(k_abs0 + row)) {                   // a row of its own, whatever K and V hold there
+#pragma unroll
+            for (int e = 0; e < 32; e++) rv[e] = rk[e] = 0u;
+        }
         if (seg < 0) {                                    // the tiles are through with their products: room for two blocks a warp
             const uint32_t at = base + (uint32_t)(warp - 2) * 8192u;
             const int row0 = k_abs0 + (warp & 3) * 32;
@@ -1000,10 +1036,10 @@ __device__ __forceinline__ void dkdv_body(const CUtensorMap &map_q, const CUtens
     }
 }
 
-template <int DH, bool PACKED>
+template <int DH, bool PACKED, bool CLEAR>
 __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v,
                                         const CUtensorMap &map_do, const CUtensorMap &map_ke, const CUtensorMap &map_ve,
-                                        const CUtensorMap &map_dq, const BwdParams<DH> &p, uint8_t *smem_raw, int block_x, int h0) {
+                                        const CUtensorMap &map_kg, const CUtensorMap &map_vg, const CUtensorMap &map_dq, const BwdParams<DH> &p, uint8_t *smem_raw, int block_x, int h0) {
     typedef Bwd<DH> W;
     constexpr int T = W::kIn, KS = W::kKStages, IT = W::IT;
     const uint32_t raw = smem_u32(smem_raw);
@@ -1068,16 +1104,18 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
             load_rows<DH, SUB_BYTES>(sdO, &map_do, q_full, h0, qt0);
             uint32_t ks = 0, kph = 0;
             for (int j = 0; j < nkv; j++) {
-                const int row = span.tile(j0 + j) * IT, keys = keys_of(j);
+                const int tile = span.tile(j0 + j), keys = keys_of(j);
+                const bool part = j0 + j < span.ns && j0 + j == p.edge, gap = tile == p.gap.tile;
+                const int row = tile * IT - (gap ? p.gap.from : 0);
                 const uint32_t bytes = (uint32_t)keys * DH * 2u;
                 if (!mbar_wait(k_empty + 8 * ks, kph ^ 1u, abort_flag)) break;
                 mbar_expect_tx(k_full + 8 * ks, bytes);
-                load_tile<DH, W::kInSub>(sK + ks * T, keys < IT ? &map_ke : &map_k, k_full + 8 * ks, g, row);
+                load_tile<DH, W::kInSub>(sK + ks * T, part ? &map_ke : gap ? &map_kg : &map_k, k_full + 8 * ks, g, row);
                 if (++ks == KS) { ks = 0; kph ^= 1u; }
                 const uint32_t vs = j & 1, vph = (j >> 1) & 1;
                 if (!mbar_wait(v_empty + 8 * vs, vph ^ 1u, abort_flag)) break;
                 mbar_expect_tx(v_full + 8 * vs, bytes);
-                load_tile<DH, W::kInSub>(sV + vs * T, keys < IT ? &map_ve : &map_v, v_full + 8 * vs, g, row);
+                load_tile<DH, W::kInSub>(sV + vs * T, part ? &map_ve : gap ? &map_vg : &map_v, v_full + 8 * vs, g, row);
             }
         }
     } else if (warp == 1) {
@@ -1089,6 +1127,7 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
         uint32_t ks_s = 0, kph_s = 0, ks_q = 0;
         auto issue_s = [&](int j) -> bool {        // S = Q K^T
             if (!mbar_wait_warp(k_full + 8 * ks_s, kph_s, abort_flag)) return false;
+            if (CLEAR) clear_unseen<DH, IT, W::kInSub>(p.w, sK + ks_s * T, span.tile(j0 + j) * IT, lane);
             tc_fence_after();
             const uint32_t k_lo = klo(sK + ks_s * T);
 #pragma unroll
@@ -1100,6 +1139,7 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
         auto issue_dp = [&](int j) -> bool {       // dP = dO V^T
             const uint32_t vs = j & 1;
             if (!mbar_wait_warp(v_full + 8 * vs, (j >> 1) & 1, abort_flag)) return false;
+            if (CLEAR) clear_unseen<DH, IT, W::kInSub>(p.w, sV + vs * T, span.tile(j0 + j) * IT, lane);
             tc_fence_after();
             const uint32_t v_lo = klo(sV + vs * T);
 #pragma unroll
@@ -1257,13 +1297,14 @@ __device__ __forceinline__ void dq_body(const CUtensorMap &map_q, const CUtensor
     }
 }
 
-template <int DH, bool PACKED>
+template <int DH, bool PACKED, bool CLEAR>
 __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
     attn_window_bwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                            const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
                            const __grid_constant__ CUtensorMap map_qi, const __grid_constant__ CUtensorMap map_ki,
                            const __grid_constant__ CUtensorMap map_vi, const __grid_constant__ CUtensorMap map_doi,
                            const __grid_constant__ CUtensorMap map_ke, const __grid_constant__ CUtensorMap map_ve,
+                           const __grid_constant__ CUtensorMap map_kg, const __grid_constant__ CUtensorMap map_vg,
                            const __grid_constant__ CUtensorMap map_dq, const __grid_constant__ CUtensorMap map_dk,
                            const __grid_constant__ CUtensorMap map_dv, const __grid_constant__ CUtensorMap map_part,
                            const __grid_constant__ BwdParams<DH> p) {
@@ -1285,7 +1326,7 @@ __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
     } else {
         const int i = b < p.n_dq_first ? b : b - p.n_dkdv, tiles = (p.w.n + p.template tokens<PACKED>() - 1) / p.template tokens<PACKED>();
         const int c = PACKED ? i / p.split : i;
-        dq_body<DH, PACKED>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, map_dq, p, smem_raw, tiles - 1 - c % tiles, c / tiles * p.template heads<PACKED>());
+        dq_body<DH, PACKED, CLEAR>(map_q, map_ki, map_vi, map_do, map_ke, map_ve, map_kg, map_vg, map_dq, p, smem_raw, tiles - 1 - c % tiles, c / tiles * p.template heads<PACKED>());
     }
 }
 
@@ -1334,9 +1375,15 @@ bool tile_map(CUtensorMap *m, const bf16 *p, int64_t rows, int heads, uint32_t b
 template <int T>
 void edge_of(const WindowShape &w, int unit, int &edge, int &keys) {
     edge = w.sinks % T ? w.sinks / T : -1;
-    keys = (w.sinks % T + unit - 1) / unit * unit;
-    if (keys == T) edge = -1;
-    if (edge < 0) keys = unit;
+    keys = edge < 0 ? unit : (w.sinks % T + unit - 1) / unit * unit;
+}
+
+// The two maps of k or v that end with the sinks and begin with the windows' first row (stand-ins where no tile needs them).
+template <int DH>
+bool key_maps(CUtensorMap *edge, CUtensorMap *gap, const bf16 *x, const WindowShape &w, int edge_tile, uint32_t edge_keys, Gap g, uint32_t tile) {
+    const int64_t kv = (int64_t)w.q0 + w.n, from = g.tile < 0 ? 0 : g.from;
+    return tile_map<DH>(edge, x, edge_tile < 0 ? kv : w.sinks, w.Hkv, edge_keys) &&
+           tile_map<DH>(gap, x + from * w.Hkv * DH, kv - from, w.Hkv, tile);
 }
 
 template <int DH>
@@ -1362,7 +1409,9 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
     while (heads < 32 && G % (2 * heads) == 0) heads *= 2;          // whole rows to a warp, which stores its 32 by itself
     int64_t items = tile_of(heads);
     p.split = 1;
-    if (2 * items <= slots) {
+    bool clear;
+    p.gap = gap_of<KT>(w, clear);
+    if (2 * items <= slots && !clear) {
         // few rows: any divisor of the group, and clusters that share an item's key tiles
         int best = 1;
         for (int d = 2; d <= G && d <= TILE; d++)
@@ -1385,23 +1434,24 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
     if (items > 0x7fffffff / 2) return STREAMBP_E_SHAPE;
     p.items = (int)items;
     edge_of<KT>(w, 16, p.edge, p.edge_keys);
-    CUtensorMap mq, mk, mv, ke, ve, mo;
+    CUtensorMap mq, mk, mv, ke, ve, kg, vg, mo;
     if (!make_heads_map(&mq, q, w.n, w.Hq, DH, 64, (uint32_t)p.heads, (uint32_t)p.tokens, false) || !tile_map<DH>(&mk, k, kv, w.Hkv, KT) ||
-        !tile_map<DH>(&mv, v, kv, w.Hkv, KT) || !tile_map<DH>(&ke, k, kv, w.Hkv, (uint32_t)p.edge_keys) ||
-        !tile_map<DH>(&ve, v, kv, w.Hkv, (uint32_t)p.edge_keys))
+        !tile_map<DH>(&mv, v, kv, w.Hkv, KT) || !key_maps<DH>(&ke, &kg, k, w, p.edge, (uint32_t)p.edge_keys, p.gap, KT) ||
+        !key_maps<DH>(&ve, &vg, v, w, p.edge, (uint32_t)p.edge_keys, p.gap, KT))
         return STREAMBP_E_CUDA;
     if (p.split > 1) {
         static PerDevice configured;
-        if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, true>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
-        return launch_clusters(attn_window_fwd_kernel<DH, true>, dim3((unsigned)(p.items * p.split)), F::kThreads, F::kSmem, p.split, 1, st, mq, mk, mv,
-                               ke, ve, mk, p);
+        if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, true, false>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+        return launch_clusters(attn_window_fwd_kernel<DH, true, false>, dim3((unsigned)(p.items * p.split)), F::kThreads, F::kSmem, p.split, 1, st, mq, mk, mv,
+                               ke, ve, kg, vg, mk, p);
     }
     if (!make_heads_map(&mo, o, w.n, w.Hq, DH, 32, (uint32_t)p.heads, 32u / (uint32_t)p.heads, false, CU_TENSOR_MAP_SWIZZLE_64B)) return STREAMBP_E_CUDA;
-    static PerDevice configured;
-    if (!configured.get([] { return opt_in_smem(attn_window_fwd_kernel<DH, false>, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
     void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
-                   const FwdParams) = attn_window_fwd_kernel<DH, false>;
-    SBP_LAUNCH(kernel, p.items < slots ? p.items : slots, F::kThreads, F::kSmem, st, mq, mk, mv, ke, ve, mo, p);
+                   const CUtensorMap, const CUtensorMap, const FwdParams) =
+        clear ? attn_window_fwd_kernel<DH, false, true> : attn_window_fwd_kernel<DH, false, false>;
+    static PerDevice configured[2];
+    if (!configured[clear].get([&] { return opt_in_smem(kernel, F::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+    SBP_LAUNCH(kernel, p.items < slots ? p.items : slots, F::kThreads, F::kSmem, st, mq, mk, mv, ke, ve, kg, vg, mo, p);
     return STREAMBP_OK;
 }
 
@@ -1416,14 +1466,17 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     p.work = key_work<TILE>(w, IT, bwd_heads(w, IT), DH == 64 ? kBwdSlots64 : kBwdSlots128);
     const uint32_t heads = (uint32_t)p.work.heads, tokens = TILE / heads;
     edge_of<IT>(w, 32, p.edge, p.edge_keys);
+    bool clear;
+    p.gap = gap_of<IT>(w, clear);
     const int64_t kv = (int64_t)w.q0 + w.n;
     const uint32_t edge = (uint32_t)p.edge_keys;
-    CUtensorMap m[14];       // resident tiles of q, k, v, dO; inner tiles of the same; edge tiles of k, v; blocks of dq, dk, dv, part
+    // resident tiles of q, k, v, dO; inner tiles of the same; edge and gap tiles of k, v; blocks of dq, dk, dv, part
+    CUtensorMap m[16];
     auto rows_map = [&](CUtensorMap *x, const bf16 *a, uint32_t rows) { return make_heads_map(x, a, w.n, w.Hq, DH, 64, heads, rows, false); };
     if (!rows_map(&m[0], q, tokens) || !tile_map<DH>(&m[1], k, kv, w.Hkv, TILE) || !tile_map<DH>(&m[2], v, kv, w.Hkv, TILE) ||
         !rows_map(&m[3], dout, tokens) || !rows_map(&m[4], q, (uint32_t)p.work.tq) || !tile_map<DH>(&m[5], k, kv, w.Hkv, IT) ||
-        !tile_map<DH>(&m[6], v, kv, w.Hkv, IT) || !rows_map(&m[7], dout, (uint32_t)p.work.tq) || !tile_map<DH>(&m[8], k, kv, w.Hkv, edge) ||
-        !tile_map<DH>(&m[9], v, kv, w.Hkv, edge))
+        !tile_map<DH>(&m[6], v, kv, w.Hkv, IT) || !rows_map(&m[7], dout, (uint32_t)p.work.tq) || !key_maps<DH>(&m[8], &m[14], k, w, p.edge, edge, p.gap, IT) ||
+        !key_maps<DH>(&m[9], &m[15], v, w, p.edge, edge, p.gap, IT))
         return STREAMBP_E_CUDA;
     const bool f32 = mode != GRAD_BF16_SET;
     const CUtensorMapSwizzle swizzle = f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
@@ -1469,20 +1522,21 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     p.split = split > 1 && count - left > 2 + joined / 16 ? (int)split : 1;
     p.n_dkdv = (int)n_dkdv;
     p.n_dq_first = p.split > 1 ? (int)n_dq * p.split : 4 * span > 5 * (w.Hq / w.Hkv / p.work.heads) * walk ? (int)n_dq : 0;
-    const bool packed = heads > 1 || p.split > 1;
+    const int variant = clear ? 2 : heads > 1 || p.split > 1 ? 1 : 0;
     void (*kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
                    const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
-                   const CUtensorMap, const CUtensorMap, const BwdParams<DH>) = packed ? attn_window_bwd_kernel<DH, true> : attn_window_bwd_kernel<DH, false>;
-    static PerDevice configured[2];
-    if (!configured[packed].get([&] { return opt_in_smem(kernel, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
+                   const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const BwdParams<DH>) =
+        variant == 2 ? attn_window_bwd_kernel<DH, true, true> : variant == 1 ? attn_window_bwd_kernel<DH, true, false> : attn_window_bwd_kernel<DH, false, false>;
+    static PerDevice configured[3];
+    if (!configured[variant].get([&] { return opt_in_smem(kernel, W::kSmem) ? 1 : 0; })) return STREAMBP_E_CUDA;
     if (p.split > 1) {
         const int64_t ctas = (n_dkdv + n_dq * p.split + p.split - 1) / p.split * p.split;
         const int st_ = launch_clusters(kernel, dim3((unsigned)ctas), W::kThreads, W::kSmem, p.split, 1, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7],
-                                        m[8], m[9], m[10], m[11], m[12], m[13], p);
+                                        m[8], m[9], m[14], m[15], m[10], m[11], m[12], m[13], p);
         if (st_ != STREAMBP_OK) return st_;
     } else {
         SBP_LAUNCH(kernel, (unsigned)(n_dkdv + n_dq), W::kThreads, W::kSmem, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7], m[8], m[9],
-                   m[10], m[11], m[12], m[13], p);
+                   m[14], m[15], m[10], m[11], m[12], m[13], p);
     }
     const auto &k_ = p.work;
     if (k_.segs > 1 || k_.wsegs > 1)

@@ -11,19 +11,28 @@ namespace {
 
 constexpr int TILE = 32;
 
-// dst[r][c] = src[(row0 + r) * stride + c], 32 rows of DH values, zeros from `rows` on
-template <typename T, int DH>
-__device__ __forceinline__ void load_rows(float *dst, const T *src, int row0, int rows, int64_t stride) {
+// dst[r][c] = src[(row0 + r) * stride + c], 32 rows of DH values, zeros from `rows` on and in rows `skip`
+template <typename T, int DH, typename Skip>
+__device__ __forceinline__ void load_rows(float *dst, const T *src, int row0, int rows, int64_t stride, Skip skip) {
     constexpr int LD = DH + 4, N = Vec<T>::N;
     for (int i = threadIdx.x; i < 32 * (DH / N); i += 256) {
         const int r = i / (DH / N), c = (i % (DH / N)) * N;
         Vec<T> v;
 #pragma unroll
         for (int e = 0; e < N; e++) v.v[e] = 0.f;
-        if (row0 + r < rows) v.load(src + (int64_t)(row0 + r) * stride + c);
+        if (row0 + r < rows && !skip(row0 + r)) v.load(src + (int64_t)(row0 + r) * stride + c);
 #pragma unroll
         for (int e = 0; e < N; e++) dst[r * LD + c + e] = v.v[e];
     }
+}
+template <typename T, int DH>
+__device__ __forceinline__ void load_rows(float *dst, const T *src, int row0, int rows, int64_t stride) {
+    load_rows<T, DH>(dst, src, row0, rows, stride, [](int) { return false; });
+}
+// of K or V: rows that no query sees may hold anything
+template <typename T, int DH>
+__device__ __forceinline__ void load_keys(float *dst, const T *src, int row0, const WindowShape &w) {
+    load_rows<T, DH>(dst, src, row0, w.q0 + w.n, (int64_t)w.Hkv * DH, [&](int r) { return w.unseen(r); });
 }
 // s[i] = <A[4 warp + i], B[lane]>
 template <int DH>
@@ -70,8 +79,8 @@ __global__ void __launch_bounds__(256)
     for (int j = 0; j < span.count(); j++) {
         const int k0 = span.tile(j) * TILE;
         __syncthreads();
-        load_rows<T, DH>(Ks, k + (int64_t)g * DH, k0, kv, (int64_t)w.Hkv * DH);
-        load_rows<T, DH>(Vs, v + (int64_t)g * DH, k0, kv, (int64_t)w.Hkv * DH);
+        load_keys<T, DH>(Ks, k + (int64_t)g * DH, k0, w);
+        load_keys<T, DH>(Vs, v + (int64_t)g * DH, k0, w);
         __syncthreads();
         float s[4];
         dots<DH>(Qs, Ks, wp, lane, s);
@@ -173,8 +182,8 @@ __global__ void __launch_bounds__(256)
     int kt, begin, end, seg;
     work.item(w, item, kt, begin, end, seg);
     const int k0 = kt * TILE;
-    load_rows<T, DH>(Ks, k + (int64_t)g * DH, k0, kv, (int64_t)w.Hkv * DH);
-    load_rows<T, DH>(Vs, v + (int64_t)g * DH, k0, kv, (int64_t)w.Hkv * DH);
+    load_keys<T, DH>(Ks, k + (int64_t)g * DH, k0, w);
+    load_keys<T, DH>(Vs, v + (int64_t)g * DH, k0, w);
     float ak[NE][4], av[NE][4];
 #pragma unroll
     for (int e = 0; e < NE; e++)
@@ -259,8 +268,8 @@ __global__ void __launch_bounds__(256)
     for (int j = 0; j < span.count(); j++) {
         const int k0 = span.tile(j) * TILE;
         __syncthreads();
-        load_rows<T, DH>(Ks, k + (int64_t)g * DH, k0, kv, (int64_t)w.Hkv * DH);
-        load_rows<T, DH>(Vs, v + (int64_t)g * DH, k0, kv, (int64_t)w.Hkv * DH);
+        load_keys<T, DH>(Ks, k + (int64_t)g * DH, k0, w);
+        load_keys<T, DH>(Vs, v + (int64_t)g * DH, k0, w);
         __syncthreads();
         float p[4], ds[4];
         p_ds<DH>(Qs, Ds, Ks, Vs, lse_s, delta_s, wp, lane, w, w.q0 + r0, k0, scale, p, ds);

@@ -9,18 +9,21 @@
 
 namespace sbp {
 
-struct WindowShape {
-    int n, q0;            // query rows of the chunk and the absolute row of the first; keys are 0 .. q0 + n - 1
-    int Hq, Hkv;
-    int window;           // >= 1, at most q0 + n
-    int sinks;            // >= 0, at most q0 + n
-};
-
 #ifdef __CUDACC__
 #define SBP_HD __host__ __device__ __forceinline__
 #else
 #define SBP_HD inline
 #endif
+
+struct WindowShape {
+    int n, q0;            // query rows of the chunk and the absolute row of the first; keys are 0 .. q0 + n - 1
+    int Hq, Hkv;
+    int window;           // >= 1, at most q0 + n
+    int sinks;            // >= 0, at most q0 + n
+    // Rows of k and v that no query of the chunk sees may hold anything.  They are sinks .. seen_from() - 1, where there are any.
+    SBP_HD int seen_from() const { return q0 - window + 1; }
+    SBP_HD bool unseen(int j) const { return j >= sinks && j < seen_from(); }
+};
 
 // Key tiles of T keys that some query of rows first .. last (absolute) sees: the sink tiles 0 .. ns - 1, then lo .. hi.
 struct KeySpan {

@@ -220,6 +220,28 @@ def test_keys_that_no_query_sees_are_not_read(dtype):
     assert bool((grads[1][2:1000 - 49] == 0).all()) and bool((grads[2][2:1000 - 49] == 0).all())
 
 
+@pytest.mark.parametrize("dtype,dh,Hq,Hkv,n,q0,window,sinks", [
+    (BF, 64, 8, 2, 300, 1000, 333, 5), (BF, 128, 8, 2, 300, 1000, 333, 5), (BF, 128, 28, 4, 5, 1000, 333, 70),
+    (BF, 64, 16, 1, 1, 500, 100, 129), (BF, 128, 2, 2, 130, 250, 200, 0), (BF, 128, 32, 32, 700, 430, 300, 33),
+    (BF, 64, 32, 32, 700, 430, 300, 33), (BF, 128, 1, 1, 200, 100, 60, 30), (BF, 64, 8, 2, 200, 100, 60, 30),
+    (BF, 64, 40, 1, 700, 200, 170, 20), (F32, 64, 4, 2, 100, 300, 77, 5), (F32, 128, 2, 1, 40, 100, 90, 7)])
+def test_rows_that_no_query_sees_may_hold_anything(dtype, dh, Hq, Hkv, n, q0, window, sinks):
+    """NaN, infinities and the largest values in every row of k and v that no query of the chunk sees, also where such a row
+    shares a tile with visible ones."""
+    c = Case(n, q0, Hq, Hkv, dh, window, sinks, dtype)
+    see = torch.from_numpy(visible(n, q0, window, sinks).any(0)).cuda()
+    c.k[~see], c.v[~see] = 0.0, 0.0
+    o, lse = c.forward()
+    want = [o, lse] + list(c.backward(o, lse)) + ([] if dtype == F32 else list(c.backward(o, lse, BF)))
+    for bad in (float("nan"), float("inf"), -float("inf"), torch.finfo(dtype).max):
+        c.k[~see], c.v[~see] = bad, -bad
+        o, lse = c.forward()
+        got = [o, lse] + list(c.backward(o, lse)) + ([] if dtype == F32 else list(c.backward(o, lse, BF)))
+        for a, b in zip(want, got):
+            assert torch.equal(a, b)
+    assert bool((got[3][~see] == 0).all()) and bool((got[4][~see] == 0).all())
+
+
 def test_large_scores():
     """Scores of several hundred: the running maximum grows by large steps, weights of far keys vanish."""
     c = Case(300, 100, 2, 1, 128, 150, 4, std=3.0)
