@@ -20,7 +20,8 @@
 // and the sink tile that the window does not reach is cut to its sinks (16 columns for up to 16 of them).  32 rows of four
 // heads span 96 keys fewer than 128 rows of one (16384 rows, window 128, heads of 64: 96 -> 86 us).
 // What bounds it: the exponentials and the conversions around them, ~770 of the ~1600 cycles of a CTA's step of 128 x 64
-// scores, and the latencies that two chains do not hide.
+// scores, and the latencies that two chains do not hide.  2048 rows behind 14336, window 4096, 32:8 heads of 128: 148 us,
+// 930 TFLOP/s; 16384 rows, window 4096: 850 us, 1130 TFLOP/s.
 //
 // Backward (attn_window_bwd_kernel): two CTA roles in one grid, both deterministic (no floating-point atomics).
 //   dK/dV: one CTA per (key tile, KV head) loops over the query heads of the group and the query tiles that see the tile;
@@ -32,8 +33,9 @@
 // Softmax work is split in time (P for dV first, then dS), packed operands stay in tensor memory, every product is a full
 // tile; gradients leave through blocks of shared memory and TMA stores or adds, fp32 sums rounded once.
 // What bounds it: one iteration's chain of products and exponentials, ~2900 (dK/dV) and ~2500 cycles (dQ) for 128 x 128
-// scores at heads of 128, of which the products are ~1300.  Heads of 64 run two CTAs with inner tiles of 64 per SM.
-//
+// scores at heads of 128, of which the tensor pipe is busy 2048 and 1536.  Heads of 64 run two CTAs with inner tiles of 64 per
+// SM.  1024 rows behind 7168, window 2048, 28:4 heads of 128: 113 us (670 TFLOP/s counting five products a pair); 8191
+// rows, window 512, 32:8 heads of 64: 225 us.
 //
 // All mbarrier waits are bounded (sm100.cuh).
 #include <cstring>
