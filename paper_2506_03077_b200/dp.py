@@ -182,6 +182,8 @@ class ShardedAdamW:
         self.world = world if world is not None else (dist.get_world_size(group) if ready else 1)
         if grads.world != self.world or shard.numel() != grads.shard_elems:
             raise ValueError(f"the bucket is laid out for {grads.world} ranks, the group has {self.world}")
+        if not weight_decay.keys() <= grads.table.keys():
+            raise ValueError(f"no such tensors: {sorted(weight_decay.keys() - grads.table.keys())}")
         self.B, self.params, self.shard, self.group = B, params, shard, group
         lo, hi = grads.shard_range(self.rank)
         self.param = params.flat[lo:hi]
@@ -208,6 +210,8 @@ class ShardedAdamW:
         """On the current stream."""
         if self.plan is not None:
             self.B.grad_norm(self.plan, max_norm, self.norm, self.scale, self.ws)
+        else:
+            self.norm.zero_()
         if self.world > 1:
             total = self.norm.double().square_()
             dist.all_reduce(total, group=self.group)

@@ -66,18 +66,18 @@ def host_kernels():
     B.AdamWPlan, B.grad_norm, B.adamw_step = HostPlan, host_norm, host_step
 
 
-def inputs(step):
+def inputs(step, shapes=SHAPES):
     g = torch.Generator().manual_seed(step)
-    return {k: torch.randn(s, generator=g) for k, s in SHAPES.items()}
+    return {k: torch.randn(s, generator=g) for k, s in shapes.items()}
 
 
-def whole(steps, bad=None):
+def whole(steps, bad=None, shapes=SHAPES):
     """The same steps unsharded, in 64 bits."""
-    p = {k: v.to(torch.bfloat16).double() for k, v in inputs(100).items()}
+    p = {k: v.to(torch.bfloat16).double() for k, v in inputs(100, shapes).items()}
     m, v, k = ({n: torch.zeros_like(x) for n, x in p.items()} for _ in range(2)), None, 0
     m, v = m
     for s in range(steps):
-        g = {n: x.double() for n, x in inputs(s).items()}
+        g = {n: x.double() for n, x in inputs(s, shapes).items()}
         k += 1
         if s == bad:
             continue
@@ -90,13 +90,13 @@ def whole(steps, bad=None):
     return p
 
 
-def run_steps(rank, world, steps, bad=None):
-    b = dp.GradBucket(SHAPES, world, device="cpu")
-    params = dp.ParamBucket(b, {k: v.to(torch.bfloat16) for k, v in inputs(100).items()})
+def run_steps(rank, world, steps, bad=None, shapes=SHAPES):
+    b = dp.GradBucket(shapes, world, device="cpu")
+    params = dp.ParamBucket(b, {k: v.to(torch.bfloat16) for k, v in inputs(100, shapes).items()})
     shard = torch.zeros(b.shard_elems)
-    opt = dp.ShardedAdamW(params, b, shard, DECAY, bits=32)
+    opt = dp.ShardedAdamW(params, b, shard, {k: v for k, v in DECAY.items() if k in shapes}, bits=32)
     for s in range(steps):
-        for k, v in inputs(s).items():
+        for k, v in inputs(s, shapes).items():
             b.views[k].copy_(v / world)
         if s == bad and rank == world - 1:
             b.views["w_down"][0, 0] = float("nan")
@@ -108,31 +108,32 @@ def run_steps(rank, world, steps, bad=None):
     return {k: v.float().clone() for k, v in params.views.items()}
 
 
-def _rank_main(rank, world, port, q, bad):
+def _rank_main(rank, world, port, q, bad, shapes):
     os.environ.update(MASTER_ADDR="127.0.0.1", MASTER_PORT=str(port), RANK=str(rank), WORLD_SIZE=str(world))
     dist.init_process_group("gloo", rank=rank, world_size=world)
     host_kernels()
-    got = run_steps(rank, world, 3, bad)
+    got = run_steps(rank, world, 3, bad, shapes)
     q.put((rank, {k: v.numpy() for k, v in got.items()}))
     dist.barrier()
     dist.destroy_process_group()
 
 
-@pytest.mark.parametrize("bad", [None, 1])
-def test_two_ranks_step_as_one(bad):
-    """`bad`: a gradient that is not a number on one rank leaves that step out on both."""
-    world, port = 2, 29731 + (bad or 0)
+@pytest.mark.parametrize("bad,shapes", [(None, SHAPES), (1, SHAPES), (None, {"g1": (40,)})], ids=["three", "bad", "empty"])
+def test_two_ranks_step_as_one(bad, shapes):
+    """bad: a gradient that is not a number on one rank leaves that step out on both.  empty: the second rank's shard holds
+    padding only."""
+    world, port = 2, 29731 + (bad or 0) + 2 * (shapes is not SHAPES)
     ctx = mp.get_context("spawn")
     q = ctx.Queue()
-    procs = [ctx.Process(target=_rank_main, args=(r, world, port, q, bad)) for r in range(world)]
+    procs = [ctx.Process(target=_rank_main, args=(r, world, port, q, bad, shapes)) for r in range(world)]
     for p in procs:
         p.start()
     got = dict(q.get(timeout=120) for _ in procs)
     for p in procs:
         p.join(60)
         assert p.exitcode == 0
-    want = whole(3, bad)
-    for k in SHAPES:
+    want = whole(3, bad, shapes)
+    for k in shapes:
         assert np.array_equal(got[0][k], got[1][k])
         # the master copy is exact to fp32 roundings; the parameters are it, rounded once to bf16
         assert np.allclose(got[0][k], want[k].numpy(), rtol=2.0 ** -8 * 1.01, atol=1e-6)
@@ -147,3 +148,5 @@ def test_sizes_must_match():
         dp.ShardedAdamW(params, b, torch.zeros(8), DECAY, rank=0, world=2)
     with pytest.raises(ValueError):
         dp.ShardedAdamW(params, b, torch.zeros(b.shard_elems), DECAY, bits=4, rank=0, world=2)
+    with pytest.raises(ValueError):
+        dp.ShardedAdamW(params, b, torch.zeros(b.shard_elems), {"wqq": 0.1}, rank=0, world=2)
