@@ -289,6 +289,53 @@ def test_capture_and_other_stream():
     assert torch.equal(o, o2)
 
 
+def test_calls_at_once_and_replayed():
+    """Calls of every way to cut the work (clusters, segments, persistent CTAs), each with its own workspace: on streams of
+    their own at the same time, and captured into graphs that are replayed at the same time, give the bits that they give
+    alone."""
+    cases = [Case(5, 2000, 28, 4, 128, 1024, 4), Case(20, 3000, 16, 1, 64, 2500, 0), Case(2000, 0, 16, 1, 128, 2000, 0),
+             Case(700, 300, 32, 8, 64, 200, 33), Case(1, 900, 8, 8, 128, 900, 0), Case(200, 100, 40, 1, 64, 60, 30)]
+    want = []
+    for c in cases:
+        o, lse = c.forward()
+        want.append([o, lse] + list(c.backward(o, lse, BF)))
+    out = [[torch.empty_like(x) for x in w] for w in want]
+    ws = [B.alloc_workspace(B.attention_window_workspace_bytes(c.n, c.q0, c.Hq, c.Hkv, c.dh, c.window, c.sinks)) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+
+    def call(c, x, w):
+        B.attention_window_forward(c.q, c.k, c.v, c.q0, c.window, c.sinks, x[0], x[1])
+        B.attention_window_backward(c.q, c.k, c.v, x[0], c.do, x[1], c.q0, c.window, c.sinks, x[2], x[3], x[4], w)
+
+    def same():
+        torch.cuda.synchronize()
+        for a, b, w in zip(want, out, ws):
+            assert all(torch.equal(x, y) for x, y in zip(a, b)) and B.last_device_status(w) == B.OK
+            for y in b:
+                y.fill_(float("nan"))
+        torch.cuda.synchronize()
+
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, x, w, s in zip(cases, out, ws, streams):
+            with torch.cuda.stream(s):
+                call(c, x, w)
+    same()
+    graphs = []
+    for c, x, w in zip(cases, out, ws):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(c, x, w)
+        graphs.append(g)
+    same_before = [x[0].isnan().all() for x in out]
+    assert all(bool(b) for b in same_before)              # captured, not run
+    for _ in range(3):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    same()
+
+
 def test_gradient_against_differences():
     """Directional derivatives of sum(O * dO) by central differences of the fp32 forward."""
     c = Case(70, 30, 2, 1, 64, 25, 3, F32)
