@@ -116,31 +116,47 @@ __device__ __forceinline__ void finish_vec(const EpiParams &p, const uint32_t (&
     }
 }
 // The same where rows do not start on 16-byte boundaries, or the columns end inside the block: the block is transposed
-// through shared memory (column index exchanged with the row's bits, so that neither side has bank conflicts) and walked row
-// by row with a lane per column: consecutive addresses instead of one element of each of 32 rows.
-template <int ACT>
+// through shared memory (16-byte groups exchanged with the row's bits, so that neither side has bank conflicts) and walked
+// row by row with a lane per column: consecutive addresses instead of one element of each of 32 rows.  Eight rows at a time,
+// without a branch among them, and the residuals of the next eight under way: 8000 x 1997 x 1024 with a residual 107 -> 68 us,
+// with GELU and z kept 94 -> 70 (2000 columns: 47).
+template <int ACT, bool RES>
 __device__ __forceinline__ void finish_rows(const EpiParams &p, const uint32_t (&r)[32], float *stage, int lane, int row0, int col0) {
 #pragma unroll
-    for (int e = 0; e < 32; e++) stage[lane * 32 + (e ^ lane)] = __uint_as_float(r[e]);
+    for (int j = 0; j < 8; j++) {
+        const uint32_t w[4] = {r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]};
+        st_shared_v4(smem_u32(stage) + (uint32_t)(lane * 128 + ((j ^ (lane & 7)) << 4)), w);
+    }
     __syncwarp();
     const int col = col0 + lane;
     if (col < p.N) {
         const float b = p.bias ? __bfloat162float(p.bias[col]) : 0.f;
         const int rows = p.M - row0 < 32 ? p.M - row0 : 32;
+        const bf16 *res_at = RES ? p.residual + (long long)row0 * p.ldr + col : nullptr;
+        bf16 *pre_at = p.pre ? p.pre + (long long)row0 * p.ldp + col : nullptr, *c_at = p.C + (long long)row0 * p.ldc + col;
+        bf16 ahead[8];
+        auto request = [&](int i) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) ahead[k] = i + k < rows ? res_at[(i + k) * p.ldr] : __float2bfloat16_rn(0.f);
+        };
+        if (RES) request(0);
 #pragma unroll 1
-        for (int i = 0; i < rows; i += 8) {         // eight residuals requested before the first store (which may be to them)
-            float res[8];
+        for (int i = 0; i < rows; i += 8) {         // eight rows at a time, the residuals of the next ones requested first
+            float res[8], z[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) res[k] = RES ? __bfloat162float(ahead[k]) : 0.f;
+            if (RES) request(i + 8);
+#pragma unroll
+            for (int k = 0; k < 8; k++) z[k] = stage[(i + k) * 32 + (((lane >> 2) ^ k) << 2) + (lane & 3)] + b;
+            if (pre_at)
+#pragma unroll
+                for (int k = 0; k < 8; k++)
+                    if (i + k < rows) pre_at[(i + k) * p.ldp] = __float2bfloat16_rn(z[k]);
+#pragma unroll
+            for (int k = 0; k < 8; k++) z[k] = activate<ACT, true>(z[k]) + res[k];
 #pragma unroll
             for (int k = 0; k < 8; k++)
-                res[k] = p.residual && i + k < rows ? __bfloat162float(p.residual[(long long)(row0 + i + k) * p.ldr + col]) : 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; k++) {
-                if (i + k >= rows) break;
-                const long long row = row0 + i + k;
-                const float z = stage[(i + k) * 32 + (lane ^ (i + k))] + b;
-                if (p.pre) p.pre[row * p.ldp + col] = __float2bfloat16_rn(z);
-                p.C[row * p.ldc + col] = __float2bfloat16_rn(activate<ACT, true>(z) + res[k]);
-            }
+                if (i + k < rows) c_at[(i + k) * p.ldc] = __float2bfloat16_rn(z[k]);
         }
     }
     __syncwarp();
@@ -259,7 +275,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1) gemm_a
                     fetch(c + 2);
                     finish_vec<ACT>(p, r, now, smem_u32(stage), lane, row0, col0);
                 } else {
-                    finish_rows<ACT>(p, r, stage, lane, row0, col0);
+                    if (p.residual) finish_rows<ACT, true>(p, r, stage, lane, row0, col0);
+                    else finish_rows<ACT, false>(p, r, stage, lane, row0, col0);
                 }
             }
             tc_fence_before();
