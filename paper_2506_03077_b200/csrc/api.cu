@@ -927,7 +927,7 @@ size_t streambp_gemm_epilogue_workspace_bytes(int64_t M, int64_t N) {
     if (M < 1 || N < 1 || M > (1ll << 30) || N > (1ll << 30)) return 0;
     Arena a(nullptr);
     a.take_bytes(kHeaderBytes);
-    a.take<float>((size_t)gemm_epilogue_splits(M, N) * (size_t)N);
+    a.take<float>((size_t)gemm_epilogue_splits(M, N) * 2 * (size_t)N);      // rows of two classes (epilogue_bwd.cu)
     return a.size();
 }
 
@@ -949,7 +949,7 @@ int streambp_gemm_epilogue_backward(const void *dC, int64_t ldd, const void *pre
         if (workspace_bytes < streambp_gemm_epilogue_workspace_bytes(M, N)) return STREAMBP_E_WORKSPACE;
         Arena a(workspace);
         a.take_bytes(kHeaderBytes);
-        partials = a.take<float>((size_t)gemm_epilogue_splits(M, N) * (size_t)N);
+        partials = a.take<float>((size_t)gemm_epilogue_splits(M, N) * 2 * (size_t)N);      // rows of two classes (epilogue_bwd.cu)
     }
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     call_state().cuda_error = 0;

@@ -3,11 +3,11 @@
 //
 // HBM-bound: dC and z are read once, dz is written once.  A block owns a strip of 64 columns (a 128-byte row segment in
 // bf16, eight threads of one 16-byte load each) and walks its rows 32 at a time, keeping the sums of its columns in
-// registers; a grid of (strips, row splits) fills the GPU.  The splits of a strip, up to eight of them, are a cluster that adds
-// its sums in their order; more of them leave their sums in `partials`, which a second small kernel adds in the same order:
-// no atomics, the same inputs give the same bits.  What bounds it: four rows in
-// flight a thread as raw 16-byte words and four blocks an SM read at 4.2 - 4.7 TB/s (2048 x 14336 with GELU: 42 us for
-// 176 MB; 8192 x 4096 with SiLU: 43 us for 201 MB); unpacked as they arrive they cost twice the registers and half the blocks.
+// registers; a grid of (strips, row splits) fills the GPU.  The splits of a strip leave their sums in `partials`, which a second
+// small kernel adds in their order, or for small products are a cluster that adds them itself: no atomics, the same inputs
+// give the same bits.  What bounds it: four rows in flight a thread as raw 16-byte words and four blocks an SM read at 4.2 -
+// 4.7 TB/s (2048 x 14336 with GELU: 42 us for 176 MB; 8192 x 4096 with SiLU: 43 us for 201 MB); unpacked as they arrive they
+// cost twice the registers and half the blocks.
 #include <type_traits>
 
 #include "activation.cuh"
@@ -79,6 +79,79 @@ __global__ void __launch_bounds__(256)
     s_sum[tr][tc] = sum;
     __syncthreads();
     put_sums(to, (s_sum[0][tc] + s_sum[1][tc]) + (s_sum[2][tc] + s_sum[3][tc]), col, N, joined);
+}
+
+// bf16 rows that start anywhere, those of all matrices alike: a warp to a row, a lane to two columns, read and written as the
+// 4-byte word they make.  In rows that start on a word (class 0) a strip's words hold columns 64 b .. 64 b + 63, in the others
+// (class 1) columns 64 b - 1 .. 64 b + 62; a warp's rows are eight apart and so of one class, and the classes' sums are rows
+// of `partials` of their own.  A lane per column has half as much under way (5000 x 19001 with SiLU: 168 us against 130; 2048 x
+// 8191: 38.6 and 32.4).
+template <bool WORD>
+__device__ __forceinline__ uint32_t load_two(const bf16 *p, bool lo, bool hi) {
+    if (WORD) return *reinterpret_cast<const uint32_t *>(p);
+    const uint16_t *u = reinterpret_cast<const uint16_t *>(p);
+    return (lo ? (uint32_t)u[0] : 0u) | (hi ? (uint32_t)u[1] << 16 : 0u);
+}
+template <int ACT>
+__global__ void __launch_bounds__(256, 4)
+    epilogue_bwd_words_kernel(const bf16 *dC, int64_t ldd, const bf16 *pre, int64_t ldp, int64_t M, int N, int64_t rows_per_split,
+                              bf16 *dZ, int64_t ldz, Sums to) {
+    pdl_enter();
+    constexpr int kAhead = 8, kWarps = 8;
+    __shared__ float s_sum[kWarps][kStrip];
+    __shared__ int s_class[kWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t first = blockIdx.y * rows_per_split, end = first + rows_per_split < M ? first + rows_per_split : M, row0 = first + warp;
+    const int cls = (int)((reinterpret_cast<uintptr_t>(dC) >> 1) + (uint64_t)row0 * (uint64_t)ldd) & 1;
+    const int col = blockIdx.x * kStrip + 2 * lane - cls;
+    const bool lo = col >= 0 && col < N, hi = col + 1 < N;
+    float sum_lo = 0.f, sum_hi = 0.f;
+    auto rows = [&](auto whole) {                     // one loop without a branch between its loads for warps of whole words
+        constexpr bool kWord = decltype(whole)::value;
+        for (int64_t r0 = row0; r0 < end; r0 += kWarps * kAhead) {
+            uint32_t d[kAhead], z[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; a++) {
+                const int64_t r = r0 + kWarps * a < end ? r0 + kWarps * a : r0;      // past the end: the first row again, not used
+                d[a] = load_two<kWord>(dC + r * ldd + col, lo, hi);
+                if (ACT != STREAMBP_ACT_NONE) z[a] = load_two<kWord>(pre + r * ldp + col, lo, hi);
+            }
+#pragma unroll
+            for (int a = 0; a < kAhead; a++) {
+                const int64_t r = r0 + kWarps * a;
+                if (r >= end) break;
+                float x = __uint_as_float(d[a] << 16), y = __uint_as_float(d[a] & 0xFFFF0000u);
+                if (ACT != STREAMBP_ACT_NONE) {
+                    x = __fmul_rn(x, slope<ACT, true>(__uint_as_float(z[a] << 16)));
+                    y = __fmul_rn(y, slope<ACT, true>(__uint_as_float(z[a] & 0xFFFF0000u)));
+                }
+                sum_lo += x;
+                sum_hi += y;
+                if (dZ) {
+                    bf16 *at = dZ + r * ldz + col;
+                    if (kWord) *reinterpret_cast<__nv_bfloat162 *>(at) = __floats2bfloat162_rn(x, y);
+                    else {
+                        if (lo) at[0] = __float2bfloat16_rn(x);
+                        if (hi) at[1] = __float2bfloat16_rn(y);
+                    }
+                }
+            }
+        }
+    };
+    if (__all_sync(0xffffffffu, lo && hi)) rows(std::true_type());
+    else rows(std::false_type());
+    if (!to.partials) return;
+    s_sum[warp][2 * lane] = sum_lo;
+    s_sum[warp][2 * lane + 1] = sum_hi;
+    if (lane == 0) s_class[warp] = cls;
+    __syncthreads();
+    const int of = threadIdx.x / kStrip, j = threadIdx.x % kStrip, c = blockIdx.x * kStrip + j - of;
+    if (of < 2 && c >= 0 && c < N) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; w++) t += s_class[w] == of ? s_sum[w][j] : 0.f;
+        to.partials[((int64_t)blockIdx.y * 2 + of) * N + c] = t;
+    }
 }
 
 template <typename T, int ACT>
@@ -180,6 +253,17 @@ int launch(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int64
         return launch_clusters(kernel, grid, 256, 0, 1, splits, st, dC, ldd, pre, ldp, M, (int)N, per, dZ, ldz, to);
     }
     if (dbias) to.partials = partials;
+    if constexpr (std::is_same<T, bf16>::value) {
+        auto start = [](const void *q, int64_t ld) { return (int)((reinterpret_cast<uintptr_t>(q) >> 1) & 1) + 2 * (int)(ld & 1); };
+        if (!vec && (ACT == STREAMBP_ACT_NONE || start(pre, ldp) == start(dC, ldd)) && (!dZ || start(dZ, ldz) == start(dC, ldd))) {
+            // one strip more where N is a multiple of its width: class 1 ends a column short
+            SBP_LAUNCH(epilogue_bwd_words_kernel<ACT>, dim3((unsigned)(N / kStrip + 1), (unsigned)splits), 256, 0, st, dC, ldd, pre, ldp, M, (int)N,
+                       per, dZ, ldz, to);
+            if (!dbias) return STREAMBP_OK;
+            SBP_LAUNCH(epilogue_sum_kernel, (unsigned)((N + 255) / 256), 256, 0, st, partials, 2 * splits, (int)N, dbias, accumulate ? 1 : 0, hdr);
+            return STREAMBP_OK;
+        }
+    }
     SBP_LAUNCH(kernel, grid, 256, 0, st, dC, ldd, pre, ldp, M, (int)N, per, dZ, ldz, to);
     if (dbias)
         SBP_LAUNCH(epilogue_sum_kernel, (unsigned)((N + 255) / 256), 256, 0, st, partials, splits, (int)N, dbias, accumulate ? 1 : 0, hdr);

@@ -204,6 +204,38 @@ def test_backward(act, dtype, M, N, extra):
     assert torch.equal(D, G)
 
 
+@pytest.mark.parametrize("M,N,ld,shift", [(2100, 63, 63, 0), (2100, 64, 65, 0), (2100, 64, 64, 1), (2100, 128, 129, 1), (2101, 191, 191, 1),
+                                         (2049, 1001, 1001, 0), (2049, 1002, 1002, 0), (2049, 1002, 1003, 1), (300, 15001, 15001, 0), (2100, 1, 1, 1),
+                                         (5000, 2, 3, 0)])
+def test_backward_of_rows_that_start_anywhere(M, N, ld, shift):
+    """bf16 rows of odd length or pitch, from an odd element on: the first and the last columns, and what lies around them."""
+    def place(x):
+        buf = torch.full((M * ld + shift + 64,), FENCE, dtype=torch.bfloat16, device="cuda")
+        view = buf[shift:shift + M * ld].as_strided((M, N), (ld, 1))
+        view.copy_(x)
+        return view, buf
+    D, _ = place(rand(0, M, N, dtype=torch.bfloat16))
+    Z, _ = place(rand(1, M, N, dtype=torch.bfloat16) * 2)
+    G, gbuf = place(torch.zeros(M, N, dtype=torch.bfloat16, device="cuda"))
+    db = torch.full((N + 16,), FENCE, device="cuda")
+    need = B.gemm_epilogue_workspace_bytes(M, N)
+    ws = torch.full((need + 256,), 7, dtype=torch.uint8, device="cuda")
+    B.gemm_epilogue_backward(D, Z, "silu", G, db[:N], ws[:need])
+    d64, s64 = f64(D), slope64(f64(Z), "silu")
+    ref = d64 * s64
+    e = 2.0 ** -18 * np.abs(d64) + 2 * E32 * np.abs(ref)
+    assert (np.abs(f64(G) - ref) <= e + HALF[torch.bfloat16] * (np.abs(ref) + e)).all()
+    assert (np.abs(f64(db[:N]) - ref.sum(0)) <= e.sum(0) + M * E32 * np.abs(ref).sum(0)).all()
+    outside = torch.ones_like(gbuf, dtype=torch.bool)
+    outside[shift:shift + M * ld].as_strided((M, N), (ld, 1)).fill_(False)
+    assert bool((gbuf[outside] == FENCE).all()) and bool((db[N:] == FENCE).all()) and bool((ws[need:] == 7).all())
+    first = db.clone()
+    B.gemm_epilogue_backward(D, Z, "silu", None, db[:N], ws[:need])
+    assert torch.equal(db, first)
+    B.gemm_epilogue_backward(D, Z, "silu", D)
+    assert torch.equal(D, G)
+
+
 def test_gradient_against_differences():
     """sum(C * D) as a function of z: the backward's dZ against central differences of the forward in fp32."""
     M, N, h = 5, 40, 2.0 ** -6
