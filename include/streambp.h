@@ -477,7 +477,9 @@ int streambp_attention_backward_static(const void *q, const void *k, const void 
  * the last block may be shorter): code c of the block stands for e4m3(c) * 2^(s - 127).  s is the block's largest biased
  * fp32 exponent less 7, at least 1; 255 marks a block that held an infinity or a NaN (all its values read as NaN).  What
  * is held in `v` is the ROOT of the second moment, and a root that is not zero is held as at least 2^-9 * 2^(s - 127).
- * The update of the parameter uses the new moments before they are rounded.  Start from zero codes and scale bytes of 1
+ * The update of the parameter uses the new moments before they are rounded.  What is rounded to codes is the plain fp32
+ * evaluation, every operation rounded: x = g scale, m = (beta1 m) + ((1 - beta1) x), root of (beta2 (v v)) + (((1 - beta2) x) x),
+ * so that an implementation in other fp32 arithmetic decides the same ties.  Start from zero codes and scale bytes of 1
  * (any byte below 255 does).
  *
  * step: NULL (t = cfg->step >= 1), or one int64 in device memory that is read when the kernel runs (a value below 1
@@ -498,7 +500,7 @@ typedef struct {
     float weight_decay;
 } streambp_adamw_tensor;
 typedef struct {
-    float lr, beta1, beta2, eps;
+    double lr, beta1, beta2, eps;   /* 1 - beta is formed in double */
     int32_t param_dtype;  /* streambp_dtype */
     int32_t state_dtype;  /* streambp_state_dtype */
     int64_t step;

@@ -79,7 +79,7 @@ class AdamWTensorC(C.Structure):
 
 
 class AdamWCfgC(C.Structure):
-    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("param_dtype", C.c_int32), ("state_dtype", C.c_int32), ("step", C.c_int64)]
 
 

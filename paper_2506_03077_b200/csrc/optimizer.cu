@@ -35,7 +35,8 @@ struct StepParams {
     streambp_adamw_tensor t[CAP];
     int piece_begin[CAP + 1];        // pieces of tensor i: piece_begin[i] .. piece_begin[i + 1] - 1
     int n;
-    float lr, beta1, beta2, eps;
+    double lr64, beta1_64, beta2_64; // for a step number on the device
+    float lr, beta1, beta2, rest1, rest2, eps;      // rest: 1 - beta
     float step_size, inv_root_bc2;   // lr / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
     const float *grad_scale;         // optional
     const int64_t *step;             // optional: the step number is read from the device
@@ -151,13 +152,41 @@ __device__ __forceinline__ uint32_t block_max2(uint32_t v) {
 }
 
 struct Rates {
-    float gs, lr, b1, b2, eps, step_size, inv_root_bc2;
-    float g1, g2, root_b2;      // gs (1 - beta1), gs sqrt(1 - beta2), sqrt(beta2)
+    float gs, lr, b1, b2, rest1, rest2, eps, step_size, inv_root_bc2;
 };
 __device__ __forceinline__ float fast_sqrt(float x) {
     float y;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// Roots of eight values, each rounded to nearest: from an approximate inverse root y, the root v y corrected by its exact
+// residual (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  The residual is
+// exact where it is no subnormal number: eight values of which one is too small or too large go through powers of four.
+__device__ __forceinline__ float corrected_root(float v) {
+    float y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaxf(v, 1e-28f)));      // 0 stays 0
+    const float s = v * y;
+    return fmaf(fmaf(-s, s, v), 0.5f * y, s);
+}
+__device__ __forceinline__ void roots8(float (&v)[8]) {
+    float top = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        odd |= v[e] < 1e-28f && v[e] > 0.f;
+        top = max_abs(top, v[e]);
+    }
+    if (!odd && top < 1e37f) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = corrected_root(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const bool small = v[e] < 1.f;
+            const float w = corrected_root(v[e] * (small ? 0x1p96f : 0x1p-32f)) * (small ? 0x1p-48f : 0x1p16f);
+            v[e] = isinf(v[e]) ? v[e] : w;
+        }
+    }
 }
 __device__ __forceinline__ float fast_rcp(float x) {
     float y;
@@ -200,8 +229,8 @@ __device__ __forceinline__ void step_piece_f32(const streambp_adamw_tensor &t, l
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const float x = g[k][e] * r.gs;
-            m[k][e] = fmaf(r.b1, m[k][e], (1.f - r.b1) * x);
-            v[k][e] = fmaf(r.b2, v[k][e], (1.f - r.b2) * x * x);
+            m[k][e] = fmaf(r.b1, m[k][e], r.rest1 * x);
+            v[k][e] = fmaf(r.b2, v[k][e], r.rest2 * x * x);
             p[k][e] = moved(r, p[k][e], decay, m[k][e], fast_sqrt(v[k][e]));
         }
         store4(mp + off[k], valid[k], m[k]);
@@ -252,18 +281,22 @@ __device__ __forceinline__ void step_piece_mx8(const streambp_adamw_tensor &t, l
             cv[0] = load_codes(vc + off, lo); cv[1] = load_codes(vc + off + 4, hi);
         }
         const uint32_t sm = FULL || valid > 0 ? ms[off / kBlock] : 1u, sv = FULL || valid > 0 ? vs[off / kBlock] : 1u;
-        // beta1 and the root of beta2 go into the scales of the old moments: fewer operations an element than decoding
-        // first and updating then, in a kernel that runs close to the issue rate
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            decode4(cm[h], scale_value(sm) * r.b1, half(m, h));
-            decode4(cv[h], scale_value(sv) * r.root_b2, half(u, h));
+            decode4(cm[h], scale_value(sm), half(m, h));
+            decode4(cv[h], scale_value(sv), half(u, h));
         }
+        // every operation rounded by itself, the root to the nearest: a code that another evaluation of the formula in fp32
+        // would round the other way changes what it stands for by up to an eighth, and with it the next step
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            const float x = g[e] * r.g2;
-            m[e] = fmaf(g[e], r.g1, m[e]);
-            u[e] = fast_sqrt(fmaf(u[e], u[e], x * x));
+            g[e] *= r.gs;
+            m[e] = __fadd_rn(__fmul_rn(r.b1, m[e]), __fmul_rn(r.rest1, g[e]));
+            u[e] = __fadd_rn(__fmul_rn(r.b2, __fmul_rn(u[e], u[e])), __fmul_rn(__fmul_rn(r.rest2, g[e]), g[e]));
+        }
+        roots8(u);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
             p[e] = moved(r, p[e], decay, m[e], u[e]);
             if (!FULL && e >= valid) m[e] = u[e] = 0.f;
         }
@@ -279,7 +312,7 @@ __device__ __forceinline__ void step_piece_mx8(const streambp_adamw_tensor &t, l
             wm[h] = encode4<false>(half(m, h), nm, [](int) { return false; });
             // not zero is decided from what the root is made of: its square may have vanished in fp32
             wv[h] = encode4<true>(half(u, h), nv, [&](int e) {
-                return 4 * h + e < valid && (g[4 * h + e] * r.g2 != 0.f || (cv[h] >> (8 * e) & 0x7fu) != 0u);
+                return 4 * h + e < valid && (g[4 * h + e] != 0.f || (cv[h] >> (8 * e) & 0x7fu) != 0u);
             });
         }
         if constexpr (FULL) {
@@ -314,31 +347,28 @@ __device__ __forceinline__ void step_piece(const streambp_adamw_tensor &t, long 
     else step_piece_f32<P, MASTER, FULL>(t, base, r);
 }
 
-// Blocks per SM: moments in 8 bits are bound by the issue rate and by the loads in flight together, five blocks of 48
-// registers beat four of 64 and three of 80 (233 M bf16 parameters: 0.54 ms a step, 5.2 TB/s; 0.55, 0.61); moments in
-// 32 bits need nothing but loads in flight, three blocks with four units of them a thread run at the copy rate (40 M
-// parameters with a master copy: 0.186 ms, 6.4 TB/s).
+// Blocks per SM: moments in 8 bits are bound by the issue rate and by the loads in flight together, four blocks of 64
+// registers take 0.56 ms for 233 M bf16 parameters (5.0 TB/s), five of 48 0.57, three of 80 0.65; moments in 32 bits need
+// nothing but loads in flight, three blocks with four units of them a thread run at the copy rate (40 M parameters with a
+// master copy: 0.186 ms, 6.4 TB/s).
 // P: parameter type, MX8: moments in 8 bits.  With a master copy the parameter is the rounded master and is not read.
 template <typename P, bool MX8, int CAP>
-__global__ void __launch_bounds__(kThreads, MX8 ? 5 : 3) adamw_kernel(const __grid_constant__ StepParams<CAP> a) {
+__global__ void __launch_bounds__(kThreads, MX8 ? 4 : 3) adamw_kernel(const __grid_constant__ StepParams<CAP> a) {
     pdl_enter();
     __shared__ float s_rate[2];
-    Rates r{a.grad_scale ? *a.grad_scale : 1.f, a.lr, a.beta1, a.beta2, a.eps, a.step_size, a.inv_root_bc2};
+    Rates r{a.grad_scale ? *a.grad_scale : 1.f, a.lr, a.beta1, a.beta2, a.rest1, a.rest2, a.eps, a.step_size, a.inv_root_bc2};
     if (!isfinite(r.gs)) return;              // the gradients were not finite: the step is left out, the same for every block
     if (a.step) {
         if (threadIdx.x == 0) {
             const long long t = *a.step;
             const double n = t < 1 ? 1.0 : (double)t;
-            s_rate[0] = (float)((double)a.lr / (1.0 - pow((double)a.beta1, n)));
-            s_rate[1] = (float)(1.0 / sqrt(1.0 - pow((double)a.beta2, n)));
+            s_rate[0] = (float)(a.lr64 / (1.0 - pow(a.beta1_64, n)));
+            s_rate[1] = (float)(1.0 / sqrt(1.0 - pow(a.beta2_64, n)));
         }
         __syncthreads();
         r.step_size = s_rate[0];
         r.inv_root_bc2 = s_rate[1];
     }
-    r.g1 = r.gs * (1.f - r.b1);
-    r.g2 = r.gs * sqrtf(1.f - r.b2);
-    r.root_b2 = sqrtf(r.b2);
     const int pieces = a.piece_begin[a.n];
     for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
         const int i = find_tensor(a.piece_begin, a.n, piece);
@@ -434,8 +464,13 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_consta
 }
 __device__ __forceinline__ void put_norm(double squares, float max_norm, float *norm, float *scale) {
     const double s = sqrt(squares);
-    *norm = (float)s;
-    if (scale) *scale = isfinite(s) ? (float)fmin(1.0, (double)max_norm / (s + 1e-6)) : __uint_as_float(0x7fc00000u);
+    const float n = (float)s;
+    *norm = n;
+    if (!scale) return;
+    // of the norm as it is given, in fp32: whoever forms the factor from it has the same
+    if (!isfinite(s)) *scale = __uint_as_float(0x7fc00000u);
+    else if (isinf(n)) *scale = (float)((double)max_norm / s);
+    else *scale = fminf(1.f, __fmul_rn(__frcp_rn(__fadd_rn(n, 1e-6f)), max_norm));
 }
 // Few pieces, one to each team of kThreads in a cluster, whose blocks' shares are added in their order.  One launch where the
 // other way takes two: 20 tensors of 60 000 elements in all, norm and step, 13.4 us of the host's time against 15.1, the
@@ -559,7 +594,9 @@ int launch_adamw(const streambp_adamw_cfg &c, const streambp_adamw_tensor *tenso
         }
         if (a.n == 0) break;
         a.piece_begin[a.n] = (int)pieces;
-        a.lr = c.lr; a.beta1 = c.beta1; a.beta2 = c.beta2; a.eps = c.eps;
+        a.lr64 = c.lr; a.beta1_64 = c.beta1; a.beta2_64 = c.beta2;
+        a.lr = (float)c.lr; a.beta1 = (float)c.beta1; a.beta2 = (float)c.beta2; a.eps = (float)c.eps;
+        a.rest1 = (float)(1.0 - c.beta1); a.rest2 = (float)(1.0 - c.beta2);
         a.step_size = step_size;
         a.inv_root_bc2 = inv_root_bc2;
         a.grad_scale = grad_scale;
@@ -624,8 +661,8 @@ int streambp_adamw_step(const streambp_adamw_cfg *cfg, const streambp_adamw_tens
     if (n < 0) return STREAMBP_E_SHAPE;
     if (cfg->param_dtype != STREAMBP_F32 && cfg->param_dtype != STREAMBP_BF16) return STREAMBP_E_DTYPE;
     if (cfg->state_dtype != STREAMBP_STATE_F32 && cfg->state_dtype != STREAMBP_STATE_MX8) return STREAMBP_E_DTYPE;
-    if (!(cfg->lr >= 0.f) || !(cfg->beta1 >= 0.f && cfg->beta1 < 1.f) || !(cfg->beta2 >= 0.f && cfg->beta2 < 1.f) ||
-        !(cfg->eps >= 0.f) || std::isinf(cfg->lr) || std::isinf(cfg->eps) || (!step && cfg->step < 1))
+    if (!(cfg->lr >= 0.0) || !(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) ||
+        !(cfg->eps >= 0.0) || std::isinf((float)cfg->lr) || std::isinf((float)cfg->eps) || (!step && cfg->step < 1))
         return STREAMBP_E_SHAPE;
     if ((grad_scale && (reinterpret_cast<uintptr_t>(grad_scale) & 3u)) || (step && (reinterpret_cast<uintptr_t>(step) & 7u)))
         return STREAMBP_E_ALIGN;
@@ -640,8 +677,8 @@ int streambp_adamw_step(const streambp_adamw_cfg *cfg, const streambp_adamw_tens
     }
     begin_call();
     const double t = step ? 1.0 : (double)cfg->step;
-    const float step_size = (float)((double)cfg->lr / (1.0 - std::pow((double)cfg->beta1, t)));
-    const float inv_root_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow((double)cfg->beta2, t)));
+    const float step_size = (float)(cfg->lr / (1.0 - std::pow(cfg->beta1, t)));
+    const float inv_root_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, t)));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     NvtxRange range("streambp_adamw_step");
     if (cfg->param_dtype == STREAMBP_F32)

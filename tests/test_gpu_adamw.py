@@ -78,7 +78,9 @@ def block_scale(x):
 
 
 def check_step(case, before, step, gs=1.0, h=H):
-    lr, b1, b2, eps = (f32(h[k]) for k in ("lr", "beta1", "beta2", "eps"))
+    # taken in double by the call, which rounds each of beta, 1 - beta and the rates once: what a term's bound counts for its
+    # constant.  (In 32 bits 1 - 0.95 would be 5e-7 off, relatively, before any of it.)
+    lr, b1, b2, eps = (h[k] for k in ("lr", "beta1", "beta2", "eps"))
     for t, old in zip(case.tensors, before):
         g = old["grad"].double().cpu().numpy() * gs
         m = b1 * old["m64"] + (1 - b1) * g
@@ -251,6 +253,44 @@ def test_grad_norm_of_huge_tiny_and_broken_gradients():
     g[999] = float("inf")
     B.grad_norm(c.plan, 1.0, norm, scale, ws)
     assert np.isinf(norm.item()) and np.isnan(scale.item())
+
+
+def plain_mx8(x, keep=False):
+    b = x.view(-1, 32)
+    e = (b.abs().amax(1).view(torch.int32) >> 23).sub(7).clamp(min=1)
+    y = b * ((254 - e) << 23).view(torch.float32)[:, None]
+    if keep:
+        y = torch.where((b > 0) & (y < 2.0 ** -9), 2.0 ** -9, y)
+    return y.to(torch.float8_e4m3fn).view(torch.uint8).view(-1), e.to(torch.uint8)
+
+
+def mx8_values(codes, scale):
+    return (codes.view(torch.float8_e4m3fn).float().view(-1, 32) * (scale.int() << 23).view(torch.float32)[:, None]).view(-1)
+
+
+@pytest.mark.parametrize("size", [1e-14, 1e-7, 1e-3, 1.0, 1e8, 1e15, 2e18])
+def test_codes_are_those_of_the_plain_evaluation(size):
+    """Three steps in 8 bits leave the codes that torch's fp32 operations, each rounded by itself, leave: a tie decided the
+    other way would be an eighth of the value off.  Gradients whose squares are small, ordinary and near the top."""
+    n = 1 << 18
+    g = torch.Generator(device="cuda").manual_seed(int(np.log10(size)) + 50)
+    t = {"param": torch.zeros(n, device="cuda"), "weight_decay": 0.0}
+    t |= {x: torch.zeros(n, dtype=torch.uint8, device="cuda") for x in ("m", "v")}
+    t |= {x: torch.ones(n // 32, dtype=torch.uint8, device="cuda") for x in ("m_scale", "v_scale")}
+    t["grad"] = torch.zeros(n, device="cuda")
+    plan = B.AdamWPlan([t])
+    ref = {x: t[x].clone() for x in ("m", "v", "m_scale", "v_scale")}
+    scale = torch.tensor([0.7], device="cuda")
+    for step in range(1, 4):
+        t["grad"].copy_(torch.randn(n, generator=g, device="cuda") * size)
+        x = t["grad"] * scale
+        m = 0.9 * mx8_values(ref["m"], ref["m_scale"]) + (1 - 0.9) * x
+        v = 0.95 * mx8_values(ref["v"], ref["v_scale"]).square() + (1 - 0.95) * x * x
+        ref["m"], ref["m_scale"] = plain_mx8(m)
+        ref["v"], ref["v_scale"] = plain_mx8(v.sqrt(), keep=True)
+        B.adamw_step(plan, 1e-3, 0.9, 0.95, 1e-8, step, grad_scale=scale)
+        for k, want in ref.items():
+            assert torch.equal(t[k], want), k
 
 
 def test_mx8_codes_stand_for_their_values():
