@@ -161,22 +161,19 @@ __device__ __forceinline__ float fast_sqrt(float x) {
 }
 // Roots of eight values, each rounded to nearest: from an approximate inverse root y, the root v y corrected by its exact
 // residual (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  The residual is
-// exact where it is no subnormal number: eight values of which one is too small or too large go through powers of four.
+// exact where it is no subnormal number: eight values of which one is too small (or 0) or too large go through powers of four.
 __device__ __forceinline__ float corrected_root(float v) {
     float y;
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaxf(v, 1e-28f)));      // 0 stays 0
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v));
     const float s = v * y;
     return fmaf(fmaf(-s, s, v), 0.5f * y, s);
 }
 __device__ __forceinline__ void roots8(float (&v)[8]) {
-    float top = 0.f;
+    constexpr uint32_t kLeast = 0x11000000u, kMost = 0x7d000000u;     // 2^-93 and 2^123 as bits, which order like the values
     bool odd = false;
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-        odd |= v[e] < 1e-28f && v[e] > 0.f;
-        top = max_abs(top, v[e]);
-    }
-    if (!odd && top < 1e37f) {
+    for (int e = 0; e < 8; e++) odd |= __float_as_uint(v[e]) - kLeast > kMost - kLeast;
+    if (!odd) {
 #pragma unroll
         for (int e = 0; e < 8; e++) v[e] = corrected_root(v[e]);
     } else {
@@ -184,7 +181,7 @@ __device__ __forceinline__ void roots8(float (&v)[8]) {
         for (int e = 0; e < 8; e++) {
             const bool small = v[e] < 1.f;
             const float w = corrected_root(v[e] * (small ? 0x1p96f : 0x1p-32f)) * (small ? 0x1p-48f : 0x1p16f);
-            v[e] = isinf(v[e]) ? v[e] : w;
+            v[e] = isinf(v[e]) || v[e] == 0.f ? v[e] : w;
         }
     }
 }
