@@ -1380,12 +1380,13 @@ void edge_of(const WindowShape &w, int unit, int &edge, int &keys) {
     keys = edge < 0 ? unit : (w.sinks % T + unit - 1) / unit * unit;
 }
 
-// The two maps of k or v that end with the sinks and begin with the windows' first row (stand-ins where no tile needs them).
+// The two maps of k or v that end with the sinks and begin with the windows' first row; `all`, unused, where no tile needs them.
 template <int DH>
-bool key_maps(CUtensorMap *edge, CUtensorMap *gap, const bf16 *x, const WindowShape &w, int edge_tile, uint32_t edge_keys, Gap g, uint32_t tile) {
-    const int64_t kv = (int64_t)w.q0 + w.n, from = g.tile < 0 ? 0 : g.from;
-    return tile_map<DH>(edge, x, edge_tile < 0 ? kv : w.sinks, w.Hkv, edge_keys) &&
-           tile_map<DH>(gap, x + from * w.Hkv * DH, kv - from, w.Hkv, tile);
+bool key_maps(CUtensorMap *edge, CUtensorMap *gap, const CUtensorMap &all, const bf16 *x, const WindowShape &w, int edge_tile, uint32_t edge_keys,
+              Gap g, uint32_t tile) {
+    *edge = *gap = all;
+    return (edge_tile < 0 || tile_map<DH>(edge, x, w.sinks, w.Hkv, edge_keys)) &&
+           (g.tile < 0 || tile_map<DH>(gap, x + (int64_t)g.from * w.Hkv * DH, (int64_t)w.q0 + w.n - g.from, w.Hkv, tile));
 }
 
 template <int DH>
@@ -1438,8 +1439,8 @@ int fwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const WindowShape &w, b
     edge_of<KT>(w, 16, p.edge, p.edge_keys);
     CUtensorMap mq, mk, mv, ke, ve, kg, vg, mo;
     if (!make_heads_map(&mq, q, w.n, w.Hq, DH, 64, (uint32_t)p.heads, (uint32_t)p.tokens, false) || !tile_map<DH>(&mk, k, kv, w.Hkv, KT) ||
-        !tile_map<DH>(&mv, v, kv, w.Hkv, KT) || !key_maps<DH>(&ke, &kg, k, w, p.edge, (uint32_t)p.edge_keys, p.gap, KT) ||
-        !key_maps<DH>(&ve, &vg, v, w, p.edge, (uint32_t)p.edge_keys, p.gap, KT))
+        !tile_map<DH>(&mv, v, kv, w.Hkv, KT) || !key_maps<DH>(&ke, &kg, mk, k, w, p.edge, (uint32_t)p.edge_keys, p.gap, KT) ||
+        !key_maps<DH>(&ve, &vg, mv, v, w, p.edge, (uint32_t)p.edge_keys, p.gap, KT))
         return STREAMBP_E_CUDA;
     if (p.split > 1) {
         static PerDevice configured;
@@ -1477,8 +1478,8 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
     auto rows_map = [&](CUtensorMap *x, const bf16 *a, uint32_t rows) { return make_heads_map(x, a, w.n, w.Hq, DH, 64, heads, rows, false); };
     if (!rows_map(&m[0], q, tokens) || !tile_map<DH>(&m[1], k, kv, w.Hkv, TILE) || !tile_map<DH>(&m[2], v, kv, w.Hkv, TILE) ||
         !rows_map(&m[3], dout, tokens) || !rows_map(&m[4], q, (uint32_t)p.work.tq) || !tile_map<DH>(&m[5], k, kv, w.Hkv, IT) ||
-        !tile_map<DH>(&m[6], v, kv, w.Hkv, IT) || !rows_map(&m[7], dout, (uint32_t)p.work.tq) || !key_maps<DH>(&m[8], &m[14], k, w, p.edge, edge, p.gap, IT) ||
-        !key_maps<DH>(&m[9], &m[15], v, w, p.edge, edge, p.gap, IT))
+        !tile_map<DH>(&m[6], v, kv, w.Hkv, IT) || !rows_map(&m[7], dout, (uint32_t)p.work.tq) || !key_maps<DH>(&m[8], &m[14], m[5], k, w, p.edge, edge, p.gap, IT) ||
+        !key_maps<DH>(&m[9], &m[15], m[6], v, w, p.edge, edge, p.gap, IT))
         return STREAMBP_E_CUDA;
     const bool f32 = mode != GRAD_BF16_SET;
     const CUtensorMapSwizzle swizzle = f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
