@@ -1541,10 +1541,7 @@ int bwd_any(const bf16 *q, const bf16 *k, const bf16 *v, const bf16 *o, const bf
         SBP_LAUNCH(kernel, (unsigned)(n_dkdv + n_dq), W::kThreads, W::kSmem, st, m[0], m[1], m[2], m[3], m[4], m[5], m[6], m[7], m[8], m[9],
                    m[14], m[15], m[10], m[11], m[12], m[13], p);
     }
-    const auto &k_ = p.work;
-    if (k_.segs > 1 || k_.wsegs > 1)
-        return attention_window_join(part, TILE, k_.st, k_.segs, k_.wt0, k_.wsegs, p.part_rows, w, DH, mode, dk, dv, st);
-    return STREAMBP_OK;
+    return attention_window_join(part, p.work, w, DH, mode, dk, dv, st);
 }
 
 }  // namespace

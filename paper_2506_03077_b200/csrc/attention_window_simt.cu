@@ -347,25 +347,22 @@ int bwd(const T *q, const T *k, const T *v, const T *o, const T *dout, const flo
                work, dk, dv, mode, part, part_rows);
     SBP_LAUNCH((window_dq_kernel<T, DH>), dim3((w.n + TILE - 1) / TILE, w.Hq), 256, smem, st, q, k, v, dout, lse,
                (const float *)delta, w, dq, mode);
-    if (work.segs > 1)
-        return attention_window_join(part, TILE, work.st, work.segs, work.wt0, work.wsegs, part_rows, w, DH, mode, dk, dv, st);
-    return STREAMBP_OK;
+    return attention_window_join(part, work, w, DH, mode, dk, dv, st);
 }
 
 }  // namespace
 
-int attention_window_join(const float *part, int tile, int st, int segs, int wt0, int wsegs, int rows, const WindowShape &w, int dh,
-                          int mode, void *dk, void *dv, cudaStream_t stream) {
-    // keys of the leading tiles: all of them where every row is joined, else the sinks
-    const int64_t kv = (int64_t)w.q0 + w.n, whole = (int64_t)st * tile < kv ? (int64_t)st * tile : kv;
-    const int64_t lead = segs > 1 ? (wsegs > 1 ? whole : w.sinks) : 0, behind = wsegs > 1 ? kv - (int64_t)wt0 * tile : 0;
-    const int64_t count = (lead + behind) * w.Hkv * (dh / 2), blocks = (count + 255) / 256;
+template <int TK>
+int attention_window_join(const float *part, const KeyWork<TK> &work, const WindowShape &w, int dh, int mode, void *dk, void *dv,
+                          cudaStream_t stream) {
+    const int64_t lead = work.join_lead(w), count = (lead + work.join_behind(w)) * w.Hkv * (dh / 2), blocks = (count + 255) / 256;
     if (blocks > 0x7fffffff) return STREAMBP_E_SHAPE;
     if (count == 0) return STREAMBP_OK;
-    SBP_LAUNCH(window_join_kernel, (unsigned)blocks, 256, 0, stream, part, tile, st, segs, wt0, wsegs, (int)lead, rows, w.Hkv, dh, count, dk,
-               dv, mode);
+    SBP_LAUNCH(window_join_kernel, (unsigned)blocks, 256, 0, stream, part, TK, work.st, work.segs, work.wt0, work.wsegs, (int)lead,
+               work.slot_rows(w), w.Hkv, dh, count, dk, dv, mode);
     return STREAMBP_OK;
 }
+template int attention_window_join<128>(const float *, const KeyWork<128> &, const WindowShape &, int, int, void *, void *, cudaStream_t);
 
 template <typename T>
 int attention_window_fwd_simt(const T *q, const T *k, const T *v, const WindowShape &w, int dh, T *o, float *lse, cudaStream_t st) {

@@ -466,10 +466,12 @@ template <typename T>
 int attention_window_bwd_simt(const T *q, const T *k, const T *v, const T *o, const T *dout, const float *lse, const WindowShape &w,
                               int dh, int mode, void *dq, void *dk, void *dv, float *delta, float *part, WsHeader *hdr,
                               cudaStream_t st);
-// Sums of key tiles whose work is cut: segments added in their order, then to where the gradients go.  Tiles are `tile` keys,
-// the first `st` with `segs` segments, the others, from `wt0`, with `wsegs`; `rows` rows to a workspace slot.
-int attention_window_join(const float *part, int tile, int st, int segs, int wt0, int wsegs, int rows, const WindowShape &w, int dh,
-                          int mode, void *dk, void *dv, cudaStream_t stream);
+// Sums of key tiles whose work is cut: segments added in their order, then to where the gradients go.  Nothing is launched
+// where no key's work is.
+template <int TK> struct KeyWork;
+template <int TK>
+int attention_window_join(const float *part, const KeyWork<TK> &work, const WindowShape &w, int dh, int mode, void *dk, void *dv,
+                          cudaStream_t stream);
 
 // LM head pieces
 int count_valid_labels(const int64_t *labels, int64_t T, int64_t vocab, int64_t ignore, WsHeader *hdr,

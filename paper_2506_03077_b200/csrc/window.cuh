@@ -78,6 +78,16 @@ template <int TK> struct KeyWork {
         const int r = full() ? TK : w.sinks - kt * TK;
         return r < TK ? (r > 0 ? r : 0) : TK;
     }
+    // Keys whose sums are joined: the first join_lead, of the sink tiles (all of their rows, or the sinks), and the join_behind
+    // from tile wt0 on
+    SBP_HD long long join_lead(const WindowShape &w) const {
+        const long long kv = (long long)w.q0 + w.n, whole = (long long)st * TK < kv ? (long long)st * TK : kv;
+        return segs > 1 ? (full() ? whole : w.sinks) : 0;
+    }
+    SBP_HD long long join_behind(const WindowShape &w) const {
+        const long long behind = (long long)w.q0 + w.n - (long long)wt0 * TK;
+        return full() && behind > 0 ? behind : 0;          // none where the sink tiles are all the tiles, the last of them a short one
+    }
     SBP_HD int slot_rows(const WindowShape &w) const { return full() || w.sinks > TK ? TK : w.sinks; }
     // floats of the workspace: [item][Hkv][dK, dV][slot_rows][dh]
     size_t part_floats(const WindowShape &w, int dh) const {
