@@ -168,7 +168,8 @@ class ShardedAdamW:
     """One AdamW step of a layer's parameters, each rank on its shard of the summed gradients: the moments and the fp32
     master copy exist once over all ranks.  `shard` is what DataParallelLayerBackward.exchange leaves (wait() first).
     step() clips by the norm over the whole layer (an all-reduce of one number), updates this rank's slice on the library's
-    kernels and gathers the rounded parameters of all ranks.  A norm that is not finite leaves every rank's slice as it was.
+    kernels and gathers the rounded parameters of all ranks.  A norm that is not finite leaves every rank's slice as it was, and
+    the step does not count (`steps`, on the device: the updates so far).
 
     weight_decay: per tensor name (missing: 0).  bits: 32, or 8 for moments in blocks of 32 e4m3 codes."""
 
@@ -218,7 +219,7 @@ class ShardedAdamW:
             self.norm.copy_(total.sqrt_())
             # what grad_norm writes for one rank; norm - norm is NaN where the norm is not finite
             self.scale.copy_((max_norm / (self.norm + 1e-6)).clamp_(max=1.0) + (self.norm - self.norm))
-        self.steps += 1
+        self.steps += torch.isfinite(self.scale)          # on the device: the host does not wait for the norm
         if self.plan is not None:
             self.B.adamw_step(self.plan, lr, beta1, beta2, eps, self.steps, grad_scale=self.scale)
         if self.world > 1:
