@@ -154,31 +154,28 @@ __device__ __forceinline__ uint32_t block_max2(uint32_t v) {
 struct Rates {
     float gs, lr, b1, b2, rest1, rest2, eps, step_size, inv_root_bc2;
 };
-__device__ __forceinline__ float fast_sqrt(float x) {
-    float y;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// Roots of eight values, each rounded to nearest: from an approximate inverse root y, the root v y corrected by its exact
+// Roots of N values, each rounded to nearest: from an approximate inverse root y, the root v y corrected by its exact
 // residual (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  The residual is
-// exact where it is no subnormal number: eight values of which one is too small (or 0) or too large go through powers of four.
+// exact where it is no subnormal number: values of which one is too small (or 0) or too large go through powers of four, so that
+// subnormal second moments (gradients around 1e-19) have their roots too.
 __device__ __forceinline__ float corrected_root(float v) {
     float y;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v));
     const float s = v * y;
     return fmaf(fmaf(-s, s, v), 0.5f * y, s);
 }
-__device__ __forceinline__ void roots8(float (&v)[8]) {
+template <int N>
+__device__ __forceinline__ void roots(float (&v)[N]) {
     constexpr uint32_t kLeast = 0x11000000u, kMost = 0x7d000000u;     // 2^-93 and 2^123 as bits, which order like the values
     bool odd = false;
 #pragma unroll
-    for (int e = 0; e < 8; e++) odd |= __float_as_uint(v[e]) - kLeast > kMost - kLeast;
+    for (int e = 0; e < N; e++) odd |= __float_as_uint(v[e]) - kLeast > kMost - kLeast;
     if (!odd) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = corrected_root(v[e]);
+        for (int e = 0; e < N; e++) v[e] = corrected_root(v[e]);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
+        for (int e = 0; e < N; e++) {
             const bool small = v[e] < 1.f;
             const float w = corrected_root(v[e] * (small ? 0x1p96f : 0x1p-32f)) * (small ? 0x1p-48f : 0x1p16f);
             v[e] = isinf(v[e]) || v[e] == 0.f ? v[e] : w;
@@ -223,13 +220,16 @@ __device__ __forceinline__ void step_piece_f32(const streambp_adamw_tensor &t, l
     }
 #pragma unroll
     for (int k = 0; k < kUnroll; k++) {
+        float u[4];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const float x = g[k][e] * r.gs;
             m[k][e] = fmaf(r.b1, m[k][e], r.rest1 * x);
-            v[k][e] = fmaf(r.b2, v[k][e], r.rest2 * x * x);
-            p[k][e] = moved(r, p[k][e], decay, m[k][e], fast_sqrt(v[k][e]));
+            u[e] = v[k][e] = fmaf(r.b2, v[k][e], r.rest2 * x * x);
         }
+        roots(u);
+#pragma unroll
+        for (int e = 0; e < 4; e++) p[k][e] = moved(r, p[k][e], decay, m[k][e], u[e]);
         store4(mp + off[k], valid[k], m[k]);
         store4(vp + off[k], valid[k], v[k]);
         if constexpr (MASTER) store4(master + off[k], valid[k], p[k]);
@@ -291,7 +291,7 @@ __device__ __forceinline__ void step_piece_mx8(const streambp_adamw_tensor &t, l
             m[e] = __fadd_rn(__fmul_rn(r.b1, m[e]), __fmul_rn(r.rest1, g[e]));
             u[e] = __fadd_rn(__fmul_rn(r.b2, __fmul_rn(u[e], u[e])), __fmul_rn(__fmul_rn(r.rest2, g[e]), g[e]));
         }
-        roots8(u);
+        roots(u);
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             p[e] = moved(r, p[e], decay, m[e], u[e]);
