@@ -36,8 +36,11 @@ struct StepParams {
     int piece_begin[CAP + 1];        // pieces of tensor i: piece_begin[i] .. piece_begin[i + 1] - 1
     int n;
     double lr64, beta1_64, beta2_64; // for a step number on the device
-    float lr, beta1, beta2, rest1, rest2, eps;      // rest: 1 - beta
-    float step_size, inv_root_bc2;   // lr / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
+    float lr, beta1, beta2, rest1, rest2;           // rest: 1 - beta
+    // power times eps, lr / (1 - beta1^step) and 1 / sqrt(1 - beta2^step): a power of two that keeps the divisor in the range of
+    // the reciprocal, which reads subnormal numbers as zero and gives zero for results that are some (1 but for extreme eps)
+    double power;
+    float eps, step_size, inv_root_bc2;
     const float *grad_scale;         // optional
     const int64_t *step;             // optional: the step number is read from the device
 };
@@ -359,8 +362,8 @@ __global__ void __launch_bounds__(kThreads, MX8 ? 4 : 3) adamw_kernel(const __gr
         if (threadIdx.x == 0) {
             const long long t = *a.step;
             const double n = t < 1 ? 1.0 : (double)t;
-            s_rate[0] = (float)(a.lr64 / (1.0 - pow(a.beta1_64, n)));
-            s_rate[1] = (float)(1.0 / sqrt(1.0 - pow(a.beta2_64, n)));
+            s_rate[0] = (float)(a.power * a.lr64 / (1.0 - pow(a.beta1_64, n)));
+            s_rate[1] = (float)(a.power / sqrt(1.0 - pow(a.beta2_64, n)));
         }
         __syncthreads();
         r.step_size = s_rate[0];
@@ -575,7 +578,7 @@ int grid_for(int64_t pieces, int per_sm) {
 // launch, and the usual layer of a dozen tensors should not pay for two hundred.
 template <typename P, bool MX8, int CAP>
 int launch_adamw(const streambp_adamw_cfg &c, const streambp_adamw_tensor *tensors, int n, const float *grad_scale,
-                 const int64_t *step, float step_size, float inv_root_bc2, cudaStream_t st) {
+                 const int64_t *step, double power, double step_size, double inv_root_bc2, cudaStream_t st) {
     StepParams<CAP> a;
     int i = 0;
     while (i < n) {
@@ -592,10 +595,12 @@ int launch_adamw(const streambp_adamw_cfg &c, const streambp_adamw_tensor *tenso
         if (a.n == 0) break;
         a.piece_begin[a.n] = (int)pieces;
         a.lr64 = c.lr; a.beta1_64 = c.beta1; a.beta2_64 = c.beta2;
-        a.lr = (float)c.lr; a.beta1 = (float)c.beta1; a.beta2 = (float)c.beta2; a.eps = (float)c.eps;
+        a.lr = (float)c.lr; a.beta1 = (float)c.beta1; a.beta2 = (float)c.beta2;
         a.rest1 = (float)(1.0 - c.beta1); a.rest2 = (float)(1.0 - c.beta2);
-        a.step_size = step_size;
-        a.inv_root_bc2 = inv_root_bc2;
+        a.power = power;
+        a.eps = (float)power * (float)c.eps;           // of eps in 32 bits, as the rest of the step takes it
+        a.step_size = (float)(power * step_size);
+        a.inv_root_bc2 = (float)(power * inv_root_bc2);
         a.grad_scale = grad_scale;
         a.step = step;
         SBP_LAUNCH((adamw_kernel<P, MX8, CAP>), grid_for(pieces, 8), kThreads, 0, st, a);
@@ -640,9 +645,9 @@ int launch_norm(const float *const *grads, const int64_t *counts, int n, double 
 }
 template <typename P, bool MX8>
 int launch_adamw_any(const streambp_adamw_cfg &c, const streambp_adamw_tensor *tensors, int n, const float *grad_scale,
-                     const int64_t *step, float step_size, float inv_root_bc2, cudaStream_t st) {
-    if (n <= 32) return launch_adamw<P, MX8, 32>(c, tensors, n, grad_scale, step, step_size, inv_root_bc2, st);
-    return launch_adamw<P, MX8, 256>(c, tensors, n, grad_scale, step, step_size, inv_root_bc2, st);
+                     const int64_t *step, double power, double step_size, double inv_root_bc2, cudaStream_t st) {
+    if (n <= 32) return launch_adamw<P, MX8, 32>(c, tensors, n, grad_scale, step, power, step_size, inv_root_bc2, st);
+    return launch_adamw<P, MX8, 256>(c, tensors, n, grad_scale, step, power, step_size, inv_root_bc2, st);
 }
 
 }  // namespace
@@ -674,15 +679,18 @@ int streambp_adamw_step(const streambp_adamw_cfg *cfg, const streambp_adamw_tens
     }
     begin_call();
     const double t = step ? 1.0 : (double)cfg->step;
-    const float step_size = (float)(cfg->lr / (1.0 - std::pow(cfg->beta1, t)));
-    const float inv_root_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, t)));
+    const double step_size = cfg->lr / (1.0 - std::pow(cfg->beta1, t));
+    const double inv_root_bc2 = 1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, t));
+    // a root is at most 2^64 and its factor below 2^30, so only eps takes a divisor out of 2^-126 .. 2^126 (a root that is not zero is
+    // at least 2^-75), and 2^24 brings the smallest one back (a rate that this would overflow keeps its own power)
+    const double power = cfg->eps > 0x1p125 ? 0x1p-8 : (cfg->eps > 0.0 && cfg->eps < 0x1p-126 && step_size < 0x1p100 ? 0x1p24 : 1.0);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     NvtxRange range("streambp_adamw_step");
     if (cfg->param_dtype == STREAMBP_F32)
-        return mx8 ? launch_adamw_any<float, true>(*cfg, tensors, n, grad_scale, step, step_size, inv_root_bc2, st)
-                   : launch_adamw_any<float, false>(*cfg, tensors, n, grad_scale, step, step_size, inv_root_bc2, st);
-    return mx8 ? launch_adamw_any<bf16, true>(*cfg, tensors, n, grad_scale, step, step_size, inv_root_bc2, st)
-               : launch_adamw_any<bf16, false>(*cfg, tensors, n, grad_scale, step, step_size, inv_root_bc2, st);
+        return mx8 ? launch_adamw_any<float, true>(*cfg, tensors, n, grad_scale, step, power, step_size, inv_root_bc2, st)
+                   : launch_adamw_any<float, false>(*cfg, tensors, n, grad_scale, step, power, step_size, inv_root_bc2, st);
+    return mx8 ? launch_adamw_any<bf16, true>(*cfg, tensors, n, grad_scale, step, power, step_size, inv_root_bc2, st)
+               : launch_adamw_any<bf16, false>(*cfg, tensors, n, grad_scale, step, power, step_size, inv_root_bc2, st);
 }
 
 size_t streambp_grad_norm_workspace_bytes(void) { return kHeaderBytes + sizeof(double) * 4096; }

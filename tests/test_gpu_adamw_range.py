@@ -1,4 +1,4 @@
-"""AdamW at the ends of the range of fp32: second moments below the smallest normal number."""
+"""AdamW at the ends of the range of fp32: second moments and divisors below the smallest normal number."""
 import numpy as np
 import pytest
 import torch
@@ -33,3 +33,27 @@ def test_second_moments_below_the_normal_range(eps, n):
     move = 10 * m[seen] / (np.sqrt(v[seen] / (1 - 0.95)) + eps)
     assert np.isfinite(p[seen]).all()
     assert (np.abs(p[seen] + move) <= 8 * E32 * np.abs(move)).all()
+
+
+@pytest.mark.parametrize("state", ["f32", "mx8"])
+@pytest.mark.parametrize("eps,lr,least,most", [(1e-39, 1e-17, -37, -24), (1e-40, 1e-17, -37, -24), (2.0 ** -130, 1e-17, -37, -24),
+                                               (1e38, 1e37, -3, 0)])
+def test_divisors_outside_the_normal_range(eps, lr, least, most, state):
+    """eps alone is the divisor: beside a small one the squares of the gradients vanish in fp32, beside a huge one their roots
+    do.  A parameter without a gradient stays, the others move by lr g / eps.  Bound: a small eps is the subnormal number
+    that fp32 makes of it, so may m be for the smallest gradients (half a step of them); the constant and the product of m are two
+    roundings, the reciprocal's ulp two, the product with m and the rate two; the parameter's own is one of the result."""
+    n = 1024
+    g = torch.logspace(least, most, n, device="cuda")
+    g[::5] = 0
+    t = {"param": torch.ones(n, device="cuda"), "grad": g}
+    if state == "f32":
+        t |= {k: torch.zeros(n, device="cuda") for k in ("m", "v")}
+    else:
+        t |= {k: torch.zeros(n, dtype=torch.uint8, device="cuda") for k in ("m", "v")}
+        t |= {k: torch.ones(n // 32, dtype=torch.uint8, device="cuda") for k in ("m_scale", "v_scale")}
+    B.adamw_step(B.AdamWPlan([t]), lr, 0.9, 0.95, eps, 1)
+    p, x, eps = t["param"].double().cpu().numpy(), g.double().cpu().numpy(), float(np.float32(eps))
+    move = lr * x / eps
+    assert (p[x == 0] == 1).all() and move.max() > 1e-3
+    assert (np.abs(p - (1 - move)) <= 6.01 * E32 * move + 10 * lr / eps * 2.0 ** -150 + E32 * np.abs(1 - move)).all()
