@@ -1,10 +1,11 @@
-"""AdamW at the ends of the range of fp32: second moments and divisors below the smallest normal number."""
+"""AdamW at the ends of the range of fp32: second moments and divisors below the smallest normal number, roots at the ties
+of the codes."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2506_03077_b200 import binding as B
-from test_gpu_adamw import E32
+from test_gpu_adamw import E32, mx8_values, plain_mx8
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +58,24 @@ def test_divisors_outside_the_normal_range(eps, lr, least, most, state):
     move = lr * x / eps
     assert (p[x == 0] == 1).all() and move.max() > 1e-3
     assert (np.abs(p - (1 - move)) <= 6.01 * E32 * move + 10 * lr / eps * 2.0 ** -150 + E32 * np.abs(1 - move)).all()
+
+
+def test_roots_at_the_ties_of_the_codes():
+    """With beta2 = 0 the new second moment is x^2 rounded, and its root rounded to nearest is x again.  x lies halfway
+    between two codes of its block, and a bit to either side, in every exponent that squares allow: a root that is off in its
+    last bit leaves another code."""
+    xs = []
+    for e in range(-60, 61):
+        for mant in range(8):
+            tie = np.float32((1 + (mant + 0.5) / 8) * 2.0 ** e)
+            xs += [np.nextafter(tie, np.float32(0)), tie, np.nextafter(tie, np.float32(np.inf)), np.float32(1.75 * 2.0 ** e)]
+    n = len(xs)
+    assert n % 32 == 0                            # one exponent to a block
+    x = torch.from_numpy(np.array(xs, dtype=np.float32)).cuda()
+    t = {"param": torch.zeros(n, device="cuda"), "grad": x, "weight_decay": 0.0}
+    t |= {k: torch.zeros(n, dtype=torch.uint8, device="cuda") for k in ("m", "v")}
+    t |= {k: torch.ones(n // 32, dtype=torch.uint8, device="cuda") for k in ("m_scale", "v_scale")}
+    B.adamw_step(B.AdamWPlan([t]), 1e-3, 0.9, 0.0, 1e-8, 1)
+    codes, scale = plain_mx8(x, keep=True)
+    assert torch.equal(t["v"], codes) and torch.equal(t["v_scale"], scale)
+    assert torch.equal(mx8_values(t["v"], t["v_scale"]), mx8_values(codes, scale))
