@@ -521,8 +521,9 @@ int streambp_grad_norm(const float *const *grads, const int64_t *counts, int32_t
 
 /*
  * Values <-> the 8-bit form above, for starting a state from given moments, checkpoints and inspection.  keep_nonzero:
- * positive values are held as at least the smallest code (the rule of the second moment's root).  out_dtype float or
- * bf16 (both exact).
+ * positive values are held as at least the smallest code (the rule of the second moment's root).  out_dtype float (exact)
+ * or bf16 (exact for scale bytes of 3 and more; below, codes finer than bf16's smallest number 2^-133 are rounded, the
+ * smallest to 0).
  */
 int streambp_mx8_encode(const float *values, int64_t count, int32_t keep_nonzero, uint8_t *codes, uint8_t *scales,
                         void *cuda_stream);

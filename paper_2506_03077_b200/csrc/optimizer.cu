@@ -8,7 +8,8 @@
 //
 // Moments in 8 bits: blocks of 32 consecutive elements of a tensor share a power of two 2^(s - 127) (one byte s) and
 // hold e4m3 codes.  s = (biased exponent of the block's largest magnitude) - 7, at least 1: the largest code is then
-// below 256 and never saturates, and decoding is exact in fp32 and in bf16.  The second moment is held as its ROOT,
+// below 256 and never saturates, and decoding is exact in fp32, and in bf16 for s of 3 and more (below, the smallest codes are
+// finer than bf16's 2^-133: rounded).  The second moment is held as its ROOT,
 // which halves the exponent range it needs (17 octaves from the smallest code to the largest are 34 of v), and a root
 // that is not zero is held as at least the smallest code 2^-9: a second moment rounded to zero beside a first moment
 // that is not would make the next step's quotient jump by 1 / sqrt(1 - beta2).

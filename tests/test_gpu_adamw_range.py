@@ -79,3 +79,20 @@ def test_roots_at_the_ties_of_the_codes():
     codes, scale = plain_mx8(x, keep=True)
     assert torch.equal(t["v"], codes) and torch.equal(t["v_scale"], scale)
     assert torch.equal(mx8_values(t["v"], t["v_scale"]), mx8_values(codes, scale))
+
+
+def test_codes_under_the_smallest_scales():
+    """Every code under scale bytes 1 .. 4: fp32 holds them all, bf16 those under 3 and more; finer ones are rounded to nearest."""
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda").repeat(4)
+    scales = torch.arange(1, 5, dtype=torch.uint8, device="cuda").repeat_interleave(8)
+    ref = codes.view(torch.float8_e4m3fn).double() * torch.exp2(scales.double() - 127).repeat_interleave(32)
+    some = ~torch.isnan(ref)
+    out, rounded = torch.empty(1024, device="cuda"), torch.empty(1024, device="cuda", dtype=torch.bfloat16)
+    B.mx8_decode(codes, scales, out)
+    B.mx8_decode(codes, scales, rounded)
+    assert torch.equal(out.double()[some], ref[some]) and bool(torch.isnan(out[~some]).all())
+    # multiples of 2^-135 against bf16's of 2^-133, ties to even
+    want = torch.where(ref.abs() < 2.0 ** -126, torch.round(ref * 2.0 ** 133) * 2.0 ** -133, ref)
+    assert torch.equal(rounded.double()[some], want[some]) and bool(torch.isnan(rounded[~some]).all())
+    exact = some & (torch.arange(1024, device="cuda") >= 512)
+    assert torch.equal(rounded.double()[exact], ref[exact]) and not torch.equal(rounded.double()[some], ref[some])
