@@ -67,10 +67,11 @@ __device__ __forceinline__ float slope(float z) {
             return fmaf(z * kInvSqrt2Pi, bell, c);
         } else return fmaf(z * kInvSqrt2Pi, expf(-0.5f * z * z), 0.5f * (1.f + erff(z * kSqrtHalf)));
     } else if constexpr (ACT == STREAMBP_ACT_GELU_TANH) {
-        // with s = sigmoid(2a): 0.5 (1 + tanh a) = s and 0.5 (1 - tanh^2 a) = 2 s (1 - s)
-        const float z2 = z * z, a = kGeluA * fmaf(kGeluB * z2, z, z);
-        const float s = sigmoid<FAST>(2.f * a);
-        return fmaf(2.f * z * s * (1.f - s), kGeluA * fmaf(3.f * kGeluB, z2, 1.f), s);
+        // with s = sigmoid(2a): 0.5 (1 + tanh a) = s and 0.5 (1 - tanh^2 a) = 2 s (1 - s).  The factors z of z^2 are applied to
+        // z s (1 - s) one by one: that is zero long before z^2 overflows, and zero times infinity is not.
+        const float a = kGeluA * fmaf(kGeluB * z * z, z, z);
+        const float s = sigmoid<FAST>(2.f * a), w = z * s * (1.f - s);
+        return fmaf(2.f * kGeluA, fmaf(3.f * kGeluB * z, z * w, w), s);
     } else if constexpr (ACT == STREAMBP_ACT_SILU) {
         const float s = sigmoid<FAST>(z);
         return s * fmaf(z, 1.f - s, 1.f);
