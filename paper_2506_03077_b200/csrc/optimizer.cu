@@ -470,7 +470,7 @@ __device__ __forceinline__ void put_norm(double squares, float max_norm, float *
     if (!scale) return;
     // of the norm as it is given, in fp32: whoever forms the factor from it has the same
     if (!isfinite(s)) *scale = __uint_as_float(0x7fc00000u);
-    else if (isinf(n)) *scale = (float)((double)max_norm / s);
+    else if (isinf(n)) *scale = fminf(1.f, (float)((double)max_norm / s));      // (max_norm may be infinite)
     else *scale = fminf(1.f, __fmul_rn(__frcp_rn(__fadd_rn(n, 1e-6f)), max_norm));
 }
 // Few pieces, one to each team of kThreads in a cluster, whose blocks' shares are added in their order.  One launch where the

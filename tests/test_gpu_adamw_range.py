@@ -96,3 +96,22 @@ def test_codes_under_the_smallest_scales():
     assert torch.equal(rounded.double()[some], want[some]) and bool(torch.isnan(rounded[~some]).all())
     exact = some & (torch.arange(1024, device="cuda") >= 512)
     assert torch.equal(rounded.double()[exact], ref[exact]) and not torch.equal(rounded.double()[some], ref[some])
+
+
+@pytest.mark.parametrize("n", [1000, 200_000])
+@pytest.mark.parametrize("most", [float("inf"), 3e38, 1.0])
+def test_norms_that_overflow_fp32(n, most):
+    """A finite sum of squares whose root is above fp32's range: the norm is infinite, the factor what the formula gives, 1 for
+    no bound.  One launch and several."""
+    t = {"param": torch.zeros(n, device="cuda"), "grad": torch.full((n,), 1e38, device="cuda")}
+    t |= {k: torch.zeros(n, device="cuda") for k in ("m", "v")}
+    plan, ws = B.AdamWPlan([t]), B.alloc_workspace(B.grad_norm_workspace_bytes())
+    norm, scale = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    B.grad_norm(plan, most, norm, scale, ws)
+    want = min(1.0, float(np.float32(most)) / (float(np.float32(1e38)) * np.sqrt(float(n))))
+    assert np.isinf(norm.item())
+    # the result's rounding, of a subnormal number where the bound is small
+    assert abs(scale.item() - want) <= E32 * want * 1.01 + 2.0 ** -150
+    t["grad"].fill_(1e-3)
+    B.grad_norm(plan, float("inf"), norm, scale, ws)
+    assert scale.item() == 1.0
