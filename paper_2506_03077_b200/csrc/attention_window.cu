@@ -1317,14 +1317,9 @@ __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
     const int b = (int)blockIdx.x;
     const bool dq_role = b < p.n_dq_first || b >= p.n_dq_first + p.n_dkdv && !(PACKED && p.split > 1);
     if (!dq_role) {
-        const int c = b - p.n_dq_first;
+        const int c = b - p.n_dq_first;                       // no cluster holds both roles: the dQ CTAs fill theirs
         if (!PACKED || c < p.n_dkdv)
             dkdv_body<DH, PACKED>(map_qi, map_k, map_v, map_doi, map_dk, map_dv, map_part, p, smem_raw, c / p.w.Hkv, c % p.w.Hkv);
-        if (PACKED && p.split > 1) {                          // the two barriers of a cluster whose last CTAs have the dQ role
-            __syncwarp();
-            cluster_sync_all();
-            cluster_sync_all();
-        }
     } else {
         const int i = b < p.n_dq_first ? b : b - p.n_dkdv, tiles = (p.w.n + p.template tokens<PACKED>() - 1) / p.template tokens<PACKED>();
         const int c = PACKED ? i / p.split : i;
