@@ -360,7 +360,10 @@ int window_shape(int64_t n, int64_t q0, int32_t Hq, int32_t Hkv, int32_t dh, int
     return STREAMBP_OK;
 }
 // scratch of the windowed backward: delta, then the sums of the sink segments (the larger of the two engines' needs)
-struct WindowScratch { float *delta, *part; };
+struct WindowScratch {
+    float *delta, *part;
+    std::vector<size_t> guards;   // debug mode: offsets of the guards behind the sub-buffers
+};
 size_t window_scratch(const WindowShape &w, int dh, void *base, WindowScratch *out) {
     Arena a(base);
     a.take_bytes(kHeaderBytes);
@@ -369,6 +372,19 @@ size_t window_scratch(const WindowShape &w, int dh, void *base, WindowScratch *o
                               : key_work<128>(w, kBwdRows128, bwd_heads(w, kBwdRows128), kBwdSlots128).part_floats(w, dh),
                  y = key_work<32>(w, 32, 1, 0).part_floats(w, dh);
     out->part = a.take<float>(x > y ? x : y);
+    out->guards = a.guards;
+    return a.size();
+}
+// scratch of the epilogue's gradient: the row splits' column sums, rows of two classes (epilogue_bwd.cu)
+struct EpilogueScratch {
+    float *partials;
+    std::vector<size_t> guards;
+};
+size_t epilogue_scratch(int64_t M, int64_t N, void *base, EpilogueScratch *out) {
+    Arena a(base);
+    a.take_bytes(kHeaderBytes);
+    out->partials = a.take<float>((size_t)gemm_epilogue_splits(M, N) * 2 * (size_t)N);
+    out->guards = a.guards;
     return a.size();
 }
 
@@ -775,14 +791,17 @@ int streambp_attention_window_backward(const void *q, const void *k, const void 
     call_state().launches = 0;
     WsHeader *hdr = static_cast<WsHeader *>(workspace);
     const int mode = grad_dtype == STREAMBP_BF16 ? GRAD_BF16_SET : (accumulate ? GRAD_F32_ADD : GRAD_F32_SET);
+    SBP_TRY(ws_guards_arm(workspace, s.guards, st));      // (a kernel of the call clears the status, which the check may set)
     if (tc)
-        return attention_window_bwd_tc((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o, lse, w,
-                                       head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
-    if (dtype == STREAMBP_BF16)
-        return attention_window_bwd_simt<bf16>((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o,
-                                               lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
-    return attention_window_bwd_simt<float>((const float *)q, (const float *)k, (const float *)v, (const float *)o,
-                                            (const float *)d_o, lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st);
+        SBP_TRY(attention_window_bwd_tc((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o, lse, w,
+                                        head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st));
+    else if (dtype == STREAMBP_BF16)
+        SBP_TRY(attention_window_bwd_simt<bf16>((const bf16 *)q, (const bf16 *)k, (const bf16 *)v, (const bf16 *)o, (const bf16 *)d_o,
+                                                lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st));
+    else
+        SBP_TRY(attention_window_bwd_simt<float>((const float *)q, (const float *)k, (const float *)v, (const float *)o,
+                                                 (const float *)d_o, lse, w, head_dim, mode, dq, dk, dv, s.delta, s.part, hdr, st));
+    return ws_guards_check(workspace, s.guards, hdr, st);
 }
 
 int streambp_product_kernel(void) { return gemm_tc_variant(); }
@@ -925,10 +944,8 @@ int streambp_gemm_epilogue(const void *A, int64_t lda, const void *W, int64_t ld
 
 size_t streambp_gemm_epilogue_workspace_bytes(int64_t M, int64_t N) {
     if (M < 1 || N < 1 || M > (1ll << 30) || N > (1ll << 30)) return 0;
-    Arena a(nullptr);
-    a.take_bytes(kHeaderBytes);
-    a.take<float>((size_t)gemm_epilogue_splits(M, N) * 2 * (size_t)N);      // rows of two classes (epilogue_bwd.cu)
-    return a.size();
+    EpilogueScratch s;
+    return epilogue_scratch(M, N, nullptr, &s);
 }
 
 int streambp_gemm_epilogue_backward(const void *dC, int64_t ldd, const void *pre, int64_t ldp, int32_t activation, int64_t M,
@@ -943,22 +960,23 @@ int streambp_gemm_epilogue_backward(const void *dC, int64_t ldd, const void *pre
     if (activation != STREAMBP_ACT_NONE) SBP_TRY(check_matrix(pre, ldp, N, es));
     if (dZ) SBP_TRY(check_matrix(dZ, ldz, N, es));
     if ((dZ == dC && ldz != ldd) || (dZ && dZ == pre && activation != STREAMBP_ACT_NONE && ldz != ldp)) return STREAMBP_E_SHAPE;
-    float *partials = nullptr;
+    EpilogueScratch s{};
     if (dbias) {
         if (!aligned(dbias, 4) || !aligned(workspace, 256)) return STREAMBP_E_ALIGN;
-        if (workspace_bytes < streambp_gemm_epilogue_workspace_bytes(M, N)) return STREAMBP_E_WORKSPACE;
-        Arena a(workspace);
-        a.take_bytes(kHeaderBytes);
-        partials = a.take<float>((size_t)gemm_epilogue_splits(M, N) * 2 * (size_t)N);      // rows of two classes (epilogue_bwd.cu)
+        if (workspace_bytes < epilogue_scratch(M, N, workspace, &s)) return STREAMBP_E_WORKSPACE;
     }
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     call_state().cuda_error = 0;
     call_state().launches = 0;
+    WsHeader *hdr = static_cast<WsHeader *>(workspace);
+    SBP_TRY(ws_guards_arm(workspace, s.guards, st));      // (a kernel of the call clears the status, which the check may set)
     if (dtype == STREAMBP_F32)
-        return gemm_epilogue_bwd<float>((const float *)dC, ldd, (const float *)pre, ldp, activation, M, N, (float *)dZ, ldz,
-                                        dbias, accumulate != 0, partials, static_cast<WsHeader *>(workspace), st);
-    return gemm_epilogue_bwd<bf16>((const bf16 *)dC, ldd, (const bf16 *)pre, ldp, activation, M, N, (bf16 *)dZ, ldz, dbias,
-                                   accumulate != 0, partials, static_cast<WsHeader *>(workspace), st);
+        SBP_TRY(gemm_epilogue_bwd<float>((const float *)dC, ldd, (const float *)pre, ldp, activation, M, N, (float *)dZ, ldz,
+                                         dbias, accumulate != 0, s.partials, hdr, st));
+    else
+        SBP_TRY(gemm_epilogue_bwd<bf16>((const bf16 *)dC, ldd, (const bf16 *)pre, ldp, activation, M, N, (bf16 *)dZ, ldz, dbias,
+                                        accumulate != 0, s.partials, hdr, st));
+    return ws_guards_check(workspace, s.guards, hdr, st);
 }
 
 int streambp_gemm_swiglu(const void *A, int64_t lda, const void *w_gate, const void *w_up, int64_t ldb, int64_t M,
