@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from bisect import bisect_left
 from dataclasses import dataclass
 from typing import Dict, List, Optional, Sequence
 
@@ -766,7 +767,7 @@ class AdamWPlan:
     alive).  Each entry is a dict: param (fp32 or bf16), grad (fp32), m, v, optional master (fp32, bf16 parameters
     only), optional weight_decay (0).  m and v are fp32, or uint8 codes with m_scale and v_scale (uint8, one per 32
     elements).  All entries share the parameter's and the moments' types and one device; tensors that a step writes
-    must not overlap."""
+    must not overlap one another or a gradient."""
 
     def __init__(self, tensors: Sequence[Dict]):
         what = "AdamWPlan"
@@ -811,6 +812,10 @@ class AdamWPlan:
             written += [(pa, pa + size_p * count), (ma_, ma_ + size_m * count), (va, va + size_m * count)]
         written = sorted(x for x in written if x[0] < x[1])
         _want(all(x[1] <= y[0] for x, y in zip(written, written[1:])), what, "tensors that a step writes overlap")
+        starts = [x[0] for x in written]
+        for a, count in zip(self.grads, self.counts):                 # the written tensor that starts last before a gradient's end
+            at = bisect_left(starts, a + 4 * count) - 1 if count else -1
+            _want(at < 0 or written[at][1] <= a, what, "a gradient overlaps a tensor that the step writes")
 
     def __len__(self) -> int:
         return len(self.tensors)
