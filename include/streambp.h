@@ -369,7 +369,7 @@ int streambp_gemm_swiglu(const void *A, int64_t lda, const void *w_gate, const v
  * accumulated product and rounded once; the activation reads the unrounded z.  residual may be C itself (same ld).
  * bf16 runs on the tcgen05 product kernel where A and W are 16-byte aligned with leading dimensions that are multiples
  * of 8; N, ldc, ldr and ldp are free (multiples of 8 are faster).  float, and bf16 operands outside that rule, run on
- * CUDA cores.  STREAMBP_E_ALIGN where a pointer does not have its elements' alignment.
+ * CUDA cores (up to 64 * 65535 rows).  STREAMBP_E_ALIGN where a pointer does not have its elements' alignment.
  *   ACT_GELU is z/2 (1 + erf(z / sqrt 2)), ACT_GELU_TANH its tanh form, ACT_SILU z sigmoid(z).
  *
  * Backward: dZ = dC act'(pre) (rounded once; dZ may be dC or pre, or NULL where only dbias is wanted) and, unless NULL,

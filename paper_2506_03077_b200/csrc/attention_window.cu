@@ -20,8 +20,8 @@
 // and the sink tile that the window does not reach is cut to its sinks (16 columns for up to 16 of them).  32 rows of four
 // heads span 96 keys fewer than 128 rows of one (16384 rows, window 128, heads of 64: 96 -> 86 us).
 // What bounds it: the exponentials and the conversions around them, ~770 of the ~1600 cycles of a CTA's step of 128 x 64
-// scores, and the latencies that two chains do not hide.  2048 rows behind 14336, window 4096, 32:8 heads of 128: 148 us,
-// 930 TFLOP/s; 16384 rows, window 4096: 850 us, 1130 TFLOP/s.
+// scores, and the latencies that two chains do not hide.  2048 rows behind 14336, window 4096, 32:8 heads of 128: 160 us,
+// 860 TFLOP/s among calls on other inputs (146 us, 940 TFLOP/s in a short run of the same); 16384 rows, window 4096: 870 us.
 //
 // Backward (attn_window_bwd_kernel): two CTA roles in one grid, both deterministic (no floating-point atomics).
 //   dK/dV: one CTA per (key tile, KV head) loops over the query heads of the group and the query tiles that see the tile;
@@ -34,8 +34,8 @@
 // tile; gradients leave through blocks of shared memory and TMA stores or adds, fp32 sums rounded once.
 // What bounds it: one iteration's chain of products and exponentials, ~2900 (dK/dV) and ~2500 cycles (dQ) for 128 x 128
 // scores at heads of 128, of which the tensor pipe is busy 2048 and 1536.  Heads of 64 run two CTAs with inner tiles of 64 per
-// SM.  1024 rows behind 7168, window 2048, 28:4 heads of 128: 113 us (670 TFLOP/s counting five products a pair); 8191
-// rows, window 512, 32:8 heads of 64: 225 us.
+// SM.  1024 rows behind 7168, window 2048, 28:4 heads of 128: 128 us (590 TFLOP/s counting five products a pair); 8191
+// rows, window 512, 32:8 heads of 64: 242 us.
 //
 // All mbarrier waits are bounded (sm100.cuh).
 #include <cstring>
@@ -651,7 +651,7 @@ struct BwdParams {
     float *part;          // sums of segments: [item][Hkv][dK, dV][part_rows][DH]
     int part_rows;
     int mode;             // GradMode of dk, dv (dq: fp32 or bf16, always overwritten)
-    Gap gap;              // dQ role, like
+    Gap gap;              // dQ role: the first tile of the windows where no query sees its first rows
     int edge, edge_keys;  // dQ role: the sink tile that holds sinks in its first rows only (-1: none), those rows rounded up to 32
     int split;                      // PACKED: CTAs that share a dQ item's key tiles, a cluster (1: none)
     int n_dkdv, n_dq_first;         // dK/dV CTAs; dQ CTAs that are dispatched before them (all or none)
@@ -1327,7 +1327,9 @@ __global__ void __launch_bounds__(Bwd<DH>::kThreads, Bwd<DH>::kBlocks)
     }
 }
 
-// delta[h, i] = sum_j dO[i, h, j] O[i, h, j]: one 16-byte load of each per thread, DH / 8 threads to a row
+// delta[h, i] = sum_j dO[i, h, j] O[i, h, j]: one 16-byte load of each per thread, DH / 8 threads to a row.  O is the stored one,
+// so delta carries its rounding, which is what remains where a row sees few keys and dP - delta cancels; sum_j P dP in 32 bits
+// would need the products of a pass of its own.
 template <int DH>
 __global__ void __launch_bounds__(256) window_delta_kernel(const bf16 *o, const bf16 *dout, int n, int Hq, float *delta, WsHeader *hdr,
                                                            void *dk, void *dv, long long unseen16) {

@@ -250,8 +250,8 @@ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 // Debug mode (environment STREAMBP_WS_GUARD set, read once per process): every sub-buffer is followed by a
 // 256-byte guard that the schedulers fill with a pattern before the first launch of a call and check after the
 // last one; a kernel that wrote past the end of its sub-buffer shows up as STREAMBP_E_WORKSPACE_GUARD in
-// streambp_last_device_status (detail = index of the sub-buffer).  The stand-in for a memory checker on a pool
-// where none can be run.  Workspace sizes grow accordingly, consistently in the size queries and in the calls.
+// streambp_last_device_status (detail = index of the sub-buffer).  The stand-in for a memory checker where
+// none can be run.  Workspace sizes grow accordingly, consistently in the size queries and in the calls.
 bool ws_guard_enabled();
 constexpr size_t kGuardBytes = 256;
 struct Arena {
@@ -348,7 +348,7 @@ int gemm_epilogue_take_fault();
 template <typename T>
 int gemm_simt_epilogue(const GemmEpilogue<T> &g, cudaStream_t st);
 // dZ = dC * act'(pre) (dZ may be dC or pre, or nullptr where only the column sums are wanted) and, unless nullptr,
-// dbias[n] (+)= sum over rows of dZ before it is rounded; partials: [gemm_epilogue_splits(M, N), N] floats
+// dbias[n] (+)= sum over rows of dZ before it is rounded; partials: [2 gemm_epilogue_splits(M, N), N] floats
 int gemm_epilogue_splits(int64_t M, int64_t N);
 template <typename T>
 int gemm_epilogue_bwd(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int act, int64_t M, int64_t N, T *dZ, int64_t ldz,

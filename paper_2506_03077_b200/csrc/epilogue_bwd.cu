@@ -6,7 +6,7 @@
 // registers; a grid of (strips, row splits) fills the GPU.  The splits of a strip leave their sums in `partials`, which a second
 // small kernel adds in their order, or for small products are a cluster that adds them itself: no atomics, the same inputs
 // give the same bits.  What bounds it: four rows in flight a thread as raw 16-byte words and four blocks an SM read at 4.2 -
-// 4.7 TB/s (2048 x 14336 with GELU: 42 us for 176 MB; 8192 x 4096 with SiLU: 43 us for 201 MB); unpacked as they arrive they
+// 4.7 TB/s (2048 x 14336 with GELU: 42 us for 176 MB, its tanh form 39; 8192 x 4096 with SiLU: 43 us for 201 MB); unpacked as they arrive they
 // cost twice the registers and half the blocks.
 #include <type_traits>
 
@@ -18,10 +18,9 @@ namespace {
 
 constexpr int kStrip = 64, kRowsAtOnce = 32, kClusterSplits = 8;
 
-// rows and strips of any alignment: a lane per column (consecutive addresses), four rows at a time, eight in flight
 // Where a block's sums of its 64 columns go (threads 0 .. 63): the workspace, or through the cluster to dbias.
 struct Sums {
-    float *partials;          // [splits][N]; null: no sums are wanted, or a cluster joins them
+    float *partials;          // [splits][N], or [2 splits][N] of the word kernel's two classes; null: no sums are wanted, or a cluster joins them
     float *dbias;             // cluster
     int accumulate;
     WsHeader *hdr;
@@ -43,6 +42,7 @@ __device__ __forceinline__ void put_sums(const Sums &to, float s, int col, int N
     cluster_sync_all();                       // no block leaves while another may read its sums
 }
 
+// rows and strips of any alignment: a lane per column (consecutive addresses), four rows at a time, eight in flight
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
     epilogue_bwd_any_kernel(const T *dC, int64_t ldd, const T *pre, int64_t ldp, int64_t M, int N, int64_t rows_per_split, T *dZ,

@@ -10,7 +10,6 @@ namespace sbp {
 namespace {
 constexpr int BM = 64, BN = 64, BK = 16, LDS = 68;
 
-// A element (m,k) at A[m*sam + k*sak]; B element (k,n) at B[k*sbk + n*sbn]
 struct NoEpilogue {};
 template <typename T>
 struct ActEpilogue {
@@ -19,6 +18,7 @@ struct ActEpilogue {
     T *pre;
     int64_t ldp;
 };
+// A element (m,k) at A[m*sam + k*sak]; B element (k,n) at B[k*sbk + n*sbn].
 // EPI < 0: C (+)= op(A, B) (+ bias); else the activation with that number, `x` the residual and the kept sum
 template <typename TI, typename TC, bool A_KCONTIG, bool B_KCONTIG, int EPI = -1, typename X = NoEpilogue>
 __global__ void __launch_bounds__(256)

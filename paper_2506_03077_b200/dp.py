@@ -169,7 +169,8 @@ class ShardedAdamW:
     master copy exist once over all ranks.  `shard` is what DataParallelLayerBackward.exchange leaves (wait() first).
     step() clips by the norm over the whole layer (an all-reduce of one number), updates this rank's slice on the library's
     kernels and gathers the rounded parameters of all ranks.  A norm that is not finite leaves every rank's slice as it was, and
-    the step does not count (`steps`, on the device: the updates so far).
+    the step does not count (`steps`, on the device: the updates so far).  Over several ranks a norm beyond
+    fp32's range is such a norm.
 
     weight_decay: per tensor name (missing: 0).  bits: 32, or 8 for moments in blocks of 32 e4m3 codes."""
 
