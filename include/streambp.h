@@ -419,7 +419,8 @@ int streambp_attention_backward(const void *q, const void *k, const void *v, con
  * the chunk (rows q0 .. q0+n-1, keys 0 .. q0+n-1) as above; head_dim 64 or 128, both on tensor cores for bf16; q0 + n <= 2^30.
  * Only key tiles that some query sees are read, so a chunk costs what its window holds however long the prefix is; rows of
  * k and v that no query of the call sees may hold anything.  Rows that some query sees must be finite: to another query of
- * the same tile such a key has weight 0, and 0 times an infinity is NaN.
+ * the same tile such a key has weight 0, and 0 times an infinity is NaN.  Scores are taken below 2^30 in magnitude (in base 2);
+ * lse is one fp32 number, so scores of 2^x leave P of the backward a relative error of 2^(x - 23).
  *
  * Backward: lse and o are those of the forward call.  grad_dtype STREAMBP_F32: dq is overwritten, dk and dv [q0+n,
  * n_kv_heads, head_dim] are overwritten (accumulate = 0) or added to (1: the key-prefix accumulators of a streamed
