@@ -115,3 +115,15 @@ def test_norms_that_overflow_fp32(n, most):
     t["grad"].fill_(1e-3)
     B.grad_norm(plan, float("inf"), norm, scale, ws)
     assert scale.item() == 1.0
+
+
+@pytest.mark.parametrize("eps,lr,size", [(1e-40, 1e-17, 1e-24), (1e-8, 1e-3, 1.0), (1e38, 1e37, 1.0)])
+def test_step_number_on_the_device_under_any_eps(eps, lr, size):
+    """The rates formed by the kernel from a step number in device memory and by the host, each from doubles rounded once: the
+    moves differ by a rounding of each of the two rates at most."""
+    g, out = torch.logspace(-3, 0, 999, device="cuda") * size, []
+    for step in (3, torch.tensor([3], device="cuda")):
+        t = {"param": torch.zeros_like(g), "grad": g, "m": torch.zeros_like(g), "v": torch.zeros_like(g)}
+        B.adamw_step(B.AdamWPlan([t]), lr, 0.9, 0.95, eps, step)
+        out.append(t["param"].double())
+    assert bool((out[0] != 0).all()) and bool(((out[0] - out[1]).abs() <= 4 * E32 * out[0].abs()).all())
