@@ -47,24 +47,15 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
-// eight elements of a row from column `col` on; where fewer are left, those
-__device__ __forceinline__ uint4 load_piece(const bf16 *row, int col, int N) {
-    if (col + 8 <= N) return *reinterpret_cast<const uint4 *>(row + col);
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    const uint16_t *u = reinterpret_cast<const uint16_t *>(row);
-#pragma unroll
-    for (int e = 0; e < 7; e++)
-        if (col + e < N) w[e >> 1] |= (uint32_t)u[col + e] << (16 * (e & 1));
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
 __device__ __forceinline__ void st_shared_v4(uint32_t at, const uint32_t (&w)[4]) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
 
 // 32 rows (one per lane) x 32 columns of the tile: z = accumulator + bias, then pre, activation, residual, C.  The blocks
 // of pre and C leave through shared memory (rows of 64 bytes, 64-byte swizzle: no bank conflicts) as TMA stores, which also
-// clip the rows and columns behind the matrix: as 16-byte stores of 32 different rows they took the memory pipe four times
-// as many accesses as they have lines.
+// clip the rows behind the matrix and whole groups of 8 columns (of a group that the matrix ends in they write all 16 bytes:
+// such a block goes through finish_rows).  As 16-byte stores of 32 different rows they took the memory pipe four times as many
+// accesses as they have lines.
 template <int ACT>
 __device__ __forceinline__ void finish_vec(const EpiParams &p, const uint32_t (&r)[32], const uint4 (&rs)[4], uint32_t stage,
                                            int lane, int row0, int col0) {
@@ -77,17 +68,11 @@ __device__ __forceinline__ void finish_vec(const EpiParams &p, const uint32_t (&
         float z[8];
 #pragma unroll
         for (int e = 0; e < 8; e++) z[e] = __uint_as_float(r[8 * j + e]);
-        if (p.bias && col0 + 8 * j < p.N) {            // the bias ends on a multiple of 8 columns or is read element by element
-            if (col0 + 8 * j + 8 <= p.N) {
-                Vec<bf16> b;
-                b.load(p.bias + col0 + 8 * j);
+        if (p.bias && col0 + 8 * j < p.N) {            // no group ends outside the matrix
+            Vec<bf16> b;
+            b.load(p.bias + col0 + 8 * j);
 #pragma unroll
-                for (int e = 0; e < 8; e++) z[e] += b.v[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    if (col0 + 8 * j + e < p.N) z[e] += __bfloat162float(p.bias[col0 + 8 * j + e]);
-            }
+            for (int e = 0; e < 8; e++) z[e] += b.v[e];
         }
         uint32_t w[4];
         if (p.pre) {
@@ -115,13 +100,15 @@ __device__ __forceinline__ void finish_vec(const EpiParams &p, const uint32_t (&
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
 }
-// The same where rows do not start on 16-byte boundaries, or the columns end inside the block: the block is transposed
+// The same where rows do not start on 16-byte boundaries, or the columns end inside a group of 8: the block is transposed
 // through shared memory (16-byte groups exchanged with the row's bits, so that neither side has bank conflicts) and walked
 // row by row with a lane per column: consecutive addresses instead of one element of each of 32 rows.  Eight rows at a time,
 // without a branch among them, and the residuals of the next eight under way: 8000 x 1997 x 1024 with a residual 107 -> 68 us,
 // with GELU and z kept 94 -> 70 (2000 columns: 47).
 template <int ACT, bool RES>
 __device__ __forceinline__ void finish_rows(const EpiParams &p, const uint32_t (&r)[32], float *stage, int lane, int row0, int col0) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");        // of blocks that went as TMA stores
+    __syncwarp();
 #pragma unroll
     for (int j = 0; j < 8; j++) {
         const uint32_t w[4] = {r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]};
@@ -250,15 +237,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1) gemm_a
             const int row0 = (tile % p.tiles_m) * PM + 128 * (int)rank + quarter * 32, n0 = (tile / p.tiles_m) * p.bn;
             const int row = row0 + lane;
             const uint32_t acc = tmem + buf * PBN + ((uint32_t)(quarter * 32) << 16);
-            // the residual of a block is requested one block ahead (the first before the products are done); rows start on
-            // 16-byte boundaries here, so a ragged last block is read in whole 16-byte pieces where its row goes on that far
+            // blocks of whole groups of 8 columns; the residual of such a block is requested one block ahead (the first before
+            // the products are done)
+            auto groups = [&](int col0) { return p.vec && (col0 + 32 <= p.N || (p.N & 7) == 0); };
             uint4 rs[4];
             auto fetch = [&](int c) {
                 const int col0 = n0 + c * 32;
-                if (p.residual && p.vec && row < p.M && c < p.bn / 32) {
+                if (p.residual && groups(col0) && row < p.M && c < p.bn / 32) {
 #pragma unroll
                     for (int j = 0; j < 4; j++)
-                        if (col0 + 8 * j < p.N) rs[j] = load_piece(p.residual + (long long)row * p.ldr, col0 + 8 * j, p.N);
+                        if (col0 + 8 * j < p.N) rs[j] = *reinterpret_cast<const uint4 *>(p.residual + (long long)row * p.ldr + col0 + 8 * j);
                 }
             };
             fetch(half);
@@ -270,7 +258,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1) gemm_a
                 if (col0 >= p.N || row0 >= p.M) break;                // uniform across the warp
                 uint32_t r[32];
                 tmem_ld32(acc + c * 32, r);
-                if (p.vec) {
+                if (groups(col0)) {
                     const uint4 now[4] = {rs[0], rs[1], rs[2], rs[3]};
                     fetch(c + 2);
                     finish_vec<ACT>(p, r, now, smem_u32(stage), lane, row0, col0);
