@@ -253,7 +253,8 @@ __device__ __forceinline__ bool mma_tile(const GroupParams &p, const TileRef &t,
 
 // One epilogue warp: rows m_base + 32 * quarter .. + 31 of tile t, all BN columns, from the accumulator at `acc`
 // (lane = row).  fp32 output: 32 x 32 blocks staged in shared memory with the 128-byte swizzle the tensor map expects,
-// then a TMA store, or a TMA reduce-add when accumulating; bf16 output: 16-byte stores from registers.
+// then a TMA store, or a TMA reduce-add when accumulating; bf16 output: 16-byte stores from registers.  Of a 16-byte group that
+// the matrix ends in a TMA store writes all 16 bytes: the block of such columns is written element by element.
 __device__ __forceinline__ void epilogue_rows(const GroupParams &p, const TileRef &t, int m_base, int quarter, int lane,
                                               uint32_t acc, uint32_t epi, uint32_t &staged) {
     const uint32_t fl = pick(p.flags, t.q);
@@ -361,7 +362,17 @@ __device__ __forceinline__ void epilogue_rows(const GroupParams &p, const TileRe
         if (col0 >= Nq) break;               // uniform across the warp
         uint32_t r[32];
         tmem_ld32(taddr + c * 32, r);
-        if (fl & F_OUT_F32) {
+        if ((fl & F_OUT_F32) && col0 + 32 > Nq && (Nq & 3)) {
+            if (row < Mq) {
+                float *out = reinterpret_cast<float *>(pick(p.C, t.q)) + (long long)row * pick(p.ldc, t.q) + col0;
+#pragma unroll
+                for (int e = 0; e < 32; e++)
+                    if (col0 + e < Nq) {
+                        const float v = __uint_as_float(r[e]) + (bias ? __bfloat162float(bias[col0 + e]) : 0.f);
+                        out[e] = fl & F_ACC ? out[e] + v : v;
+                    }
+            }
+        } else if (fl & F_OUT_F32) {
             // stage the warp's 32 x 32 block (row = lane) with the 128-byte swizzle the tensor map expects
             const uint32_t buf_s = epi + (uint32_t)(quarter * 2 + (staged & 1u)) * EPI_BUF_BYTES;
             staged++;
