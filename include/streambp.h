@@ -441,6 +441,118 @@ int streambp_attention_window_backward(const void *q, const void *k, const void 
                                        int engine, void *cuda_stream);
 
 /*
+ * (No counterpart in the paper.)  What a model's two ends need beside the products: log-probabilities of given tokens,
+ * distillation from a teacher's top logits, layer norm, the embedding lookup and its gradient.  Matrices here have rows that
+ * may start anywhere (ld in elements, aligned to their elements); rows that start on 16 bytes are faster.
+ *
+ * Log-probabilities.  Row i of logits ([rows, vocab], float or bf16) has p = softmax(z / temperature).
+ *     lse = log sum exp(z / temperature),  logp = z[token] / temperature - lse,  entropy = - sum p log p,
+ *     top_ids [rows, k] = the k largest logits' ids, largest first, of equal ones the lowest id first, top_logp their log p.
+ * tokens [rows] may be NULL (then logp must be); a row whose token is ignore_index takes no part: its logits are not read,
+ * logp, lse and entropy are 0, top_ids -1 and top_logp -inf.  A token outside the vocabulary is treated like that and reported
+ * as STREAMBP_E_BAD_LABEL.  Every output is optional, one has to be there; 0 <= k <= STREAMBP_TOP_MAX, k <= vocab <= 2^27,
+ * rows <= 2^27.  Logits of -inf have probability 0; a row of nothing else has lse, logp and top_logp -inf and entropy 0.  A
+ * row with a NaN or +inf has NaN for all of them and top_ids -1.  2^-20 <= temperature <= 2^20, here and below; z / temperature
+ * stays within the range of fp32.
+ *
+ * Backward: d_logits = (d_logp (onehot(token) - p) + d_lse p - d_entropy p (log p + entropy)) / temperature, rounded once, with
+ * p from the given lse; each of the three row gradients may be NULL (d_entropy needs entropy).  d_logits may be logits
+ * (same ld).  Rows that take no part are written as 0.  Lists of alternatives have no gradient.
+ */
+#define STREAMBP_TOP_MAX 128
+size_t streambp_token_logprobs_workspace_bytes(void);
+int streambp_token_logprobs(const void *logits, int64_t ld, int64_t rows, int64_t vocab, int32_t dtype, const int64_t *tokens,
+                            int64_t ignore_index, float temperature, int32_t k, float *logp, float *lse, float *entropy,
+                            float *top_logp, int64_t *top_ids, void *workspace, size_t workspace_bytes, void *cuda_stream);
+int streambp_token_logprobs_backward(const void *logits, int64_t ld, int64_t rows, int64_t vocab, int32_t dtype,
+                                     const int64_t *tokens, int64_t ignore_index, float temperature, const float *lse,
+                                     const float *entropy, const float *d_logp, const float *d_lse, const float *d_entropy,
+                                     void *d_logits, int64_t ldd, void *cuda_stream);
+
+/*
+ * Distillation from a teacher's top logits: the loss of each row and its gradient in one call.  Row i has k entries
+ * (ids[i, e], values[i, e]; id -1: no entry), p = softmax(logits / temperature) over the whole vocabulary.
+ *     tail = 0: q = softmax(values / temperature) over the row's entries,  row_loss = sum q (log q - log p[id])
+ *     tail = 1: q = exp(values), log-probabilities of the teacher at this temperature; what they leave of 1 is one more
+ *               outcome, the unlisted tokens together:  row_loss = sum q (log q - log p[id]) + q_r log(q_r / p_r),
+ *               q_r = max(0, 1 - sum q), p_r the sum of p over unlisted tokens (left out where no token is left for it)
+ *     d_logits = weight[i] d row_loss / d logits, rounded once
+ * A token listed more than once is the sum of its entries in the gradient.  weight (NULL: 1) carries what the objective
+ * multiplies a row by (1 / N, a mixing factor, temperature^2); a row of weight 0, or without entries, takes no part: its logits
+ * are not read, row_loss and d_logits are 0.  row_loss is not weighted.  row_loss and d_logits (type of the logits; may be
+ * logits, same ld) are optional, one has to be there.  ids of rows that take part outside -1 .. vocab - 1 are treated as
+ * absent and reported as STREAMBP_E_BAD_LABEL.  1 <= k <= STREAMBP_TOP_MAX, vocab <= STREAMBP_DISTILL_MAX_VOCAB, rows <= 2^27.
+ * Logits of -inf have probability 0 (the loss is +inf where one is listed with q > 0); a NaN or +inf makes its row NaN.
+ */
+#define STREAMBP_DISTILL_MAX_VOCAB 393216
+typedef struct {
+    int32_t k;
+    int32_t tail;
+    float temperature;
+} streambp_distill_cfg;
+size_t streambp_distill_topk_workspace_bytes(void);
+int streambp_distill_topk(const streambp_distill_cfg *distill, const void *logits, int64_t ld, int64_t rows, int64_t vocab,
+                          int32_t dtype, const int64_t *ids, const float *values, const float *weight, float *row_loss,
+                          void *d_logits, int64_t ldd, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * The same two over the streamed LM head (Sec. 3.2.1): the logits of H [T, d_model] exist for one chunk only.
+ * streambp_lmhead_logprobs scores given tokens (what streambp_lmhead_rl_backward takes as logp_old and logp_ref) and lists
+ * alternatives (what the distilling head takes as ids and values); arguments as in streambp_token_logprobs, ignore_index of
+ * cfg; chunks whose tokens are all ignored are skipped on the device.
+ * streambp_lmhead_distill_backward: *loss = sum over rows of weight row_loss (weight [T] is required; rows of weight 0 take no
+ * part, chunks or groups of them are skipped); row_loss [T] is optional; dH, d_w_vocab, d_g_final, accumulate and wgrad_group
+ * as in streambp_lmhead_ce_backward_grouped.  STREAMBP_E_NO_VALID_LABELS where every weight is 0 (loss and gradients are 0).
+ */
+size_t streambp_lmhead_logprobs_workspace_bytes(const streambp_head_cfg *cfg, int64_t T, int64_t chunk);
+int streambp_lmhead_logprobs(const streambp_head_cfg *cfg, const void *g_final, const void *w_vocab, const void *H,
+                             const int64_t *tokens, int64_t T, int64_t chunk, float temperature, int32_t k, float *logp,
+                             float *lse, float *entropy, float *top_logp, int64_t *top_ids, void *workspace,
+                             size_t workspace_bytes, void *cuda_stream);
+size_t streambp_lmhead_distill_workspace_bytes(const streambp_head_cfg *cfg, int64_t T, int64_t chunk, int32_t wgrad_group);
+int streambp_lmhead_distill_backward(const streambp_head_cfg *cfg, const streambp_distill_cfg *distill, const void *g_final,
+                                     const void *w_vocab, const void *H, const int64_t *ids, const float *values,
+                                     const float *weight, int64_t T, int64_t chunk, int32_t wgrad_group, int accumulate,
+                                     float *loss, float *row_loss, void *dH, float *d_w_vocab, float *d_g_final,
+                                     void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Layer norm over the d columns of each row, in fp32 with one rounding:
+ *     y = (x - mean) rstd gain + bias,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ * x, y [rows, d] and gain, bias [d] are of `dtype`; gain and bias are optional (1 and 0), mean and rstd (fp32 [rows], what the
+ * backward reads) too.  y may be x (same ld).  rows <= 2^31 - 1, d <= 2^20.
+ * Backward, with xhat = (x - mean) rstd and g = dy gain:
+ *     dx = (g - mean(g) - xhat mean(g xhat)) rstd + add,   d_gain (+)= sum over rows of dy xhat,  d_bias (+)= sum of dy
+ * add (the gradient that goes around the norm) is optional; dx, d_gain and d_bias (fp32 [d], overwritten or with accumulate
+ * = 1 added to) are optional, one has to be there; dx may be dy, x or add (same ld).  The sums are joined in a fixed order.
+ * The workspace is needed for the sums only.
+ */
+int streambp_layernorm_forward(const void *x, int64_t ldx, const void *gain, const void *bias, float eps, int64_t rows, int64_t d,
+                               int32_t dtype, void *y, int64_t ldy, float *mean, float *rstd, void *cuda_stream);
+size_t streambp_layernorm_workspace_bytes(int64_t rows, int64_t d);
+int streambp_layernorm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *gain, const float *mean,
+                                const float *rstd, const void *add, int64_t ldadd, int64_t rows, int64_t d, int32_t dtype,
+                                void *dx, int64_t lddx, float *d_gain, float *d_bias, int accumulate, void *workspace,
+                                size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Embedding: out[t] = scale table[ids[t]] (table [vocab, d], out [n, d] of `dtype`, rounded once).  A token equal to padding_id
+ * has a row of zeros and no gradient (a value outside the vocabulary, such as -1: no token is padding).  Ids outside the
+ * vocabulary are treated like padding and reported as STREAMBP_E_BAD_LABEL (detail: the first).
+ * Backward: d_table (fp32 [vocab, d], dense) = or, with accumulate = 1, += scale times the sums of d_out's rows by id, formed
+ * over the tokens sorted by id and joined in a fixed order (reproducible bit by bit); rows of no token are 0 or stay as they
+ * are (they are not read).  1 <= n < 2^30, vocab < 2^31 - 1, d <= 2^20.
+ */
+size_t streambp_embedding_workspace_bytes(void);
+int streambp_embedding_forward(const void *table, int64_t ld, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, int32_t dtype,
+                               float scale, int64_t padding_id, void *out, int64_t ldo, void *workspace, size_t workspace_bytes,
+                               void *cuda_stream);
+size_t streambp_embedding_backward_workspace_bytes(int64_t n, int64_t vocab, int64_t d);
+int streambp_embedding_backward(const void *d_out, int64_t ldo, const int64_t *ids, int64_t n, int64_t vocab, int64_t d,
+                                int32_t dtype, float scale, int64_t padding_id, int accumulate, float *d_table, void *workspace,
+                                size_t workspace_bytes, void *cuda_stream);
+
+/*
  * (No counterpart in the paper.)  streambp_attention_backward for callers that have no device buffer
  * to offer for `delta` and cannot obtain one when they call: host code in a latency-critical loop
  * where cudaMalloc / cudaFree would stall the whole device, a plug-in whose host framework already owns

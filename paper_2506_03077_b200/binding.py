@@ -44,6 +44,12 @@ EXPORTS = (
     "streambp_mx8_decode", "streambp_gemm_epilogue", "streambp_gemm_epilogue_workspace_bytes",
     "streambp_gemm_epilogue_backward", "streambp_attention_window_forward", "streambp_attention_window_workspace_bytes",
     "streambp_attention_window_backward",
+    "streambp_token_logprobs_workspace_bytes", "streambp_token_logprobs", "streambp_token_logprobs_backward",
+    "streambp_distill_topk_workspace_bytes", "streambp_distill_topk", "streambp_lmhead_logprobs_workspace_bytes",
+    "streambp_lmhead_logprobs", "streambp_lmhead_distill_workspace_bytes", "streambp_lmhead_distill_backward",
+    "streambp_layernorm_forward", "streambp_layernorm_workspace_bytes", "streambp_layernorm_backward",
+    "streambp_embedding_workspace_bytes", "streambp_embedding_forward", "streambp_embedding_backward_workspace_bytes",
+    "streambp_embedding_backward",
 )
 
 
@@ -64,6 +70,10 @@ class HeadCfgC(C.Structure):
 
 class RlCfgC(C.Structure):
     _fields_ = [("objective", C.c_int32), ("beta", C.c_float), ("clip_eps", C.c_float)]
+
+
+class DistillCfgC(C.Structure):
+    _fields_ = [("k", C.c_int32), ("tail", C.c_int32), ("temperature", C.c_float)]
 
 
 class GemmProblemC(C.Structure):
@@ -204,6 +214,28 @@ def lib() -> C.CDLL:
     L.streambp_mx8_encode.argtypes = [vp, i64, i32, vp, vp, vp]
     L.streambp_mx8_decode.restype = C.c_int
     L.streambp_mx8_decode.argtypes = [vp, vp, i64, vp, i32, vp]
+    f32 = C.c_float
+    for name, restype, argtypes in (
+            ("streambp_token_logprobs_workspace_bytes", sz, []),
+            ("streambp_token_logprobs", C.c_int, [vp, i64, i64, i64, i32, vp, i64, f32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+            ("streambp_token_logprobs_backward", C.c_int, [vp, i64, i64, i64, i32, vp, i64, f32, vp, vp, vp, vp, vp, vp, i64, vp]),
+            ("streambp_distill_topk_workspace_bytes", sz, []),
+            ("streambp_distill_topk", C.c_int, [C.POINTER(DistillCfgC), vp, i64, i64, i64, i32, vp, vp, vp, vp, vp, i64, vp, sz, vp]),
+            ("streambp_lmhead_logprobs_workspace_bytes", sz, [C.POINTER(HeadCfgC), i64, i64]),
+            ("streambp_lmhead_logprobs", C.c_int, [C.POINTER(HeadCfgC), vp, vp, vp, vp, i64, i64, f32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+            ("streambp_lmhead_distill_workspace_bytes", sz, [C.POINTER(HeadCfgC), i64, i64, i32]),
+            ("streambp_lmhead_distill_backward", C.c_int, [C.POINTER(HeadCfgC), C.POINTER(DistillCfgC), vp, vp, vp, vp, vp, vp, i64, i64,
+                                                           i32, C.c_int, vp, vp, vp, vp, vp, vp, sz, vp]),
+            ("streambp_layernorm_forward", C.c_int, [vp, i64, vp, vp, f32, i64, i64, i32, vp, i64, vp, vp, vp]),
+            ("streambp_layernorm_workspace_bytes", sz, [i64, i64]),
+            ("streambp_layernorm_backward", C.c_int, [vp, i64, vp, i64, vp, vp, vp, vp, i64, i64, i64, i32, vp, i64, vp, vp, C.c_int, vp,
+                                                      sz, vp]),
+            ("streambp_embedding_workspace_bytes", sz, []),
+            ("streambp_embedding_forward", C.c_int, [vp, i64, vp, i64, i64, i64, i32, f32, i64, vp, i64, vp, sz, vp]),
+            ("streambp_embedding_backward_workspace_bytes", sz, [i64, i64, i64]),
+            ("streambp_embedding_backward", C.c_int, [vp, i64, vp, i64, i64, i64, i32, f32, i64, C.c_int, vp, vp, sz, vp])):
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = restype, argtypes
     _lib = L
     return L
 
@@ -884,4 +916,233 @@ def mx8_decode(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, str
                  out.data_ptr(), _dtype_code(out.dtype))
     if check:
         _check(st, "streambp_mx8_decode")
+    return st
+
+
+# ---- the ends of a model ------------------------------------------------------------------------------------------
+TOP_MAX = 128
+DISTILL_MAX_VOCAB = 393216
+
+
+def _vectors(what: str, dev: int, shape: tuple, **tensors) -> list:
+    """Addresses of optional contiguous tensors of one shape: name=(tensor, dtype)."""
+    out = []
+    for name, (t, dtype) in tensors.items():
+        if t is not None and (t.get_device() != dev or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{what}: {name} is a contiguous {dtype} tensor {shape} on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        out.append(None if t is None else t.data_ptr())
+    return out
+
+
+def _space(what: str, dev: int, workspace: Optional[torch.Tensor]) -> tuple:
+    """(address, bytes) of a workspace, (None, 0) for None."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"{what}: workspace is contiguous, on cuda:{dev}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _matrix(what: str, name: str, t: torch.Tensor) -> int:
+    """The device of a CUDA matrix."""
+    _want(t.is_cuda and t.dim() == 2, what, f"{name} is a CUDA matrix")
+    return t.get_device()
+
+
+def token_logprobs_workspace_bytes() -> int:
+    return int(lib().streambp_token_logprobs_workspace_bytes())
+
+
+def _score_outputs(what: str, dev: int, n: int, tokens, logp, lse, entropy, top_logp, top_ids) -> tuple:
+    f, i = torch.float32, torch.int64
+    rows = _vectors(what, dev, (n,), tokens=(tokens, i), logp=(logp, f), lse=(lse, f), entropy=(entropy, f))
+    lists = [t for t in (top_logp, top_ids) if t is not None]
+    _want(all(t.dim() == 2 for t in lists), what, "top_logp and top_ids are [rows, k]")
+    k = lists[0].shape[1] if lists else 0
+    return rows, k, _vectors(what, dev, (n, k), top_logp=(top_logp, f), top_ids=(top_ids, i))
+
+
+def token_logprobs(logits, tokens, workspace, logp=None, lse=None, entropy=None, top_logp=None, top_ids=None,
+                   temperature: float = 1.0, ignore_index: int = -100, stream=None, check: bool = True) -> int:
+    """streambp_token_logprobs; logits [rows, vocab] fp32 or bf16 with contiguous rows, tokens int64 [rows] or None, logp, lse,
+    entropy fp32 [rows], top_logp fp32 and top_ids int64 [rows, k]; outputs that are None are not formed."""
+    what, dev = "token_logprobs", _matrix("token_logprobs", "logits", logits)
+    n, V = logits.shape
+    z = _rows(what, dev, logits.dtype, (n, V), logits)
+    rows, k, lists = _score_outputs(what, dev, n, tokens, logp, lse, entropy, top_logp, top_ids)
+    st = _launch(what, dev, stream, lib().streambp_token_logprobs, z[0], z[1], n, V, _dtype_code(logits.dtype), rows[0], ignore_index,
+                 temperature, k, *rows[1:], *lists, *_space(what, dev, workspace))
+    if check:
+        _check(st, "streambp_token_logprobs")
+    return st
+
+
+def token_logprobs_backward(logits, tokens, lse, entropy, d_logits, d_logp=None, d_lse=None, d_entropy=None,
+                            temperature: float = 1.0, ignore_index: int = -100, stream=None, check: bool = True) -> int:
+    """streambp_token_logprobs_backward; lse and entropy (None without d_entropy) of the forward call, d_logits like logits
+    (or logits itself)."""
+    what, dev = "token_logprobs_backward", _matrix("token_logprobs_backward", "logits", logits)
+    n, V = logits.shape
+    z, d = (_rows(what, dev, logits.dtype, (n, V), t) for t in (logits, d_logits))
+    f = torch.float32
+    v = _vectors(what, dev, (n,), tokens=(tokens, torch.int64), lse=(lse, f), entropy=(entropy, f), d_logp=(d_logp, f), d_lse=(d_lse, f),
+                 d_entropy=(d_entropy, f))
+    st = _launch(what, dev, stream, lib().streambp_token_logprobs_backward, z[0], z[1], n, V, _dtype_code(logits.dtype), v[0],
+                 ignore_index, temperature, *v[1:], d[0], d[1])
+    if check:
+        _check(st, "streambp_token_logprobs_backward")
+    return st
+
+
+def distill_topk_workspace_bytes() -> int:
+    return int(lib().streambp_distill_topk_workspace_bytes())
+
+
+def _entries(what: str, dev: int, n: int, ids, values) -> tuple:
+    _want(ids.dim() == 2, what, "ids and values are [rows, k]")
+    k = ids.shape[1]
+    return k, _vectors(what, dev, (n, k), ids=(ids, torch.int64), values=(values, torch.float32))
+
+
+def distill_topk(logits, ids, values, row_loss, workspace, d_logits=None, weight=None, temperature: float = 1.0,
+                 tail: bool = False, stream=None, check: bool = True) -> int:
+    """streambp_distill_topk; logits [rows, vocab] fp32 or bf16 with contiguous rows, ids int64 and values fp32 [rows, k], weight
+    and row_loss fp32 [rows] (optional), d_logits like logits (or logits itself, or None)."""
+    what, dev = "distill_topk", _matrix("distill_topk", "logits", logits)
+    n, V = logits.shape
+    z, d = (_rows(what, dev, logits.dtype, (n, V), t) for t in (logits, d_logits))
+    k, entries = _entries(what, dev, n, ids, values)
+    w = _vectors(what, dev, (n,), weight=(weight, torch.float32), row_loss=(row_loss, torch.float32))
+    cfg = DistillCfgC(k, 1 if tail else 0, temperature)
+    st = _launch(what, dev, stream, lib().streambp_distill_topk, C.byref(cfg), z[0], z[1], n, V, _dtype_code(logits.dtype), *entries, *w,
+                 d[0], d[1], *_space(what, dev, workspace))
+    if check:
+        _check(st, "streambp_distill_topk")
+    return st
+
+
+def _head_args(what: str, cfg: HeadConfig, g_final, w_vocab, H) -> int:
+    """Checks what a head reads and returns the device."""
+    dev = _matrix(what, "H", H)
+    d, V = cfg.d_model, cfg.vocab
+    for name, t, shape in (("H", H, (H.shape[0], d)), ("g_final", g_final, (d,)), ("w_vocab", w_vocab, (V, d))):
+        if t.get_device() != dev or t.dtype != cfg.dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{what}: {name} is a contiguous {cfg.dtype} tensor {shape} on cuda:{dev}")
+    return dev
+
+
+def lmhead_logprobs_workspace_bytes(cfg: HeadConfig, T: int, chunk: int) -> int:
+    c = cfg.c()
+    return int(lib().streambp_lmhead_logprobs_workspace_bytes(C.byref(c), T, chunk))
+
+
+def lmhead_logprobs(cfg: HeadConfig, g_final, w_vocab, H, tokens, chunk: int, workspace, logp=None, lse=None, entropy=None,
+                    top_logp=None, top_ids=None, temperature: float = 1.0, stream=None, check: bool = True) -> int:
+    """streambp_lmhead_logprobs: token_logprobs of the head's logits, which exist for one chunk of H [T, d_model] at a time."""
+    what = "lmhead_logprobs"
+    dev = _head_args(what, cfg, g_final, w_vocab, H)
+    T = H.shape[0]
+    rows, k, lists = _score_outputs(what, dev, T, tokens, logp, lse, entropy, top_logp, top_ids)
+    c = cfg.c()
+    st = _launch(what, dev, stream, lib().streambp_lmhead_logprobs, C.byref(c), g_final.data_ptr(), w_vocab.data_ptr(), H.data_ptr(),
+                 rows[0], T, chunk, temperature, k, *rows[1:], *lists, *_space(what, dev, workspace))
+    if check:
+        _check(st, "streambp_lmhead_logprobs")
+    return st
+
+
+def lmhead_distill_workspace_bytes(cfg: HeadConfig, T: int, chunk: int, wgrad_group: int = 1) -> int:
+    c = cfg.c()
+    return int(lib().streambp_lmhead_distill_workspace_bytes(C.byref(c), T, chunk, wgrad_group))
+
+
+def lmhead_distill_backward(cfg: HeadConfig, g_final, w_vocab, H, ids, values, weight, chunk: int, loss, dH, d_w_vocab, d_g_final,
+                            workspace, row_loss=None, temperature: float = 1.0, tail: bool = False, accumulate: bool = False,
+                            stream=None, check: bool = True, wgrad_group: int = 1) -> int:
+    """streambp_lmhead_distill_backward: the streamed head under distill_topk's loss; weight fp32 [T]."""
+    what = "lmhead_distill_backward"
+    dev = _head_args(what, cfg, g_final, w_vocab, H)
+    T, d, V = H.shape[0], cfg.d_model, cfg.vocab
+    k, entries = _entries(what, dev, T, ids, values)
+    f = torch.float32
+    w = _vectors(what, dev, (T,), weight=(weight, f), row_loss=(row_loss, f))
+    for name, t, dtype, shape in (("loss", loss, f, (1,)), ("dH", dH, cfg.dtype, (T, d)), ("d_w_vocab", d_w_vocab, f, (V, d)),
+                                  ("d_g_final", d_g_final, f, (d,))):
+        _vectors(what, dev, shape, **{name: (t, dtype)})
+    c, dc = cfg.c(), DistillCfgC(k, 1 if tail else 0, temperature)
+    st = _launch(what, dev, stream, lib().streambp_lmhead_distill_backward, C.byref(c), C.byref(dc), g_final.data_ptr(), w_vocab.data_ptr(),
+                 H.data_ptr(), *entries, w[0], T, chunk, wgrad_group, 1 if accumulate else 0, loss.data_ptr(), w[1], dH.data_ptr(),
+                 d_w_vocab.data_ptr(), d_g_final.data_ptr(), *_space(what, dev, workspace))
+    if check:
+        _check(st, "streambp_lmhead_distill_backward")
+    return st
+
+
+def layernorm_forward(x, gain, bias, eps: float, y, mean=None, rstd=None, stream=None, check: bool = True) -> int:
+    """streambp_layernorm_forward; x, y [rows, d] with contiguous rows (y may be x), gain and bias [d] of the same type or None,
+    mean and rstd fp32 [rows] or None."""
+    what, dev, dt = "layernorm_forward", _matrix("layernorm_forward", "x", x), x.dtype
+    n, d = x.shape
+    a, o = (_rows(what, dev, dt, (n, d), t) for t in (x, y))
+    g = _vectors(what, dev, (d,), gain=(gain, dt), bias=(bias, dt))
+    s = _vectors(what, dev, (n,), mean=(mean, torch.float32), rstd=(rstd, torch.float32))
+    st = _launch(what, dev, stream, lib().streambp_layernorm_forward, a[0], a[1], *g, eps, n, d, _dtype_code(dt), o[0], o[1], *s)
+    if check:
+        _check(st, "streambp_layernorm_forward")
+    return st
+
+
+def layernorm_workspace_bytes(rows: int, d: int) -> int:
+    return int(lib().streambp_layernorm_workspace_bytes(rows, d))
+
+
+def layernorm_backward(dy, x, gain, mean, rstd, dx=None, d_gain=None, d_bias=None, add=None, workspace=None,
+                       accumulate: bool = False, stream=None, check: bool = True) -> int:
+    """streambp_layernorm_backward; dy, x, add, dx [rows, d], d_gain and d_bias fp32 [d] (overwritten, or added to)."""
+    what, dev, dt = "layernorm_backward", _matrix("layernorm_backward", "x", x), x.dtype
+    n, d = x.shape
+    g, a, r, o = (_rows(what, dev, dt, (n, d), t) for t in (dy, x, add, dx))
+    w = _vectors(what, dev, (d,), gain=(gain, dt), d_gain=(d_gain, torch.float32), d_bias=(d_bias, torch.float32))
+    s = _vectors(what, dev, (n,), mean=(mean, torch.float32), rstd=(rstd, torch.float32))
+    st = _launch(what, dev, stream, lib().streambp_layernorm_backward, g[0], g[1], a[0], a[1], w[0], *s, r[0], r[1], n, d,
+                 _dtype_code(dt), o[0], o[1], w[1], w[2], 1 if accumulate else 0, *_space(what, dev, workspace))
+    if check:
+        _check(st, "streambp_layernorm_backward")
+    return st
+
+
+def embedding_workspace_bytes() -> int:
+    return int(lib().streambp_embedding_workspace_bytes())
+
+
+def embedding_forward(table, ids, out, workspace, scale: float = 1.0, padding_id: int = -1, stream=None, check: bool = True) -> int:
+    """streambp_embedding_forward; table [vocab, d], ids int64 [n], out [n, d] of the table's type, rows contiguous."""
+    what, dev, dt = "embedding_forward", _matrix("embedding_forward", "table", table), table.dtype
+    (V, d), n = table.shape, ids.numel()
+    t, o = _rows(what, dev, dt, (V, d), table), _rows(what, dev, dt, (n, d), out)
+    i = _vectors(what, dev, (n,), ids=(ids, torch.int64))
+    st = _launch(what, dev, stream, lib().streambp_embedding_forward, t[0], t[1], i[0], n, V, d, _dtype_code(dt), scale, padding_id, o[0],
+                 o[1], *_space(what, dev, workspace))
+    if check:
+        _check(st, "streambp_embedding_forward")
+    return st
+
+
+def embedding_backward_workspace_bytes(n: int, vocab: int, d: int) -> int:
+    return int(lib().streambp_embedding_backward_workspace_bytes(n, vocab, d))
+
+
+def embedding_backward(d_out, ids, d_table, workspace, scale: float = 1.0, padding_id: int = -1, accumulate: bool = False,
+                       stream=None, check: bool = True) -> int:
+    """streambp_embedding_backward; d_out [n, d] with contiguous rows, d_table fp32 [vocab, d] (overwritten, or added to)."""
+    what, dev, dt = "embedding_backward", _matrix("embedding_backward", "d_out", d_out), d_out.dtype
+    n, d = d_out.shape
+    _want(d_table.dim() == 2 and d_table.shape[1] == d, what, "d_table is [vocab, d]")
+    V = d_table.shape[0]
+    g = _rows(what, dev, dt, (n, d), d_out)
+    i = _vectors(what, dev, (n,), ids=(ids, torch.int64)) + _vectors(what, dev, (V, d), d_table=(d_table, torch.float32))
+    st = _launch(what, dev, stream, lib().streambp_embedding_backward, g[0], g[1], i[0], n, V, d, _dtype_code(dt), scale, padding_id,
+                 1 if accumulate else 0, i[1], *_space(what, dev, workspace))
+    if check:
+        _check(st, "streambp_embedding_backward")
     return st

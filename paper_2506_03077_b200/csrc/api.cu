@@ -1,5 +1,6 @@
 // extern "C" boundary: argument validation, dtype dispatch, status handling.
 #include <atomic>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <type_traits>
@@ -10,6 +11,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "common.cuh"
+#include "embedding.cuh"
 #include "window.cuh"
 
 namespace sbp {
@@ -386,6 +388,65 @@ size_t epilogue_scratch(int64_t M, int64_t N, void *base, EpilogueScratch *out) 
     out->partials = a.take<float>((size_t)gemm_epilogue_splits(M, N) * 2 * (size_t)N);
     out->guards = a.guards;
     return a.size();
+}
+
+// header of a workspace that holds nothing else
+size_t status_scratch(void *base, std::vector<size_t> *guards) {
+    Arena a(base);
+    a.take_bytes(kHeaderBytes);
+    if (guards) *guards = a.guards;
+    return a.size();
+}
+// scratch of the layer norm's gradient: the blocks' sums
+struct NormScratch {
+    float *partials;
+    std::vector<size_t> guards;
+};
+size_t norm_scratch(int64_t rows, int64_t d, void *base, NormScratch *out) {
+    Arena a(base);
+    a.take_bytes(kHeaderBytes);
+    out->partials = a.take<float>((size_t)layernorm_blocks(rows, d) * 2 * (size_t)d);
+    out->guards = a.guards;
+    return a.size();
+}
+// scratch of the embedding's gradient: two copies of the keys and tokens, the counts of the sort, the chunks' partial sums
+struct EmbeddingScratch {
+    EmbeddingPlan plan;
+    int *keys[2], *tokens[2], *counts;
+    float *partials;
+    std::vector<size_t> guards;
+};
+size_t embedding_scratch(int64_t n, int64_t vocab, int64_t d, void *base, EmbeddingScratch *out) {
+    Arena a(base);
+    a.take_bytes(kHeaderBytes);
+    out->plan = embedding_plan(n, vocab, d);
+    for (int i = 0; i < 2; i++) {
+        out->keys[i] = a.take<int>(n);
+        out->tokens[i] = a.take<int>(n);
+    }
+    out->counts = a.take<int>((size_t)256 * out->plan.tiles);
+    out->partials = a.take<float>((size_t)out->plan.chunks * 2 * (size_t)d);
+    out->guards = a.guards;
+    return a.size();
+}
+int check_dtype(int32_t dtype) { return dtype == STREAMBP_F32 || dtype == STREAMBP_BF16 ? STREAMBP_OK : STREAMBP_E_DTYPE; }
+int check_rows_of_logits(int64_t rows, int64_t vocab, int64_t most_vocab, float temperature) {
+    if (rows < 1 || rows > (1ll << 27) || vocab < 1 || vocab > most_vocab) return STREAMBP_E_SHAPE;
+    return temperature >= 0x1p-20f && temperature <= 0x1p20f ? STREAMBP_OK : STREAMBP_E_SHAPE;
+}
+int check_distill(const streambp_distill_cfg *c) {
+    if (!c) return STREAMBP_E_NULL;
+    if (c->k < 1 || c->k > STREAMBP_TOP_MAX || c->tail < 0 || c->tail > 1) return STREAMBP_E_SHAPE;
+    return STREAMBP_OK;
+}
+int check_embedding(int64_t n, int64_t vocab, int64_t d, int32_t dtype, float scale) {
+    SBP_TRY(check_dtype(dtype));
+    if (n < 1 || n >= (1ll << 30) || vocab < 1 || vocab >= 0x7fffffffll || d < 1 || d > (1ll << 20)) return STREAMBP_E_SHAPE;
+    return scale - scale == 0.f ? STREAMBP_OK : STREAMBP_E_SHAPE;
+}
+void start_call() {
+    call_state().cuda_error = 0;
+    call_state().launches = 0;
 }
 
 // weights with the bias pointers dropped when the configuration has no bias
@@ -994,6 +1055,261 @@ int streambp_gemm_swiglu(const void *A, int64_t lda, const void *w_gate, const v
                                 (float *)u, (float *)m, N, st);
     return mm_swiglu<bf16>(M, N, K, (const bf16 *)A, lda, (const bf16 *)w_gate, (const bf16 *)w_up, ldb, (bf16 *)g, (bf16 *)u,
                            (bf16 *)m, N, st);
+}
+
+// ---- the ends of a model ----------------------------------------------------------------------------------------------
+size_t streambp_token_logprobs_workspace_bytes(void) { return status_scratch(nullptr, nullptr); }
+
+int streambp_token_logprobs(const void *logits, int64_t ld, int64_t rows, int64_t vocab, int32_t dtype, const int64_t *tokens,
+                            int64_t ignore_index, float temperature, int32_t k, float *logp, float *lse, float *entropy,
+                            float *top_logp, int64_t *top_ids, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!logits || !workspace || (logp && !tokens)) return STREAMBP_E_NULL;
+    SBP_TRY(check_dtype(dtype));
+    SBP_TRY(check_rows_of_logits(rows, vocab, 1ll << 27, temperature));
+    if (k < 0 || k > STREAMBP_TOP_MAX || k > vocab) return STREAMBP_E_SHAPE;
+    if (!logp && !lse && !entropy && !(k && (top_logp || top_ids))) return STREAMBP_E_NULL;
+    SBP_TRY(check_matrix(logits, ld, vocab, dtype == STREAMBP_F32 ? 4 : 2));
+    if (!aligned(tokens, 8) || !aligned(logp, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(top_logp, 4) ||
+        !aligned(top_ids, 8) || !aligned(workspace, 256))
+        return STREAMBP_E_ALIGN;
+    std::vector<size_t> guards;
+    if (workspace_bytes < status_scratch(workspace, &guards)) return STREAMBP_E_WORKSPACE;
+    if (!top_logp && !top_ids) k = 0;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    start_call();
+    WsHeader *hdr = static_cast<WsHeader *>(workspace);
+    SBP_TRY(ws_guards_arm(workspace, guards, st));        // (a kernel of the call writes the status)
+    if (dtype == STREAMBP_F32)
+        SBP_TRY(token_logprobs<float>((const float *)logits, ld, rows, vocab, tokens, ignore_index, temperature, k, logp, lse, entropy,
+                                      top_logp, top_ids, hdr, st));
+    else
+        SBP_TRY(token_logprobs<bf16>((const bf16 *)logits, ld, rows, vocab, tokens, ignore_index, temperature, k, logp, lse, entropy,
+                                     top_logp, top_ids, hdr, st));
+    return ws_guards_check(workspace, guards, hdr, st);
+}
+
+int streambp_token_logprobs_backward(const void *logits, int64_t ld, int64_t rows, int64_t vocab, int32_t dtype,
+                                     const int64_t *tokens, int64_t ignore_index, float temperature, const float *lse,
+                                     const float *entropy, const float *d_logp, const float *d_lse, const float *d_entropy,
+                                     void *d_logits, int64_t ldd, void *cuda_stream) {
+    if (!logits || !lse || !d_logits || (d_entropy && !entropy) || (d_logp && !tokens)) return STREAMBP_E_NULL;
+    SBP_TRY(check_dtype(dtype));
+    SBP_TRY(check_rows_of_logits(rows, vocab, 1ll << 27, temperature));
+    const int es = dtype == STREAMBP_F32 ? 4 : 2;
+    SBP_TRY(check_matrix(logits, ld, vocab, es));
+    SBP_TRY(check_matrix(d_logits, ldd, vocab, es));
+    if (logits == d_logits && ld != ldd) return STREAMBP_E_SHAPE;
+    if (!aligned(tokens, 8) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(d_logp, 4) || !aligned(d_lse, 4) ||
+        !aligned(d_entropy, 4))
+        return STREAMBP_E_ALIGN;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    start_call();
+    if (dtype == STREAMBP_F32)
+        return token_logprobs_bwd<float>((const float *)logits, ld, rows, vocab, tokens, ignore_index, temperature, lse, entropy, d_logp,
+                                         d_lse, d_entropy, (float *)d_logits, ldd, st);
+    return token_logprobs_bwd<bf16>((const bf16 *)logits, ld, rows, vocab, tokens, ignore_index, temperature, lse, entropy, d_logp,
+                                    d_lse, d_entropy, (bf16 *)d_logits, ldd, st);
+}
+
+size_t streambp_distill_topk_workspace_bytes(void) { return status_scratch(nullptr, nullptr); }
+
+int streambp_distill_topk(const streambp_distill_cfg *distill, const void *logits, int64_t ld, int64_t rows, int64_t vocab,
+                          int32_t dtype, const int64_t *ids, const float *values, const float *weight, float *row_loss,
+                          void *d_logits, int64_t ldd, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    SBP_TRY(check_distill(distill));
+    if (!logits || !ids || !values || (!row_loss && !d_logits) || !workspace) return STREAMBP_E_NULL;
+    SBP_TRY(check_dtype(dtype));
+    SBP_TRY(check_rows_of_logits(rows, vocab, STREAMBP_DISTILL_MAX_VOCAB, distill->temperature));
+    const int es = dtype == STREAMBP_F32 ? 4 : 2;
+    SBP_TRY(check_matrix(logits, ld, vocab, es));
+    if (d_logits) SBP_TRY(check_matrix(d_logits, ldd, vocab, es));
+    if (logits == d_logits && ld != ldd) return STREAMBP_E_SHAPE;
+    if (!aligned(ids, 8) || !aligned(values, 4) || !aligned(weight, 4) || !aligned(row_loss, 4) || !aligned(workspace, 256))
+        return STREAMBP_E_ALIGN;
+    std::vector<size_t> guards;
+    if (workspace_bytes < status_scratch(workspace, &guards)) return STREAMBP_E_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    start_call();
+    WsHeader *hdr = static_cast<WsHeader *>(workspace);
+    SBP_TRY(ws_guards_arm(workspace, guards, st));        // (a kernel of the call writes the status)
+    const DistillRows ds{distill->k, distill->tail != 0, distill->temperature, ids, values, weight, row_loss};
+    if (dtype == STREAMBP_F32)
+        SBP_TRY((distill_topk<float, float>((const float *)logits, ld, rows, vocab, ds, (float *)d_logits, ldd, hdr, st)));
+    else
+        SBP_TRY((distill_topk<bf16, bf16>((const bf16 *)logits, ld, rows, vocab, ds, (bf16 *)d_logits, ldd, hdr, st)));
+    return ws_guards_check(workspace, guards, hdr, st);
+}
+
+size_t streambp_lmhead_logprobs_workspace_bytes(const streambp_head_cfg *cfg, int64_t T, int64_t chunk) {
+    if (check_head_cfg(cfg) != STREAMBP_OK || T < 1 || chunk < 1) return 0;
+    return cfg->dtype == STREAMBP_F32 ? lmhead_logprobs_workspace<float>(*cfg, T, chunk) : lmhead_logprobs_workspace<bf16>(*cfg, T, chunk);
+}
+
+int streambp_lmhead_logprobs(const streambp_head_cfg *cfg, const void *g_final, const void *w_vocab, const void *H,
+                             const int64_t *tokens, int64_t T, int64_t chunk, float temperature, int32_t k, float *logp,
+                             float *lse, float *entropy, float *top_logp, int64_t *top_ids, void *workspace,
+                             size_t workspace_bytes, void *cuda_stream) {
+    SBP_TRY(check_head_cfg(cfg));
+    if (!g_final || !w_vocab || !H || !workspace || (logp && !tokens)) return STREAMBP_E_NULL;
+    if (chunk < 1) return STREAMBP_E_SHAPE;
+    SBP_TRY(check_rows_of_logits(T, cfg->vocab, 1ll << 27, temperature));
+    if (k < 0 || k > STREAMBP_TOP_MAX || k > cfg->vocab) return STREAMBP_E_SHAPE;
+    if (!logp && !lse && !entropy && !(k && (top_logp || top_ids))) return STREAMBP_E_NULL;
+    if (!aligned(g_final, 16) || !aligned(w_vocab, 16) || !aligned(H, 16) || !aligned(tokens, 8) || !aligned(logp, 4) ||
+        !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(top_logp, 4) || !aligned(top_ids, 8) || !aligned(workspace, 256))
+        return STREAMBP_E_ALIGN;
+    if (workspace_bytes < streambp_lmhead_logprobs_workspace_bytes(cfg, T, chunk)) return STREAMBP_E_WORKSPACE;
+    if (!top_logp && !top_ids) k = 0;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    SBP_TRY(begin_call(workspace, st));
+    if (cfg->dtype == STREAMBP_F32)
+        return lmhead_logprobs<float>(*cfg, (const float *)g_final, (const float *)w_vocab, (const float *)H, tokens, T, chunk,
+                                      temperature, k, logp, lse, entropy, top_logp, top_ids, workspace, st);
+    return lmhead_logprobs<bf16>(*cfg, (const bf16 *)g_final, (const bf16 *)w_vocab, (const bf16 *)H, tokens, T, chunk, temperature, k,
+                                 logp, lse, entropy, top_logp, top_ids, workspace, st);
+}
+
+size_t streambp_lmhead_distill_workspace_bytes(const streambp_head_cfg *cfg, int64_t T, int64_t chunk, int32_t wgrad_group) {
+    if (check_head_cfg(cfg) != STREAMBP_OK || T < 1 || chunk < 1 || wgrad_group < 1) return 0;
+    return cfg->dtype == STREAMBP_F32 ? lmhead_distill_workspace<float>(*cfg, T, chunk, wgrad_group)
+                                      : lmhead_distill_workspace<bf16>(*cfg, T, chunk, wgrad_group);
+}
+
+int streambp_lmhead_distill_backward(const streambp_head_cfg *cfg, const streambp_distill_cfg *distill, const void *g_final,
+                                     const void *w_vocab, const void *H, const int64_t *ids, const float *values,
+                                     const float *weight, int64_t T, int64_t chunk, int32_t wgrad_group, int accumulate,
+                                     float *loss, float *row_loss, void *dH, float *d_w_vocab, float *d_g_final,
+                                     void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    SBP_TRY(check_head_cfg(cfg));
+    SBP_TRY(check_distill(distill));
+    if (chunk < 1 || wgrad_group < 1) return STREAMBP_E_SHAPE;
+    SBP_TRY(check_rows_of_logits(T, cfg->vocab, STREAMBP_DISTILL_MAX_VOCAB, distill->temperature));
+    if (!g_final || !w_vocab || !H || !ids || !values || !weight || !loss || !dH || !d_w_vocab || !d_g_final || !workspace)
+        return STREAMBP_E_NULL;
+    if (!aligned(g_final, 16) || !aligned(w_vocab, 16) || !aligned(H, 16) || !aligned(dH, 16) || !aligned(d_w_vocab, 16) ||
+        !aligned(d_g_final, 16) || !aligned(ids, 8) || !aligned(values, 4) || !aligned(weight, 4) || !aligned(loss, 4) ||
+        !aligned(row_loss, 4) || !aligned(workspace, 256))
+        return STREAMBP_E_ALIGN;
+    if (workspace_bytes < streambp_lmhead_distill_workspace_bytes(cfg, T, chunk, wgrad_group)) return STREAMBP_E_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    SBP_TRY(begin_call(workspace, st));
+    const DistillRows ds{distill->k, distill->tail != 0, distill->temperature, ids, values, weight, row_loss};
+    if (cfg->dtype == STREAMBP_F32)
+        return lmhead_backward<float>(*cfg, (const float *)g_final, (const float *)w_vocab, (const float *)H, nullptr, T, chunk,
+                                      accumulate != 0, loss, nullptr, (float *)dH, d_w_vocab, d_g_final, workspace, st, nullptr,
+                                      nullptr, wgrad_group, &ds);
+    return lmhead_backward<bf16>(*cfg, (const bf16 *)g_final, (const bf16 *)w_vocab, (const bf16 *)H, nullptr, T, chunk,
+                                 accumulate != 0, loss, nullptr, (bf16 *)dH, d_w_vocab, d_g_final, workspace, st, nullptr, nullptr,
+                                 wgrad_group, &ds);
+}
+
+int streambp_layernorm_forward(const void *x, int64_t ldx, const void *gain, const void *bias, float eps, int64_t rows, int64_t d,
+                               int32_t dtype, void *y, int64_t ldy, float *mean, float *rstd, void *cuda_stream) {
+    if (!x || !y) return STREAMBP_E_NULL;
+    SBP_TRY(check_dtype(dtype));
+    if (rows < 1 || rows > 0x7fffffffll || d < 1 || d > (1ll << 20) || !(eps >= 0.f) || !(eps < INFINITY)) return STREAMBP_E_SHAPE;
+    const int es = dtype == STREAMBP_F32 ? 4 : 2;
+    SBP_TRY(check_matrix(x, ldx, d, es));
+    SBP_TRY(check_matrix(y, ldy, d, es));
+    if (x == y && ldx != ldy) return STREAMBP_E_SHAPE;
+    if (!aligned(gain, es) || !aligned(bias, es) || !aligned(mean, 4) || !aligned(rstd, 4)) return STREAMBP_E_ALIGN;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    start_call();
+    if (dtype == STREAMBP_F32)
+        return layernorm_fwd<float>((const float *)x, ldx, (const float *)gain, (const float *)bias, eps, rows, d, (float *)y, ldy, mean,
+                                    rstd, st);
+    return layernorm_fwd<bf16>((const bf16 *)x, ldx, (const bf16 *)gain, (const bf16 *)bias, eps, rows, d, (bf16 *)y, ldy, mean, rstd, st);
+}
+
+size_t streambp_layernorm_workspace_bytes(int64_t rows, int64_t d) {
+    if (rows < 1 || rows > 0x7fffffffll || d < 1 || d > (1ll << 20)) return 0;
+    NormScratch s;
+    return norm_scratch(rows, d, nullptr, &s);
+}
+
+int streambp_layernorm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *gain, const float *mean,
+                                const float *rstd, const void *add, int64_t ldadd, int64_t rows, int64_t d, int32_t dtype,
+                                void *dx, int64_t lddx, float *d_gain, float *d_bias, int accumulate, void *workspace,
+                                size_t workspace_bytes, void *cuda_stream) {
+    const bool sums = d_gain || d_bias;
+    if (!dy || !x || !mean || !rstd || (!dx && !sums) || (sums && !workspace)) return STREAMBP_E_NULL;
+    SBP_TRY(check_dtype(dtype));
+    if (rows < 1 || rows > 0x7fffffffll || d < 1 || d > (1ll << 20)) return STREAMBP_E_SHAPE;
+    const int es = dtype == STREAMBP_F32 ? 4 : 2;
+    SBP_TRY(check_matrix(dy, lddy, d, es));
+    SBP_TRY(check_matrix(x, ldx, d, es));
+    if (add) SBP_TRY(check_matrix(add, ldadd, d, es));
+    if (dx) SBP_TRY(check_matrix(dx, lddx, d, es));
+    if (dx && ((dx == dy && lddx != lddy) || (dx == x && lddx != ldx) || (dx == add && lddx != ldadd))) return STREAMBP_E_SHAPE;
+    if (!aligned(gain, es) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(d_gain, 4) || !aligned(d_bias, 4)) return STREAMBP_E_ALIGN;
+    NormScratch s{};
+    if (sums) {
+        if (!aligned(workspace, 256)) return STREAMBP_E_ALIGN;
+        if (workspace_bytes < norm_scratch(rows, d, workspace, &s)) return STREAMBP_E_WORKSPACE;
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    start_call();
+    WsHeader *hdr = static_cast<WsHeader *>(workspace);
+    SBP_TRY(ws_guards_arm(workspace, s.guards, st));      // (a kernel of the call clears the status, which the check may set)
+    if (dtype == STREAMBP_F32)
+        SBP_TRY(layernorm_bwd<float>((const float *)dy, lddy, (const float *)x, ldx, (const float *)gain, mean, rstd, (const float *)add,
+                                     ldadd, rows, d, (float *)dx, lddx, d_gain, d_bias, accumulate != 0, s.partials, hdr, st));
+    else
+        SBP_TRY(layernorm_bwd<bf16>((const bf16 *)dy, lddy, (const bf16 *)x, ldx, (const bf16 *)gain, mean, rstd, (const bf16 *)add, ldadd,
+                                    rows, d, (bf16 *)dx, lddx, d_gain, d_bias, accumulate != 0, s.partials, hdr, st));
+    return ws_guards_check(workspace, s.guards, hdr, st);
+}
+
+size_t streambp_embedding_workspace_bytes(void) { return status_scratch(nullptr, nullptr); }
+
+int streambp_embedding_forward(const void *table, int64_t ld, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, int32_t dtype,
+                               float scale, int64_t padding_id, void *out, int64_t ldo, void *workspace, size_t workspace_bytes,
+                               void *cuda_stream) {
+    if (!table || !ids || !out || !workspace) return STREAMBP_E_NULL;
+    SBP_TRY(check_embedding(n, vocab, d, dtype, scale));
+    const int es = dtype == STREAMBP_F32 ? 4 : 2;
+    SBP_TRY(check_matrix(table, ld, d, es));
+    SBP_TRY(check_matrix(out, ldo, d, es));
+    if (!aligned(ids, 8) || !aligned(workspace, 256)) return STREAMBP_E_ALIGN;
+    std::vector<size_t> guards;
+    if (workspace_bytes < status_scratch(workspace, &guards)) return STREAMBP_E_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    start_call();
+    WsHeader *hdr = static_cast<WsHeader *>(workspace);
+    SBP_TRY(ws_guards_arm(workspace, guards, st));        // (a kernel of the call writes the status)
+    if (dtype == STREAMBP_F32)
+        SBP_TRY(embedding_fwd<float>((const float *)table, ld, ids, n, vocab, d, scale, padding_id, (float *)out, ldo, hdr, st));
+    else
+        SBP_TRY(embedding_fwd<bf16>((const bf16 *)table, ld, ids, n, vocab, d, scale, padding_id, (bf16 *)out, ldo, hdr, st));
+    return ws_guards_check(workspace, guards, hdr, st);
+}
+
+size_t streambp_embedding_backward_workspace_bytes(int64_t n, int64_t vocab, int64_t d) {
+    if (check_embedding(n, vocab, d, STREAMBP_F32, 1.f) != STREAMBP_OK) return 0;
+    EmbeddingScratch s;
+    return embedding_scratch(n, vocab, d, nullptr, &s);
+}
+
+int streambp_embedding_backward(const void *d_out, int64_t ldo, const int64_t *ids, int64_t n, int64_t vocab, int64_t d,
+                                int32_t dtype, float scale, int64_t padding_id, int accumulate, float *d_table, void *workspace,
+                                size_t workspace_bytes, void *cuda_stream) {
+    if (!d_out || !ids || !d_table || !workspace) return STREAMBP_E_NULL;
+    SBP_TRY(check_embedding(n, vocab, d, dtype, scale));
+    SBP_TRY(check_matrix(d_out, ldo, d, dtype == STREAMBP_F32 ? 4 : 2));
+    if (!aligned(ids, 8) || !aligned(d_table, 16) || !aligned(workspace, 256)) return STREAMBP_E_ALIGN;
+    EmbeddingScratch s;
+    if (workspace_bytes < embedding_scratch(n, vocab, d, workspace, &s)) return STREAMBP_E_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    start_call();
+    WsHeader *hdr = static_cast<WsHeader *>(workspace);
+    SBP_TRY(ws_guards_arm(workspace, s.guards, st));      // (a kernel of the call writes the status)
+    if (dtype == STREAMBP_F32)
+        SBP_TRY(embedding_bwd<float>((const float *)d_out, ldo, ids, n, vocab, d, scale, padding_id, d_table, accumulate != 0, s.plan,
+                                     s.keys, s.tokens, s.counts, s.partials, hdr, st));
+    else
+        SBP_TRY(embedding_bwd<bf16>((const bf16 *)d_out, ldo, ids, n, vocab, d, scale, padding_id, d_table, accumulate != 0, s.plan, s.keys,
+                                    s.tokens, s.counts, s.partials, hdr, st));
+    return ws_guards_check(workspace, s.guards, hdr, st);
 }
 
 }  // extern "C"

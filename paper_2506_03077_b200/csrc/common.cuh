@@ -511,6 +511,53 @@ template <typename T>
 int embedding_scatter_add(const T *dx, const int64_t *ids, int64_t rows, int d, int64_t vocab, float *d_embed,
                           cudaStream_t st);
 
+// Rows of logits: token log-probabilities with entropy and the k largest (hdr, if given, gets the status), and their gradient.
+template <typename T>
+int token_logprobs(const T *logits, int64_t ld, int64_t rows, int64_t vocab, const int64_t *tokens, int64_t ignore,
+                   float temperature, int k, float *logp, float *lse, float *entropy, float *top_logp, int64_t *top_ids,
+                   WsHeader *hdr, cudaStream_t st);
+template <typename T>
+int token_logprobs_bwd(const T *logits, int64_t ld, int64_t rows, int64_t vocab, const int64_t *tokens, int64_t ignore,
+                       float temperature, const float *lse, const float *entropy, const float *d_logp, const float *d_lse,
+                       const float *d_entropy, T *d_logits, int64_t ldd, cudaStream_t st);
+// Distillation from a teacher's top logits (TO: type of the gradient).  ids, values, weight, row_loss of the first row.
+struct DistillRows {
+    int k;
+    bool tail;
+    float temperature;
+    const int64_t *ids;
+    const float *values;
+    const float *weight;      // optional (the LM head needs it)
+    float *row_loss;          // optional
+};
+template <typename T, typename TO>
+int distill_topk(const T *logits, int64_t ld, int64_t rows, int64_t vocab, const DistillRows &ds, TO *d_logits, int64_t ldd,
+                 WsHeader *hdr, cudaStream_t st);
+// For the LM head: marks[t] = 0 where row t takes part, else 1; ids outside the vocabulary go into the status.
+int distill_marks(const DistillRows &ds, int64_t T, int64_t vocab, int64_t *marks, WsHeader *hdr, cudaStream_t st);
+// loss sum of the header += sum of weight * row_loss
+int loss_accumulate_weighted(const float *row_loss, const float *weight, int64_t rows, WsHeader *hdr, cudaStream_t st);
+
+// Layer norm; blocks that share the rows of a backward pass, partials: [layernorm_blocks][2][d]
+template <typename T>
+int layernorm_fwd(const T *x, int64_t ldx, const T *gain, const T *bias, float eps, int64_t rows, int64_t d, T *y, int64_t ldy,
+                  float *mean, float *rstd, cudaStream_t st);
+int layernorm_blocks(int64_t rows, int64_t d);
+template <typename T>
+int layernorm_bwd(const T *dy, int64_t lddy, const T *x, int64_t ldx, const T *gain, const float *mean, const float *rstd,
+                  const T *add, int64_t ldadd, int64_t rows, int64_t d, T *dx, int64_t lddx, float *dgain, float *dbias,
+                  bool accumulate, float *partials, WsHeader *hdr, cudaStream_t st);
+
+// Embedding lookup with a scale, and its gradient by sorted tokens (embedding.cuh)
+struct EmbeddingPlan;
+template <typename T>
+int embedding_fwd(const T *table, int64_t ld, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, float scale,
+                  int64_t padding, T *out, int64_t ldo, WsHeader *hdr, cudaStream_t st);
+template <typename T>
+int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, float scale, int64_t padding,
+                  float *d_table, bool accumulate, const EmbeddingPlan &p, int *const (&keys)[2], int *const (&tokens)[2],
+                  int *counts, float *partials, WsHeader *hdr, cudaStream_t st);
+
 // Grouped products used by the schedulers: independent problems that become ready together go out as one
 // launch (tensor cores) or one after the other (CUDA cores); a problem may sum several K segments.
 template <typename T>
@@ -585,12 +632,21 @@ template <typename T>
 size_t lmhead_workspace(const streambp_head_cfg &c, int64_t T_, int64_t chunk, int wgrad_group = 1);
 // rl == nullptr: SFT cross-entropy (labels = targets); else the RL objective described by *rl (labels = the
 // sampled tokens, rl->logp_* etc. indexed by absolute row), `ell` optional (DPO).  wgrad_group >= 1: the vocabulary
-// weight gradient is formed once per group of that many chunks.
+// weight gradient is formed once per group of that many chunks.  distill: the loss is that of a teacher's lists instead (labels
+// are not read; their workspace holds the marks of the rows that take part).
 template <typename T>
 int lmhead_backward(const streambp_head_cfg &c, const T *g_final, const T *w_vocab, const T *H, const int64_t *labels,
                     int64_t T_, int64_t chunk, bool accumulate, float *loss, int64_t *n_valid, T *dH, float *d_w_vocab,
                     float *d_g_final, void *ws, cudaStream_t st, const RlRows *rl = nullptr, float *ell = nullptr,
-                    int wgrad_group = 1);
+                    int wgrad_group = 1, const DistillRows *distill = nullptr);
+template <typename T>
+size_t lmhead_distill_workspace(const streambp_head_cfg &c, int64_t T_, int64_t chunk, int wgrad_group);
+template <typename T>
+size_t lmhead_logprobs_workspace(const streambp_head_cfg &c, int64_t T_, int64_t chunk);
+template <typename T>
+int lmhead_logprobs(const streambp_head_cfg &c, const T *g_final, const T *w_vocab, const T *H, const int64_t *tokens, int64_t T_,
+                    int64_t chunk, float temperature, int k, float *logp, float *lse, float *entropy, float *top_logp,
+                    int64_t *top_ids, void *ws, cudaStream_t st);
 
 template <typename T>
 size_t model_workspace(const streambp_model_cfg &c, int64_t T_, int64_t chunk_layer, int64_t chunk_head);

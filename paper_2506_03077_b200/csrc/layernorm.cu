@@ -1,0 +1,408 @@
+// Layer norm: y = (x - mean) rstd gain + bias over the columns of each row, and its gradient with the sums of gain and bias.
+//
+//   xhat = (x - mean) rstd,  g = dy gain,  dx = (g - mean(g) - xhat mean(g xhat)) rstd (+ add)
+//   dgain = sum over rows of dy xhat,  dbias = sum over rows of dy
+// A row's values stay in registers between the passes over it, so that all tensors cross HBM once.  Rows go to blocks of as
+// many threads as hold them; the column sums stay in the threads that own the columns while a block walks its rows, and the
+// blocks' sums are joined in their order by a second launch (no atomics: equal inputs give equal bits).
+#include <algorithm>
+
+#include "sm100.cuh"
+
+namespace sbp {
+
+namespace {
+constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32;
+
+// N elements at a time: 16 bytes, or one where a pointer, a leading dimension or the width is not made of 16-byte groups.
+// They stay in their storage type while they wait.
+template <typename T, int N> struct Pack {
+    uint4 w;
+    __device__ __forceinline__ void load(const T *p) { w = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void clear() { w = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void get(float (&x)[N]) const {
+        Vec<T> a;
+        a.load(reinterpret_cast<const T *>(&w));
+#pragma unroll
+        for (int i = 0; i < N; i++) x[i] = a.v[i];
+    }
+    static __device__ __forceinline__ void store(T *p, const float (&x)[N]) {
+        Vec<T> a;
+#pragma unroll
+        for (int i = 0; i < N; i++) a.v[i] = x[i];
+        a.store(p);
+    }
+};
+template <typename T> struct Pack<T, 1> {
+    T w;
+    __device__ __forceinline__ void load(const T *p) { w = *p; }
+    __device__ __forceinline__ void clear() { w = from_f32<T>(0.f); }
+    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = to_f32(w); }
+    static __device__ __forceinline__ void store(T *p, const float (&x)[1]) { *p = from_f32<T>(x[0]); }
+};
+
+// Sums of two values over the threads of a row: one warp (no barrier), or the block (one barrier; `slot` alternates).
+template <bool WARP>
+__device__ __forceinline__ float2 row_sum(float a, float b, float2 (*red)[kMaxWarps], int slot) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+    }
+    if (WARP) return make_float2(a, b);
+    if ((threadIdx.x & 31) == 0) red[slot][threadIdx.x >> 5] = make_float2(a, b);
+    __syncthreads();
+    float2 s = make_float2(0.f, 0.f);
+    for (int w = 0; w < (int)(blockDim.x >> 5); w++) {
+        s.x += red[slot][w].x;
+        s.y += red[slot][w].y;
+    }
+    return s;
+}
+
+template <typename T>
+struct NormArgs {
+    const T *x, *gain, *bias;           // gain and bias are optional
+    T *y;
+    float *mean, *rstd;                 // optional
+    int64_t rows, ldx, ldy;
+    int d;
+    float eps;
+};
+
+// WARP: a warp to a row, else a block
+template <typename T, int N, int NV, bool WARP>
+__global__ void __launch_bounds__(kMaxThreads) norm_fwd_kernel(NormArgs<T> a) {
+    pdl_enter();
+    __shared__ float2 red[2][kMaxWarps];
+    const int lanes = WARP ? 32 : blockDim.x, lane = WARP ? threadIdx.x & 31 : threadIdx.x;
+    const int64_t r = WARP ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
+    if (r >= a.rows) return;
+    const T *x = a.x + r * a.ldx;
+    Pack<T, N> p[NV];
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+        const int c = (lane + j * lanes) * N;
+        if (c < a.d) p[j].load(x + c);
+        else p[j].clear();
+    }
+    float s = 0.f, v[N];
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+        p[j].get(v);
+#pragma unroll
+        for (int i = 0; i < N; i++) s += v[i];
+    }
+    const float mean = row_sum<WARP>(s, 0.f, red, 0).x / (float)a.d;
+    s = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+        if ((lane + j * lanes) * N >= a.d) continue;
+        p[j].get(v);
+#pragma unroll
+        for (int i = 0; i < N; i++) s = fmaf(v[i] - mean, v[i] - mean, s);
+    }
+    const float rstd = rsqrtf(row_sum<WARP>(s, 0.f, red, 1).x / (float)a.d + a.eps);
+    if (lane == 0) {
+        if (a.mean) a.mean[r] = mean;
+        if (a.rstd) a.rstd[r] = rstd;
+    }
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+        const int c = (lane + j * lanes) * N;
+        if (c >= a.d) continue;
+        float g[N], b[N];
+        Pack<T, N> q;
+        p[j].get(v);
+#pragma unroll
+        for (int i = 0; i < N; i++) v[i] = (v[i] - mean) * rstd;
+        if (a.gain) {
+            q.load(a.gain + c);
+            q.get(g);
+#pragma unroll
+            for (int i = 0; i < N; i++) v[i] *= g[i];
+        }
+        if (a.bias) {
+            q.load(a.bias + c);
+            q.get(b);
+#pragma unroll
+            for (int i = 0; i < N; i++) v[i] += b[i];
+        }
+        Pack<T, N>::store(a.y + r * a.ldy + c, v);
+    }
+}
+
+// rows too wide for registers: the row is read three times (the second and third time from L2)
+template <typename T>
+__global__ void __launch_bounds__(kMaxThreads) norm_fwd_wide_kernel(NormArgs<T> a) {
+    pdl_enter();
+    __shared__ float2 red[2][kMaxWarps];
+    const int64_t r = blockIdx.x;
+    const T *x = a.x + r * a.ldx;
+    float s = 0.f;
+    for (int c = threadIdx.x; c < a.d; c += blockDim.x) s += to_f32(x[c]);
+    const float mean = row_sum<false>(s, 0.f, red, 0).x / (float)a.d;
+    s = 0.f;
+    for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
+        const float v = to_f32(x[c]) - mean;
+        s = fmaf(v, v, s);
+    }
+    const float rstd = rsqrtf(row_sum<false>(s, 0.f, red, 1).x / (float)a.d + a.eps);
+    if (threadIdx.x == 0) {
+        if (a.mean) a.mean[r] = mean;
+        if (a.rstd) a.rstd[r] = rstd;
+    }
+    for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
+        float v = (to_f32(x[c]) - mean) * rstd;
+        if (a.gain) v *= to_f32(a.gain[c]);
+        if (a.bias) v += to_f32(a.bias[c]);
+        a.y[r * a.ldy + c] = from_f32<T>(v);
+    }
+}
+
+template <typename T>
+struct NormGradArgs {
+    const T *dy, *x, *gain, *add;       // gain and add are optional
+    const float *mean, *rstd;
+    T *dx;                              // optional
+    float *partials;                    // [blocks][2][d], null where no sums are wanted
+    int64_t rows, lddy, ldx, ldadd, lddx;
+    int d;
+};
+
+template <typename T, int N, int NV>
+__global__ void __launch_bounds__(kMaxThreads) norm_bwd_kernel(NormGradArgs<T> a) {
+    pdl_enter();
+    __shared__ float2 red[2][kMaxWarps];
+    const int lanes = blockDim.x, lane = threadIdx.x;
+    float sg[NV][N], sb[NV][N];
+#pragma unroll
+    for (int j = 0; j < NV; j++)
+#pragma unroll
+        for (int i = 0; i < N; i++) sg[j][i] = sb[j][i] = 0.f;
+    Pack<T, N> gain[NV];
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+        const int c = (lane + j * lanes) * N;
+        gain[j].clear();
+        if (a.gain && c < a.d) gain[j].load(a.gain + c);
+    }
+    int slot = 0;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, slot ^= 1) {
+        Pack<T, N> dy[NV], x[NV], add[NV];
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const int c = (lane + j * lanes) * N;
+            dy[j].clear();
+            x[j].clear();
+            add[j].clear();
+            if (c >= a.d) continue;
+            dy[j].load(a.dy + r * a.lddy + c);
+            x[j].load(a.x + r * a.ldx + c);
+            if (a.add) add[j].load(a.add + r * a.ldadd + c);
+        }
+        const float mean = a.mean[r], rstd = a.rstd[r];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            if ((lane + j * lanes) * N >= a.d) continue;
+            float g[N], h[N], w[N];
+            dy[j].get(g);
+            x[j].get(h);
+            gain[j].get(w);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                h[i] = (h[i] - mean) * rstd;
+                sg[j][i] = fmaf(g[i], h[i], sg[j][i]);
+                sb[j][i] += g[i];
+                if (a.gain) g[i] *= w[i];
+                s1 += g[i];
+                s2 = fmaf(g[i], h[i], s2);
+            }
+        }
+        if (!a.dx) continue;
+        const float2 s = row_sum<false>(s1, s2, red, slot);
+        const float m1 = s.x / (float)a.d, m2 = s.y / (float)a.d;
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const int c = (lane + j * lanes) * N;
+            if (c >= a.d) continue;
+            float g[N], h[N], w[N], t[N];
+            dy[j].get(g);
+            x[j].get(h);
+            gain[j].get(w);
+            add[j].get(t);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                if (a.gain) g[i] *= w[i];
+                g[i] = fmaf(g[i] - m1 - (h[i] - mean) * rstd * m2, rstd, t[i]);
+            }
+            Pack<T, N>::store(a.dx + r * a.lddx + c, g);
+        }
+    }
+    if (!a.partials) return;
+    float *out = a.partials + (int64_t)blockIdx.x * 2 * a.d;
+#pragma unroll
+    for (int j = 0; j < NV; j++)
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const int c = (lane + j * lanes) * N + i;
+            if (c >= a.d) continue;
+            out[c] = sg[j][i];
+            out[a.d + c] = sb[j][i];
+        }
+}
+
+// wide rows: dx row by row, the row read twice
+template <typename T>
+__global__ void __launch_bounds__(kMaxThreads) norm_bwd_wide_kernel(NormGradArgs<T> a) {
+    pdl_enter();
+    __shared__ float2 red[2][kMaxWarps];
+    const int64_t r = blockIdx.x;
+    const float mean = a.mean[r], rstd = a.rstd[r];
+    const T *dy = a.dy + r * a.lddy, *x = a.x + r * a.ldx;
+    float s1 = 0.f, s2 = 0.f;
+    for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
+        const float g = to_f32(dy[c]) * (a.gain ? to_f32(a.gain[c]) : 1.f);
+        s1 += g;
+        s2 = fmaf(g, (to_f32(x[c]) - mean) * rstd, s2);
+    }
+    const float2 s = row_sum<false>(s1, s2, red, 0);
+    const float m1 = s.x / (float)a.d, m2 = s.y / (float)a.d;
+    for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
+        const float g = to_f32(dy[c]) * (a.gain ? to_f32(a.gain[c]) : 1.f);
+        const float v = (g - m1 - (to_f32(x[c]) - mean) * rstd * m2) * rstd;
+        a.dx[r * a.lddx + c] = from_f32<T>(v + (a.add ? to_f32(a.add[r * a.ldadd + c]) : 0.f));
+    }
+}
+// wide rows: column sums of a split of the rows
+template <typename T>
+__global__ void __launch_bounds__(256) norm_bwd_wide_sums_kernel(NormGradArgs<T> a, int splits) {
+    pdl_enter();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= a.d) return;
+    float sg = 0.f, sb = 0.f;
+    for (int64_t r = blockIdx.y; r < a.rows; r += splits) {
+        const float g = to_f32(a.dy[r * a.lddy + c]);
+        sg = fmaf(g, (to_f32(a.x[r * a.ldx + c]) - a.mean[r]) * a.rstd[r], sg);
+        sb += g;
+    }
+    float *out = a.partials + (int64_t)blockIdx.y * 2 * a.d;
+    out[c] = sg;
+    out[a.d + c] = sb;
+}
+
+// dgain, dbias (+)= the blocks' sums, added in their order: 32 columns and 8 sections of the blocks to a block
+__global__ void __launch_bounds__(256) norm_join_kernel(const float *__restrict__ partials, int blocks, int d, float *dgain,
+                                                        float *dbias, int accumulate, WsHeader *hdr) {
+    pdl_enter();
+    __shared__ float s_part[8][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    if (blockIdx.x == 0 && threadIdx.x == 0) clear_status(hdr);
+    const int64_t c = (int64_t)blockIdx.x * 32 + x;         // of both sums, one behind the other
+    const int per = (blocks + 7) / 8, b0 = y * per, b1 = min(b0 + per, blocks);
+    float s = 0.f;
+    if (c < 2 * (int64_t)d) {
+#pragma unroll 8
+        for (int b = b0; b < b1; b++) s += partials[(int64_t)b * 2 * d + c];
+    }
+    s_part[y][x] = s;
+    __syncthreads();
+    if (y || c >= 2 * (int64_t)d) return;
+    for (int i = 1; i < 8; i++) s += s_part[i][x];
+    float *to = c < d ? (dgain ? dgain + c : nullptr) : (dbias ? dbias + (c - d) : nullptr);
+    if (to) *to = accumulate ? *to + s : s;
+}
+
+template <typename T>
+bool grouped(const void *p, int64_t ld) {
+    return p == nullptr || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % Vec<T>::N == 0);
+}
+constexpr int64_t kWide = 8192;     // columns above which rows are not held in registers
+
+template <typename T, int N, int NV>
+int launch_fwd(const NormArgs<T> &a, cudaStream_t st) {
+    const int groups = (a.d + N - 1) / N;
+    if (groups <= 32 * NV) {
+        SBP_LAUNCH((norm_fwd_kernel<T, N, NV, true>), (unsigned)((a.rows + 7) / 8), 256, 0, st, a);
+    } else {
+        const int threads = ((groups + NV - 1) / NV + 31) / 32 * 32;
+        SBP_LAUNCH((norm_fwd_kernel<T, N, NV, false>), (unsigned)a.rows, threads, 0, st, a);
+    }
+    return STREAMBP_OK;
+}
+template <typename T, int N, int NV>
+int launch_bwd(const NormGradArgs<T> &a, int blocks, cudaStream_t st) {
+    const int groups = (a.d + N - 1) / N;
+    const int threads = ((groups + NV - 1) / NV + 31) / 32 * 32;
+    SBP_LAUNCH((norm_bwd_kernel<T, N, NV>), (unsigned)blocks, threads, 0, st, a);
+    return STREAMBP_OK;
+}
+}  // namespace
+
+// Blocks that walk the rows of a backward pass (a function of the sizes alone, so that the order of the sums is the same
+// everywhere and the workspace query needs no GPU).
+int layernorm_blocks(int64_t rows, int64_t d) {
+    const int64_t most = d > kWide ? std::max<int64_t>(1, 148 * 8 * 256 / d) : 148 * 4;
+    return (int)std::min<int64_t>(rows, most);
+}
+
+template <typename T>
+int layernorm_fwd(const T *x, int64_t ldx, const T *gain, const T *bias, float eps, int64_t rows, int64_t d, T *y, int64_t ldy,
+                  float *mean, float *rstd, cudaStream_t st) {
+    const NormArgs<T> a{x, gain, bias, y, mean, rstd, rows, ldx, ldy, (int)d, eps};
+    constexpr int N = Vec<T>::N;
+    if (d > kWide) {
+        SBP_LAUNCH(norm_fwd_wide_kernel<T>, (unsigned)rows, kMaxThreads, 0, st, a);
+        return STREAMBP_OK;
+    }
+    if (d % N == 0 && grouped<T>(x, ldx) && grouped<T>(y, ldy) && grouped<T>(gain, 0) && grouped<T>(bias, 0)) {
+        const int64_t groups = d / N;
+        if (groups <= 32) return launch_fwd<T, N, 1>(a, st);
+        if (groups <= 1024) return launch_fwd<T, N, 2>(a, st);
+        return launch_fwd<T, N, 4>(a, st);
+    }
+    return d <= 1024 ? launch_fwd<T, 1, 4>(a, st) : launch_fwd<T, 1, 16>(a, st);
+}
+
+template <typename T>
+int layernorm_bwd(const T *dy, int64_t lddy, const T *x, int64_t ldx, const T *gain, const float *mean, const float *rstd,
+                  const T *add, int64_t ldadd, int64_t rows, int64_t d, T *dx, int64_t lddx, float *dgain, float *dbias,
+                  bool accumulate, float *partials, WsHeader *hdr, cudaStream_t st) {
+    const bool sums = dgain || dbias;
+    const NormGradArgs<T> a{dy, x, gain, add, mean, rstd, dx, sums ? partials : nullptr, rows, lddy, ldx, ldadd, lddx, (int)d};
+    const int blocks = layernorm_blocks(rows, d);
+    constexpr int N = Vec<T>::N;
+    if (d > kWide) {
+        // (the sums first: dx may lie where dy or x does)
+        if (sums)
+            SBP_LAUNCH(norm_bwd_wide_sums_kernel<T>, dim3((unsigned)((d + 255) / 256), (unsigned)blocks), 256, 0, st, a, blocks);
+        if (dx) SBP_LAUNCH(norm_bwd_wide_kernel<T>, (unsigned)rows, kMaxThreads, 0, st, a);
+    } else if (d % N == 0 && grouped<T>(x, ldx) && grouped<T>(dy, lddy) && grouped<T>(add, ldadd) && grouped<T>(dx, lddx) &&
+               grouped<T>(gain, 0)) {
+        const int64_t groups = d / N;
+        if (groups <= 128) SBP_TRY((launch_bwd<T, N, 1>(a, blocks, st)));
+        else if (groups <= 1024) SBP_TRY((launch_bwd<T, N, 2>(a, blocks, st)));
+        else SBP_TRY((launch_bwd<T, N, 4>(a, blocks, st)));
+    } else {
+        if (d <= 1024) SBP_TRY((launch_bwd<T, 1, 4>(a, blocks, st)));
+        else SBP_TRY((launch_bwd<T, 1, 16>(a, blocks, st)));
+    }
+    if (sums)
+        SBP_LAUNCH(norm_join_kernel, (unsigned)((2 * d + 31) / 32), 256, 0, st, partials, blocks, (int)d, dgain, dbias,
+                   accumulate ? 1 : 0, hdr);
+    return STREAMBP_OK;
+}
+
+template int layernorm_fwd<float>(const float *, int64_t, const float *, const float *, float, int64_t, int64_t, float *, int64_t,
+                                  float *, float *, cudaStream_t);
+template int layernorm_fwd<bf16>(const bf16 *, int64_t, const bf16 *, const bf16 *, float, int64_t, int64_t, bf16 *, int64_t,
+                                 float *, float *, cudaStream_t);
+template int layernorm_bwd<float>(const float *, int64_t, const float *, int64_t, const float *, const float *, const float *,
+                                  const float *, int64_t, int64_t, int64_t, float *, int64_t, float *, float *, bool, float *,
+                                  WsHeader *, cudaStream_t);
+template int layernorm_bwd<bf16>(const bf16 *, int64_t, const bf16 *, int64_t, const bf16 *, const float *, const float *,
+                                 const bf16 *, int64_t, int64_t, int64_t, bf16 *, int64_t, float *, float *, bool, float *,
+                                 WsHeader *, cudaStream_t);
+
+}  // namespace sbp

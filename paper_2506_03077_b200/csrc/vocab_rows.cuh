@@ -1,0 +1,123 @@
+// Rows of logits that start anywhere: a row as 16-byte groups of memory, and the values' order.
+#pragma once
+
+#include "sm100.cuh"
+
+namespace sbp {
+
+// Row of n elements at p, seen as aligned 16-byte groups: group v holds the elements v N - off .. v N - off + N - 1, of
+// which the first and the last group may hold some only.  Those are read element by element: nothing outside the row is read.
+template <typename T>
+struct RowGroups {
+    static constexpr int N = Vec<T>::N;
+    const T *base;       // p, aligned down (never read in front of p)
+    int off, n, groups;
+    __device__ __forceinline__ RowGroups(const T *p, int n_) {
+        off = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+        base = p - off;
+        n = n_;
+        groups = (int)(((int64_t)off + n + N - 1) / N);
+    }
+    __device__ __forceinline__ int first(int v) const { return v * N - off; }                      // element index of the group
+    __device__ __forceinline__ bool whole(int v) const { return first(v) >= 0 && first(v) <= n - N; }
+    // values of group v, `fill` where the row has none
+    __device__ __forceinline__ void load(int v, float (&x)[N], float fill) const {
+        if (whole(v)) {
+            Vec<T> a;
+            a.load(base + (int64_t)v * N);
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = a.v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const int e = first(v) + i;
+                x[i] = e >= 0 && e < n ? to_f32(base[(int64_t)v * N + i]) : fill;
+            }
+        }
+    }
+};
+
+// One block's look through `count` ids, several loads in flight: the first i for which bad(ids[i], i) goes into the header as
+// E_BAD_LABEL with detail i / per, or OK.  (One block does it, so that a call needs no launch to clear its status.)
+template <typename F>
+__device__ __forceinline__ void report_first(const int64_t *__restrict__ ids, int64_t count, int64_t per, WsHeader *hdr, F bad) {
+    __shared__ unsigned long long s_first;
+    constexpr unsigned long long kNone = ~0ull;
+    if (threadIdx.x == 0) s_first = kNone;
+    __syncthreads();
+    unsigned long long first = kNone;
+    for (int64_t i0 = threadIdx.x; i0 < count; i0 += 8 * (int64_t)blockDim.x) {
+        int64_t id[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) {
+            const int64_t i = i0 + u * (int64_t)blockDim.x;
+            id[u] = ids[i < count ? i : i0];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; u++) {
+            const int64_t i = i0 + u * (int64_t)blockDim.x;
+            if (i < count && bad(id[u], i) && (unsigned long long)i < first) first = (unsigned long long)i;
+        }
+    }
+    if (first != kNone) atomicMin(&s_first, first);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        hdr->status = s_first == kNone ? STREAMBP_OK : STREAMBP_E_BAD_LABEL;
+        hdr->detail = s_first == kNone ? 0 : (int)(s_first / (unsigned long long)per);
+    }
+    __syncthreads();
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// A temperature's reciprocal in two floats: x / tau as x hi + x lo loses no more than the rounding of the result.
+struct Heat {
+    float hi, lo;
+};
+inline Heat make_heat(float temperature) {
+    const double r = 1.0 / (double)temperature;
+    Heat h;
+    h.hi = (float)r;
+    h.lo = (float)(r - (double)h.hi);
+    return h;
+}
+
+// The order of a list of alternatives as one number: larger values first, of equal ones (the two zeros are equal) the lower
+// index first.  No two elements of a row share a number; 0 stands for none.  The value must not be NaN.
+__device__ __forceinline__ unsigned long long order_of(float value, int index) {
+    const uint32_t u = __float_as_uint(value + 0.f);
+    const uint32_t key = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return (unsigned long long)key << 32 | (uint32_t)~index;
+}
+__device__ __forceinline__ float value_of(unsigned long long o) {
+    const uint32_t key = (uint32_t)(o >> 32);
+    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+__device__ __forceinline__ int index_of(unsigned long long o) { return (int)~(uint32_t)o; }
+
+// Softmax statistics of a set of logits: their maximum m, S = sum of exp((z - m) / tau), and W = sum of the same times
+// (z - m).  All terms of S are positive and all of W negative, so neither loses digits; an empty set has m = -inf, S = W = 0.
+// A NaN or +inf among the logits makes S NaN.
+struct RowStats {
+    float m, S, W;
+};
+// Distances below a maximum count as at most this far (their exponential is 0 at every temperature that is allowed), so that
+// logits of -inf or of the type's lowest value add 0 to W and not 0 times an infinity.
+constexpr float kDeep = -1e30f;
+__device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ RowStats join(const RowStats &a, const RowStats &b, float c) {
+    RowStats r;
+    r.m = fmaxf(a.m, b.m);
+    const float m = finite_or_zero(r.m), da = a.m - m, db = b.m - m;
+    const float fa = exp2_approx(da * c), fb = exp2_approx(db * c);
+    r.S = a.S * fa + b.S * fb;
+    r.W = fa * fmaf(fmaxf(da, kDeep), a.S, a.W) + fb * fmaf(fmaxf(db, kDeep), b.S, b.W);
+    return r;
+}
+
+}  // namespace sbp
