@@ -9,89 +9,168 @@
 namespace sbp {
 
 namespace {
-constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxTop = STREAMBP_TOP_MAX, kCandidates = 1024, kMaxCluster = 8;
+constexpr int kMaxTop = STREAMBP_TOP_MAX, kCandidates = 1056, kMaxCluster = 8;
 
 __device__ __forceinline__ void st_remote_f32(uint32_t a, float v) { st_remote_u32(a, __float_as_uint(v)); }
+__device__ __forceinline__ float value_of_key(uint32_t key) { return value_of((unsigned long long)key << 32); }
+__device__ __forceinline__ uint32_t key_of(float v) { return (uint32_t)(order_of(v, 0) >> 32); }
 
 // The list of a row's segment: its k largest elements in order.
 //
-// A thread's elements are a stripe of the segment, and each thread knows the first of its largest (`best`, 0: none).  The
-// k-th largest of these is not above the k-th largest element, and at most k stripes reach it: only those are read again,
-// and what reaches it there (mostly little more than k elements) is ranked by counting.
-template <typename T>
+// A thread's elements (every THREADS-th whole group) are cut into kParts parts (fewer where it has few), and the pass over the
+// row leaves each part's largest value in `part`.  Of m >= k disjoint sets of elements, the k-th largest of the sets' largest
+// values is not above the k-th largest element; the sets are 32 groups of threads where k is well below 32 (one warp finds
+// the bound), else the threads.  Only parts that reach the bound hold what is on the list: mostly little more than k parts, each
+// a few groups, are read again, and what reaches the bound there (mostly little more than k elements) is ranked by counting.
+template <typename T, int THREADS>
 struct TopOfSegment {
+    static constexpr int kParts = THREADS > 256 ? 2 : 8, kOf32 = 24;
     unsigned long long cand[kCandidates];
-    int stripe[kThreads];
-    int n_cand, n_stripes;
+    float part[kParts][THREADS];
+    unsigned short item[kParts * THREADS];       // parts that reach the bound: part * THREADS + thread
+    uint32_t set[32], s_bound;
+    int n_cand, n_items, n_warp[THREADS / 32];
 
-    // elements of the stripes in the list that reach `bound`; kept in cand where `keep`
-    __device__ __forceinline__ void scan(const RowGroups<T> &row, int g0, int g1, unsigned long long bound, int n_str, bool keep) {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __device__ __forceinline__ void offer(float x, int e, uint32_t bound, bool keep, int &mine) {
+        if (key_of(x) < bound) return;
+        if (keep) {
+            const int at = atomicAdd(&n_cand, 1);
+            if (at < kCandidates) cand[at] = order_of(x, e);
+        } else {
+            mine++;
+        }
+    }
+    // elements of the listed parts and of the segment's ragged ends with key >= bound, kept in cand where there is room
+    __device__ __forceinline__ void gather(const RowGroups<T> &row, int g0, int g1, int w0, int w1, int per_part, uint32_t bound, bool keep) {
+        constexpr int N = RowGroups<T>::N;
+        const int n = n_items * per_part;
         int mine = 0;
-        for (int s = warp; s < n_str; s += kWarps)
-            for (int v = g0 + stripe[s] + lane * kThreads; v < g1; v += 32 * kThreads) {
-                float x[RowGroups<T>::N];
-                row.load(v, x, 0.f);
+        for (int q = threadIdx.x; q < n; q += THREADS) {
+            const int it = item[q / per_part], v = w0 + it % THREADS + (it / THREADS * per_part + q % per_part) * THREADS;
+            if (v >= w1) continue;
+            float x[N];
+            row.load(v, x, 0.f);
 #pragma unroll
-                for (int i = 0; i < RowGroups<T>::N; i++) {
-                    const int e = row.first(v) + i;
-                    if (e < 0 || e >= row.n) continue;
-                    const unsigned long long o = order_of(x[i], e);
-                    if (o < bound) continue;
-                    if (keep) {
-                        const int at = atomicAdd(&n_cand, 1);
-                        if (at < kCandidates) cand[at] = o;
-                    } else {
-                        mine++;
-                    }
-                }
-            }
+            for (int i = 0; i < N; i++) offer(x[i], row.first(v) + i, bound, keep, mine);
+        }
+        if (threadIdx.x < 2 * N) {
+            // (one group at each end, which may be the same one)
+            const int v = threadIdx.x < N ? g0 : g1 - 1, e = row.first(v) + threadIdx.x % N;
+            if (g0 < g1 && (v < w0 || v >= w1) && !(threadIdx.x >= N && v == g0) && e >= 0 && e < row.n)
+                offer(to_f32(row.base[(int64_t)v * N + threadIdx.x % N]), e, bound, keep, mine);
+        }
         if (!keep && mine) atomicAdd(&n_cand, mine);
     }
+    __device__ __forceinline__ void restart() {
+        __syncthreads();
+        if (threadIdx.x == 0) n_cand = 0;
+        __syncthreads();
+    }
 
-    __device__ __forceinline__ void list(const RowGroups<T> &row, int g0, int g1, unsigned long long best, int k,
+    // best: the largest value of this thread's elements, if it has any
+    __device__ __forceinline__ void list(const RowGroups<T> &row, int g0, int g1, int w0, int w1, int per_part, bool has, float best, int k,
                                          unsigned long long *out) {
-        unsigned long long bound = 0;
-        if (__syncthreads_count(best != 0) > k)
-            for (int bit = 63; bit >= 0; bit--) {
-                const unsigned long long trial = bound | 1ull << bit;
-                const int reach = __syncthreads_count(best >= trial);
+        constexpr int N = RowGroups<T>::N;
+        const int tid = threadIdx.x, lane = tid & 31;
+        uint32_t bound = 0;
+        const uint32_t key = has ? key_of(best) : 0;
+        if (tid == 0) n_cand = n_items = 0;
+        for (int i = tid; i < k; i += THREADS) out[i] = 0;
+        if (k <= kOf32 && w1 - w0 >= THREADS) {
+            uint32_t top = key;
+#pragma unroll
+            for (int o = THREADS / 64; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            if (tid % (THREADS / 32) == 0) set[tid / (THREADS / 32)] = top;
+            __syncthreads();
+            if (tid < 32) {
+                const uint32_t mine = set[lane];
+                int above = 0;
+#pragma unroll
+                for (int j = 0; j < 32; j++) {
+                    const uint32_t other = __shfl_sync(0xffffffffu, mine, j);
+                    above += other > mine || (other == mine && j < lane);
+                }
+                if (above == k - 1) s_bound = mine;         // (0 where fewer than k sets have elements)
+            }
+            __syncthreads();
+            bound = s_bound;
+        } else if (__syncthreads_count(has) > k) {
+            for (int bit = 31; bit >= 0; bit--) {
+                const uint32_t trial = bound | 1u << bit;
+                const int reach = __syncthreads_count(key >= trial);
                 if (reach >= k) bound = trial;
                 if (reach == k) break;
             }
-        if (threadIdx.x == 0) n_cand = n_stripes = 0;
-        for (int i = threadIdx.x; i < k; i += kThreads) out[i] = 0;
-        __syncthreads();
-        if (best != 0 && best >= bound) stripe[atomicAdd(&n_stripes, 1)] = threadIdx.x;
-        __syncthreads();
-        const int n_str = n_stripes;
-        scan(row, g0, g1, bound, n_str, true);
-        __syncthreads();
-        if (n_cand > kCandidates) {
-            // rows whose large elements crowd into few stripes: a higher bound, bit by bit, until few enough reach it
-            unsigned long long b = 0;
-            for (int bit = 63; bit >= 0; bit--) {
-                __syncthreads();
-                if (threadIdx.x == 0) n_cand = 0;
-                __syncthreads();
-                scan(row, g0, g1, b | 1ull << bit, n_str, false);
-                __syncthreads();
-                const int reach = n_cand;
-                if (reach >= k) b |= 1ull << bit;
-                if (reach >= k && reach <= kCandidates) break;
-            }
-            __syncthreads();
-            if (threadIdx.x == 0) n_cand = 0;
-            __syncthreads();
-            scan(row, g0, g1, b, n_str, true);
-            __syncthreads();
         }
-        const int n = n_cand;
-        for (int i = threadIdx.x; i < n; i += kThreads) {
+        __syncthreads();
+        if (has && key >= bound)
+            for (int p = 0; p < kParts; p++)
+                if (w0 + tid + p * per_part * THREADS < w1 && key_of(part[p][tid]) >= bound)
+                    item[atomicAdd(&n_items, 1)] = (unsigned short)(p * THREADS + tid);
+        __syncthreads();
+        gather(row, g0, g1, w0, w1, per_part, bound, true);
+        __syncthreads();
+        bool ties = false;
+        if (n_cand > kCandidates) {
+            // many equal values at the bound, or large values crowded into few parts: the k-th largest value itself, bit by
+            // bit where more than the list's length lie above the bound
+            restart();
+            gather(row, g0, g1, w0, w1, per_part, bound + 1, true);
+            __syncthreads();
+            if (n_cand > kCandidates) {
+                uint32_t b = 0;
+                for (int bit = 31; bit >= 0; bit--) {
+                    restart();
+                    gather(row, g0, g1, w0, w1, per_part, b | 1u << bit, false);
+                    __syncthreads();
+                    if (n_cand >= k) b |= 1u << bit;
+                }
+                bound = b;
+                restart();
+                gather(row, g0, g1, w0, w1, per_part, bound + 1, true);
+                __syncthreads();
+            }
+            ties = n_cand < k;
+        }
+        const int n = min(n_cand, kCandidates);
+        for (int i = tid; i < n; i += THREADS) {
             const unsigned long long o = cand[i];
             int rank = 0;
+#pragma unroll 4
             for (int j = 0; j < n; j++) rank += cand[j] > o;
             if (rank < k) out[rank] = o;
+        }
+        if (ties) {
+            // behind them the first elements of the bound's value, looked for in the row's order
+            int have = n;
+            for (int v0 = g0; v0 < g1 && have < k; v0 += THREADS) {
+                const int v = v0 + tid;
+                float x[N];
+                uint32_t equal = 0;
+                if (v < g1) {
+                    row.load(v, x, 0.f);
+#pragma unroll
+                    for (int i = 0; i < N; i++) {
+                        const int e = row.first(v) + i;
+                        if (e >= 0 && e < row.n && key_of(x[i]) == bound) equal |= 1u << i;
+                    }
+                }
+                int before = __popc(equal);
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int t = __shfl_up_sync(0xffffffffu, before, o);
+                    if (lane >= o) before += t;
+                }
+                if (lane == 31) n_warp[tid >> 5] = before;
+                __syncthreads();
+                int at = have + before - __popc(equal);
+                for (int w = 0; w < THREADS / 32; w++) {
+                    if (w < (tid >> 5)) at += n_warp[w];
+                    have += n_warp[w];
+                }
+                for (; equal && at < k; equal &= equal - 1, at++) out[at] = order_of(value_of_key(bound), row.first(v) + __ffs(equal) - 1);
+                __syncthreads();
+            }
         }
         __syncthreads();
     }
@@ -108,21 +187,86 @@ struct ScoreArgs {
     const int *gate;
 };
 
-// One pass over the row with the running maximum and sums in every thread, `cluster` blocks to a row where there are few
-// rows.  Bound by HBM: a row of logits is read once; what the list reads again (k stripes) is a few kilobytes in L2.
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const T *__restrict__ logits, ScoreArgs a, int cluster) {
-    pdl_enter();
-    constexpr int N = RowGroups<T>::N, U = 16 / N;
-    if (gated_off(a.gate)) return;
-    __shared__ RowStats s_warp[kWarps], s_cta[kMaxCluster];
-    __shared__ TopOfSegment<T> top;
+// Adds the values of x (all at or below st.m) to the statistics.
+template <typename T, bool ENT, int U>
+__device__ __forceinline__ void add_batch(const Raw<T> (&x)[U], float c, Pair &S, Pair &W, float m) {
+    constexpr int H = RowGroups<T>::N / 2;
+    const Pair minus(-m, -m), cc(c, c);
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        Pair p[H];
+        x[u].pairs(p);
+#pragma unroll
+        for (int i = 0; i < H; i++) {
+            const Pair d = p[i] + minus, t = d * cc;
+            float a, b;
+            t.get(a, b);
+            const Pair e(exp2_approx(a), exp2_approx(b));
+            S = S + e;
+            if (ENT) W = fma2(e, d, W);
+        }
+    }
+}
+// The same where some are so far below it that e * d is not the 0 it has to be.
+template <typename T, int U>
+__device__ __forceinline__ void add_deep_batch(const Raw<T> (&x)[U], float c, Pair &S, Pair &W, float m) {
+    constexpr int H = RowGroups<T>::N / 2;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        Pair p[H];
+        x[u].pairs(p);
+#pragma unroll
+        for (int i = 0; i < H; i++) {
+            float a, b;
+            p[i].get(a, b);
+            a -= m;
+            b -= m;
+            const Pair e(exp2_approx(a * c), exp2_approx(b * c));
+            S = S + e;
+            W = fma2(e, Pair(fmaxf(a, kDeep), fmaxf(b, kDeep)), W);
+        }
+    }
+}
+
+// A thread's running maximum and sums.
+template <typename T, bool ENT, int U>
+struct Running {
+    float m = -INFINITY, largest = -INFINITY;        // of all, and of the part
+    Pair S = Pair(0.f, 0.f), W = Pair(0.f, 0.f);
+    __device__ __forceinline__ void add(const Raw<T> (&x)[U], float c) {
+        float mx = x[0].largest(), mn = x[0].smallest();
+#pragma unroll
+        for (int u = 1; u < U; u++) {
+            mx = fmaxf(mx, x[u].largest());
+            if (ENT) mn = fminf(mn, x[u].smallest());
+        }
+        largest = fmaxf(largest, mx);
+        if (mx > m) {
+            if (m > -INFINITY) {
+                const float dm = fmaxf(m - mx, kDeep), f = exp2_approx(dm * c);
+                const Pair ff(f, f);
+                if (ENT) W = ff * fma2(Pair(dm, dm), S, W);
+                S = S * ff;
+            }
+            m = mx;
+        }
+        const float at = finite_or_zero(m);
+        if (ENT && !(mn - at > kDeep)) add_deep_batch<T, U>(x, c, S, W, at);
+        else add_batch<T, ENT, U>(x, c, S, W, at);
+    }
+};
+
+// One pass over the row with the running maximum and sums in every thread.  Bound by HBM: a row of logits is read once; what
+// the list reads again is a few kilobytes.  Blocks of 256 threads, one to a row, where there are rows to fill the GPU; else
+// blocks of 1024 and up to eight to a row, so that a thread has all of its loads in flight at once.
+template <typename T, bool TOP, bool ENT, int THREADS>
+__device__ __forceinline__ void score_row(const T *__restrict__ logits, const ScoreArgs &a, int cluster) {
+    constexpr int U = 4, kWarps = THREADS / 32, kParts = TopOfSegment<T, THREADS>::kParts;
+    __shared__ RowStats s_warp[kWarps], s_row, s_cta[kMaxCluster];
+    __shared__ TopOfSegment<T, TOP ? THREADS : 32> top;
     __shared__ unsigned long long s_list[TOP ? kMaxTop : 1], s_lists[TOP ? kMaxCluster * kMaxTop : 1];
     const int64_t r = blockIdx.x / cluster;
-    const int rank = (int)(blockIdx.x % cluster), tid = threadIdx.x;
-    if (blockIdx.x == 0 && a.hdr)
-        report_first(a.tokens, a.tokens ? a.rows : 0, 1, a.hdr,
-                     [&](int64_t y, int64_t) { return y != a.ignore && (y < 0 || y >= a.vocab); });
+    const int rank = (int)(blockIdx.x % cluster), tid = threadIdx.x, lane = tid & 31;
     const int64_t y = a.tokens ? a.tokens[r] : 0;
     if (a.tokens && (y == a.ignore || y < 0 || y >= a.vocab)) {
         if (rank == 0) {
@@ -132,7 +276,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const T *__res
                 if (a.entropy) a.entropy[r] = 0.f;
             }
             if (TOP)
-                for (int i = tid; i < a.k; i += kThreads) {
+                for (int i = tid; i < a.k; i += THREADS) {
                     if (a.top_logp) a.top_logp[r * a.k + i] = -INFINITY;
                     if (a.top_ids) a.top_ids[r * a.k + i] = -1;
                 }
@@ -142,108 +286,129 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const T *__res
     if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (waited for before the others' memory is written)
     const RowGroups<T> row(logits + r * a.ld, a.vocab);
     const int per = (row.groups + cluster - 1) / cluster;
-    const int g0 = min(rank * per, row.groups), g1 = min(g0 + per, row.groups);
+    const int g0 = min(rank * per, row.groups), g1 = min(g0 + per, row.groups);         // the segment's groups
+    const int w0 = max(g0, row.whole_begin()), w1 = max(w0, min(g1, row.whole_end()));  // the whole ones among them
+    // groups of a thread in one part: whole batches
+    const int rounds = (w1 - w0 + THREADS - 1) / THREADS, per_part = max(1, ((rounds + kParts - 1) / kParts + U - 1) / U) * U;
     const float c = a.heat.hi * kLog2e;
-    RowStats st{-INFINITY, 0.f, 0.f};
-    int first = g0 + tid < g1 ? max(0, row.first(g0 + tid)) : -1;      // where the largest so far came first
-    for (int v0 = g0 + tid; v0 < g1; v0 += U * kThreads) {
-        float x[U][N];
+    const float zy = rank == 0 && tid == 0 && a.logp ? to_f32(logits[r * a.ld + y]) : 0.f;
+    Running<T, ENT, U> run;
+    for (int p = 0; p < (TOP ? kParts : 1); p++) {
+        run.largest = -INFINITY;
+        const int end = TOP ? min(w1, w0 + (p + 1) * per_part * THREADS) : w1;
+        int v0 = w0 + p * per_part * THREADS + tid;
+        Raw<T> x[U];
+        for (; v0 + (U - 1) * THREADS < end; v0 += U * THREADS) {
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int v = v0 + u * kThreads;
-            if (v < g1) {
-                row.load(v, x[u], -INFINITY);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; i++) x[u][i] = -INFINITY;
-            }
+            for (int u = 0; u < U; u++) row.load_whole(v0 + u * THREADS, x[u]);
+            run.add(x, c);
         }
-        float mx = x[0][0];
+        if (v0 < end) {
 #pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int i = 0; i < N; i++) mx = fmaxf(mx, x[u][i]);
-        if (mx > st.m) {
-            if (st.m > -INFINITY) {
-                const float dm = fmaxf(st.m - mx, kDeep), f = exp2_approx(dm * c);
-                st.W = f * fmaf(dm, st.S, st.W);
-                st.S *= f;
+            for (int u = 0; u < U; u++) {
+                if (v0 + u * THREADS < end) row.load_whole(v0 + u * THREADS, x[u]);
+                else x[u].fill(-INFINITY);
             }
-            st.m = mx;
-            if (TOP) {
-#pragma unroll
-                for (int u = U - 1; u >= 0; u--)
-#pragma unroll
-                    for (int i = N - 1; i >= 0; i--)
-                        if (x[u][i] == mx) first = row.first(v0 + u * kThreads) + i;
-            }
+            run.add(x, c);
         }
-        const float m = finite_or_zero(st.m);
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int i = 0; i < N; i++) {
-                const float d = x[u][i] - m, e = exp2_approx(d * c);
-                st.S += e;
-                st.W = fmaf(e, fmaxf(d, kDeep), st.W);
-            }
+        if (TOP) top.part[p][tid] = run.largest;
     }
-    const unsigned long long best = TOP && first >= 0 ? order_of(st.m, first) : 0;
+    bool has = w0 + tid < w1;
+    if (tid == 0 && g0 < g1 && (w0 != g0 || w1 != g1)) {        // the ragged ends
+        Raw<T> x[U];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        RowStats b;
-        b.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-        b.S = __shfl_xor_sync(0xffffffffu, st.S, o);
-        b.W = __shfl_xor_sync(0xffffffffu, st.W, o);
-        st = join(st, b, c);
+        for (int u = 0; u < U; u++) x[u].fill(-INFINITY);
+        if (w0 != g0) row.load(g0, x[0]);
+        if (w1 != g1 && g1 - 1 >= w0) row.load(g1 - 1, x[1]);
+        run.add(x, c);
+        has = true;
     }
-    if ((tid & 31) == 0) s_warp[tid >> 5] = st;
+    RowStats st;
+    {
+        float lo, hi;
+        run.S.get(lo, hi);
+        st.S = lo + hi;
+        run.W.get(lo, hi);
+        st.W = lo + hi;
+        st.m = run.m;
+    }
+    auto joined = [&](int first) {          // over the lanes of a warp
+#pragma unroll
+        for (int o = first; o > 0; o >>= 1) {
+            RowStats b;
+            b.m = __shfl_xor_sync(0xffffffffu, st.m, o);
+            b.S = __shfl_xor_sync(0xffffffffu, st.S, o);
+            b.W = __shfl_xor_sync(0xffffffffu, st.W, o);
+            st = join(st, b, c);
+        }
+    };
+    joined(16);
+    if (lane == 0) s_warp[tid >> 5] = st;
     __syncthreads();
-    st = s_warp[0];
-    for (int w = 1; w < kWarps; w++) st = join(st, s_warp[w], c);
-    if (cluster > 1) {
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (tid < cluster) {
-            const uint32_t to = map_to_cta(smem_u32(&s_cta[rank]), tid);
-            st_remote_f32(to, st.m);
-            st_remote_f32(to + 4, st.S);
-            st_remote_f32(to + 8, st.W);
+    if (tid < 32) {
+        st = lane < kWarps ? s_warp[lane] : RowStats{-INFINITY, 0.f, 0.f};
+        joined(kWarps / 2);
+        if (lane == 0) s_row = st;
+        if (cluster > 1) {
+            st.m = __shfl_sync(0xffffffffu, st.m, 0);
+            st.S = __shfl_sync(0xffffffffu, st.S, 0);
+            st.W = __shfl_sync(0xffffffffu, st.W, 0);
+            asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+            if (lane < cluster) {
+                const uint32_t to = map_to_cta(smem_u32(&s_cta[rank]), lane);
+                st_remote_f32(to, st.m);
+                st_remote_f32(to + 4, st.S);
+                st_remote_f32(to + 8, st.W);
+            }
+            __syncwarp();
         }
-        cluster_sync_all();
-        st = s_cta[0];
-        for (int w = 1; w < cluster; w++) st = join(st, s_cta[w], c);
+    } else if (cluster > 1) {
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
-    const float m = finite_or_zero(st.m), logS = logf(st.S);
+    if (cluster > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");      // (waited for where the whole row's sums are needed)
+    __syncthreads();
+    if constexpr (TOP)
+        if (s_row.S < INFINITY) top.list(row, g0, g1, w0, w1, per_part, has, run.m, a.k, s_list);     // (else the row is broken, and has no list)
+    if (cluster > 1) {
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        if (tid < 32) {
+            st = lane < cluster ? s_cta[lane] : RowStats{-INFINITY, 0.f, 0.f};
+            joined(kMaxCluster / 2);
+            if (lane == 0) s_row = st;
+        }
+        __syncthreads();
+    }
+    st = s_row;
+    const float top_m = finite_or_zero(st.m), logS = logf(st.S);
     const bool none = st.S == 0.f, broken = !(st.S < INFINITY);
     auto logp_of = [&](float z) {
-        const float d = z - m;
+        const float d = z - top_m;
         return none ? -INFINITY : broken ? NAN : d > -INFINITY ? fmaf(d, a.heat.hi, fmaf(d, a.heat.lo, -logS)) : -INFINITY;
     };
     if (rank == 0 && tid == 0) {
-        if (a.logp) a.logp[r] = logp_of(to_f32(logits[r * a.ld + y]));
-        if (a.lse) a.lse[r] = broken ? NAN : fmaf(m, a.heat.hi, fmaf(m, a.heat.lo, logS));
-        if (a.entropy) a.entropy[r] = none ? 0.f : broken ? NAN : logS - (st.W / st.S) * a.heat.hi;
+        if (a.logp) a.logp[r] = logp_of(zy);
+        if (a.lse) a.lse[r] = broken ? NAN : fmaf(top_m, a.heat.hi, fmaf(top_m, a.heat.lo, logS));
+        if (ENT) a.entropy[r] = none ? 0.f : broken ? NAN : logS - (st.W / st.S) * a.heat.hi;
     }
     if constexpr (TOP) {
         if (broken) {       // (the same in every block of the row)
             if (rank == 0)
-                for (int i = tid; i < a.k; i += kThreads) {
+                for (int i = tid; i < a.k; i += THREADS) {
                     if (a.top_logp) a.top_logp[r * a.k + i] = NAN;
                     if (a.top_ids) a.top_ids[r * a.k + i] = -1;
                 }
             return;
         }
-        top.list(row, g0, g1, best, a.k, s_list);
         if (cluster > 1) {
             const uint32_t to = map_to_cta(smem_u32(s_lists + rank * kMaxTop), 0);
-            for (int i = tid; i < a.k; i += kThreads) {
+            for (int i = tid; i < a.k; i += THREADS) {
                 st_remote_u32(to + 8 * i, (uint32_t)s_list[i]);
                 st_remote_u32(to + 8 * i + 4, (uint32_t)(s_list[i] >> 32));
             }
-            cluster_sync_all();
+            asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
             if (rank != 0) return;
             // an element's place is the number of larger ones: its own list's and, by bisection, the others'
-            for (int i = tid; i < cluster * a.k; i += kThreads) {
+            for (int i = tid; i < cluster * a.k; i += THREADS) {
                 const int l = i / a.k;
                 const unsigned long long o = s_lists[l * kMaxTop + i % a.k];
                 int place = i % a.k;
@@ -261,14 +426,26 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const T *__res
             }
             __syncthreads();
         }
-        for (int i = tid; i < a.k; i += kThreads) {
+        for (int i = tid; i < a.k; i += THREADS) {
             if (a.top_logp) a.top_logp[r * a.k + i] = logp_of(value_of(s_list[i]));
             if (a.top_ids) a.top_ids[r * a.k + i] = index_of(s_list[i]);
         }
     }
 }
 
-// dz = (dlogp (1[y] - p) + dlse p - dH p (log p + H)) / tau; each thread a few groups of one row, a row cut over blocks.
+template <typename T, bool TOP, bool ENT, int THREADS>
+__global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T *__restrict__ logits, ScoreArgs a, int cluster) {
+    pdl_enter();
+    if (gated_off(a.gate)) return;
+    score_row<T, TOP, ENT, THREADS>(logits, a, cluster);
+    // (the last block of the first row: where a row has several, another one writes the results)
+    if ((int)blockIdx.x == cluster - 1 && a.hdr)
+        report_first(a.tokens, a.tokens ? a.rows : 0, 1, a.hdr,
+                     [&](int64_t y, int64_t) { return y != a.ignore && (y < 0 || y >= a.vocab); });
+}
+
+// dz = (dlogp (1[y] - p) + dlse p - dH p (log p + H)) / tau.  Reads and writes the row once; about ten operations an
+// element, so that two bytes in and two out still leave HBM the bound.
 struct ScoreGradArgs {
     const int64_t *tokens;      // optional
     int64_t ignore, ld, ldd;
@@ -276,55 +453,82 @@ struct ScoreGradArgs {
     Heat heat;
     const float *lse, *entropy, *d_logp, *d_lse, *d_entropy;    // entropy with d_entropy; the three gradients are optional
 };
-constexpr int kGradGroups = 4;
-template <typename T>
-__global__ void __launch_bounds__(kThreads) token_logprobs_bwd_kernel(const T *logits, T *d_logits, ScoreGradArgs a) {
+constexpr int kGradThreads = 256, kGradGroups = 4, kGradRounds = 4;
+template <typename T, bool LO>
+__global__ void __launch_bounds__(kGradThreads) token_logprobs_bwd_kernel(const T *logits, T *d_logits, ScoreGradArgs a) {
     pdl_enter();
-    constexpr int N = RowGroups<T>::N;
+    constexpr int N = RowGroups<T>::N, H = N / 2;
     const int64_t r = blockIdx.x;
     T *d = d_logits + r * a.ldd;
-    const RowGroups<T> out(d, a.vocab);
+    const RowGroups<T> out(d, a.vocab), in(logits + r * a.ld, a.vocab);
     const int64_t y = a.tokens ? a.tokens[r] : -1;
-    const bool part = !a.tokens || (y != a.ignore && y >= 0 && y < a.vocab);
-    const RowGroups<T> in(logits + r * a.ld, a.vocab);
-    const bool same = in.off == out.off;
-    const float lse = part ? a.lse[r] : 0.f, gp = part && a.d_logp && a.tokens ? a.d_logp[r] : 0.f, gl = part && a.d_lse ? a.d_lse[r] : 0.f;
-    const float gh = part && a.d_entropy ? a.d_entropy[r] : 0.f, H = part && a.d_entropy ? a.entropy[r] : 0.f;
-    const float c0 = gl - gp - gh * H;
-    const bool none = lse == -INFINITY;      // every logit is -inf: p is 0
-    auto grad = [&](float z, int e) {
-        const float lp = fmaf(z, a.heat.hi, fmaf(z, a.heat.lo, -lse));
-        float p = exp2_approx(lp * kLog2e);
-        if (z == -INFINITY) p = 0.f;
-        float g = p * (p > 0.f || p != p ? fmaf(-gh, lp, c0) : 0.f);
-        if (none) g = 0.f;
-        if (e == y) g += gp;
-        return fmaf(g, a.heat.hi, g * a.heat.lo);
+    const bool none = a.lse[r] == -INFINITY;       // every logit is -inf: p is 0
+    const float lse = none ? 0.f : a.lse[r];
+    const float gp = a.d_logp ? a.d_logp[r] : 0.f, gl = a.d_lse ? a.d_lse[r] : 0.f, gh = a.d_entropy ? a.d_entropy[r] : 0.f;
+    const float ent = a.d_entropy ? a.entropy[r] : 0.f, tau = a.heat.hi;
+    const bool part = !a.tokens || (y != a.ignore && y >= 0 && y < a.vocab), same = in.off == out.off;
+    const float c0 = (gl - gp - gh * ent) * tau, c1 = -gh * tau;
+    // logits below this (-inf among them) count as this: their p is 0, and so is its product with log p
+    const float least = (lse - 1e4f) / tau;
+    const int per_block = kGradRounds * kGradGroups * kGradThreads;
+    const int g0 = blockIdx.y * per_block, g1 = min(out.groups, g0 + per_block);
+    const float inv_hi = a.heat.hi, inv_lo = a.heat.lo;
+    auto grad = [&](Pair z) {
+        float l[2], q[2];
+        z.get(l[0], l[1]);
+        z = Pair(max_nan(l[0], least), max_nan(l[1], least));
+        Pair lp = fma2(z, Pair(inv_hi, inv_hi), Pair(-lse, -lse));
+        if (LO) lp = fma2(z, Pair(inv_lo, inv_lo), lp);
+        (lp * Pair(kLog2e, kLog2e)).get(q[0], q[1]);
+        return Pair(exp2_approx(q[0]), exp2_approx(q[1])) * fma2(lp, Pair(c1, c1), Pair(c0, c0));
     };
-    const int v0 = (blockIdx.y * kGradGroups) * kThreads + threadIdx.x;
-    float x[kGradGroups][N];
+    if (part && same) {
+        const int w0 = max(g0, out.whole_begin()), w1 = min(g1, out.whole_end());
+        const int at = part && a.d_logp ? (int)((y + out.off) / N) : -1, in_at = (int)((y + out.off) % N);     // the token's group
+        auto one = [&](int v, const Raw<T> &x) {
+            Pair p[H];
+            x.pairs(p);
+            Vec<T> o;
 #pragma unroll
-    for (int u = 0; u < kGradGroups; u++) {
-        const int v = v0 + u * kThreads;
-        if (!part || v >= out.groups) continue;
-        if (same) {
-            in.load(v, x[u], 0.f);
-        } else {
+            for (int i = 0; i < H; i++) grad(p[i]).get(o.v[2 * i], o.v[2 * i + 1]);
+            if (v == at) {
 #pragma unroll
-            for (int i = 0; i < N; i++) {
-                const int e = out.first(v) + i;
-                x[u][i] = e >= 0 && e < a.vocab ? to_f32(logits[r * a.ld + e]) : 0.f;
+                for (int i = 0; i < N; i++)
+                    if (i == in_at) o.v[i] = fmaf(gp, tau, o.v[i]);
             }
-        }
-    }
+            o.store(d + out.first(v));
+        };
+        Raw<T> x[kGradGroups];
+        int v0 = w0 + threadIdx.x;
+        for (; v0 + (kGradGroups - 1) * kGradThreads < w1; v0 += kGradGroups * kGradThreads) {
 #pragma unroll
-    for (int u = 0; u < kGradGroups; u++) {
-        const int v = v0 + u * kThreads;
-        if (v >= out.groups) continue;
+            for (int u = 0; u < kGradGroups; u++) in.load_whole(v0 + u * kGradThreads, x[u]);
+#pragma unroll
+            for (int u = 0; u < kGradGroups; u++) one(v0 + u * kGradThreads, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kGradGroups; u++)
+            if (v0 + u * kGradThreads < w1) in.load_whole(v0 + u * kGradThreads, x[u]);
+#pragma unroll
+        for (int u = 0; u < kGradGroups; u++)
+            if (v0 + u * kGradThreads < w1) one(v0 + u * kGradThreads, x[u]);
+    }
+    // element by element: the ragged ends, rows that start elsewhere than their gradient, zeros
+    auto slow = [&](int v) {
         const int e0 = out.first(v);
         Vec<T> o;
 #pragma unroll
-        for (int i = 0; i < N; i++) o.v[i] = part ? grad(x[u][i], e0 + i) : 0.f;
+        for (int i = 0; i < H; i++) {
+            const int e = e0 + 2 * i;
+            Pair g(0.f, 0.f);
+            if (part)
+                g = grad(Pair(e >= 0 && e < a.vocab ? to_f32(logits[r * a.ld + e]) : least,
+                              e + 1 >= 0 && e + 1 < a.vocab ? to_f32(logits[r * a.ld + e + 1]) : least));
+            g.get(o.v[2 * i], o.v[2 * i + 1]);
+#pragma unroll
+            for (int j = 0; j < 2; j++)
+                if (part && e + j == y) o.v[2 * i + j] = fmaf(gp, tau, o.v[2 * i + j]);
+        }
         if (out.whole(v)) {
             o.store(d + e0);
         } else {
@@ -332,15 +536,30 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_bwd_kernel(const T *l
             for (int i = 0; i < N; i++)
                 if (e0 + i >= 0 && e0 + i < a.vocab) d[e0 + i] = from_f32<T>(o.v[i]);
         }
+    };
+    if (!part || !same) {
+        for (int v = g0 + threadIdx.x; v < g1; v += kGradThreads) slow(v);
+    } else if (threadIdx.x < 2 && g0 < g1) {
+        const int v = threadIdx.x ? g1 - 1 : g0;
+        if (!out.whole(v) && !(threadIdx.x && v == g0)) slow(v);
     }
 }
 
-// Blocks to a row: enough for two blocks an SM where rows are few, none with less than two groups a thread.
+// Where rows fill the GPU several times, blocks of 256 threads take one each; fewer rows are cut over as many blocks of 1024
+// as fit at once (one an SM), none with less than a batch of loads a thread.
+constexpr int64_t kFewRows = 148;
 template <typename T>
 int row_cluster(int64_t rows, int64_t vocab) {
     int c = 1;
-    while (c < kMaxCluster && rows * c < 2 * 148 && vocab / (2 * c) >= 2 * kThreads * Vec<T>::N) c *= 2;
+    while (c < kMaxCluster && rows * 2 * c <= 148 && vocab / (2 * c) >= 1024 * Vec<T>::N) c *= 2;
     return c;
+}
+template <typename T, bool TOP, bool ENT>
+int launch_score(const T *logits, const ScoreArgs &a, cudaStream_t st) {
+    if (a.rows > kFewRows || a.vocab <= 256 * 4 * Vec<T>::N)
+        return launch_clusters(token_logprobs_kernel<T, TOP, ENT, 256>, dim3((unsigned)a.rows), 256, 0, 1, 1, st, logits, a, 1);
+    const int c = row_cluster<T>(a.rows, a.vocab);
+    return launch_clusters(token_logprobs_kernel<T, TOP, ENT, 1024>, dim3((unsigned)(a.rows * c)), 1024, 0, c, 1, st, logits, a, c);
 }
 }  // namespace
 
@@ -350,17 +569,17 @@ int token_logprobs(const T *logits, int64_t ld, int64_t rows, int64_t vocab, con
                    WsHeader *hdr, cudaStream_t st) {
     const ScoreArgs a{tokens, ignore, rows, ld, (int)vocab, k, make_heat(temperature), logp, lse, entropy, top_logp, top_ids, hdr,
                       call_state().gate};
-    const int c = row_cluster<T>(rows, vocab);
-    auto kernel = k ? token_logprobs_kernel<T, true> : token_logprobs_kernel<T, false>;
-    return launch_clusters(kernel, dim3((unsigned)(rows * c)), kThreads, 0, c, 1, st, logits, a, c);
+    if (k) return entropy ? launch_score<T, true, true>(logits, a, st) : launch_score<T, true, false>(logits, a, st);
+    return entropy ? launch_score<T, false, true>(logits, a, st) : launch_score<T, false, false>(logits, a, st);
 }
 template <typename T>
 int token_logprobs_bwd(const T *logits, int64_t ld, int64_t rows, int64_t vocab, const int64_t *tokens, int64_t ignore,
                        float temperature, const float *lse, const float *entropy, const float *d_logp, const float *d_lse,
                        const float *d_entropy, T *d_logits, int64_t ldd, cudaStream_t st) {
     const ScoreGradArgs a{tokens, ignore, ld, ldd, (int)vocab, make_heat(temperature), lse, entropy, d_logp, d_lse, d_entropy};
-    const int64_t groups = (vocab + Vec<T>::N - 1) / Vec<T>::N + 1, per = kThreads * kGradGroups;
-    SBP_LAUNCH(token_logprobs_bwd_kernel<T>, dim3((unsigned)rows, (unsigned)((groups + per - 1) / per)), kThreads, 0, st, logits,
+    const int64_t groups = (vocab + Vec<T>::N - 1) / Vec<T>::N + 1, per = kGradThreads * kGradGroups * kGradRounds;
+    auto kernel = a.heat.lo != 0.f ? token_logprobs_bwd_kernel<T, true> : token_logprobs_bwd_kernel<T, false>;
+    SBP_LAUNCH(kernel, dim3((unsigned)rows, (unsigned)((groups + per - 1) / per)), kGradThreads, 0, st, logits,
                d_logits, a);
     return STREAMBP_OK;
 }

@@ -5,38 +5,6 @@
 
 namespace sbp {
 
-// Row of n elements at p, seen as aligned 16-byte groups: group v holds the elements v N - off .. v N - off + N - 1, of
-// which the first and the last group may hold some only.  Those are read element by element: nothing outside the row is read.
-template <typename T>
-struct RowGroups {
-    static constexpr int N = Vec<T>::N;
-    const T *base;       // p, aligned down (never read in front of p)
-    int off, n, groups;
-    __device__ __forceinline__ RowGroups(const T *p, int n_) {
-        off = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
-        base = p - off;
-        n = n_;
-        groups = (int)(((int64_t)off + n + N - 1) / N);
-    }
-    __device__ __forceinline__ int first(int v) const { return v * N - off; }                      // element index of the group
-    __device__ __forceinline__ bool whole(int v) const { return first(v) >= 0 && first(v) <= n - N; }
-    // values of group v, `fill` where the row has none
-    __device__ __forceinline__ void load(int v, float (&x)[N], float fill) const {
-        if (whole(v)) {
-            Vec<T> a;
-            a.load(base + (int64_t)v * N);
-#pragma unroll
-            for (int i = 0; i < N; i++) x[i] = a.v[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; i++) {
-                const int e = first(v) + i;
-                x[i] = e >= 0 && e < n ? to_f32(base[(int64_t)v * N + i]) : fill;
-            }
-        }
-    }
-};
-
 // One block's look through `count` ids, several loads in flight: the first i for which bad(ids[i], i) goes into the header as
 // E_BAD_LABEL with detail i / per, or OK.  (One block does it, so that a call needs no launch to clear its status.)
 template <typename F>
@@ -74,6 +42,124 @@ __device__ __forceinline__ float exp2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+// the larger of two; NaN where one is
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// Two fp32 operations in one instruction.
+struct Pair {
+    unsigned long long v;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
+// 16 bytes of a row as they came, their largest and smallest value (NaN left out), and their values as pairs.
+template <typename T> struct Raw;
+template <> struct Raw<float> {
+    uint4 w;
+    __device__ __forceinline__ float largest() const {
+        return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+    }
+    __device__ __forceinline__ float smallest() const {
+        return fminf(fminf(__uint_as_float(w.x), __uint_as_float(w.y)), fminf(__uint_as_float(w.z), __uint_as_float(w.w)));
+    }
+    __device__ __forceinline__ void fill(float v) { w = make_uint4(__float_as_uint(v), __float_as_uint(v), __float_as_uint(v), __float_as_uint(v)); }
+    __device__ __forceinline__ void pairs(Pair (&p)[2]) const {
+        p[0] = Pair(__uint_as_float(w.x), __uint_as_float(w.y));
+        p[1] = Pair(__uint_as_float(w.z), __uint_as_float(w.w));
+    }
+};
+template <> struct Raw<bf16> {
+    uint4 w;
+    static __device__ __forceinline__ __nv_bfloat162 two(uint32_t u) { return *reinterpret_cast<__nv_bfloat162 *>(&u); }
+    __device__ __forceinline__ float largest() const {
+        const __nv_bfloat162 a = __hmax2(__hmax2(two(w.x), two(w.y)), __hmax2(two(w.z), two(w.w)));
+        return fmaxf(__low2float(a), __high2float(a));
+    }
+    __device__ __forceinline__ float smallest() const {
+        const __nv_bfloat162 a = __hmin2(__hmin2(two(w.x), two(w.y)), __hmin2(two(w.z), two(w.w)));
+        return fminf(__low2float(a), __high2float(a));
+    }
+    __device__ __forceinline__ void fill(float v) {
+        const uint32_t h = __float_as_uint(v) >> 16, u = h << 16 | h;        // (v is a bf16 value)
+        w = make_uint4(u, u, u, u);
+    }
+    __device__ __forceinline__ void pairs(Pair (&p)[4]) const {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) p[i] = Pair(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u));
+    }
+};
+
+// Row of n elements at p, seen as aligned 16-byte groups: group v holds the elements v N - off .. v N - off + N - 1, of
+// which the first and the last group may hold some only.  Those are read element by element: nothing outside the row is read.
+template <typename T>
+struct RowGroups {
+    static constexpr int N = Vec<T>::N;
+    const T *base;       // p, aligned down (never read in front of p)
+    int off, n, groups;
+    __device__ __forceinline__ RowGroups(const T *p, int n_) {
+        off = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+        base = p - off;
+        n = n_;
+        groups = (int)(((int64_t)off + n + N - 1) / N);
+    }
+    __device__ __forceinline__ int first(int v) const { return v * N - off; }                      // element index of the group
+    __device__ __forceinline__ bool whole(int v) const { return first(v) >= 0 && first(v) <= n - N; }
+    // the groups that the row fills: whole_begin .. whole_end - 1 (none where the second is not larger)
+    __device__ __forceinline__ int whole_begin() const { return off ? 1 : 0; }
+    __device__ __forceinline__ int whole_end() const { return (int)(((int64_t)off + n) / N); }
+    __device__ __forceinline__ void load_whole(int v, Raw<T> &x) const { x.w = *reinterpret_cast<const uint4 *>(base + (int64_t)v * N); }
+    // group v as it is, -inf where the row has no element
+    __device__ __forceinline__ void load(int v, Raw<T> &x) const {
+        if (whole(v)) {
+            x.w = *reinterpret_cast<const uint4 *>(base + (int64_t)v * N);
+        } else {
+            T t[N];
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const int e = first(v) + i;
+                t[i] = e >= 0 && e < n ? base[(int64_t)v * N + i] : from_f32<T>(-INFINITY);
+            }
+            memcpy(&x.w, t, 16);
+        }
+    }
+    // values of group v, `fill` where the row has none
+    __device__ __forceinline__ void load(int v, float (&x)[N], float fill) const {
+        if (whole(v)) {
+            Vec<T> a;
+            a.load(base + (int64_t)v * N);
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = a.v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const int e = first(v) + i;
+                x[i] = e >= 0 && e < n ? to_f32(base[(int64_t)v * N + i]) : fill;
+            }
+        }
+    }
+};
 
 // A temperature's reciprocal in two floats: x / tau as x hi + x lo loses no more than the rounding of the result.
 struct Heat {
