@@ -409,10 +409,10 @@ size_t norm_scratch(int64_t rows, int64_t d, void *base, NormScratch *out) {
     out->guards = a.guards;
     return a.size();
 }
-// scratch of the embedding's gradient: two copies of the keys and tokens, the counts of the sort, the chunks' partial sums
+// scratch of the embedding's gradient: keys and tokens (twice where the sort takes several launches), its counts, the chunks' partial sums
 struct EmbeddingScratch {
     EmbeddingPlan plan;
-    int *keys[2], *tokens[2], *counts;
+    int *keys[2], *tokens[2], *counts, *owners;
     float *partials;
     std::vector<size_t> guards;
 };
@@ -420,12 +420,17 @@ size_t embedding_scratch(int64_t n, int64_t vocab, int64_t d, void *base, Embedd
     Arena a(base);
     a.take_bytes(kHeaderBytes);
     out->plan = embedding_plan(n, vocab, d);
-    for (int i = 0; i < 2; i++) {
+    for (int i = 0; i < (out->plan.one_launch ? 1 : 2); i++) {
         out->keys[i] = a.take<int>(n);
         out->tokens[i] = a.take<int>(n);
     }
-    out->counts = a.take<int>((size_t)256 * out->plan.tiles);
-    out->partials = a.take<float>((size_t)out->plan.chunks * 2 * (size_t)d);
+    if (out->plan.one_launch) {
+        out->keys[1] = out->keys[0];
+        out->tokens[1] = out->tokens[0];
+    }
+    out->counts = a.take<int>(embedding_counts(out->plan));
+    out->owners = a.take<int>((size_t)out->plan.chunks + 1);
+    out->partials = a.take<float>((size_t)out->plan.chunks * 2 * (size_t)out->plan.partial_width);
     out->guards = a.guards;
     return a.size();
 }
@@ -1305,10 +1310,10 @@ int streambp_embedding_backward(const void *d_out, int64_t ldo, const int64_t *i
     SBP_TRY(ws_guards_arm(workspace, s.guards, st));      // (a kernel of the call writes the status)
     if (dtype == STREAMBP_F32)
         SBP_TRY(embedding_bwd<float>((const float *)d_out, ldo, ids, n, vocab, d, scale, padding_id, d_table, accumulate != 0, s.plan,
-                                     s.keys, s.tokens, s.counts, s.partials, hdr, st));
+                                     s.keys, s.tokens, s.counts, s.owners, s.partials, hdr, st));
     else
         SBP_TRY(embedding_bwd<bf16>((const bf16 *)d_out, ldo, ids, n, vocab, d, scale, padding_id, d_table, accumulate != 0, s.plan, s.keys,
-                                    s.tokens, s.counts, s.partials, hdr, st));
+                                    s.tokens, s.counts, s.owners, s.partials, hdr, st));
     return ws_guards_check(workspace, s.guards, hdr, st);
 }
 

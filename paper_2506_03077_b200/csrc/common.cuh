@@ -556,7 +556,7 @@ int embedding_fwd(const T *table, int64_t ld, const int64_t *ids, int64_t n, int
 template <typename T>
 int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, float scale, int64_t padding,
                   float *d_table, bool accumulate, const EmbeddingPlan &p, int *const (&keys)[2], int *const (&tokens)[2],
-                  int *counts, float *partials, WsHeader *hdr, cudaStream_t st);
+                  int *counts, int *owners, float *partials, WsHeader *hdr, cudaStream_t st);
 
 // Grouped products used by the schedulers: independent problems that become ready together go out as one
 // launch (tensor cores) or one after the other (CUDA cores); a problem may sum several K segments.

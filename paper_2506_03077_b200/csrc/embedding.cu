@@ -13,7 +13,7 @@
 namespace sbp {
 
 namespace {
-constexpr int kThreads = 256, kWarps = kThreads / 32, kBins = 256;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 // ---- lookup: a warp to a token's piece of kPiece bytes ------------------------------------------------------------------
 template <typename T>
@@ -41,19 +41,22 @@ __global__ void __launch_bounds__(kThreads) embedding_lookup_kernel(LookupArgs<T
     T *to = a.out + t * a.ldo;
     const int c0 = (blockIdx.y * kLookupGroups * 32 + (threadIdx.x & 31)) * N;
     if constexpr (GROUPED) {
-        Vec<T> x[kLookupGroups];
+        Raw<T> x[kLookupGroups];                // (as they came until all are on the way)
 #pragma unroll
         for (int u = 0; u < kLookupGroups; u++) {
             const int c = c0 + u * 32 * N;
-            if (c < a.d && !zero) x[u].load(from + c);
+            x[u].w = make_uint4(0, 0, 0, 0);
+            if (c < a.d && !zero) x[u].w = *reinterpret_cast<const uint4 *>(from + c);
         }
 #pragma unroll
         for (int u = 0; u < kLookupGroups; u++) {
             const int c = c0 + u * 32 * N;
             if (c >= a.d) continue;
+            Vec<T> o;
+            o.load(reinterpret_cast<const T *>(&x[u].w));
 #pragma unroll
-            for (int i = 0; i < N; i++) x[u].v[i] = zero ? 0.f : x[u].v[i] * a.scale;
-            x[u].store(to + c);
+            for (int i = 0; i < N; i++) o.v[i] = zero ? 0.f : o.v[i] * a.scale;
+            o.store(to + c);
         }
     } else {
 #pragma unroll
@@ -65,66 +68,213 @@ __global__ void __launch_bounds__(kThreads) embedding_lookup_kernel(LookupArgs<T
 }
 
 // ---- sort ---------------------------------------------------------------------------------------------------------------
-// Tokens that take no part have the key `vocab`, which comes last.
-__device__ __forceinline__ int key_of(int64_t id, int64_t vocab, int64_t padding) {
-    return id == padding || id < 0 || id >= vocab ? (int)vocab : (int)id;
-}
-struct SortPass {
-    const int64_t *ids;         // first pass: keys come from here, tokens are the positions
-    const int *keys, *tokens;
-    int *keys_out, *tokens_out, *counts;        // counts: [kBins][tiles]
-    int64_t vocab, padding;
-    int n, tile, shift;
-    WsHeader *hdr;              // first pass: the status
-};
-__device__ __forceinline__ int sort_key(const SortPass &p, int i) {
-    return p.ids ? key_of(p.ids[i], p.vocab, p.padding) : p.keys[i];
-}
-__global__ void __launch_bounds__(kThreads) sort_count_kernel(SortPass p) {
-    pdl_enter();
-    const int tiles = gridDim.x - (p.hdr ? 1 : 0), tile = blockIdx.x;
-    if (tile == tiles) {
-        report_first(p.ids, p.n, 1, p.hdr, [&](int64_t id, int64_t) { return id != p.padding && (id < 0 || id >= p.vocab); });
-        return;
-    }
-    __shared__ int s_bins[kBins];
-    s_bins[threadIdx.x] = 0;
-    __syncthreads();
-    const int i1 = min(p.n, (tile + 1) * p.tile);
-    for (int i = tile * p.tile + threadIdx.x; i < i1; i += kThreads) atomicAdd(&s_bins[sort_key(p, i) >> p.shift & (kBins - 1)], 1);
-    __syncthreads();
-    p.counts[threadIdx.x * tiles + tile] = s_bins[threadIdx.x];
-}
-__global__ void __launch_bounds__(kThreads) sort_move_kernel(SortPass p) {
-    pdl_enter();
-    const int tiles = gridDim.x, tile = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    __shared__ int s_next[kBins], s_warp[kWarps][kBins], s_sum[kWarps];
-    // where this tile's elements of bin `tid` begin: behind all smaller bins and the bin's part in the tiles before
-    int all = 0, before = 0;
-    for (int t = 0; t < tiles; t++) {
-        const int c = p.counts[tid * tiles + t];
-        all += c;
-        if (t < tile) before += c;
-    }
-    int up = all;
+// Keys are ids; tokens that take no part have the key `vocab`, which comes last.  A pass sorts by one digit of up to 9 bits
+// and keeps the order of equal digits: rank within the warp by matching lanes, warps and blocks behind one another.
+constexpr int kDigit = 9, kBins = 1 << kDigit, kNoneBad = 0x7fffffff;
+
+__device__ __forceinline__ bool no_part(int64_t id, int64_t vocab, int64_t padding) { return id == padding || id < 0 || id >= vocab; }
+
+// exclusive sums over kBins values, one in each of the first kBins threads of a block (s_sum: kBins / 32 ints)
+__device__ __forceinline__ int bins_before(int count, int *s_sum) {
+    const int tid = threadIdx.x, lane = tid & 31;
+    int up = count;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int x = __shfl_up_sync(0xffffffffu, up, o);
         if (lane >= o) up += x;
     }
-    if (lane == 31) s_sum[warp] = up;
+    if (lane == 31 && tid < kBins) s_sum[tid >> 5] = up;
     __syncthreads();
-    int base = up - all + before;
-    for (int w = 0; w < warp; w++) base += s_sum[w];
-    s_next[tid] = base;
-    const int i1 = min(p.n, (tile + 1) * p.tile);
-    for (int i0 = tile * p.tile; i0 < i1; i0 += kThreads) {
+    int base = up - count;
+    if (tid < kBins)
+        for (int w = 0; w < (tid >> 5); w++) base += s_sum[w];
+    return base;
+}
+
+struct SortArgs {
+    const int64_t *ids;
+    int *keys, *tokens;         // sorted
+    int *owners;                // [0] is set to 0 here (embedding_runs_kernel)
+    float *zero;                // optional: the table to clear, `zeros` floats
+    int64_t zeros, vocab, padding;
+    int n, passes;
+    WsHeader *hdr;
+};
+// Up to 64 K tokens: one cluster of up to eight blocks sorts in one launch, keys and tokens in registers, handed over through
+// shared memory; the other blocks of the launch clear the table meanwhile.
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortBlocks = 8;
+template <int ITEMS>
+__global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(SortArgs a, int cluster) {
+    pdl_enter();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if ((int)blockIdx.x >= cluster) {
+        const int64_t step = (int64_t)(gridDim.x - cluster) * kSortThreads, at = (int64_t)(blockIdx.x - cluster) * kSortThreads + tid;
+        float4 *z = reinterpret_cast<float4 *>(a.zero);
+        for (int64_t i = at; i < a.zeros / 4; i += step) z[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at < a.zeros % 4) a.zero[a.zeros / 4 * 4 + at] = 0.f;
+        return;
+    }
+    constexpr int kHold = ITEMS * kSortThreads;             // elements of a block
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    int2 *s_hold = reinterpret_cast<int2 *>(s_raw);
+    unsigned short *s_count = reinterpret_cast<unsigned short *>(s_raw + sizeof(int2) * kHold);     // [warps][kBins]
+    __shared__ int s_total[kSortBlocks][kBins], s_base[kBins], s_sum[kBins / 32], s_bad[kSortBlocks], s_worst;
+    const int rank = blockIdx.x;
+    if (tid == 0) s_worst = kNoneBad;
+    __syncthreads();
+    int key[ITEMS], token[ITEMS], bad = kNoneBad;
+#pragma unroll
+    for (int j = 0; j < ITEMS; j++) {
+        token[j] = rank * kHold + (warp * ITEMS + j) * 32 + lane;
+        key[j] = (int)a.vocab;
+        if (token[j] < a.n) {
+            const int64_t id = a.ids[token[j]];
+            if (!no_part(id, a.vocab, a.padding)) key[j] = (int)id;
+            else if (id != a.padding) bad = min(bad, token[j]);
+        }
+    }
+    if (bad != kNoneBad) atomicMin(&s_worst, bad);
+    if (rank == 0 && tid == 0) a.owners[0] = 0;
+    for (int pass = 0; pass < a.passes; pass++) {
+        const int shift = pass * kDigit;
+        for (int i = tid; i < kSortWarps * kBins / 2; i += kSortThreads) reinterpret_cast<int *>(s_count)[i] = 0;
+        __syncthreads();
+        unsigned short place[ITEMS], *mine = s_count + warp * kBins;
+#pragma unroll
+        for (int j = 0; j < ITEMS; j++) {
+            // (elements behind the last token are of no bin)
+            const int bin = token[j] < a.n ? key[j] >> shift & (kBins - 1) : -1;
+            const unsigned same = __match_any_sync(0xffffffffu, bin);
+            const int lower = __popc(same & ((1u << lane) - 1));
+            place[j] = bin >= 0 ? (unsigned short)(mine[bin] + lower) : 0;
+            __syncwarp();
+            if (bin >= 0 && lower == 0) mine[bin] = (unsigned short)(mine[bin] + __popc(same));
+            __syncwarp();
+        }
+        __syncthreads();
+        if (tid < kBins) {
+            int at = 0;
+#pragma unroll 8
+            for (int w = 0; w < kSortWarps; w++) {
+                const int c = s_count[w * kBins + tid];
+                s_count[w * kBins + tid] = (unsigned short)at;
+                at += c;
+            }
+            for (int q = 0; q < cluster; q++) st_remote_u32(map_to_cta(smem_u32(&s_total[rank][tid]), q), (uint32_t)at);
+        }
+        if (pass == 0 && tid == kSortThreads - 1) st_remote_u32(map_to_cta(smem_u32(&s_bad[rank]), 0), (uint32_t)s_worst);
+        __syncwarp();
+        cluster_sync_all();
+        int all = 0, before = 0;
+        if (tid < kBins)
+            for (int q = 0; q < cluster; q++) {
+                const int c = s_total[q][tid];
+                all += c;
+                if (q < rank) before += c;
+            }
+        const int base = bins_before(all, s_sum) + before;
+        if (tid < kBins) s_base[tid] = base;
+        __syncthreads();
+        const bool last = pass == a.passes - 1;
+#pragma unroll
+        for (int j = 0; j < ITEMS; j++) {
+            if (token[j] >= a.n) continue;
+            const int bin = key[j] >> shift & (kBins - 1), to = s_base[bin] + s_count[warp * kBins + bin] + place[j];
+            if (last) {
+                a.keys[to] = key[j];
+                a.tokens[to] = token[j];
+            } else {
+                const uint32_t at = map_to_cta(smem_u32(s_hold + to % kHold), to / kHold);
+                asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(at), "r"(key[j]), "r"(token[j]) : "memory");
+            }
+        }
+        if (last) break;
+        __syncwarp();
+        cluster_sync_all();
+#pragma unroll
+        for (int j = 0; j < ITEMS; j++) {
+            const int at = (warp * ITEMS + j) * 32 + lane;
+            token[j] = a.n;
+            if (rank * kHold + at < a.n) {
+                const int2 e = s_hold[at];
+                key[j] = e.x;
+                token[j] = e.y;
+            }
+        }
+    }
+    if (rank == 0 && tid == 0) {
+        int worst = kNoneBad;
+        for (int q = 0; q < cluster; q++) worst = min(worst, s_bad[q]);
+        a.hdr->status = worst == kNoneBad ? STREAMBP_OK : STREAMBP_E_BAD_LABEL;
+        a.hdr->detail = worst == kNoneBad ? 0 : worst;
+    }
+}
+
+// More tokens: two launches a pass over up to 64 tiles of the list.
+struct SortPass {
+    const int64_t *ids;         // first pass: keys come from here, tokens are the positions
+    const int *keys, *tokens;
+    int *keys_out, *tokens_out, *counts;        // counts: [kBins][tiles], then [tiles] the first token outside the vocabulary
+    int *owners;
+    int64_t vocab, padding;
+    int n, tile, shift;
+    WsHeader *hdr;
+};
+__device__ __forceinline__ int sort_key(const SortPass &p, int i, int &bad) {
+    if (!p.ids) return p.keys[i];
+    const int64_t id = p.ids[i];
+    if (!no_part(id, p.vocab, p.padding)) return (int)id;
+    if (id != p.padding) bad = min(bad, i);
+    return (int)p.vocab;
+}
+__global__ void __launch_bounds__(kBins) sort_count_kernel(SortPass p) {
+    pdl_enter();
+    const int tiles = gridDim.x, tile = blockIdx.x, tid = threadIdx.x;
+    __shared__ int s_bins[kBins], s_bad;
+    s_bins[tid] = 0;
+    if (tid == 0) s_bad = kNoneBad;
+    __syncthreads();
+    const int64_t i1 = min((int64_t)p.n, (int64_t)(tile + 1) * p.tile);
+    int bad = kNoneBad;
+#pragma unroll 4
+    for (int64_t i = (int64_t)tile * p.tile + tid; i < i1; i += kBins)
+        atomicAdd(&s_bins[sort_key(p, (int)i, bad) >> p.shift & (kBins - 1)], 1);
+    if (bad != kNoneBad) atomicMin(&s_bad, bad);
+    __syncthreads();
+    p.counts[tid * tiles + tile] = s_bins[tid];
+    if (p.ids && tid == 0) p.counts[kBins * tiles + tile] = s_bad;
+}
+__global__ void __launch_bounds__(kBins) sort_move_kernel(SortPass p) {
+    pdl_enter();
+    constexpr int kWarps = kBins / 32;
+    const int tiles = gridDim.x, tile = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ int s_next[kBins], s_warp[kWarps][kBins], s_sum[kWarps];
+    if (p.ids && tile == 0 && tid == 0) {
+        int worst = kNoneBad;
+        for (int t = 0; t < tiles; t++) worst = min(worst, p.counts[kBins * tiles + t]);
+        p.hdr->status = worst == kNoneBad ? STREAMBP_OK : STREAMBP_E_BAD_LABEL;
+        p.hdr->detail = worst == kNoneBad ? 0 : worst;
+        p.owners[0] = 0;
+    }
+    // where this tile's elements of bin `tid` begin: behind all smaller bins and the bin's part in the tiles before
+    int all = 0, before = 0;
+#pragma unroll 8
+    for (int t = 0; t < tiles; t++) {
+        const int c = p.counts[tid * tiles + t];
+        all += c;
+        if (t < tile) before += c;
+    }
+    s_next[tid] = bins_before(all, s_sum) + before;
+    const int64_t i1 = min((int64_t)p.n, (int64_t)(tile + 1) * p.tile);
+    int unused = kNoneBad;
+    for (int64_t i0 = (int64_t)tile * p.tile; i0 < i1; i0 += kBins) {
+#pragma unroll
         for (int w = 0; w < kWarps; w++) s_warp[w][tid] = 0;
         __syncthreads();
-        const int i = i0 + tid;
+        const int64_t i = i0 + tid;
         int key = 0, bin = -1;
         if (i < i1) {
-            key = sort_key(p, i);
+            key = sort_key(p, (int)i, unused);
             bin = key >> p.shift & (kBins - 1);
         }
         const unsigned same = __match_any_sync(0xffffffffu, bin);
@@ -133,6 +283,7 @@ __global__ void __launch_bounds__(kThreads) sort_move_kernel(SortPass p) {
         __syncthreads();
         {   // bin `tid`: the warps' places, and where the next round begins
             int at = s_next[tid];
+#pragma unroll
             for (int w = 0; w < kWarps; w++) {
                 const int c = s_warp[w][tid];
                 s_warp[w][tid] = at;
@@ -144,54 +295,82 @@ __global__ void __launch_bounds__(kThreads) sort_move_kernel(SortPass p) {
         if (bin >= 0) {
             const int to = s_warp[warp][bin] + rank;
             p.keys_out[to] = key;
-            p.tokens_out[to] = p.ids ? i : p.tokens[i];
+            p.tokens_out[to] = p.ids ? (int)i : p.tokens[i];
         }
         __syncthreads();
     }
 }
 
 // ---- sums of runs -------------------------------------------------------------------------------------------------------
+// 16 bytes of a row where rows are made of them (N > 1), else one element, as they came; and their values.
+template <typename T, int N> struct Piece {
+    typedef uint4 In;
+    static __device__ __forceinline__ void load(const T *p, In &x) { x = *reinterpret_cast<const uint4 *>(p); }
+    static __device__ __forceinline__ void get(const In &x, float (&v)[Vec<T>::N]) {
+        Vec<T> t;
+        t.load(reinterpret_cast<const T *>(&x));
+#pragma unroll
+        for (int i = 0; i < Vec<T>::N; i++) v[i] = t.v[i];
+    }
+};
+template <typename T> struct Piece<T, 1> {
+    typedef T In;
+    static __device__ __forceinline__ void load(const T *p, In &x) { x = *p; }
+    template <int M> static __device__ __forceinline__ void get(const In &x, float (&v)[M]) { v[0] = to_f32(x); }
+};
 template <typename T>
 struct RunArgs {
     const int *keys, *tokens;       // sorted
     const T *dy;
-    float *d_table, *partials;      // partials: [chunks][2][d]; 0: of a run that began before, 1: of one that goes on (a chunk inside one run: 0)
+    float *d_table, *partials;      // partials: [chunks][2][dp]; 0: of a run that began before, 1: of one that goes on (a chunk inside one run: 0)
+    int *owners;                    // [0] how many, then the chunks in which a run begins that goes on
     int64_t ldy;
-    int n, chunk, d, vocab, accumulate;
+    int n, chunk, d, dp, vocab, accumulate;
     float scale;
 };
-constexpr int kMaxChunk = 128;
+constexpr int kMaxChunk = 128, kRunThreads = 256;
+// Each thread owns the columns of one 16-byte group of d_out and walks the chunk, four rows of d_out (and, added to, of the
+// table) in flight.  What bounds it is HBM: d_out once, the table's rows once in each direction.
 template <typename T, int N>
-__global__ void __launch_bounds__(kThreads) embedding_runs_kernel(RunArgs<T> a) {
+__global__ void __launch_bounds__(kRunThreads) embedding_runs_kernel(RunArgs<T> a) {
     pdl_enter();
     __shared__ int s_key[kMaxChunk + 2], s_tok[kMaxChunk];
-    const int i0 = blockIdx.x * a.chunk, len = min(a.chunk, a.n - i0);
-    for (int i = threadIdx.x; i < len + 2; i += kThreads) {
-        const int at = i0 + i - 1;
+    const int64_t i0 = (int64_t)blockIdx.x * a.chunk;
+    const int len = (int)min((int64_t)a.chunk, a.n - i0);
+    for (int i = threadIdx.x; i < len + 2; i += blockDim.x) {
+        const int64_t at = i0 + i - 1;
         s_key[i] = at >= 0 && at < a.n ? a.keys[at] : -1;
     }
-    for (int i = threadIdx.x; i < len; i += kThreads) s_tok[i] = a.tokens[i0 + i];
+    for (int i = threadIdx.x; i < len; i += blockDim.x) s_tok[i] = a.tokens[i0 + i];
     __syncthreads();
-    const int c = (blockIdx.y * kThreads + threadIdx.x) * N;
+    if (blockIdx.y == 0 && threadIdx.x == 0) {
+        const int key = s_key[len];
+        bool began = false;         // in an earlier chunk
+        if (s_key[len + 1] == key && key < a.vocab) {
+            began = s_key[1] == key && s_key[0] == key;
+            if (!began) a.owners[1 + atomicAdd(a.owners, 1)] = blockIdx.x;      // (their order does not matter)
+        }
+    }
+    const int c = (blockIdx.y * blockDim.x + threadIdx.x) * N;
     if (c >= a.d) return;
     float sum[N];
 #pragma unroll
     for (int e = 0; e < N; e++) sum[e] = 0.f;
     bool begun = s_key[0] == s_key[1];          // the run began in an earlier chunk
     constexpr int U = 4;
-    for (int i = 0; i < len; i += U) {
-        float x[U][N];
+    for (int i = 0; i < len && s_key[i + 1] < a.vocab; i += U) {
+        // (values stay as they came until all are on the way)
+        typename Piece<T, N>::In x[U];
+        typename Piece<float, N>::In old[U][sizeof(float) / sizeof(T)];
 #pragma unroll
         for (int u = 0; u < U; u++) {
             if (i + u >= len || s_key[i + u + 1] >= a.vocab) continue;
-            const T *p = a.dy + (int64_t)s_tok[i + u] * a.ldy + c;
-            if constexpr (N == 1) {
-                x[u][0] = to_f32(*p);
-            } else {
-                Vec<T> v;
-                v.load(p);
+            Piece<T, N>::load(a.dy + (int64_t)s_tok[i + u] * a.ldy + c, x[u]);
+            // the table's row of a run that ends here (a crossing run's is read for nothing, at most twice a chunk)
+            if (a.accumulate && s_key[i + u + 2] != s_key[i + u + 1]) {
+                const float *t = a.d_table + (int64_t)s_key[i + u + 1] * a.d + c;
 #pragma unroll
-                for (int e = 0; e < N; e++) x[u][e] = v.v[e];
+                for (int e = 0; e < N; e += 4) Piece<float, N>::load(t + e, old[u][e / 4]);
             }
         }
 #pragma unroll
@@ -199,19 +378,35 @@ __global__ void __launch_bounds__(kThreads) embedding_runs_kernel(RunArgs<T> a) 
             if (i + u >= len) continue;
             const int key = s_key[i + u + 1];
             if (key >= a.vocab) continue;
+            float v[N];
+            Piece<T, N>::get(x[u], v);
 #pragma unroll
-            for (int e = 0; e < N; e++) sum[e] += x[u][e];
+            for (int e = 0; e < N; e++) sum[e] += v[e];
             const bool last = i + u + 1 == len, goes_on = s_key[i + u + 2] == key;
             if (goes_on && !last) continue;
             float *to;
             if (begun || goes_on) {
-                to = a.partials + ((int64_t)blockIdx.x * 2 + (begun ? 0 : 1)) * a.d + c;
-#pragma unroll
-                for (int e = 0; e < N; e++) to[e] = sum[e];
+                to = a.partials + ((int64_t)blockIdx.x * 2 + (begun ? 0 : 1)) * a.dp + c;
             } else {
                 to = a.d_table + (int64_t)key * a.d + c;
+                if (a.accumulate) {
 #pragma unroll
-                for (int e = 0; e < N; e++) to[e] = a.accumulate ? fmaf(sum[e], a.scale, to[e]) : sum[e] * a.scale;
+                    for (int e = 0; e < N; e += 4) {
+                        float o[4];
+                        Piece<float, N>::get(old[u][e / 4], o);
+#pragma unroll
+                        for (int f = 0; f < 4 && e + f < N; f++) sum[e + f] = fmaf(sum[e + f], a.scale, o[f]);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; e++) sum[e] *= a.scale;
+                }
+            }
+            if constexpr (N == 1) {
+                *to = sum[0];
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; e += 4) *reinterpret_cast<float4 *>(to + e) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
             }
             begun = false;
 #pragma unroll
@@ -220,43 +415,101 @@ __global__ void __launch_bounds__(kThreads) embedding_runs_kernel(RunArgs<T> a) 
     }
 }
 
-// The partial sums of a run that crosses chunks, by the block of the chunk that it begins in: 32 columns, 8 sections of chunks.
+// The partial sums of a run that crosses chunks, 128 columns at a time (an item): a warp adds those of a run of up to kShort
+// chunks, a block's warps a section each of a longer one's, and the sections are added in order.
 struct JoinArgs {
-    const int *keys;
+    const int *keys, *owners;
     const float *partials;
     float *d_table;
-    int n, chunk, d, vocab, accumulate;
+    int n, chunk, chunks, d, dp, vocab, accumulate;
     float scale;
 };
-__global__ void __launch_bounds__(kThreads) embedding_join_kernel(JoinArgs a) {
+constexpr int kShort = 128;
+__global__ void __launch_bounds__(256) embedding_join_kernel(JoinArgs a) {
     pdl_enter();
-    const int b = blockIdx.x, last = min((b + 1) * a.chunk, a.n) - 1;
-    const int key = a.keys[last];
-    if (last + 1 >= a.n || key >= a.vocab || a.keys[last + 1] != key) return;               // no run goes on
-    if (a.keys[b * a.chunk] == key && b > 0 && a.keys[b * a.chunk - 1] == key) return;      // it began before
-    // the run's last element: the last one with this key
-    int lo = last + 1, hi = a.n - 1;
-    while (lo < hi) {
-        const int mid = lo + (hi - lo + 1) / 2;
-        if (a.keys[mid] == key) lo = mid;
-        else hi = mid - 1;
+    __shared__ float4 s_sum[8][32];
+    __shared__ int s_first[8], s_last[8], s_key[8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int strips = (a.d + 127) / 128;
+    const int64_t items = (int64_t)a.owners[0] * strips;
+    // eight items a block, one where the blocks suffice for that (long runs are then spread best)
+    const int each = items > gridDim.x ? 8 : 1;
+    for (int64_t it0 = (int64_t)blockIdx.x * each; it0 < items; it0 += (int64_t)gridDim.x * each) {
+        const int64_t it = it0 + warp;
+        const bool own = warp < each && it < items;
+        int b = 0, last = 0, key = 0;
+        const int c = (int)(it % strips) * 128 + lane * 4;
+        float old[4] = {0.f, 0.f, 0.f, 0.f};
+        auto before = [&](int k, int col) {
+            const float *t = a.d_table + (int64_t)k * a.d + col;
+            if (a.accumulate)
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (col + e < a.d) old[e] = t[e];
+        };
+        if (own) {
+            b = a.owners[1 + it / strips];
+            key = a.keys[(int64_t)(b + 1) * a.chunk - 1];
+            // the last chunk that begins with this key: 32 guesses at a time, the next 32 chunks first
+            auto same = [&](int64_t q) { return q < a.chunks && a.keys[q * a.chunk] == key; };
+            unsigned yes = __ballot_sync(0xffffffffu, same(b + 2 + lane));
+            last = b + 1 + (yes == 0xffffffffu ? 32 : __ffs(~yes) - 1);
+            if (yes == 0xffffffffu) {
+                int64_t step = 1;
+                while (step * 32 < a.chunks) step *= 32;
+                for (; step >= 1; step /= 32) {
+                    yes = __ballot_sync(0xffffffffu, same(last + (lane + 1) * step));
+                    last += (int)((yes == 0xffffffffu ? 32 : __ffs(~yes) - 1) * step);
+                }
+            }
+            if (last - b <= kShort) before(key, c);
+        }
+        // chunk from's sum of its last run and the first runs of chunks q0 .. q1 - 1
+        auto add = [&](int col, int from, bool with_from, int q0, int q1) {
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (col >= a.dp) return s;
+            if (with_from) s = *reinterpret_cast<const float4 *>(a.partials + ((int64_t)from * 2 + 1) * a.dp + col);
+#pragma unroll 8
+            for (int q = q0; q < q1; q++) {
+                const float4 t = *reinterpret_cast<const float4 *>(a.partials + (int64_t)q * 2 * a.dp + col);
+                s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+            }
+            return s;
+        };
+        auto put = [&](float4 s, int k, int col) {
+            const float v[4] = {s.x, s.y, s.z, s.w};
+            float *to = a.d_table + (int64_t)k * a.d + col;
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (col + e < a.d) to[e] = fmaf(v[e], a.scale, old[e]);
+        };
+        if (own && last - b <= kShort) put(add(c, b, true, b + 1, last + 1), key, c);
+        const bool is_long = own && last - b > kShort;
+        if (!__syncthreads_or(is_long)) continue;
+        if (lane == 0) {
+            s_first[warp] = is_long ? b : -1;
+            s_last[warp] = last;
+            s_key[warp] = key;
+        }
+        __syncthreads();
+        for (int w = 0; w < each; w++) {
+            const int first = s_first[w];
+            if (first < 0) continue;
+            const int per = (s_last[w] - first + 7) / 8, q0 = first + 1 + warp * per, col = (int)((it0 + w) % strips) * 128 + lane * 4;
+            if (warp == 0) before(s_key[w], col);
+            s_sum[warp][lane] = add(col, first, warp == 0, q0, min(q0 + per, s_last[w] + 1));
+            __syncthreads();
+            if (warp == 0) {
+                float4 s = s_sum[0][lane];
+                for (int i = 1; i < 8; i++) {
+                    const float4 t = s_sum[i][lane];
+                    s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+                }
+                put(s, s_key[w], col);
+            }
+            __syncthreads();
+        }
     }
-    const int b1 = lo / a.chunk;                // chunks b (slot 1) and b + 1 .. b1 (slot 0)
-    __shared__ float s_sum[8][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.y * 32 + x;
-    const int per = (b1 - b + 7) / 8, q0 = b + 1 + y * per, q1 = min(q0 + per, b1 + 1);
-    float s = 0.f;
-    if (c < a.d) {
-        if (y == 0) s = a.partials[((int64_t)b * 2 + 1) * a.d + c];
-#pragma unroll 4
-        for (int q = q0; q < q1; q++) s += a.partials[(int64_t)q * 2 * a.d + c];
-    }
-    s_sum[y][x] = s;
-    __syncthreads();
-    if (y || c >= a.d) return;
-    for (int i = 1; i < 8; i++) s += s_sum[i][x];
-    float *to = a.d_table + (int64_t)key * a.d + c;
-    *to = a.accumulate ? fmaf(s, a.scale, *to) : s * a.scale;
 }
 
 }  // namespace
@@ -264,17 +517,33 @@ __global__ void __launch_bounds__(kThreads) embedding_join_kernel(JoinArgs a) {
 EmbeddingPlan embedding_plan(int64_t n, int64_t vocab, int64_t d) {
     EmbeddingPlan p;
     p.passes = 1;
-    while (p.passes < 4 && (vocab >> (8 * p.passes)) != 0) p.passes++;          // (`vocab` itself is a key)
-    // tiles of the sort: at most 64, whole rounds of a block
+    while (p.passes < 4 && (vocab >> (kDigit * p.passes)) != 0) p.passes++;     // (`vocab` itself is a key)
+    p.one_launch = n <= (int64_t)kSortBlocks * kSortThreads * 8;
+    // tiles of the sort's launches: at most 64, whole rounds of a block
     const int64_t per = (n + 63) / 64;
-    p.tile = (int)std::max<int64_t>(1024, (per + kThreads - 1) / kThreads * kThreads);
+    p.tile = (int)((per + kBins - 1) / kBins * kBins);
     p.tiles = (int)((n + p.tile - 1) / p.tile);
     // chunks of the sorted list: about sixteen blocks of 256 threads with 8 columns each an SM
     const int64_t strips = (d + 2047) / 2048;
     p.chunk = (int)std::min<int64_t>(kMaxChunk, std::max<int64_t>(8, n * strips / (148 * 16)));
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
+    p.partial_width = (int)((d + 3) / 4 * 4);
     return p;
 }
+int embedding_counts(const EmbeddingPlan &p) { return p.one_launch ? 0 : (kBins + 1) * p.tiles; }
+
+namespace {
+template <int ITEMS>
+int launch_sort(const SortArgs &a, int cluster, int64_t zero_blocks, cudaStream_t st) {
+    static PerDevice ready;
+    constexpr int smem = ITEMS * kSortThreads * 8 + kSortWarps * kBins * 2;
+    auto kernel = sort_cluster_kernel<ITEMS>;
+    if (!ready.get([&] { return cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) ? 1 : 0; }))
+        return STREAMBP_E_CUDA;
+    const int64_t blocks = cluster + (zero_blocks + cluster - 1) / cluster * cluster;
+    return launch_clusters(kernel, dim3((unsigned)blocks), kSortThreads, smem, cluster, 1, st, a, cluster);
+}
+}  // namespace
 
 template <typename T>
 int embedding_fwd(const T *table, int64_t ld, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, float scale,
@@ -293,23 +562,42 @@ int embedding_fwd(const T *table, int64_t ld, const int64_t *ids, int64_t n, int
 template <typename T>
 int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, float scale, int64_t padding,
                   float *d_table, bool accumulate, const EmbeddingPlan &p, int *const (&keys)[2], int *const (&tokens)[2],
-                  int *counts, float *partials, WsHeader *hdr, cudaStream_t st) {
-    if (!accumulate) SBP_TRY(fill_zero(d_table, sizeof(float) * (size_t)vocab * d, st));
-    for (int i = 0; i < p.passes; i++) {
-        SortPass s{i ? nullptr : ids, keys[(i + 1) & 1], tokens[(i + 1) & 1], keys[i & 1], tokens[i & 1], counts, vocab, padding,
-                   (int)n, p.tile, 8 * i, i ? nullptr : hdr};
-        SBP_LAUNCH(sort_count_kernel, (unsigned)(p.tiles + (i ? 0 : 1)), kThreads, 0, st, s);
-        SBP_LAUNCH(sort_move_kernel, (unsigned)p.tiles, kThreads, 0, st, s);
+                  int *counts, int *owners, float *partials, WsHeader *hdr, cudaStream_t st) {
+    int done = 0;
+    if (p.one_launch) {
+        const SortArgs s{ids, keys[0], tokens[0], owners, accumulate ? nullptr : d_table, accumulate ? 0 : vocab * d, vocab, padding, (int)n,
+                         p.passes, hdr};
+        int cluster = 1;
+        while (cluster < kSortBlocks && n > (int64_t)cluster * kSortThreads) cluster *= 2;
+        const int64_t each = (n + (int64_t)cluster * kSortThreads - 1) / ((int64_t)cluster * kSortThreads);
+        const int64_t zero = std::min<int64_t>(148, (s.zeros + 4 * kSortThreads - 1) / (4 * kSortThreads));
+        if (each <= 1) SBP_TRY(launch_sort<1>(s, cluster, zero, st));
+        else if (each <= 2) SBP_TRY(launch_sort<2>(s, cluster, zero, st));
+        else if (each <= 4) SBP_TRY(launch_sort<4>(s, cluster, zero, st));
+        else SBP_TRY(launch_sort<8>(s, cluster, zero, st));
+    } else {
+        if (!accumulate) SBP_TRY(fill_zero(d_table, sizeof(float) * (size_t)vocab * d, st));
+        for (int i = 0; i < p.passes; i++) {
+            const SortPass s{i ? nullptr : ids, keys[(i + 1) & 1], tokens[(i + 1) & 1], keys[i & 1], tokens[i & 1], counts, owners, vocab,
+                             padding, (int)n, p.tile, kDigit * i, hdr};
+            SBP_LAUNCH(sort_count_kernel, (unsigned)p.tiles, kBins, 0, st, s);
+            SBP_LAUNCH(sort_move_kernel, (unsigned)p.tiles, kBins, 0, st, s);
+        }
+        done = (p.passes - 1) & 1;
     }
-    const int done = (p.passes - 1) & 1;
-    const RunArgs<T> r{keys[done], tokens[done], dy, d_table, partials, ldy, (int)n, p.chunk, (int)d, (int)vocab, accumulate ? 1 : 0, scale};
+    const RunArgs<T> r{keys[done], tokens[done], dy, d_table, partials, owners, ldy, (int)n, p.chunk, (int)d, p.partial_width, (int)vocab,
+                       accumulate ? 1 : 0, scale};
     constexpr int N = Vec<T>::N;
-    if (d % N == 0 && ldy % N == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0)
-        SBP_LAUNCH((embedding_runs_kernel<T, N>), dim3((unsigned)p.chunks, (unsigned)((d / N + kThreads - 1) / kThreads)), kThreads, 0, st, r);
-    else
-        SBP_LAUNCH((embedding_runs_kernel<T, 1>), dim3((unsigned)p.chunks, (unsigned)((d + kThreads - 1) / kThreads)), kThreads, 0, st, r);
-    const JoinArgs j{keys[done], partials, d_table, (int)n, p.chunk, (int)d, (int)vocab, accumulate ? 1 : 0, scale};
-    if (p.chunks > 1) SBP_LAUNCH(embedding_join_kernel, dim3((unsigned)p.chunks, (unsigned)((d + 31) / 32)), kThreads, 0, st, j);
+    const bool grouped = d % N == 0 && ldy % N == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0;
+    const int64_t groups = grouped ? d / N : d, strips = (groups + kRunThreads - 1) / kRunThreads;
+    const int threads = (int)(((groups + strips - 1) / strips + 31) / 32 * 32);
+    if (grouped) SBP_LAUNCH((embedding_runs_kernel<T, N>), dim3((unsigned)p.chunks, (unsigned)strips), threads, 0, st, r);
+    else SBP_LAUNCH((embedding_runs_kernel<T, 1>), dim3((unsigned)p.chunks, (unsigned)strips), threads, 0, st, r);
+    if (p.chunks == 1) return STREAMBP_OK;
+    const JoinArgs j{keys[done], owners, partials, d_table, (int)n, p.chunk, p.chunks, (int)d, p.partial_width, (int)vocab,
+                     accumulate ? 1 : 0, scale};
+    const int64_t most = (int64_t)p.chunks * ((d + 127) / 128);
+    SBP_LAUNCH(embedding_join_kernel, (unsigned)std::min<int64_t>(most, 148 * 8), 256, 0, st, j);
     return STREAMBP_OK;
 }
 
@@ -318,8 +606,8 @@ template int embedding_fwd<float>(const float *, int64_t, const int64_t *, int64
 template int embedding_fwd<bf16>(const bf16 *, int64_t, const int64_t *, int64_t, int64_t, int64_t, float, int64_t, bf16 *, int64_t,
                                  WsHeader *, cudaStream_t);
 template int embedding_bwd<float>(const float *, int64_t, const int64_t *, int64_t, int64_t, int64_t, float, int64_t, float *, bool,
-                                  const EmbeddingPlan &, int *const (&)[2], int *const (&)[2], int *, float *, WsHeader *, cudaStream_t);
+                                  const EmbeddingPlan &, int *const (&)[2], int *const (&)[2], int *, int *, float *, WsHeader *, cudaStream_t);
 template int embedding_bwd<bf16>(const bf16 *, int64_t, const int64_t *, int64_t, int64_t, int64_t, float, int64_t, float *, bool,
-                                 const EmbeddingPlan &, int *const (&)[2], int *const (&)[2], int *, float *, WsHeader *, cudaStream_t);
+                                 const EmbeddingPlan &, int *const (&)[2], int *const (&)[2], int *, int *, float *, WsHeader *, cudaStream_t);
 
 }  // namespace sbp

@@ -6,10 +6,13 @@
 namespace sbp {
 
 struct EmbeddingPlan {
-    int passes;             // of the sort, 8 bits each
-    int tile, tiles;        // tokens of a block of the sort, blocks
+    int passes;             // of the sort
+    bool one_launch;        // of the sort, in a cluster
+    int tile, tiles;        // else: tokens of a block of the sort, blocks
     int chunk, chunks;      // entries of the sorted list that are summed by one block, blocks
+    int partial_width;      // floats of a row of partial sums
 };
 EmbeddingPlan embedding_plan(int64_t n, int64_t vocab, int64_t d);
+int embedding_counts(const EmbeddingPlan &p);      // ints the sort's launches hand on
 
 }  // namespace sbp
