@@ -206,4 +206,73 @@ __device__ __forceinline__ RowStats join(const RowStats &a, const RowStats &b, f
     return r;
 }
 
+// Adds the values of x (all at or below m) to the sums of a thread.
+template <typename T, bool ENT, int U>
+__device__ __forceinline__ void add_batch(const Raw<T> (&x)[U], float c, Pair &S, Pair &W, float m) {
+    constexpr int H = RowGroups<T>::N / 2;
+    const Pair minus(-m, -m), cc(c, c);
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        Pair p[H];
+        x[u].pairs(p);
+#pragma unroll
+        for (int i = 0; i < H; i++) {
+            const Pair d = p[i] + minus, t = d * cc;
+            float a, b;
+            t.get(a, b);
+            const Pair e(exp2_approx(a), exp2_approx(b));
+            S = S + e;
+            if (ENT) W = fma2(e, d, W);
+        }
+    }
+}
+// The same where some are so far below it that e * d is not the 0 it has to be.
+template <typename T, int U>
+__device__ __forceinline__ void add_deep_batch(const Raw<T> (&x)[U], float c, Pair &S, Pair &W, float m) {
+    constexpr int H = RowGroups<T>::N / 2;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        Pair p[H];
+        x[u].pairs(p);
+#pragma unroll
+        for (int i = 0; i < H; i++) {
+            float a, b;
+            p[i].get(a, b);
+            a -= m;
+            b -= m;
+            const Pair e(exp2_approx(a * c), exp2_approx(b * c));
+            S = S + e;
+            W = fma2(e, Pair(fmaxf(a, kDeep), fmaxf(b, kDeep)), W);
+        }
+    }
+}
+
+// A thread's running maximum and sums.
+template <typename T, bool ENT, int U>
+struct Running {
+    float m = -INFINITY, largest = -INFINITY;        // of all, and of the part
+    Pair S = Pair(0.f, 0.f), W = Pair(0.f, 0.f);
+    __device__ __forceinline__ void add(const Raw<T> (&x)[U], float c) {
+        float mx = x[0].largest(), mn = x[0].smallest();
+#pragma unroll
+        for (int u = 1; u < U; u++) {
+            mx = fmaxf(mx, x[u].largest());
+            if (ENT) mn = fminf(mn, x[u].smallest());
+        }
+        largest = fmaxf(largest, mx);
+        if (mx > m) {
+            if (m > -INFINITY) {
+                const float dm = fmaxf(m - mx, kDeep), f = exp2_approx(dm * c);
+                const Pair ff(f, f);
+                if (ENT) W = ff * fma2(Pair(dm, dm), S, W);
+                S = S * ff;
+            }
+            m = mx;
+        }
+        const float at = finite_or_zero(m);
+        if (ENT && !(mn - at > kDeep)) add_deep_batch<T, U>(x, c, S, W, at);
+        else add_batch<T, ENT, U>(x, c, S, W, at);
+    }
+};
+
 }  // namespace sbp
