@@ -484,7 +484,7 @@ int streambp_token_logprobs_backward(const void *logits, int64_t ld, int64_t row
  * absent and reported as STREAMBP_E_BAD_LABEL.  1 <= k <= STREAMBP_TOP_MAX, vocab <= STREAMBP_DISTILL_MAX_VOCAB, rows <= 2^27.
  * Logits of -inf have probability 0 (the loss is +inf where one is listed with q > 0); a NaN or +inf makes its row NaN.
  */
-#define STREAMBP_DISTILL_MAX_VOCAB 393216
+#define STREAMBP_DISTILL_MAX_VOCAB (1 << 22)
 typedef struct {
     int32_t k;
     int32_t tail;
@@ -538,7 +538,7 @@ int streambp_layernorm_backward(const void *dy, int64_t lddy, const void *x, int
 /*
  * Embedding: out[t] = scale table[ids[t]] (table [vocab, d], out [n, d] of `dtype`, rounded once).  A token equal to padding_id
  * has a row of zeros and no gradient (a value outside the vocabulary, such as -1: no token is padding).  Ids outside the
- * vocabulary are treated like padding and reported as STREAMBP_E_BAD_LABEL (detail: the first).
+ * vocabulary are treated like padding and reported as STREAMBP_E_BAD_LABEL.
  * Backward: d_table (fp32 [vocab, d], dense) = or, with accumulate = 1, += scale times the sums of d_out's rows by id, formed
  * over the tokens sorted by id and joined in a fixed order (reproducible bit by bit); rows of no token are 0 or stay as they
  * are (they are not read).  1 <= n < 2^30, vocab < 2^31 - 1, d <= 2^20.

@@ -921,7 +921,7 @@ def mx8_decode(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, str
 
 # ---- the ends of a model ------------------------------------------------------------------------------------------
 TOP_MAX = 128
-DISTILL_MAX_VOCAB = 393216
+DISTILL_MAX_VOCAB = 1 << 22
 
 
 def _vectors(what: str, dev: int, shape: tuple, **tensors) -> list:

@@ -726,7 +726,7 @@ int streambp_last_device_status(void *workspace, void *cuda_stream) {
     if (!cuda_ok(cudaMemcpyAsync(&h, workspace, sizeof(h), cudaMemcpyDeviceToHost, st))) return STREAMBP_E_CUDA;
     if (!cuda_ok(cudaStreamSynchronize(st))) return STREAMBP_E_CUDA;
     const int f1 = gemm_tc_take_fault(), f2 = attention_tc_take_fault(), f3 = wait_probe_take_fault(),
-              f4 = gemm_epilogue_take_fault(), f5 = attention_window_take_fault(), f6 = distill_take_fault();
+              f4 = gemm_epilogue_take_fault(), f5 = attention_window_take_fault(), f6 = layernorm_take_fault();
     if (f1 < 0 || f2 < 0 || f3 < 0 || f4 < 0 || f5 < 0 || f6 < 0) return STREAMBP_E_CUDA;
     if (f1 > 0 || f2 > 0 || f3 > 0 || f4 > 0 || f5 > 0 || f6 > 0) return STREAMBP_E_DEVICE_TIMEOUT;
     return h.status;

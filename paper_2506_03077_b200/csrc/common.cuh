@@ -406,6 +406,7 @@ int cast_from_f32(const float *in, int64_t n, T *out, cudaStream_t st);
 template <typename T>
 int add_cast(const float *a, const float *b, int64_t n, T *out, cudaStream_t st);
 int fill_zero(void *p, size_t bytes, cudaStream_t st);
+int clear_status_launch(WsHeader *hdr, cudaStream_t st);
 int ws_guard_selftest(void *ws, size_t bytes, int overrun, cudaStream_t st);
 
 // Attention of one chunk of queries against the key/value prefix [0, q0 + n).
@@ -533,7 +534,6 @@ struct DistillRows {
 template <typename T, typename TO>
 int distill_topk(const T *logits, int64_t ld, int64_t rows, int64_t vocab, const DistillRows &ds, TO *d_logits, int64_t ldd,
                  WsHeader *hdr, cudaStream_t st);
-int distill_take_fault();      // (a bounded wait for a row's copy)
 // For the LM head: marks[t] = 0 where row t takes part, else 1; ids outside the vocabulary go into the status.
 int distill_marks(const DistillRows &ds, int64_t T, int64_t vocab, int64_t *marks, WsHeader *hdr, cudaStream_t st);
 // loss sum of the header += sum of weight * row_loss
@@ -544,6 +544,7 @@ template <typename T>
 int layernorm_fwd(const T *x, int64_t ldx, const T *gain, const T *bias, float eps, int64_t rows, int64_t d, T *y, int64_t ldy,
                   float *mean, float *rstd, cudaStream_t st);
 int layernorm_blocks(int64_t rows, int64_t d);
+int layernorm_take_fault();      // (a bounded wait for a row's copy)
 template <typename T>
 int layernorm_bwd(const T *dy, int64_t lddy, const T *x, int64_t ldx, const T *gain, const float *mean, const float *rstd,
                   const T *add, int64_t ldadd, int64_t rows, int64_t d, T *dx, int64_t lddx, float *dgain, float *dbias,

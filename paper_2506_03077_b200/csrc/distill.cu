@@ -11,16 +11,17 @@
 namespace sbp {
 
 namespace {
-constexpr int kThreads = 512, kCompute = kThreads - 32, kComputeWarps = kCompute / 32, kMaxTop = STREAMBP_TOP_MAX, kMaxCluster = 8;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxTop = STREAMBP_TOP_MAX, kTopWarps = kMaxTop / 32, kMaxCluster = 8, kHash = 512;
 
 struct DistillArgs {
     const int64_t *ids;
     const float *values, *weight;       // weight is optional
     float *row_loss;                    // optional
     int64_t rows, ld, ldd;
-    int vocab, k, tail;
+    int vocab, k;
     Heat heat;
-    WsHeader *hdr;                      // optional: the first row with an id outside the vocabulary goes there
+    WsHeader *hdr;                      // optional: a row with an id outside the vocabulary goes there
+    bool scan;                          // found by one block, else by each row's
     const int *gate;
 };
 
@@ -29,180 +30,69 @@ __device__ __forceinline__ void st_remote_f64(uint32_t a, double v) {
 }
 
 // What a block knows of its segment of a row, for the others: the maximum m, the sums of exp((z - m) / tau) over its tokens
-// (with a tail: over the unlisted and over the listed ones), and sum q (log q - z / tau) over the entries that lie in it.
+// and, with a tail, over the unlisted ones, and sum q (log q - z / tau) over the entries that lie in it.
 struct Segment {
     float m, S, rest, pad;
     double loss;
 };
-struct Entries {
-    int id[kMaxTop], place[kMaxTop], first[kMaxTop];    // the token (-1: none), where its logit lies in this block's shared memory (-1: elsewhere), the entry that lists it first
-    float z[kMaxTop], q[kMaxTop], q_all[kMaxTop];       // of the first entry of a token; q_all: the q of all its entries
-    double logq[kMaxTop];
-    double mass, rest;                                  // sum of the q, and what is left for the tail
-    float mass_f, rest_f;
-};
 
-// The row's entries, by one warp.  With a tail what is left of 1 is a difference, so those exponentials are taken in 64 bits.
-__device__ __forceinline__ void read_entries(const DistillArgs &a, int64_t r, Entries &s) {
-    constexpr int J = kMaxTop / 32;
-    const int lane = threadIdx.x & 31;
-    float t[J], top = -INFINITY;
-    int id[J];
-    bool any = false;
+// sums over the first kTopWarps warps, for their threads (every thread of the block calls; one barrier)
+__device__ __forceinline__ void entry_sums(double &a, double &b, double (*red)[2]) {
+    const int warp = threadIdx.x >> 5;
+    if (warp < kTopWarps) {
 #pragma unroll
-    for (int j = 0; j < J; j++) {
-        const int i = lane + 32 * j;
-        id[j] = -1;
-        t[j] = -INFINITY;
-        if (i < a.k) {
-            const int64_t x = a.ids[r * a.k + i];
-            const float v = a.values[r * a.k + i];
-            if (x >= 0 && x < a.vocab) {
-                id[j] = (int)x;
-                t[j] = v;
-                any = true;
-            }
-            s.id[i] = id[j];
+        for (int o = 16; o > 0; o >>= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+            b += __shfl_xor_sync(0xffffffffu, b, o);
         }
-        top = fmaxf(top, t[j]);
+        if ((threadIdx.x & 31) == 0) {
+            red[warp][0] = a;
+            red[warp][1] = b;
+        }
     }
-    if (a.tail) {
-        double q[J], sum = 0.0;
+    __syncthreads();
+    a = b = 0.0;
 #pragma unroll
-        for (int j = 0; j < J; j++) {
-            q[j] = 0.0;
-            if (32 * j < a.k && id[j] >= 0) q[j] = exp((double)t[j]);
-            sum += q[j];
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-#pragma unroll
-        for (int j = 0; j < J; j++)
-            if (lane + 32 * j < a.k) {
-                s.q[lane + 32 * j] = (float)q[j];
-                s.logq[lane + 32 * j] = (double)t[j];
-            }
-        any = __any_sync(0xffffffffu, any);
-        if (lane == 0) s.rest = any ? fmax(0.0, 1.0 - sum) : 0.0;
-    } else {
-        top = warp_max(top);
-        const float t0 = finite_or_zero(top);
-        float q[J], sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < J; j++) {
-            q[j] = id[j] < 0 ? 0.f : expf(fmaf(t[j] - t0, a.heat.hi, (t[j] - t0) * a.heat.lo));
-            if (t[j] == -INFINITY) q[j] = 0.f;
-            sum += q[j];
-        }
-        sum = warp_sum(sum);
-        const double inv = (double)a.heat.hi + (double)a.heat.lo, logsum = (double)logf(sum);
-        const float over = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-        for (int j = 0; j < J; j++)
-            if (lane + 32 * j < a.k) {
-                s.q[lane + 32 * j] = q[j] * over;
-                s.logq[lane + 32 * j] = ((double)t[j] - (double)t0) * inv - logsum;
-            }
-        if (lane == 0) s.rest = 0.0;
-    }
-    // (of the q as they are held, so that their roundings weigh log q - log p and not each of the two)
-    __syncwarp();
-    double mass = 0.0;
-#pragma unroll
-    for (int j = 0; j < J; j++)
-        if (lane + 32 * j < a.k) mass += (double)s.q[lane + 32 * j];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
-    if (lane == 0) {
-        s.mass = mass;
-        s.mass_f = (float)mass;
-        s.rest_f = (float)s.rest;
+    for (int w = 0; w < kTopWarps; w++) {
+        a += red[w][0];
+        b += red[w][1];
     }
 }
 
-// Which entries lie in elements e0 .. e1 - 1 (at s_row + id - first), and which list the same token; by the same warp.  A hash
-// table (kHash ints) tells whether any token is listed twice; only then every pair is looked at.
-constexpr int kHash = 512;
-__device__ __forceinline__ void place_entries(const DistillArgs &a, int e0, int e1, int first_element, Entries &s, int *table) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int i = 0; i < kHash / 128; i++) reinterpret_cast<int4 *>(table)[lane + 32 * i] = make_int4(-1, -1, -1, -1);
-    __syncwarp();
-    bool twice = false;
-    for (int i = lane; i < a.k; i += 32) {
-        const int id = s.id[i];
-        if (id < 0) continue;
-        for (uint32_t at = (uint32_t)id * 2654435761u >> 23;; at = (at + 1) & (kHash - 1)) {       // (at most kMaxTop of the places are taken)
-            const int was = atomicCAS(table + at, -1, id);
-            twice |= was == id;
-            if (was == -1 || was == id) break;
-        }
-    }
-    twice = __any_sync(0xffffffffu, twice);
-    for (int i = lane; i < a.k; i += 32) {
-        const int id = s.id[i];
-        int first = i;
-        float q = s.q[i];
-        if (twice && id >= 0) {
-            q = 0.f;
-            for (int j = a.k - 1; j >= 0; j--)
-                if (s.id[j] == id) {
-                    first = j;
-                    q += s.q[j];
-                }
-        }
-        s.first[i] = first;
-        s.q_all[i] = q;
-        s.place[i] = id >= e0 && id < e1 ? id - first_element : -1;
-    }
-}
-
-__device__ __forceinline__ void compute_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kCompute) : "memory"); }
-
-// The part of a row that one block of a cluster holds.
-template <typename T, typename TO>
-struct RowSegment {
-    int n, groups, g0, w0, w1, e0, e1, first;     // groups in all and from where; the whole ones among them (counted from g0); elements, and the one at the start of the block's buffer
-    __device__ __forceinline__ RowSegment(const T *p, int vocab, int rank, int log_cluster) {
-        const RowGroups<T> row(p, vocab);
-        n = vocab;
-        const int per = (row.groups + (1 << log_cluster) - 1) >> log_cluster;
-        g0 = min(rank * per, row.groups);
-        const int g1 = min(g0 + per, row.groups);
-        groups = g1 - g0;
-        w0 = max(g0, row.whole_begin()) - g0;
-        w1 = max(w0, min(g1, row.whole_end()) - g0);
-        first = row.first(g0);
-        e0 = max(0, first);
-        e1 = g1 > g0 ? min(vocab, row.first(g1)) : e0;
-    }
-    // by one warp: the whole groups by the copy engine, the ragged ends element by element; all of it reports to `bar`
-    __device__ __forceinline__ void copy(const T *p, T *s_row, uint32_t bar) const {
-        constexpr int N = RowGroups<T>::N;
-        const int lane = threadIdx.x & 31, end = lane / N, v = end ? groups - 1 : 0;
-        if (end < 2 && groups > 0 && (v < w0 || v >= w1)) {
-            const int e = first + v * N + lane % N;
-            s_row[v * N + lane % N] = e >= 0 && e < n ? p[e] : from_f32<T>(-INFINITY);
-        }
-        __syncwarp();
-        if (lane == 0) {
-            const uint32_t bytes = (uint32_t)(w1 - w0) * 16;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // (what was read and written here before comes first)
-            mbar_expect_tx(bar, bytes);
-            if (bytes)
-                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                                 smem_u32(s_row + w0 * N)), "l"(p + (first + w0 * N)), "r"(bytes), "r"(bar)
-                             : "memory");
-        }
-        __syncwarp();
-    }
-    __device__ __forceinline__ void zeros(TO *d) const {
-        constexpr int NO = Vec<TO>::N;
+// `cluster` blocks to a row, a segment each: the sums while the segment streams in, the other blocks' sums, the gradient while it
+// streams in again and out.  The second reading comes from L2 (row_cluster keeps what is under way well below its size), so
+// HBM reads a row once and writes its gradient once, which is what bounds the kernel.  Thread i < k has entry i.
+//
+// With a tail the mass of the unlisted tokens has to be a sum of its own: a difference of two sums would lose it where the
+// list has nearly all.  A bit for each group of 16 bytes tells the streaming sum to leave out groups with listed tokens, whose
+// unlisted ones are added by the group's first entry.  Listed tokens' gradients are written over those of the streaming pass.
+template <typename T, typename TO, bool TAIL>
+__device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const DistillArgs &a, int cluster) {
+    constexpr int N = RowGroups<T>::N, NO = Vec<TO>::N, U = 4;
+    extern __shared__ uint32_t s_bits[];                // TAIL: a bit for each group of the segment
+    __shared__ int s_hash[kHash], s_id[kMaxTop];
+    __shared__ float s_q[kMaxTop];
+    __shared__ double s_red[kTopWarps][2], s_red2[kTopWarps][2];
+    __shared__ RowStats s_warp[kWarps];
+    __shared__ Segment s_seg[kMaxCluster];
+    const int64_t r = blockIdx.x / cluster;
+    const int rank = (int)(blockIdx.x % cluster), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const float w = a.weight ? a.weight[r] : 1.f, c = a.heat.hi * kLog2e;
+    const double inv = (double)a.heat.hi + (double)a.heat.lo;
+    const T *z = logits + r * a.ld;
+    const RowGroups<T> row(z, a.vocab);
+    TO *d = d_logits ? d_logits + r * a.ldd : nullptr;
+    const int per = (row.groups + cluster - 1) / cluster;
+    const int g0 = min(rank * per, row.groups), g1 = min(g0 + per, row.groups);
+    const int w0 = max(g0, row.whole_begin()), w1 = max(w0, min(g1, row.whole_end()));
+    const int e0 = max(0, row.first(g0)), e1 = g1 > g0 ? min(a.vocab, row.first(g1)) : e0;      // elements of the segment
+    auto zeros = [&] {
+        if (!d) return;
         const RowGroups<TO> out(d + e0, e1 - e0);
         Vec<TO> zero;
 #pragma unroll
         for (int i = 0; i < NO; i++) zero.v[i] = 0.f;
-        for (int v = threadIdx.x; v < out.groups; v += kCompute) {
+        for (int v = tid; v < out.groups; v += kThreads) {
             const int f = out.first(v);
             if (out.whole(v)) {
                 zero.store(d + e0 + f);
@@ -212,318 +102,326 @@ struct RowSegment {
                     if (f + i >= 0 && f + i < e1 - e0) d[e0 + f + i] = from_f32<TO>(0.f);
             }
         }
+    };
+    if (w == 0.f) {         // the row takes no part
+        zeros();
+        if (rank == 0 && tid == 0 && a.row_loss) a.row_loss[r] = 0.f;
+        return;
     }
-};
-
-// Persistent clusters of up to eight blocks, two blocks an SM (so that one's loads, barriers and stores are the other's time to
-// compute), take rows in turn.  A row's logits stay in the blocks' shared memory from the sums to the gradient, so they are
-// read from HBM once and the gradient is written once, which is what bounds the kernel.  The last warp reads and places
-// the next row's entries, writes the listed tokens' gradients of the row before over those of the streaming pass, and its
-// loss.  With a tail the listed tokens are taken out of the row first (their logits become -inf), so that the mass of the others is a
-// sum of its own and not a difference.
-template <typename T, typename TO>
-__global__ void __launch_bounds__(kThreads, 2) distill_kernel(const T *logits, TO *d_logits, DistillArgs a, int log_cluster) {
-    pdl_enter();
-    if (gated_off(a.gate)) return;
-    constexpr int N = RowGroups<T>::N, U = 4, NO = Vec<TO>::N;
-    extern __shared__ __align__(128) unsigned char s_raw[];
-    __shared__ __align__(16) int s_hash[kHash];
-    __shared__ __align__(8) unsigned long long s_bar;       // the row is there
-    __shared__ int s_abort;
-    __shared__ RowStats s_warp[kComputeWarps];
-    // (a block may post a row's statistics while another's last warp finishes the row two before: four places)
-    __shared__ Segment s_seg[4][kMaxCluster];
-    __shared__ Entries s_entries[2];
-    __shared__ float s_at[2], s_of_p[2], s_rest[2], s_total[2];
-    const int cluster = 1 << log_cluster, rank = (int)(blockIdx.x & (cluster - 1)), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int64_t step = gridDim.x >> log_cluster;
-    const float c = a.heat.hi * kLog2e;
-    const bool reader = warp == kComputeWarps;
-    auto weight = [&](int64_t r) { return r < a.rows ? (a.weight ? a.weight[r] : 1.f) : 0.f; };
-    // (rows that start alike in their 16 bytes are cut alike)
-    const bool alike = (a.ld * sizeof(T)) % 16 == 0;
-    RowSegment<T, TO> sg(logits, a.vocab, rank, log_cluster);
-    auto segment = [&](int64_t r) { return alike ? sg : RowSegment<T, TO>(logits + r * a.ld, a.vocab, rank, log_cluster); };
-    // the last warp's part for a row that is done but for its listed tokens
-    auto finish = [&](int64_t r, float w, int slot, int at_seg) {
-        const Entries &s = s_entries[slot];
-        const float at = s_at[slot], total = s_total[slot], rest = s_rest[slot];
-        const double rest_q = rest == 0.f ? 0.0 : s.rest;
-        const bool none = s.mass_f == 0.f && s.rest_f == 0.f;
-        const float scale = fmaf(w, a.heat.hi, w * a.heat.lo), of_p = s_of_p[slot];
-        if (d_logits && !none)
-            for (int i = lane; i < a.k; i += 32)
-                if (s.place[i] >= 0 && s.first[i] == i)
-                    d_logits[r * a.ldd + s.id[i]] = from_f32<TO>(scale * fmaf(of_p, exp2_approx((s.z[i] - at) * c), -s.q_all[i]));
-        if (rank == 0 && a.row_loss) {
-            double loss = lane < cluster ? s_seg[at_seg][lane].loss : 0.0;
+    if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (waited for before the others' memory is written)
+    // entry tid
+    int id = -1;
+    float t = -INFINITY;
+    if (tid < a.k) {
+        const int64_t x = a.ids[r * a.k + tid];
+        if (x >= 0 && x < a.vocab) {
+            id = (int)x;
+            t = a.values[r * a.k + tid];
+        } else if (x != -1 && a.hdr && !a.scan && rank == 0) {
+            set_status(a.hdr, STREAMBP_E_BAD_LABEL, (int)r);
+        }
+    }
+    const bool here = id >= e0 && id < e1;
+    bool shared_group = false;          // any two of the segment's entries
+    if (TAIL) {
+        for (int i = tid; i < (g1 - g0 + 31) / 32; i += kThreads) s_bits[i] = 0;
+        __syncthreads();
+        const int g = here ? (id + row.off) / N - g0 : 0;
+        if (here) shared_group = atomicOr(&s_bits[g >> 5], 1u << (g & 31)) >> (g & 31) & 1;
+        shared_group = __syncthreads_or(shared_group);
+    }
+    // the sums over the segment (TAIL: but for groups with listed tokens)
+    Running<T, false> run;
+    {
+        auto skip = [&](int v, Raw<T> &x) {
+            if (TAIL && (s_bits[(v - g0) >> 5] >> ((v - g0) & 31) & 1)) x.fill(-INFINITY);
+        };
+        Raw<T> x[U];
+        int v = w0 + tid;
+        for (; v + (U - 1) * kThreads < w1; v += U * kThreads) {
 #pragma unroll
-            for (int o = kMaxCluster / 2; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-            const double inv = (double)a.heat.hi + (double)a.heat.lo, logS = total == 0.f ? 0.0 : (double)logf(total);
-            if (s.mass != 0.0) loss += s.mass * ((double)at * inv + logS);
-            if (rest_q != 0.0) loss += rest_q * (double)(logf((float)rest_q) - logf(rest / total));
-            if (lane == 0) a.row_loss[r] = none ? 0.f : (float)loss;
+            for (int u = 0; u < U; u++) row.load_whole(v + u * kThreads, x[u]);
+#pragma unroll
+            for (int u = 0; u < U; u++) skip(v + u * kThreads, x[u]);
+            run.add(x, c);
+        }
+        if (v < w1) {
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                if (v + u * kThreads < w1) row.load_whole(v + u * kThreads, x[u]);
+                else x[u].fill(-INFINITY);
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (v + u * kThreads < w1) skip(v + u * kThreads, x[u]);
+            run.add(x, c);
+        }
+        if (tid >= kThreads - 2 && g0 < g1) {           // the ragged ends (one group at each, which may be the same one)
+            const int v = tid == kThreads - 2 ? g0 : g1 - 1;
+            if ((v < w0 || v >= w1) && !(tid == kThreads - 1 && v == g0)) {
+                Raw<T> y[1];
+                row.load(v, y[0]);
+                skip(v, y[0]);
+                run.add(y, c);
+            }
+        }
+    }
+    float m = run.m, S;
+    {
+        float lo, hi;
+        run.S.get(lo, hi);
+        S = lo + hi;
+    }
+    // entries: which token was listed before, the q, the logit
+    if (tid < kMaxTop) {
+        s_id[tid] = id;
+        for (int i = tid; i < kHash; i += kMaxTop) s_hash[i] = -1;
+    }
+    const float zi = here ? to_f32(z[id]) : -INFINITY;
+    __syncthreads();
+    if (warp < kTopWarps) {
+        const float top = warp_max(t);
+        if (lane == 0) s_warp[warp].W = top;
+    }
+    bool twice = false;
+    if (id >= 0)
+        for (uint32_t at = (uint32_t)id * 2654435761u >> 23;; at = (at + 1) & (kHash - 1)) {       // (at most kMaxTop of the places are taken)
+            const int was = atomicCAS(&s_hash[at], -1, id);
+            twice |= was == id;
+            if (was == -1 || was == id) break;
+        }
+    const bool any_twice = __syncthreads_or(twice);
+    float t0 = s_warp[0].W;
+#pragma unroll
+    for (int i = 1; i < kTopWarps; i++) t0 = fmaxf(t0, s_warp[i].W);
+    t0 = finite_or_zero(t0);
+    // (with a tail what is left of 1 is a difference, so those exponentials are taken in 64 bits)
+    double e = 0.0;
+    if (id >= 0) e = TAIL ? exp((double)t) : t == -INFINITY ? 0.0 : (double)expf(fmaf(t - t0, a.heat.hi, (t - t0) * a.heat.lo));
+    double sum = e, listed = id >= 0 ? 1.0 : 0.0;
+    entry_sums(sum, listed, s_red);
+    const float q = TAIL ? (float)e : sum == 0.0 ? 0.f : (float)e / (float)sum;
+    double mass = (double)q, loss = 0.0;        // (of the q as they are held, so that their roundings weigh log q - log p and not each of the two)
+    if (here && q != 0.f) loss = (double)q * ((TAIL ? (double)t : ((double)t - (double)t0) * inv - (double)logf((float)sum)) - (double)zi * inv);
+    if (tid < kMaxTop) s_q[tid] = q;
+    entry_sums(mass, loss, s_red2);
+    const double rest_all = TAIL && listed != 0.0 ? fmax(0.0, 1.0 - sum) : 0.0;
+    // the entry that lists its token first has the q of all that do
+    bool first = here;
+    float q_all = q;
+    if (any_twice && here) {
+        q_all = 0.f;
+        for (int j = a.k - 1; j >= 0; j--)
+            if (s_id[j] == id) {
+                first = j == tid;
+                q_all += s_q[j];
+            }
+    }
+    float m_rest = m, rest = S;
+    if (TAIL && here) {
+        // the first entry of a group adds its unlisted tokens; each token's first entry the token
+        const int g = (id + row.off) / N;
+        bool of_group = true;
+        uint32_t mask = 1u << ((id + row.off) % N);
+        if (shared_group)
+            for (int j = 0; j < a.k; j++) {
+                const int other = s_id[j];
+                if (other < e0 || other >= e1 || (other + row.off) / N != g) continue;
+                if (j < tid) of_group = false;
+                mask |= 1u << ((other + row.off) % N);
+            }
+        float x[N], best = m;
+        row.load(g, x, -INFINITY);
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            if (!of_group || (mask >> i & 1)) x[i] = -INFINITY;
+            best = fmaxf(best, x[i]);
+        }
+        const float at = finite_or_zero(best);
+        rest = S * exp2_approx((m - at) * c);
+#pragma unroll
+        for (int i = 0; i < N; i++) rest += exp2_approx((x[i] - at) * c);
+        m_rest = best;
+    }
+    if (TAIL) {
+        // both sums relative to one maximum
+        m = first ? fmaxf(m_rest, zi) : m_rest;
+        const float at = finite_or_zero(m);
+        rest *= exp2_approx((m_rest - at) * c);
+        S = rest + (first ? exp2_approx((zi - at) * c) : 0.f);
+    }
+    auto joined = [&](int from) {          // over the lanes of a warp
+#pragma unroll
+        for (int o = from; o > 0; o >>= 1) {
+            const float m2 = __shfl_xor_sync(0xffffffffu, m, o), S2 = __shfl_xor_sync(0xffffffffu, S, o);
+            const float both = fmaxf(m, m2), at = finite_or_zero(both), f = exp2_approx((m - at) * c), f2 = exp2_approx((m2 - at) * c);
+            S = S * f + S2 * f2;
+            if (TAIL) rest = rest * f + __shfl_xor_sync(0xffffffffu, rest, o) * f2;
+            m = both;
         }
     };
-    int64_t r = blockIdx.x >> log_cluster;
-    float w = weight(r), w_next = weight(r + step), w_before = 0.f;
-    const uint32_t bar = smem_u32(&s_bar);
-    T *s_row = reinterpret_cast<T *>(s_raw);
-    uint32_t parity = 0;
-    if (tid == 0) {
-        s_abort = 0;
-        mbar_init(bar, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (reader) {
-        if (w != 0.f) {
-            const RowSegment<T, TO> seg = segment(r);
-            read_entries(a, r, s_entries[0]);
-            place_entries(a, seg.e0, seg.e1, seg.first, s_entries[0], s_hash);
-        }
-    }
-    if (cluster > 1) cluster_sync_all();        // (all blocks are there before one writes into another's memory)
+    joined(16);
+    __syncthreads();        // (s_warp was read)
+    if (lane == 0) s_warp[warp] = RowStats{m, S, rest};
     __syncthreads();
-    int slot = 0, turn = 0;
-    for (; r < a.rows; r += step, slot ^= 1, turn = (turn + 1) & 3) {
-        const float w_later = weight(r + 2 * step);
-        if (reader) {
-            // (after a wait that ran out nothing more is copied)
-            if (w != 0.f && *(volatile int *)&s_abort == 0) segment(r).copy(logits + r * a.ld, s_row, bar);
-            if (w != 0.f && cluster > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-            if (w_before != 0.f) finish(r - step, w_before, slot ^ 1, (turn + 3) & 3);
-            __syncwarp();
-            if (w_next != 0.f) {
-                const RowSegment<T, TO> seg = segment(r + step);
-                read_entries(a, r + step, s_entries[slot ^ 1]);
-                place_entries(a, seg.e0, seg.e1, seg.first, s_entries[slot ^ 1], s_hash);
-            }
-            if (w == 0.f && rank == 0 && lane == 0 && a.row_loss) a.row_loss[r] = 0.f;
-            if (w != 0.f && cluster > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        } else {
-            if (!alike) sg = segment(r);
-            TO *d = d_logits ? d_logits + r * a.ldd : nullptr;
-            if (w == 0.f) {         // the row takes no part
-                if (d) sg.zeros(d);
-            } else {
-                Entries &s = s_entries[slot];
-                mbar_wait(bar, parity, &s_abort);
-                parity ^= 1;
-                if (a.tail) {
-                    if (tid < a.k && s.place[tid] >= 0 && s.first[tid] == tid) {
-                        s.z[tid] = to_f32(s_row[s.place[tid]]);
-                        s_row[s.place[tid]] = from_f32<T>(-INFINITY);
-                    }
-                    compute_sync();
-                }
-                const int n = sg.groups;
-                Running<T, false, U> run;
-                auto at_group = [&](int v) { return *reinterpret_cast<const uint4 *>(s_row + v * N); };
-                int v = tid;
-                for (; v + (U - 1) * kCompute < n; v += U * kCompute) {
-                    Raw<T> x[U];
+    if (warp == 0) {
+        const RowStats st = lane < kWarps ? s_warp[lane] : RowStats{-INFINITY, 0.f, 0.f};
+        m = st.m;
+        S = st.S;
+        rest = st.W;
+        joined(kWarps / 2);
+        m = __shfl_sync(0xffffffffu, m, 0);
+        S = __shfl_sync(0xffffffffu, S, 0);
+        rest = __shfl_sync(0xffffffffu, rest, 0);
+        if (cluster > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        if (lane < cluster) {
+            const uint32_t to = map_to_cta(smem_u32(&s_seg[rank]), lane);
+            st_remote_u32(to, __float_as_uint(m));
+            st_remote_u32(to + 4, __float_as_uint(S));
+            st_remote_u32(to + 8, __float_as_uint(rest));
+            st_remote_f64(to + 16, loss);
+        }
+        __syncwarp();
+    } else if (cluster > 1) {
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    }
+    if (cluster > 1) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    else __syncthreads();
+    // the row: every eight lanes join the segments for themselves
+    Segment g{-INFINITY, 0.f, 0.f, 0.f, 0.0};
+    if ((lane & (kMaxCluster - 1)) < cluster) g = s_seg[lane & (kMaxCluster - 1)];
+    float at = g.m;
 #pragma unroll
-                    for (int u = 0; u < U; u++) x[u].w = at_group(v + u * kCompute);
-                    run.add(x, c);
-                }
-                if (v < n) {
-                    Raw<T> x[U];
+    for (int o = kMaxCluster / 2; o > 0; o >>= 1) at = fmaxf(at, __shfl_xor_sync(0xffffffffu, at, o));
+    at = finite_or_zero(at);
+    const float f = exp2_approx((g.m - at) * c);
+    float total = g.S * f;
+    rest = g.rest * f;
 #pragma unroll
-                    for (int u = 0; u < U; u++) {
-                        if (v + u * kCompute < n) x[u].w = at_group(v + u * kCompute);
-                        else x[u].fill(-INFINITY);
-                    }
-                    run.add(x, c);
-                }
-                float m = run.m, S;
-                {
-                    float lo, hi;
-                    run.S.get(lo, hi);
-                    S = lo + hi;
-                }
-                // over the lanes of a warp
-                auto joined = [&] {
-                    const float top = warp_max(m), at = finite_or_zero(top);
-                    S = warp_sum(S * exp2_approx((m - at) * c));
-                    m = top;
-                };
-                joined();
-                if (lane == 0) s_warp[warp] = RowStats{m, S, 0.f};
-                compute_sync();
-                if (warp == 0) {
-                    const RowStats st = lane < kComputeWarps ? s_warp[lane] : RowStats{-INFINITY, 0.f, 0.f};
-                    m = st.m;
-                    S = st.S;
-                    joined();
-                    float rest = S;
-                    if (a.tail) {       // the listed tokens come back
-                        float top = m;
-                        for (int i = lane; i < a.k; i += 32)
-                            if (s.place[i] >= 0 && s.first[i] == i) top = fmaxf(top, s.z[i]);
-                        top = warp_max(top);
-                        const float at = finite_or_zero(top);
-                        rest = S * exp2_approx((m - at) * c);
-                        float listed = 0.f;
-                        for (int i = lane; i < a.k; i += 32)
-                            if (s.place[i] >= 0 && s.first[i] == i) listed += exp2_approx((s.z[i] - at) * c);
-                        S = rest + warp_sum(listed);
-                        m = top;
-                    }
-                    if (lane < cluster) {
-                        const uint32_t to = map_to_cta(smem_u32(&s_seg[turn][rank]), lane);
-                        st_remote_u32(to, __float_as_uint(m));
-                        st_remote_u32(to + 4, __float_as_uint(S));
-                        st_remote_u32(to + 8, __float_as_uint(rest));
-                    }
-                } else if (warp == 1) {
-                    const double inv = (double)a.heat.hi + (double)a.heat.lo;
-                    double loss = 0.0;
-                    for (int i = lane; i < a.k; i += 32) {
-                        if (s.place[i] < 0) continue;
-                        if (!a.tail) s.z[i] = to_f32(s_row[s.place[i]]);
-                        const float q = s.q[i];
-                        if (q != 0.f) loss += (double)q * (s.logq[i] - (double)(a.tail ? s.z[s.first[i]] : s.z[i]) * inv);
-                    }
+    for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
+        total += __shfl_xor_sync(0xffffffffu, total, o);
+        if (TAIL) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+    }
+    const float rest_q = TAIL && rest != 0.f ? (float)rest_all : 0.f;      // (or there is no token for the tail)
+    const bool none = mass == 0.0 && rest_all == 0.0;                       // no entries: the row takes no part
+    const float of_p = total == 0.f ? 0.f : ((float)mass + rest_q) / total, scale = fmaf(w, a.heat.hi, w * a.heat.lo);
+    const float factor = scale * (of_p - (rest_q != 0.f ? rest_q / rest : 0.f));
+    if (rank == 0 && warp == kWarps - 1 && a.row_loss) {
+        double l = lane < kMaxCluster ? g.loss : 0.0;
 #pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-                    if (lane < cluster) st_remote_f64(map_to_cta(smem_u32(&s_seg[turn][rank].loss), lane), loss);
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        const double logS = total == 0.f ? 0.0 : (double)logf(total);
+        if (mass != 0.0) l += mass * ((double)at * inv + logS);
+        if (rest_q != 0.f) l += rest_all * (double)(logf(rest_q) - logf(rest / total));
+        if (lane == 0) a.row_loss[r] = none ? 0.f : (float)l;
+    }
+    if (none) {
+        zeros();
+        return;
+    }
+    if (!d) return;
+    // the gradient; a segment's part of the row and of the gradient may start differently in their 16 bytes
+    auto grad = [&](Pair x) {
+        float y[2];
+        ((x + Pair(-at, -at)) * Pair(c, c)).get(y[0], y[1]);
+        return Pair(exp2_approx(y[0]), exp2_approx(y[1])) * Pair(factor, factor);
+    };
+    const RowGroups<TO> out(d, a.vocab);
+    const int lead = row.off - out.off;         // element 0 of out's group 0 is element `lead` of the row's groups
+    // groups of the gradient that begin in the segment
+    auto from = [&](int group) { return group <= 0 ? 0 : group >= row.groups ? out.groups : (group * N - lead + NO - 1) / NO; };
+    const int v0 = from(g0), v1 = from(g1), x0 = max(v0, out.whole_begin()), x1 = min(v1, out.whole_end());
+    if (lead % N == 0) {
+        // (they are made of whole groups of the row)
+        constexpr int H = NO / N;
+        const T *src = row.base + lead;
+        for (int v = x0 + tid; v < x1; v += U * kThreads) {
+            Raw<T> x[U][H];
+#pragma unroll
+            for (int u = 0; u < U; u++)
+#pragma unroll
+                for (int h = 0; h < H; h++)
+                    if (v + u * kThreads < x1) x[u][h].w = *reinterpret_cast<const uint4 *>(src + (int64_t)(v + u * kThreads) * NO + h * N);
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                if (v + u * kThreads >= x1) continue;
+                Vec<TO> o;
+#pragma unroll
+                for (int h = 0; h < H; h++) {
+                    Pair p[N / 2];
+                    x[u][h].pairs(p);
+#pragma unroll
+                    for (int i = 0; i < N / 2; i++) grad(p[i]).get(o.v[h * N + 2 * i], o.v[h * N + 2 * i + 1]);
                 }
-                __syncwarp();
-                if (cluster > 1) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-                else compute_sync();
-                // the row: every eight lanes join the segments for themselves
-                Segment g{-INFINITY, 0.f, 0.f, 0.f, 0.0};
-                if ((lane & (kMaxCluster - 1)) < cluster) g = s_seg[turn][lane & (kMaxCluster - 1)];
-                float at = g.m;
-#pragma unroll
-                for (int o = kMaxCluster / 2; o > 0; o >>= 1) at = fmaxf(at, __shfl_xor_sync(0xffffffffu, at, o));
-                at = finite_or_zero(at);
-                const float f = exp2_approx((g.m - at) * c);
-                float total = g.S * f, rest = g.rest * f;
-#pragma unroll
-                for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
-                    total += __shfl_xor_sync(0xffffffffu, total, o);
-                    if (a.tail) rest += __shfl_xor_sync(0xffffffffu, rest, o);
-                }
-                const float mass = s.mass_f, rest_q = a.tail && rest != 0.f ? s.rest_f : 0.f;      // (or there is no token for the tail)
-                const bool none = mass == 0.f && s.rest_f == 0.f;                                   // no entries: the row takes no part
-                const float of_p = total == 0.f ? 0.f : (mass + rest_q) / total, scale = fmaf(w, a.heat.hi, w * a.heat.lo);
-                const float factor = scale * (of_p - (rest_q != 0.f ? rest_q / rest : 0.f));
-                if (tid == 0) {
-                    s_at[slot] = at;
-                    s_of_p[slot] = of_p;
-                    s_rest[slot] = rest;
-                    s_total[slot] = total;
-                }
-                if (d && none) {
-                    sg.zeros(d);
-                } else if (d) {
-                    auto grad = [&](Pair z) {
-                        float x[2];
-                        ((z + Pair(-at, -at)) * Pair(c, c)).get(x[0], x[1]);
-                        return Pair(exp2_approx(x[0]), exp2_approx(x[1])) * Pair(factor, factor);
-                    };
-                    TO *to = d + sg.e0;
-                    const RowGroups<TO> out(to, sg.e1 - sg.e0);
-                    const T *from = s_row + (sg.e0 - sg.first);
-                    const int lead = sg.e0 - sg.first - out.off;         // element 0 of out's group 0 lies at s_row + lead
-                    const int whole = out.whole_end();
-                    if (lead % N == 0) {
-                        // groups of the gradient are made of whole groups of the row
-                        for (int v = tid + out.whole_begin(); v < whole; v += kCompute) {
-                            Vec<TO> o;
-#pragma unroll
-                            for (int i = 0; i < NO; i += N) {
-                                Raw<T> x;
-                                x.w = *reinterpret_cast<const uint4 *>(s_row + lead + v * NO + i);
-                                Pair p[N / 2];
-                                x.pairs(p);
-#pragma unroll
-                                for (int j = 0; j < N / 2; j++) grad(p[j]).get(o.v[i + 2 * j], o.v[i + 2 * j + 1]);
-                            }
-                            o.store(to + out.first(v));
-                        }
-                    } else {
-                        for (int v = tid + out.whole_begin(); v < whole; v += kCompute) {
-                            Vec<TO> o;
-                            const int f = out.first(v);
-#pragma unroll
-                            for (int i = 0; i < NO; i += 2) grad(Pair(to_f32(from[f + i]), to_f32(from[f + i + 1]))).get(o.v[i], o.v[i + 1]);
-                            o.store(to + f);
-                        }
-                    }
-                    if (tid < 2 * NO) {         // the ragged ends (one group at each, which may be the same one)
-                        const int v = tid < NO ? 0 : out.groups - 1, f = out.first(v) + tid % NO;
-                        if (out.groups > 0 && !out.whole(v) && !(tid >= NO && v == 0) && f >= 0 && f < out.n) {
-                            float g, unused;
-                            grad(Pair(to_f32(from[f]), 0.f)).get(g, unused);
-                            to[f] = from_f32<TO>(g);
-                        }
-                    }
-                }
+                o.store(d + out.first(v + u * kThreads));
             }
         }
-        __syncthreads();
-        w_before = w;
-        w = w_next;
-        w_next = w_later;
+    } else {
+        for (int v = x0 + tid; v < x1; v += kThreads) {
+            Vec<TO> o;
+            const int first_element = out.first(v);
+#pragma unroll
+            for (int i = 0; i < NO; i += 2) grad(Pair(to_f32(z[first_element + i]), to_f32(z[first_element + i + 1]))).get(o.v[i], o.v[i + 1]);
+            o.store(d + first_element);
+        }
     }
-    if (reader && w_before != 0.f) finish(r - step, w_before, slot ^ 1, (turn + 3) & 3);
-    // (the last block of the first cluster looks through the ids)
-    if ((int)blockIdx.x == cluster - 1 && a.hdr)
+    for (int i = tid; i < 2 * NO; i += kThreads) {      // the row's ragged ends (one group at each, which may be the same one)
+        const int v = i < NO ? 0 : out.groups - 1, element = out.first(v) + i % NO;
+        if (v < v0 || v >= v1 || out.whole(v) || (i >= NO && v == 0) || element < 0 || element >= a.vocab) continue;
+        float y, unused;
+        grad(Pair(to_f32(z[element]), 0.f)).get(y, unused);
+        d[element] = from_f32<TO>(y);
+    }
+    // listed tokens: by the block that wrote the group they lie in
+    const int mine = id >= 0 ? (id + out.off) / NO : -1;
+    bool writes = mine >= v0 && mine < v1;
+    if (lead % N == 0 && NO == N) writes = first;
+    float z_mine = zi;
+    if (!(lead % N == 0 && NO == N) && writes) {
+        // (its logit and its other entries may belong to another block)
+        z_mine = to_f32(z[id]);
+        q_all = 0.f;
+        for (int j = a.k - 1; j >= 0; j--)
+            if (s_id[j] == id) {
+                writes = j == tid;
+                q_all += s_q[j];
+            }
+    }
+    __syncthreads();
+    if (writes) d[id] = from_f32<TO>(scale * fmaf(of_p, exp2_approx((z_mine - at) * c), -q_all));
+}
+
+template <typename T, typename TO, bool TAIL>
+__global__ void __launch_bounds__(kThreads, 4) distill_kernel(const T *logits, TO *d_logits, DistillArgs a, int cluster) {
+    pdl_enter();
+    if (gated_off(a.gate)) return;
+    distill_row<T, TO, TAIL>(logits, d_logits, a, cluster);
+    // (the last block of the first row: where a row has several, another one writes the results)
+    if ((int)blockIdx.x == cluster - 1 && a.hdr && a.scan)
         report_first(a.ids, a.rows * a.k, a.k, a.hdr, [&](int64_t id, int64_t i) {
             return (id < -1 || id >= a.vocab) && (!a.weight || a.weight[i / a.k] != 0.f);
         });
 }
 
-// Blocks to a row: as few as hold it with two blocks an SM, and more where there are SMs for them and each thread keeps a
-// group.  Rows that eight such blocks do not hold have one block an SM.
-constexpr int kShared = 100 << 10, kSharedLong = 208 << 10;
+// Blocks to a row: so many that the rows under way (four blocks an SM) stay below kUnderWay bytes, which L2 has to hold until
+// they are read again, beside their gradients; more where rows are few, none with less than two groups a thread.
+constexpr int64_t kUnderWay = 64 << 20;
 template <typename T>
 int row_cluster(int64_t rows, int64_t vocab) {
     int c = 1;
-    while (c < kMaxCluster && (vocab * (int64_t)sizeof(T) + 32 * c > (int64_t)c * kShared ||
-                               (rows * 2 * c <= 148 && vocab / (2 * c) >= kCompute * Vec<T>::N)))
+    while (c < kMaxCluster && vocab / (2 * c) >= 2 * kThreads * Vec<T>::N &&
+           (148 * 4 / c * vocab * (int64_t)sizeof(T) > kUnderWay || rows * c < 2 * 148))
         c *= 2;
     return c;
 }
 
-// Clusters of c blocks that the GPU holds at once.
-template <typename F>
-int resident_clusters(F kernel, int c, int smem) {
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3((unsigned)(296 / c * c));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)smem;
-    cudaLaunchAttribute attr[1];
-    memset(attr, 0, sizeof(attr));
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)c;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (!cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedLong)) ||
-        !cuda_ok(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg)))
-        return 0;
-    return n;
-}
-
 template <typename T, typename TO>
-int launch(const T *logits, TO *d_logits, const DistillArgs &a, cudaStream_t st) {
+int launch(const T *logits, TO *d_logits, const DistillArgs &a, bool tail, cudaStream_t st) {
     const int c = row_cluster<T>(a.rows, a.vocab);
     const int64_t groups = (a.vocab + Vec<T>::N - 1) / Vec<T>::N + 1;
-    const int smem = (groups + c - 1) / c * 16 <= kShared ? kShared : kSharedLong;
-    static PerDevice clusters[2][4];
-    auto kernel = distill_kernel<T, TO>;
-    int log_c = 0;
-    while (1 << log_c < c) log_c++;
-    const int most = clusters[smem == kSharedLong][log_c].get([&] { return resident_clusters(kernel, c, smem); });
-    if (most < 1) return STREAMBP_E_CUDA;
-    // (rows are dealt out evenly)
-    const int64_t turns = (a.rows + most - 1) / most, n = (a.rows + turns - 1) / turns;
-    return launch_clusters(kernel, dim3((unsigned)(n * c)), kThreads, smem, c, 1, st, logits, d_logits, a, log_c);
+    const int smem = tail ? (int)(((groups + c - 1) / c + 31) / 32 * 4) : 0;
+    auto kernel = tail ? distill_kernel<T, TO, true> : distill_kernel<T, TO, false>;
+    return launch_clusters(kernel, dim3((unsigned)(a.rows * c)), kThreads, smem, c, 1, st, logits, d_logits, a, c);
 }
 }  // namespace
 
@@ -531,11 +429,12 @@ template <typename T, typename TO>
 int distill_topk(const T *logits, int64_t ld, int64_t rows, int64_t vocab, const DistillRows &ds, TO *d_logits, int64_t ldd,
                  WsHeader *hdr, cudaStream_t st) {
     if (rows <= 0) return STREAMBP_OK;
-    const DistillArgs a{ds.ids, ds.values, ds.weight, ds.row_loss, rows, ld, ldd, (int)vocab, ds.k, ds.tail ? 1 : 0,
-                        make_heat(ds.temperature), hdr, call_state().gate};
-    return launch<T, TO>(logits, d_logits, a, st);
+    const bool scan = rows * ds.k <= kScanMost;
+    if (hdr && !scan) SBP_TRY(clear_status_launch(hdr, st));
+    const DistillArgs a{ds.ids, ds.values, ds.weight, ds.row_loss, rows, ld, ldd, (int)vocab, ds.k,
+                        make_heat(ds.temperature), hdr, scan, call_state().gate};
+    return launch<T, TO>(logits, d_logits, a, ds.tail, st);
 }
-int distill_take_fault() { return take_fault_local(); }
 template int distill_topk<float, float>(const float *, int64_t, int64_t, int64_t, const DistillRows &, float *, int64_t, WsHeader *,
                                         cudaStream_t);
 template int distill_topk<bf16, bf16>(const bf16 *, int64_t, int64_t, int64_t, const DistillRows &, bf16 *, int64_t, WsHeader *,

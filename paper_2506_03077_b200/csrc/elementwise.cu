@@ -533,6 +533,15 @@ int ws_guard_selftest(void *ws, size_t bytes, int overrun, cudaStream_t st) {
     return ws_guards_check(ws, a.guards, hdr, st);
 }
 
+__global__ void clear_status_kernel(WsHeader *hdr) {
+    pdl_enter();
+    clear_status(hdr);
+}
+int clear_status_launch(WsHeader *hdr, cudaStream_t st) {
+    SBP_LAUNCH(clear_status_kernel, 1, 1, 0, st, hdr);
+    return STREAMBP_OK;
+}
+
 int fill_zero(void *p, size_t bytes, cudaStream_t st) {
     if (bytes == 0 || p == nullptr) return STREAMBP_OK;
     return cuda_ok(cudaMemsetAsync(p, 0, bytes, st)) ? STREAMBP_OK : STREAMBP_E_CUDA;

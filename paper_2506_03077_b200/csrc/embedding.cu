@@ -25,18 +25,20 @@ struct LookupArgs {
     int d;
     float scale;
     WsHeader *hdr;
+    bool scan;              // one block looks for ids outside the table, else each token's warp
 };
 constexpr int kLookupGroups = 4;
 template <typename T, bool GROUPED>
 __global__ void __launch_bounds__(kThreads) embedding_lookup_kernel(LookupArgs<T> a) {
     pdl_enter();
     constexpr int N = GROUPED ? Vec<T>::N : 1;
-    if (blockIdx.x == 0 && blockIdx.y == 0)
+    if (blockIdx.x == 0 && blockIdx.y == 0 && a.scan)
         report_first(a.ids, a.n, 1, a.hdr, [&](int64_t id, int64_t) { return id != a.padding && (id < 0 || id >= a.vocab); });
     const int64_t t = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
     if (t >= a.n) return;
     const int64_t id = a.ids[t];
     const bool zero = id == a.padding || id < 0 || id >= a.vocab;
+    if (zero && !a.scan && id != a.padding && blockIdx.y == 0 && (threadIdx.x & 31) == 0) set_status(a.hdr, STREAMBP_E_BAD_LABEL, (int)t);
     const T *from = a.table + (zero ? 0 : id) * a.ld;
     T *to = a.out + t * a.ldo;
     const int c0 = (blockIdx.y * kLookupGroups * 32 + (threadIdx.x & 31)) * N;
@@ -548,7 +550,9 @@ int launch_sort(const SortArgs &a, int cluster, int64_t zero_blocks, cudaStream_
 template <typename T>
 int embedding_fwd(const T *table, int64_t ld, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, float scale,
                   int64_t padding, T *out, int64_t ldo, WsHeader *hdr, cudaStream_t st) {
-    const LookupArgs<T> a{table, ids, out, n, vocab, ld, ldo, padding, (int)d, scale, hdr};
+    const bool scan = n <= kScanMost || d * (int64_t)sizeof(T) >= kScanRow;
+    if (!scan) SBP_TRY(clear_status_launch(hdr, st));
+    const LookupArgs<T> a{table, ids, out, n, vocab, ld, ldo, padding, (int)d, scale, hdr, scan};
     constexpr int N = Vec<T>::N;
     const bool grouped = d % N == 0 && ld % N == 0 && ldo % N == 0 && reinterpret_cast<uintptr_t>(table) % 16 == 0 &&
                          reinterpret_cast<uintptr_t>(out) % 16 == 0;

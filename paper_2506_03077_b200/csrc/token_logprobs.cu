@@ -183,7 +183,8 @@ struct ScoreArgs {
     Heat heat;
     float *logp, *lse, *entropy, *top_logp;     // all optional
     int64_t *top_ids;
-    WsHeader *hdr;              // optional: the first token outside the vocabulary goes there
+    WsHeader *hdr;              // optional: a token outside the vocabulary goes there
+    bool scan;                  // found by one block, else by each row's
     const int *gate;
 };
 
@@ -202,6 +203,7 @@ __device__ __forceinline__ void score_row(const T *__restrict__ logits, const Sc
     if (a.tokens && (y == a.ignore || y < 0 || y >= a.vocab)) {
         if (rank == 0) {
             if (tid == 0) {
+                if (y != a.ignore && a.hdr && !a.scan) set_status(a.hdr, STREAMBP_E_BAD_LABEL, (int)r);
                 if (a.logp) a.logp[r] = 0.f;
                 if (a.lse) a.lse[r] = 0.f;
                 if (a.entropy) a.entropy[r] = 0.f;
@@ -223,7 +225,7 @@ __device__ __forceinline__ void score_row(const T *__restrict__ logits, const Sc
     const int rounds = (w1 - w0 + THREADS - 1) / THREADS, per_part = max(1, ((rounds + kParts - 1) / kParts + U - 1) / U) * U;
     const float c = a.heat.hi * kLog2e;
     const float zy = rank == 0 && tid == 0 && a.logp ? to_f32(logits[r * a.ld + y]) : 0.f;
-    Running<T, ENT, U> run;
+    Running<T, ENT> run;
     for (int p = 0; p < (TOP ? kParts : 1); p++) {
         run.largest = -INFINITY;
         const int end = TOP ? min(w1, w0 + (p + 1) * per_part * THREADS) : w1;
@@ -370,7 +372,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T *__rest
     if (gated_off(a.gate)) return;
     score_row<T, TOP, ENT, THREADS>(logits, a, cluster);
     // (the last block of the first row: where a row has several, another one writes the results)
-    if ((int)blockIdx.x == cluster - 1 && a.hdr)
+    if ((int)blockIdx.x == cluster - 1 && a.hdr && a.scan)
         report_first(a.tokens, a.tokens ? a.rows : 0, 1, a.hdr,
                      [&](int64_t y, int64_t) { return y != a.ignore && (y < 0 || y >= a.vocab); });
 }
@@ -498,7 +500,9 @@ template <typename T>
 int token_logprobs(const T *logits, int64_t ld, int64_t rows, int64_t vocab, const int64_t *tokens, int64_t ignore,
                    float temperature, int k, float *logp, float *lse, float *entropy, float *top_logp, int64_t *top_ids,
                    WsHeader *hdr, cudaStream_t st) {
-    const ScoreArgs a{tokens, ignore, rows, ld, (int)vocab, k, make_heat(temperature), logp, lse, entropy, top_logp, top_ids, hdr,
+    const bool scan = rows <= kScanMost || vocab * (int64_t)sizeof(T) >= kScanRow;
+    if (hdr && !scan) SBP_TRY(clear_status_launch(hdr, st));
+    const ScoreArgs a{tokens, ignore, rows, ld, (int)vocab, k, make_heat(temperature), logp, lse, entropy, top_logp, top_ids, hdr, scan,
                       call_state().gate};
     if (k) return entropy ? launch_score<T, true, true>(logits, a, st) : launch_score<T, true, false>(logits, a, st);
     return entropy ? launch_score<T, false, true>(logits, a, st) : launch_score<T, false, false>(logits, a, st);

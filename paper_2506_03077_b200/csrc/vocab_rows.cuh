@@ -5,8 +5,11 @@
 
 namespace sbp {
 
-// One block's look through `count` ids, several loads in flight: the first i for which bad(ids[i], i) goes into the header as
-// E_BAD_LABEL with detail i / per, or OK.  (One block does it, so that a call needs no launch to clear its status.)
+// Up to kScanMost ids one block of a call looks through, which saves a launch that clears the status; more are looked at by the
+// blocks that use them, behind such a launch (clear_status_launch).
+constexpr int64_t kScanMost = 1 << 14, kScanRow = 4096;     // (however many, where each stands for so many bytes of a row: then the rest of the call takes longer)
+// That block's look through `count` ids, several loads in flight: the first i for which bad(ids[i], i) goes into the header as
+// E_BAD_LABEL with detail i / per, or OK.
 template <typename F>
 __device__ __forceinline__ void report_first(const int64_t *__restrict__ ids, int64_t count, int64_t per, WsHeader *hdr, F bad) {
     __shared__ unsigned long long s_first;
@@ -248,11 +251,11 @@ __device__ __forceinline__ void add_deep_batch(const Raw<T> (&x)[U], float c, Pa
 }
 
 // A thread's running maximum and sums.
-template <typename T, bool ENT, int U>
+template <typename T, bool ENT>
 struct Running {
     float m = -INFINITY, largest = -INFINITY;        // of all, and of the part
     Pair S = Pair(0.f, 0.f), W = Pair(0.f, 0.f);
-    __device__ __forceinline__ void add(const Raw<T> (&x)[U], float c) {
+    template <int U> __device__ __forceinline__ void add(const Raw<T> (&x)[U], float c) {
         float mx = x[0].largest(), mn = x[0].smallest();
 #pragma unroll
         for (int u = 1; u < U; u++) {

@@ -183,3 +183,15 @@ def test_gradient_by_differences():
             down[:, j] -= h
             slope = (reference(up, ids, values, None, 1.5, tail)[0] - reference(down, ids, values, None, 1.5, tail)[0]) / (2 * h)
             assert ((d[:, j].double() - slope).abs() <= 1e-4).all()          # h^2 / 6 of third derivatives below 1
+
+
+def test_many_rows_with_ids_outside():
+    """more than one block looks through"""
+    z = logits_of(1000, 300, BF)
+    ids, values = teacher(z, 20, 1.0, True)
+    check(z, ids, values, None, 1.0, True)
+    ids[999, 3] = 300
+    distill(z, ids, values, tail=True, status=B.E_BAD_LABEL)
+    w = torch.ones(1000, device="cuda")
+    w[999] = 0
+    distill(z, ids, values, w, tail=True)

@@ -108,3 +108,16 @@ def test_wide_key_range():
     B.embedding_backward(dy, ids, table, ws, accumulate=True)
     want = torch.zeros(V, 1, dtype=torch.float64, device="cuda").index_add(0, ids, dy.double())
     assert ((table.double() - want).abs() <= 2e-5 * 100).all()
+
+
+def test_lookup_of_many_tokens_with_ids_outside():
+    """more than one block looks through"""
+    n = 20000
+    table, ids = matrix(100, 8, BF), torch.randint(100, (n,), device="cuda")
+    out = lookup(table, ids, torch.empty(n, 8, dtype=BF, device="cuda"))
+    assert torch.equal(out, table[ids])
+    ids[n - 1] = 100
+    out = lookup(table, ids, out, status=B.E_BAD_LABEL)
+    assert torch.equal(out[:-1], table[ids[:-1]]) and (out[-1] == 0).all()
+    ids[n - 1] = -1
+    lookup(table, ids, out)

@@ -209,3 +209,15 @@ def test_rows_behind_and_between_are_left(dtype=BF):
     fw = score(z, t)
     B.token_logprobs_backward(z, t, fw["lse"], None, buf[2:8, 11:911], d_logp=torch.ones(6, device="cuda"))
     assert (buf[:2] == 3).all() and (buf[8:] == 3).all() and (buf[:, :11] == 3).all() and (buf[:, 911:] == 3).all()
+
+
+def test_many_rows_with_tokens_outside():
+    """more than one block looks through"""
+    z = logits_of(20000, 40, BF)
+    t = tokens_of(20000, 40, ignored=3)
+    check(z, t, 3)
+    t[19999] = 40
+    got = score(z, t, 3, status=B.E_BAD_LABEL)
+    assert got["logp"][19999] == 0 and (got["top_ids"][19999] == -1).all()
+    t[19999] = 5
+    score(z, t, 3)
