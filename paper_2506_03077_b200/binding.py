@@ -928,9 +928,12 @@ def _vectors(what: str, dev: int, shape: tuple, **tensors) -> list:
     """Addresses of optional contiguous tensors of one shape: name=(tensor, dtype)."""
     out = []
     for name, (t, dtype) in tensors.items():
-        if t is not None and (t.get_device() != dev or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+        if t is None:
+            out.append(None)
+        elif t.get_device() == dev and t.dtype == dtype and t.shape == shape and t.is_contiguous():
+            out.append(t.data_ptr())
+        else:
             raise ValueError(f"{what}: {name} is a contiguous {dtype} tensor {shape} on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        out.append(None if t is None else t.data_ptr())
     return out
 
 

@@ -429,7 +429,7 @@ size_t embedding_scratch(int64_t n, int64_t vocab, int64_t d, void *base, Embedd
         out->tokens[1] = out->tokens[0];
     }
     out->counts = a.take<int>(embedding_counts(out->plan));
-    out->owners = a.take<int>((size_t)out->plan.chunks + 1);
+    out->owners = a.take<int>(4 * ((size_t)out->plan.chunks + 1));
     out->partials = a.take<float>((size_t)out->plan.chunks * 2 * (size_t)out->plan.partial_width);
     out->guards = a.guards;
     return a.size();

@@ -325,9 +325,9 @@ struct RunArgs {
     const int *keys, *tokens;       // sorted
     const T *dy;
     float *d_table, *partials;      // partials: [chunks][2][dp]; 0: of a run that began before, 1: of one that goes on (a chunk inside one run: 0)
-    int *owners;                    // [0] how many, then the chunks in which a run begins that goes on
+    int *owners;                    // [0] how many runs go on behind the chunk they begin in; from [4] on their chunk, last chunk and key, four ints each
     int64_t ldy;
-    int n, chunk, d, dp, vocab, accumulate;
+    int n, chunk, chunks, d, dp, vocab, accumulate;
     float scale;
 };
 constexpr int kMaxChunk = 128, kRunThreads = 256;
@@ -345,22 +345,13 @@ __global__ void __launch_bounds__(kRunThreads) embedding_runs_kernel(RunArgs<T> 
     }
     for (int i = threadIdx.x; i < len; i += blockDim.x) s_tok[i] = a.tokens[i0 + i];
     __syncthreads();
-    if (blockIdx.y == 0 && threadIdx.x == 0) {
-        const int key = s_key[len];
-        bool began = false;         // in an earlier chunk
-        if (s_key[len + 1] == key && key < a.vocab) {
-            began = s_key[1] == key && s_key[0] == key;
-            if (!began) a.owners[1 + atomicAdd(a.owners, 1)] = blockIdx.x;      // (their order does not matter)
-        }
-    }
     const int c = (blockIdx.y * blockDim.x + threadIdx.x) * N;
-    if (c >= a.d) return;
     float sum[N];
 #pragma unroll
     for (int e = 0; e < N; e++) sum[e] = 0.f;
     bool begun = s_key[0] == s_key[1];          // the run began in an earlier chunk
     constexpr int U = 4;
-    for (int i = 0; i < len && s_key[i + 1] < a.vocab; i += U) {
+    for (int i = 0; i < len && s_key[i + 1] < a.vocab && c < a.d; i += U) {
         // (values stay as they came until all are on the way)
         typename Piece<T, N>::In x[U];
         typename Piece<float, N>::In old[U][sizeof(float) / sizeof(T)];
@@ -415,15 +406,37 @@ __global__ void __launch_bounds__(kRunThreads) embedding_runs_kernel(RunArgs<T> 
             for (int e = 0; e < N; e++) sum[e] = 0.f;
         }
     }
+    __syncwarp();
+    if (blockIdx.y == 0 && threadIdx.x < 32) {
+        const int key = s_key[len], lane = threadIdx.x;
+        // a run that goes on, and did not begin in an earlier chunk
+        if (s_key[len + 1] == key && key < a.vocab && !(s_key[1] == key && s_key[0] == key)) {
+            // the last chunk that begins with this key: 32 guesses at a time, the next 32 chunks first
+            auto same = [&](int64_t q) { return q < a.chunks && a.keys[q * a.chunk] == key; };
+            int last = blockIdx.x + 1;          // begins with it
+            unsigned yes = __ballot_sync(0xffffffffu, same(last + 1 + lane));
+            last += yes == 0xffffffffu ? 32 : __ffs(~yes) - 1;
+            if (yes == 0xffffffffu) {
+                int64_t step = 1;
+                while (step * 32 < a.chunks) step *= 32;
+                for (; step >= 1; step /= 32) {
+                    yes = __ballot_sync(0xffffffffu, same(last + (lane + 1) * step));
+                    last += (int)((yes == 0xffffffffu ? 32 : __ffs(~yes) - 1) * step);
+                }
+            }
+            // (their order does not matter)
+            if (lane == 0) reinterpret_cast<int4 *>(a.owners)[1 + atomicAdd(a.owners, 1)] = make_int4(blockIdx.x, last, key, 0);
+        }
+    }
 }
 
 // The partial sums of a run that crosses chunks, 128 columns at a time (an item): a warp adds those of a run of up to kShort
 // chunks, a block's warps a section each of a longer one's, and the sections are added in order.
 struct JoinArgs {
-    const int *keys, *owners;
+    const int *owners;
     const float *partials;
     float *d_table;
-    int n, chunk, chunks, d, dp, vocab, accumulate;
+    int d, dp, accumulate;
     float scale;
 };
 constexpr int kShort = 128;
@@ -450,20 +463,10 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(JoinArgs a) {
                     if (col + e < a.d) old[e] = t[e];
         };
         if (own) {
-            b = a.owners[1 + it / strips];
-            key = a.keys[(int64_t)(b + 1) * a.chunk - 1];
-            // the last chunk that begins with this key: 32 guesses at a time, the next 32 chunks first
-            auto same = [&](int64_t q) { return q < a.chunks && a.keys[q * a.chunk] == key; };
-            unsigned yes = __ballot_sync(0xffffffffu, same(b + 2 + lane));
-            last = b + 1 + (yes == 0xffffffffu ? 32 : __ffs(~yes) - 1);
-            if (yes == 0xffffffffu) {
-                int64_t step = 1;
-                while (step * 32 < a.chunks) step *= 32;
-                for (; step >= 1; step /= 32) {
-                    yes = __ballot_sync(0xffffffffu, same(last + (lane + 1) * step));
-                    last += (int)((yes == 0xffffffffu ? 32 : __ffs(~yes) - 1) * step);
-                }
-            }
+            const int4 o = reinterpret_cast<const int4 *>(a.owners)[1 + it / strips];
+            b = o.x;
+            last = o.y;
+            key = o.z;
             if (last - b <= kShort) before(key, c);
         }
         // chunk from's sum of its last run and the first runs of chunks q0 .. q1 - 1
@@ -525,9 +528,9 @@ EmbeddingPlan embedding_plan(int64_t n, int64_t vocab, int64_t d) {
     const int64_t per = (n + 63) / 64;
     p.tile = (int)((per + kBins - 1) / kBins * kBins);
     p.tiles = (int)((n + p.tile - 1) / p.tile);
-    // chunks of the sorted list: about sixteen blocks of 256 threads with 8 columns each an SM
+    // chunks of the sorted list: about eight blocks of 256 threads with 8 columns each an SM
     const int64_t strips = (d + 2047) / 2048;
-    p.chunk = (int)std::min<int64_t>(kMaxChunk, std::max<int64_t>(8, n * strips / (148 * 16)));
+    p.chunk = (int)std::min<int64_t>(kMaxChunk, std::max<int64_t>(8, n * strips / (148 * 8)));
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
     p.partial_width = (int)((d + 3) / 4 * 4);
     return p;
@@ -589,7 +592,7 @@ int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64
         }
         done = (p.passes - 1) & 1;
     }
-    const RunArgs<T> r{keys[done], tokens[done], dy, d_table, partials, owners, ldy, (int)n, p.chunk, (int)d, p.partial_width, (int)vocab,
+    const RunArgs<T> r{keys[done], tokens[done], dy, d_table, partials, owners, ldy, (int)n, p.chunk, p.chunks, (int)d, p.partial_width, (int)vocab,
                        accumulate ? 1 : 0, scale};
     constexpr int N = Vec<T>::N;
     const bool grouped = d % N == 0 && ldy % N == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0;
@@ -598,8 +601,7 @@ int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64
     if (grouped) SBP_LAUNCH((embedding_runs_kernel<T, N>), dim3((unsigned)p.chunks, (unsigned)strips), threads, 0, st, r);
     else SBP_LAUNCH((embedding_runs_kernel<T, 1>), dim3((unsigned)p.chunks, (unsigned)strips), threads, 0, st, r);
     if (p.chunks == 1) return STREAMBP_OK;
-    const JoinArgs j{keys[done], owners, partials, d_table, (int)n, p.chunk, p.chunks, (int)d, p.partial_width, (int)vocab,
-                     accumulate ? 1 : 0, scale};
+    const JoinArgs j{owners, partials, d_table, (int)d, p.partial_width, accumulate ? 1 : 0, scale};
     const int64_t most = (int64_t)p.chunks * ((d + 127) / 128);
     SBP_LAUNCH(embedding_join_kernel, (unsigned)std::min<int64_t>(most, 148 * 8), 256, 0, st, j);
     return STREAMBP_OK;

@@ -26,11 +26,16 @@ template <typename T, int N> struct Pack {
 #pragma unroll
         for (int i = 0; i < N; i++) x[i] = a.v[i];
     }
-    static __device__ __forceinline__ void store(T *p, const float (&x)[N]) {
+    __device__ __forceinline__ void set(const float (&x)[N]) {
         Vec<T> a;
 #pragma unroll
         for (int i = 0; i < N; i++) a.v[i] = x[i];
-        a.store(p);
+        a.store(reinterpret_cast<T *>(&w));
+    }
+    static __device__ __forceinline__ void store(T *p, const float (&x)[N]) {
+        Pack q;
+        q.set(x);
+        *reinterpret_cast<uint4 *>(p) = q.w;
     }
 };
 template <typename T> struct Pack<T, 1> {
@@ -39,6 +44,68 @@ template <typename T> struct Pack<T, 1> {
     __device__ __forceinline__ void clear() { w = from_f32<T>(0.f); }
     __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = to_f32(w); }
     static __device__ __forceinline__ void store(T *p, const float (&x)[1]) { *p = from_f32<T>(x[0]); }
+};
+
+// Rows that start anywhere, in columns of 16 bytes: a thread's N columns lie across two aligned groups of memory, which are read
+// whole and shifted into place; what it stores is shifted back, each aligned group made of its own columns and its lower
+// neighbour's.  Groups that leave the row, and where two warps meet, go element by element.
+template <typename T> struct AnyRow {
+    static constexpr int N = Vec<T>::N;
+    T *p;
+    int off, d;         // elements between the aligned group that holds column 0 and column 0
+    __device__ __forceinline__ AnyRow(const T *row, int d_) : p(const_cast<T *>(row)), off((int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T))), d(d_) {}
+    // elements s .. s + N - 1 of the 2 N in a and b
+    static __device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, int s) {
+        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        const int words = sizeof(T) == 2 ? s >> 1 : s;
+        if (words & 2) {
+#pragma unroll
+            for (int i = 0; i < 6; i++) w[i] = w[i + 2];
+        }
+        if (words & 1) {
+#pragma unroll
+            for (int i = 0; i < 7; i++) w[i] = w[i + 1];
+        }
+        if (sizeof(T) == 2 && (s & 1)) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // columns c .. c + N - 1 (c a multiple of N), 0 behind the last
+    __device__ __forceinline__ uint4 load(int c) const {
+        const T *g = p + (c - off);
+        if (off == 0 && c + N <= d) return *reinterpret_cast<const uint4 *>(g);
+        if (c >= N && c - off + 2 * N <= d) return shifted(*reinterpret_cast<const uint4 *>(g), *reinterpret_cast<const uint4 *>(g + N), off);
+        T t[N];
+#pragma unroll
+        for (int i = 0; i < N; i++) t[i] = c + i < d ? p[c + i] : from_f32<T>(0.f);
+        uint4 w;
+        memcpy(&w, t, 16);
+        return w;
+    }
+    // by whole warps whose lanes hold neighbouring columns (c beyond d: none)
+    __device__ __forceinline__ void store(int c, const uint4 &own) const {
+        const int lane = threadIdx.x & 31;
+        uint4 below;
+        below.x = __shfl_up_sync(0xffffffffu, own.x, 1);
+        below.y = __shfl_up_sync(0xffffffffu, own.y, 1);
+        below.z = __shfl_up_sync(0xffffffffu, own.z, 1);
+        below.w = __shfl_up_sync(0xffffffffu, own.w, 1);
+        if (c >= d) return;
+        if (off == 0 && c + N <= d) {
+            *reinterpret_cast<uint4 *>(p + c) = own;
+            return;
+        }
+        const bool together = off != 0 && lane > 0 && c + N <= d;              // with the lower neighbour's last `off`
+        if (together) *reinterpret_cast<uint4 *>(p + (c - off)) = shifted(below, own, N - off);
+        const int begin = together ? N - off : 0, end = off != 0 && lane < 31 && c + 2 * N <= d ? N - off : N;
+        T t[N];
+        memcpy(t, &own, 16);
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            if (i >= begin && i < end && c + i < d) p[c + i] = t[i];
+    }
 };
 
 // Sums of two values over the threads of a row: one warp (no barrier), or the block (one barrier; `slot` alternates).
@@ -70,8 +137,8 @@ struct NormArgs {
     float eps;
 };
 
-// WARP: a warp to a row, else a block
-template <typename T, int N, int NV, bool WARP>
+// WARP: a warp to a row, else a block.  ANY: rows that start anywhere.
+template <typename T, int N, int NV, bool WARP, bool ANY>
 __global__ void __launch_bounds__(kMaxThreads) norm_fwd_kernel(NormArgs<T> a) {
     pdl_enter();
     __shared__ float2 red[2][kMaxWarps];
@@ -79,11 +146,15 @@ __global__ void __launch_bounds__(kMaxThreads) norm_fwd_kernel(NormArgs<T> a) {
     const int64_t r = WARP ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
     if (r >= a.rows) return;
     const T *x = a.x + r * a.ldx;
+    auto fetch = [&](Pack<T, N> &q, const T *row, int c) {
+        if constexpr (ANY) q.w = AnyRow<T>(row, a.d).load(c);
+        else q.load(row + c);
+    };
     Pack<T, N> p[NV];
 #pragma unroll
     for (int j = 0; j < NV; j++) {
         const int c = (lane + j * lanes) * N;
-        if (c < a.d) p[j].load(x + c);
+        if (c < a.d) fetch(p[j], x, c);
         else p[j].clear();
     }
     float s = 0.f, v[N];
@@ -97,10 +168,12 @@ __global__ void __launch_bounds__(kMaxThreads) norm_fwd_kernel(NormArgs<T> a) {
     s = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; j++) {
-        if ((lane + j * lanes) * N >= a.d) continue;
+        const int c = (lane + j * lanes) * N;
+        if (c >= a.d) continue;
         p[j].get(v);
 #pragma unroll
-        for (int i = 0; i < N; i++) s = fmaf(v[i] - mean, v[i] - mean, s);
+        for (int i = 0; i < N; i++)
+            if (!ANY || c + i < a.d) s = fmaf(v[i] - mean, v[i] - mean, s);
     }
     const float rstd = rsqrtf(row_sum<WARP>(s, 0.f, red, 1).x / (float)a.d + a.eps);
     if (lane == 0) {
@@ -110,25 +183,30 @@ __global__ void __launch_bounds__(kMaxThreads) norm_fwd_kernel(NormArgs<T> a) {
 #pragma unroll
     for (int j = 0; j < NV; j++) {
         const int c = (lane + j * lanes) * N;
-        if (c >= a.d) continue;
+        if (!ANY && c >= a.d) continue;
         float g[N], b[N];
         Pack<T, N> q;
         p[j].get(v);
 #pragma unroll
         for (int i = 0; i < N; i++) v[i] = (v[i] - mean) * rstd;
-        if (a.gain) {
-            q.load(a.gain + c);
+        if (c < a.d && a.gain) {
+            fetch(q, a.gain, c);
             q.get(g);
 #pragma unroll
             for (int i = 0; i < N; i++) v[i] *= g[i];
         }
-        if (a.bias) {
-            q.load(a.bias + c);
+        if (c < a.d && a.bias) {
+            fetch(q, a.bias, c);
             q.get(b);
 #pragma unroll
             for (int i = 0; i < N; i++) v[i] += b[i];
         }
-        Pack<T, N>::store(a.y + r * a.ldy + c, v);
+        if constexpr (ANY) {
+            q.set(v);
+            AnyRow<T>(a.y + r * a.ldy, a.d).store(c, q.w);
+        } else {
+            Pack<T, N>::store(a.y + r * a.ldy + c, v);
+        }
     }
 }
 
@@ -525,16 +603,25 @@ bool grouped(const void *p, int64_t ld) {
 }
 constexpr int64_t kWide = 8192;     // columns above which rows are not held in registers
 
-template <typename T, int N, int NV>
+template <typename T, int NV, bool ANY>
 int launch_fwd(const NormArgs<T> &a, cudaStream_t st) {
+    constexpr int N = Vec<T>::N;
     const int groups = (a.d + N - 1) / N;
     if (groups <= 32 * NV) {
-        SBP_LAUNCH((norm_fwd_kernel<T, N, NV, true>), (unsigned)((a.rows + 7) / 8), 256, 0, st, a);
+        SBP_LAUNCH((norm_fwd_kernel<T, N, NV, true, ANY>), (unsigned)((a.rows + 7) / 8), 256, 0, st, a);
     } else {
         const int threads = ((groups + NV - 1) / NV + 31) / 32 * 32;
-        SBP_LAUNCH((norm_fwd_kernel<T, N, NV, false>), (unsigned)a.rows, threads, 0, st, a);
+        SBP_LAUNCH((norm_fwd_kernel<T, N, NV, false, ANY>), (unsigned)a.rows, threads, 0, st, a);
     }
     return STREAMBP_OK;
+}
+template <typename T, bool ANY>
+int choose_fwd(const NormArgs<T> &a, cudaStream_t st) {
+    // (four groups a thread where rows fill the GPU: 16384 x 4096 bf16 in 50 us and 4 rows in 3.0, with two 58 and 2.4)
+    const int64_t groups = (a.d + Vec<T>::N - 1) / Vec<T>::N;
+    if (groups <= 32) return launch_fwd<T, 1, ANY>(a, st);
+    if (groups <= 1024 && a.rows < 4 * 148) return launch_fwd<T, 2, ANY>(a, st);
+    return launch_fwd<T, 4, ANY>(a, st);
 }
 template <typename T, int N, int NV>
 int launch_bwd(const NormGradArgs<T> &a, int blocks, cudaStream_t st) {
@@ -581,14 +668,7 @@ int layernorm_fwd(const T *x, int64_t ldx, const T *gain, const T *bias, float e
         else SBP_LAUNCH((norm_fwd_wide_kernel<T, 1>), (unsigned)rows, kWideThreads, 0, st, a);
         return STREAMBP_OK;
     }
-    if (whole) {
-        // (four groups a thread where rows fill the GPU: 16384 x 4096 bf16 in 50 us and 4 rows in 3.0, with two 58 and 2.4)
-        const int64_t groups = d / N;
-        if (groups <= 32) return launch_fwd<T, N, 1>(a, st);
-        if (groups <= 1024 && rows < 4 * 148) return launch_fwd<T, N, 2>(a, st);
-        return launch_fwd<T, N, 4>(a, st);
-    }
-    return d <= 1024 ? launch_fwd<T, 1, 4>(a, st) : launch_fwd<T, 1, 16>(a, st);
+    return whole ? choose_fwd<T, false>(a, st) : choose_fwd<T, true>(a, st);
 }
 
 template <typename T>
