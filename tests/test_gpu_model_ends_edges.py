@@ -1,0 +1,102 @@
+"""Calls of a model's ends that the documentation allows and the other tests do not make: lists longer than what a mask leaves,
+crowded rows, gains that start anywhere, one workspace for calls one after another, the workspaces' guards."""
+import math
+import os
+import subprocess
+import sys
+
+import pytest
+import torch
+
+from paper_2506_03077_b200 import binding as B
+from test_gpu_distill import check as check_distill
+from test_gpu_distill import teacher
+from test_gpu_layernorm import EPS, forward, gradients, matrix
+from test_gpu_logprobs import BF, F32, check, logits_of, reference, score
+
+pytestmark = pytest.mark.gpu
+GUARDED = "STREAMBP_WS_GUARD" in os.environ       # read by the library once per process: below, in one of its own
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("rows,V", [(2, 33001), (200, 33000), (3, 1000), (160, 9)])
+@pytest.mark.parametrize("left", [1, 5, 127])
+@pytest.mark.parametrize("floor", [-math.inf, "lowest"])
+def test_lists_longer_than_what_a_mask_leaves(rows, V, left, floor, dtype):
+    z = logits_of(rows, V, dtype)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    keep = torch.zeros(rows, V, dtype=torch.bool, device="cuda").scatter_(1, torch.randint(V, (rows, left), generator=g, device="cuda"), True)
+    z = torch.where(keep, z, torch.finfo(dtype).min if floor == "lowest" else floor)
+    k = min(V, 128)
+    got, ref = score(z, None, k), reference(z, None, k, 1.0)
+    assert torch.equal(got["top_ids"], ref["top_ids"])
+    assert (got["top_logp"].isneginf() == ref["top_logp"].isneginf()).all() and not got["entropy"].isnan().any()
+
+
+@pytest.mark.parametrize("rows", [2, 160])
+def test_many_large_values_in_few_threads(rows):
+    """more values above the first bound than the candidates' list holds: every thousandth group, all of them different"""
+    V = 400000
+    i = torch.arange(V, device="cuda")
+    z = torch.where((i // 4) % 1024 < 8, 50 + (i * 7919 % 100003) / 10000, -(i % 13).float()).expand(rows, V).contiguous()
+    for k in (7, 24, 100):
+        check(z, None, k)
+
+
+def test_the_same_row_as_one_of_few_and_one_of_many():
+    """blocks of either kind list and score alike"""
+    z = logits_of(400, 20000, BF)
+    few, many = score(z[:4], None, 50), score(z, None, 50)
+    assert torch.equal(few["top_ids"], many["top_ids"][:4])
+    for x in ("lse", "entropy", "top_logp"):
+        assert ((few[x] - many[x][:4]).nan_to_num().abs() <= 3e-5 + 2.0 ** -22 * many[x][:4].abs().nan_to_num()).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("d", [64, 1025, 4096])
+def test_gains_that_start_anywhere(d, dtype):
+    x, dy = matrix(6, d, dtype).contiguous(), matrix(6, d, dtype, seed=4).contiguous()
+    gain, bias = matrix(1, d + 1, dtype, seed=1, mean=1.0)[0].contiguous(), matrix(1, d + 3, dtype, seed=2)[0].contiguous()
+    y, mean, rstd = forward(x, gain[1:], bias[3:])
+    want = torch.nn.functional.layer_norm(x.double(), (d,), gain[1:].double(), bias[3:].double(), EPS)
+    assert ((y.double() - want).abs() <= torch.finfo(dtype).eps / 2 * want.abs() + 2e-5 * (1 + want.abs())).all()
+    other = gradients(x, dy, gain[1:].clone(), mean, rstd)
+    for a, b in zip(gradients(x, dy, gain[1:], mean, rstd), other):
+        assert ((a.double() - b.double()).abs() <= torch.finfo(dtype).eps * b.double().abs() + 2e-5 * b.double().abs().max()).all()
+
+
+def test_one_workspace_for_calls_in_turn():
+    """a call leaves nothing in it that the next minds, whatever it held"""
+    n, V, d = 500, 900, 40
+    ids = torch.randint(V, (n,), device="cuda")
+    dy = matrix(n, d, BF)
+    need = max(B.embedding_backward_workspace_bytes(n, V, d), B.layernorm_workspace_bytes(n, d), 4096)
+    ws = torch.randint(256, (need,), dtype=torch.uint8, device="cuda")
+    first = torch.empty(V, d, device="cuda")
+    B.embedding_backward(dy, ids, first, ws)
+    x = matrix(n, d, BF)
+    _, mean, rstd = forward(x, None, None)
+    B.layernorm_backward(dy, x, None, mean, rstd, d_gain=torch.empty(d, device="cuda"), workspace=ws)
+    B.embedding_forward(dy, torch.full((3,), 10 ** 6, device="cuda"), torch.empty(3, d, device="cuda", dtype=BF), ws)
+    assert B.last_device_status(ws) == B.E_BAD_LABEL
+    again = torch.empty(V, d, device="cuda")
+    B.embedding_backward(dy, ids, again, ws)
+    assert torch.equal(first, again) and B.last_device_status(ws) == B.OK
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_vocabularies_beyond_a_clusters_shared_memory(dtype):
+    z = logits_of(2, 1_000_003, dtype)
+    for tail in (False, True):
+        ids, values = teacher(z, 40, 1.0, tail)
+        check_distill(z, ids, values, None, 1.0, tail)
+
+
+def test_in_a_process_with_guards():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    assert not GUARDED
+    sel = ["tests/test_gpu_layernorm.py::test_backward", "tests/test_gpu_embedding.py::test_gradient", "tests/test_gpu_embedding.py::test_gradient_of_crowds",
+           "tests/test_gpu_model_ends.py", "tests/test_gpu_logprobs.py::test_rows", "tests/test_gpu_distill.py::test_rows"]
+    r = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "-m", "gpu", "-p", "no:cacheprovider"] + sel, cwd=root,
+                       env=dict(os.environ, STREAMBP_WS_GUARD="1"), capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
