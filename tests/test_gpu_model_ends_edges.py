@@ -8,6 +8,7 @@ import sys
 import pytest
 import torch
 
+import test_gpu_layernorm as norms
 from paper_2506_03077_b200 import binding as B
 from test_gpu_distill import check as check_distill
 from test_gpu_distill import teacher
@@ -63,6 +64,14 @@ def test_gains_that_start_anywhere(d, dtype):
     other = gradients(x, dy, gain[1:].clone(), mean, rstd)
     for a, b in zip(gradients(x, dy, gain[1:], mean, rstd), other):
         assert ((a.double() - b.double()).abs() <= torch.finfo(dtype).eps * b.double().abs() + 2e-5 * b.double().abs().max()).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("n,d", [(600, 127), (600, 129), (4, 255), (4, 257), (600, 511), (600, 513), (593, 1023), (592, 1537), (591, 1537), (600, 8191)])
+def test_norms_of_rows_that_start_anywhere(n, d, dtype):
+    """where a thread has another number of columns, and a warp its first or last"""
+    norms.test_forward(n, d, 0, 0, 0.5, dtype)
+    norms.test_backward(n, d, 3, 1, True, dtype)
 
 
 def test_one_workspace_for_calls_in_turn():
