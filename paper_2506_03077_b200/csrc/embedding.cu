@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(SortArgs a, 
     unsigned short *s_count = reinterpret_cast<unsigned short *>(s_raw + sizeof(int2) * kHold);     // [warps][kBins]
     __shared__ int s_total[kSortBlocks][kBins], s_base[kBins], s_sum[kBins / 32], s_bad[kSortBlocks], s_worst;
     const int rank = blockIdx.x;
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");       // (waited for before the others' memory is written)
     if (tid == 0) s_worst = kNoneBad;
     __syncthreads();
     int key[ITEMS], token[ITEMS], bad = kNoneBad;
@@ -154,6 +155,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(SortArgs a, 
             __syncwarp();
         }
         __syncthreads();
+        if (pass == 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         if (tid < kBins) {
             int at = 0;
 #pragma unroll 8
