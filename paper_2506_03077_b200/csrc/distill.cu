@@ -36,7 +36,13 @@ struct Segment {
     double loss;
 };
 
-// sums over the first kTopWarps warps, for their threads (every thread of the block calls; one barrier)
+__device__ __forceinline__ double entry_sum(const double (*red)[2], int which) {
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kTopWarps; w++) s += red[w][which];
+    return s;
+}
+// sums over the first kTopWarps warps (every thread of the block calls; one barrier), which stay in red for entry_sum
 __device__ __forceinline__ void entry_sums(double &a, double &b, double (*red)[2]) {
     const int warp = threadIdx.x >> 5;
     if (warp < kTopWarps) {
@@ -51,16 +57,12 @@ __device__ __forceinline__ void entry_sums(double &a, double &b, double (*red)[2
         }
     }
     __syncthreads();
-    a = b = 0.0;
-#pragma unroll
-    for (int w = 0; w < kTopWarps; w++) {
-        a += red[w][0];
-        b += red[w][1];
-    }
+    a = entry_sum(red, 0);
+    b = entry_sum(red, 1);
 }
 
-// `cluster` blocks to a row, a segment each: the sums while the segment streams in, the other blocks' sums, the gradient while it
-// streams in again and out.  The second reading comes from L2 (row_cluster keeps what is under way well below its size), so
+// `cluster` blocks to a row, a segment each: the entries while the segment comes to L2, the sums while it streams in, the other
+// blocks' sums, the gradient while it streams in again and out.  The second reading comes from L2 (row_cluster keeps what is under way well below its size), so
 // HBM reads a row once and writes its gradient once, which is what bounds the kernel.  Thread i < k has entry i.
 //
 // With a tail the mass of the unlisted tokens has to be a sum of its own: a difference of two sums would lose it where the
@@ -71,7 +73,7 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
     constexpr int N = RowGroups<T>::N, NO = Vec<TO>::N, U = 4;
     extern __shared__ uint32_t s_bits[];                // TAIL: a bit for each group of the segment
     __shared__ int s_hash[kHash], s_id[kMaxTop];
-    __shared__ float s_q[kMaxTop];
+    __shared__ float s_q[kMaxTop], s_top[kTopWarps];
     __shared__ double s_red[kTopWarps][2], s_red2[kTopWarps][2];
     __shared__ RowStats s_warp[kWarps];
     __shared__ Segment s_seg[kMaxCluster];
@@ -103,32 +105,105 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
             }
         }
     };
+    // (asked for at once)
+    int64_t id64 = -1;
+    float t = -INFINITY;
+    if (tid < a.k) {
+        id64 = a.ids[r * a.k + tid];
+        t = a.values[r * a.k + tid];
+    }
     if (w == 0.f) {         // the row takes no part
         zeros();
         if (rank == 0 && tid == 0 && a.row_loss) a.row_loss[r] = 0.f;
         return;
     }
     if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (waited for before the others' memory is written)
+    if (warp == kWarps - 1) {           // the segment is on its way to L2 while the entries are dealt with
+        constexpr int kPiece = 256;
+        for (int v = w0 + lane * kPiece; v < w1; v += 32 * kPiece)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row.base + (int64_t)v * N), "r"(16 * min(kPiece, w1 - v)) : "memory");
+    }
     // entry tid
     int id = -1;
-    float t = -INFINITY;
-    if (tid < a.k) {
-        const int64_t x = a.ids[r * a.k + tid];
-        if (x >= 0 && x < a.vocab) {
-            id = (int)x;
-            t = a.values[r * a.k + tid];
-        } else if (x != -1 && a.hdr && !a.scan && rank == 0) {
-            set_status(a.hdr, STREAMBP_E_BAD_LABEL, (int)r);
-        }
-    }
+    if (id64 >= 0 && id64 < a.vocab) id = (int)id64;
+    else if (id64 != -1 && a.hdr && !a.scan && rank == 0) set_status(a.hdr, STREAMBP_E_BAD_LABEL, (int)r);
+    if (id < 0) t = -INFINITY;
     const bool here = id >= e0 && id < e1;
-    bool shared_group = false;          // any two of the segment's entries
-    if (TAIL) {
+    const float zi = here ? to_f32(z[id]) : -INFINITY;
+    // which token was listed before, which groups have listed tokens, the q
+    if (tid < kMaxTop) {
+        s_id[tid] = id;
+        for (int i = tid; i < kHash; i += kMaxTop) s_hash[i] = -1;
+        const float top = warp_max(t);
+        if (lane == 0) s_top[warp] = top;
+    }
+    if (TAIL)
         for (int i = tid; i < (g1 - g0 + 31) / 32; i += kThreads) s_bits[i] = 0;
-        __syncthreads();
-        const int g = here ? (id + row.off) / N - g0 : 0;
-        if (here) shared_group = atomicOr(&s_bits[g >> 5], 1u << (g & 31)) >> (g & 31) & 1;
-        shared_group = __syncthreads_or(shared_group);
+    __syncthreads();
+    bool shared_group = false;          // any two of the segment's entries
+    if (TAIL && here) {
+        const int g = (id + row.off) / N - g0;
+        shared_group = atomicOr(&s_bits[g >> 5], 1u << (g & 31)) >> (g & 31) & 1;
+    }
+    bool twice = false;
+    if (id >= 0)
+        for (uint32_t at = (uint32_t)id * 2654435761u >> 23;; at = (at + 1) & (kHash - 1)) {       // (at most kMaxTop of the places are taken)
+            const int was = atomicCAS(&s_hash[at], -1, id);
+            twice |= was == id;
+            if (was == -1 || was == id) break;
+        }
+    const bool any_twice = __syncthreads_or(twice);
+    if (TAIL) shared_group = __syncthreads_or(shared_group);
+    float t0 = s_top[0];
+#pragma unroll
+    for (int i = 1; i < kTopWarps; i++) t0 = fmaxf(t0, s_top[i]);
+    t0 = finite_or_zero(t0);
+    // (with a tail what is left of 1 is a difference, so those exponentials are taken in 64 bits)
+    double e = 0.0;
+    if (id >= 0) e = TAIL ? exp((double)t) : t == -INFINITY ? 0.0 : (double)expf(fmaf(t - t0, a.heat.hi, (t - t0) * a.heat.lo));
+    double sum = e, listed = id >= 0 ? 1.0 : 0.0;
+    entry_sums(sum, listed, s_red);
+    const float q = TAIL ? (float)e : sum == 0.0 ? 0.f : (float)e / (float)sum;
+    if (tid < kMaxTop) s_q[tid] = q;
+    {
+        double q_sum = (double)q, l = 0.0;      // (of the q as they are held, so that their roundings weigh log q - log p and not each of the two)
+        if (here && q != 0.f) l = (double)q * ((TAIL ? (double)t : ((double)t - (double)t0) * inv - (double)logf((float)sum)) - (double)zi * inv);
+        entry_sums(q_sum, l, s_red2);
+    }
+    // the entry that lists its token first has the q of all that do
+    bool first = here;
+    float q_all = q;
+    if (any_twice && here) {
+        q_all = 0.f;
+        for (int j = a.k - 1; j >= 0; j--)
+            if (s_id[j] == id) {
+                first = j == tid;
+                q_all += s_q[j];
+            }
+    }
+    float m_own = -INFINITY, rest_own = 0.f;    // TAIL: of the unlisted tokens beside the entry's
+    if (TAIL && here) {
+        // the first entry of a group adds its unlisted tokens; each token's first entry the token
+        const int g = (id + row.off) / N;
+        bool of_group = true;
+        uint32_t mask = 1u << ((id + row.off) % N);
+        if (shared_group)
+            for (int j = 0; j < a.k; j++) {
+                const int other = s_id[j];
+                if (other < e0 || other >= e1 || (other + row.off) / N != g) continue;
+                if (j < tid) of_group = false;
+                mask |= 1u << ((other + row.off) % N);
+            }
+        float x[N];
+        row.load(g, x, -INFINITY);
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            if (!of_group || (mask >> i & 1)) x[i] = -INFINITY;
+            m_own = fmaxf(m_own, x[i]);
+        }
+        const float at = finite_or_zero(m_own);
+#pragma unroll
+        for (int i = 0; i < N; i++) rest_own += exp2_approx((x[i] - at) * c);
     }
     // the sums over the segment (TAIL: but for groups with listed tokens)
     Running<T, false> run;
@@ -166,88 +241,20 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
             }
         }
     }
-    float m = run.m, S;
+    const double mass = entry_sum(s_red2, 0), loss = entry_sum(s_red2, 1);
+    const double rest_all = TAIL && entry_sum(s_red, 1) != 0.0 ? fmax(0.0, 1.0 - entry_sum(s_red, 0)) : 0.0;
+    float m = run.m, S, rest = 0.f;
     {
         float lo, hi;
         run.S.get(lo, hi);
         S = lo + hi;
     }
-    // entries: which token was listed before, the q, the logit
-    if (tid < kMaxTop) {
-        s_id[tid] = id;
-        for (int i = tid; i < kHash; i += kMaxTop) s_hash[i] = -1;
-    }
-    const float zi = here ? to_f32(z[id]) : -INFINITY;
-    __syncthreads();
-    if (warp < kTopWarps) {
-        const float top = warp_max(t);
-        if (lane == 0) s_warp[warp].W = top;
-    }
-    bool twice = false;
-    if (id >= 0)
-        for (uint32_t at = (uint32_t)id * 2654435761u >> 23;; at = (at + 1) & (kHash - 1)) {       // (at most kMaxTop of the places are taken)
-            const int was = atomicCAS(&s_hash[at], -1, id);
-            twice |= was == id;
-            if (was == -1 || was == id) break;
-        }
-    const bool any_twice = __syncthreads_or(twice);
-    float t0 = s_warp[0].W;
-#pragma unroll
-    for (int i = 1; i < kTopWarps; i++) t0 = fmaxf(t0, s_warp[i].W);
-    t0 = finite_or_zero(t0);
-    // (with a tail what is left of 1 is a difference, so those exponentials are taken in 64 bits)
-    double e = 0.0;
-    if (id >= 0) e = TAIL ? exp((double)t) : t == -INFINITY ? 0.0 : (double)expf(fmaf(t - t0, a.heat.hi, (t - t0) * a.heat.lo));
-    double sum = e, listed = id >= 0 ? 1.0 : 0.0;
-    entry_sums(sum, listed, s_red);
-    const float q = TAIL ? (float)e : sum == 0.0 ? 0.f : (float)e / (float)sum;
-    double mass = (double)q, loss = 0.0;        // (of the q as they are held, so that their roundings weigh log q - log p and not each of the two)
-    if (here && q != 0.f) loss = (double)q * ((TAIL ? (double)t : ((double)t - (double)t0) * inv - (double)logf((float)sum)) - (double)zi * inv);
-    if (tid < kMaxTop) s_q[tid] = q;
-    entry_sums(mass, loss, s_red2);
-    const double rest_all = TAIL && listed != 0.0 ? fmax(0.0, 1.0 - sum) : 0.0;
-    // the entry that lists its token first has the q of all that do
-    bool first = here;
-    float q_all = q;
-    if (any_twice && here) {
-        q_all = 0.f;
-        for (int j = a.k - 1; j >= 0; j--)
-            if (s_id[j] == id) {
-                first = j == tid;
-                q_all += s_q[j];
-            }
-    }
-    float m_rest = m, rest = S;
-    if (TAIL && here) {
-        // the first entry of a group adds its unlisted tokens; each token's first entry the token
-        const int g = (id + row.off) / N;
-        bool of_group = true;
-        uint32_t mask = 1u << ((id + row.off) % N);
-        if (shared_group)
-            for (int j = 0; j < a.k; j++) {
-                const int other = s_id[j];
-                if (other < e0 || other >= e1 || (other + row.off) / N != g) continue;
-                if (j < tid) of_group = false;
-                mask |= 1u << ((other + row.off) % N);
-            }
-        float x[N], best = m;
-        row.load(g, x, -INFINITY);
-#pragma unroll
-        for (int i = 0; i < N; i++) {
-            if (!of_group || (mask >> i & 1)) x[i] = -INFINITY;
-            best = fmaxf(best, x[i]);
-        }
-        const float at = finite_or_zero(best);
-        rest = S * exp2_approx((m - at) * c);
-#pragma unroll
-        for (int i = 0; i < N; i++) rest += exp2_approx((x[i] - at) * c);
-        m_rest = best;
-    }
     if (TAIL) {
         // both sums relative to one maximum
-        m = first ? fmaxf(m_rest, zi) : m_rest;
+        const float m_run = m;
+        m = fmaxf(fmaxf(m_run, m_own), first ? zi : -INFINITY);
         const float at = finite_or_zero(m);
-        rest *= exp2_approx((m_rest - at) * c);
+        rest = S * exp2_approx((m_run - at) * c) + rest_own * exp2_approx((m_own - at) * c);
         S = rest + (first ? exp2_approx((zi - at) * c) : 0.f);
     }
     auto joined = [&](int from) {          // over the lanes of a warp
@@ -261,7 +268,6 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
         }
     };
     joined(16);
-    __syncthreads();        // (s_warp was read)
     if (lane == 0) s_warp[warp] = RowStats{m, S, rest};
     __syncthreads();
     if (warp == 0) {
