@@ -119,7 +119,7 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
     }
     if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (waited for before the others' memory is written)
     if (warp == kWarps - 1) {           // the segment is on its way to L2 while the entries are dealt with
-        constexpr int kPiece = 256;
+        constexpr int kPiece = 1024;
         for (int v = w0 + lane * kPiece; v < w1; v += 32 * kPiece)
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row.base + (int64_t)v * N), "r"(16 * min(kPiece, w1 - v)) : "memory");
     }
