@@ -103,7 +103,7 @@ struct SortArgs {
     WsHeader *hdr;
 };
 // Up to 64 K tokens: one cluster of up to eight blocks sorts in one launch, keys and tokens in registers, handed over through
-// shared memory; the other blocks of the launch clear the table meanwhile.
+// shared memory; the other blocks of the launch clear a small table meanwhile.
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortBlocks = 8;
 template <int ITEMS>
 __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(SortArgs a, int cluster) {
@@ -331,14 +331,53 @@ struct RunArgs {
     int64_t ldy;
     int n, chunk, chunks, d, dp, vocab, accumulate;
     float scale;
+    int clears;                     // blocks that clear the table's other rows
 };
+// Rows of the table's part `part` of `parts` that have no token: whether a row has one its thread finds in the sorted keys, seven
+// keys at a time; a warp to a row clears.
+__device__ __forceinline__ void clear_others(const int *__restrict__ keys, int n, float *d_table, int64_t vocab, int d, int part, int parts) {
+    __shared__ int s_has[256];
+    const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x >> 5;
+    const int64_t r0 = vocab * part / parts, r1 = vocab * (part + 1) / parts;
+    for (int64_t r = r0; r < r1; r += blockDim.x) {
+        int lo = 0, left = n;               // the first key that is not below the row lies in lo .. lo + left
+        while (left > 0) {
+            const int step = left / 8 + 1;
+            int below = 0;
+#pragma unroll
+            for (int i = 1; i < 8; i++) {
+                const int at = i * step - 1;
+                if (at < left) below += keys[lo + at] < r + tid;
+            }
+            lo += below * step;
+            left = min(left - below * step, step - 1);
+        }
+        s_has[tid] = lo < n && keys[lo] == r + tid;
+        __syncthreads();
+        for (int i = tid >> 5; i < (int)blockDim.x && r + i < r1; i += warps) {
+            if (s_has[i]) continue;
+            float *to = d_table + (r + i) * d;
+            if (d % 4 == 0)
+                for (int c = lane * 4; c < d; c += 128) *reinterpret_cast<float4 *>(to + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+            else
+                for (int c = lane; c < d; c += 32) to[c] = 0.f;
+        }
+        __syncthreads();
+    }
+}
 constexpr int kMaxChunk = 128, kRunThreads = 256;
+constexpr int64_t kSmallTable = 16 << 20;       // elements
 // Each thread owns the columns of one 16-byte group of d_out and walks the chunk, four rows of d_out (and, added to, of the
 // table) in flight.  What bounds it is HBM: d_out once, the table's rows once in each direction.
 template <typename T, int N>
 __global__ void __launch_bounds__(kRunThreads) embedding_runs_kernel(RunArgs<T> a) {
     pdl_enter();
     __shared__ int s_key[kMaxChunk + 2], s_tok[kMaxChunk];
+    if ((int)blockIdx.x >= a.chunks) {
+        const int part = (blockIdx.x - a.chunks) * gridDim.y + blockIdx.y;
+        if (part < a.clears) clear_others(a.keys, a.n, a.d_table, a.vocab, a.d, part, a.clears);
+        return;
+    }
     const int64_t i0 = (int64_t)blockIdx.x * a.chunk;
     const int len = (int)min((int64_t)a.chunk, a.n - i0);
     for (int i = threadIdx.x; i < len + 2; i += blockDim.x) {
@@ -541,7 +580,8 @@ int embedding_counts(const EmbeddingPlan &p) { return p.one_launch ? 0 : (kBins 
 
 namespace {
 template <int ITEMS>
-int launch_sort(const SortArgs &a, int cluster, int64_t zero_blocks, cudaStream_t st) {
+int launch_sort(const SortArgs &a, int cluster, cudaStream_t st) {
+    const int64_t zero_blocks = std::min<int64_t>(148, (a.zeros + 4 * kSortThreads - 1) / (4 * kSortThreads));
     static PerDevice ready;
     constexpr int smem = ITEMS * kSortThreads * 8 + kSortWarps * kBins * 2;
     auto kernel = sort_cluster_kernel<ITEMS>;
@@ -573,19 +613,20 @@ int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64
                   float *d_table, bool accumulate, const EmbeddingPlan &p, int *const (&keys)[2], int *const (&tokens)[2],
                   int *counts, int *owners, float *partials, WsHeader *hdr, cudaStream_t st) {
     int done = 0;
+    // A small table is cleared beside the sort (50 tokens, 4096 x 256: 10 us, with its rows without tokens cleared beside the sums
+    // 13); a large one beside the sums, where tokens' rows need not be cleared (16384 tokens, 152064 x 3584: 373 us against 566).
+    const bool clear_first = !accumulate && p.one_launch && vocab * d <= kSmallTable;
     if (p.one_launch) {
-        const SortArgs s{ids, keys[0], tokens[0], owners, accumulate ? nullptr : d_table, accumulate ? 0 : vocab * d, vocab, padding, (int)n,
+        const SortArgs s{ids, keys[0], tokens[0], owners, clear_first ? d_table : nullptr, clear_first ? vocab * d : 0, vocab, padding, (int)n,
                          p.passes, hdr};
         int cluster = 1;
         while (cluster < kSortBlocks && n > (int64_t)cluster * kSortThreads) cluster *= 2;
         const int64_t each = (n + (int64_t)cluster * kSortThreads - 1) / ((int64_t)cluster * kSortThreads);
-        const int64_t zero = std::min<int64_t>(148, (s.zeros + 4 * kSortThreads - 1) / (4 * kSortThreads));
-        if (each <= 1) SBP_TRY(launch_sort<1>(s, cluster, zero, st));
-        else if (each <= 2) SBP_TRY(launch_sort<2>(s, cluster, zero, st));
-        else if (each <= 4) SBP_TRY(launch_sort<4>(s, cluster, zero, st));
-        else SBP_TRY(launch_sort<8>(s, cluster, zero, st));
+        if (each <= 1) SBP_TRY(launch_sort<1>(s, cluster, st));
+        else if (each <= 2) SBP_TRY(launch_sort<2>(s, cluster, st));
+        else if (each <= 4) SBP_TRY(launch_sort<4>(s, cluster, st));
+        else SBP_TRY(launch_sort<8>(s, cluster, st));
     } else {
-        if (!accumulate) SBP_TRY(fill_zero(d_table, sizeof(float) * (size_t)vocab * d, st));
         for (int i = 0; i < p.passes; i++) {
             const SortPass s{i ? nullptr : ids, keys[(i + 1) & 1], tokens[(i + 1) & 1], keys[i & 1], tokens[i & 1], counts, owners, vocab,
                              padding, (int)n, p.tile, kDigit * i, hdr};
@@ -594,14 +635,19 @@ int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64
         }
         done = (p.passes - 1) & 1;
     }
-    const RunArgs<T> r{keys[done], tokens[done], dy, d_table, partials, owners, ldy, (int)n, p.chunk, p.chunks, (int)d, p.partial_width, (int)vocab,
-                       accumulate ? 1 : 0, scale};
     constexpr int N = Vec<T>::N;
     const bool grouped = d % N == 0 && ldy % N == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0;
     const int64_t groups = grouped ? d / N : d, strips = (groups + kRunThreads - 1) / kRunThreads;
     const int threads = (int)(((groups + strips - 1) / strips + 31) / 32 * 32);
-    if (grouped) SBP_LAUNCH((embedding_runs_kernel<T, N>), dim3((unsigned)p.chunks, (unsigned)strips), threads, 0, st, r);
-    else SBP_LAUNCH((embedding_runs_kernel<T, 1>), dim3((unsigned)p.chunks, (unsigned)strips), threads, 0, st, r);
+    // (64 KB a block, less where its threads are fewer than those rows, more where the GPU is full of them)
+    const int64_t clears = accumulate || clear_first
+                               ? 0
+                               : std::min<int64_t>({148 * 2048 / threads, vocab, std::max(vocab * d / 16384 + 1, (vocab + threads - 1) / threads)});
+    const RunArgs<T> r{keys[done], tokens[done], dy, d_table, partials, owners, ldy, (int)n, p.chunk, p.chunks, (int)d, p.partial_width, (int)vocab,
+                       accumulate ? 1 : 0, scale, (int)clears};
+    const dim3 grid((unsigned)(p.chunks + (clears + strips - 1) / strips), (unsigned)strips);
+    if (grouped) SBP_LAUNCH((embedding_runs_kernel<T, N>), grid, threads, 0, st, r);
+    else SBP_LAUNCH((embedding_runs_kernel<T, 1>), grid, threads, 0, st, r);
     if (p.chunks == 1) return STREAMBP_OK;
     const JoinArgs j{owners, partials, d_table, (int)d, p.partial_width, accumulate ? 1 : 0, scale};
     const int64_t most = (int64_t)p.chunks * ((d + 127) / 128);

@@ -342,21 +342,18 @@ __device__ __forceinline__ void score_row(const T *__restrict__ logits, const Sc
             }
             asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
             if (rank != 0) return;
-            // an element's place is the number of larger ones: its own list's and, by bisection, the others'
+            // an element's place is the number of larger ones, by bisection of all lists at once
             for (int i = tid; i < cluster * a.k; i += THREADS) {
-                const int l = i / a.k;
-                const unsigned long long o = s_lists[l * kMaxTop + i % a.k];
-                int place = i % a.k;
-                for (int q = 0; q < cluster && o; q++) {
-                    if (q == l) continue;
-                    int lo = 0, hi = a.k;
-                    while (lo < hi) {
-                        const int mid = (lo + hi) / 2;
-                        if (s_lists[q * kMaxTop + mid] > o) lo = mid + 1;
-                        else hi = mid;
-                    }
-                    place += lo;
+                const unsigned long long o = s_lists[i / a.k * kMaxTop + i % a.k];
+                int larger[kMaxCluster] = {}, place = 0;
+                for (int step = kMaxTop; step > 0; step >>= 1) {
+                    if (step > a.k) continue;
+#pragma unroll
+                    for (int q = 0; q < kMaxCluster; q++)
+                        if (q < cluster && larger[q] + step <= a.k && s_lists[q * kMaxTop + larger[q] + step - 1] > o) larger[q] += step;
                 }
+#pragma unroll
+                for (int q = 0; q < kMaxCluster; q++) place += larger[q];
                 if (o && place < a.k) s_list[place] = o;
             }
             __syncthreads();

@@ -109,3 +109,21 @@ def test_in_a_process_with_guards():
     r = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "-m", "gpu", "-p", "no:cacheprovider"] + sel, cwd=root,
                        env=dict(os.environ, STREAMBP_WS_GUARD="1"), capture_output=True, text=True, timeout=900)
     assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("n,V,d", [(1, 70000, 260), (9, 5000, 4099), (3000, 20011, 1001), (70000, 60, 33), (66000, 300001, 60)])
+def test_embedding_gradients_that_overwrite_large_tables(n, V, d, dtype):
+    """rows without tokens are cleared by other blocks than those of small tables: the first and last rows, tokens of every row"""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    ids = torch.randint(V, (n,), generator=g, device="cuda")
+    ids[-1] = V - 1
+    dy = matrix(n, d, dtype)
+    out = torch.full((V, d), float("nan"), device="cuda")
+    ws = B.alloc_workspace(B.embedding_backward_workspace_bytes(n, V, d))
+    B.embedding_backward(dy, ids, out, ws)
+    want = torch.zeros(V, d, device="cuda", dtype=torch.float64).index_add_(0, ids, dy.double())
+    size = torch.zeros(V, d, device="cuda", dtype=torch.float64).index_add_(0, ids, dy.double().abs())
+    assert B.last_device_status(ws) == B.OK
+    # a row's sum is a chunk's values one after another, then the chunks' sums: fewer than 400 roundings
+    assert ((out.double() - want).abs() <= 400 * 2.0 ** -24 * size).all()
