@@ -335,7 +335,7 @@ struct RunArgs {
 };
 // Rows of the table's part `part` of `parts` that have no token: whether a row has one its thread finds in the sorted keys, seven
 // keys at a time; a warp to a row clears.
-__device__ __forceinline__ void clear_others(const int *__restrict__ keys, int n, float *d_table, int64_t vocab, int d, int part, int parts) {
+static __device__ __noinline__ void clear_others(const int *__restrict__ keys, int n, float *d_table, int64_t vocab, int d, int part, int parts) {
     __shared__ int s_has[256];
     const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x >> 5;
     const int64_t r0 = vocab * part / parts, r1 = vocab * (part + 1) / parts;

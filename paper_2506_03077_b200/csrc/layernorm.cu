@@ -298,18 +298,22 @@ __global__ void __launch_bounds__(kMaxThreads) norm_bwd_kernel(NormGradArgs<T> a
 // The same for rows of whole 16-byte groups, brought into shared memory by the copy engine `stages` rows ahead: the sums of the
 // columns take most of the registers, so rows that wait there would be few.  A row's place is free again when all threads have
 // taken their part into registers, which the barrier of the row's sums tells.
-template <typename T, int NV>
-__global__ void __launch_bounds__(kMaxThreads) norm_bwd_ring_kernel(NormGradArgs<T> a, int stages) {
+// TEAMS > 1: that many warps to a block, each with rows and a ring of its own (narrow rows, whose barriers would cost most).
+template <typename T, int NV, int TEAMS>
+__global__ void __launch_bounds__(TEAMS > 1 ? TEAMS * 32 : kMaxThreads) norm_bwd_ring_kernel(NormGradArgs<T> a, int stages) {
     pdl_enter();
     constexpr int N = Vec<T>::N, kMaxStages = 8;
+    constexpr bool WARP = TEAMS > 1;
     extern __shared__ __align__(128) unsigned char s_raw[];
     __shared__ float2 red[2][kMaxWarps];
-    __shared__ __align__(8) unsigned long long s_full[kMaxStages];
+    __shared__ __align__(8) unsigned long long s_full[TEAMS][kMaxStages];
     __shared__ int s_abort;
-    const int lanes = blockDim.x, lane = threadIdx.x, row_bytes = a.d * (int)sizeof(T), streams = a.add ? 3 : 2;
-    auto stage = [&](int s, int stream) { return s_raw + (size_t)(s * streams + stream) * row_bytes; };
-    auto fetch = [&](int64_t r, int s) {            // by thread 0
-        const uint32_t bar = smem_u32(&s_full[s]);
+    const int lanes = WARP ? 32 : blockDim.x, lane = WARP ? threadIdx.x & 31 : threadIdx.x, team = WARP ? threadIdx.x >> 5 : 0;
+    const int row_bytes = a.d * (int)sizeof(T), streams = a.add ? 3 : 2;
+    const int64_t first = (int64_t)blockIdx.x * TEAMS + team, step = (int64_t)gridDim.x * TEAMS;       // rows
+    auto stage = [&](int s, int stream) { return s_raw + (size_t)((team * stages + s) * streams + stream) * row_bytes; };
+    auto fetch = [&](int64_t r, int s) {            // by lane 0
+        const uint32_t bar = smem_u32(&s_full[team][s]);
         mbar_expect_tx(bar, (uint32_t)(streams * row_bytes));
         auto copy = [&](const T *p, int stream) {
             asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
@@ -320,12 +324,12 @@ __global__ void __launch_bounds__(kMaxThreads) norm_bwd_ring_kernel(NormGradArgs
         copy(a.x + r * a.ldx, 1);
         if (a.add) copy(a.add + r * a.ldadd, 2);
     };
+    if (threadIdx.x == 0) s_abort = 0;
     if (lane == 0) {
-        s_abort = 0;
-        for (int s = 0; s < stages; s++) mbar_init(smem_u32(&s_full[s]), 1);
+        for (int s = 0; s < stages; s++) mbar_init(smem_u32(&s_full[team][s]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int s = 0; s < stages; s++)
-            if (blockIdx.x + (int64_t)s * gridDim.x < a.rows) fetch(blockIdx.x + (int64_t)s * gridDim.x, s);
+            if (first + s * step < a.rows) fetch(first + s * step, s);
     }
     float sg[NV][N], sb[NV][N];
     Pack<T, N> gain[NV];
@@ -337,13 +341,13 @@ __global__ void __launch_bounds__(kMaxThreads) norm_bwd_ring_kernel(NormGradArgs
         gain[j].clear();
         if (a.gain && c < a.d) gain[j].load(a.gain + c);
     }
-    float mean = a.mean[blockIdx.x], rstd = a.rstd[blockIdx.x];
+    float mean = first < a.rows ? a.mean[first] : 0.f, rstd = first < a.rows ? a.rstd[first] : 0.f;
     __syncthreads();
     int slot = 0, at = 0, phase = 0;
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, slot ^= 1) {
-        const bool more = r + gridDim.x < a.rows;
-        const float mean_next = more ? a.mean[r + gridDim.x] : 0.f, rstd_next = more ? a.rstd[r + gridDim.x] : 0.f;
-        mbar_wait_warp(smem_u32(&s_full[at]), phase, &s_abort);
+    for (int64_t r = first; r < a.rows; r += step, slot ^= 1) {
+        const bool more = r + step < a.rows;
+        const float mean_next = more ? a.mean[r + step] : 0.f, rstd_next = more ? a.rstd[r + step] : 0.f;
+        mbar_wait_warp(smem_u32(&s_full[team][at]), phase, &s_abort);
         Pack<T, N> dy[NV], x[NV], add[NV];
 #pragma unroll
         for (int j = 0; j < NV; j++) {
@@ -374,10 +378,11 @@ __global__ void __launch_bounds__(kMaxThreads) norm_bwd_ring_kernel(NormGradArgs
                 s2 = fmaf(g[i], h[i], s2);
             }
         }
-        const float2 s = row_sum<false>(s1, s2, red, slot);
-        if (lane == 0 && r + (int64_t)stages * gridDim.x < a.rows && *(volatile int *)&s_abort == 0) {
+        const float2 s = row_sum<WARP>(s1, s2, red, slot);
+        if (WARP) __syncwarp();
+        if (lane == 0 && r + stages * step < a.rows && *(volatile int *)&s_abort == 0) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            fetch(r + (int64_t)stages * gridDim.x, at);
+            fetch(r + stages * step, at);
         }
         if (++at == stages) {
             at = 0;
@@ -407,14 +412,30 @@ __global__ void __launch_bounds__(kMaxThreads) norm_bwd_ring_kernel(NormGradArgs
     }
     if (!a.partials) return;
     float *out = a.partials + (int64_t)blockIdx.x * 2 * a.d;
+    // the warps' sums, one on another in the rings' place, the last warp's on all
+    float *own = reinterpret_cast<float *>(s_raw);
+    for (int t = 0; t < TEAMS; t++) {
+        if (WARP) __syncthreads();
+        if (t != team) continue;
 #pragma unroll
-    for (int j = 0; j < NV; j++) {
-        const int c = (lane + j * lanes) * N;
-        if (c >= a.d) continue;
+        for (int j = 0; j < NV; j++) {
+            const int c = (lane + j * lanes) * N;
+            if (c >= a.d) continue;
 #pragma unroll
-        for (int i = 0; i < N; i += 4) {
-            *reinterpret_cast<float4 *>(out + c + i) = make_float4(sg[j][i], sg[j][i + 1], sg[j][i + 2], sg[j][i + 3]);
-            *reinterpret_cast<float4 *>(out + a.d + c + i) = make_float4(sb[j][i], sb[j][i + 1], sb[j][i + 2], sb[j][i + 3]);
+            for (int i = 0; i < N; i += 4) {
+                float4 g = make_float4(sg[j][i], sg[j][i + 1], sg[j][i + 2], sg[j][i + 3]), b = make_float4(sb[j][i], sb[j][i + 1], sb[j][i + 2], sb[j][i + 3]);
+                auto add = [](float4 x, const float *y) {
+                    const float4 z = *reinterpret_cast<const float4 *>(y);
+                    return make_float4(x.x + z.x, x.y + z.y, x.z + z.z, x.w + z.w);
+                };
+                if (t > 0) {
+                    g = add(g, own + c + i);
+                    b = add(b, own + a.d + c + i);
+                }
+                float *to = t == TEAMS - 1 ? out : own;
+                *reinterpret_cast<float4 *>(to + c + i) = g;
+                *reinterpret_cast<float4 *>(to + a.d + c + i) = b;
+            }
         }
     }
 }
@@ -540,6 +561,7 @@ template <typename T>
 bool grouped(const void *p, int64_t ld) {
     return p == nullptr || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % Vec<T>::N == 0);
 }
+constexpr int64_t kNarrow = 4096;   // rows of few groups from which on each is a warp's (65536 x 768 bf16 in 72 us, as a block's 116; 8192 in 17 and 25)
 constexpr int64_t kWide = 8192;     // columns above which rows are not held in registers
 
 template <typename T, int N, int NV>
@@ -556,14 +578,14 @@ int launch_fwd(const NormArgs<T> &a, cudaStream_t st) {
 }
 // Shared memory of an SM for the rows under way, and blocks that share it
 constexpr int kRingBytes = 208 << 10;
-template <typename T, int NV>
+template <typename T, int NV, int TEAMS = 1>
 int launch_ring(const NormGradArgs<T> &a, int blocks, cudaStream_t st) {
-    const int groups = a.d / Vec<T>::N, threads = ((groups + NV - 1) / NV + 31) / 32 * 32;
-    const int each = (blocks + 147) / 148, row = (a.add ? 3 : 2) * a.d * (int)sizeof(T);
-    const int64_t turns = (a.rows + blocks - 1) / blocks;
+    const int groups = a.d / Vec<T>::N, threads = TEAMS > 1 ? TEAMS * 32 : ((groups + NV - 1) / NV + 31) / 32 * 32;
+    const int each = (blocks + 147) / 148, row = TEAMS * (a.add ? 3 : 2) * a.d * (int)sizeof(T);
+    const int64_t turns = (a.rows + TEAMS * (int64_t)blocks - 1) / (TEAMS * (int64_t)blocks);
     const int stages = (int)std::max<int64_t>(1, std::min<int64_t>({8, turns, kRingBytes / (each * row)}));
     static PerDevice ready;
-    auto kernel = norm_bwd_ring_kernel<T, NV>;
+    auto kernel = norm_bwd_ring_kernel<T, NV, TEAMS>;
     if (!ready.get([&] { return cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes)) ? 1 : 0; }))
         return STREAMBP_E_CUDA;
     SBP_LAUNCH(kernel, (unsigned)blocks, threads, stages * row, st, a, stages);
@@ -608,7 +630,7 @@ int layernorm_bwd(const T *dy, int64_t lddy, const T *x, int64_t ldx, const T *g
                   bool accumulate, float *partials, WsHeader *hdr, cudaStream_t st) {
     const bool sums = dgain || dbias;
     const NormGradArgs<T> a{dy, x, gain, add, mean, rstd, dx, sums ? partials : nullptr, rows, lddy, ldx, ldadd, lddx, (int)d};
-    const int blocks = layernorm_blocks(rows, d);
+    int blocks = layernorm_blocks(rows, d);
     constexpr int N = Vec<T>::N;
     const bool whole = d % N == 0 && grouped<T>(x, ldx) && grouped<T>(dy, lddy) && grouped<T>(add, ldadd) && grouped<T>(dx, lddx) &&
                        grouped<T>(gain, 0);
@@ -626,7 +648,14 @@ int layernorm_bwd(const T *dy, int64_t lddy, const T *x, int64_t ldx, const T *g
     } else if (whole) {
         // sixteen columns a thread (their sums take 32 registers), fewer where a row is short
         const int64_t groups = d / N;
-        if (groups <= 128) SBP_TRY((launch_ring<T, 1>(a, blocks, st)));
+        if (groups <= (N == 4 ? 128 : 96) && rows >= kNarrow) {
+            // (the sums of four bf16 groups a lane leave too few warps an SM)
+            blocks = std::min(blocks, 148 * (groups <= 64 ? 6 : 3));
+            if (groups <= 32) SBP_TRY((launch_ring<T, 1, 4>(a, blocks, st)));
+            else if (groups <= 64) SBP_TRY((launch_ring<T, 2, 4>(a, blocks, st)));
+            else if (N > 4 || groups <= 96) SBP_TRY((launch_ring<T, 3, 4>(a, blocks, st)));
+            else SBP_TRY((launch_ring<T, 16 / N, 4>(a, blocks, st)));
+        } else if (groups <= 128) SBP_TRY((launch_ring<T, 1>(a, blocks, st)));
         else SBP_TRY((launch_ring<T, 16 / N>(a, blocks, st)));
     } else {
         SBP_LAUNCH((norm_bwd_kernel<T, 16>), (unsigned)blocks, (unsigned)((d + 511) / 512 * 32), 0, st, a);

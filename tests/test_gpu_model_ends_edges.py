@@ -127,3 +127,11 @@ def test_embedding_gradients_that_overwrite_large_tables(n, V, d, dtype):
     assert B.last_device_status(ws) == B.OK
     # a row's sum is a chunk's values one after another, then the chunks' sums: fewer than 400 roundings
     assert ((out.double() - want).abs() <= 400 * 2.0 ** -24 * size).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("n,d", [(4096, 8), (4097, 256), (5000, 264), (4099, 512), (9000, 384), (4100, 768), (4096, 776), (7001, 16)])
+def test_norms_of_many_narrow_rows(n, d, dtype):
+    """a warp's rows and a block's, the sums of a block's warps"""
+    norms.test_backward(n, d, 0, 0, False, dtype)
+    norms.test_backward(n, d, 8, 0, True, dtype)
