@@ -4,6 +4,11 @@
 //   list only:  q = softmax(t / tau) over the entries,   L = sum q_i (log q_i - log p_ci),  Q = 1, q_r = 0
 //   with tail:  q_i = exp t_i,  q_r = 1 - sum q_i,  L as above + q_r log(q_r / p_r),  p_r the mass of unlisted tokens,  Q = sum q_i + q_r
 //   dL/dz_j = (Q p_j - sum_{c_i = j} q_i) / tau for listed j,  (Q p_j - q_r p_j / p_r) / tau for the others
+//
+// Bound by HBM, one reading and one writing of a row, as far as the phases of a block (entries, sums, the others' sums, gradient)
+// hide one another's.  Measured: 1024 x 152064 fp32 with 32 entries 220 us (5.7 TB/s), 2048 x 32000 with 64 and a tail 100 (5.3);
+// bf16 has twice the exponentials a byte: 2048 x 152064 in 255 us (4.9), 1500 x 50001 with 100 entries and a tail 72 (3.8; two and
+// a half rounds of rows on the GPU).
 #include <algorithm>
 
 #include "vocab_rows.cuh"

@@ -1,10 +1,14 @@
 // Embedding lookup with a scale, and its gradient by sorted tokens.
 //
 //   out[t] = scale table[id_t],      d_table[v] (+)= scale sum over t with id_t = v of d_out[t]
-// The gradient sorts the tokens by id (stable, by digits of 8 bits), so that equal ids lie side by side in token order, cuts the
+// The gradient sorts the tokens by id (stable, by digits of 9 bits), so that equal ids lie side by side in token order, cuts the
 // sorted list into chunks of equal length and sums the runs of a chunk in order.  A run that crosses chunks leaves one partial
 // sum a chunk in the workspace; a second launch adds them in order.  So a token that fills half the batch costs no more than
 // many that come once, and equal inputs give equal bits.
+//
+// Bound by HBM: a looked-up row in and out, a gradient row in and a row of the table in and out.  Measured: lookup of 32768 rows of
+// 3584 bf16 in 52 us (6.2 TB/s with rows that come again from L2); gradient of the same into 152064 rows 139 us: sort 21, sums 96
+// (5.7 TB/s), joins 12, launches.
 #include <algorithm>
 
 #include "embedding.cuh"
@@ -333,13 +337,30 @@ struct RunArgs {
     float scale;
     int clears;                     // blocks that clear the table's other rows
 };
-// Rows of the table's part `part` of `parts` that have no token: whether a row has one its thread finds in the sorted keys, seven
-// keys at a time; a warp to a row clears.
+// Rows r0 .. r1 - 1 of the table that have no token are cleared, a warp to a row; find(r) tells the block in s_has which of the
+// rows from r on have one, as many as it has threads.
+template <typename F>
+__device__ __forceinline__ void clear_rows(float *d_table, int d, int64_t r0, int64_t r1, int *s_has, F find) {
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    for (int64_t r = r0; r < r1; r += blockDim.x) {
+        find(r);
+        __syncthreads();
+        for (int i = threadIdx.x >> 5; i < (int)blockDim.x && r + i < r1; i += warps) {
+            if (s_has[i]) continue;
+            float *to = d_table + (r + i) * d;
+            if (d % 4 == 0)
+                for (int c = lane * 4; c < d; c += 128) *reinterpret_cast<float4 *>(to + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+            else
+                for (int c = lane; c < d; c += 32) to[c] = 0.f;
+        }
+        __syncthreads();
+    }
+}
+// The table's part `part` of `parts`; whether a row has a token its thread finds in the sorted keys, seven keys at a time.
 static __device__ __noinline__ void clear_others(const int *__restrict__ keys, int n, float *d_table, int64_t vocab, int d, int part, int parts) {
     __shared__ int s_has[256];
-    const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x >> 5;
-    const int64_t r0 = vocab * part / parts, r1 = vocab * (part + 1) / parts;
-    for (int64_t r = r0; r < r1; r += blockDim.x) {
+    const int tid = threadIdx.x;
+    clear_rows(d_table, d, vocab * part / parts, vocab * (part + 1) / parts, s_has, [&](int64_t r) {
         int lo = 0, left = n;               // the first key that is not below the row lies in lo .. lo + left
         while (left > 0) {
             const int step = left / 8 + 1;
@@ -353,17 +374,7 @@ static __device__ __noinline__ void clear_others(const int *__restrict__ keys, i
             left = min(left - below * step, step - 1);
         }
         s_has[tid] = lo < n && keys[lo] == r + tid;
-        __syncthreads();
-        for (int i = tid >> 5; i < (int)blockDim.x && r + i < r1; i += warps) {
-            if (s_has[i]) continue;
-            float *to = d_table + (r + i) * d;
-            if (d % 4 == 0)
-                for (int c = lane * 4; c < d; c += 128) *reinterpret_cast<float4 *>(to + c) = make_float4(0.f, 0.f, 0.f, 0.f);
-            else
-                for (int c = lane; c < d; c += 32) to[c] = 0.f;
-        }
-        __syncthreads();
-    }
+    });
 }
 constexpr int kMaxChunk = 128, kRunThreads = 256;
 constexpr int64_t kSmallTable = 16 << 20;       // elements
@@ -468,6 +479,104 @@ __global__ void __launch_bounds__(kRunThreads) embedding_runs_kernel(RunArgs<T> 
             // (their order does not matter)
             if (lane == 0) reinterpret_cast<int4 *>(a.owners)[1 + atomicAdd(a.owners, 1)] = make_int4(blockIdx.x, last, key, 0);
         }
+    }
+}
+
+// Up to kFewTokens tokens, in one launch without a sort: the block of a token that is the first with its id adds all of them, in
+// their order, eight rows in flight.  Bound by latency: 50 tokens of 256 columns with the rest of 4096 rows cleared in 4.5 us (by
+// sort, sums and joins 10), 128 tokens of two ids in 9.0 (10.6; 512 of them would take 57 against 14, though 512 of many ids 11).
+constexpr int kFewTokens = 128;
+template <typename T>
+struct FewArgs {
+    const int64_t *ids;
+    const T *dy;
+    float *d_table;
+    int64_t ldy, vocab, padding;
+    int n, d, accumulate, clears;
+    float scale;
+    WsHeader *hdr;
+};
+template <typename T, int N>
+__global__ void __launch_bounds__(kRunThreads) embedding_few_kernel(FewArgs<T> a) {
+    pdl_enter();
+    constexpr int U = 8;
+    __shared__ int s_id[kFewTokens], s_bad, s_has[kRunThreads];
+    const int tid = threadIdx.x, lane = tid & 31, t = blockIdx.x;
+    if (tid == 0) s_bad = kNoneBad;
+    __syncthreads();
+    for (int i = tid; i < kFewTokens; i += blockDim.x) {
+        const int64_t id = i < a.n ? a.ids[i] : a.padding;
+        const bool none = i >= a.n || no_part(id, a.vocab, a.padding);
+        s_id[i] = none ? -1 : (int)id;
+        if (none && id != a.padding) atomicMin(&s_bad, i);
+    }
+    __syncthreads();
+    if (t == 0 && blockIdx.y == 0 && tid == 0) {
+        a.hdr->status = s_bad == kNoneBad ? STREAMBP_OK : STREAMBP_E_BAD_LABEL;
+        a.hdr->detail = s_bad == kNoneBad ? 0 : s_bad;
+    }
+    if (t >= a.n) {
+        const int part = (t - a.n) * gridDim.y + blockIdx.y;
+        if (part < a.clears)
+            clear_rows(a.d_table, a.d, a.vocab * part / a.clears, a.vocab * (part + 1) / a.clears, s_has, [&](int64_t r) {
+                s_has[tid] = 0;
+                __syncthreads();
+                for (int i = tid; i < a.n; i += blockDim.x)
+                    if (s_id[i] >= r && s_id[i] < r + blockDim.x) s_has[s_id[i] - r] = 1;
+            });
+        return;
+    }
+    const int id = s_id[t], c = (blockIdx.y * blockDim.x + tid) * N;
+    if (id < 0) return;
+    uint32_t same[kFewTokens / 32];             // the tokens with this id
+#pragma unroll
+    for (int w = 0; w < kFewTokens / 32; w++) same[w] = __ballot_sync(0xffffffffu, s_id[w * 32 + lane] == id);
+    bool first = true;
+#pragma unroll
+    for (int w = 0; w < kFewTokens / 32; w++) first = first && (w * 32 > t || (same[w] & (t - w * 32 >= 32 ? ~0u : (1u << (t - w * 32)) - 1)) == 0);
+    if (!first || c >= a.d) return;
+    float *to = a.d_table + (int64_t)id * a.d + c;
+    typename Piece<float, N>::In old[sizeof(float) / sizeof(T)];
+    if (a.accumulate) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) Piece<float, N>::load(to + e, old[e / 4]);
+    }
+    float sum[N];
+#pragma unroll
+    for (int e = 0; e < N; e++) sum[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewTokens / 32; w++)
+        for (uint32_t left = same[w]; left;) {
+            typename Piece<T, N>::In x[U];
+            int have = 0;
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                if (!left) continue;
+                Piece<T, N>::load(a.dy + (int64_t)(w * 32 + __ffs(left) - 1) * a.ldy + c, x[u]);
+                left &= left - 1;
+                have = u + 1;
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                if (u >= have) continue;
+                float v[N];
+                Piece<T, N>::get(x[u], v);
+#pragma unroll
+                for (int e = 0; e < N; e++) sum[e] += v[e];
+            }
+        }
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+        if (a.accumulate) Piece<float, N>::get(old[e / 4], o);
+#pragma unroll
+        for (int f = 0; f < 4 && e + f < N; f++) sum[e + f] = fmaf(sum[e + f], a.scale, o[f]);
+    }
+    if constexpr (N == 1) {
+        *to = sum[0];
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) *reinterpret_cast<float4 *>(to + e) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
     }
 }
 
@@ -612,9 +721,24 @@ template <typename T>
 int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, float scale, int64_t padding,
                   float *d_table, bool accumulate, const EmbeddingPlan &p, int *const (&keys)[2], int *const (&tokens)[2],
                   int *counts, int *owners, float *partials, WsHeader *hdr, cudaStream_t st) {
+    constexpr int N = Vec<T>::N;
+    const bool grouped = d % N == 0 && ldy % N == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0;
+    const int64_t groups = grouped ? d / N : d, strips = (groups + kRunThreads - 1) / kRunThreads;
+    int threads = (int)(((groups + strips - 1) / strips + 31) / 32 * 32);
+    if (n <= kFewTokens && !accumulate) threads = std::max(threads, 128);       // (for the rows that are cleared)
+    // Blocks that clear rows: 64 KB each, less where its threads are fewer than those rows, more where the GPU is full of them.
+    const int64_t clears =
+        accumulate ? 0 : std::min<int64_t>({148 * 2048 / threads, vocab, std::max(vocab * d / 16384 + 1, (vocab + threads - 1) / threads)});
+    if (n <= kFewTokens) {
+        const FewArgs<T> f{ids, dy, d_table, ldy, vocab, padding, (int)n, (int)d, accumulate ? 1 : 0, (int)clears, scale, hdr};
+        const dim3 grid((unsigned)(n + (clears + strips - 1) / strips), (unsigned)strips);
+        if (grouped) SBP_LAUNCH((embedding_few_kernel<T, N>), grid, threads, 0, st, f);
+        else SBP_LAUNCH((embedding_few_kernel<T, 1>), grid, threads, 0, st, f);
+        return STREAMBP_OK;
+    }
     int done = 0;
-    // A small table is cleared beside the sort (50 tokens, 4096 x 256: 10 us, with its rows without tokens cleared beside the sums
-    // 13); a large one beside the sums, where tokens' rows need not be cleared (16384 tokens, 152064 x 3584: 373 us against 566).
+    // A small table is cleared beside the sort (3000 tokens, 50001 x 64: 17.7 us, with its rows without tokens cleared beside the
+    // sums 20.5); a large one beside the sums, where tokens' rows need not be cleared (16384 tokens, 152064 x 3584: 373 us against 566).
     const bool clear_first = !accumulate && p.one_launch && vocab * d <= kSmallTable;
     if (p.one_launch) {
         const SortArgs s{ids, keys[0], tokens[0], owners, clear_first ? d_table : nullptr, clear_first ? vocab * d : 0, vocab, padding, (int)n,
@@ -635,20 +759,11 @@ int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64
         }
         done = (p.passes - 1) & 1;
     }
-    constexpr int N = Vec<T>::N;
-    const bool grouped = d % N == 0 && ldy % N == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0;
-    const int64_t groups = grouped ? d / N : d, strips = (groups + kRunThreads - 1) / kRunThreads;
-    const int threads = (int)(((groups + strips - 1) / strips + 31) / 32 * 32);
-    // (64 KB a block, less where its threads are fewer than those rows, more where the GPU is full of them)
-    const int64_t clears = accumulate || clear_first
-                               ? 0
-                               : std::min<int64_t>({148 * 2048 / threads, vocab, std::max(vocab * d / 16384 + 1, (vocab + threads - 1) / threads)});
     const RunArgs<T> r{keys[done], tokens[done], dy, d_table, partials, owners, ldy, (int)n, p.chunk, p.chunks, (int)d, p.partial_width, (int)vocab,
-                       accumulate ? 1 : 0, scale, (int)clears};
-    const dim3 grid((unsigned)(p.chunks + (clears + strips - 1) / strips), (unsigned)strips);
+                       accumulate ? 1 : 0, scale, clear_first ? 0 : (int)clears};
+    const dim3 grid((unsigned)(p.chunks + (r.clears + strips - 1) / strips), (unsigned)strips);
     if (grouped) SBP_LAUNCH((embedding_runs_kernel<T, N>), grid, threads, 0, st, r);
     else SBP_LAUNCH((embedding_runs_kernel<T, 1>), grid, threads, 0, st, r);
-    if (p.chunks == 1) return STREAMBP_OK;
     const JoinArgs j{owners, partials, d_table, (int)d, p.partial_width, accumulate ? 1 : 0, scale};
     const int64_t most = (int64_t)p.chunks * ((d + 127) / 128);
     SBP_LAUNCH(embedding_join_kernel, (unsigned)std::min<int64_t>(most, 148 * 8), 256, 0, st, j);

@@ -2,6 +2,11 @@
 //
 // Per row, with p = softmax(z / tau):  lse = log sum exp(z / tau),  logp = z_y / tau - lse,
 // H = - sum p log p = log S - W / (tau S) of the statistics S, W of vocab_rows.cuh, and the k largest logits.
+//
+// Bound by HBM where rows are many.  Measured: 1024 x 152064 fp32 without a list in 97 us (6.4 TB/s, a copy's rate), with 16
+// alternatives 104 (6.0); 2048 x 152064 bf16 in 103 and 123 us (6.0 and 5.1 TB/s: twice the exponentials a byte).  3 rows of 152064
+// in 11 us, half of which is the list: its bound, what reaches it, the ranks and the cluster's join come one after another.
+// Gradient: 2048 x 32003 bf16 in 42 us (5.6 TB/s with what skipped rows save), 2048 x 152064 fp32 in 379 (6.6).
 #include <algorithm>
 
 #include "vocab_rows.cuh"

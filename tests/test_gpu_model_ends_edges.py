@@ -135,3 +135,25 @@ def test_norms_of_many_narrow_rows(n, d, dtype):
     """a warp's rows and a block's, the sums of a block's warps"""
     norms.test_backward(n, d, 0, 0, False, dtype)
     norms.test_backward(n, d, 8, 0, True, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("n,V,d", [(1, 1, 1), (31, 5, 40), (32, 1000, 2056), (33, 7, 33), (64, 3, 4099), (128, 1, 512), (128, 200, 96), (129, 4, 64)])
+def test_embedding_gradients_of_few_tokens(n, V, d, accumulate, dtype):
+    """tokens of one id across all words of the search, padding and ids outside the table among them"""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    ids = torch.randint(V, (n,), generator=g, device="cuda")
+    if n > 8:
+        ids[3], ids[n // 2], ids[n - 1] = -1, V, -1
+    dy = matrix(n, d, dtype, 8, 0)
+    start = matrix(V, d, F32, seed=9).contiguous()
+    out = start.clone() if accumulate else torch.full((V, d), float("nan"), device="cuda")
+    ws = B.alloc_workspace(B.embedding_backward_workspace_bytes(n, V, d))
+    B.embedding_backward(dy, ids, out, ws, scale=0.5, padding_id=-1, accumulate=accumulate)
+    assert B.last_device_status(ws) == (B.E_BAD_LABEL if n > 8 else B.OK)
+    part = (ids >= 0) & (ids < V)
+    sums = lambda x: torch.zeros(V, d, device="cuda", dtype=torch.float64).index_add_(0, ids[part], x.double()[part])
+    want = 0.5 * sums(dy) + (start.double() if accumulate else 0.0)
+    # at most 130 roundings of the sum, one of the result
+    assert ((out.double() - want).abs() <= 130 * 2.0 ** -25 * sums(dy.abs()) + 2.0 ** -24 * want.abs()).all()
