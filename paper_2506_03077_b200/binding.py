@@ -587,7 +587,7 @@ def _rows(what: str, dev: int, dtype: torch.dtype, shape: tuple, t: Optional[tor
     """(address, leading dimension) of a matrix whose rows are contiguous; (None, 0) for None."""
     if t is None:
         return None, 0
-    if t.get_device() != dev or t.dtype != dtype or tuple(t.shape) != shape:
+    if t.get_device() != dev or t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{what}: expected a {dtype} tensor {shape} on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     rows, cols = t.stride()
     if (cols != 1 and shape[1] > 1) or (rows < shape[1] and shape[0] > 1):
@@ -943,7 +943,7 @@ def _space(what: str, dev: int, workspace: Optional[torch.Tensor]) -> tuple:
         return None, 0
     if workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError(f"{what}: workspace is contiguous, on cuda:{dev}")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def _matrix(what: str, name: str, t: torch.Tensor) -> int:
@@ -959,9 +959,11 @@ def token_logprobs_workspace_bytes() -> int:
 def _score_outputs(what: str, dev: int, n: int, tokens, logp, lse, entropy, top_logp, top_ids) -> tuple:
     f, i = torch.float32, torch.int64
     rows = _vectors(what, dev, (n,), tokens=(tokens, i), logp=(logp, f), lse=(lse, f), entropy=(entropy, f))
-    lists = [t for t in (top_logp, top_ids) if t is not None]
-    _want(all(t.dim() == 2 for t in lists), what, "top_logp and top_ids are [rows, k]")
-    k = lists[0].shape[1] if lists else 0
+    lists = top_logp if top_logp is not None else top_ids
+    if lists is None:
+        return rows, 0, (None, None)
+    _want(lists.dim() == 2, what, "top_logp and top_ids are [rows, k]")
+    k = lists.shape[1]
     return rows, k, _vectors(what, dev, (n, k), top_logp=(top_logp, f), top_ids=(top_ids, i))
 
 
@@ -986,7 +988,8 @@ def token_logprobs_backward(logits, tokens, lse, entropy, d_logits, d_logp=None,
     (or logits itself)."""
     what, dev = "token_logprobs_backward", _matrix("token_logprobs_backward", "logits", logits)
     n, V = logits.shape
-    z, d = (_rows(what, dev, logits.dtype, (n, V), t) for t in (logits, d_logits))
+    z = _rows(what, dev, logits.dtype, (n, V), logits)
+    d = z if d_logits is logits else _rows(what, dev, logits.dtype, (n, V), d_logits)
     f = torch.float32
     v = _vectors(what, dev, (n,), tokens=(tokens, torch.int64), lse=(lse, f), entropy=(entropy, f), d_logp=(d_logp, f), d_lse=(d_lse, f),
                  d_entropy=(d_entropy, f))
@@ -1013,7 +1016,8 @@ def distill_topk(logits, ids, values, row_loss, workspace, d_logits=None, weight
     and row_loss fp32 [rows] (optional), d_logits like logits (or logits itself, or None)."""
     what, dev = "distill_topk", _matrix("distill_topk", "logits", logits)
     n, V = logits.shape
-    z, d = (_rows(what, dev, logits.dtype, (n, V), t) for t in (logits, d_logits))
+    z = _rows(what, dev, logits.dtype, (n, V), logits)
+    d = z if d_logits is logits else _rows(what, dev, logits.dtype, (n, V), d_logits)
     k, entries = _entries(what, dev, n, ids, values)
     w = _vectors(what, dev, (n,), weight=(weight, torch.float32), row_loss=(row_loss, torch.float32))
     cfg = DistillCfgC(k, 1 if tail else 0, temperature)
@@ -1104,7 +1108,8 @@ def layernorm_backward(dy, x, gain, mean, rstd, dx=None, d_gain=None, d_bias=Non
     """streambp_layernorm_backward; dy, x, add, dx [rows, d], d_gain and d_bias fp32 [d] (overwritten, or added to)."""
     what, dev, dt = "layernorm_backward", _matrix("layernorm_backward", "x", x), x.dtype
     n, d = x.shape
-    g, a, r, o = (_rows(what, dev, dt, (n, d), t) for t in (dy, x, add, dx))
+    nd = (n, d)
+    g, a, r, o = _rows(what, dev, dt, nd, dy), _rows(what, dev, dt, nd, x), _rows(what, dev, dt, nd, add), _rows(what, dev, dt, nd, dx)
     w = _vectors(what, dev, (d,), gain=(gain, dt), d_gain=(d_gain, torch.float32), d_bias=(d_bias, torch.float32))
     s = _vectors(what, dev, (n,), mean=(mean, torch.float32), rstd=(rstd, torch.float32))
     st = _launch(what, dev, stream, lib().streambp_layernorm_backward, g[0], g[1], a[0], a[1], w[0], *s, r[0], r[1], n, d,
