@@ -8,7 +8,7 @@
 // Statistics and sums are fp32, the variance from the differences to the mean; y and dx are rounded once.
 //
 // Measured at 16384 x 4096 bf16: forward 49 us (5.5 TB/s; 84 % of a copy's rate), gradient with a residual's gradient added and
-// both sums 99 us (5.4 TB/s; 83 %).  fp32: 8192 x 4096 in 43 and 83 us.  Rows that start anywhere are moved by single elements and
+// both sums 99 us (5.4 TB/s; 83 %).  fp32, 8192 x 4096 without a residual: 42 and 71 us.  Rows that start anywhere are moved by single elements and
 // bound by their instructions: 8192 x 4097 bf16 in 50 and 104 us (2.7 and 1.9 TB/s), the gradient in fp32 with a residual 120 us
 // (4.5 TB/s).  (Loading the two aligned groups around such a thread's columns and shifting them into place: 63 and 162 us.)
 #include <algorithm>
