@@ -443,7 +443,9 @@ int streambp_attention_window_backward(const void *q, const void *k, const void 
 /*
  * (No counterpart in the paper.)  What a model's two ends need beside the products: log-probabilities of given tokens,
  * distillation from a teacher's top logits, layer norm, the embedding lookup and its gradient.  Matrices here have rows that
- * may start anywhere (ld in elements, aligned to their elements); rows that start on 16 bytes are faster.
+ * may start anywhere (ld in elements, aligned to their elements); rows that start on 16 bytes are faster.  Inputs and outputs
+ * do not overlap but where an output may be an input, in its place; calls that may run at the same time have workspaces of
+ * their own.
  *
  * Log-probabilities.  Row i of logits ([rows, vocab], float or bf16) has p = softmax(z / temperature).
  *     lse = log sum exp(z / temperature),  logp = z[token] / temperature - lse,  entropy = - sum p log p,

@@ -8,9 +8,10 @@
 // Statistics and sums are fp32, the variance from the differences to the mean; y and dx are rounded once.
 //
 // Measured at 16384 x 4096 bf16: forward 49 us (5.5 TB/s; 84 % of a copy's rate), gradient with a residual's gradient added and
-// both sums 99 us (5.4 TB/s; 83 %).  fp32, 8192 x 4096 without a residual: 42 and 71 us.  Rows that start anywhere are moved by single elements and
-// bound by their instructions: 8192 x 4097 bf16 in 50 and 104 us (2.7 and 1.9 TB/s), the gradient in fp32 with a residual 120 us
-// (4.5 TB/s).  (Loading the two aligned groups around such a thread's columns and shifting them into place: 63 and 162 us.)
+// both sums 99 us (5.4 TB/s; 83 %).  fp32, 8192 x 4096 without a residual: 42 and 71 us.  Rows that start anywhere are moved by
+// single elements and bound by their instructions: 8192 x 4097 bf16 in 50 and 104 us (2.7 and 1.9 TB/s), the gradient in fp32
+// with a residual 120 us (4.5 TB/s).  (Loading the two aligned groups around such a thread's columns and shifting them into
+// place: 63 and 162 us.)
 #include <algorithm>
 #include <type_traits>
 
@@ -409,6 +410,10 @@ __global__ void __launch_bounds__(TEAMS > 1 ? TEAMS * 32 : kMaxThreads) norm_bwd
         }
         mean = mean_next;
         rstd = rstd_next;
+    }
+    if (*(volatile int *)&s_abort) {        // give copies that are still in flight time to land before shared memory is released
+        const unsigned long long t0 = global_timer();
+        while (global_timer() - t0 < 200000ull) {}
     }
     if (!a.partials) return;
     float *out = a.partials + (int64_t)blockIdx.x * 2 * a.d;
