@@ -567,7 +567,7 @@ bool grouped(const void *p, int64_t ld) {
     return p == nullptr || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % Vec<T>::N == 0);
 }
 constexpr int64_t kNarrow = 4096;   // rows of few groups from which on each is a warp's (65536 x 768 bf16 in 72 us, as a block's 116; 8192 in 17 and 25)
-constexpr int64_t kWide = 8192;     // columns above which rows are not held in registers
+constexpr int64_t kWide = 8192;     // columns above which a gradient's rows are not held by a block
 
 template <typename T, int N, int NV>
 int launch_fwd_warps(const NormArgs<T> &a, cudaStream_t st) {
@@ -614,7 +614,9 @@ int layernorm_fwd(const T *x, int64_t ldx, const T *gain, const T *bias, float e
     const NormArgs<T> a{x, gain, bias, y, mean, rstd, rows, ldx, ldy, (int)d, eps};
     constexpr int N = Vec<T>::N;
     const bool whole = d % N == 0 && grouped<T>(x, ldx) && grouped<T>(y, ldy) && grouped<T>(gain, 0) && grouped<T>(bias, 0);
-    if (d > kWide) {
+    // (held by blocks of up to 512 threads: 2048 x 16384 bf16 in 31 us, read three times 51; by 1024 threads 1024 x 32768 in 42, read
+    // three times 36)
+    if (d > kMaxThreads * (whole ? 4 * N : 16)) {
         if (whole) SBP_LAUNCH((norm_fwd_wide_kernel<T, N>), (unsigned)rows, kWideThreads, 0, st, a);
         else SBP_LAUNCH((norm_fwd_wide_kernel<T, 1>), (unsigned)rows, kWideThreads, 0, st, a);
         return STREAMBP_OK;

@@ -157,3 +157,11 @@ def test_embedding_gradients_of_few_tokens(n, V, d, accumulate, dtype):
     want = 0.5 * sums(dy) + (start.double() if accumulate else 0.0)
     # at most 130 roundings of the sum, one of the result
     assert ((out.double() - want).abs() <= 130 * 2.0 ** -25 * sums(dy.abs()) + 2.0 ** -24 * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("n,d", [(3, 12288), (600, 9001), (2, 16384), (2, 16385), (2, 16392), (2, 32768), (2, 32776)])
+def test_norms_of_wide_rows(n, d, dtype):
+    """the widest rows that a block holds, and the next"""
+    norms.test_forward(n, d, 0, 0, 0.5, dtype)
+    norms.test_forward(n, d, 8, 0, 30.0, dtype)
