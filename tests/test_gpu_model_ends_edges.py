@@ -165,3 +165,52 @@ def test_norms_of_wide_rows(n, d, dtype):
     """the widest rows that a block holds, and the next"""
     norms.test_forward(n, d, 0, 0, 0.5, dtype)
     norms.test_forward(n, d, 8, 0, 30.0, dtype)
+
+
+@pytest.mark.parametrize("n,V,d", [(50, 900, 64), (3000, 500, 72), (3000, 20011, 1000), (70000, 2000, 16)])
+def test_embedding_gradients_captured_and_two_at_once(n, V, d):
+    """replays read what is there then, and write every row; two of them run at the same time with workspaces of their own"""
+    streams, calls = [torch.cuda.Stream() for _ in range(2)], []
+    for s in streams:
+        ids, dy = torch.zeros(n, dtype=torch.int64, device="cuda"), torch.zeros(n, d, device="cuda")
+        out, ws = torch.empty(V, d, device="cuda"), B.alloc_workspace(B.embedding_backward_workspace_bytes(n, V, d))
+        B.embedding_backward(dy, ids, out, ws)                     # (attributes of the kernels are set outside the capture)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            B.embedding_backward(dy, ids, out, ws)
+        calls.append((ids, dy, out, ws, graph))
+    for round_ in range(3):
+        for i, (ids, dy, out, ws, graph) in enumerate(calls):
+            g = torch.Generator(device="cuda").manual_seed(10 * round_ + i)
+            ids.copy_(torch.randint(V, (n,), generator=g, device="cuda") // (1 + 2 * round_))
+            dy.copy_(torch.randn(n, d, generator=g, device="cuda"))
+            out.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for s, call in zip(streams, calls):
+            with torch.cuda.stream(s):
+                call[4].replay()
+        torch.cuda.synchronize()
+        for ids, dy, out, ws, graph in calls:
+            want = torch.zeros(V, d, device="cuda", dtype=torch.float64).index_add_(0, ids, dy.double())
+            size = torch.zeros(V, d, device="cuda", dtype=torch.float64).index_add_(0, ids, dy.double().abs())
+            assert B.last_device_status(ws) == B.OK
+            # fewer than 400 roundings to a row's sum (a chunk's values, then the chunks)
+            assert ((out.double() - want).abs() <= 400 * 2.0 ** -24 * size).all()
+
+
+def test_norm_gradients_two_at_once():
+    streams, calls = [torch.cuda.Stream() for _ in range(2)], []
+    for i, (n, d) in enumerate(((5000, 768), (900, 1537))):
+        x, dy = matrix(n, d, BF, seed=i), matrix(n, d, BF, seed=7 + i)
+        _, mean, rstd = forward(x, None, None)
+        calls.append((x, dy, None, mean, rstd, gradients(x, dy, None, mean, rstd)))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for s, (x, dy, gain, mean, rstd, _) in zip(streams, calls):
+            with torch.cuda.stream(s):
+                got.append(gradients(x, dy, gain, mean, rstd))
+        torch.cuda.synchronize()
+        for a, call in zip(got, calls):
+            assert all(torch.equal(x, y) for x, y in zip(a, call[5]))
