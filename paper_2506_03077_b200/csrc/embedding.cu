@@ -124,7 +124,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(SortArgs a, 
     extern __shared__ __align__(16) unsigned char s_raw[];
     int2 *s_hold = reinterpret_cast<int2 *>(s_raw);
     unsigned short *s_count = reinterpret_cast<unsigned short *>(s_raw + sizeof(int2) * kHold);     // [warps][kBins]
-    __shared__ int s_total[kSortBlocks][kBins], s_base[kBins], s_sum[kBins / 32], s_bad[kSortBlocks], s_worst;
+    __shared__ uint32_t s_total[kSortBlocks][kBins / 2];
+    __shared__ int s_base[kBins], s_sum[kBins / 32], s_bad[kSortBlocks], s_worst;
     const int rank = blockIdx.x;
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");       // (waited for before the others' memory is written)
     if (tid == 0) s_worst = kNoneBad;
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(SortArgs a, 
     if (rank == 0 && tid == 0) a.owners[0] = 0;
     for (int pass = 0; pass < a.passes; pass++) {
         const int shift = pass * kDigit;
-        for (int i = tid; i < kSortWarps * kBins / 2; i += kSortThreads) reinterpret_cast<int *>(s_count)[i] = 0;
+        for (int i = tid; i < kSortWarps * kBins / 8; i += kSortThreads) reinterpret_cast<uint4 *>(s_count)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
         unsigned short place[ITEMS], *mine = s_count + warp * kBins;
 #pragma unroll
@@ -160,15 +161,15 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(SortArgs a, 
         }
         __syncthreads();
         if (pass == 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        if (tid < kBins) {
-            int at = 0;
+        if (tid < kBins / 2) {          // two bins a thread, added as one word (a block's counts are below 2^14)
+            uint32_t at = 0, *count = reinterpret_cast<uint32_t *>(s_count) + tid;
 #pragma unroll 8
             for (int w = 0; w < kSortWarps; w++) {
-                const int c = s_count[w * kBins + tid];
-                s_count[w * kBins + tid] = (unsigned short)at;
+                const uint32_t c = count[w * kBins / 2];
+                count[w * kBins / 2] = at;
                 at += c;
             }
-            for (int q = 0; q < cluster; q++) st_remote_u32(map_to_cta(smem_u32(&s_total[rank][tid]), q), (uint32_t)at);
+            for (int q = 0; q < cluster; q++) st_remote_u32(map_to_cta(smem_u32(&s_total[rank][tid]), q), at);
         }
         if (pass == 0 && tid == kSortThreads - 1) st_remote_u32(map_to_cta(smem_u32(&s_bad[rank]), 0), (uint32_t)s_worst);
         __syncwarp();
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(SortArgs a, 
         int all = 0, before = 0;
         if (tid < kBins)
             for (int q = 0; q < cluster; q++) {
-                const int c = s_total[q][tid];
+                const int c = reinterpret_cast<const unsigned short *>(s_total[q])[tid];
                 all += c;
                 if (q < rank) before += c;
             }
