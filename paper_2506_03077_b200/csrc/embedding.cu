@@ -7,8 +7,8 @@
 // many that come once, and equal inputs give equal bits.
 //
 // Bound by HBM: a looked-up row in and out, a gradient row in and a row of the table in and out.  Measured: lookup of 32768 rows of
-// 3584 bf16 in 52 us (6.2 TB/s with rows that come again from L2); gradient of the same into 152064 rows 139 us: sort 21, sums 96
-// (5.7 TB/s), joins 12, launches.
+// 3584 bf16 in 52 us (6.2 TB/s with rows that come again from L2); gradient of the same into 152064 rows 127 us: sort 15, sums 96
+// (6.1 TB/s), joins 12, launches.
 #include <algorithm>
 
 #include "embedding.cuh"
