@@ -445,6 +445,134 @@ __global__ void __launch_bounds__(TEAMS > 1 ? TEAMS * 32 : kMaxThreads) norm_bwd
     }
 }
 
+// Rows wider than registers hold, in a block of up to 1024 threads: only the columns' sums stay there, and a row is read from the
+// ring once for its sums and again for dx.  Its place is filled again behind the barrier of the next row's sums.
+template <typename T>
+__global__ void __launch_bounds__(kWideThreads) norm_bwd_wide_ring_kernel(NormGradArgs<T> a, int stages) {
+    pdl_enter();
+    constexpr int N = Vec<T>::N, NV = 16 / N, kMaxStages = 8;
+    extern __shared__ __align__(128) unsigned char s_raw[];
+    __shared__ float2 red[2][kMaxWarps];
+    __shared__ __align__(8) unsigned long long s_full[kMaxStages];
+    __shared__ int s_abort;
+    const int lanes = blockDim.x, lane = threadIdx.x, row_bytes = a.d * (int)sizeof(T), streams = a.add ? 3 : 2;
+    const int64_t step = gridDim.x;
+    auto stage = [&](int s, int stream) { return s_raw + (size_t)(s * streams + stream) * row_bytes; };
+    auto fetch = [&](int64_t r, int s) {            // by thread 0
+        const uint32_t bar = smem_u32(&s_full[s]);
+        mbar_expect_tx(bar, (uint32_t)(streams * row_bytes));
+        auto copy = [&](const T *p, int stream) {
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                             smem_u32(stage(s, stream))), "l"(p), "r"(row_bytes), "r"(bar)
+                         : "memory");
+        };
+        copy(a.dy + r * a.lddy, 0);
+        copy(a.x + r * a.ldx, 1);
+        if (a.add) copy(a.add + r * a.ldadd, 2);
+    };
+    if (lane == 0) {
+        s_abort = 0;
+        for (int s = 0; s < stages; s++) mbar_init(smem_u32(&s_full[s]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int s = 0; s < stages; s++)
+            if (blockIdx.x + s * step < a.rows) fetch(blockIdx.x + s * step, s);
+    }
+    float sg[NV][N], sb[NV][N];
+#pragma unroll
+    for (int j = 0; j < NV; j++)
+#pragma unroll
+        for (int i = 0; i < N; i++) sg[j][i] = sb[j][i] = 0.f;
+    __syncthreads();
+    int slot = 0, at = 0, phase = 0;
+    for (int64_t r = blockIdx.x; r < a.rows; r += step, slot ^= 1) {
+        const float mean = a.mean[r], rstd = a.rstd[r];
+        mbar_wait_warp(smem_u32(&s_full[at]), phase, &s_abort);
+        const T *dy = reinterpret_cast<const T *>(stage(at, 0)), *x = reinterpret_cast<const T *>(stage(at, 1));
+        auto both = [&](int c, float (&g)[N], float (&h)[N]) {       // dy and xhat
+            Pack<T, N> p;
+            p.load(dy + c);
+            p.get(g);
+            p.load(x + c);
+            p.get(h);
+#pragma unroll
+            for (int i = 0; i < N; i++) h[i] = (h[i] - mean) * rstd;
+        };
+        auto times_gain = [&](int c, float (&g)[N]) {
+            if (!a.gain) return;
+            float w[N];
+            Pack<T, N> p;
+            p.load(a.gain + c);
+            p.get(w);
+#pragma unroll
+            for (int i = 0; i < N; i++) g[i] *= w[i];
+        };
+        float s1 = 0.f, s2 = 0.f, g[N], h[N];
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const int c = (lane + j * lanes) * N;
+            if (c >= a.d) continue;
+            both(c, g, h);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                sg[j][i] = fmaf(g[i], h[i], sg[j][i]);
+                sb[j][i] += g[i];
+            }
+            times_gain(c, g);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                s1 += g[i];
+                s2 = fmaf(g[i], h[i], s2);
+            }
+        }
+        const float2 s = row_sum<false>(s1, s2, red, slot);
+        if (lane == 0 && r != blockIdx.x && r + (stages - 1) * step < a.rows && *(volatile int *)&s_abort == 0) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            fetch(r + (stages - 1) * step, at == 0 ? stages - 1 : at - 1);
+        }
+        if (a.dx) {
+            const float m1 = s.x / (float)a.d, m2 = s.y / (float)a.d;
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                const int c = (lane + j * lanes) * N;
+                if (c >= a.d) continue;
+                both(c, g, h);
+                times_gain(c, g);
+                float t[N];
+#pragma unroll
+                for (int i = 0; i < N; i++) t[i] = 0.f;
+                if (a.add) {
+                    Pack<T, N> p;
+                    p.load(reinterpret_cast<const T *>(stage(at, 2)) + c);
+                    p.get(t);
+                }
+#pragma unroll
+                for (int i = 0; i < N; i++) g[i] = fmaf(g[i] - m1 - h[i] * m2, rstd, t[i]);
+                Pack<T, N>::store(a.dx + r * a.lddx + c, g);
+            }
+        }
+        if (++at == stages) {
+            at = 0;
+            phase ^= 1;
+        }
+    }
+    if (*(volatile int *)&s_abort) {        // give copies that are still in flight time to land before shared memory is released
+        const unsigned long long t0 = global_timer();
+        while (global_timer() - t0 < 200000ull) {}
+    }
+    if (!a.partials) return;
+    float *out = a.partials + (int64_t)blockIdx.x * 2 * a.d;
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+        const int c = (lane + j * lanes) * N;
+        if (c >= a.d) continue;
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            *reinterpret_cast<float4 *>(out + c + i) = make_float4(sg[j][i], sg[j][i + 1], sg[j][i + 2], sg[j][i + 3]);
+            *reinterpret_cast<float4 *>(out + a.d + c + i) = make_float4(sb[j][i], sb[j][i + 1], sb[j][i + 2], sb[j][i + 3]);
+        }
+    }
+}
+
 // wide rows: dx row by row, the row read twice
 template <typename T, int N>
 __global__ void __launch_bounds__(kWideThreads) norm_bwd_wide_kernel(NormGradArgs<T> a) {
@@ -596,6 +724,16 @@ int launch_ring(const NormGradArgs<T> &a, int blocks, cudaStream_t st) {
     SBP_LAUNCH(kernel, (unsigned)blocks, threads, stages * row, st, a, stages);
     return STREAMBP_OK;
 }
+template <typename T>
+int launch_wide_ring(const NormGradArgs<T> &a, int blocks, int row, cudaStream_t st) {
+    static PerDevice ready;
+    auto kernel = norm_bwd_wide_ring_kernel<T>;
+    if (!ready.get([&] { return cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes)) ? 1 : 0; }))
+        return STREAMBP_E_CUDA;
+    const int stages = std::min(8, kRingBytes / row);
+    SBP_LAUNCH(kernel, (unsigned)blocks, (unsigned)((a.d + 511) / 512 * 32), stages * row, st, a, stages);
+    return STREAMBP_OK;
+}
 }  // namespace
 
 int layernorm_take_fault() { return take_fault_local(); }
@@ -641,7 +779,11 @@ int layernorm_bwd(const T *dy, int64_t lddy, const T *x, int64_t ldx, const T *g
     constexpr int N = Vec<T>::N;
     const bool whole = d % N == 0 && grouped<T>(x, ldx) && grouped<T>(dy, lddy) && grouped<T>(add, ldadd) && grouped<T>(dx, lddx) &&
                        grouped<T>(gain, 0);
-    if (d > kWide) {
+    const int64_t row = (add ? 3 : 2) * d * (int64_t)sizeof(T);
+    if (whole && d > kWide && d <= 16 * kWideThreads && 2 * row <= kRingBytes) {
+        blocks = std::min(blocks, 148);
+        SBP_TRY((launch_wide_ring<T>(a, blocks, (int)row, st)));
+    } else if (d > kWide) {
         // (the sums first: dx may lie where dy or x does)
         const int64_t strips = (d / (whole ? N : 1) + 127) / 128;
         if (sums) {

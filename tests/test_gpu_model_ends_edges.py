@@ -160,9 +160,11 @@ def test_embedding_gradients_of_few_tokens(n, V, d, accumulate, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
-@pytest.mark.parametrize("n,d", [(3, 12288), (600, 9001), (2, 16384), (2, 16385), (2, 16392), (2, 32768), (2, 32776)])
+@pytest.mark.parametrize("n,d", [(3, 12288), (600, 9001), (450, 8200), (2, 16384), (2, 16385), (5, 16392), (200, 20488), (2, 32768), (2, 32776)])
 def test_norms_of_wide_rows(n, d, dtype):
-    """the widest rows that a block holds, and the next"""
+    """the widest rows that a block or a cluster of two or four holds, and the next"""
+    norms.test_backward(n, d, 0, 0, False, dtype)
+    norms.test_backward(n, d, 8, 0, True, dtype)
     norms.test_forward(n, d, 0, 0, 0.5, dtype)
     norms.test_forward(n, d, 8, 0, 30.0, dtype)
 
