@@ -8,19 +8,26 @@
 // Statistics and sums are fp32, the variance from the differences to the mean; y and dx are rounded once.
 //
 // Measured at 16384 x 4096 bf16: forward 49 us (5.5 TB/s; 84 % of a copy's rate), gradient with a residual's gradient added and
-// both sums 99 us (5.4 TB/s; 83 %).  fp32, 8192 x 4096 without a residual: 42 and 71 us.  Rows that start anywhere are moved by
-// single elements and bound by their instructions: 8192 x 4097 bf16 in 50 and 104 us (2.7 and 1.9 TB/s), the gradient in fp32
-// with a residual 120 us (4.5 TB/s).  (Loading the two aligned groups around such a thread's columns and shifting them into
-// place: 63 and 162 us.)
+// both sums 90 us (5.9 TB/s; 91 %), by two fp32 operations to an instruction: by one each 99, as without the residual, so that
+// instructions weigh as much as memory there; forward that changes nothing.  fp32, 8192 x 4096 without a residual: 42 and 71 us.
+// Rows that start anywhere are moved by single elements and bound by their instructions: 8192 x 4097 bf16 in 50 and 104 us (2.7
+// and 1.9 TB/s), the gradient in fp32 with a residual 120 us (4.5 TB/s).  (Loading the two aligned groups around such a thread's
+// columns and shifting them into place: 63 and 162 us.)
 #include <algorithm>
 #include <type_traits>
 
-#include "sm100.cuh"
+#include "vocab_rows.cuh"
 
 namespace sbp {
 
 namespace {
 constexpr int kMaxThreads = 512, kWideThreads = 1024, kMaxWarps = kWideThreads / 32;
+
+__device__ __forceinline__ float sum_of(Pair p) {
+    float a, b;
+    p.get(a, b);
+    return a + b;
+}
 
 // N elements at a time: 16 bytes, or one where a pointer, a leading dimension or the width is not made of 16-byte groups.
 // They stay in their storage type while they wait.
@@ -33,6 +40,17 @@ template <typename T, int N> struct Pack {
         a.load(reinterpret_cast<const T *>(&w));
 #pragma unroll
         for (int i = 0; i < N; i++) x[i] = a.v[i];
+    }
+    __device__ __forceinline__ void get(Pair (&x)[N / 2]) const {
+        Raw<T> r;
+        r.w = w;
+        r.pairs(x);
+    }
+    static __device__ __forceinline__ void store(T *p, const Pair (&x)[N / 2]) {
+        float v[N];
+#pragma unroll
+        for (int i = 0; i < N / 2; i++) x[i].get(v[2 * i], v[2 * i + 1]);
+        store(p, v);
     }
     __device__ __forceinline__ void set(const float (&x)[N]) {
         Vec<T> a;
@@ -296,6 +314,13 @@ __global__ void __launch_bounds__(kMaxThreads) norm_bwd_kernel(NormGradArgs<T> a
     }
 }
 
+__device__ __forceinline__ float4 four(Pair a, Pair b) {
+    float4 f;
+    a.get(f.x, f.y);
+    b.get(f.z, f.w);
+    return f;
+}
+
 // The same for rows of whole 16-byte groups, brought into shared memory by the copy engine `stages` rows ahead: the sums of the
 // columns take most of the registers, so rows that wait there would be few.  A row's place is free again when all threads have
 // taken their part into registers, which the barrier of the row's sums tells.
@@ -303,7 +328,7 @@ __global__ void __launch_bounds__(kMaxThreads) norm_bwd_kernel(NormGradArgs<T> a
 template <typename T, int NV, int TEAMS>
 __global__ void __launch_bounds__(TEAMS > 1 ? TEAMS * 32 : kMaxThreads) norm_bwd_ring_kernel(NormGradArgs<T> a, int stages) {
     pdl_enter();
-    constexpr int N = Vec<T>::N, kMaxStages = 8;
+    constexpr int N = Vec<T>::N, H = N / 2, kMaxStages = 8;
     constexpr bool WARP = TEAMS > 1;
     extern __shared__ __align__(128) unsigned char s_raw[];
     __shared__ float2 red[2][kMaxWarps];
@@ -332,12 +357,12 @@ __global__ void __launch_bounds__(TEAMS > 1 ? TEAMS * 32 : kMaxThreads) norm_bwd
         for (int s = 0; s < stages; s++)
             if (first + s * step < a.rows) fetch(first + s * step, s);
     }
-    float sg[NV][N], sb[NV][N];
+    Pair sg[NV][H], sb[NV][H];
     Pack<T, N> gain[NV];
 #pragma unroll
     for (int j = 0; j < NV; j++) {
 #pragma unroll
-        for (int i = 0; i < N; i++) sg[j][i] = sb[j][i] = 0.f;
+        for (int i = 0; i < H; i++) sg[j][i] = sb[j][i] = Pair(0.f, 0.f);
         const int c = (lane + j * lanes) * N;
         gain[j].clear();
         if (a.gain && c < a.d) gain[j].load(a.gain + c);
@@ -361,25 +386,26 @@ __global__ void __launch_bounds__(TEAMS > 1 ? TEAMS * 32 : kMaxThreads) norm_bwd
             x[j].load(reinterpret_cast<const T *>(stage(at, 1)) + c);
             if (a.add) add[j].load(reinterpret_cast<const T *>(stage(at, 2)) + c);
         }
-        float s1 = 0.f, s2 = 0.f;
+        const Pair minus_mean(-mean, -mean), rstd2(rstd, rstd);
+        Pair s1(0.f, 0.f), s2(0.f, 0.f);
 #pragma unroll
         for (int j = 0; j < NV; j++) {
             if ((lane + j * lanes) * N >= a.d) continue;
-            float g[N], h[N], w[N];
+            Pair g[H], h[H], w[H];
             dy[j].get(g);
             x[j].get(h);
             gain[j].get(w);
 #pragma unroll
-            for (int i = 0; i < N; i++) {
-                h[i] = (h[i] - mean) * rstd;
-                sg[j][i] = fmaf(g[i], h[i], sg[j][i]);
-                sb[j][i] += g[i];
-                if (a.gain) g[i] *= w[i];
-                s1 += g[i];
-                s2 = fmaf(g[i], h[i], s2);
+            for (int i = 0; i < H; i++) {
+                h[i] = (h[i] + minus_mean) * rstd2;
+                sg[j][i] = fma2(g[i], h[i], sg[j][i]);
+                sb[j][i] = sb[j][i] + g[i];
+                if (a.gain) g[i] = g[i] * w[i];
+                s1 = s1 + g[i];
+                s2 = fma2(g[i], h[i], s2);
             }
         }
-        const float2 s = row_sum<WARP>(s1, s2, red, slot);
+        const float2 s = row_sum<WARP>(sum_of(s1), sum_of(s2), red, slot);
         if (WARP) __syncwarp();
         if (lane == 0 && r + stages * step < a.rows && *(volatile int *)&s_abort == 0) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -391,19 +417,20 @@ __global__ void __launch_bounds__(TEAMS > 1 ? TEAMS * 32 : kMaxThreads) norm_bwd
         }
         if (a.dx) {
             const float m1 = s.x / (float)a.d, m2 = s.y / (float)a.d;
+            const Pair minus_m1(-m1, -m1), minus_m2(-m2, -m2);
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 const int c = (lane + j * lanes) * N;
                 if (c >= a.d) continue;
-                float g[N], h[N], w[N], t[N];
+                Pair g[H], h[H], w[H], t[H];
                 dy[j].get(g);
                 x[j].get(h);
                 gain[j].get(w);
                 add[j].get(t);
 #pragma unroll
-                for (int i = 0; i < N; i++) {
-                    if (a.gain) g[i] *= w[i];
-                    g[i] = fmaf(g[i] - m1 - (h[i] - mean) * rstd * m2, rstd, t[i]);
+                for (int i = 0; i < H; i++) {
+                    if (a.gain) g[i] = g[i] * w[i];
+                    g[i] = fma2(fma2((h[i] + minus_mean) * rstd2, minus_m2, g[i] + minus_m1), rstd2, t[i]);
                 }
                 Pack<T, N>::store(a.dx + r * a.lddx + c, g);
             }
@@ -428,7 +455,7 @@ __global__ void __launch_bounds__(TEAMS > 1 ? TEAMS * 32 : kMaxThreads) norm_bwd
             if (c >= a.d) continue;
 #pragma unroll
             for (int i = 0; i < N; i += 4) {
-                float4 g = make_float4(sg[j][i], sg[j][i + 1], sg[j][i + 2], sg[j][i + 3]), b = make_float4(sb[j][i], sb[j][i + 1], sb[j][i + 2], sb[j][i + 3]);
+                float4 g = four(sg[j][i / 2], sg[j][i / 2 + 1]), b = four(sb[j][i / 2], sb[j][i / 2 + 1]);
                 auto add = [](float4 x, const float *y) {
                     const float4 z = *reinterpret_cast<const float4 *>(y);
                     return make_float4(x.x + z.x, x.y + z.y, x.z + z.z, x.w + z.w);
@@ -446,11 +473,12 @@ __global__ void __launch_bounds__(TEAMS > 1 ? TEAMS * 32 : kMaxThreads) norm_bwd
 }
 
 // Rows wider than registers hold, in a block of up to 1024 threads: only the columns' sums stay there, and a row is read from the
-// ring once for its sums and again for dx.  Its place is filled again behind the barrier of the next row's sums.
+// ring once for its sums and again for dx (2048 x 16384 bf16 in 70 us; dx and the sums by a launch each, rows from memory, 126).
+// Its place is filled again behind the barrier of the next row's sums.
 template <typename T>
 __global__ void __launch_bounds__(kWideThreads) norm_bwd_wide_ring_kernel(NormGradArgs<T> a, int stages) {
     pdl_enter();
-    constexpr int N = Vec<T>::N, NV = 16 / N, kMaxStages = 8;
+    constexpr int N = Vec<T>::N, NV = 16 / N, H = N / 2, kMaxStages = 8;
     extern __shared__ __align__(128) unsigned char s_raw[];
     __shared__ float2 red[2][kMaxWarps];
     __shared__ __align__(8) unsigned long long s_full[kMaxStages];
@@ -477,76 +505,78 @@ __global__ void __launch_bounds__(kWideThreads) norm_bwd_wide_ring_kernel(NormGr
         for (int s = 0; s < stages; s++)
             if (blockIdx.x + s * step < a.rows) fetch(blockIdx.x + s * step, s);
     }
-    float sg[NV][N], sb[NV][N];
+    Pair sg[NV][H], sb[NV][H];
 #pragma unroll
     for (int j = 0; j < NV; j++)
 #pragma unroll
-        for (int i = 0; i < N; i++) sg[j][i] = sb[j][i] = 0.f;
+        for (int i = 0; i < H; i++) sg[j][i] = sb[j][i] = Pair(0.f, 0.f);
     __syncthreads();
     int slot = 0, at = 0, phase = 0;
     for (int64_t r = blockIdx.x; r < a.rows; r += step, slot ^= 1) {
         const float mean = a.mean[r], rstd = a.rstd[r];
         mbar_wait_warp(smem_u32(&s_full[at]), phase, &s_abort);
         const T *dy = reinterpret_cast<const T *>(stage(at, 0)), *x = reinterpret_cast<const T *>(stage(at, 1));
-        auto both = [&](int c, float (&g)[N], float (&h)[N]) {       // dy and xhat
+        const Pair minus_mean(-mean, -mean), rstd2(rstd, rstd);
+        auto both = [&](int c, Pair (&g)[H], Pair (&h)[H]) {       // dy and xhat
             Pack<T, N> p;
             p.load(dy + c);
             p.get(g);
             p.load(x + c);
             p.get(h);
 #pragma unroll
-            for (int i = 0; i < N; i++) h[i] = (h[i] - mean) * rstd;
+            for (int i = 0; i < H; i++) h[i] = (h[i] + minus_mean) * rstd2;
         };
-        auto times_gain = [&](int c, float (&g)[N]) {
+        auto times_gain = [&](int c, Pair (&g)[H]) {
             if (!a.gain) return;
-            float w[N];
+            Pair w[H];
             Pack<T, N> p;
             p.load(a.gain + c);
             p.get(w);
 #pragma unroll
-            for (int i = 0; i < N; i++) g[i] *= w[i];
+            for (int i = 0; i < H; i++) g[i] = g[i] * w[i];
         };
-        float s1 = 0.f, s2 = 0.f, g[N], h[N];
+        Pair s1(0.f, 0.f), s2(0.f, 0.f), g[H], h[H];
 #pragma unroll
         for (int j = 0; j < NV; j++) {
             const int c = (lane + j * lanes) * N;
             if (c >= a.d) continue;
             both(c, g, h);
 #pragma unroll
-            for (int i = 0; i < N; i++) {
-                sg[j][i] = fmaf(g[i], h[i], sg[j][i]);
-                sb[j][i] += g[i];
+            for (int i = 0; i < H; i++) {
+                sg[j][i] = fma2(g[i], h[i], sg[j][i]);
+                sb[j][i] = sb[j][i] + g[i];
             }
             times_gain(c, g);
 #pragma unroll
-            for (int i = 0; i < N; i++) {
-                s1 += g[i];
-                s2 = fmaf(g[i], h[i], s2);
+            for (int i = 0; i < H; i++) {
+                s1 = s1 + g[i];
+                s2 = fma2(g[i], h[i], s2);
             }
         }
-        const float2 s = row_sum<false>(s1, s2, red, slot);
+        const float2 s = row_sum<false>(sum_of(s1), sum_of(s2), red, slot);
         if (lane == 0 && r != blockIdx.x && r + (stages - 1) * step < a.rows && *(volatile int *)&s_abort == 0) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             fetch(r + (stages - 1) * step, at == 0 ? stages - 1 : at - 1);
         }
         if (a.dx) {
             const float m1 = s.x / (float)a.d, m2 = s.y / (float)a.d;
+            const Pair minus_m1(-m1, -m1), minus_m2(-m2, -m2);
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 const int c = (lane + j * lanes) * N;
                 if (c >= a.d) continue;
                 both(c, g, h);
                 times_gain(c, g);
-                float t[N];
+                Pair t[H];
 #pragma unroll
-                for (int i = 0; i < N; i++) t[i] = 0.f;
+                for (int i = 0; i < H; i++) t[i] = Pair(0.f, 0.f);
                 if (a.add) {
                     Pack<T, N> p;
                     p.load(reinterpret_cast<const T *>(stage(at, 2)) + c);
                     p.get(t);
                 }
 #pragma unroll
-                for (int i = 0; i < N; i++) g[i] = fmaf(g[i] - m1 - h[i] * m2, rstd, t[i]);
+                for (int i = 0; i < H; i++) g[i] = fma2(fma2(h[i], minus_m2, g[i] + minus_m1), rstd2, t[i]);
                 Pack<T, N>::store(a.dx + r * a.lddx + c, g);
             }
         }
@@ -567,8 +597,8 @@ __global__ void __launch_bounds__(kWideThreads) norm_bwd_wide_ring_kernel(NormGr
         if (c >= a.d) continue;
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
-            *reinterpret_cast<float4 *>(out + c + i) = make_float4(sg[j][i], sg[j][i + 1], sg[j][i + 2], sg[j][i + 3]);
-            *reinterpret_cast<float4 *>(out + a.d + c + i) = make_float4(sb[j][i], sb[j][i + 1], sb[j][i + 2], sb[j][i + 3]);
+            *reinterpret_cast<float4 *>(out + c + i) = four(sg[j][i / 2], sg[j][i / 2 + 1]);
+            *reinterpret_cast<float4 *>(out + a.d + c + i) = four(sb[j][i / 2], sb[j][i / 2 + 1]);
         }
     }
 }
@@ -694,7 +724,7 @@ template <typename T>
 bool grouped(const void *p, int64_t ld) {
     return p == nullptr || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % Vec<T>::N == 0);
 }
-constexpr int64_t kNarrow = 4096;   // rows of few groups from which on each is a warp's (65536 x 768 bf16 in 72 us, as a block's 116; 8192 in 17 and 25)
+constexpr int64_t kNarrow = 4096;   // rows of few groups from which on each is a warp's (65536 x 768 bf16 in 69 us, as a block's 116; 8192 in 17 and 25)
 constexpr int64_t kWide = 8192;     // columns above which a gradient's rows are not held by a block
 
 template <typename T, int N, int NV>
