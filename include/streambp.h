@@ -477,7 +477,8 @@ int streambp_token_logprobs_backward(const void *logits, int64_t ld, int64_t row
  *     tail = 0: q = softmax(values / temperature) over the row's entries,  row_loss = sum q (log q - log p[id])
  *     tail = 1: q = exp(values), log-probabilities of the teacher at this temperature; what they leave of 1 is one more
  *               outcome, the unlisted tokens together:  row_loss = sum q (log q - log p[id]) + q_r log(q_r / p_r),
- *               q_r = max(0, 1 - sum q), p_r the sum of p over unlisted tokens (left out where no token is left for it)
+ *               q_r = max(0, 1 - sum q), p_r the sum of p over unlisted tokens, however far below the listed ones
+ *               (left out where no unlisted token has a finite logit)
  *     d_logits = weight[i] d row_loss / d logits, rounded once
  * A token listed more than once is the sum of its entries in the gradient.  weight (NULL: 1) carries what the objective
  * multiplies a row by (1 / N, a mixing factor, temperature^2); a row of weight 0, or without entries, takes no part: its logits

@@ -6,9 +6,9 @@
 //   dL/dz_j = (Q p_j - sum_{c_i = j} q_i) / tau for listed j,  (Q p_j - q_r p_j / p_r) / tau for the others
 //
 // Bound by HBM, one reading and one writing of a row, as far as the phases of a block (entries, sums, the others' sums, gradient)
-// hide one another's.  Measured: 1024 x 152064 fp32 with 32 entries 220 us (5.7 TB/s), 2048 x 32000 with 64 and a tail 100 (5.3);
-// bf16 has twice the exponentials a byte: 2048 x 152064 in 255 us (4.9), 1500 x 50001 with 100 entries and a tail 72 (3.8; two and
-// a half rounds of rows on the GPU).
+// hide one another's.  Measured: 1024 x 152064 fp32 with 32 entries 220 us (5.7 TB/s), 2048 x 32000 with 64 and a tail 101 (5.2);
+// bf16 has twice the exponentials a byte: 2048 x 152064 in 255 us (4.9), 1500 x 50001 with 100 entries and a tail 73 (3.7; two and
+// a half rounds of rows on the GPU).  A maximum of its own for the unlisted tokens takes 1 us of the two with a tail.
 #include <algorithm>
 
 #include "vocab_rows.cuh"
@@ -34,10 +34,11 @@ __device__ __forceinline__ void st_remote_f64(uint32_t a, double v) {
     asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(a), "d"(v) : "memory");
 }
 
-// What a block knows of its segment of a row, for the others: the maximum m, the sums of exp((z - m) / tau) over its tokens
-// and, with a tail, over the unlisted ones, and sum q (log q - z / tau) over the entries that lie in it.
+// What a block knows of its segment of a row, for the others: the maximum m and the sum S of exp((z - m) / tau) over its tokens
+// (with a tail: over the listed ones, and the same of the unlisted ones by themselves), and sum q (log q - z / tau) over the
+// entries that lie in it.
 struct Segment {
-    float m, S, rest, pad;
+    float m, S, m_rest, rest;
     double loss;
 };
 
@@ -71,7 +72,8 @@ __device__ __forceinline__ void entry_sums(double &a, double &b, double (*red)[2
 // HBM reads a row once and writes its gradient once, which is what bounds the kernel.  Thread i < k has entry i.
 //
 // With a tail the mass of the unlisted tokens has to be a sum of its own: a difference of two sums would lose it where the
-// list has nearly all.  A bit for each group of 16 bytes tells the streaming sum to leave out groups with listed tokens, whose
+// list has nearly all.  And it has a maximum of its own: relative to the row's it underflows where the student is sure of listed
+// tokens (87 tau above the others), which is where the tail has most to say.  A bit for each group of 16 bytes tells the streaming sum to leave out groups with listed tokens, whose
 // unlisted ones are added by the group's first entry.  Listed tokens' gradients are written over those of the streaming pass.
 template <typename T, typename TO, bool TAIL>
 __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const DistillArgs &a, int cluster) {
@@ -80,7 +82,7 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
     __shared__ int s_hash[kHash], s_id[kMaxTop];
     __shared__ float s_q[kMaxTop], s_top[kTopWarps];
     __shared__ double s_red[kTopWarps][2], s_red2[kTopWarps][2];
-    __shared__ RowStats s_warp[kWarps];
+    __shared__ float4 s_warp[kWarps];
     __shared__ Segment s_seg[kMaxCluster];
     const int64_t r = blockIdx.x / cluster;
     const int rank = (int)(blockIdx.x % cluster), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -248,48 +250,54 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
     }
     const double mass = entry_sum(s_red2, 0), loss = entry_sum(s_red2, 1);
     const double rest_all = TAIL && entry_sum(s_red, 1) != 0.0 ? fmax(0.0, 1.0 - entry_sum(s_red, 0)) : 0.0;
-    float m = run.m, S, rest = 0.f;
+    float m = run.m, S, m_rest = -INFINITY, rest = 0.f;
     {
         float lo, hi;
         run.S.get(lo, hi);
         S = lo + hi;
     }
+    auto join = [&](float &m1, float &S1, float m2, float S2) {
+        const float both = fmaxf(m1, m2), at = finite_or_zero(both);
+        S1 = S1 * exp2_approx((m1 - at) * c) + S2 * exp2_approx((m2 - at) * c);
+        m1 = both;
+    };
     if (TAIL) {
-        // both sums relative to one maximum
-        const float m_run = m;
-        m = fmaxf(fmaxf(m_run, m_own), first ? zi : -INFINITY);
-        const float at = finite_or_zero(m);
-        rest = S * exp2_approx((m_run - at) * c) + rest_own * exp2_approx((m_own - at) * c);
-        S = rest + (first ? exp2_approx((zi - at) * c) : 0.f);
+        m_rest = m;
+        rest = S;
+        join(m_rest, rest, m_own, rest_own);
+        m = fmaxf(-INFINITY, first ? zi : -INFINITY);           // (-inf for NaN, which S tells)
+        S = first ? exp2_approx((zi - finite_or_zero(m)) * c) : 0.f;
     }
     auto joined = [&](int from) {          // over the lanes of a warp
 #pragma unroll
         for (int o = from; o > 0; o >>= 1) {
-            const float m2 = __shfl_xor_sync(0xffffffffu, m, o), S2 = __shfl_xor_sync(0xffffffffu, S, o);
-            const float both = fmaxf(m, m2), at = finite_or_zero(both), f = exp2_approx((m - at) * c), f2 = exp2_approx((m2 - at) * c);
-            S = S * f + S2 * f2;
-            if (TAIL) rest = rest * f + __shfl_xor_sync(0xffffffffu, rest, o) * f2;
-            m = both;
+            join(m, S, __shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, S, o));
+            if (TAIL) join(m_rest, rest, __shfl_xor_sync(0xffffffffu, m_rest, o), __shfl_xor_sync(0xffffffffu, rest, o));
         }
     };
     joined(16);
-    if (lane == 0) s_warp[warp] = RowStats{m, S, rest};
+    if (lane == 0) s_warp[warp] = make_float4(m, S, m_rest, rest);
     __syncthreads();
     if (warp == 0) {
-        const RowStats st = lane < kWarps ? s_warp[lane] : RowStats{-INFINITY, 0.f, 0.f};
-        m = st.m;
-        S = st.S;
-        rest = st.W;
+        const float4 st = lane < kWarps ? s_warp[lane] : make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+        m = st.x;
+        S = st.y;
+        m_rest = st.z;
+        rest = st.w;
         joined(kWarps / 2);
         m = __shfl_sync(0xffffffffu, m, 0);
         S = __shfl_sync(0xffffffffu, S, 0);
+        m_rest = __shfl_sync(0xffffffffu, m_rest, 0);
         rest = __shfl_sync(0xffffffffu, rest, 0);
         if (cluster > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         if (lane < cluster) {
             const uint32_t to = map_to_cta(smem_u32(&s_seg[rank]), lane);
             st_remote_u32(to, __float_as_uint(m));
             st_remote_u32(to + 4, __float_as_uint(S));
-            st_remote_u32(to + 8, __float_as_uint(rest));
+            if (TAIL) {
+                st_remote_u32(to + 8, __float_as_uint(m_rest));
+                st_remote_u32(to + 12, __float_as_uint(rest));
+            }
             st_remote_f64(to + 16, loss);
         }
         __syncwarp();
@@ -299,31 +307,39 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
     if (cluster > 1) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
     else __syncthreads();
     // the row: every eight lanes join the segments for themselves
-    Segment g{-INFINITY, 0.f, 0.f, 0.f, 0.0};
+    Segment g{-INFINITY, 0.f, -INFINITY, 0.f, 0.0};
     if ((lane & (kMaxCluster - 1)) < cluster) g = s_seg[lane & (kMaxCluster - 1)];
-    float at = g.m;
+    float at = g.m, at_rest = TAIL ? g.m_rest : -INFINITY;
 #pragma unroll
-    for (int o = kMaxCluster / 2; o > 0; o >>= 1) at = fmaxf(at, __shfl_xor_sync(0xffffffffu, at, o));
-    at = finite_or_zero(at);
-    const float f = exp2_approx((g.m - at) * c);
-    float total = g.S * f;
-    rest = g.rest * f;
+    for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
+        at = fmaxf(at, __shfl_xor_sync(0xffffffffu, at, o));
+        if (TAIL) at_rest = fmaxf(at_rest, __shfl_xor_sync(0xffffffffu, at_rest, o));
+    }
+    at = finite_or_zero(fmaxf(at, at_rest));
+    float total = g.S * exp2_approx((g.m - at) * c);
+    rest = TAIL ? g.rest * exp2_approx((g.m_rest - finite_or_zero(at_rest)) * c) : 0.f;
 #pragma unroll
     for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
         total += __shfl_xor_sync(0xffffffffu, total, o);
         if (TAIL) rest += __shfl_xor_sync(0xffffffffu, rest, o);
     }
-    const float rest_q = TAIL && rest != 0.f ? (float)rest_all : 0.f;      // (or there is no token for the tail)
+    const float lower = TAIL ? exp2_approx((at_rest - at) * c) : 0.f;      // of sums relative to at_rest, to have them relative to at
+    if (TAIL) total = fmaf(rest, lower, total);
+    // (rest is 0 where every unlisted logit is -inf, and at least 1 elsewhere: its largest term)
+    const float rest_q = TAIL && rest != 0.f ? (float)rest_all : 0.f;
     const bool none = mass == 0.0 && rest_all == 0.0;                       // no entries: the row takes no part
     const float of_p = total == 0.f ? 0.f : ((float)mass + rest_q) / total, scale = fmaf(w, a.heat.hi, w * a.heat.lo);
-    const float factor = scale * (of_p - (rest_q != 0.f ? rest_q / rest : 0.f));
+    // An unlisted token's gradient is (Q p_j - q_r p_j / p_r) w / tau.  Both terms are multiples of exp((z_j - at_rest) / tau), which
+    // does not underflow where p_j / p_r matters.  (A listed token's may overflow there: its gradient is written over it.)
+    const float from_at = rest_q != 0.f ? at_rest : at;
+    const float factor = scale * (rest_q != 0.f ? fmaf(of_p, lower, -rest_q / rest) : of_p);
     if (rank == 0 && warp == kWarps - 1 && a.row_loss) {
         double l = lane < kMaxCluster ? g.loss : 0.0;
 #pragma unroll
         for (int o = kMaxCluster / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
         const double logS = total == 0.f ? 0.0 : (double)logf(total);
         if (mass != 0.0) l += mass * ((double)at * inv + logS);
-        if (rest_q != 0.f) l += rest_all * (double)(logf(rest_q) - logf(rest / total));
+        if (rest_q != 0.f) l += rest_all * ((double)logf(rest_q) - log((double)rest / (double)total) - ((double)at_rest - (double)at) * inv);
         if (lane == 0) a.row_loss[r] = none ? 0.f : (float)l;
     }
     if (none) {
@@ -334,7 +350,7 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
     // the gradient; a segment's part of the row and of the gradient may start differently in their 16 bytes
     auto grad = [&](Pair x) {
         float y[2];
-        ((x + Pair(-at, -at)) * Pair(c, c)).get(y[0], y[1]);
+        ((x + Pair(-from_at, -from_at)) * Pair(c, c)).get(y[0], y[1]);
         return Pair(exp2_approx(y[0]), exp2_approx(y[1])) * Pair(factor, factor);
     };
     const RowGroups<TO> out(d, a.vocab);
