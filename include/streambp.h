@@ -683,10 +683,16 @@ int streambp_product_kernel(void);
  * aligned; guards are used here whether or not STREAMBP_WS_GUARD is set), fills the guards, has a kernel write
  * `overrun` floats past the end of the second sub-buffer (0: none), checks the guards and records the outcome in the
  * workspace header: afterwards streambp_last_device_status is STREAMBP_OK or STREAMBP_E_WORKSPACE_GUARD.
+ *
+ * streambp_test_sort_cluster: the largest cluster that streambp_embedding_backward's sort may take, 0 .. 16 blocks, in every
+ * call of the process from then on; returns what it was (16 at first).  8 is what a device without room for larger
+ * clusters has; with less than that calls of more than 128 and up to 65536 tokens are refused as STREAMBP_E_CUDA, as where
+ * such a device cannot be asked.  Host-only.
  */
 int streambp_test_expire_wait(uint64_t limit_ns, void *cuda_stream);
 int streambp_test_workspace_guard(void *workspace, size_t workspace_bytes, int32_t overrun, void *cuda_stream);
 int streambp_test_per_device_value(int ordinal, int value);
+int streambp_test_sort_cluster(int blocks);
 
 #ifdef __cplusplus
 }

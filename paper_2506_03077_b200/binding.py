@@ -36,7 +36,7 @@ EXPORTS = (
     "streambp_profile_enable", "streambp_profile_read", "streambp_product_kernel",
     "streambp_attention_forward", "streambp_attention_backward", "streambp_attention_backward_static",
     "streambp_lmhead_rl_backward", "streambp_layer_backward_packed",
-    "streambp_test_expire_wait", "streambp_test_per_device_value",
+    "streambp_test_expire_wait", "streambp_test_per_device_value", "streambp_test_sort_cluster",
     "streambp_layer_workspace_bytes_grouped", "streambp_layer_backward_grouped", "streambp_test_workspace_guard",
     "streambp_lmhead_workspace_bytes_grouped", "streambp_lmhead_ce_backward_grouped",
     "streambp_lmhead_rl_backward_grouped",
@@ -191,6 +191,8 @@ def lib() -> C.CDLL:
     L.streambp_test_workspace_guard.argtypes = [vp, sz, i32, vp]
     L.streambp_test_per_device_value.restype = C.c_int
     L.streambp_test_per_device_value.argtypes = [C.c_int, C.c_int]
+    L.streambp_test_sort_cluster.restype = C.c_int
+    L.streambp_test_sort_cluster.argtypes = [C.c_int]
     L.streambp_gemm_epilogue.restype = C.c_int
     L.streambp_gemm_epilogue.argtypes = [vp, i64, vp, i64, i64, i64, i64, vp, i32, vp, i64, vp, i64, vp, i64, i32, vp]
     L.streambp_gemm_epilogue_workspace_bytes.restype = sz

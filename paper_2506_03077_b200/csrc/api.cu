@@ -897,6 +897,11 @@ int streambp_test_per_device_value(int ordinal, int value) {
     return got;
 }
 
+int streambp_test_sort_cluster(int blocks) {
+    if (blocks < 0 || blocks > 16) return STREAMBP_E_SHAPE;
+    return embedding_cap_sort(blocks);
+}
+
 void streambp_profile_enable(int on) {
     g_prof_on = on != 0;
     g_prof_used = 0;

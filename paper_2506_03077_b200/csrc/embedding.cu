@@ -10,6 +10,7 @@
 // 3584 bf16 in 52 us (6.2 TB/s with rows that come again from L2); gradient of the same into 152064 rows 127 us: sort 15, sums 96
 // (6.1 TB/s), joins 12, launches.
 #include <algorithm>
+#include <atomic>
 
 #include "embedding.cuh"
 #include "vocab_rows.cuh"
@@ -689,8 +690,10 @@ EmbeddingPlan embedding_plan(int64_t n, int64_t vocab, int64_t d) {
 int embedding_counts(const EmbeddingPlan &p) { return p.one_launch ? 0 : (kBins + 1) * p.tiles; }
 
 namespace {
+std::atomic<int> g_sort_cap{kSortBlocks};
 template <int ITEMS> constexpr int kSortSmem = ITEMS * kSortThreads * 8 + kSortWarps * kBins * 2;
-// The largest cluster of the sort that the device can hold, 0 for an error.
+// The largest cluster of the sort that the device can hold, 0 for an error (of which a call with less than kSortPortable is refused:
+// the plan counts on that many).
 template <int ITEMS>
 int sort_cluster_limit() {
     static PerDevice cache;
@@ -719,12 +722,13 @@ int sort_cluster_limit() {
 }
 template <int ITEMS>
 int launch_sort(const SortArgs &a, int cluster, cudaStream_t st) {
-    if (sort_cluster_limit<ITEMS>() < cluster) return STREAMBP_E_CUDA;
     const int64_t zero_blocks = std::min<int64_t>(148, (a.zeros + 4 * kSortThreads - 1) / (4 * kSortThreads));
     const int64_t blocks = cluster + (zero_blocks + cluster - 1) / cluster * cluster;
     return launch_clusters(sort_cluster_kernel<ITEMS>, dim3((unsigned)blocks), kSortThreads, kSortSmem<ITEMS>, cluster, 1, st, a, cluster);
 }
 }  // namespace
+
+int embedding_cap_sort(int blocks) { return g_sort_cap.exchange(blocks); }
 
 template <typename T>
 int embedding_fwd(const T *table, int64_t ld, const int64_t *ids, int64_t n, int64_t vocab, int64_t d, float scale,
@@ -769,7 +773,9 @@ int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64
         const SortArgs s{ids, keys[0], tokens[0], owners, clear_first ? d_table : nullptr, clear_first ? vocab * d : 0, vocab, padding, (int)n,
                          p.passes, hdr};
         // (sixteen blocks: 65536 tokens 94 us against 104, 32768 127 against 132)
-        const int most = std::min({sort_cluster_limit<1>(), sort_cluster_limit<2>(), sort_cluster_limit<4>()});
+        const int most = std::min({sort_cluster_limit<1>(), sort_cluster_limit<2>(), sort_cluster_limit<4>(), sort_cluster_limit<8>(),
+                                   g_sort_cap.load()});
+        if (most < kSortPortable) return STREAMBP_E_CUDA;       // (fewer blocks would leave tokens out)
         int cluster = 1;
         while (cluster < most && n > (int64_t)cluster * kSortThreads) cluster *= 2;
         const int64_t each = (n + (int64_t)cluster * kSortThreads - 1) / ((int64_t)cluster * kSortThreads);

@@ -14,5 +14,6 @@ struct EmbeddingPlan {
 };
 EmbeddingPlan embedding_plan(int64_t n, int64_t vocab, int64_t d);
 int embedding_counts(const EmbeddingPlan &p);      // ints the sort's launches hand on
+int embedding_cap_sort(int blocks);                // of a cluster of the sort at most (a test's); returns what it was
 
 }  // namespace sbp
