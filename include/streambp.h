@@ -481,10 +481,10 @@ int streambp_token_logprobs_backward(const void *logits, int64_t ld, int64_t row
  *               (left out where no unlisted token has a finite logit)
  *     d_logits = weight[i] d row_loss / d logits, rounded once
  * A token listed more than once is the sum of its entries in the gradient.  weight (NULL: 1) carries what the objective
- * multiplies a row by (1 / N, a mixing factor, temperature^2); a row of weight 0, or without entries, takes no part: its logits
- * are not read, row_loss and d_logits are 0.  row_loss is not weighted.  row_loss and d_logits (type of the logits; may be
- * logits, same ld) are optional, one has to be there.  ids of rows that take part outside -1 .. vocab - 1 are treated as
- * absent and reported as STREAMBP_E_BAD_LABEL.  1 <= k <= STREAMBP_TOP_MAX, vocab <= STREAMBP_DISTILL_MAX_VOCAB, rows <= 2^27.
+ * multiplies a row by (1 / N, a mixing factor, temperature^2); a row of weight 0 takes no part: its logits are not read, row_loss
+ * and d_logits are 0.  Nor does a row without entries, whatever its logits hold.  row_loss is not weighted.  row_loss and
+ * d_logits (type of the logits; may be logits, same ld) are optional, one has to be there.  ids outside -1 .. vocab - 1 are
+ * treated as absent and, in rows of a weight other than 0, reported as STREAMBP_E_BAD_LABEL.  1 <= k <= STREAMBP_TOP_MAX, vocab <= STREAMBP_DISTILL_MAX_VOCAB, rows <= 2^27.
  * Logits of -inf have probability 0 (the loss is +inf where one is listed with q > 0); a NaN or +inf makes its row NaN.
  */
 #define STREAMBP_DISTILL_MAX_VOCAB (1 << 22)
@@ -503,9 +503,9 @@ int streambp_distill_topk(const streambp_distill_cfg *distill, const void *logit
  * streambp_lmhead_logprobs scores given tokens (what streambp_lmhead_rl_backward takes as logp_old and logp_ref) and lists
  * alternatives (what the distilling head takes as ids and values); arguments as in streambp_token_logprobs, ignore_index of
  * cfg; chunks whose tokens are all ignored are skipped on the device.
- * streambp_lmhead_distill_backward: *loss = sum over rows of weight row_loss (weight [T] is required; rows of weight 0 take no
- * part, chunks or groups of them are skipped); row_loss [T] is optional; dH, d_w_vocab, d_g_final, accumulate and wgrad_group
- * as in streambp_lmhead_ce_backward_grouped.  STREAMBP_E_NO_VALID_LABELS where every weight is 0 (loss and gradients are 0).
+ * streambp_lmhead_distill_backward: *loss = sum over rows of weight row_loss (weight [T] is required; rows that take no part,
+ * by their weight or for want of entries, add nothing, and chunks or groups of them are skipped); row_loss [T] is optional; dH,
+ * d_w_vocab, d_g_final, accumulate and wgrad_group as in streambp_lmhead_ce_backward_grouped.  STREAMBP_E_NO_VALID_LABELS where every weight is 0 (loss and gradients are 0).
  */
 size_t streambp_lmhead_logprobs_workspace_bytes(const streambp_head_cfg *cfg, int64_t T, int64_t chunk);
 int streambp_lmhead_logprobs(const streambp_head_cfg *cfg, const void *g_final, const void *w_vocab, const void *H,

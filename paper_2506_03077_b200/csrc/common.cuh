@@ -534,7 +534,8 @@ struct DistillRows {
 template <typename T, typename TO>
 int distill_topk(const T *logits, int64_t ld, int64_t rows, int64_t vocab, const DistillRows &ds, TO *d_logits, int64_t ldd,
                  WsHeader *hdr, cudaStream_t st);
-// For the LM head: marks[t] = 0 where row t takes part, else 1; ids outside the vocabulary go into the status.
+// For the LM head: marks[t] = 0 where row t takes part (it has a weight and an entry), else 1; rows with a weight are counted in
+// n_valid, ids of theirs outside the vocabulary go into the status.
 int distill_marks(const DistillRows &ds, int64_t T, int64_t vocab, int64_t *marks, WsHeader *hdr, cudaStream_t st);
 // loss sum of the header += sum of weight * row_loss
 int loss_accumulate_weighted(const float *row_loss, const float *weight, int64_t rows, WsHeader *hdr, cudaStream_t st);

@@ -74,7 +74,7 @@ int lmhead_backward(const streambp_head_cfg &c, const T *g_final, const T *w_voc
         if (distill->row_loss) SBP_TRY(fill_zero(distill->row_loss, sizeof(float) * T_, st));     // rows of skipped chunks keep this zero
     }
     // N is global: it is counted before the chunk loop so that every chunk scales by the same 1/N
-    SBP_TRY(count_valid_labels(labels, T_, V, ignore, s.hdr, st));
+    if (!distill) SBP_TRY(count_valid_labels(labels, T_, V, ignore, s.hdr, st));
     SBP_TRY(count_valid_per_chunk(labels, T_, cn, ignore, s.chunk_valid, st));
     const int64_t k = s.slots;
     if (k > 1) SBP_TRY(count_valid_per_chunk(labels, T_, k * cn, ignore, s.group_valid, st));

@@ -131,3 +131,49 @@ def test_the_streamed_head_with_a_remainder_far_below(chunk, group, dtype):
     assert abs(loss.item() - total.item()) <= (1e-4 if dtype == F32 else 2e-2) * abs(total.item())
     for got, ref in zip((dH, dg, dW), torch.autograd.grad(total, (H, g, W))):
         assert relative(got, ref) <= TOL[dtype]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("chunk,group", [(64, 1), (32, 2)])
+def test_chunks_without_entries_are_not_read(chunk, group, dtype):
+    """rows without entries take no part, whatever their hidden states are, as those of weight 0"""
+    h = Head(dtype)
+    h.H[64:128] = math.inf
+    ids = torch.randint(h.V, (h.T, 5), device="cuda")
+    values = torch.zeros(h.T, 5, device="cuda")
+    one, some = torch.full((h.T,), 1.0 / h.T, device="cuda"), torch.full((h.T,), 1.0 / h.T, device="cuda")
+    some[64:128] = 0
+    want = h.distill(ids, values, some, chunk, group)
+    ids[64:128] = -1
+    got = h.distill(ids, values, one, chunk, group)
+    for a, b in zip(got, want):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+    h.H.fill_(math.nan)
+    ids.fill_(-1)
+    for x in h.distill(ids, values, one, chunk, group):       # (weights are there: this is no call without any)
+        assert (x == 0).all()
+    h.distill(ids, values, 0 * one, chunk, group, status=B.E_NO_VALID_LABELS)
+    ids[70, 2] = h.V
+    h.distill(ids, values, one, chunk, group, status=B.E_BAD_LABEL)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("n,V", [(5, 4099), (3, 100001), (700, 3000)])
+def test_rows_without_entries(n, V, tail):
+    """in blocks alone and in clusters, all ids absent or outside, beside rows with a single one at any place of the list"""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    z = torch.randn(n, V, generator=g, device="cuda")
+    z[1::2] = math.nan
+    for k in (1, 33, 128):
+        ids = torch.full((n, k), -1, device="cuda")
+        ids[0::2, k - 1] = torch.randint(V, (len(ids[0::2]),), generator=g, device="cuda")
+        values = torch.full((n, k), -0.5, device="cuda")
+        w = torch.ones(n, device="cuda")
+        loss, d = distill(z, ids, values, w, 1.0, tail)
+        assert (loss[1::2] == 0).all() and (d[1::2] == 0).all()
+        want_l, want_g, size = definition(z[0:3:2], ids[0:3:2, k - 1:], values[0:3:2, k - 1:], 1.0, 1.0, tail)
+        assert ((loss[0:3:2].double() - want_l).abs() <= 4 * SUM + 2.0 ** -22 * 40 + 2.0 ** -23 * want_l.abs()).all()
+        assert ((d[0:3:2].double() - want_g).abs() <= (half_step(F32) + 2 * SUM) * size + 1e-30).all()
+        ids[1, 0] = V
+        again = distill(z, ids, values, w, 1.0, tail, status=B.E_BAD_LABEL)
+        assert torch.equal(again[0], loss) and torch.equal(again[1], d)
