@@ -458,7 +458,8 @@ int streambp_attention_window_backward(const void *q, const void *k, const void 
  * stays within the range of fp32.
  *
  * Backward: d_logits = (d_logp (onehot(token) - p) + d_lse p - d_entropy p (log p + entropy)) / temperature, rounded once, with
- * p from the given lse; each of the three row gradients may be NULL (d_entropy needs entropy).  d_logits may be logits
+ * p = exp(z / temperature - lse) of the given lse (whose rounding, 2^-24 |lse|, is a relative error of p: where |lse| is above
+ * some 1e5 it shows); each of the three row gradients may be NULL (d_entropy needs entropy).  d_logits may be logits
  * (same ld).  Rows that take no part are written as 0.  Lists of alternatives have no gradient.
  */
 #define STREAMBP_TOP_MAX 128

@@ -405,17 +405,21 @@ __global__ void __launch_bounds__(kGradThreads) token_logprobs_bwd_kernel(const 
     const float ent = a.d_entropy ? a.entropy[r] : 0.f, tau = a.heat.hi;
     const bool part = !a.tokens || (y != a.ignore && y >= 0 && y < a.vocab), same = in.off == out.off;
     const float c0 = (gl - gp - gh * ent) * tau, c1 = -gh * tau;
-    // logits below this (-inf among them) count as this: their p is 0, and so is its product with log p
-    const float least = (lse - 1e4f) / tau;
+    // log p below this (-inf among them) counts as this: p is 0, and so is its product with log p.  (log p and not the logit, whose
+    // bound lse - 1e4 would be lse itself where lse is large: p of a masked token 1.)
+    constexpr float kLeast = -1e4f, kLowest = -3.402823466e38f;
     const int per_block = kGradRounds * kGradGroups * kGradThreads;
     const int g0 = blockIdx.y * per_block, g1 = min(out.groups, g0 + per_block);
     const float inv_hi = a.heat.hi, inv_lo = a.heat.lo;
     auto grad = [&](Pair z) {
         float l[2], q[2];
-        z.get(l[0], l[1]);
-        z = Pair(max_nan(l[0], least), max_nan(l[1], least));
         Pair lp = fma2(z, Pair(inv_hi, inv_hi), Pair(-lse, -lse));
-        if (LO) lp = fma2(z, Pair(inv_lo, inv_lo), lp);
+        if (LO) {
+            z.get(l[0], l[1]);          // (-inf times the second part of 1 / tau may be +inf)
+            lp = fma2(Pair(max_nan(l[0], kLowest), max_nan(l[1], kLowest)), Pair(inv_lo, inv_lo), lp);
+        }
+        lp.get(l[0], l[1]);
+        lp = Pair(max_nan(l[0], kLeast), max_nan(l[1], kLeast));
         (lp * Pair(kLog2e, kLog2e)).get(q[0], q[1]);
         return Pair(exp2_approx(q[0]), exp2_approx(q[1])) * fma2(lp, Pair(c1, c1), Pair(c0, c0));
     };
@@ -459,8 +463,8 @@ __global__ void __launch_bounds__(kGradThreads) token_logprobs_bwd_kernel(const 
             const int e = e0 + 2 * i;
             Pair g(0.f, 0.f);
             if (part)
-                g = grad(Pair(e >= 0 && e < a.vocab ? to_f32(logits[r * a.ld + e]) : least,
-                              e + 1 >= 0 && e + 1 < a.vocab ? to_f32(logits[r * a.ld + e + 1]) : least));
+                g = grad(Pair(e >= 0 && e < a.vocab ? to_f32(logits[r * a.ld + e]) : 0.f,
+                              e + 1 >= 0 && e + 1 < a.vocab ? to_f32(logits[r * a.ld + e + 1]) : 0.f));
             g.get(o.v[2 * i], o.v[2 * i + 1]);
 #pragma unroll
             for (int j = 0; j < 2; j++)
