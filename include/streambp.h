@@ -442,10 +442,11 @@ int streambp_attention_window_backward(const void *q, const void *k, const void 
 
 /*
  * (No counterpart in the paper.)  What a model's two ends need beside the products: log-probabilities of given tokens,
- * distillation from a teacher's top logits, layer norm, the embedding lookup and its gradient.  Matrices here have rows that
- * may start anywhere (ld in elements, aligned to their elements); rows that start on 16 bytes are faster.  Inputs and outputs
- * do not overlap but where an output may be an input, in its place; calls that may run at the same time have workspaces of
- * their own.
+ * distillation from a teacher's top logits, layer norm, the embedding lookup and its gradient.  Matrices with a leading
+ * dimension (ld, in elements) have rows that may start anywhere, aligned to their elements; rows that start on 16 bytes are
+ * faster.  Those without one start on 16 bytes: the table's gradient, and what the streamed heads read and write beside their
+ * vectors over tokens and their lists.  A workspace starts on 256 bytes.  Inputs and outputs do not overlap but where an output
+ * may be an input, in its place; calls that may run at the same time have workspaces of their own.
  *
  * Log-probabilities.  Row i of logits ([rows, vocab], float or bf16) has p = softmax(z / temperature).
  *     lse = log sum exp(z / temperature),  logp = z[token] / temperature - lse,  entropy = - sum p log p,
@@ -485,7 +486,8 @@ int streambp_token_logprobs_backward(const void *logits, int64_t ld, int64_t row
  * multiplies a row by (1 / N, a mixing factor, temperature^2); a row of weight 0 takes no part: its logits are not read, row_loss
  * and d_logits are 0.  Nor does a row without entries, whatever its logits hold.  row_loss is not weighted.  row_loss and
  * d_logits (type of the logits; may be logits, same ld) are optional, one has to be there.  ids outside -1 .. vocab - 1 are
- * treated as absent and, in rows of a weight other than 0, reported as STREAMBP_E_BAD_LABEL.  1 <= k <= STREAMBP_TOP_MAX, vocab <= STREAMBP_DISTILL_MAX_VOCAB, rows <= 2^27.
+ * treated as absent and, in rows of a weight other than 0, reported as STREAMBP_E_BAD_LABEL.  1 <= k <= STREAMBP_TOP_MAX,
+ * vocab <= STREAMBP_DISTILL_MAX_VOCAB, rows <= 2^27.
  * Logits of -inf have probability 0 (the loss is +inf where one is listed with q > 0); a NaN or +inf makes its row NaN.
  */
 #define STREAMBP_DISTILL_MAX_VOCAB (1 << 22)
@@ -543,7 +545,8 @@ int streambp_layernorm_backward(const void *dy, int64_t lddy, const void *x, int
  * Embedding: out[t] = scale table[ids[t]] (table [vocab, d], out [n, d] of `dtype`, rounded once).  A token equal to padding_id
  * has a row of zeros and no gradient (a value outside the vocabulary, such as -1: no token is padding).  Ids outside the
  * vocabulary are treated like padding and reported as STREAMBP_E_BAD_LABEL.
- * Backward: d_table (fp32 [vocab, d], dense) = or, with accumulate = 1, += scale times the sums of d_out's rows by id, formed
+ * Backward: d_table (fp32 [vocab, d], dense, on 16 bytes; a view into a flat bucket of gradients begins at a multiple of four
+ * elements) = or, with accumulate = 1, += scale times the sums of d_out's rows by id, formed
  * over the tokens sorted by id and joined in a fixed order (reproducible bit by bit); rows of no token are 0 or stay as they
  * are (they are not read).  1 <= n < 2^30, vocab < 2^31 - 1, d <= 2^20.
  */

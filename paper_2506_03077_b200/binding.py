@@ -1144,7 +1144,8 @@ def embedding_backward_workspace_bytes(n: int, vocab: int, d: int) -> int:
 
 def embedding_backward(d_out, ids, d_table, workspace, scale: float = 1.0, padding_id: int = -1, accumulate: bool = False,
                        stream=None, check: bool = True) -> int:
-    """streambp_embedding_backward; d_out [n, d] with contiguous rows, d_table fp32 [vocab, d] (overwritten, or added to)."""
+    """streambp_embedding_backward; d_out [n, d] with contiguous rows, d_table contiguous fp32 [vocab, d] on 16 bytes
+    (overwritten, or added to)."""
     what, dev, dt = "embedding_backward", _matrix("embedding_backward", "d_out", d_out), d_out.dtype
     n, d = d_out.shape
     _want(d_table.dim() == 2 and d_table.shape[1] == d, what, "d_table is [vocab, d]")
