@@ -508,7 +508,8 @@ int streambp_distill_topk(const streambp_distill_cfg *distill, const void *logit
  * cfg; chunks whose tokens are all ignored are skipped on the device.
  * streambp_lmhead_distill_backward: *loss = sum over rows of weight row_loss (weight [T] is required; rows that take no part,
  * by their weight or for want of entries, add nothing, and chunks or groups of them are skipped); row_loss [T] is optional; dH,
- * d_w_vocab, d_g_final, accumulate and wgrad_group as in streambp_lmhead_ce_backward_grouped.  STREAMBP_E_NO_VALID_LABELS where every weight is 0 (loss and gradients are 0).
+ * d_w_vocab, d_g_final, accumulate and wgrad_group as in streambp_lmhead_ce_backward_grouped.  STREAMBP_E_NO_VALID_LABELS where
+ * every weight is 0 (loss and gradients are 0).
  */
 size_t streambp_lmhead_logprobs_workspace_bytes(const streambp_head_cfg *cfg, int64_t T, int64_t chunk);
 int streambp_lmhead_logprobs(const streambp_head_cfg *cfg, const void *g_final, const void *w_vocab, const void *H,
