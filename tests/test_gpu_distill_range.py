@@ -177,3 +177,20 @@ def test_rows_without_entries(n, V, tail):
         ids[1, 0] = V
         again = distill(z, ids, values, w, 1.0, tail, status=B.E_BAD_LABEL)
         assert torch.equal(again[0], loss) and torch.equal(again[1], d)
+
+
+@pytest.mark.parametrize("gap", [0.0, 88.0, 300.0])
+def test_gradients_far_below_by_differences(gap):
+    z = torch.randn(2, 40, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    ids = torch.tensor([[3, 17, 4], [39, 0, 20]], device="cuda")
+    z.scatter_add_(1, ids, torch.full((2, 3), gap, device="cuda"))
+    values = torch.tensor([0.5, 0.2, 0.1], dtype=torch.float64).log().float().cuda().repeat(2, 1)
+    _, d = distill(z, ids, values, None, 1.0, True)
+    h = 2.0 ** -8
+    for j in (0, 3, 20, 25):
+        up, down = z.double(), z.double()
+        up[:, j] += h
+        down[:, j] -= h
+        slope = (definition(up, ids, values, 1.0, 1.0, True)[0] - definition(down, ids, values, 1.0, 1.0, True)[0]) / (2 * h)
+        # h^2 / 6 of third derivatives of log-sums (below 1 / 2 each, times Q + q_r), the terms' 3e-5, losses of up to 100 in 64 bits
+        assert ((d[:, j].double() - slope).abs() <= 2e-6 * 1.2 + 3e-5 * 2 + 1e-10).all()
