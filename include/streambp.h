@@ -454,7 +454,7 @@ int streambp_attention_window_backward(const void *q, const void *k, const void 
  * tokens [rows] may be NULL (then logp must be); a row whose token is ignore_index takes no part: its logits are not read,
  * logp, lse and entropy are 0, top_ids -1 and top_logp -inf.  A token outside the vocabulary is treated like that and reported
  * as STREAMBP_E_BAD_LABEL.  Every output is optional, one has to be there; 0 <= k <= STREAMBP_TOP_MAX, k <= vocab <= 2^27,
- * rows <= 2^27.  Logits of -inf have probability 0; a row of nothing else has lse, logp and top_logp -inf and entropy 0.  A
+ * 1 <= rows <= 2^27, here and below.  Logits of -inf have probability 0; a row of nothing else has lse, logp and top_logp -inf and entropy 0.  A
  * row with a NaN or +inf has NaN for all of them and top_ids -1.  2^-20 <= temperature <= 2^20, here and below; z / temperature
  * stays within the range of fp32.
  *
@@ -487,7 +487,7 @@ int streambp_token_logprobs_backward(const void *logits, int64_t ld, int64_t row
  * and d_logits are 0.  Nor does a row without entries, whatever its logits hold.  row_loss is not weighted.  row_loss and
  * d_logits (type of the logits; may be logits, same ld) are optional, one has to be there.  ids outside -1 .. vocab - 1 are
  * treated as absent and, in rows of a weight other than 0, reported as STREAMBP_E_BAD_LABEL.  1 <= k <= STREAMBP_TOP_MAX,
- * vocab <= STREAMBP_DISTILL_MAX_VOCAB, rows <= 2^27.
+ * vocab <= STREAMBP_DISTILL_MAX_VOCAB.
  * Logits of -inf have probability 0 (the loss is +inf where one is listed with q > 0); a NaN or +inf makes its row NaN.
  */
 #define STREAMBP_DISTILL_MAX_VOCAB (1 << 22)
@@ -527,7 +527,7 @@ int streambp_lmhead_distill_backward(const streambp_head_cfg *cfg, const streamb
  * Layer norm over the d columns of each row, in fp32 with one rounding:
  *     y = (x - mean) rstd gain + bias,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
  * x, y [rows, d] and gain, bias [d] are of `dtype`; gain and bias are optional (1 and 0), mean and rstd (fp32 [rows], what the
- * backward reads) too.  y may be x (same ld).  rows <= 2^31 - 1, d <= 2^20.
+ * backward reads) too.  y may be x (same ld).  1 <= rows <= 2^31 - 1, 1 <= d <= 2^20.
  * Backward, with xhat = (x - mean) rstd and g = dy gain:
  *     dx = (g - mean(g) - xhat mean(g xhat)) rstd + add,   d_gain (+)= sum over rows of dy xhat,  d_bias (+)= sum of dy
  * add (the gradient that goes around the norm) is optional; dx, d_gain and d_bias (fp32 [d], overwritten or with accumulate
