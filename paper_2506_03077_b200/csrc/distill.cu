@@ -73,8 +73,9 @@ __device__ __forceinline__ void entry_sums(double &a, double &b, double (*red)[2
 //
 // With a tail the mass of the unlisted tokens has to be a sum of its own: a difference of two sums would lose it where the
 // list has nearly all.  And it has a maximum of its own: relative to the row's it underflows where the student is sure of listed
-// tokens (87 tau above the others), which is where the tail has most to say.  A bit for each group of 16 bytes tells the streaming sum to leave out groups with listed tokens, whose
-// unlisted ones are added by the group's first entry.  Listed tokens' gradients are written over those of the streaming pass.
+// tokens (87 tau above the others), which is where the tail has most to say.  A bit for each group of 16 bytes tells the streaming
+// sum to leave out groups with listed tokens, whose unlisted ones are added by the group's first entry.  Listed tokens' gradients
+// are written over those of the streaming pass.
 template <typename T, typename TO, bool TAIL>
 __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const DistillArgs &a, int cluster) {
     constexpr int N = RowGroups<T>::N, NO = Vec<TO>::N, U = 4;
@@ -242,7 +243,7 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
                 if (v + u * kThreads < w1) skip(v + u * kThreads, x[u]);
             run.add(x, c);
         }
-        if (tid >= kThreads - 2 && g0 < g1 && listed != 0.0) {           // the ragged ends (one group at each, which may be the same one)
+        if (tid >= kThreads - 2 && g0 < g1 && listed != 0.0) {      // the ragged ends (one group at each, which may be the same one)
             const int v = tid == kThreads - 2 ? g0 : g1 - 1;
             if ((v < w0 || v >= w1) && !(tid == kThreads - 1 && v == g0)) {
                 Raw<T> y[1];
@@ -327,7 +328,7 @@ __device__ __forceinline__ void distill_row(const T *logits, TO *d_logits, const
         total += __shfl_xor_sync(0xffffffffu, total, o);
         if (TAIL) rest += __shfl_xor_sync(0xffffffffu, rest, o);
     }
-    const float lower = TAIL ? exp2_approx((at_rest - at) * c) : 0.f;      // of sums relative to at_rest, to have them relative to at
+    const float lower = TAIL ? exp2_approx((at_rest - at) * c) : 0.f;      // turns sums relative to at_rest into sums relative to at
     if (TAIL) total = fmaf(rest, lower, total);
     // (rest is 0 where every unlisted logit is -inf, and at least 1 elsewhere: its largest term)
     const float rest_q = TAIL && rest != 0.f ? (float)rest_all : 0.f;

@@ -777,7 +777,7 @@ int embedding_bwd(const T *dy, int64_t ldy, const int64_t *ids, int64_t n, int64
                                    g_sort_cap.load()});
         if (most < kSortPortable) return STREAMBP_E_CUDA;       // (fewer blocks would leave tokens out)
         int cluster = 1;
-        while (cluster < most && n > (int64_t)cluster * kSortThreads) cluster *= 2;
+        while (2 * cluster <= most && n > (int64_t)cluster * kSortThreads) cluster *= 2;
         const int64_t each = (n + (int64_t)cluster * kSortThreads - 1) / ((int64_t)cluster * kSortThreads);
         if (each <= 1) SBP_TRY(launch_sort<1>(s, cluster, st));
         else if (each <= 2) SBP_TRY(launch_sort<2>(s, cluster, st));

@@ -28,6 +28,8 @@ def test_clusters_of_eight(n, V, d, cap):
     assert cap(8) == 16
     check(dy, ids, V)
     assert torch.equal(gradient(dy, ids, V), want)
+    cap(15)                                         # (no cluster of fifteen: eight)
+    assert torch.equal(gradient(dy, ids, V), want)
 
 
 def test_smaller_clusters_are_refused(cap):
